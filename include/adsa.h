@@ -283,6 +283,124 @@ int adsa_step_static(const adsa_params* p, adsa_seq* seqs, const void* q, const 
                      const void* v_new, void* out, float* lse, int32_t* sel_idx, int32_t* sel_cnt,
                      int32_t* keep_map, uint32_t flags, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------------------------------
+ * Prompts: rotary positions, tokens that enter the caches many at a time, their attention, and decode attention for sequences that
+ * share a prompt.  The entry points below take the same parameters and records as those above, one layer per call; sel_groups != 1
+ * is ADSA_ERR_UNSUPPORTED in all of them.
+ */
+#define ADSA_MAX_AXES 3
+
+typedef enum { ADSA_PAIR_HALVES = 0,       /* pair i of a row: elements i and i + head_dim/2 */
+               ADSA_PAIR_NEIGHBOURS = 1    /* elements 2i and 2i + 1 */
+} adsa_pairing;
+
+/* [host] Rotary positions with up to three axes (row and column; time, height and width; a plain line).  A token with the
+   coordinates c has pair i of its q and k rows turned by the angle  sum over a of c[a] * freq[a][i]  radians:
+   (x, y) -> (x cos - y sin, y cos + x sin).  A pair that an axis does not turn has frequency 0 there.  Angles are formed and reduced
+   in 64 bits, so far positions lose nothing.  A token at absolute position t has, where none are given, the coordinates
+     t < grid_origin (P):                      c[a] = text[a] * t
+     image token at (row r, column c) else:    c[a] = origin[a] * P + row[a] * r + col[a] * c */
+typedef struct adsa_rope {
+  const double* freq;          /* device [n_axes][head_dim/2]; 16-byte aligned */
+  int32_t n_axes;              /* 1..ADSA_MAX_AXES */
+  int32_t pairing;             /* adsa_pairing */
+  int32_t text[ADSA_MAX_AXES], origin[ADSA_MAX_AXES], row[ADSA_MAX_AXES], col[ADSA_MAX_AXES];
+} adsa_rope;
+
+/* [host] New tokens of a batch, packed one sequence behind the other.  Token begin[b] + j of sequence b belongs in slot slot0[b] + j.
+   The slots of a sequence have to be in position order (under ADSA_EVICT_REUSE_SLOT: before its first eviction). */
+typedef struct adsa_tokens {
+  int32_t n_tokens;            /* T >= 1: tokens of all sequences */
+  int32_t max_len;             /* no sequence has more new tokens than this; 1..cap */
+  const int32_t* begin;        /* device [n_seq + 1], ascending from 0 to n_tokens */
+  const int32_t* slot0;        /* device [n_seq] */
+  const int32_t* pos0;         /* device [n_seq] absolute position of each sequence's first new token, or NULL: one behind that of slot
+                                  slot0 - 1, 0 in an empty cache.  (Members of a shared prompt have caches that begin behind it) */
+  const int32_t* coords;       /* device [T][n_axes] coordinates instead of those that follow from positions, or NULL */
+  int64_t q_stride, k_stride, v_stride;   /* elements from one token's row to the next in q, k, v of adsa_append (rows of a packed
+                                             projection); 0: no gap.  Multiples of 16 bytes */
+} adsa_tokens;
+
+typedef enum { ADSA_MASK_CAUSAL = 0,       /* a token sees itself and the slots before its own */
+               ADSA_MASK_PREFIX = 1        /* besides, tokens among the first n_keep_prefix slots see each other both ways */
+} adsa_mask;
+
+/* [host] What is done to scaled scores z = q.k * softmax_scale before the softmax; NULL: nothing, causal. */
+typedef struct adsa_mods {
+  float softcap;               /* > 0: z <- softcap * tanh(z / softcap); 0: not */
+  int32_t mask;                /* adsa_mask (adsa_prefill) */
+  const float* slopes;         /* device, one per query head: z <- z - slopes[head] * |difference of absolute positions|, after the cap; or NULL */
+  const int32_t* doc;          /* device [n_seq][doc_stride]: document of every slot; a token sees only its own document's slots, and a
+                                  negative number marks a slot that neither sees nor is seen; or NULL (adsa_prefill only) */
+  int64_t doc_stride;          /* >= cap */
+} adsa_mods;
+
+/* [host] Prompts that sequences of a launch share: group g's prompt is the resident slots of a record of its own (filled by adsa_append
+   like any other, with strides and a capacity of its own, same head count, head_dim and dtype), and its members are the sequences
+   members[g] .. members[g+1] - 1.  Members' own caches hold only what comes behind the prompt. */
+typedef struct adsa_shared {
+  int32_t n_groups;            /* 1..n_seq */
+  int32_t max_prompt;          /* capacity of the prompts' records: none has more slots (<= ADSA_MAX_CAP) */
+  int32_t max_members;         /* no group has more members; 1..n_seq */
+  int32_t reserved;
+  const adsa_seq* prompts;     /* device [n_groups]; k, v, pos, n_res and status are read */
+  const int32_t* members;      /* device [n_groups + 1], ascending from 0 to n_seq */
+  int64_t kv_slot_stride, kv_head_stride;    /* of the prompts' caches, elements */
+} adsa_shared;
+
+/*
+ * Rotate the query token's q and k of every sequence, at the position its record's step says (grid_origin + step - 1), or at
+ * coords [n_seq][n_axes]:
+ *   q, k      [n_seq] rows of n_heads * max(q_per_kv, 1) and of n_heads heads, q_stride and k_stride elements apart (0: no gap);
+ *             dtype, or fp32 with ADSA_FLAG_NEW_F32 and a bf16 cache
+ *   q_out, k_out  dtype [n_seq][heads][head_dim]; may be q and k themselves where those are dtype without gaps
+ * Rotated in fp32, rounded once.  Inactive sequences (step < 0 or a status) get zeros.  flags: ADSA_FLAG_NEW_F32.
+ */
+int adsa_rotate(const adsa_params* p, const adsa_rope* rope, const adsa_seq* seqs, const int32_t* coords, const void* q,
+                const void* k, int64_t q_stride, int64_t k_stride, void* q_out, void* k_out, uint32_t flags, void* stream);
+
+/*
+ * New tokens enter the caches: k rows rotated, v rows as they are, q rows rotated to q_out (dtype [T][heads][head_dim]; q and q_out may
+ * both be NULL).  rope NULL: nothing is turned.  q, k, v are dtype, or fp32 with ADSA_FLAG_NEW_F32 and a bf16 cache (rounded once).
+ * Per sequence with new tokens (whatever its step): slot0 <= n_res is required, slots from slot0 on are overwritten, and n_res becomes
+ * slot0 + its number of tokens; the same call may be made again, and a smaller slot0 takes tokens back.  pos and zero scores
+ * are written, pending_slot,
+ * compacted and the running V-cosine state are reset, and step becomes the number of image tokens resident, as if the last
+ * token were the query token; ADSA_FLAG_ADVANCE adds 1 to it.  Sequences without new tokens are left alone.
+ * A record that does not fit (n_res, slot0 or a count out of range, a hole, positions beyond the grid: ADSA_SEQ_BAD_STATE;
+ * more tokens than slots: ADSA_SEQ_CACHE_FULL) gets its status set, nothing else, and zeros in q_out.
+ * flags: ADSA_FLAG_NEW_F32, ADSA_FLAG_ADVANCE.
+ */
+int adsa_append(const adsa_params* p, const adsa_tokens* tokens, const adsa_rope* rope, adsa_seq* seqs, const void* q,
+                const void* k, const void* v, void* q_out, uint32_t flags, void* stream);
+
+/*
+ * Attention of those tokens over slots 0 .. slot0 + tokens - 1 of their sequences (already resident), masked and with scores changed
+ * as mods say, any number of tokens from one on:
+ *   q    dtype [T][heads][head_dim] (rotated)        out  dtype [T][heads][head_dim]        lse  float [T][heads]
+ * A row that sees nothing gives zeros and lse = -INFINITY; what masked slots hold, infinities and NaN included, changes nothing.
+ * For ADSA_SCORE_ATTN_MASS and unless ADSA_FLAG_NO_ACCUMULATE is set, score[h][slot] gains the probability that the tokens' query
+ * heads of cache head h gave the slot.  Sums are taken in the same order whatever the launch does: results repeat bit by bit.
+ * A sequence with a status or without those slots (ADSA_SEQ_BAD_STATE) gets zeros.
+ * flags: ADSA_FLAG_NO_ACCUMULATE, ADSA_FLAG_ADVANCE (step += 1 for every sequence with new tokens, where adsa_append did not).
+ */
+int adsa_prefill(const adsa_params* p, const adsa_tokens* tokens, const adsa_mods* mods, adsa_seq* seqs, const void* q,
+                 void* out, float* lse, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
+size_t adsa_prefill_workspace_bytes(const adsa_params* p, const adsa_tokens* tokens);   /* 0 if the parameters are invalid */
+
+/*
+ * adsa_attend for sequences that share prompts, with scores changed as mods say (mask and doc: NULL or not read): softmax over the group's prompt and
+ * the sequence's own list (sel_idx, sel_cnt, as adsa_select leaves them), one pass over a prompt for all its members.  Arguments as in
+ * adsa_attend, whose scores, append and advance happen alike; own lists may be empty (only the prompt is attended), a sequence with
+ * nothing at all gives zeros and lse = -INFINITY; one that is inactive, has a status, or whose prompt's record has one or more slots
+ * than max_prompt, zeros.  ADSA_SCORE_VCOS_FUSED: ADSA_ERR_UNSUPPORTED.
+ * flags: ADSA_FLAG_NO_ACCUMULATE, ADSA_FLAG_APPEND, ADSA_FLAG_NEW_F32, ADSA_FLAG_ADVANCE.
+ */
+int adsa_attend_shared(const adsa_params* p, const adsa_shared* shared, const adsa_mods* mods, adsa_seq* seqs, const void* q,
+                       const void* k_new, const void* v_new, const int32_t* sel_idx, const int32_t* sel_cnt, void* out,
+                       float* lse, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
+size_t adsa_shared_workspace_bytes(const adsa_params* p, const adsa_shared* shared);    /* 0 if the parameters are invalid */
+
 /* Timing hook for benchmarks: when enabled, adsa_attend/adsa_step attach a start and a stop HIP
    event to every attention-kernel dispatch on the caller's stream (in adsa_step, where that kernel ranks for itself or plans
    evictions, those are part of it; kernels that merge split lists are not).  adsa_profile_read

@@ -80,6 +80,7 @@ class LayerBatch:
             raise B.AdsaError(-2, "adsa_workspace_bytes (invalid parameters)")
         self.workspace = torch.empty(ws, dtype=torch.uint8, device=dev)
         B.adsa_workspace_init(p, self.workspace)
+        self.prompt_workspace = None
 
     # ---- host -> device
     def set_sequence(self, b: int, *, k: np.ndarray, v: np.ndarray, pos: np.ndarray,
@@ -151,10 +152,33 @@ class LayerBatch:
         B.adsa_step(self.params, self.seqs, q, k_new, v_new, self.out, self.lse, self.sel_idx, self.sel_cnt,
                     self.keep_map, self.workspace, flags, stream)
 
-
     def step_static(self, q, k_new, v_new, flags: int = 0, stream=None):
         B.adsa_step_static(self.params, self.seqs, q, k_new, v_new, self.out, self.lse, self.sel_idx, self.sel_cnt,
                            self.keep_map, flags, stream)
+
+    # ---- prompts
+    def _space(self, need: int, where: str) -> torch.Tensor:
+        """Workspace of at least `need` bytes, kept for the calls to come (the first call of a size allocates: make it before a
+        graph is captured)."""
+        if need == 0:
+            raise B.AdsaError(-2, where + " (invalid parameters)")
+        if self.prompt_workspace is None or self.prompt_workspace.numel() < need:
+            self.prompt_workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return self.prompt_workspace
+
+    def rotate(self, rope, q, k, q_out, k_out, coords=None, flags: int = 0, stream=None, q_stride: int = 0, k_stride: int = 0):
+        B.adsa_rotate(self.params, rope, self.seqs, q, k, q_out, k_out, coords, flags, stream, q_stride, k_stride)
+
+    def append(self, tokens, rope, q, k, v, q_out, flags: int = 0, stream=None):
+        B.adsa_append(self.params, tokens, rope, self.seqs, q, k, v, q_out, flags, stream)
+
+    def prefill(self, tokens, q, out, lse, mods=None, flags: int = 0, stream=None):
+        ws = self._space(B.adsa_prefill_workspace_bytes(self.params, tokens), "adsa_prefill")
+        B.adsa_prefill(self.params, tokens, mods, self.seqs, q, out, lse, ws, flags, stream)
+
+    def attend_shared(self, shared, q, k_new=None, v_new=None, flags: int = 0, mods=None, stream=None):
+        ws = self._space(B.adsa_shared_workspace_bytes(self.params, shared), "adsa_attend_shared")
+        B.adsa_attend_shared(self.params, shared, mods, self.seqs, q, k_new, v_new, self.sel_idx, self.sel_cnt, self.out, self.lse, ws, flags, stream)
 
 
 class ModelBatch(LayerBatch):

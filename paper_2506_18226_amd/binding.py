@@ -23,6 +23,9 @@ FLAG_NO_COMPACT, FLAG_NO_ACCUMULATE, FLAG_PLAN_APPEND, FLAG_APPEND, FLAG_ADVANCE
 SEQ_CACHE_FULL, SEQ_BAD_STATE, SEQ_SEL_OVERFLOW = 1, 2, 4
 MAX_CAP = 8192
 EVICT_ROW_END, EVICT_WHEN_FULL, EVICT_REUSE_SLOT = 0, 1, 2
+MAX_AXES = 3
+PAIRINGS = {"halves": 0, "neighbours": 1}
+MASK_CAUSAL, MASK_PREFIX = 0, 1
 
 ERRORS = {0: "ADSA_OK", -1: "ADSA_ERR_NULL", -2: "ADSA_ERR_SHAPE", -3: "ADSA_ERR_DTYPE", -4: "ADSA_ERR_ALIGN",
           -5: "ADSA_ERR_CAPACITY", -6: "ADSA_ERR_WORKSPACE", -7: "ADSA_ERR_LAUNCH", -8: "ADSA_ERR_UNSUPPORTED",
@@ -30,7 +33,8 @@ ERRORS = {0: "ADSA_OK", -1: "ADSA_ERR_NULL", -2: "ADSA_ERR_SHAPE", -3: "ADSA_ERR
 STATIC_SCRATCH_BYTES = 4 << 20
 
 EXPORTS = ["adsa_workspace_bytes", "adsa_workspace_init", "adsa_select", "adsa_attend", "adsa_compact", "adsa_step",
-           "adsa_step_static",
+           "adsa_step_static", "adsa_rotate", "adsa_append", "adsa_prefill", "adsa_prefill_workspace_bytes", "adsa_attend_shared",
+           "adsa_shared_workspace_bytes",
            "adsa_profile_enable", "adsa_profile_read", "adsa_strerror", "adsa_version"]
 
 
@@ -46,6 +50,37 @@ class AdsaParams(C.Structure):
         ("softmax_scale", C.c_float), ("win_recent_m", C.c_int32), ("evict_policy", C.c_int32),
         ("q_per_kv", C.c_int32),
     ]
+
+
+class _HostStruct(C.Structure):
+    """A host struct of device pointers: it keeps the tensors they belong to alive."""
+
+    def _hold(self, *tensors):
+        self.held = tensors
+        return self
+
+
+class AdsaRope(_HostStruct):
+    """Mirror of `adsa_rope` (host struct)."""
+    _fields_ = [("freq", C.c_void_p), ("n_axes", C.c_int32), ("pairing", C.c_int32), ("text", C.c_int32 * MAX_AXES),
+                ("origin", C.c_int32 * MAX_AXES), ("row", C.c_int32 * MAX_AXES), ("col", C.c_int32 * MAX_AXES)]
+
+
+class AdsaTokens(_HostStruct):
+    """Mirror of `adsa_tokens` (host struct)."""
+    _fields_ = [("n_tokens", C.c_int32), ("max_len", C.c_int32), ("begin", C.c_void_p), ("slot0", C.c_void_p), ("pos0", C.c_void_p),
+                ("coords", C.c_void_p), ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64)]
+
+
+class AdsaMods(_HostStruct):
+    """Mirror of `adsa_mods` (host struct)."""
+    _fields_ = [("softcap", C.c_float), ("mask", C.c_int32), ("slopes", C.c_void_p), ("doc", C.c_void_p), ("doc_stride", C.c_int64)]
+
+
+class AdsaShared(_HostStruct):
+    """Mirror of `adsa_shared` (host struct)."""
+    _fields_ = [("n_groups", C.c_int32), ("max_prompt", C.c_int32), ("max_members", C.c_int32), ("reserved", C.c_int32),
+                ("prompts", C.c_void_p), ("members", C.c_void_p), ("kv_slot_stride", C.c_int64), ("kv_head_stride", C.c_int64)]
 
 
 # Mirror of `adsa_seq` (device struct array), 96 bytes per entry.
@@ -101,6 +136,19 @@ def load_library() -> C.CDLL:
         lib.adsa_step.argtypes = [pp, vp, vp, vp, vp, vp, f32p, i32p, i32p, i32p, C.c_uint32, vp, C.c_size_t, vp]
         lib.adsa_step_static.restype = C.c_int
         lib.adsa_step_static.argtypes = [pp, vp, vp, vp, vp, vp, f32p, i32p, i32p, i32p, C.c_uint32, vp]
+        rp, tp, mp, sp = C.POINTER(AdsaRope), C.POINTER(AdsaTokens), C.POINTER(AdsaMods), C.POINTER(AdsaShared)
+        lib.adsa_rotate.restype = C.c_int
+        lib.adsa_rotate.argtypes = [pp, rp, vp, i32p, vp, vp, C.c_int64, C.c_int64, vp, vp, C.c_uint32, vp]
+        lib.adsa_append.restype = C.c_int
+        lib.adsa_append.argtypes = [pp, tp, rp, vp, vp, vp, vp, vp, C.c_uint32, vp]
+        lib.adsa_prefill.restype = C.c_int
+        lib.adsa_prefill.argtypes = [pp, tp, mp, vp, vp, vp, f32p, C.c_uint32, vp, C.c_size_t, vp]
+        lib.adsa_prefill_workspace_bytes.restype = C.c_size_t
+        lib.adsa_prefill_workspace_bytes.argtypes = [pp, tp]
+        lib.adsa_attend_shared.restype = C.c_int
+        lib.adsa_attend_shared.argtypes = [pp, sp, mp, vp, vp, vp, vp, i32p, i32p, vp, f32p, C.c_uint32, vp, C.c_size_t, vp]
+        lib.adsa_shared_workspace_bytes.restype = C.c_size_t
+        lib.adsa_shared_workspace_bytes.argtypes = [pp, sp]
         lib.adsa_profile_enable.restype = C.c_int
         lib.adsa_profile_enable.argtypes = [C.c_int]
         lib.adsa_profile_read.restype = C.c_int
@@ -252,6 +300,87 @@ def adsa_step_static(params, seqs, q, k_new, v_new, out, lse, sel_idx, sel_cnt, 
                       seqs, q, k_new, v_new, out, lse, sel_idx, sel_cnt, keep_map)
     if rc != 0:
         raise AdsaError(rc, "adsa_step_static")
+
+
+def _axes(name, values, n):
+    values = tuple(int(x) for x in values)
+    if len(values) != n:
+        raise ValueError(f"{name}: one number for each of {n} axes expected")
+    return (C.c_int32 * MAX_AXES)(*values)
+
+
+def _expect(name, x, dtype, *shape):
+    """A device tensor that the C side reads as dtype without gaps (raw integers go through unchecked)."""
+    if x is None or isinstance(x, int):
+        return
+    if str(x.dtype) != f"torch.{dtype}" or not x.is_contiguous() or (shape and tuple(x.shape) != shape):
+        raise ValueError(f"{name}: a contiguous {dtype} tensor{' of shape ' + str(shape) if shape else ''} expected")
+
+
+def make_rope(freq, *, pairing="halves", text, origin, row, col) -> AdsaRope:
+    """Fill `adsa_rope`.  freq: fp64 device tensor [axes][head_dim / 2], radians by which one unit of each axis turns each pair; the other
+    arguments hold one integer per axis (see include/adsa.h for the rule from position to coordinates)."""
+    _expect("freq", freq, "float64")
+    if freq.dim() != 2 or not 1 <= freq.shape[0] <= MAX_AXES:
+        raise ValueError(f"freq: [1..{MAX_AXES}][head_dim / 2] expected")
+    n = freq.shape[0]
+    return AdsaRope(_ptr(freq), n, PAIRINGS[pairing], _axes("text", text, n), _axes("origin", origin, n), _axes("row", row, n),
+                    _axes("col", col, n))._hold(freq)
+
+
+def make_tokens(begin, slot0, n_tokens, max_len, *, pos0=None, coords=None, q_stride=0, k_stride=0, v_stride=0) -> AdsaTokens:
+    """Fill `adsa_tokens`: int32 device tensors begin [n_seq + 1], slot0 and pos0 [n_seq], coords [n_tokens][axes]."""
+    for name, x in (("begin", begin), ("slot0", slot0), ("pos0", pos0), ("coords", coords)):
+        _expect(name, x, "int32")
+    return AdsaTokens(n_tokens, max_len, _ptr(begin), _ptr(slot0), _ptr(pos0), _ptr(coords), q_stride, k_stride, v_stride)._hold(
+        begin, slot0, pos0, coords)
+
+
+def make_mods(*, softcap=0.0, mask=MASK_CAUSAL, slopes=None, doc=None) -> AdsaMods:
+    """Fill `adsa_mods`: slopes float32 [query heads], doc int32 [n_seq][>= cap], both on the device."""
+    _expect("slopes", slopes, "float32")
+    _expect("doc", doc, "int32")
+    return AdsaMods(softcap, mask, _ptr(slopes), _ptr(doc), 0 if doc is None else doc.shape[-1])._hold(slopes, doc)
+
+
+def make_shared(prompt_params, prompts, members, *, max_members) -> AdsaShared:
+    """Fill `adsa_shared`: the records `prompts` (one per group) of caches made for prompt_params, and int32 members [n_groups + 1]."""
+    _expect("members", members, "int32")
+    p = prompt_params
+    return AdsaShared(p.n_seq, p.cap, max_members, 0, _ptr(prompts), _ptr(members), p.kv_slot_stride, p.kv_head_stride)._hold(prompts, members)
+
+
+def _host(x):
+    return None if x is None else C.byref(x)
+
+
+def adsa_rotate(params, rope, seqs, q, k, q_out, k_out, coords=None, flags=0, stream=None, q_stride=0, k_stride=0) -> None:
+    _check(load_library().adsa_rotate(_host(params), _host(rope), _ptr(seqs), _ptr(coords), _ptr(q), _ptr(k), q_stride, k_stride, _ptr(q_out),
+                                      _ptr(k_out), flags, _stream(stream)), "adsa_rotate")
+
+
+def adsa_append(params, tokens, rope, seqs, q, k, v, q_out, flags=0, stream=None) -> None:
+    _check(load_library().adsa_append(_host(params), _host(tokens), _host(rope), _ptr(seqs), _ptr(q), _ptr(k), _ptr(v), _ptr(q_out), flags,
+                                      _stream(stream)), "adsa_append")
+
+
+def adsa_prefill_workspace_bytes(params, tokens) -> int:
+    return int(load_library().adsa_prefill_workspace_bytes(_host(params), _host(tokens)))
+
+
+def adsa_prefill(params, tokens, mods, seqs, q, out, lse, workspace, flags=0, stream=None) -> None:
+    _check(load_library().adsa_prefill(_host(params), _host(tokens), _host(mods), _ptr(seqs), _ptr(q), _ptr(out), _ptr(lse), flags,
+                                       _ptr(workspace), _nbytes(workspace), _stream(stream)), "adsa_prefill")
+
+
+def adsa_shared_workspace_bytes(params, shared) -> int:
+    return int(load_library().adsa_shared_workspace_bytes(_host(params), _host(shared)))
+
+
+def adsa_attend_shared(params, shared, mods, seqs, q, k_new, v_new, sel_idx, sel_cnt, out, lse, workspace, flags=0, stream=None) -> None:
+    _check(load_library().adsa_attend_shared(_host(params), _host(shared), _host(mods), _ptr(seqs), _ptr(q), _ptr(k_new), _ptr(v_new),
+                                             _ptr(sel_idx), _ptr(sel_cnt), _ptr(out), _ptr(lse), flags, _ptr(workspace), _nbytes(workspace),
+                                             _stream(stream)), "adsa_attend_shared")
 
 
 def adsa_profile_enable(on: bool) -> None:

@@ -11,7 +11,7 @@ LIB_DIR = os.path.join(_HERE, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libadsa_hip.so")
 NATIVE_PATH = os.path.join(LIB_DIR, "_adsa_native.so")       # CPython side of binding.py
 CEILING_PATH = os.path.join(LIB_DIR, "read_ceiling")
-SOURCES = ["api.hip", "select_compact.hip", "attend.hip", "attend_gqa.hip", "vcos.hip"]
+SOURCES = ["api.hip", "select_compact.hip", "attend.hip", "attend_gqa.hip", "vcos.hip", "prompt_api.hip", "rotary.hip", "prompt.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -44,7 +44,7 @@ def build_library(verbose: bool = False) -> str:
         objs.append(obj)
         jobs.append(([hipcc, *flags, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c",
                       os.path.join(CSRC, src), "-o", obj], verbose))
-    with ThreadPoolExecutor(max_workers=min(len(jobs), 6)) as pool:
+    with ThreadPoolExecutor(max_workers=min(len(jobs), 8)) as pool:
         list(pool.map(_compile_one, jobs))
     _compile_one(([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB_PATH], verbose))
     # measurement aid: the plain-read ceiling the attention kernel's roofline fraction is read against

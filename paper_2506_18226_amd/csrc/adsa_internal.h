@@ -124,6 +124,51 @@ hipError_t launch_step_finish(const adsa_params& p, adsa_seq* seqs, int32_t* kee
 hipError_t gqa_prepare_kernels();
 hipError_t vcos_prepare_kernels();
 
+// Checks a caller's parameters and turns them into those the kernels run with (api.hip).
+int resolve_params(const adsa_params* p, adsa_params* eff);
+int ensure_device_ready();
+static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// ---- prompts (prompt_api.hip checks and plans, rotary.hip and prompt.hip launch)
+struct PromptPlan {
+  bool few;             // a workgroup's waves share up to 32 rows and split the keys (else 32 rows each, all keys)
+  int tiles;            // row tiles per (sequence, cache head)
+  int chunks;           // parts the keys are split into
+};
+PromptPlan make_prompt_plan(const adsa_params& p, const adsa_tokens& t);
+struct PromptWorkspace {
+  size_t part_ml_off;   // float [T][hq][chunks][2]   (m, l) of split keys
+  size_t part_acc_off;  // float [T][hq][chunks][head_dim]
+  size_t norm_off;      // float [T][hq][2]   (m, 1 / l) of every row, for the attention mass
+  size_t total;
+};
+PromptWorkspace make_prompt_workspace(const adsa_params& p, const adsa_tokens& t, const PromptPlan& plan);
+
+struct SharedPlan {
+  int prompt_tiles;     // tiles of 32 (member, query head) rows per (group, cache head)
+  int prompt_chunks, own_chunks;       // parts that a prompt's slots and a list are split into
+};
+SharedPlan make_shared_plan(const adsa_params& p, const adsa_shared& s);
+struct SharedWorkspace {
+  size_t logits_off;    // float [n_seq][hq][sel_cap rounded up to 4]   scores of own lists, log2 units
+  size_t part_ml_off;   // float [n_seq][hq][prompt_chunks + own_chunks][2]
+  size_t part_acc_off;  // float [n_seq][hq][prompt_chunks + own_chunks][head_dim]
+  size_t total;
+  int lg_stride;
+};
+SharedWorkspace make_shared_workspace(const adsa_params& p, const SharedPlan& plan);
+
+hipError_t launch_rotate(const adsa_params& p, const adsa_rope& rope, const adsa_seq* seqs, const int32_t* coords, const void* q, const void* k,
+                         int64_t q_stride, int64_t k_stride, void* q_out, void* k_out, bool in_f32, hipStream_t st);
+hipError_t launch_append(const adsa_params& p, const adsa_tokens& t, const adsa_rope* rope, adsa_seq* seqs, const void* q, const void* k, const void* v,
+                         void* q_out, bool in_f32, bool advance, hipStream_t st);
+hipError_t launch_prefill(const adsa_params& p, const adsa_tokens& t, const adsa_mods& mods, const PromptPlan& plan, adsa_seq* seqs, const void* q, void* out,
+                          float* lse, char* ws, const PromptWorkspace& w, bool accumulate, bool advance, hipStream_t st);
+hipError_t launch_attend_shared(const adsa_params& p, const adsa_shared& s, const adsa_mods& mods, const SharedPlan& plan, adsa_seq* seqs, const void* q,
+                                const void* k_new, const void* v_new, const int32_t* sel_idx, const int32_t* sel_cnt, void* out, float* lse, char* ws,
+                                const SharedWorkspace& w, bool accumulate, bool append, bool advance, bool new_f32, hipStream_t st);
+hipError_t prompt_prepare_kernels();
+
 }  // namespace adsa
 
 // What the launch rules decide for parameters p, for tests that have to know which way a call goes (host only; not in adsa.h).

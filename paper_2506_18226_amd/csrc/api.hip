@@ -7,8 +7,6 @@
 namespace adsa {
 namespace {
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 int validate_resolved(const adsa_params* p) {
   if (!p) return ADSA_ERR_NULL;
   if (p->dtype != ADSA_F32 && p->dtype != ADSA_BF16) return ADSA_ERR_DTYPE;
@@ -54,6 +52,8 @@ int validate_resolved(const adsa_params* p) {
   return ADSA_OK;
 }
 
+}  // namespace
+
 // The parameters the kernels run with.  sel_groups == 1: the caller's own.  sel_groups == n_heads (one attended
 // set, one eviction history per head; Eq. 4 does not say which): every (sequence, head) IS a sequence of one cache
 // head -- the caller passes n_seq * n_heads records, record b * n_heads + h describing head h of sequence b (its K/V
@@ -76,18 +76,25 @@ int resolve_params(const adsa_params* p, adsa_params* eff) {
   return validate_resolved(eff);
 }
 
+namespace {
+
 // Per-device set-up that must not sit next to a launch (it would end up inside captured graphs, and tools that
 // intercept launches see it interleaved with them): done at the library's first call on a device.
 bool g_device_ready[64] = {};
+
+}  // namespace
+
 int ensure_device_ready() {
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return ADSA_ERR_LAUNCH;
   if (!g_device_ready[dev]) {
-    if (gqa_prepare_kernels() != hipSuccess || vcos_prepare_kernels() != hipSuccess) return ADSA_ERR_LAUNCH;
+    if (gqa_prepare_kernels() != hipSuccess || vcos_prepare_kernels() != hipSuccess || prompt_prepare_kernels() != hipSuccess) return ADSA_ERR_LAUNCH;
     g_device_ready[dev] = true;
   }
   return ADSA_OK;
 }
+
+namespace {
 
 int check_workspace(const adsa_params* p, const void* ws, size_t bytes, AttendPlan* plan, Workspace* w) {
   *plan = make_attend_plan(*p);

@@ -1,0 +1,1151 @@
+// Attention of many query rows over one set of keys, on the matrix cores (gfx950): prompts over the caches they have just entered
+// (adsa_prefill), and decode steps of sequences that share a prompt (adsa_attend_shared).
+//
+//  k_prompt, k_prompt_finish: a tile of (token, query head) rows of one (sequence, cache head) against the slots up to its last row's.
+//  k_prompt_mass: the probability every slot received, a second pass over the scores with each row's normaliser known: a workgroup owns
+//    its slots and takes the rows in order, so no atomics and one order of summation.
+//  k_shared, k_shared_finish: tiles of a group's (member, query head) rows against parts of the group's prompt, and each sequence's own
+//    list (the rows are then the query heads of a cache head), all as workgroups of one launch; the second kernel joins the parts.
+//
+// All of them turn around one tile product.  Scores are formed transposed, S^T = K Q^T (a 32x32 block: A = 32 keys, B = 32 rows), so a lane
+// holds 16 scores of ONE row (its column, lane % 32): maxima and sums are sums over registers and one exchange of the wave's halves,
+// and P^T is, register by register, the B operand of O^T = V^T P^T; the order of keys that this fixes within an instruction
+// is met on the other side by how V^T is fetched, bf16 by transposing LDS loads, so P never goes through memory.
+// Scores are held in fp32 and in units of log 2 (exp2 is the hardware's); so are sums, maxima and outputs until the end.  P enters the second
+// product in the cache's type: for bf16 that rounds each probability by 2^-9 at most, as much as the output's own rounding.
+#include <algorithm>
+#include <type_traits>
+
+#include "adsa_device.h"
+
+namespace adsa {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLowest = -3.4028234663852886e38f;     // the maximum of a row that has seen no key: z - kLowest is never NaN
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+#define ADSA_LDS __attribute__((address_space(3)))
+typedef ADSA_LDS char lchar;
+
+// What is done to scores before the softmax.
+struct Mods {
+  const float* slopes;         // per query head, or NULL
+  const int32_t* doc;          // [n_seq][doc_stride], or NULL
+  long long doc_stride;
+  float cap_in, cap_out;       // softmax scale / cap, cap * log2(e); cap_out 0: no cap
+  float scale_log2;            // softmax scale * log2(e)
+};
+
+// The keys of a workgroup, one (sequence, cache head): entries [begin, end) of a list of slots, or the slots themselves.
+struct Keys {
+  const gchar* k;              // row of slot 0
+  const gchar* v;
+  long long stride_b;
+  const gint* list;
+  const gint* pos;             // of slots (slopes)
+  const gint* doc;             // of slots
+  gfloat* logits;              // own lists: scores of row 0 of the tile, log2 units; the next row's lg_stride on
+  int lg_stride, lg_rows;
+  int begin, end, last_slot, skip;     // skip: a slot that is not attended
+};
+
+// A lane's row: what it sees are keys below `limit` (of its document).
+struct Row {
+  int limit, pos, doc;
+  float slope;                 // log2 units
+};
+
+template <int EB, int D> struct Layout {
+  static constexpr int RB = D * EB, CPR = RB / 16;         // bytes and 16-byte pieces of a row
+  // A row's pieces are permuted so that the 16 lanes of an LDS access that read the same piece of 16 rows (K), or 4 rows' pieces of
+  // 16 columns (V), meet all banks.
+  static __device__ __forceinline__ int swz_k(int row) { return CPR == 8 ? (row >> 1) & 7 : row & 15; }
+  static __device__ __forceinline__ int swz_v(int row) {
+    return EB == 4 ? ((row >> 2) & 1) << 3 : CPR == 8 ? ((row >> 1) & 1) << 2 : (row & 3) << 2;
+  }
+};
+
+__device__ __forceinline__ uint4 lds16(const lchar* p) {
+  const u32x4 v = *(const ADSA_LDS u32x4*)p;
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+__device__ __forceinline__ void put16(lchar* p, const uint4& x) { *(ADSA_LDS u32x4*)p = u32x4{x.x, x.y, x.z, x.w}; }
+
+__device__ __forceinline__ bool bf16_bad(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
+__device__ __forceinline__ uint32_t bf16_finite(uint32_t w) {            // infinities and NaN as 0
+  if ((w & 0x7F80u) == 0x7F80u) w &= 0xFFFF0000u;
+  if ((w & 0x7F800000u) == 0x7F800000u) w &= 0xFFFFu;
+  return w;
+}
+__device__ __forceinline__ bool f32_bad(float x) { return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u; }
+
+// scores of 16 elements: fp32 sum q.k -> log2 units
+template <int EB>
+__device__ __forceinline__ float capped(float s, const Mods& mods) {
+  const float t = s * mods.cap_in;
+  if constexpr (EB == 4) return mods.cap_out * tanhf(t);
+  // tanh t = 1 - 2 / (e^2t + 1): off by 2^-23 of 1, far below the rounding of bf16 inputs
+  return mods.cap_out * fmaf(-2.0f, __builtin_amdgcn_rcpf(fast_exp2(t * (2.0f * kLog2e)) + 1.0f), 1.0f);
+}
+
+template <int EB, int D, int WR, int WK, int KT> struct Shape {
+  static constexpr int kThreads = WR * WK * kWave;
+  static constexpr int kRows = 32 * WR;                // rows of a workgroup's tile
+  static constexpr int TK = WK * KT;                   // keys of a step
+  static constexpr int kMeta = 2 * TK * Layout<EB, D>::RB;             // LDS: K, V, then per key: position (float), document, flag
+  static constexpr int kStep = kMeta + 3 * TK * 4;
+  static constexpr int kMerge = WK > 1 ? WK * (D / 32) * 16 * kWave * 4 + 2 * WK * kWave * 4 : 0;       // over the same memory, behind the loop
+  static constexpr int kLds = kStep > kMerge ? kStep : kMerge;
+};
+
+// The attention of a workgroup's rows (32 per row wave; a lane's q pieces in qf) over its keys.  Afterwards m, l (of the lane's row, both halves of
+// the wave alike) and the wave's share of the unnormalised outputs: acc[r], r in [0, D / 32 * 16 / WK), are the
+// elements of register r + wk * (...) of the D / 32 transposed 32x32 blocks.
+template <int EB, int D, int WR, int WK, int KT, bool MOD, bool LIST>
+struct Tile {
+  using L = Layout<EB, D>;
+  using S = Shape<EB, D, WR, WK, KT>;
+  static constexpr int NT = S::kThreads, TK = S::TK, CPR = L::CPR, RB = L::RB, SUB = KT / 32, DT = D / 32;
+  static constexpr int RPT = NT / CPR, NL = TK / RPT;                   // rows per round of the threads; rounds
+  static constexpr int kMine = DT * 16 / WK;                            // output registers of a lane after the waves' merge
+  static_assert(TK % RPT == 0 && NT >= TK && kMine % 4 == 0, "whole rounds");
+
+  const Mods& mods;
+  const Keys& keys;
+  lchar* const lds;
+  const int tid, lane, col, half, wr, wk;
+  uint4 qf[CPR / 2];
+  Row row;
+  f32x16 acc[DT];
+  float m, l;
+  // the next step's rows on their way
+  uint4 kr[NL], vr[NL];
+  int slot_next[NL];           // LIST: slots of the step after it
+  int meta_slot;
+  float meta_pos;
+  int meta_doc;
+
+  __device__ __forceinline__ Tile(const Mods& mods_, const Keys& keys_, lchar* lds_)
+      : mods(mods_), keys(keys_), lds(lds_), tid(threadIdx.x), lane(threadIdx.x % kWave), col(lane % 32), half(lane / 32),
+        wr(__builtin_amdgcn_readfirstlane(tid / kWave) % WR), wk(__builtin_amdgcn_readfirstlane(tid / kWave) / WR) {}
+
+  __device__ __forceinline__ void load_q(const gchar* q_row) {
+#pragma unroll
+    for (int s = 0; s < CPR / 2; ++s) qf[s] = load16(q_row + (2 * s + half) * 16);
+  }
+
+  // entry of the list, or the key itself, brought into the cache; the slot that is not attended: its neighbour in the list instead
+  // (rows of the cache that hold nothing yet must not reach the sums, not even times 0)
+  __device__ __forceinline__ int slot_at(int key) const {
+    const int at = min(key, keys.end - 1);
+    if constexpr (!LIST) return at;
+    int s = keys.list[at];
+    if (s == keys.skip) s = keys.list[at > keys.begin ? at - 1 : min(at + 1, keys.end - 1)];
+    return min(max(s, 0), keys.last_slot);
+  }
+  __device__ __forceinline__ void load_slots(int base) {
+    if constexpr (LIST) {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) slot_next[i] = slot_at(base + tid / CPR + i * RPT);
+    }
+  }
+  __device__ __forceinline__ void load_rows(int base) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int slot = LIST ? slot_next[i] : slot_at(base + tid / CPR + i * RPT);
+      const long long off = (long long)slot * keys.stride_b + (tid % CPR) * 16;
+      kr[i] = load16(keys.k + off);
+      vr[i] = load16(keys.v + off);
+    }
+    if (tid < TK) {
+      const int at = min(base + tid, keys.end - 1);
+      if constexpr (LIST) meta_slot = keys.list[at];
+      if constexpr (MOD) {
+        const int slot = slot_at(base + tid);
+        meta_pos = mods.slopes ? (float)keys.pos[slot] : 0.0f;
+        meta_doc = keys.doc ? keys.doc[slot] : 0;
+      }
+    }
+  }
+  __device__ __forceinline__ void store_rows() {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int r = tid / CPR + i * RPT, c = tid % CPR;
+      put16(lds + r * RB + ((c ^ L::swz_k(r)) << 4), kr[i]);
+      put16(lds + TK * RB + r * RB + ((c ^ L::swz_v(r)) << 4), vr[i]);
+    }
+    if (tid < TK) {
+      ADSA_LDS int* const meta = (ADSA_LDS int*)(lds + S::kMeta);
+      if constexpr (MOD) { meta[tid] = __float_as_int(meta_pos); meta[TK + tid] = meta_doc; }
+      if constexpr (LIST) meta[2 * TK + tid] = meta_slot == keys.skip;
+    }
+  }
+
+  // O^T += V^T P^T over the 32 keys from row r0 of the step; TIDY: infinities and NaN of V count as 0
+  template <bool TIDY>
+  __device__ __forceinline__ void add_values(int r0, const float* p) {
+    const lchar* const v = lds + TK * RB;
+    if constexpr (EB == 2) {
+      bf16x8 pb[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const u32x4 w = {pack2_bf16(p[8 * t], p[8 * t + 1]), pack2_bf16(p[8 * t + 2], p[8 * t + 3]), pack2_bf16(p[8 * t + 4], p[8 * t + 5]),
+                         pack2_bf16(p[8 * t + 6], p[8 * t + 7])};
+        pb[t] = __builtin_bit_cast(bf16x8, w);
+      }
+      // element j of a lane of half h belongs to key 16 t + 8 (j / 4) + 4 h + j % 4: where the score register 8 t + j has it.  A transposing load
+      // gives lane i of 16 column i of 4 rows of 16 elements, of which lane 4 r + c addresses 4 elements of row r from column 4 c on.
+      const int vrow = r0 + half * 4 + (lane % 16) / 4, vcol = ((lane / 16) & 1) * 16 + (lane % 4) * 4;
+      const lchar* const at = v + vrow * RB + (vcol % 8) * 2;
+      const int sw = L::swz_v(vrow);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const lchar* const from = at + (((dt * 4 + vcol / 8) ^ sw) << 4);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ADSA_LDS i16x4*)(from + (16 * t) * RB));
+          const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ADSA_LDS i16x4*)(from + (16 * t + 8) * RB));
+          const u32x2 a = __builtin_bit_cast(u32x2, lo), b = __builtin_bit_cast(u32x2, hi);
+          u32x4 w = {a.x, a.y, b.x, b.y};
+          if constexpr (TIDY) w = u32x4{bf16_finite(w.x), bf16_finite(w.y), bf16_finite(w.z), bf16_finite(w.w)};
+          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pb[t], acc[dt], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = r0 + (i / 4) * 8 + half * 4 + i % 4, sw = L::swz_v(key);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          float a = *(const ADSA_LDS float*)(v + key * RB + (((dt * 8 + col / 4) ^ sw) << 4) + (col % 4) * 4);
+          if constexpr (TIDY) a = f32_bad(a) ? 0.0f : a;
+          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[i], acc[dt], 0, 0, 0);
+        }
+      }
+    }
+  }
+  // whether V of these 32 keys holds an infinity or a NaN
+  __device__ __forceinline__ bool values_bad(int r0) const {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 32 * CPR / kWave; ++i) {
+      const uint4 w = lds16(lds + TK * RB + r0 * RB + (i * kWave + lane) * 16);
+      if constexpr (EB == 2) bad |= bf16_bad(w.x) || bf16_bad(w.y) || bf16_bad(w.z) || bf16_bad(w.w);
+      else bad |= f32_bad(__uint_as_float(w.x)) || f32_bad(__uint_as_float(w.y)) || f32_bad(__uint_as_float(w.z)) || f32_bad(__uint_as_float(w.w));
+    }
+    return __ballot(bad) != 0;
+  }
+  // ... and what those give the rows that see their key (rare: one key after the other)
+  __device__ __forceinline__ void add_bad_values(int r0, const float* p) {
+    for (int key = 0; key < 32; ++key) {
+      const int reg = key / 8 * 4 + key % 4;
+      float x = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x = i == reg ? p[i] : x;
+      x = __shfl(x, col + 32 * ((key >> 2) & 1));
+      const int r = r0 + key, sw = L::swz_v(r);
+      const lchar* const v = lds + TK * RB + r * RB;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int d = dt * 32 + (i / 4) * 8 + half * 4 + i % 4, at = (((d * EB / 16) ^ sw) << 4) + d * EB % 16;
+          float a;
+          if constexpr (EB == 2) a = __uint_as_float((uint32_t)*(const ADSA_LDS uint16_t*)(v + at) << 16);
+          else a = *(const ADSA_LDS float*)(v + at);
+          if (x > 0.0f && f32_bad(a)) acc[dt][i] += x * a;
+        }
+    }
+  }
+
+  // one step's keys of this wave; masked: some row does not see all of them
+  __device__ __forceinline__ void fold(int base, bool masked) {
+    const int r0 = wk * KT;
+    f32x16 s[SUB];
+    const lchar* const krow = lds + (r0 + col) * RB;
+    const int sw = L::swz_k(r0 + col);
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+      s[u] = f32x16{};
+#pragma unroll
+      for (int c = 0; c < CPR / 2; ++c) {
+        const uint4 a = lds16(krow + u * 32 * RB + (((2 * c + half) ^ sw) << 4));
+        if constexpr (EB == 2) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, qf[c]), s[u], 0, 0, 0);
+        else {
+          const uint32_t ka[4] = {a.x, a.y, a.z, a.w}, qa[4] = {qf[c].x, qf[c].y, qf[c].z, qf[c].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(ka[e]), __uint_as_float(qa[e]), s[u], 0, 0, 0);
+        }
+      }
+    }
+    const float scale = MOD ? 1.0f : mods.scale_log2;
+    const ADSA_LDS int* const meta = (const ADSA_LDS int*)(lds + S::kMeta) + r0;
+    if constexpr (MOD) {
+      if (mods.cap_out != 0.0f) {
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[u][i] = capped<EB>(s[u][i], mods);
+      } else {
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[u][i] *= mods.scale_log2;
+      }
+      if (mods.slopes) {
+        const float here = (float)row.pos;
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            s[u][i] = fmaf(-row.slope, fabsf(here - __int_as_float(meta[u * 32 + (i / 4) * 8 + half * 4 + i % 4])), s[u][i]);
+      }
+    }
+    if (masked) {
+#pragma unroll
+      for (int u = 0; u < SUB; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int k = u * 32 + (i / 4) * 8 + half * 4 + i % 4;
+          bool seen = base + r0 + k < row.limit;
+          if constexpr (LIST) seen &= meta[2 * TK + k] == 0;
+          if constexpr (MOD)
+            if (keys.doc) seen &= meta[TK + k] == row.doc;
+          s[u][i] = seen ? s[u][i] : -INFINITY;
+        }
+    }
+    if constexpr (LIST) {
+      if (keys.logits && col < keys.lg_rows) {       // (entries past the list: the row's padding, or the next chunk's, which must stay)
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int k = base + r0 + u * 32 + (i / 4) * 8 + half * 4 + i % 4;
+            if (k < keys.end) keys.logits[(size_t)col * keys.lg_stride + k] = s[u][i] * scale;
+          }
+      }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int u = 0; u < SUB; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = max2(mx, s[u][i]);
+    mx = xor_max<32>(mx) * scale;
+    if (__ballot(mx > m) != 0) {                     // some row's maximum rose: bring every row's state to its new one
+      const float m_new = max2(m, mx), corr = fast_exp2(m - m_new);
+      m = m_new;
+      l *= corr;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[dt][i] *= corr;
+    }
+    float p[SUB][16], sum = 0.0f;
+#pragma unroll
+    for (int u = 0; u < SUB; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        p[u][i] = fast_exp2(fmaf(s[u][i], scale, -m));
+        sum += p[u][i];
+      }
+    l += sum;
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+      if (masked && values_bad(r0 + u * 32)) {
+        add_bad_values(r0 + u * 32, p[u]);
+        add_values<true>(r0 + u * 32, p[u]);
+      } else add_values<false>(r0 + u * 32, p[u]);
+    }
+  }
+
+  __device__ __forceinline__ void run() {
+    m = kLowest;
+    l = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x16{};
+    // keys that all rows of the wave see, and that none sees any more
+    int lo = row.limit, hi = row.limit;
+#pragma unroll
+    for (int x = 1; x < 32; x <<= 1) { lo = min(lo, __shfl_xor(lo, x)); hi = max(hi, __shfl_xor(hi, x)); }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
+    load_slots(keys.begin);
+    load_rows(keys.begin);
+    load_slots(keys.begin + TK);
+    for (int base = keys.begin; base < keys.end; base += TK) {
+      __syncthreads();                               // (the step before has been read)
+      store_rows();
+      __syncthreads();
+      if (base + TK < keys.end) {
+        load_rows(base + TK);
+        load_slots(base + 2 * TK);
+      }
+      const int first = base + wk * KT;
+      if (first < hi) {
+        bool masked = first + KT > lo;
+        if constexpr (MOD) masked |= keys.doc != nullptr;
+        if constexpr (LIST) {
+          if (keys.skip >= 0) {
+            const ADSA_LDS int* const flag = (const ADSA_LDS int*)(lds + S::kMeta) + 2 * TK + wk * KT;
+            masked |= __ballot(lane < KT && flag[lane % KT] != 0) != 0;
+          }
+        }
+        fold(base, masked);
+      }
+    }
+    l = xor_sum<32>(l);
+    if constexpr (WK > 1) {                          // the waves' states meet in LDS
+      ADSA_LDS float* const a = (ADSA_LDS float*)lds;
+      ADSA_LDS float* const ml = a + WK * DT * 16 * kWave;
+      __syncthreads();
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) a[((wk * DT + dt) * 16 + i) * kWave + lane] = acc[dt][i];
+      ml[wk * kWave + lane] = m;
+      ml[(WK + wk) * kWave + lane] = l;
+      __syncthreads();
+      float w[WK], M = kLowest, sum = 0.0f;
+#pragma unroll
+      for (int k = 0; k < WK; ++k) M = fmaxf(M, ml[k * kWave + lane]);
+#pragma unroll
+      for (int k = 0; k < WK; ++k) {
+        w[k] = fast_exp2(ml[k * kWave + lane] - M);
+        sum = fmaf(ml[(WK + k) * kWave + lane], w[k], sum);
+      }
+      m = M;
+      l = sum;
+#pragma unroll
+      for (int r = 0; r < kMine; ++r) {
+        float x = 0.0f;
+#pragma unroll
+        for (int k = 0; k < WK; ++k) x = fmaf(a[(k * DT * 16 + wk * kMine + r) * kWave + lane], w[k], x);
+        acc[r / 16][r % 16] = x;
+      }
+    }
+  }
+  // first of the 4 consecutive elements that registers r .. r + 3 of the wave's share hold
+  __device__ __forceinline__ int element(int r) const {
+    const int i = (WK > 1 ? wk * kMine : 0) + r;
+    return i / 16 * 32 + i % 16 / 4 * 8 + half * 4;
+  }
+};
+
+template <int EB>
+__device__ __forceinline__ void store4(gchar* p, float a, float b, float c, float d) {
+  if constexpr (EB == 4) *(ADSA_GLOBAL u32x4*)p = u32x4{__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d)};
+  else *(ADSA_GLOBAL u32x2*)p = u32x2{pack2_bf16(a, b), pack2_bf16(c, d)};
+}
+
+// ---------------------------------------------------------------------------------------------------- prompts
+struct PromptArgs {
+  adsa_seq* seqs;
+  const int32_t* begin;
+  const int32_t* slot0;
+  const char* q;
+  char* out;
+  float* lse;
+  float* part_ml;
+  float* part_acc;
+  float* norm;                 // NULL: no attention mass wanted
+  Mods mods;
+  long long slot_stride_b, head_stride_b;
+  int n_seq, n_tokens, max_len, h, G, cap, mask, tiles, chunks, advance;
+};
+
+// A sequence's new tokens: where they stand in the packed rows and in the cache.
+struct Prompt {
+  int from, len, slot0, prefix, status;      // status: 0, or why the record does not fit
+};
+__device__ __forceinline__ Prompt prompt_of(const PromptArgs& A, int b) {
+  const ADSA_GLOBAL adsa_seq& sq = ((const ADSA_GLOBAL adsa_seq*)A.seqs)[b];
+  Prompt pr;
+  pr.from = ((const gint*)A.begin)[b];
+  pr.len = ((const gint*)A.begin)[b + 1] - pr.from;
+  pr.slot0 = ((const gint*)A.slot0)[b];
+  pr.status = sq.status;
+  const int n_res = sq.n_res;
+  pr.prefix = A.mask == ADSA_MASK_PREFIX ? sq.n_keep_prefix : 0;
+  if (pr.from < 0 || pr.len < 0 || pr.len > A.n_tokens || pr.from > A.n_tokens - pr.len) pr.len = 0;        // (begin[] is not what it should be)
+  if (pr.status == 0 && (n_res < 0 || n_res > A.cap || pr.slot0 < 0 || pr.len > A.max_len || pr.slot0 > n_res - pr.len)) pr.status = ADSA_SEQ_BAD_STATE;
+  return pr;
+}
+// keys below this are seen by the token in slot s
+__device__ __forceinline__ int limit_of(const Prompt& pr, int s) {
+  return s < pr.prefix ? max(s + 1, min(pr.prefix, pr.slot0 + pr.len)) : s + 1;
+}
+
+// (pair of sequence and cache head, unit) of a workgroup: workgroups are dealt round robin to the 8 dies, so pairs are dealt by eights and a
+// pair's units, which read the same K and V, follow each other on one die.
+__device__ __forceinline__ void pair_of(unsigned id, unsigned units, int* pair, int* unit) {
+  const unsigned y = id / 8;
+  *pair = (int)(y / units * 8 + id % 8);
+  *unit = (int)(y % units);
+}
+
+template <int EB, int D, int WR, int WK, int KT, bool MOD>
+__global__ __launch_bounds__(WR * WK * kWave) void k_prompt(PromptArgs A) {
+  using T = Tile<EB, D, WR, WK, KT, MOD, false>;
+  using S = typename T::S;
+  extern __shared__ __align__(16) char s_lds[];
+  int pair, unit;
+  pair_of(blockIdx.x, (unsigned)(A.tiles * A.chunks), &pair, &unit);
+  if (pair >= A.n_seq * A.h) return;
+  const int b = pair / A.h, head = pair % A.h, chunk = unit % A.chunks, tile = A.tiles - 1 - unit / A.chunks;     // (the longest rows first)
+  const int tid = threadIdx.x, hq = A.h * A.G;
+  ADSA_GLOBAL adsa_seq& sq = ((ADSA_GLOBAL adsa_seq*)A.seqs)[b];
+  const Prompt pr = prompt_of(A, b);
+  if (pr.status != 0) {                              // zeros, by the workgroups of the sequence together
+    if (chunk != 0) return;
+    if (head == 0 && tile == 0 && tid == 0 && sq.status == 0) sq.status = pr.status;
+    for (long long r = tile; r < pr.len; r += A.tiles) {
+      const size_t at = ((size_t)(pr.from + r) * hq + head * A.G);
+      for (int o = tid; o < A.G * D * EB / 4; o += S::kThreads) ((gint*)(A.out + at * D * EB))[o] = 0;
+      for (int o = tid; o < A.G; o += S::kThreads) ((gfloat*)A.lse)[at + o] = 0.0f;
+    }
+    return;
+  }
+  const int rows = pr.len * A.G, row0 = tile * S::kRows;
+  if (row0 >= rows) return;
+  if (A.advance && head == 0 && tile == 0 && chunk == 0 && tid == 0) sq.step = sq.step + 1;
+
+  Keys keys;
+  keys.k = (const gchar*)sq.k + head * A.head_stride_b;
+  keys.v = (const gchar*)sq.v + head * A.head_stride_b;
+  keys.stride_b = A.slot_stride_b;
+  keys.list = nullptr;
+  keys.pos = (const gint*)sq.pos;
+  keys.doc = A.mods.doc ? (const gint*)A.mods.doc + b * A.mods.doc_stride : nullptr;
+  keys.logits = nullptr;
+  keys.skip = -1;
+  // what the tile's last row sees (a row of the prefix may see more than later rows)
+  const int last_slot = pr.slot0 + min(row0 + S::kRows, rows) / A.G - 1 + (min(row0 + S::kRows, rows) % A.G != 0 ? 1 : 0);
+  const int first_slot = pr.slot0 + row0 / A.G;
+  const int n = max(limit_of(pr, last_slot), limit_of(pr, first_slot));
+  const int per = A.chunks == 1 ? n : ((n + A.chunks - 1) / A.chunks + 31) / 32 * 32;
+  keys.begin = min(n, chunk * per);
+  keys.end = min(n, keys.begin + per);
+
+  T t(A.mods, keys, (lchar*)s_lds);
+  const int r = row0 + t.wr * 32 + t.col;            // the lane's row; past the last one: that one again, not stored
+  const bool valid = r < rows;
+  const int rr = min(r, rows - 1), token = rr / A.G, qh = head * A.G + rr % A.G, slot = pr.slot0 + token;
+  const size_t at = (size_t)(pr.from + token) * hq + qh;
+  t.row.limit = min(limit_of(pr, slot), keys.end);   // (a step past the end of a part repeats its last key)
+  t.row.pos = 0;
+  t.row.doc = 0;
+  t.row.slope = 0.0f;
+  if constexpr (MOD) {
+    if (A.mods.slopes) { t.row.pos = keys.pos[slot]; t.row.slope = ((const gfloat*)A.mods.slopes)[qh] * kLog2e; }
+    if (keys.doc) {
+      t.row.doc = keys.doc[slot];
+      if (t.row.doc < 0) t.row.limit = 0;
+    }
+  }
+  t.load_q((const gchar*)A.q + at * (D * EB));
+  t.run();
+  if (!valid) return;
+  if (A.chunks > 1) {
+    gfloat* const acc = (gfloat*)A.part_acc + (at * A.chunks + chunk) * D;
+#pragma unroll
+    for (int i = 0; i < T::kMine; i += 4)
+      store4<4>((gchar*)(acc + t.element(i)), t.acc[i / 16][i % 16], t.acc[i / 16][i % 16 + 1], t.acc[i / 16][i % 16 + 2], t.acc[i / 16][i % 16 + 3]);
+    if (t.half == 0 && t.wk == 0) {
+      gfloat* const ml = (gfloat*)A.part_ml + (at * A.chunks + chunk) * 2;
+      ml[0] = t.m;
+      ml[1] = t.l;
+    }
+    return;
+  }
+  const float inv = t.l > 0.0f ? 1.0f / t.l : t.l == 0.0f ? 0.0f : t.l;       // (a NaN stays one)
+  gchar* const out = (gchar*)A.out + at * (D * EB);
+#pragma unroll
+  for (int i = 0; i < T::kMine; i += 4)
+    store4<EB>(out + t.element(i) * EB, t.acc[i / 16][i % 16] * inv, t.acc[i / 16][i % 16 + 1] * inv, t.acc[i / 16][i % 16 + 2] * inv,
+               t.acc[i / 16][i % 16 + 3] * inv);
+  if (t.half == 0 && t.wk == 0) {
+    ((gfloat*)A.lse)[at] = t.l == 0.0f ? -INFINITY : (t.m + __log2f(t.l)) * kLn2;
+    if (A.norm) { ((gfloat*)A.norm)[2 * at] = t.m; ((gfloat*)A.norm)[2 * at + 1] = inv; }
+  }
+}
+
+// Split keys: a wave joins the parts of one row.
+template <int EB, int D>
+__global__ __launch_bounds__(256) void k_prompt_finish(PromptArgs A) {
+  const int lane = threadIdx.x % kWave, hq = A.h * A.G;
+  const size_t at = (size_t)blockIdx.x * (256 / kWave) + threadIdx.x / kWave;
+  if (at >= (size_t)A.n_tokens * hq) return;
+  const int token = (int)(at / hq);
+  // its sequence: the last one that begins at or before the token
+  int lo = 0, hi = A.n_seq;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (((const gint*)A.begin)[mid] <= token) lo = mid; else hi = mid;
+  }
+  const Prompt pr = prompt_of(A, lo);
+  if (pr.status != 0 || token < pr.from || token >= pr.from + pr.len) return;           // (zeros already)
+  const gfloat* const ml = (const gfloat*)A.part_ml + at * A.chunks * 2;
+  const gfloat* const acc = (const gfloat*)A.part_acc + at * A.chunks * D;
+  float M = kLowest, L = 0.0f, x[D / kWave];
+  for (int c = 0; c < A.chunks; ++c) M = fmaxf(M, ml[2 * c]);
+#pragma unroll
+  for (int e = 0; e < D / kWave; ++e) x[e] = 0.0f;
+  for (int c = 0; c < A.chunks; ++c) {
+    const float w = fast_exp2(ml[2 * c] - M);
+    L = fmaf(ml[2 * c + 1], w, L);
+#pragma unroll
+    for (int e = 0; e < D / kWave; ++e) x[e] = fmaf(acc[(size_t)c * D + e * kWave + lane], w, x[e]);
+  }
+  const float inv = L > 0.0f ? 1.0f / L : L == 0.0f ? 0.0f : L;
+#pragma unroll
+  for (int e = 0; e < D / kWave; ++e) {
+    const size_t o = at * D + e * kWave + lane;
+    if constexpr (EB == 4) ((gfloat*)A.out)[o] = x[e] * inv;
+    else ((ADSA_GLOBAL uint16_t*)A.out)[o] = (uint16_t)f32_to_bf16_rne(x[e] * inv);
+  }
+  if (lane == 0) {
+    ((gfloat*)A.lse)[at] = L == 0.0f ? -INFINITY : (M + __log2f(L)) * kLn2;
+    if (A.norm) { ((gfloat*)A.norm)[2 * at] = M; ((gfloat*)A.norm)[2 * at + 1] = inv; }
+  }
+}
+
+// score[head][slot] += sum over rows of the probability they gave the slot.  A wave keeps 32 slots' K rows as the B operand and meets 64
+// rows per step, from the first that can see the slots on; scores come untransposed (a lane's column is a slot), so a lane sums its own.
+constexpr int kMassRows = 64, kMassKeys = 128;
+template <int EB, int D> struct MassLds {
+  static constexpr int kInfo = kMassRows * Layout<EB, D>::RB;          // q rows, then per row: m, 1 / l, limit, slope, position, document
+  static constexpr int kLds = kInfo + 6 * kMassRows * 4;
+};
+template <int EB, int D, bool MOD>
+__global__ __launch_bounds__(256) void k_prompt_mass(PromptArgs A, int key_tiles) {
+  using L = Layout<EB, D>;
+  constexpr int CPR = L::CPR, RB = L::RB, RPT = 256 / CPR, NL = kMassRows / RPT;
+  extern __shared__ __align__(16) char s_lds[];
+  lchar* const lds = (lchar*)s_lds;
+  int pair, tile;
+  pair_of(blockIdx.x, (unsigned)key_tiles, &pair, &tile);
+  if (pair >= A.n_seq * A.h) return;
+  const int b = pair / A.h, head = pair % A.h, tid = threadIdx.x, lane = tid % kWave, col = lane % 32, half = lane / 32;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave), hq = A.h * A.G;
+  const Prompt pr = prompt_of(A, b);
+  const int n = pr.slot0 + pr.len, key0 = tile * kMassKeys, rows = pr.len * A.G;
+  if (pr.status != 0 || pr.len == 0 || key0 >= n) return;
+  const ADSA_GLOBAL adsa_seq& sq = ((const ADSA_GLOBAL adsa_seq*)A.seqs)[b];
+  const int key = key0 + wave * 32 + col, slot = min(key, n - 1);
+  const gint* const doc = A.mods.doc ? (const gint*)A.mods.doc + b * A.mods.doc_stride : nullptr;
+  uint4 kf[CPR / 2];
+  const gchar* const krow = (const gchar*)sq.k + head * A.head_stride_b + (long long)slot * A.slot_stride_b;
+#pragma unroll
+  for (int c = 0; c < CPR / 2; ++c) kf[c] = load16(krow + (2 * c + half) * 16);
+  const float kpos = MOD && A.mods.slopes ? (float)((const gint*)sq.pos)[slot] : 0.0f;
+  const int kdoc = MOD && doc ? doc[slot] : 0;
+  // the first row that sees the tile: the token of its first slot, or any where the prefix sees itself
+  const int token0 = key0 < pr.prefix ? 0 : max(0, key0 - pr.slot0);
+  uint4 qr[NL];
+  float info[6];
+  auto load = [&](int base) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int r = min(base + tid / CPR + i * RPT, rows - 1);
+      qr[i] = load16((const gchar*)A.q + ((size_t)(pr.from + r / A.G) * hq + head * A.G + r % A.G) * RB + (tid % CPR) * 16);
+    }
+    if (tid < kMassRows) {
+      const int r = min(base + tid, rows - 1), token = r / A.G, qh = head * A.G + r % A.G, s = pr.slot0 + token;
+      const size_t at = (size_t)(pr.from + token) * hq + qh;
+      info[0] = ((const gfloat*)A.norm)[2 * at];
+      info[1] = ((const gfloat*)A.norm)[2 * at + 1];
+      info[2] = __int_as_float(base + tid < rows ? limit_of(pr, s) : 0);
+      info[3] = MOD && A.mods.slopes ? ((const gfloat*)A.mods.slopes)[qh] * kLog2e : 0.0f;
+      info[4] = MOD && A.mods.slopes ? (float)((const gint*)sq.pos)[s] : 0.0f;
+      info[5] = __int_as_float(MOD && doc ? doc[s] : 0);
+      if (MOD && doc && doc[s] < 0) info[2] = __int_as_float(0);
+    }
+  };
+  float sum = 0.0f;
+  const float scale = MOD ? 1.0f : A.mods.scale_log2;
+  const ADSA_LDS float* const at = (const ADSA_LDS float*)(lds + MassLds<EB, D>::kInfo);
+  load(token0 * A.G);
+  for (int base = token0 * A.G; base < rows; base += kMassRows) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int r = tid / CPR + i * RPT;
+      put16(lds + r * RB + (((tid % CPR) ^ L::swz_k(r)) << 4), qr[i]);
+    }
+    if (tid < kMassRows) {
+#pragma unroll
+      for (int i = 0; i < 6; ++i) ((ADSA_LDS float*)(lds + MassLds<EB, D>::kInfo))[i * kMassRows + tid] = info[i];
+    }
+    __syncthreads();
+    if (base + kMassRows < rows) load(base + kMassRows);
+#pragma unroll
+    for (int u = 0; u < kMassRows / 32; ++u) {
+      f32x16 s = {};
+      const lchar* const qrow = lds + (u * 32 + col) * RB;
+      const int sw = L::swz_k(u * 32 + col);
+#pragma unroll
+      for (int c = 0; c < CPR / 2; ++c) {
+        const uint4 a = lds16(qrow + (((2 * c + half) ^ sw) << 4));
+        if constexpr (EB == 2) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, kf[c]), s, 0, 0, 0);
+        else {
+          const uint32_t qa[4] = {a.x, a.y, a.z, a.w}, ka[4] = {kf[c].x, kf[c].y, kf[c].z, kf[c].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(qa[e]), __uint_as_float(ka[e]), s, 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int r = u * 32 + (i / 4) * 8 + half * 4 + i % 4;
+        float z = s[i];
+        if constexpr (MOD) {
+          z = A.mods.cap_out != 0.0f ? capped<EB>(z, A.mods) : z * A.mods.scale_log2;
+          if (A.mods.slopes) z = fmaf(-at[3 * kMassRows + r], fabsf(at[4 * kMassRows + r] - kpos), z);
+        }
+        bool seen = key < __float_as_int(at[2 * kMassRows + r]);
+        if constexpr (MOD)
+          if (doc) seen &= __float_as_int(at[5 * kMassRows + r]) == kdoc;
+        const float p = fast_exp2(fmaf(z, scale, -at[r])) * at[kMassRows + r];
+        sum += seen ? p : 0.0f;
+      }
+    }
+  }
+  sum = xor_sum<32>(sum);
+  if (half == 0 && key < n) {
+    gfloat* const score = (gfloat*)sq.score + (size_t)head * A.cap + key;
+    *score = *score + sum;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------- shared prompts
+struct SharedArgs {
+  adsa_seq* seqs;
+  const adsa_seq* prompts;
+  const int32_t* members;
+  const char* q;
+  const char* k_new;
+  const char* v_new;
+  const int32_t* sel_idx;
+  const int32_t* sel_cnt;
+  char* out;
+  float* lse;
+  float* logits;
+  float* part_ml;
+  float* part_acc;
+  Mods mods;
+  long long slot_stride_b, head_stride_b, prompt_slot_stride_b, prompt_head_stride_b;
+  int n_seq, n_groups, h, G, cap, sel_cap, lg_stride, max_prompt, max_members;
+  int prompt_tiles, prompt_chunks, own_chunks, prompt_blocks;
+  int accumulate, append, advance, new_f32;
+};
+
+// A group's members and its prompt's slots; n < 0: not what they should be.
+struct Group {
+  int first, end, n;
+};
+__device__ __forceinline__ Group group_at(const SharedArgs& A, int g) {
+  Group gr;
+  gr.first = ((const gint*)A.members)[g];
+  gr.end = ((const gint*)A.members)[g + 1];
+  const ADSA_GLOBAL adsa_seq& pr = ((const ADSA_GLOBAL adsa_seq*)A.prompts)[g];
+  gr.n = pr.n_res;
+  if (pr.status != 0 || gr.n < 0 || gr.n > A.max_prompt || gr.first < 0 || gr.end > A.n_seq || gr.end < gr.first || gr.end - gr.first > A.max_members) gr.n = -1;
+  return gr;
+}
+
+template <int EB, int D, int WK, bool MOD>
+__global__ __launch_bounds__(WK * kWave) void k_shared(SharedArgs A) {
+  extern __shared__ __align__(16) char s_lds[];
+  const int hq = A.h * A.G, C = A.prompt_chunks + A.own_chunks;
+  Keys keys;
+  keys.doc = nullptr;
+  keys.logits = nullptr;
+  keys.skip = -1;
+  auto store = [&](auto& t, size_t at, int part) {
+    gfloat* const acc = (gfloat*)A.part_acc + (at * C + part) * D;
+    using T = std::decay_t<decltype(t)>;
+#pragma unroll
+    for (int i = 0; i < T::kMine; i += 4)
+      store4<4>((gchar*)(acc + t.element(i)), t.acc[i / 16][i % 16], t.acc[i / 16][i % 16 + 1], t.acc[i / 16][i % 16 + 2], t.acc[i / 16][i % 16 + 3]);
+    if (t.half == 0 && t.wk == 0) {
+      gfloat* const ml = (gfloat*)A.part_ml + (at * C + part) * 2;
+      ml[0] = t.m;
+      ml[1] = t.l;
+    }
+  };
+  auto nothing = [&](size_t at, int part) {          // (joined with weight 0, its outputs not read)
+    gfloat* const ml = (gfloat*)A.part_ml + (at * C + part) * 2;
+    ml[0] = kLowest;
+    ml[1] = 0.0f;
+  };
+  auto query_pos = [&](int b) {
+    const ADSA_GLOBAL adsa_seq& sq = ((const ADSA_GLOBAL adsa_seq*)A.seqs)[b];
+    return sq.grid_origin + sq.step - 1;
+  };
+  if ((int)blockIdx.x < A.prompt_blocks) {           // a tile of a group's rows over a part of its prompt
+    int unit, tile;
+    pair_of(blockIdx.x, (unsigned)A.prompt_tiles, &unit, &tile);
+    if (unit >= A.n_groups * A.h * A.prompt_chunks) return;
+    const int chunk = unit % A.prompt_chunks, head = unit / A.prompt_chunks % A.h, g = unit / A.prompt_chunks / A.h;
+    const Group gr = group_at(A, g);
+    const int rows = (gr.end - gr.first) * A.G;
+    if (gr.n < 0 || tile * 32 >= rows) return;
+    const ADSA_GLOBAL adsa_seq& pr = ((const ADSA_GLOBAL adsa_seq*)A.prompts)[g];
+    keys.k = (const gchar*)pr.k + head * A.prompt_head_stride_b;
+    keys.v = (const gchar*)pr.v + head * A.prompt_head_stride_b;
+    keys.stride_b = A.prompt_slot_stride_b;
+    keys.list = nullptr;
+    keys.pos = (const gint*)pr.pos;
+    const int per = ((gr.n + A.prompt_chunks - 1) / A.prompt_chunks + 31) / 32 * 32;
+    keys.begin = min(gr.n, chunk * per);
+    keys.end = min(gr.n, keys.begin + per);
+    Tile<EB, D, 1, WK, 32, MOD, false> t(A.mods, keys, (lchar*)s_lds);
+    const int r = tile * 32 + t.col, rr = min(r, rows - 1), b = gr.first + rr / A.G, qh = head * A.G + rr % A.G;
+    const size_t at = (size_t)b * hq + qh;
+    if (keys.begin >= keys.end) {
+      if (threadIdx.x < 32 && r < rows) nothing(at, chunk);
+      return;
+    }
+    t.row = {keys.end, MOD && A.mods.slopes ? query_pos(b) : 0, 0, MOD && A.mods.slopes ? ((const gfloat*)A.mods.slopes)[qh] * kLog2e : 0.0f};
+    t.load_q((const gchar*)A.q + at * (D * EB));
+    t.run();
+    if (r < rows) store(t, at, chunk);
+    return;
+  }
+  // one sequence's own list
+  const int id = (int)blockIdx.x - A.prompt_blocks, chunk = id % A.own_chunks, head = id / A.own_chunks % A.h, b = id / A.own_chunks / A.h;
+  const ADSA_GLOBAL adsa_seq& sq = ((const ADSA_GLOBAL adsa_seq*)A.seqs)[b];
+  if (sq.status != 0 || sq.step < 0) return;
+  const int cnt = min(max(((const gint*)A.sel_cnt)[b], 0), A.sel_cap);
+  keys.k = (const gchar*)sq.k + head * A.head_stride_b;
+  keys.v = (const gchar*)sq.v + head * A.head_stride_b;
+  keys.stride_b = A.slot_stride_b;
+  keys.list = (const gint*)A.sel_idx + (size_t)b * A.sel_cap;
+  keys.pos = (const gint*)sq.pos;
+  keys.last_slot = A.cap - 1;
+  const int pending = A.append ? sq.pending_slot : -1;
+  keys.skip = pending >= 0 && pending < A.cap ? pending : -1;
+  const int per = ((cnt + A.own_chunks - 1) / A.own_chunks + 31) / 32 * 32;
+  keys.begin = min(cnt, chunk * per);
+  keys.end = min(cnt, keys.begin + per);
+  const size_t at0 = (size_t)b * hq + head * A.G;
+  keys.logits = A.accumulate ? (gfloat*)A.logits + at0 * A.lg_stride : nullptr;
+  keys.lg_stride = A.lg_stride;
+  keys.lg_rows = A.G;
+  Tile<EB, D, 1, WK, 32, MOD, true> t(A.mods, keys, (lchar*)s_lds);
+  const size_t at = at0 + min(t.col, A.G - 1);
+  // (a part that holds the query token alone has no other row to stand in for it)
+  if (keys.begin >= keys.end || (keys.end - keys.begin == 1 && keys.list[keys.begin] == keys.skip)) {
+    if ((int)threadIdx.x < A.G) nothing(at, A.prompt_chunks + chunk);
+    return;
+  }
+  const int qh = head * A.G + min(t.col, A.G - 1);
+  t.row = {keys.end, MOD && A.mods.slopes ? query_pos(b) : 0, 0, MOD && A.mods.slopes ? ((const gfloat*)A.mods.slopes)[qh] * kLog2e : 0.0f};
+  t.load_q((const gchar*)A.q + at * (D * EB));
+  t.run();
+  if (t.col < A.G) store(t, at, A.prompt_chunks + chunk);
+}
+
+// Joins the parts of a (sequence, cache head)'s rows with the query token, whose row enters the cache, and updates the scores.
+constexpr int kMaxParts = 2 * kMaxChunks;
+template <int EB, int D>
+__global__ __launch_bounds__(256) void k_shared_finish(SharedArgs A) {
+  __shared__ float s_w[16][kMaxParts + 1], s_l[16][kMaxParts], s_lse[16], s_new[16], s_inv[16];
+  __shared__ int s_has;
+  const int b = blockIdx.x / A.h, head = blockIdx.x % A.h, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int hq = A.h * A.G, C = A.prompt_chunks + A.own_chunks;
+  const size_t at0 = (size_t)b * hq + head * A.G;
+  ADSA_GLOBAL adsa_seq& sq = ((ADSA_GLOBAL adsa_seq*)A.seqs)[b];
+  int lo = 0, hi = A.n_groups;                        // the sequence's group
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (((const gint*)A.members)[mid] <= b) lo = mid; else hi = mid;
+  }
+  const Group gr = group_at(A, lo);
+  const bool fits = gr.n >= 0 && gr.first <= b && b < gr.end, live = sq.status == 0 && sq.step >= 0;
+  if (!live || !fits) {
+    if (live && head == 0 && tid == 0) sq.status = ADSA_SEQ_BAD_STATE;
+    for (int o = tid; o < A.G * D * EB / 4; o += 256) ((gint*)(A.out + at0 * D * EB))[o] = 0;
+    for (int o = tid; o < A.G; o += 256) ((gfloat*)A.lse)[at0 + o] = 0.0f;
+    return;
+  }
+  if (tid == 0) s_has = 0;
+  const int cnt = min(max(((const gint*)A.sel_cnt)[b], 0), A.sel_cap);
+  const gint* const list = (const gint*)A.sel_idx + (size_t)b * A.sel_cap;
+  const int pending = A.append ? sq.pending_slot : -1, new_slot = pending >= 0 && pending < A.cap ? pending : -1;
+  for (int o = tid; o < A.G * C; o += 256) {
+    const int g = o / C, c = o % C;
+    const gfloat* const ml = (const gfloat*)A.part_ml + ((at0 + g) * C + c) * 2;
+    s_w[g][c] = ml[0];
+    s_l[g][c] = ml[1];
+  }
+  // the query token's own row: its score with every query head
+  constexpr int E = D / kWave;
+  float kn[E], vn[E];
+  const size_t row = ((size_t)b * A.h + head) * D;
+  __syncthreads();
+  if (new_slot >= 0) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const size_t o = row + e * kWave + lane;
+      if (EB == 4 || A.new_f32) {
+        kn[e] = ((const gfloat*)A.k_new)[o];
+        vn[e] = ((const gfloat*)A.v_new)[o];
+        if constexpr (EB == 2) {
+          kn[e] = __uint_as_float(f32_to_bf16_rne(kn[e]) << 16);
+          vn[e] = __uint_as_float(f32_to_bf16_rne(vn[e]) << 16);
+        }
+      } else {
+        kn[e] = __uint_as_float((uint32_t)((const ADSA_GLOBAL uint16_t*)A.k_new)[o] << 16);
+        vn[e] = __uint_as_float((uint32_t)((const ADSA_GLOBAL uint16_t*)A.v_new)[o] << 16);
+      }
+      if (wave == 0) {
+        gchar* const kc = (gchar*)sq.k + head * A.head_stride_b + new_slot * A.slot_stride_b;
+        gchar* const vc = (gchar*)sq.v + head * A.head_stride_b + new_slot * A.slot_stride_b;
+        if constexpr (EB == 4) { ((gfloat*)kc)[e * kWave + lane] = kn[e]; ((gfloat*)vc)[e * kWave + lane] = vn[e]; }
+        else {
+          ((ADSA_GLOBAL uint16_t*)kc)[e * kWave + lane] = (uint16_t)(__float_as_uint(kn[e]) >> 16);
+          ((ADSA_GLOBAL uint16_t*)vc)[e * kWave + lane] = (uint16_t)(__float_as_uint(vn[e]) >> 16);
+        }
+      }
+    }
+    for (int j = tid; j < cnt; j += 256)
+      if (list[j] == new_slot) s_has = 1;
+    for (int g = wave; g < A.G; g += 4) {
+      float z = 0.0f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const size_t o = (at0 + g) * D + e * kWave + lane;
+        const float x = EB == 4 ? ((const gfloat*)A.q)[o] : __uint_as_float((uint32_t)((const ADSA_GLOBAL uint16_t*)A.q)[o] << 16);
+        z = fmaf(x, kn[e], z);
+      }
+#pragma unroll
+      for (int x = 1; x < kWave; x <<= 1) z += __shfl_xor(z, x);
+      z = A.mods.cap_out != 0.0f ? capped<EB>(z, A.mods) : z * A.mods.scale_log2;      // (its distance to itself is 0)
+      if (lane == 0) s_new[g] = z;
+    }
+  }
+  __syncthreads();
+  const bool has = new_slot >= 0 && s_has != 0;
+  if (tid < A.G) {
+    float M = has ? s_new[tid] : kLowest, sum;
+    for (int c = 0; c < C; ++c) M = fmaxf(M, s_w[tid][c]);
+    const float pn = has ? fast_exp2(s_new[tid] - M) : 0.0f;
+    sum = pn;
+    for (int c = 0; c < C; ++c) {
+      const float w = s_l[tid][c] == 0.0f ? 0.0f : fast_exp2(s_w[tid][c] - M);
+      s_w[tid][c] = w;
+      sum = fmaf(s_l[tid][c], w, sum);
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    s_w[tid][C] = pn;
+    s_inv[tid] = inv;
+    s_lse[tid] = M + __log2f(sum);
+    ((gfloat*)A.lse)[at0 + tid] = sum == 0.0f ? -INFINITY : s_lse[tid] * kLn2;
+  }
+  __syncthreads();
+  for (int g = wave; g < A.G; g += 4) {
+    float x[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = has ? s_w[g][C] * vn[e] : 0.0f;
+    const gfloat* const acc = (const gfloat*)A.part_acc + (at0 + g) * C * D;
+    for (int c = 0; c < C; ++c) {
+      const float w = s_w[g][c];
+      if (s_l[g][c] == 0.0f) continue;               // (nothing was stored)
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = fmaf(acc[(size_t)c * D + e * kWave + lane], w, x[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const size_t o = (at0 + g) * D + e * kWave + lane;
+      if constexpr (EB == 4) ((gfloat*)A.out)[o] = x[e] * s_inv[g];
+      else ((ADSA_GLOBAL uint16_t*)A.out)[o] = (uint16_t)f32_to_bf16_rne(x[e] * s_inv[g]);
+    }
+  }
+  if (A.accumulate) {
+    gfloat* const score = (gfloat*)sq.score + (size_t)head * A.cap;
+    for (int j = tid; j < cnt; j += 256) {
+      const int slot = min(max(list[j], 0), A.cap - 1);
+      const bool is_new = list[j] == new_slot && new_slot >= 0;
+      float gain = 0.0f;
+      for (int g = 0; g < A.G; ++g) {
+        const float z = is_new ? s_new[g] : ((const gfloat*)A.logits)[(at0 + g) * A.lg_stride + j];
+        gain += fast_exp2(z - s_lse[g]);
+      }
+      score[slot] = score[slot] + gain;
+    }
+  }
+  if (A.advance && head == 0 && tid == 0) sq.step = sq.step + 1;
+}
+
+Mods make_mods(const adsa_params& p, const adsa_mods& m) {
+  const float scale = p.softmax_scale > 0.0f ? p.softmax_scale : 1.0f / sqrtf((float)p.head_dim);
+  Mods o;
+  o.slopes = m.slopes;
+  o.doc = m.doc;
+  o.doc_stride = m.doc_stride;
+  o.cap_in = m.softcap > 0.0f ? scale / m.softcap : 0.0f;
+  o.cap_out = m.softcap > 0.0f ? m.softcap * kLog2e : 0.0f;
+  o.scale_log2 = scale * kLog2e;
+  return o;
+}
+bool modded(const Mods& m) { return m.slopes || m.doc || m.cap_out != 0.0f; }
+
+// Shapes of the launches: many rows, 4 waves of 32 rows each over steps of 64 keys (fp32: 32); few rows, waves that split the keys.
+template <int EB> constexpr int kStepKeys = EB == 2 ? 64 : 32;
+template <int EB, int D> constexpr int kKeyWaves = EB == 4 && D == 128 ? 2 : 4;
+
+template <int EB, int D, bool MOD>
+hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStream_t st) {
+  const unsigned pairs = (unsigned)((A.n_seq * A.h + 7) / 8 * 8);
+  constexpr int KW = kKeyWaves<EB, D>, KT = kStepKeys<EB>;
+  const dim3 grid(pairs * (unsigned)(plan.tiles * plan.chunks));
+  if (plan.few) k_prompt<EB, D, 1, KW, 32, MOD><<<grid, KW * kWave, Shape<EB, D, 1, KW, 32>::kLds, st>>>(A);
+  else k_prompt<EB, D, 4, 1, KT, MOD><<<grid, 4 * kWave, Shape<EB, D, 4, 1, KT>::kLds, st>>>(A);
+  if (plan.chunks > 1) {
+    const size_t rows = (size_t)A.n_tokens * A.h * A.G;
+    k_prompt_finish<EB, D><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, st>>>(A);
+  }
+  if (A.norm) {
+    const int key_tiles = (A.cap + kMassKeys - 1) / kMassKeys;
+    k_prompt_mass<EB, D, MOD><<<dim3(pairs * (unsigned)key_tiles), 256, MassLds<EB, D>::kLds, st>>>(A, key_tiles);
+  }
+  return hipGetLastError();
+}
+
+template <int EB, int D, bool MOD>
+hipError_t shared_launches(const SharedArgs& A, hipStream_t st) {
+  constexpr int KW = kKeyWaves<EB, D>;
+  k_shared<EB, D, KW, MOD><<<dim3((unsigned)(A.prompt_blocks + A.n_seq * A.h * A.own_chunks)), KW * kWave, Shape<EB, D, 1, KW, 32>::kLds, st>>>(A);
+  k_shared_finish<EB, D><<<dim3((unsigned)(A.n_seq * A.h)), 256, 0, st>>>(A);
+  return hipGetLastError();
+}
+
+template <int EB, int D, bool MOD>
+hipError_t allow_lds() {
+  constexpr int KW = kKeyWaves<EB, D>, KT = kStepKeys<EB>;
+  const void* const kernels[] = {(const void*)k_prompt<EB, D, 1, KW, 32, MOD>, (const void*)k_prompt<EB, D, 4, 1, KT, MOD>, (const void*)k_prompt_mass<EB, D, MOD>,
+                                 (const void*)k_shared<EB, D, KW, MOD>};
+  const int bytes[] = {Shape<EB, D, 1, KW, 32>::kLds, Shape<EB, D, 4, 1, KT>::kLds, MassLds<EB, D>::kLds, Shape<EB, D, 1, KW, 32>::kLds};
+  for (int i = 0; i < 4; ++i) {
+    const hipError_t e = hipFuncSetAttribute(kernels[i], hipFuncAttributeMaxDynamicSharedMemorySize, bytes[i]);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <typename F>
+hipError_t by_type(const adsa_params& p, bool mod, F f) {
+  const bool f32 = p.dtype == ADSA_F32, wide = p.head_dim == 128;
+  using std::integral_constant;
+  auto with = [&](auto eb, auto d) { return mod ? f(eb, d, std::true_type()) : f(eb, d, std::false_type()); };
+  if (f32) return wide ? with(integral_constant<int, 4>(), integral_constant<int, 128>()) : with(integral_constant<int, 4>(), integral_constant<int, 64>());
+  return wide ? with(integral_constant<int, 2>(), integral_constant<int, 128>()) : with(integral_constant<int, 2>(), integral_constant<int, 64>());
+}
+
+size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+int query_group(const adsa_params& p) { return p.q_per_kv > 1 ? p.q_per_kv : 1; }
+
+}  // namespace
+
+hipError_t prompt_prepare_kernels() {
+  for (int dtype : {ADSA_F32, ADSA_BF16})
+    for (int d : {64, 128})
+      for (bool mod : {false, true}) {
+        adsa_params p = {};
+        p.dtype = dtype;
+        p.head_dim = d;
+        const hipError_t e = by_type(p, mod, [](auto eb, auto hd, auto m) { return allow_lds<decltype(eb)::value, decltype(hd)::value, decltype(m)::value>(); });
+        if (e != hipSuccess) return e;
+      }
+  return hipSuccess;
+}
+
+PromptPlan make_prompt_plan(const adsa_params& p, const adsa_tokens& t) {
+  const long long rows = (long long)t.max_len * query_group(p), pairs = (long long)p.n_seq * p.n_heads;
+  PromptPlan plan;
+  plan.few = rows <= 32;
+  plan.tiles = (int)((rows + (plan.few ? 31 : 127)) / (plan.few ? 32 : 128));
+  const long long groups = pairs * plan.tiles;
+  plan.chunks = (int)std::clamp<long long>(std::min<long long>((512 + groups - 1) / groups, (p.cap + 255) / 256), 1, kMaxChunks);
+  return plan;
+}
+
+PromptWorkspace make_prompt_workspace(const adsa_params& p, const adsa_tokens& t, const PromptPlan& plan) {
+  const size_t rows = (size_t)t.n_tokens * p.n_heads * query_group(p);
+  PromptWorkspace w;
+  w.part_ml_off = 0;
+  w.part_acc_off = w.part_ml_off + (plan.chunks > 1 ? up256(rows * plan.chunks * 8) : 0);
+  w.norm_off = w.part_acc_off + (plan.chunks > 1 ? up256(rows * plan.chunks * p.head_dim * 4) : 0);
+  w.total = w.norm_off + (p.score_mode == ADSA_SCORE_ATTN_MASS ? up256(rows * 8) : 0);
+  w.total = std::max<size_t>(w.total, 256);
+  return w;
+}
+
+SharedPlan make_shared_plan(const adsa_params& p, const adsa_shared& s) {
+  SharedPlan plan;
+  plan.prompt_tiles = (s.max_members * query_group(p) + 31) / 32;
+  auto parts = [](long long groups, int longest) {
+    return (int)std::clamp<long long>(std::min<long long>((512 + groups - 1) / groups, (longest + 127) / 128), 1, kMaxChunks);
+  };
+  plan.prompt_chunks = parts((long long)s.n_groups * p.n_heads * plan.prompt_tiles, s.max_prompt);
+  plan.own_chunks = parts((long long)p.n_seq * p.n_heads, p.sel_cap);
+  return plan;
+}
+
+SharedWorkspace make_shared_workspace(const adsa_params& p, const SharedPlan& plan) {
+  const size_t rows = (size_t)p.n_seq * p.n_heads * query_group(p), parts = (size_t)(plan.prompt_chunks + plan.own_chunks);
+  SharedWorkspace w;
+  w.lg_stride = (p.sel_cap + 3) / 4 * 4;
+  w.logits_off = 0;
+  w.part_ml_off = up256(rows * w.lg_stride * 4);
+  w.part_acc_off = w.part_ml_off + up256(rows * parts * 8);
+  w.total = w.part_acc_off + up256(rows * parts * p.head_dim * 4);
+  return w;
+}
+
+hipError_t launch_prefill(const adsa_params& p, const adsa_tokens& t, const adsa_mods& mods, const PromptPlan& plan, adsa_seq* seqs, const void* q, void* out,
+                          float* lse, char* ws, const PromptWorkspace& w, bool accumulate, bool advance, hipStream_t st) {
+  PromptArgs A = {};
+  A.seqs = seqs; A.begin = t.begin; A.slot0 = t.slot0; A.q = (const char*)q; A.out = (char*)out; A.lse = lse;
+  A.part_ml = (float*)(ws + w.part_ml_off);
+  A.part_acc = (float*)(ws + w.part_acc_off);
+  A.norm = accumulate ? (float*)(ws + w.norm_off) : nullptr;
+  A.mods = make_mods(p, mods);
+  A.slot_stride_b = p.kv_slot_stride * elem_bytes(p);
+  A.head_stride_b = p.kv_head_stride * elem_bytes(p);
+  A.n_seq = p.n_seq; A.n_tokens = t.n_tokens; A.max_len = t.max_len; A.h = p.n_heads; A.G = query_group(p); A.cap = p.cap; A.mask = mods.mask;
+  A.tiles = plan.tiles; A.chunks = plan.chunks; A.advance = advance ? 1 : 0;
+  return by_type(p, modded(A.mods), [&](auto eb, auto d, auto m) {
+    return prompt_launches<decltype(eb)::value, decltype(d)::value, decltype(m)::value>(A, plan, st);
+  });
+}
+
+hipError_t launch_attend_shared(const adsa_params& p, const adsa_shared& s, const adsa_mods& mods, const SharedPlan& plan, adsa_seq* seqs, const void* q,
+                                const void* k_new, const void* v_new, const int32_t* sel_idx, const int32_t* sel_cnt, void* out, float* lse, char* ws,
+                                const SharedWorkspace& w, bool accumulate, bool append, bool advance, bool new_f32, hipStream_t st) {
+  SharedArgs A = {};
+  A.seqs = seqs; A.prompts = s.prompts; A.members = s.members; A.q = (const char*)q; A.k_new = (const char*)k_new; A.v_new = (const char*)v_new;
+  A.sel_idx = sel_idx; A.sel_cnt = sel_cnt; A.out = (char*)out; A.lse = lse;
+  A.logits = (float*)(ws + w.logits_off);
+  A.part_ml = (float*)(ws + w.part_ml_off);
+  A.part_acc = (float*)(ws + w.part_acc_off);
+  A.mods = make_mods(p, mods);
+  A.mods.doc = nullptr;
+  const int eb = elem_bytes(p);
+  A.slot_stride_b = p.kv_slot_stride * eb; A.head_stride_b = p.kv_head_stride * eb;
+  A.prompt_slot_stride_b = s.kv_slot_stride * eb; A.prompt_head_stride_b = s.kv_head_stride * eb;
+  A.n_seq = p.n_seq; A.n_groups = s.n_groups; A.h = p.n_heads; A.G = query_group(p); A.cap = p.cap; A.sel_cap = p.sel_cap; A.lg_stride = w.lg_stride;
+  A.max_prompt = s.max_prompt; A.max_members = s.max_members;
+  A.prompt_tiles = plan.prompt_tiles; A.prompt_chunks = plan.prompt_chunks; A.own_chunks = plan.own_chunks;
+  A.prompt_blocks = (s.n_groups * p.n_heads * plan.prompt_chunks + 7) / 8 * 8 * plan.prompt_tiles;
+  A.accumulate = accumulate; A.append = append; A.advance = advance; A.new_f32 = new_f32;
+  return by_type(p, modded(A.mods), [&](auto eb_, auto d, auto m) {
+    return shared_launches<decltype(eb_)::value, decltype(d)::value, decltype(m)::value>(A, st);
+  });
+}
+
+}  // namespace adsa
