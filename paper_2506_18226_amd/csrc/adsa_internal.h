@@ -131,7 +131,8 @@ static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t
 
 // ---- prompts (prompt_api.hip checks and plans, rotary.hip and prompt.hip launch)
 struct PromptPlan {
-  bool few;             // a workgroup's waves share up to 32 rows and split the keys (else 32 rows each, all keys)
+  int rows;             // of a workgroup: 32 (its waves split the keys), 128 or 256 (32 or 64 for each of 4 waves)
+  bool flow;            // k_prompt_many (else k_prompt)
   int tiles;            // row tiles per (sequence, cache head)
   int chunks;           // parts the keys are split into
 };

@@ -15,6 +15,7 @@
 // product in the cache's type: for bf16 that rounds each probability by 2^-9 at most, as much as the output's own rounding.
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "adsa_device.h"
 
@@ -30,6 +31,12 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 #define ADSA_LDS __attribute__((address_space(3)))
 typedef ADSA_LDS char lchar;
+
+// f(0) .. f(N - 1), each a constant of the program
+template <typename F, int... I>
+__device__ __forceinline__ void each(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>()), ...); }
+template <int N, typename F>
+__device__ __forceinline__ void each(F f) { each(f, std::make_integer_sequence<int, N>()); }
 
 // What is done to scores before the softmax.
 struct Mods {
@@ -333,7 +340,7 @@ struct Tile {
 #pragma unroll
     for (int u = 0; u < SUB; ++u)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) mx = max2(mx, s[u][i]);
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[u][i]);           // (no asm here: a product's result takes wait states that the compiler counts)
     mx = xor_max<32>(mx) * scale;
     if (__ballot(mx > m) != 0) {                     // some row's maximum rose: bring every row's state to its new one
       const float m_new = max2(m, mx), corr = fast_exp2(m - m_new);
@@ -441,6 +448,379 @@ __device__ __forceinline__ void store4(gchar* p, float a, float b, float c, floa
   else *(ADSA_GLOBAL u32x2*)p = u32x2{pack2_bf16(a, b), pack2_bf16(c, d)};
 }
 
+// Many rows of a bf16 prompt: 4 waves of NB blocks of 32 rows each, keys in steps of 32, two steps to a tile of K and V in LDS.
+//
+// What bounds it: a block's step is D / 4 cycles of its SIMD's matrix core per key (2 x D / 16 products of 32x32x16), and about 470 cycles of vector
+// work (16 exponentials at a quarter of the rate, their arguments, sums, maxima, conversions), so neither may wait for the other.  Besides,
+// every step fetches K and V out of LDS, for 32 rows as many bytes as the LDS has cycles for: two blocks a wave (NB = 2) share a fetch.
+// So a wave takes whatever is independent at one time: the scores of step j + 1 and the outputs of step j - 1 on the matrix core, the softmax of
+// step j on the vector unit, laid out alternately by hand (one product of each block, then its share of the vector work), since the
+// compiler left alone puts all of one kind before the other.
+// A row's maximum is followed only when it has grown by more than 2^8: P stays below 2^8, and outputs are rescaled next to never.
+template <int D, int NB, bool MOD>
+struct Flow {
+  using L = Layout<2, D>;
+  static constexpr int CPR = L::CPR, RB = L::RB, DT = D / 32, KC = D / 16, VC = DT * 2, NC = KC + VC;
+  static constexpr int kThreads = 4 * kWave, kRows = 4 * NB * 32, TK = 64;
+  static constexpr int RPT = kThreads / CPR, NL = TK / RPT;
+  static constexpr int kV = 2 * TK * RB, kMeta = 2 * kV, kLds = kMeta + (MOD ? 3 * 2 * TK * 4 : 0);      // two tiles of K, of V; positions and documents of three
+  static constexpr float kGrowth = 8.0f;
+
+  const Mods& mods;
+  const Keys& keys;
+  lchar* const lds;
+  const int tid, lane, col, half, wave;
+  uint4 qf[NB][KC];
+  Row row[NB];
+  f32x16 acc[NB][DT], s[NB];
+  uint32_t p[NB][8];           // probabilities of the step before, two to a word
+  float m[NB], l[NB];
+  uint4 kr[NL], vr[NL];
+  int meta_pos, meta_doc;
+  // LDS offsets: the lane's pieces of the tile of K and of V that are read, the thread's of those that are written.  Each changes buffers
+  // with every tile (K's two lie TK * RB apart, an offset's bit of that value says which; so do V's).
+  int k_at[KC], v_at[DT], k_to, v_to;
+  uint32_t row_at[NL];         // offsets of the thread's rows of a tile from its first
+
+  __device__ __forceinline__ Flow(const Mods& mods_, const Keys& keys_, lchar* lds_)
+      : mods(mods_), keys(keys_), lds(lds_), tid(threadIdx.x), lane(threadIdx.x % kWave), col(lane % 32), half(lane / 32),
+        wave(__builtin_amdgcn_readfirstlane(tid / kWave)) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) row_at[i] = (uint32_t)((tid / CPR + i * RPT) * (int)keys.stride_b + (tid % CPR) * 16);
+#pragma unroll
+    for (int c = 0; c < KC; ++c) k_at[c] = col * RB + (((2 * c + half) ^ L::swz_k(col)) << 4);
+    const int vrow = half * 4 + (lane % 16) / 4, vcol = ((lane / 16) & 1) * 16 + (lane % 4) * 4;       // (see Tile::add_values)
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) v_at[dt] = kV + TK * RB + vrow * RB + (vcol % 8) * 2 + (((dt * 4 + vcol / 8) ^ L::swz_v(vrow)) << 4);
+    const int r = tid / CPR;                         // (rows RPT further on are permuted alike)
+    static_assert(RPT % 16 == 0, "swizzles repeat");
+    k_to = r * RB + (((tid % CPR) ^ L::swz_k(r)) << 4);
+    v_to = kV + r * RB + (((tid % CPR) ^ L::swz_v(r)) << 4);
+  }
+  __device__ __forceinline__ void change_buffers() {
+#pragma unroll
+    for (int c = 0; c < KC; ++c) k_at[c] ^= TK * RB;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) v_at[dt] ^= TK * RB;
+    k_to ^= TK * RB;
+    v_to ^= TK * RB;
+  }
+  __device__ __forceinline__ void load_q(int b, const gchar* q_row) {
+#pragma unroll
+    for (int c = 0; c < KC; ++c) qf[b][c] = load16(q_row + (2 * c + half) * 16);
+  }
+
+  // rows of a tile on their way: 32-bit offsets from the tile's first row, which hold for every tile but a last, shorter one
+  __device__ __forceinline__ void load_tile(const gchar* from, int base, uint4 (&r)[NL]) {
+    const gchar* const first = from + (long long)base * keys.stride_b;
+    const int last = keys.end - 1 - base;
+    if (last >= TK - 1) {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) r[i] = load16(first + row_at[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) r[i] = load16(first + (uint32_t)(min(tid / CPR + i * RPT, last) * (int)keys.stride_b + (tid % CPR) * 16));
+    }
+  }
+  __device__ __forceinline__ void store_k(int third) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) put16(lds + k_to + i * RPT * RB, kr[i]);
+    if constexpr (MOD)
+      if (tid < TK) {
+        ADSA_LDS int* const meta = (ADSA_LDS int*)(lds + kMeta) + third * 2 * TK;
+        meta[tid] = meta_pos;
+        meta[TK + tid] = meta_doc;
+      }
+  }
+  __device__ __forceinline__ void store_v() {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) put16(lds + v_to + i * RPT * RB, vr[i]);
+  }
+  __device__ __forceinline__ void load_meta(int base) {
+    if constexpr (MOD)
+      if (tid < TK) {
+        const int slot = min(base + tid, keys.end - 1);
+        meta_pos = mods.slopes ? __float_as_int((float)keys.pos[slot]) : 0;
+        meta_doc = keys.doc ? keys.doc[slot] : 0;
+      }
+  }
+
+  __device__ __forceinline__ uint4 k_piece(int sub, int c) const { return lds16(lds + k_at[c] + sub * 32 * RB); }
+  __device__ __forceinline__ u32x4 v_piece(int sub, int i) const {
+    const lchar* const at = lds + v_at[i / 2] + (sub * 32 + 16 * (i % 2)) * RB;
+    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ADSA_LDS i16x4*)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ADSA_LDS i16x4*)(at + 8 * RB));
+    const u32x2 a = __builtin_bit_cast(u32x2, lo), b = __builtin_bit_cast(u32x2, hi);
+    return u32x4{a.x, a.y, b.x, b.y};
+  }
+  __device__ __forceinline__ bf16x8 p_piece(int b, int t) const { return __builtin_bit_cast(bf16x8, u32x4{p[b][4 * t], p[b][4 * t + 1], p[b][4 * t + 2], p[b][4 * t + 3]}); }
+
+  // Infinities and NaN among V's rows of a step whose keys not every row sees (rare): they must not reach rows that do not see them.
+  __device__ __forceinline__ bool values_bad(int sub) const {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 32 * CPR / kWave; ++i) {
+      const uint4 w = lds16(lds + kV + (v_at[0] & (TK * RB)) + sub * 32 * RB + (i * kWave + lane) * 16);
+      bad |= bf16_bad(w.x) || bf16_bad(w.y) || bf16_bad(w.z) || bf16_bad(w.w);
+    }
+    return __ballot(bad) != 0;
+  }
+  // ... and what those give the rows that see their key: where V holds +infinity (and where -infinity, NaN counting as both) the
+  // product of ones there with ones for p > 0 says which rows have one among their keys.
+  static __device__ __forceinline__ uint32_t ones_at(uint32_t w, bool negative) {
+    auto hit = [&](uint32_t h) { return (h & 0x7FFFu) > 0x7F80u || h == (negative ? 0xFF80u : 0x7F80u); };
+    return (hit(w & 0xFFFFu) ? 0x3F80u : 0u) | (hit(w >> 16) ? 0x3F800000u : 0u);
+  }
+  __device__ __forceinline__ void add_bad_values(int sub) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int negative = 0; negative < 2; ++negative) {
+          f32x16 r = {};
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const u32x4 w = v_piece(sub, dt * 2 + t);
+            u32x4 x = {p[b][4 * t], p[b][4 * t + 1], p[b][4 * t + 2], p[b][4 * t + 3]};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = ((x[i] & 0xFFFFu) ? 0x3F80u : 0u) | ((x[i] >> 16) ? 0x3F800000u : 0u);
+            const u32x4 o = {ones_at(w.x, negative), ones_at(w.y, negative), ones_at(w.z, negative), ones_at(w.w, negative)};
+            r = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, o), __builtin_bit_cast(bf16x8, x), r, 0, 0, 0);
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[b][dt][i] += r[i] > 0.0f ? (negative ? -INFINITY : INFINITY) : 0.0f;
+        }
+  }
+
+  // pieces of the two steps' work
+  __device__ __forceinline__ void bend(int b, int i, const ADSA_LDS int* meta) {           // cap and distance of one score
+    float z = mods.cap_out != 0.0f ? capped<2>(s[b][i], mods) : s[b][i] * mods.scale_log2;
+    if (mods.slopes) z = fmaf(-row[b].slope, fabsf((float)row[b].pos - __int_as_float(meta[(i / 4) * 8 + half * 4 + i % 4])), z);
+    s[b][i] = z;
+  }
+  __device__ __forceinline__ float score_scale() const { return MOD ? 1.0f : mods.scale_log2; }
+  // The step's maximum of block b's rows; where it has grown, what the state so far has to be multiplied by.
+  __device__ __forceinline__ bool maximum(int b, float* corr) {
+    float mx = s[b][0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[b][i]);            // (no asm here: a product's result takes wait states that the compiler counts)
+    mx = xor_max<32>(mx) * score_scale();
+    const bool grows = mx > m[b] + kGrowth;
+    const float m_new = grows ? mx : m[b];
+    *corr = fast_exp2(m[b] - m_new);
+    m[b] = m_new;
+    return grows;
+  }
+  __device__ __forceinline__ uint32_t two_probabilities(int b, int i, float* sum) {
+    const float a = fast_exp2(fmaf(s[b][i], score_scale(), -m[b])), d = fast_exp2(fmaf(s[b][i + 1], score_scale(), -m[b]));
+    *sum += a;
+    *sum += d;
+    return pack2_bf16(a, d);
+  }
+  __device__ __forceinline__ void rescale(const float (&corr)[NB]) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      l[b] *= corr[b];
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[b][dt][i] *= corr[b];
+    }
+  }
+
+  // One step of keys that every row sees: the scores of K's rows (half SUB of the tile), the softmax of the scores s of the step
+  // before, the outputs of its predecessor's p with V's rows, alternately.
+  template <int SUB>
+  __device__ __forceinline__ void step(const ADSA_LDS int* meta) {
+    f32x16 next[NB];
+    uint32_t pn[NB][8];
+    float corr[NB], sum[NB];
+    bool grown = false;
+    constexpr int kAhead = 2;                        // pieces fetched ahead of their product
+    constexpr int kMax = MOD ? NC / 2 : 1;           // the maxima stand before this chunk's probabilities
+    constexpr int kE = NB * 16;                      // scores of a lane
+    uint4 kp[KC];
+    u32x4 vp[VC];
+    auto fetch = [&](auto at) {
+      constexpr int c = decltype(at)::value;
+      if constexpr (c < KC) kp[c] = k_piece(SUB, c);
+      else if constexpr (c < NC) vp[c - KC] = v_piece(SUB, c - KC);
+    };
+    each<kAhead>(fetch);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) sum[b] = 0.0f;
+    each<NC>([&](auto at) {
+      constexpr int c = decltype(at)::value;
+      fetch(std::integral_constant<int, c + kAhead>());
+      if constexpr (c < KC) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+          next[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kp[c]), __builtin_bit_cast(bf16x8, qf[b][c]), c == 0 ? f32x16{} : next[b], 0, 0, 0);
+      } else {
+        constexpr int i = c - KC;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+          acc[b][i / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vp[i]), p_piece(b, i % 2), acc[b][i / 2], 0, 0, 0);
+      }
+      if constexpr (MOD && c < kMax) {
+        constexpr int e0 = kE * c / kMax;
+        each<kE * (c + 1) / kMax - e0>([&](auto o) {
+          constexpr int e = e0 + decltype(o)::value;
+          bend(e / 16, e % 16, meta);
+        });
+      }
+      if constexpr (c == kMax) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) grown |= maximum(b, &corr[b]);
+      }
+      if constexpr (c >= kMax) {                     // this chunk's share of the probabilities
+        constexpr int kRest = NC - kMax, e0 = kE / 2 * (c - kMax) / kRest;
+        each<kE / 2 * (c + 1 - kMax) / kRest - e0>([&](auto o) {
+          constexpr int e = 2 * (e0 + decltype(o)::value);
+          pn[e / 16][e % 16 / 2] = two_probabilities(e / 16, e % 16, &sum[e / 16]);
+          asm volatile("" : "+v"(pn[e / 16][e % 16 / 2]), "+v"(sum[e / 16]));      // (here, not where p is used)
+        });
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if (__ballot(grown) != 0) rescale(corr);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      l[b] += sum[b];
+      s[b] = next[b];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[b][i] = pn[b][i];
+    }
+  }
+
+  // The same one after the other: first and last steps (which lack a part), and keys that not every row sees.
+  __device__ __forceinline__ void outputs(int sub, bool masked) {
+    const bool tidy = masked && values_bad(sub);
+    if (tidy) add_bad_values(sub);
+#pragma unroll
+    for (int i = 0; i < VC; ++i) {
+      u32x4 w = v_piece(sub, i);
+      if (tidy) w = u32x4{bf16_finite(w.x), bf16_finite(w.y), bf16_finite(w.z), bf16_finite(w.w)};
+#pragma unroll
+      for (int b = 0; b < NB; ++b) acc[b][i / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), p_piece(b, i % 2), acc[b][i / 2], 0, 0, 0);
+    }
+  }
+  __device__ __forceinline__ void scores(int sub) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) s[b] = f32x16{};
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      const uint4 k = k_piece(sub, c);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[b][c]), s[b], 0, 0, 0);
+    }
+  }
+  __device__ __forceinline__ void softmax(int base, const ADSA_LDS int* meta, bool masked) {
+    float corr[NB];
+    bool grown = false;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      if constexpr (MOD) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) bend(b, i, meta);
+      }
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int k = (i / 4) * 8 + half * 4 + i % 4;
+          bool seen = base + k < row[b].limit;
+          if constexpr (MOD)
+            if (keys.doc) seen &= meta[TK + k] == row[b].doc;
+          s[b][i] = seen ? s[b][i] : -INFINITY;
+        }
+      }
+      grown |= maximum(b, &corr[b]);
+    }
+    if (__ballot(grown) != 0) rescale(corr);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) p[b][i / 2] = two_probabilities(b, i, &sum);
+      l[b] += sum;
+    }
+  }
+
+  int lo, hi;                  // keys that all rows of the wave see, and from which on none does
+  __device__ __forceinline__ bool masked_at(int first) const {
+    bool x = first + 32 > lo;
+    if constexpr (MOD) x |= keys.doc != nullptr;
+    return x;
+  }
+  // Tile number t (of `mine` that this wave's rows see): the scores of steps 2t and 2t + 1, the softmax of 2t - 1 and 2t, the outputs of 2t - 2
+  // and 2t - 1; so K's tile t and V's tile t - 1 are read.
+  __device__ __forceinline__ const ADSA_LDS int* meta_of(int t) const { return (const ADSA_LDS int*)(lds + kMeta) + t % 3 * 2 * TK; }
+  __device__ __forceinline__ void tile(int t, int mine) {
+    if (t > mine || mine == 0) return;
+    const int base = keys.begin + t * TK;
+    for (int sub = 0; sub < 2; ++sub) {
+      if (t > 0) {
+        outputs(sub, masked_at(base - 64 + 32 * sub));
+        if (sub == 0) softmax(base - 32, meta_of(t + 2) + 32, masked_at(base - 32));
+      }
+      if (t < mine) {
+        if (sub == 1) softmax(base, meta_of(t), masked_at(base));
+        scores(sub);
+      }
+    }
+  }
+  __device__ __forceinline__ void run() {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      m[b] = kLowest;
+      l[b] = 0.0f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) acc[b][dt] = f32x16{};
+    }
+    if (keys.begin >= keys.end) return;              // (a part without keys: there is no row to load)
+    lo = hi = row[0].limit;
+#pragma unroll
+    for (int b = 1; b < NB; ++b) { lo = min(lo, row[b].limit); hi = max(hi, row[b].limit); }
+#pragma unroll
+    for (int x = 1; x < 32; x <<= 1) { lo = min(lo, __shfl_xor(lo, x)); hi = max(hi, __shfl_xor(hi, x)); }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
+    const int tiles = (keys.end - keys.begin + TK - 1) / TK, mine = max(0, (min(hi, keys.end) - keys.begin + TK - 1) / TK);
+    // tiles 1 .. open - 1 have no key that some row does not see
+    const int open = MOD && keys.doc ? 1 : min(mine, max(0, lo - 32 - keys.begin) / TK + 1);
+    load_tile(keys.k, keys.begin, kr);
+    load_meta(keys.begin);
+    store_k(0);
+    k_to ^= TK * RB;
+    __syncthreads();
+    load_tile(keys.v, keys.begin, vr);
+    if (tiles > 1) { load_tile(keys.k, keys.begin + TK, kr); load_meta(keys.begin + TK); }
+    // Between two barriers, tile t's K and tile t - 1's V are read, and tile t + 1's K and tile t's V written, into the other buffers.
+    auto next_tile = [&](int t) {
+      if (t + 1 < tiles) store_k((t + 1) % 3);
+      store_v();
+      __syncthreads();
+      change_buffers();
+      if (t + 2 < tiles) { load_tile(keys.k, keys.begin + (t + 2) * TK, kr); load_meta(keys.begin + (t + 2) * TK); }
+      if (t + 1 < tiles) load_tile(keys.v, keys.begin + (t + 1) * TK, vr);
+    };
+    tile(0, mine);
+    next_tile(0);
+    int t = 1;
+    for (; t < open; ++t) {
+      step<0>(meta_of(t + 2) + 32);
+      step<1>(meta_of(t));
+      next_tile(t);
+    }
+    for (; t <= tiles; ++t) {
+      tile(t, mine);
+      if (t < tiles) next_tile(t);
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) l[b] = xor_sum<32>(l[b]);
+  }
+};
+
 // ---------------------------------------------------------------------------------------------------- prompts
 struct PromptArgs {
   adsa_seq* seqs;
@@ -487,89 +867,153 @@ __device__ __forceinline__ void pair_of(unsigned id, unsigned units, int* pair, 
   *unit = (int)(y % units);
 }
 
+// What a workgroup of k_prompt / k_prompt_many is to do; false: nothing (left).
+struct Job {
+  Prompt pr;
+  Keys keys;
+  int b, head, chunk, row0, rows;
+};
+template <int EB, int D, int ROWS, int THREADS>
+__device__ __forceinline__ bool job_of(const PromptArgs& A, Job& J) {
+  int pair, unit;
+  pair_of(blockIdx.x, (unsigned)(A.tiles * A.chunks), &pair, &unit);
+  if (pair >= A.n_seq * A.h) return false;
+  J.b = pair / A.h;
+  J.head = pair % A.h;
+  J.chunk = unit % A.chunks;
+  const int tile = A.tiles - 1 - unit / A.chunks, tid = threadIdx.x, hq = A.h * A.G;       // (the longest rows first)
+  ADSA_GLOBAL adsa_seq& sq = ((ADSA_GLOBAL adsa_seq*)A.seqs)[J.b];
+  J.pr = prompt_of(A, J.b);
+  if (J.pr.status != 0) {                            // zeros, by the workgroups of the sequence together
+    if (J.chunk != 0) return false;
+    if (J.head == 0 && tile == 0 && tid == 0 && sq.status == 0) sq.status = J.pr.status;
+    for (long long r = tile; r < J.pr.len; r += A.tiles) {
+      const size_t at = ((size_t)(J.pr.from + r) * hq + J.head * A.G);
+      for (int o = tid; o < A.G * D * EB / 4; o += THREADS) ((gint*)(A.out + at * D * EB))[o] = 0;
+      for (int o = tid; o < A.G; o += THREADS) ((gfloat*)A.lse)[at + o] = 0.0f;
+    }
+    return false;
+  }
+  J.rows = J.pr.len * A.G;
+  J.row0 = tile * ROWS;
+  if (J.row0 >= J.rows) return false;
+  if (A.advance && J.head == 0 && tile == 0 && J.chunk == 0 && tid == 0) sq.step = sq.step + 1;
+  Keys& keys = J.keys;
+  keys.k = (const gchar*)sq.k + J.head * A.head_stride_b;
+  keys.v = (const gchar*)sq.v + J.head * A.head_stride_b;
+  keys.stride_b = A.slot_stride_b;
+  keys.list = nullptr;
+  keys.pos = (const gint*)sq.pos;
+  keys.doc = A.mods.doc ? (const gint*)A.mods.doc + J.b * A.mods.doc_stride : nullptr;
+  keys.logits = nullptr;
+  keys.skip = -1;
+  // what the tile's last row sees (a row of the prefix may see more than later rows)
+  const int end = min(J.row0 + ROWS, J.rows), last_slot = J.pr.slot0 + (end + A.G - 1) / A.G - 1, first_slot = J.pr.slot0 + J.row0 / A.G;
+  const int n = max(limit_of(J.pr, last_slot), limit_of(J.pr, first_slot));
+  const int per = A.chunks == 1 ? n : ((n + A.chunks - 1) / A.chunks + 31) / 32 * 32;
+  keys.begin = min(n, J.chunk * per);
+  keys.end = min(n, keys.begin + per);
+  return true;
+}
+// Row number r of the job (past the last one: that one again): its place among the packed rows, and what it sees.
+template <bool MOD>
+__device__ __forceinline__ size_t row_of(const PromptArgs& A, const Job& J, int r, Row& row) {
+  const int rr = min(r, J.rows - 1), token = rr / A.G, qh = J.head * A.G + rr % A.G, slot = J.pr.slot0 + token;
+  row.limit = min(limit_of(J.pr, slot), J.keys.end);   // (a step past the end of a part repeats its last key)
+  row.pos = 0;
+  row.doc = 0;
+  row.slope = 0.0f;
+  if constexpr (MOD) {
+    if (A.mods.slopes) { row.pos = J.keys.pos[slot]; row.slope = ((const gfloat*)A.mods.slopes)[qh] * kLog2e; }
+    if (J.keys.doc) {
+      row.doc = J.keys.doc[slot];
+      if (row.doc < 0) row.limit = 0;
+    }
+  }
+  return (size_t)(J.pr.from + token) * (A.h * A.G) + qh;
+}
+__device__ __forceinline__ void store_part(const PromptArgs& A, const Job& J, size_t at, float m, float l) {
+  gfloat* const ml = (gfloat*)A.part_ml + (at * A.chunks + J.chunk) * 2;
+  ml[0] = m;
+  ml[1] = l;
+}
+__device__ __forceinline__ float inverse(float l) { return l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l; }       // (a NaN stays one)
+__device__ __forceinline__ void store_lse(const PromptArgs& A, size_t at, float m, float l) {
+  ((gfloat*)A.lse)[at] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
+  if (A.norm) { ((gfloat*)A.norm)[2 * at] = m; ((gfloat*)A.norm)[2 * at + 1] = inverse(l); }
+}
+
 template <int EB, int D, int WR, int WK, int KT, bool MOD>
 __global__ __launch_bounds__(WR * WK * kWave) void k_prompt(PromptArgs A) {
   using T = Tile<EB, D, WR, WK, KT, MOD, false>;
   using S = typename T::S;
   extern __shared__ __align__(16) char s_lds[];
-  int pair, unit;
-  pair_of(blockIdx.x, (unsigned)(A.tiles * A.chunks), &pair, &unit);
-  if (pair >= A.n_seq * A.h) return;
-  const int b = pair / A.h, head = pair % A.h, chunk = unit % A.chunks, tile = A.tiles - 1 - unit / A.chunks;     // (the longest rows first)
-  const int tid = threadIdx.x, hq = A.h * A.G;
-  ADSA_GLOBAL adsa_seq& sq = ((ADSA_GLOBAL adsa_seq*)A.seqs)[b];
-  const Prompt pr = prompt_of(A, b);
-  if (pr.status != 0) {                              // zeros, by the workgroups of the sequence together
-    if (chunk != 0) return;
-    if (head == 0 && tile == 0 && tid == 0 && sq.status == 0) sq.status = pr.status;
-    for (long long r = tile; r < pr.len; r += A.tiles) {
-      const size_t at = ((size_t)(pr.from + r) * hq + head * A.G);
-      for (int o = tid; o < A.G * D * EB / 4; o += S::kThreads) ((gint*)(A.out + at * D * EB))[o] = 0;
-      for (int o = tid; o < A.G; o += S::kThreads) ((gfloat*)A.lse)[at + o] = 0.0f;
-    }
-    return;
-  }
-  const int rows = pr.len * A.G, row0 = tile * S::kRows;
-  if (row0 >= rows) return;
-  if (A.advance && head == 0 && tile == 0 && chunk == 0 && tid == 0) sq.step = sq.step + 1;
-
-  Keys keys;
-  keys.k = (const gchar*)sq.k + head * A.head_stride_b;
-  keys.v = (const gchar*)sq.v + head * A.head_stride_b;
-  keys.stride_b = A.slot_stride_b;
-  keys.list = nullptr;
-  keys.pos = (const gint*)sq.pos;
-  keys.doc = A.mods.doc ? (const gint*)A.mods.doc + b * A.mods.doc_stride : nullptr;
-  keys.logits = nullptr;
-  keys.skip = -1;
-  // what the tile's last row sees (a row of the prefix may see more than later rows)
-  const int last_slot = pr.slot0 + min(row0 + S::kRows, rows) / A.G - 1 + (min(row0 + S::kRows, rows) % A.G != 0 ? 1 : 0);
-  const int first_slot = pr.slot0 + row0 / A.G;
-  const int n = max(limit_of(pr, last_slot), limit_of(pr, first_slot));
-  const int per = A.chunks == 1 ? n : ((n + A.chunks - 1) / A.chunks + 31) / 32 * 32;
-  keys.begin = min(n, chunk * per);
-  keys.end = min(n, keys.begin + per);
-
-  T t(A.mods, keys, (lchar*)s_lds);
-  const int r = row0 + t.wr * 32 + t.col;            // the lane's row; past the last one: that one again, not stored
-  const bool valid = r < rows;
-  const int rr = min(r, rows - 1), token = rr / A.G, qh = head * A.G + rr % A.G, slot = pr.slot0 + token;
-  const size_t at = (size_t)(pr.from + token) * hq + qh;
-  t.row.limit = min(limit_of(pr, slot), keys.end);   // (a step past the end of a part repeats its last key)
-  t.row.pos = 0;
-  t.row.doc = 0;
-  t.row.slope = 0.0f;
-  if constexpr (MOD) {
-    if (A.mods.slopes) { t.row.pos = keys.pos[slot]; t.row.slope = ((const gfloat*)A.mods.slopes)[qh] * kLog2e; }
-    if (keys.doc) {
-      t.row.doc = keys.doc[slot];
-      if (t.row.doc < 0) t.row.limit = 0;
-    }
-  }
+  Job J;
+  if (!job_of<EB, D, S::kRows, S::kThreads>(A, J)) return;
+  T t(A.mods, J.keys, (lchar*)s_lds);
+  const int r = J.row0 + t.wr * 32 + t.col;
+  const size_t at = row_of<MOD>(A, J, r, t.row);
   t.load_q((const gchar*)A.q + at * (D * EB));
   t.run();
-  if (!valid) return;
-  if (A.chunks > 1) {
-    gfloat* const acc = (gfloat*)A.part_acc + (at * A.chunks + chunk) * D;
-#pragma unroll
-    for (int i = 0; i < T::kMine; i += 4)
-      store4<4>((gchar*)(acc + t.element(i)), t.acc[i / 16][i % 16], t.acc[i / 16][i % 16 + 1], t.acc[i / 16][i % 16 + 2], t.acc[i / 16][i % 16 + 3]);
-    if (t.half == 0 && t.wk == 0) {
-      gfloat* const ml = (gfloat*)A.part_ml + (at * A.chunks + chunk) * 2;
-      ml[0] = t.m;
-      ml[1] = t.l;
-    }
-    return;
-  }
-  const float inv = t.l > 0.0f ? 1.0f / t.l : t.l == 0.0f ? 0.0f : t.l;       // (a NaN stays one)
+  if (r >= J.rows) return;
+  const bool parts = A.chunks > 1;
+  const float inv = parts ? 1.0f : inverse(t.l);
+  gfloat* const acc = (gfloat*)A.part_acc + (at * A.chunks + J.chunk) * D;
   gchar* const out = (gchar*)A.out + at * (D * EB);
 #pragma unroll
-  for (int i = 0; i < T::kMine; i += 4)
-    store4<EB>(out + t.element(i) * EB, t.acc[i / 16][i % 16] * inv, t.acc[i / 16][i % 16 + 1] * inv, t.acc[i / 16][i % 16 + 2] * inv,
-               t.acc[i / 16][i % 16 + 3] * inv);
+  for (int i = 0; i < T::kMine; i += 4) {
+    const f32x16& x = t.acc[i / 16];
+    const int j = i % 16;
+    if (parts) store4<4>((gchar*)(acc + t.element(i)), x[j], x[j + 1], x[j + 2], x[j + 3]);
+    else store4<EB>(out + t.element(i) * EB, x[j] * inv, x[j + 1] * inv, x[j + 2] * inv, x[j + 3] * inv);
+  }
   if (t.half == 0 && t.wk == 0) {
-    ((gfloat*)A.lse)[at] = t.l == 0.0f ? -INFINITY : (t.m + __log2f(t.l)) * kLn2;
-    if (A.norm) { ((gfloat*)A.norm)[2 * at] = t.m; ((gfloat*)A.norm)[2 * at + 1] = inv; }
+    if (parts) store_part(A, J, at, t.m, t.l);
+    else store_lse(A, at, t.m, t.l);
+  }
+}
+
+template <int D, int NB, bool MOD>
+__global__ __launch_bounds__(4 * kWave, 2) void k_prompt_many(PromptArgs A) {
+  using F = Flow<D, NB, MOD>;
+  extern __shared__ __align__(16) char s_lds[];
+  Job J;
+  if (!job_of<2, D, F::kRows, F::kThreads>(A, J)) return;
+  F f(A.mods, J.keys, (lchar*)s_lds);
+  size_t at[NB];
+  const int r = J.row0 + f.wave * NB * 32 + f.col;
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    at[b] = row_of<MOD>(A, J, r + b * 32, f.row[b]);
+    f.load_q(b, (const gchar*)A.q + at[b] * (D * 2));
+  }
+  f.run();
+  const bool parts = A.chunks > 1;
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    if (r + b * 32 >= J.rows) continue;
+    if (parts) {
+      gfloat* const acc = (gfloat*)A.part_acc + (at[b] * A.chunks + J.chunk) * D;
+#pragma unroll
+      for (int dt = 0; dt < F::DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          store4<4>((gchar*)(acc + dt * 32 + i * 2 + f.half * 4), f.acc[b][dt][i], f.acc[b][dt][i + 1], f.acc[b][dt][i + 2], f.acc[b][dt][i + 3]);
+      if (f.half == 0) store_part(A, J, at[b], f.m[b], f.l[b]);
+      continue;
+    }
+    const float inv = inverse(f.l[b]);
+    gchar* const out = (gchar*)A.out + at[b] * (D * 2);
+#pragma unroll
+    for (int dt = 0; dt < F::DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; i += 8) {              // the halves of the wave trade 4 elements each: 8 in a row for both
+        const f32x16& x = f.acc[b][dt];
+        const u32x2 u = __builtin_amdgcn_permlane32_swap(pack2_bf16(x[i] * inv, x[i + 1] * inv), pack2_bf16(x[i + 4] * inv, x[i + 5] * inv), false, false);
+        const u32x2 v = __builtin_amdgcn_permlane32_swap(pack2_bf16(x[i + 2] * inv, x[i + 3] * inv), pack2_bf16(x[i + 6] * inv, x[i + 7] * inv), false, false);
+        store16(out + (dt * 32 + i * 2 + f.half * 8) * 2, make_uint4(u.x, v.x, u.y, v.y));
+      }
+    if (f.half == 0) store_lse(A, at[b], f.m[b], f.l[b]);
   }
 }
 
@@ -600,17 +1044,14 @@ __global__ __launch_bounds__(256) void k_prompt_finish(PromptArgs A) {
 #pragma unroll
     for (int e = 0; e < D / kWave; ++e) x[e] = fmaf(acc[(size_t)c * D + e * kWave + lane], w, x[e]);
   }
-  const float inv = L > 0.0f ? 1.0f / L : L == 0.0f ? 0.0f : L;
+  const float inv = inverse(L);
 #pragma unroll
   for (int e = 0; e < D / kWave; ++e) {
     const size_t o = at * D + e * kWave + lane;
     if constexpr (EB == 4) ((gfloat*)A.out)[o] = x[e] * inv;
     else ((ADSA_GLOBAL uint16_t*)A.out)[o] = (uint16_t)f32_to_bf16_rne(x[e] * inv);
   }
-  if (lane == 0) {
-    ((gfloat*)A.lse)[at] = L == 0.0f ? -INFINITY : (M + __log2f(L)) * kLn2;
-    if (A.norm) { ((gfloat*)A.norm)[2 * at] = M; ((gfloat*)A.norm)[2 * at + 1] = inv; }
-  }
+  if (lane == 0) store_lse(A, at, M, L);
 }
 
 // score[head][slot] += sum over rows of the probability they gave the slot.  A wave keeps 32 slots' K rows as the B operand and meets 64
@@ -1003,8 +1444,13 @@ hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStrea
   const unsigned pairs = (unsigned)((A.n_seq * A.h + 7) / 8 * 8);
   constexpr int KW = kKeyWaves<EB, D>, KT = kStepKeys<EB>;
   const dim3 grid(pairs * (unsigned)(plan.tiles * plan.chunks));
-  if (plan.few) k_prompt<EB, D, 1, KW, 32, MOD><<<grid, KW * kWave, Shape<EB, D, 1, KW, 32>::kLds, st>>>(A);
-  else k_prompt<EB, D, 4, 1, KT, MOD><<<grid, 4 * kWave, Shape<EB, D, 4, 1, KT>::kLds, st>>>(A);
+  if (plan.rows <= 32) k_prompt<EB, D, 1, KW, 32, MOD><<<grid, KW * kWave, Shape<EB, D, 1, KW, 32>::kLds, st>>>(A);
+  else if (EB == 2 && plan.flow) {
+    if constexpr (EB == 2) {
+      if (plan.rows == 128) k_prompt_many<D, 1, MOD><<<grid, 4 * kWave, Flow<D, 1, MOD>::kLds, st>>>(A);
+      else k_prompt_many<D, 2, MOD><<<grid, 4 * kWave, Flow<D, 2, MOD>::kLds, st>>>(A);
+    }
+  } else k_prompt<EB, D, 4, 1, KT, MOD><<<grid, 4 * kWave, Shape<EB, D, 4, 1, KT>::kLds, st>>>(A);
   if (plan.chunks > 1) {
     const size_t rows = (size_t)A.n_tokens * A.h * A.G;
     k_prompt_finish<EB, D><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, st>>>(A);
@@ -1027,14 +1473,19 @@ hipError_t shared_launches(const SharedArgs& A, hipStream_t st) {
 template <int EB, int D, bool MOD>
 hipError_t allow_lds() {
   constexpr int KW = kKeyWaves<EB, D>, KT = kStepKeys<EB>;
-  const void* const kernels[] = {(const void*)k_prompt<EB, D, 1, KW, 32, MOD>, (const void*)k_prompt<EB, D, 4, 1, KT, MOD>, (const void*)k_prompt_mass<EB, D, MOD>,
-                                 (const void*)k_shared<EB, D, KW, MOD>};
-  const int bytes[] = {Shape<EB, D, 1, KW, 32>::kLds, Shape<EB, D, 4, 1, KT>::kLds, MassLds<EB, D>::kLds, Shape<EB, D, 1, KW, 32>::kLds};
-  for (int i = 0; i < 4; ++i) {
-    const hipError_t e = hipFuncSetAttribute(kernels[i], hipFuncAttributeMaxDynamicSharedMemorySize, bytes[i]);
-    if (e != hipSuccess) return e;
+  hipError_t e = hipSuccess;
+  auto allow = [&](auto kernel, int bytes) {
+    if (e == hipSuccess) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  };
+  allow(k_prompt<EB, D, 1, KW, 32, MOD>, Shape<EB, D, 1, KW, 32>::kLds);
+  allow(k_prompt<EB, D, 4, 1, KT, MOD>, Shape<EB, D, 4, 1, KT>::kLds);
+  allow(k_prompt_mass<EB, D, MOD>, MassLds<EB, D>::kLds);
+  allow(k_shared<EB, D, KW, MOD>, Shape<EB, D, 1, KW, 32>::kLds);
+  if constexpr (EB == 2) {
+    allow(k_prompt_many<D, 1, MOD>, Flow<D, 1, MOD>::kLds);
+    allow(k_prompt_many<D, 2, MOD>, Flow<D, 2, MOD>::kLds);
   }
-  return hipSuccess;
+  return e;
 }
 
 template <typename F>
@@ -1067,8 +1518,10 @@ hipError_t prompt_prepare_kernels() {
 PromptPlan make_prompt_plan(const adsa_params& p, const adsa_tokens& t) {
   const long long rows = (long long)t.max_len * query_group(p), pairs = (long long)p.n_seq * p.n_heads;
   PromptPlan plan;
-  plan.few = rows <= 32;
-  plan.tiles = (int)((rows + (plan.few ? 31 : 127)) / (plan.few ? 32 : 128));
+  // (a tile's rows are reached with 32-bit offsets from its first)
+  plan.flow = p.dtype == ADSA_BF16 && p.kv_slot_stride * 2 * 64 < (1ll << 31);
+  plan.rows = rows <= 32 ? 32 : 128;
+  plan.tiles = (int)((rows + plan.rows - 1) / plan.rows);
   const long long groups = pairs * plan.tiles;
   plan.chunks = (int)std::clamp<long long>(std::min<long long>((512 + groups - 1) / groups, (p.cap + 255) / 256), 1, kMaxChunks);
   return plan;
