@@ -448,20 +448,19 @@ __device__ __forceinline__ void store4(gchar* p, float a, float b, float c, floa
   else *(ADSA_GLOBAL u32x2*)p = u32x2{pack2_bf16(a, b), pack2_bf16(c, d)};
 }
 
-// Many rows of a bf16 prompt: 4 waves of NB blocks of 32 rows each, keys in steps of 32, two steps to a tile of K and V in LDS.
+// Many rows of a bf16 prompt: W waves of 32 rows each, keys in steps of 32, two steps to a tile of K and V in LDS.
 //
-// What bounds it: a block's step is D / 4 cycles of its SIMD's matrix core per key (2 x D / 16 products of 32x32x16), and about 470 cycles of vector
-// work (16 exponentials at a quarter of the rate, their arguments, sums, maxima, conversions), so neither may wait for the other.  Besides,
-// every step fetches K and V out of LDS, for 32 rows as many bytes as the LDS has cycles for: two blocks a wave (NB = 2) share a fetch.
+// What bounds it: a step is 2 x D / 16 products of 32x32x16, 32 cycles of the SIMD's matrix core each, and about 100 vector instructions
+// (16 exponentials at half the rate, their arguments, sums, maxima, conversions), as many cycles again, so neither may wait for the other.
 // So a wave takes whatever is independent at one time: the scores of step j + 1 and the outputs of step j - 1 on the matrix core, the softmax of
-// step j on the vector unit, laid out alternately by hand (one product of each block, then its share of the vector work), since the
+// step j on the vector unit, laid out alternately by hand (a product, then its share of the vector work), since the
 // compiler left alone puts all of one kind before the other.
 // A row's maximum is followed only when it has grown by more than 2^8: P stays below 2^8, and outputs are rescaled next to never.
-template <int D, int NB, bool MOD>
+template <int D, int W, bool MOD>
 struct Flow {
   using L = Layout<2, D>;
   static constexpr int CPR = L::CPR, RB = L::RB, DT = D / 32, KC = D / 16, VC = DT * 2, NC = KC + VC;
-  static constexpr int kThreads = 4 * kWave, kRows = 4 * NB * 32, TK = 64;
+  static constexpr int kThreads = W * kWave, kRows = W * 32, TK = 64;
   static constexpr int RPT = kThreads / CPR, NL = TK / RPT;
   static constexpr int kV = 2 * TK * RB, kMeta = 2 * kV, kLds = kMeta + (MOD ? 3 * 2 * TK * 4 : 0);      // two tiles of K, of V; positions and documents of three
   static constexpr float kGrowth = 8.0f;
@@ -470,11 +469,11 @@ struct Flow {
   const Keys& keys;
   lchar* const lds;
   const int tid, lane, col, half, wave;
-  uint4 qf[NB][KC];
-  Row row[NB];
-  f32x16 acc[NB][DT], s[NB];
-  uint32_t p[NB][8];           // probabilities of the step before, two to a word
-  float m[NB], l[NB];
+  uint4 qf[KC];
+  Row row;
+  f32x16 acc[DT], s;
+  uint32_t p[8];           // probabilities of the step before, two to a word
+  float m, l;
   uint4 kr[NL], vr[NL];
   int meta_pos, meta_doc;
   // LDS offsets: the lane's pieces of the tile of K and of V that are read, the thread's of those that are written.  Each changes buffers
@@ -505,9 +504,9 @@ struct Flow {
     k_to ^= TK * RB;
     v_to ^= TK * RB;
   }
-  __device__ __forceinline__ void load_q(int b, const gchar* q_row) {
+  __device__ __forceinline__ void load_q(const gchar* q_row) {
 #pragma unroll
-    for (int c = 0; c < KC; ++c) qf[b][c] = load16(q_row + (2 * c + half) * 16);
+    for (int c = 0; c < KC; ++c) qf[c] = load16(q_row + (2 * c + half) * 16);
   }
 
   // rows of a tile on their way: 32-bit offsets from the tile's first row, which hold for every tile but a last, shorter one
@@ -552,7 +551,7 @@ struct Flow {
     const u32x2 a = __builtin_bit_cast(u32x2, lo), b = __builtin_bit_cast(u32x2, hi);
     return u32x4{a.x, a.y, b.x, b.y};
   }
-  __device__ __forceinline__ bf16x8 p_piece(int b, int t) const { return __builtin_bit_cast(bf16x8, u32x4{p[b][4 * t], p[b][4 * t + 1], p[b][4 * t + 2], p[b][4 * t + 3]}); }
+  __device__ __forceinline__ bf16x8 p_piece(int t) const { return __builtin_bit_cast(bf16x8, u32x4{p[4 * t], p[4 * t + 1], p[4 * t + 2], p[4 * t + 3]}); }
 
   // Infinities and NaN among V's rows of a step whose keys not every row sees (rare): they must not reach rows that do not see them.
   __device__ __forceinline__ bool values_bad(int sub) const {
@@ -574,71 +573,71 @@ struct Flow {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+      for (int negative = 0; negative < 2; ++negative) {
+        f32x16 r = {};
 #pragma unroll
-        for (int negative = 0; negative < 2; ++negative) {
-          f32x16 r = {};
+        for (int t = 0; t < 2; ++t) {
+          const u32x4 w = v_piece(sub, dt * 2 + t);
+          u32x4 x = {p[4 * t], p[4 * t + 1], p[4 * t + 2], p[4 * t + 3]};
 #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            const u32x4 w = v_piece(sub, dt * 2 + t);
-            u32x4 x = {p[b][4 * t], p[b][4 * t + 1], p[b][4 * t + 2], p[b][4 * t + 3]};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = ((x[i] & 0xFFFFu) ? 0x3F80u : 0u) | ((x[i] >> 16) ? 0x3F800000u : 0u);
-            const u32x4 o = {ones_at(w.x, negative), ones_at(w.y, negative), ones_at(w.z, negative), ones_at(w.w, negative)};
-            r = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, o), __builtin_bit_cast(bf16x8, x), r, 0, 0, 0);
-          }
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[b][dt][i] += r[i] > 0.0f ? (negative ? -INFINITY : INFINITY) : 0.0f;
+          for (int i = 0; i < 4; ++i) x[i] = ((x[i] & 0xFFFFu) ? 0x3F80u : 0u) | ((x[i] >> 16) ? 0x3F800000u : 0u);
+          const u32x4 o = {ones_at(w.x, negative), ones_at(w.y, negative), ones_at(w.z, negative), ones_at(w.w, negative)};
+          r = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, o), __builtin_bit_cast(bf16x8, x), r, 0, 0, 0);
         }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[dt][i] += r[i] > 0.0f ? (negative ? -INFINITY : INFINITY) : 0.0f;
+      }
   }
 
   // pieces of the two steps' work
-  __device__ __forceinline__ void bend(int b, int i, const ADSA_LDS int* meta) {           // cap and distance of one score
-    float z = mods.cap_out != 0.0f ? capped<2>(s[b][i], mods) : s[b][i] * mods.scale_log2;
-    if (mods.slopes) z = fmaf(-row[b].slope, fabsf((float)row[b].pos - __int_as_float(meta[(i / 4) * 8 + half * 4 + i % 4])), z);
-    s[b][i] = z;
+  __device__ __forceinline__ void bend(int i, const ADSA_LDS int* meta) {                  // cap and distance of one score
+    float z = mods.cap_out != 0.0f ? capped<2>(s[i], mods) : s[i] * mods.scale_log2;
+    if (mods.slopes) z = fmaf(-row.slope, fabsf((float)row.pos - __int_as_float(meta[(i / 4) * 8 + half * 4 + i % 4])), z);
+    s[i] = z;
   }
   __device__ __forceinline__ float score_scale() const { return MOD ? 1.0f : mods.scale_log2; }
-  // The step's maximum of block b's rows; where it has grown, what the state so far has to be multiplied by.
-  __device__ __forceinline__ bool maximum(int b, float* corr) {
-    float mx = s[b][0];
+  // The step's maximum; where it has grown, what the state so far has to be multiplied by.
+  __device__ __forceinline__ bool maximum(float* corr) {
+    float mx = s[0];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[b][i]);            // (no asm here: a product's result takes wait states that the compiler counts)
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);   // (no asm here: a product's result takes wait states that the compiler counts)
     mx = xor_max<32>(mx) * score_scale();
-    const bool grows = mx > m[b] + kGrowth;
-    const float m_new = grows ? mx : m[b];
-    *corr = fast_exp2(m[b] - m_new);
-    m[b] = m_new;
+    const bool grows = mx > m + kGrowth;
+    const float m_new = grows ? mx : m;
+    *corr = fast_exp2(m - m_new);
+    m = m_new;
     return grows;
   }
-  __device__ __forceinline__ uint32_t two_probabilities(int b, int i, float* sum) {
-    const float a = fast_exp2(fmaf(s[b][i], score_scale(), -m[b])), d = fast_exp2(fmaf(s[b][i + 1], score_scale(), -m[b]));
+  __device__ __forceinline__ uint32_t two_probabilities(int i, float* sum) {
+    const float a = fast_exp2(fmaf(s[i], score_scale(), -m)), d = fast_exp2(fmaf(s[i + 1], score_scale(), -m));
     *sum += a;
     *sum += d;
     return pack2_bf16(a, d);
   }
-  __device__ __forceinline__ void rescale(const float (&corr)[NB]) {
+  __device__ __forceinline__ void rescale(float corr) {
+    l *= corr;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      l[b] *= corr[b];
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[b][dt][i] *= corr[b];
-    }
+      for (int i = 0; i < 16; ++i) acc[dt][i] *= corr;
+  }
+  __device__ __forceinline__ f32x16 score_product(const uint4& k, int c, const f32x16& x) const {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[c]), x, 0, 0, 0);
+  }
+  __device__ __forceinline__ void output_product(const u32x4& v, int i) {
+    acc[i / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), p_piece(i % 2), acc[i / 2], 0, 0, 0);
   }
 
   // One step of keys that every row sees: the scores of K's rows (half SUB of the tile), the softmax of the scores s of the step
   // before, the outputs of its predecessor's p with V's rows, alternately.
   template <int SUB>
   __device__ __forceinline__ void step(const ADSA_LDS int* meta) {
-    f32x16 next[NB];
-    uint32_t pn[NB][8];
-    float corr[NB], sum[NB];
+    f32x16 next = {};
+    uint32_t pn[8];
+    float corr, sum = 0.0f;
     bool grown = false;
-    constexpr int kAhead = 2;                        // pieces fetched ahead of their product
-    constexpr int kMax = MOD ? NC / 2 : 1;           // the maxima stand before this chunk's probabilities
-    constexpr int kE = NB * 16;                      // scores of a lane
+    constexpr int kAhead = 3;                        // pieces fetched ahead of their product
+    constexpr int kMax = MOD ? NC / 2 : 1;           // the maximum stands before this chunk's probabilities
     uint4 kp[KC];
     u32x4 vp[VC];
     auto fetch = [&](auto at) {
@@ -647,50 +646,31 @@ struct Flow {
       else if constexpr (c < NC) vp[c - KC] = v_piece(SUB, c - KC);
     };
     each<kAhead>(fetch);
-#pragma unroll
-    for (int b = 0; b < NB; ++b) sum[b] = 0.0f;
     each<NC>([&](auto at) {
       constexpr int c = decltype(at)::value;
       fetch(std::integral_constant<int, c + kAhead>());
-      if constexpr (c < KC) {
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-          next[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kp[c]), __builtin_bit_cast(bf16x8, qf[b][c]), c == 0 ? f32x16{} : next[b], 0, 0, 0);
-      } else {
-        constexpr int i = c - KC;
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-          acc[b][i / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vp[i]), p_piece(b, i % 2), acc[b][i / 2], 0, 0, 0);
-      }
+      if constexpr (c < KC) next = score_product(kp[c], c, next);
+      else output_product(vp[c - KC], c - KC);
       if constexpr (MOD && c < kMax) {
-        constexpr int e0 = kE * c / kMax;
-        each<kE * (c + 1) / kMax - e0>([&](auto o) {
-          constexpr int e = e0 + decltype(o)::value;
-          bend(e / 16, e % 16, meta);
-        });
+        constexpr int e0 = 16 * c / kMax;
+        each<16 * (c + 1) / kMax - e0>([&](auto o) { bend(e0 + decltype(o)::value, meta); });
       }
-      if constexpr (c == kMax) {
-#pragma unroll
-        for (int b = 0; b < NB; ++b) grown |= maximum(b, &corr[b]);
-      }
+      if constexpr (c == kMax) grown = maximum(&corr);
       if constexpr (c >= kMax) {                     // this chunk's share of the probabilities
-        constexpr int kRest = NC - kMax, e0 = kE / 2 * (c - kMax) / kRest;
-        each<kE / 2 * (c + 1 - kMax) / kRest - e0>([&](auto o) {
-          constexpr int e = 2 * (e0 + decltype(o)::value);
-          pn[e / 16][e % 16 / 2] = two_probabilities(e / 16, e % 16, &sum[e / 16]);
-          asm volatile("" : "+v"(pn[e / 16][e % 16 / 2]), "+v"(sum[e / 16]));      // (here, not where p is used)
+        constexpr int kRest = NC - kMax, e0 = 8 * (c - kMax) / kRest;
+        each<8 * (c + 1 - kMax) / kRest - e0>([&](auto o) {
+          constexpr int e = e0 + decltype(o)::value;
+          pn[e] = two_probabilities(2 * e, &sum);
+          asm volatile("" : "+v"(pn[e]), "+v"(sum));           // (here, not where p is used)
         });
       }
       __builtin_amdgcn_sched_barrier(0);
     });
     if (__ballot(grown) != 0) rescale(corr);
+    l += sum;
+    s = next;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      l[b] += sum[b];
-      s[b] = next[b];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) p[b][i] = pn[b][i];
-    }
+    for (int i = 0; i < 8; ++i) p[i] = pn[i];
   }
 
   // The same one after the other: first and last steps (which lack a part), and keys that not every row sees.
@@ -701,49 +681,35 @@ struct Flow {
     for (int i = 0; i < VC; ++i) {
       u32x4 w = v_piece(sub, i);
       if (tidy) w = u32x4{bf16_finite(w.x), bf16_finite(w.y), bf16_finite(w.z), bf16_finite(w.w)};
-#pragma unroll
-      for (int b = 0; b < NB; ++b) acc[b][i / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), p_piece(b, i % 2), acc[b][i / 2], 0, 0, 0);
+      output_product(w, i);
     }
   }
   __device__ __forceinline__ void scores(int sub) {
+    s = f32x16{};
 #pragma unroll
-    for (int b = 0; b < NB; ++b) s[b] = f32x16{};
-#pragma unroll
-    for (int c = 0; c < KC; ++c) {
-      const uint4 k = k_piece(sub, c);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[b][c]), s[b], 0, 0, 0);
-    }
+    for (int c = 0; c < KC; ++c) s = score_product(k_piece(sub, c), c, s);
   }
   __device__ __forceinline__ void softmax(int base, const ADSA_LDS int* meta, bool masked) {
-    float corr[NB];
-    bool grown = false;
+    if constexpr (MOD) {
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      if constexpr (MOD) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) bend(b, i, meta);
-      }
-      if (masked) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int k = (i / 4) * 8 + half * 4 + i % 4;
-          bool seen = base + k < row[b].limit;
-          if constexpr (MOD)
-            if (keys.doc) seen &= meta[TK + k] == row[b].doc;
-          s[b][i] = seen ? s[b][i] : -INFINITY;
-        }
-      }
-      grown |= maximum(b, &corr[b]);
+      for (int i = 0; i < 16; ++i) bend(i, meta);
     }
+    if (masked) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int k = (i / 4) * 8 + half * 4 + i % 4;
+        bool seen = base + k < row.limit;
+        if constexpr (MOD)
+          if (keys.doc) seen &= meta[TK + k] == row.doc;
+        s[i] = seen ? s[i] : -INFINITY;
+      }
+    }
+    float corr, sum = 0.0f;
+    const bool grown = maximum(&corr);
     if (__ballot(grown) != 0) rescale(corr);
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      float sum = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) p[b][i / 2] = two_probabilities(b, i, &sum);
-      l[b] += sum;
-    }
+    for (int i = 0; i < 16; i += 2) p[i / 2] = two_probabilities(i, &sum);
+    l += sum;
   }
 
   int lo, hi;                  // keys that all rows of the wave see, and from which on none does
@@ -770,17 +736,12 @@ struct Flow {
     }
   }
   __device__ __forceinline__ void run() {
+    m = kLowest;
+    l = 0.0f;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      m[b] = kLowest;
-      l[b] = 0.0f;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) acc[b][dt] = f32x16{};
-    }
+    for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x16{};
     if (keys.begin >= keys.end) return;              // (a part without keys: there is no row to load)
-    lo = hi = row[0].limit;
-#pragma unroll
-    for (int b = 1; b < NB; ++b) { lo = min(lo, row[b].limit); hi = max(hi, row[b].limit); }
+    lo = hi = row.limit;
 #pragma unroll
     for (int x = 1; x < 32; x <<= 1) { lo = min(lo, __shfl_xor(lo, x)); hi = max(hi, __shfl_xor(hi, x)); }
     lo = __builtin_amdgcn_readfirstlane(lo);
@@ -816,8 +777,7 @@ struct Flow {
       tile(t, mine);
       if (t < tiles) next_tile(t);
     }
-#pragma unroll
-    for (int b = 0; b < NB; ++b) l[b] = xor_sum<32>(l[b]);
+    l = xor_sum<32>(l);
   }
 };
 
@@ -973,48 +933,39 @@ __global__ __launch_bounds__(WR * WK * kWave) void k_prompt(PromptArgs A) {
   }
 }
 
-template <int D, int NB, bool MOD>
-__global__ __launch_bounds__(4 * kWave, 2) void k_prompt_many(PromptArgs A) {
-  using F = Flow<D, NB, MOD>;
+template <int D, int W, bool MOD>
+__global__ __launch_bounds__(W * kWave, 2) void k_prompt_many(PromptArgs A) {
+  using F = Flow<D, W, MOD>;
   extern __shared__ __align__(16) char s_lds[];
   Job J;
   if (!job_of<2, D, F::kRows, F::kThreads>(A, J)) return;
   F f(A.mods, J.keys, (lchar*)s_lds);
-  size_t at[NB];
-  const int r = J.row0 + f.wave * NB * 32 + f.col;
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    at[b] = row_of<MOD>(A, J, r + b * 32, f.row[b]);
-    f.load_q(b, (const gchar*)A.q + at[b] * (D * 2));
-  }
+  const int r = J.row0 + f.wave * 32 + f.col;
+  const size_t at = row_of<MOD>(A, J, r, f.row);
+  f.load_q((const gchar*)A.q + at * (D * 2));
   f.run();
-  const bool parts = A.chunks > 1;
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    if (r + b * 32 >= J.rows) continue;
-    if (parts) {
-      gfloat* const acc = (gfloat*)A.part_acc + (at[b] * A.chunks + J.chunk) * D;
-#pragma unroll
-      for (int dt = 0; dt < F::DT; ++dt)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4)
-          store4<4>((gchar*)(acc + dt * 32 + i * 2 + f.half * 4), f.acc[b][dt][i], f.acc[b][dt][i + 1], f.acc[b][dt][i + 2], f.acc[b][dt][i + 3]);
-      if (f.half == 0) store_part(A, J, at[b], f.m[b], f.l[b]);
-      continue;
-    }
-    const float inv = inverse(f.l[b]);
-    gchar* const out = (gchar*)A.out + at[b] * (D * 2);
+  if (r >= J.rows) return;
+  if (A.chunks > 1) {
+    gfloat* const acc = (gfloat*)A.part_acc + (at * A.chunks + J.chunk) * D;
 #pragma unroll
     for (int dt = 0; dt < F::DT; ++dt)
 #pragma unroll
-      for (int i = 0; i < 16; i += 8) {              // the halves of the wave trade 4 elements each: 8 in a row for both
-        const f32x16& x = f.acc[b][dt];
-        const u32x2 u = __builtin_amdgcn_permlane32_swap(pack2_bf16(x[i] * inv, x[i + 1] * inv), pack2_bf16(x[i + 4] * inv, x[i + 5] * inv), false, false);
-        const u32x2 v = __builtin_amdgcn_permlane32_swap(pack2_bf16(x[i + 2] * inv, x[i + 3] * inv), pack2_bf16(x[i + 6] * inv, x[i + 7] * inv), false, false);
-        store16(out + (dt * 32 + i * 2 + f.half * 8) * 2, make_uint4(u.x, v.x, u.y, v.y));
-      }
-    if (f.half == 0) store_lse(A, at[b], f.m[b], f.l[b]);
+      for (int i = 0; i < 16; i += 4) store4<4>((gchar*)(acc + dt * 32 + i * 2 + f.half * 4), f.acc[dt][i], f.acc[dt][i + 1], f.acc[dt][i + 2], f.acc[dt][i + 3]);
+    if (f.half == 0) store_part(A, J, at, f.m, f.l);
+    return;
   }
+  const float inv = inverse(f.l);
+  gchar* const out = (gchar*)A.out + at * (D * 2);
+#pragma unroll
+  for (int dt = 0; dt < F::DT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; i += 8) {                // the halves of the wave trade 4 elements each: 8 in a row for both
+      const f32x16& x = f.acc[dt];
+      const u32x2 u = __builtin_amdgcn_permlane32_swap(pack2_bf16(x[i] * inv, x[i + 1] * inv), pack2_bf16(x[i + 4] * inv, x[i + 5] * inv), false, false);
+      const u32x2 v = __builtin_amdgcn_permlane32_swap(pack2_bf16(x[i + 2] * inv, x[i + 3] * inv), pack2_bf16(x[i + 6] * inv, x[i + 7] * inv), false, false);
+      store16(out + (dt * 32 + i * 2 + f.half * 8) * 2, make_uint4(u.x, v.x, u.y, v.y));
+    }
+  if (f.half == 0) store_lse(A, at, f.m, f.l);
 }
 
 // Split keys: a wave joins the parts of one row.
@@ -1447,8 +1398,8 @@ hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStrea
   if (plan.rows <= 32) k_prompt<EB, D, 1, KW, 32, MOD><<<grid, KW * kWave, Shape<EB, D, 1, KW, 32>::kLds, st>>>(A);
   else if (EB == 2 && plan.flow) {
     if constexpr (EB == 2) {
-      if (plan.rows == 128) k_prompt_many<D, 1, MOD><<<grid, 4 * kWave, Flow<D, 1, MOD>::kLds, st>>>(A);
-      else k_prompt_many<D, 2, MOD><<<grid, 4 * kWave, Flow<D, 2, MOD>::kLds, st>>>(A);
+      if (plan.rows == 128) k_prompt_many<D, 4, MOD><<<grid, 4 * kWave, Flow<D, 4, MOD>::kLds, st>>>(A);
+      else k_prompt_many<D, 8, MOD><<<grid, 8 * kWave, Flow<D, 8, MOD>::kLds, st>>>(A);
     }
   } else k_prompt<EB, D, 4, 1, KT, MOD><<<grid, 4 * kWave, Shape<EB, D, 4, 1, KT>::kLds, st>>>(A);
   if (plan.chunks > 1) {
@@ -1482,8 +1433,8 @@ hipError_t allow_lds() {
   allow(k_prompt_mass<EB, D, MOD>, MassLds<EB, D>::kLds);
   allow(k_shared<EB, D, KW, MOD>, Shape<EB, D, 1, KW, 32>::kLds);
   if constexpr (EB == 2) {
-    allow(k_prompt_many<D, 1, MOD>, Flow<D, 1, MOD>::kLds);
-    allow(k_prompt_many<D, 2, MOD>, Flow<D, 2, MOD>::kLds);
+    allow(k_prompt_many<D, 4, MOD>, Flow<D, 4, MOD>::kLds);
+    allow(k_prompt_many<D, 8, MOD>, Flow<D, 8, MOD>::kLds);
   }
   return e;
 }
@@ -1520,7 +1471,7 @@ PromptPlan make_prompt_plan(const adsa_params& p, const adsa_tokens& t) {
   PromptPlan plan;
   // (a tile's rows are reached with 32-bit offsets from its first)
   plan.flow = p.dtype == ADSA_BF16 && p.kv_slot_stride * 2 * 64 < (1ll << 31);
-  plan.rows = rows <= 32 ? 32 : 128;
+  plan.rows = rows <= 32 ? 32 : rows <= 128 || !plan.flow ? 128 : 256;
   plan.tiles = (int)((rows + plan.rows - 1) / plan.rows);
   const long long groups = pairs * plan.tiles;
   plan.chunks = (int)std::clamp<long long>(std::min<long long>((512 + groups - 1) / groups, (p.cap + 255) / 256), 1, kMaxChunks);
