@@ -137,4 +137,59 @@ __device__ __forceinline__ float xor_max(float x) {
   }
 }
 
+// Sum over the LPR consecutive lanes that hold one row; every lane of the group gets the sum.
+template <int LPR>
+__device__ __forceinline__ float row_sum(float x) {
+  x += dpp_f<0xB1>(x);            // quad_perm [1,0,3,2]
+  x += dpp_f<0x4E>(x);            // quad_perm [2,3,0,1]
+  x += dpp_f<0x141>(x);           // row_half_mirror: the other quad of the 8-lane group
+  if (LPR >= 16) x += dpp_f<0x140>(x);   // row_mirror: the other half of the 16-lane row
+  if (LPR >= 32) x = xor_sum<16>(x);
+  return x;
+}
+
+// 16 bytes of a row as fp32 values, and their dot product with the lane's piece of q.  bf16: two products per instruction
+// (v_dot2, fp32 sums), so q stays as it arrived and the softmax scale is applied to the sum; fp32: q is scaled beforehand.
+template <int EB> struct Elems;
+template <> struct Elems<2> {      // bf16: 8 values per 16-byte vector
+  static constexpr int N = 8;
+  uint32_t q[4];
+  __device__ __forceinline__ Elems(const uint4& r, float) : q{r.x, r.y, r.z, r.w} {}
+  static __device__ __forceinline__ void unpack(const uint4& r, float* f) {
+    f[0] = __uint_as_float(r.x << 16); f[1] = __uint_as_float(r.x & 0xFFFF0000u);
+    f[2] = __uint_as_float(r.y << 16); f[3] = __uint_as_float(r.y & 0xFFFF0000u);
+    f[4] = __uint_as_float(r.z << 16); f[5] = __uint_as_float(r.z & 0xFFFF0000u);
+    f[6] = __uint_as_float(r.w << 16); f[7] = __uint_as_float(r.w & 0xFFFF0000u);
+  }
+  __device__ __forceinline__ float dot(const uint4& r) const {
+    const uint32_t k[4] = {r.x, r.y, r.z, r.w};
+    float d = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, q[i]), __builtin_bit_cast(bf16x2, k[i]), d, false);
+    return d;
+  }
+  static __device__ __forceinline__ float scaled(float d, float scale) { return d * scale; }
+};
+template <> struct Elems<4> {      // fp32: 4 values per 16-byte vector
+  static constexpr int N = 4;
+  float q[4];
+  __device__ __forceinline__ Elems(const uint4& r, float scale) {
+    unpack(r, q);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] *= scale;
+  }
+  static __device__ __forceinline__ void unpack(const uint4& r, float* f) {
+    f[0] = __uint_as_float(r.x); f[1] = __uint_as_float(r.y);
+    f[2] = __uint_as_float(r.z); f[3] = __uint_as_float(r.w);
+  }
+  __device__ __forceinline__ float dot(const uint4& r) const {
+    float k[4], d = 0.0f;
+    unpack(r, k);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d = fmaf(q[i], k[i], d);
+    return d;
+  }
+  static __device__ __forceinline__ float scaled(float d, float) { return d; }
+};
+
 }  // namespace adsa

@@ -88,6 +88,11 @@ __device__ __forceinline__ uint32_t bf16_finite(uint32_t w) {            // infi
   if ((w & 0x7F800000u) == 0x7F800000u) w &= 0xFFFFu;
   return w;
 }
+// ones (bf16) where w's values are +infinity or -infinity; a NaN counts as both
+__device__ __forceinline__ uint32_t ones_at(uint32_t w, bool negative) {
+  auto hit = [&](uint32_t h) { return (h & 0x7FFFu) > 0x7F80u || h == (negative ? 0xFF80u : 0x7F80u); };
+  return (hit(w & 0xFFFFu) ? 0x3F80u : 0u) | (hit(w >> 16) ? 0x3F800000u : 0u);
+}
 __device__ __forceinline__ bool f32_bad(float x) { return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u; }
 
 // scores of 16 elements: fp32 sum q.k -> log2 units
@@ -98,6 +103,10 @@ __device__ __forceinline__ float capped(float s, const Mods& mods) {
   // tanh t = 1 - 2 / (e^2t + 1): off by 2^-23 of 1, far below the rounding of bf16 inputs
   return mods.cap_out * fmaf(-2.0f, __builtin_amdgcn_rcpf(fast_exp2(t * (2.0f * kLog2e)) + 1.0f), 1.0f);
 }
+
+// Two waves share a SIMD's registers, but for fp32 rows of 128, whose steps alone take half of one's.  (Within 256 registers products are formed in
+// those the vector unit works on, too; beyond, scores and outputs would be copied between the two kinds.)
+template <int EB, int D> constexpr int kWavesPerSimd = EB == 4 && D == 128 ? 1 : 2;
 
 template <int EB, int D, int WR, int WK, int KT> struct Shape {
   static constexpr int kThreads = WR * WK * kWave;
@@ -112,7 +121,8 @@ template <int EB, int D, int WR, int WK, int KT> struct Shape {
 // The attention of a workgroup's rows (32 per row wave; a lane's q pieces in qf) over its keys.  Afterwards m, l (of the lane's row, both halves of
 // the wave alike) and the wave's share of the unnormalised outputs: acc[r], r in [0, D / 32 * 16 / WK), are the
 // elements of register r + wk * (...) of the D / 32 transposed 32x32 blocks.
-template <int EB, int D, int WR, int WK, int KT, bool MOD, bool LIST>
+// ALL: every row sees every key (but the ones past the end, which repeat the last), so none can hold what must not reach a row.
+template <int EB, int D, int WR, int WK, int KT, bool MOD, bool LIST, bool ALL>
 struct Tile {
   using L = Layout<EB, D>;
   using S = Shape<EB, D, WR, WK, KT>;
@@ -192,10 +202,24 @@ struct Tile {
     }
   }
 
+  // The lane's piece of V^T for 32 elements (block dt) and 16 keys (t) of the 32 from row r0 on, bf16: element j of a lane of half h belongs to
+  // key 16 t + 8 (j / 4) + 4 h + j % 4, where the score register 8 t + j has it.  A transposing load gives lane i of 16 column i of
+  // 4 rows of 16 elements, of which lane 4 r + c addresses 4 elements of row r from column 4 c on.
+  __device__ __forceinline__ u32x4 value_piece(int r0, int dt, int t) const {
+    const int vrow = r0 + half * 4 + (lane % 16) / 4, vcol = ((lane / 16) & 1) * 16 + (lane % 4) * 4;
+    const lchar* const at = lds + TK * RB + (vrow + 16 * t) * RB + (vcol % 8) * 2 + (((dt * 4 + vcol / 8) ^ L::swz_v(vrow)) << 4);
+    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ADSA_LDS i16x4*)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ADSA_LDS i16x4*)(at + 8 * RB));
+    const u32x2 a = __builtin_bit_cast(u32x2, lo), b = __builtin_bit_cast(u32x2, hi);
+    return u32x4{a.x, a.y, b.x, b.y};
+  }
+  // fp32: element dt * 32 + lane % 32 of the key that score register i of this half belongs to
+  __device__ __forceinline__ float value(int r0, int i, int dt) const {
+    const int key = r0 + (i / 4) * 8 + half * 4 + i % 4;
+    return *(const ADSA_LDS float*)(lds + TK * RB + key * RB + (((dt * 8 + col / 4) ^ L::swz_v(key)) << 4) + (col % 4) * 4);
+  }
   // O^T += V^T P^T over the 32 keys from row r0 of the step; TIDY: infinities and NaN of V count as 0
   template <bool TIDY>
   __device__ __forceinline__ void add_values(int r0, const float* p) {
-    const lchar* const v = lds + TK * RB;
     if constexpr (EB == 2) {
       bf16x8 pb[2];
 #pragma unroll
@@ -204,35 +228,23 @@ struct Tile {
                          pack2_bf16(p[8 * t + 6], p[8 * t + 7])};
         pb[t] = __builtin_bit_cast(bf16x8, w);
       }
-      // element j of a lane of half h belongs to key 16 t + 8 (j / 4) + 4 h + j % 4: where the score register 8 t + j has it.  A transposing load
-      // gives lane i of 16 column i of 4 rows of 16 elements, of which lane 4 r + c addresses 4 elements of row r from column 4 c on.
-      const int vrow = r0 + half * 4 + (lane % 16) / 4, vcol = ((lane / 16) & 1) * 16 + (lane % 4) * 4;
-      const lchar* const at = v + vrow * RB + (vcol % 8) * 2;
-      const int sw = L::swz_v(vrow);
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const lchar* const from = at + (((dt * 4 + vcol / 8) ^ sw) << 4);
+      for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ADSA_LDS i16x4*)(from + (16 * t) * RB));
-          const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ADSA_LDS i16x4*)(from + (16 * t + 8) * RB));
-          const u32x2 a = __builtin_bit_cast(u32x2, lo), b = __builtin_bit_cast(u32x2, hi);
-          u32x4 w = {a.x, a.y, b.x, b.y};
+          u32x4 w = value_piece(r0, dt, t);
           if constexpr (TIDY) w = u32x4{bf16_finite(w.x), bf16_finite(w.y), bf16_finite(w.z), bf16_finite(w.w)};
           acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pb[t], acc[dt], 0, 0, 0);
         }
-      }
     } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int key = r0 + (i / 4) * 8 + half * 4 + i % 4, sw = L::swz_v(key);
+      for (int i = 0; i < 16; ++i)
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
-          float a = *(const ADSA_LDS float*)(v + key * RB + (((dt * 8 + col / 4) ^ sw) << 4) + (col % 4) * 4);
+          float a = value(r0, i, dt);
           if constexpr (TIDY) a = f32_bad(a) ? 0.0f : a;
           acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[i], acc[dt], 0, 0, 0);
         }
-      }
     }
   }
   // whether V of these 32 keys holds an infinity or a NaN
@@ -246,27 +258,36 @@ struct Tile {
     }
     return __ballot(bad) != 0;
   }
-  // ... and what those give the rows that see their key (rare: one key after the other)
+  // ... and what those give the rows that see their key: where V holds +infinity (and where -infinity, NaN counting as both) the
+  // product of ones there with ones for p > 0 says which rows have one among their keys.
   __device__ __forceinline__ void add_bad_values(int r0, const float* p) {
-    for (int key = 0; key < 32; ++key) {
-      const int reg = key / 8 * 4 + key % 4;
-      float x = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x = i == reg ? p[i] : x;
-      x = __shfl(x, col + 32 * ((key >> 2) & 1));
-      const int r = r0 + key, sw = L::swz_v(r);
-      const lchar* const v = lds + TK * RB + r * RB;
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
+      for (int negative = 0; negative < 2; ++negative) {
+        f32x16 r = {};
+        if constexpr (EB == 2) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int d = dt * 32 + (i / 4) * 8 + half * 4 + i % 4, at = (((d * EB / 16) ^ sw) << 4) + d * EB % 16;
-          float a;
-          if constexpr (EB == 2) a = __uint_as_float((uint32_t)*(const ADSA_LDS uint16_t*)(v + at) << 16);
-          else a = *(const ADSA_LDS float*)(v + at);
-          if (x > 0.0f && f32_bad(a)) acc[dt][i] += x * a;
+          for (int t = 0; t < 2; ++t) {
+            const u32x4 w = value_piece(r0, dt, t);
+            u32x4 x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = (p[8 * t + 2 * i] > 0.0f ? 0x3F80u : 0u) | (p[8 * t + 2 * i + 1] > 0.0f ? 0x3F800000u : 0u);
+            const u32x4 o = {ones_at(w.x, negative), ones_at(w.y, negative), ones_at(w.z, negative), ones_at(w.w, negative)};
+            r = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, o), __builtin_bit_cast(bf16x8, x), r, 0, 0, 0);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float a = value(r0, i, dt);
+            const bool hit = a != a || a == (negative ? -INFINITY : INFINITY);
+            r = __builtin_amdgcn_mfma_f32_32x32x2f32(hit ? 1.0f : 0.0f, p[i] > 0.0f ? 1.0f : 0.0f, r, 0, 0, 0);
+          }
         }
-    }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[dt][i] += r[i] > 0.0f ? (negative ? -INFINITY : INFINITY) : 0.0f;
+        __builtin_amdgcn_sched_barrier(0);           // (one after the other: registers matter here, time does not)
+      }
   }
 
   // one step's keys of this wave; masked: some row does not see all of them
@@ -362,7 +383,7 @@ struct Tile {
     l += sum;
 #pragma unroll
     for (int u = 0; u < SUB; ++u) {
-      if (masked && values_bad(r0 + u * 32)) {
+      if (!ALL && masked && values_bad(r0 + u * 32)) {
         add_bad_values(r0 + u * 32, p[u]);
         add_values<true>(r0 + u * 32, p[u]);
       } else add_values<false>(r0 + u * 32, p[u]);
@@ -565,10 +586,6 @@ struct Flow {
   }
   // ... and what those give the rows that see their key: where V holds +infinity (and where -infinity, NaN counting as both) the
   // product of ones there with ones for p > 0 says which rows have one among their keys.
-  static __device__ __forceinline__ uint32_t ones_at(uint32_t w, bool negative) {
-    auto hit = [&](uint32_t h) { return (h & 0x7FFFu) > 0x7F80u || h == (negative ? 0xFF80u : 0x7F80u); };
-    return (hit(w & 0xFFFFu) ? 0x3F80u : 0u) | (hit(w >> 16) ? 0x3F800000u : 0u);
-  }
   __device__ __forceinline__ void add_bad_values(int sub) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -586,6 +603,7 @@ struct Flow {
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[dt][i] += r[i] > 0.0f ? (negative ? -INFINITY : INFINITY) : 0.0f;
+        __builtin_amdgcn_sched_barrier(0);           // (one after the other: registers matter here, time does not)
       }
   }
 
@@ -904,8 +922,8 @@ __device__ __forceinline__ void store_lse(const PromptArgs& A, size_t at, float 
 }
 
 template <int EB, int D, int WR, int WK, int KT, bool MOD>
-__global__ __launch_bounds__(WR * WK * kWave) void k_prompt(PromptArgs A) {
-  using T = Tile<EB, D, WR, WK, KT, MOD, false>;
+__global__ __launch_bounds__(WR * WK * kWave, EB == 2 && D == 64 ? 2 : 1) void k_prompt(PromptArgs A) {
+  using T = Tile<EB, D, WR, WK, KT, MOD, false, false>;
   using S = typename T::S;
   extern __shared__ __align__(16) char s_lds[];
   Job J;
@@ -1148,8 +1166,98 @@ __device__ __forceinline__ Group group_at(const SharedArgs& A, int g) {
   return gr;
 }
 
-template <int EB, int D, int WK, bool MOD>
-__global__ __launch_bounds__(WK * kWave) void k_shared(SharedArgs A) {
+// One query head over a part of its sequence's own list: nothing is shared, so there is no matrix product; bound by the rows' way from HBM.
+// 16 bytes of a row per lane, 64 / (row bytes / 16) tokens ("a unit") per load of a wave; kRing units of K and V are on their way at any time, and
+// a unit's registers are refilled as soon as it is folded into its lanes' softmax states.  Entries that are not attended read the query's
+// row instead (whatever the cache holds there must not reach the sums, not even times 0).
+template <int EB, int D, int NW, bool MOD>
+__device__ __forceinline__ void own_list(const Mods& mods, const Keys& keys, const gchar* q_row, float slope, int q_pos, gfloat* part_ml, gfloat* part_acc, lchar* lds) {
+  constexpr int EPL = Elems<EB>::N, LPR = D / EPL, RPW = kWave / LPR, kRing = 8;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), dl = lane % LPR, ts = lane / LPR;
+  const gchar* const mine = q_row + dl * 16;
+  const Elems<EB> q(load16(mine), MOD ? 1.0f : mods.scale_log2);
+  const int units = (keys.end - keys.begin + RPW - 1) / RPW, n = units > wave ? (units - wave + NW - 1) / NW : 0;      // of this wave
+  const int first = keys.begin + wave * RPW + ts;      // the lane's entry in the wave's first unit
+  uint4 kr[kRing], vr[kRing];
+  int ent[kRing], next[kRing], pos[kRing];
+  auto entry = [&](int i) { return keys.list[min(first + i * NW * RPW, keys.end - 1)]; };
+  auto load = [&](int u, int i) {
+    const int slot = min(max(next[u], 0), keys.last_slot);
+    const bool on = first + i * NW * RPW < keys.end && next[u] != keys.skip;
+    ent[u] = on ? slot : -1;
+    const long long off = (long long)slot * keys.stride_b + dl * 16;
+    kr[u] = load_stream16(on ? keys.k + off : mine);
+    vr[u] = load_stream16(on ? keys.v + off : mine);
+    if (MOD && mods.slopes) pos[u] = keys.pos[slot];
+  };
+#pragma unroll
+  for (int u = 0; u < kRing; ++u) next[u] = entry(u);
+#pragma unroll
+  for (int u = 0; u < kRing; ++u) {
+    load(u, u);
+    next[u] = entry(u + kRing);
+  }
+  float m = kLowest, l = 0.0f, acc[EPL];
+#pragma unroll
+  for (int e = 0; e < EPL; ++e) acc[e] = 0.0f;
+  for (int i0 = 0; i0 < n; i0 += kRing)
+#pragma unroll
+    for (int u = 0; u < kRing; ++u) {
+      if (i0 + u >= n) break;                        // (uniform)
+      float z = row_sum<LPR>(q.dot(kr[u]));
+      if constexpr (MOD) {
+        z = mods.cap_out != 0.0f ? capped<EB>(z, mods) : z * mods.scale_log2;
+        if (mods.slopes) z = fmaf(-slope, fabsf((float)q_pos - (float)pos[u]), z);
+      } else z = Elems<EB>::scaled(z, mods.scale_log2);
+      z = ent[u] >= 0 ? z : -INFINITY;
+      const int j = first + (i0 + u) * NW * RPW;
+      if (keys.logits && dl == 0 && j < keys.end) keys.logits[j] = z;
+      const float m_new = fmaxf(m, z), corr = fast_exp2(m - m_new), p = fast_exp2(z - m_new);
+      m = m_new;
+      l = fmaf(l, corr, p);
+      float v[EPL];
+      Elems<EB>::unpack(vr[u], v);
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) acc[e] = fmaf(acc[e], corr, p * v[e]);
+      load(u, i0 + u + kRing);
+      next[u] = entry(i0 + u + 2 * kRing);
+    }
+  // the wave's groups of lanes, then its waves
+  float M = m;
+#pragma unroll
+  for (int x = LPR; x < kWave; x <<= 1) M = x == 8 ? xor_max<8>(M) : x == 16 ? xor_max<16>(M) : xor_max<32>(M);
+  const float w = fast_exp2(m - M);
+  l *= w;
+#pragma unroll
+  for (int x = LPR; x < kWave; x <<= 1) l = x == 8 ? xor_sum<8>(l) : x == 16 ? xor_sum<16>(l) : xor_sum<32>(l);
+  ADSA_LDS float* const s_acc = (ADSA_LDS float*)lds;
+  ADSA_LDS float* const s_ml = s_acc + NW * D;
+#pragma unroll
+  for (int e = 0; e < EPL; ++e) {
+    float x = acc[e] * w;
+#pragma unroll
+    for (int y = LPR; y < kWave; y <<= 1) x = y == 8 ? xor_sum<8>(x) : y == 16 ? xor_sum<16>(x) : xor_sum<32>(x);
+    if (ts == 0) s_acc[wave * D + dl * EPL + e] = x;
+  }
+  if (lane == 0) { s_ml[wave] = M; s_ml[NW + wave] = l; }
+  __syncthreads();
+  if (tid < D) {
+    float top = kLowest, sum = 0.0f, x = 0.0f;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) top = fmaxf(top, s_ml[k]);
+#pragma unroll
+    for (int k = 0; k < NW; ++k) {
+      const float f = fast_exp2(s_ml[k] - top);
+      sum = fmaf(s_ml[NW + k], f, sum);
+      x = fmaf(s_acc[k * D + tid], f, x);
+    }
+    part_acc[tid] = x;
+    if (tid == 0) { part_ml[0] = top; part_ml[1] = sum; }
+  }
+}
+
+template <int EB, int D, int WK, bool MOD, bool ONE>
+__global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(SharedArgs A) {
   extern __shared__ __align__(16) char s_lds[];
   const int hq = A.h * A.G, C = A.prompt_chunks + A.own_chunks;
   Keys keys;
@@ -1194,7 +1302,7 @@ __global__ __launch_bounds__(WK * kWave) void k_shared(SharedArgs A) {
     const int per = ((gr.n + A.prompt_chunks - 1) / A.prompt_chunks + 31) / 32 * 32;
     keys.begin = min(gr.n, chunk * per);
     keys.end = min(gr.n, keys.begin + per);
-    Tile<EB, D, 1, WK, 32, MOD, false> t(A.mods, keys, (lchar*)s_lds);
+    Tile<EB, D, 1, WK, 32, MOD, false, true> t(A.mods, keys, (lchar*)s_lds);
     const int r = tile * 32 + t.col, rr = min(r, rows - 1), b = gr.first + rr / A.G, qh = head * A.G + rr % A.G;
     const size_t at = (size_t)b * hq + qh;
     if (keys.begin >= keys.end) {
@@ -1225,9 +1333,20 @@ __global__ __launch_bounds__(WK * kWave) void k_shared(SharedArgs A) {
   keys.end = min(cnt, keys.begin + per);
   const size_t at0 = (size_t)b * hq + head * A.G;
   keys.logits = A.accumulate ? (gfloat*)A.logits + at0 * A.lg_stride : nullptr;
+  if constexpr (ONE) {
+    if (keys.begin >= keys.end) {
+      if (threadIdx.x == 0) nothing(at0, A.prompt_chunks + chunk);
+      return;
+    }
+    const size_t part = at0 * C + A.prompt_chunks + chunk;
+    const bool far = MOD && A.mods.slopes;
+    own_list<EB, D, WK, MOD>(A.mods, keys, (const gchar*)A.q + at0 * (D * EB), far ? ((const gfloat*)A.mods.slopes)[head] * kLog2e : 0.0f, far ? query_pos(b) : 0,
+                             (gfloat*)A.part_ml + part * 2, (gfloat*)A.part_acc + part * D, (lchar*)s_lds);
+    return;
+  }
   keys.lg_stride = A.lg_stride;
   keys.lg_rows = A.G;
-  Tile<EB, D, 1, WK, 32, MOD, true> t(A.mods, keys, (lchar*)s_lds);
+  Tile<EB, D, 1, WK, 32, MOD, true, true> t(A.mods, keys, (lchar*)s_lds);
   const size_t at = at0 + min(t.col, A.G - 1);
   // (a part that holds the query token alone has no other row to stand in for it)
   if (keys.begin >= keys.end || (keys.end - keys.begin == 1 && keys.list[keys.begin] == keys.skip)) {
@@ -1241,45 +1360,48 @@ __global__ __launch_bounds__(WK * kWave) void k_shared(SharedArgs A) {
   if (t.col < A.G) store(t, at, A.prompt_chunks + chunk);
 }
 
-// Joins the parts of a (sequence, cache head)'s rows with the query token, whose row enters the cache, and updates the scores.
+// Joins the parts of a (sequence, cache head)'s rows with the query token, whose row enters the cache, and updates the scores.  Bound by the trips
+// that depend on each other (record; parts, list and scores' logits; scores), so everything leaves as soon as its address is known.
 constexpr int kMaxParts = 2 * kMaxChunks;
-template <int EB, int D>
+template <int EB, int D, bool ONE>
 __global__ __launch_bounds__(256) void k_shared_finish(SharedArgs A) {
-  __shared__ float s_w[16][kMaxParts + 1], s_l[16][kMaxParts], s_lse[16], s_new[16], s_inv[16];
+  constexpr int NT = 256, E = D / kWave, kMaxG = ONE ? 1 : 16, kEarly = 3, kAcc = 4;
+  __shared__ float s_w[kMaxG][kMaxParts + 1], s_l[kMaxG][kMaxParts], s_lse[kMaxG], s_new[kMaxG], s_inv[kMaxG];
+  __shared__ __attribute__((aligned(16))) float s_v[D];
   __shared__ int s_has;
-  const int b = blockIdx.x / A.h, head = blockIdx.x % A.h, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  const int hq = A.h * A.G, C = A.prompt_chunks + A.own_chunks;
-  const size_t at0 = (size_t)b * hq + head * A.G;
+  const int b = blockIdx.x / A.h, head = blockIdx.x % A.h, tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int G = ONE ? 1 : A.G, hq = A.h * G, C = A.prompt_chunks + A.own_chunks;
+  const size_t at0 = (size_t)b * hq + head * G, row = ((size_t)b * A.h + head) * D;
   ADSA_GLOBAL adsa_seq& sq = ((ADSA_GLOBAL adsa_seq*)A.seqs)[b];
-  int lo = 0, hi = A.n_groups;                        // the sequence's group
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (((const gint*)A.members)[mid] <= b) lo = mid; else hi = mid;
-  }
-  const Group gr = group_at(A, lo);
-  const bool fits = gr.n >= 0 && gr.first <= b && b < gr.end, live = sq.status == 0 && sq.step >= 0;
-  if (!live || !fits) {
-    if (live && head == 0 && tid == 0) sq.status = ADSA_SEQ_BAD_STATE;
-    for (int o = tid; o < A.G * D * EB / 4; o += 256) ((gint*)(A.out + at0 * D * EB))[o] = 0;
-    for (int o = tid; o < A.G; o += 256) ((gfloat*)A.lse)[at0 + o] = 0.0f;
-    return;
-  }
-  if (tid == 0) s_has = 0;
-  const int cnt = min(max(((const gint*)A.sel_cnt)[b], 0), A.sel_cap);
   const gint* const list = (const gint*)A.sel_idx + (size_t)b * A.sel_cap;
-  const int pending = A.append ? sq.pending_slot : -1, new_slot = pending >= 0 && pending < A.cap ? pending : -1;
-  for (int o = tid; o < A.G * C; o += 256) {
-    const int g = o / C, c = o % C;
-    const gfloat* const ml = (const gfloat*)A.part_ml + ((at0 + g) * C + c) * 2;
-    s_w[g][c] = ml[0];
-    s_l[g][c] = ml[1];
+  // ---- what depends on the arguments only
+  const int status = sq.status, step = sq.step, pending = sq.pending_slot;
+  gfloat* const score = (gfloat*)sq.score + (size_t)head * A.cap;
+  int cnt = ((const gint*)A.sel_cnt)[b], g = -1;
+  for (int i = 0; i < A.n_groups; i += kWave)          // the sequence's group: the last that begins at or before it
+    g += __popcll(__ballot(i + lane < A.n_groups && ((const gint*)A.members)[min(i + lane, A.n_groups - 1)] <= b));
+  int slot[kEarly];
+  float old[kEarly], lg[kEarly];
+#pragma unroll
+  for (int k = 0; k < kEarly; ++k) {
+    slot[k] = list[min(tid + k * NT, A.sel_cap - 1)];
+    if (ONE && A.accumulate) lg[k] = ((const gfloat*)A.logits)[at0 * A.lg_stride + min(tid + k * NT, A.sel_cap - 1)];
   }
-  // the query token's own row: its score with every query head
-  constexpr int E = D / kWave;
+  for (int o = tid; o < G * C; o += NT) {
+    const gfloat* const ml = (const gfloat*)A.part_ml + (at0 * C + o) * 2;
+    s_w[o / C][o % C] = ml[0];
+    s_l[o / C][o % C] = ml[1];
+  }
+  // the parts' outputs: 4 elements of a query head per thread, the first parts at once
+  const int items = G * (D / 4), oh = tid / (D / 4), oe = tid % (D / 4) * 4;
+  auto part_of = [&](int h, int c) { return *(const ADSA_GLOBAL u32x4*)((const gfloat*)A.part_acc + ((at0 + h) * C + c) * D + oe); };
+  u32x4 parts[kAcc];
+  if (tid < items) {
+#pragma unroll
+    for (int c = 0; c < kAcc; ++c) parts[c] = part_of(oh, min(c, C - 1));
+  }
   float kn[E], vn[E];
-  const size_t row = ((size_t)b * A.h + head) * D;
-  __syncthreads();
-  if (new_slot >= 0) {
+  if (A.append) {
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const size_t o = row + e * kWave + lane;
@@ -1294,83 +1416,113 @@ __global__ __launch_bounds__(256) void k_shared_finish(SharedArgs A) {
         kn[e] = __uint_as_float((uint32_t)((const ADSA_GLOBAL uint16_t*)A.k_new)[o] << 16);
         vn[e] = __uint_as_float((uint32_t)((const ADSA_GLOBAL uint16_t*)A.v_new)[o] << 16);
       }
-      if (wave == 0) {
-        gchar* const kc = (gchar*)sq.k + head * A.head_stride_b + new_slot * A.slot_stride_b;
-        gchar* const vc = (gchar*)sq.v + head * A.head_stride_b + new_slot * A.slot_stride_b;
+    }
+  }
+  const Group gr = group_at(A, max(g, 0));
+  const bool fits = gr.n >= 0 && gr.first <= b && b < gr.end, live = status == 0 && step >= 0;
+  if (!live || !fits) {
+    if (live && head == 0 && tid == 0) sq.status = ADSA_SEQ_BAD_STATE;
+    for (int o = tid; o < G * D * EB / 4; o += NT) ((gint*)(A.out + at0 * D * EB))[o] = 0;
+    for (int o = tid; o < G; o += NT) ((gfloat*)A.lse)[at0 + o] = 0.0f;
+    return;
+  }
+  cnt = min(max(cnt, 0), A.sel_cap);
+  const int new_slot = A.append && pending >= 0 && pending < A.cap ? pending : -1;
+  bool mine = false;
+#pragma unroll
+  for (int k = 0; k < kEarly; ++k) {
+    const bool in = tid + k * NT < cnt;
+    mine |= in && slot[k] == new_slot;
+    old[k] = 0.0f;
+    if (A.accumulate && in) old[k] = score[min(max(slot[k], 0), A.cap - 1)];
+  }
+  for (int j = tid + kEarly * NT; j < cnt; j += NT) mine |= list[j] == new_slot;
+  if (tid == 0) s_has = 0;
+  __syncthreads();
+  if (new_slot >= 0) {
+    if (mine) s_has = 1;
+    if (wave == 0) {                                 // the query token's row enters the cache
+      gchar* const kc = (gchar*)sq.k + head * A.head_stride_b + new_slot * A.slot_stride_b;
+      gchar* const vc = (gchar*)sq.v + head * A.head_stride_b + new_slot * A.slot_stride_b;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
         if constexpr (EB == 4) { ((gfloat*)kc)[e * kWave + lane] = kn[e]; ((gfloat*)vc)[e * kWave + lane] = vn[e]; }
         else {
           ((ADSA_GLOBAL uint16_t*)kc)[e * kWave + lane] = (uint16_t)(__float_as_uint(kn[e]) >> 16);
           ((ADSA_GLOBAL uint16_t*)vc)[e * kWave + lane] = (uint16_t)(__float_as_uint(vn[e]) >> 16);
         }
+        s_v[e * kWave + lane] = vn[e];
       }
     }
-    for (int j = tid; j < cnt; j += 256)
-      if (list[j] == new_slot) s_has = 1;
-    for (int g = wave; g < A.G; g += 4) {
+    for (int h = wave; h < G; h += NT / kWave) {     // its score with every query head
       float z = 0.0f;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const size_t o = (at0 + g) * D + e * kWave + lane;
+        const size_t o = (at0 + h) * D + e * kWave + lane;
         const float x = EB == 4 ? ((const gfloat*)A.q)[o] : __uint_as_float((uint32_t)((const ADSA_GLOBAL uint16_t*)A.q)[o] << 16);
         z = fmaf(x, kn[e], z);
       }
-#pragma unroll
-      for (int x = 1; x < kWave; x <<= 1) z += __shfl_xor(z, x);
+      z = row_sum<32>(z);
+      z = xor_sum<32>(z);
       z = A.mods.cap_out != 0.0f ? capped<EB>(z, A.mods) : z * A.mods.scale_log2;      // (its distance to itself is 0)
-      if (lane == 0) s_new[g] = z;
+      if (lane == 0) s_new[h] = z;
     }
   }
   __syncthreads();
   const bool has = new_slot >= 0 && s_has != 0;
-  if (tid < A.G) {
-    float M = has ? s_new[tid] : kLowest, sum;
+  if (tid < G) {
+    float M = has ? s_new[tid] : kLowest;
     for (int c = 0; c < C; ++c) M = fmaxf(M, s_w[tid][c]);
     const float pn = has ? fast_exp2(s_new[tid] - M) : 0.0f;
-    sum = pn;
+    float sum = pn;
     for (int c = 0; c < C; ++c) {
       const float w = s_l[tid][c] == 0.0f ? 0.0f : fast_exp2(s_w[tid][c] - M);
       s_w[tid][c] = w;
       sum = fmaf(s_l[tid][c], w, sum);
     }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     s_w[tid][C] = pn;
-    s_inv[tid] = inv;
+    s_inv[tid] = sum == 0.0f ? 0.0f : 1.0f / sum;
     s_lse[tid] = M + __log2f(sum);
     ((gfloat*)A.lse)[at0 + tid] = sum == 0.0f ? -INFINITY : s_lse[tid] * kLn2;
   }
   __syncthreads();
-  for (int g = wave; g < A.G; g += 4) {
-    float x[E];
+  for (int o = tid; o < items; o += NT) {
+    const int h = o / (D / 4);                       // (NT is a multiple of D / 4: the same elements in every round)
+    float x[4];
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = has ? s_w[g][C] * vn[e] : 0.0f;
-    const gfloat* const acc = (const gfloat*)A.part_acc + (at0 + g) * C * D;
-    for (int c = 0; c < C; ++c) {
-      const float w = s_w[g][c];
-      if (s_l[g][c] == 0.0f) continue;               // (nothing was stored)
+    for (int e = 0; e < 4; ++e) x[e] = has ? s_w[h][C] * s_v[oe + e] : 0.0f;
+    auto add = [&](int c, const u32x4& part) {
+      const float w = s_w[h][c];
+      const bool there = s_l[h][c] != 0.0f;          // (else nothing was stored)
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = fmaf(acc[(size_t)c * D + e * kWave + lane], w, x[e]);
-    }
+      for (int e = 0; e < 4; ++e) x[e] = there ? fmaf(__uint_as_float(part[e]), w, x[e]) : x[e];
+    };
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const size_t o = (at0 + g) * D + e * kWave + lane;
-      if constexpr (EB == 4) ((gfloat*)A.out)[o] = x[e] * s_inv[g];
-      else ((ADSA_GLOBAL uint16_t*)A.out)[o] = (uint16_t)f32_to_bf16_rne(x[e] * s_inv[g]);
-    }
+    for (int c = 0; c < kAcc; ++c)
+      if (c < C) add(c, o == tid ? parts[c] : part_of(h, c));
+    for (int c = kAcc; c < C; ++c) add(c, part_of(h, c));
+    store4<EB>((gchar*)A.out + ((at0 + h) * D + oe) * EB, x[0] * s_inv[h], x[1] * s_inv[h], x[2] * s_inv[h], x[3] * s_inv[h]);
   }
   if (A.accumulate) {
-    gfloat* const score = (gfloat*)sq.score + (size_t)head * A.cap;
-    for (int j = tid; j < cnt; j += 256) {
-      const int slot = min(max(list[j], 0), A.cap - 1);
-      const bool is_new = list[j] == new_slot && new_slot >= 0;
+    auto update = [&](int j, int raw, float before, float first) {
+      const bool is_new = raw == new_slot && new_slot >= 0;
       float gain = 0.0f;
-      for (int g = 0; g < A.G; ++g) {
-        const float z = is_new ? s_new[g] : ((const gfloat*)A.logits)[(at0 + g) * A.lg_stride + j];
-        gain += fast_exp2(z - s_lse[g]);
+      if constexpr (ONE) gain = fast_exp2((is_new ? s_new[0] : first) - s_lse[0]);
+      else {
+#pragma unroll 4
+        for (int h = 0; h < G; ++h) gain += fast_exp2((is_new ? s_new[h] : ((const gfloat*)A.logits)[(at0 + h) * A.lg_stride + j]) - s_lse[h]);
       }
-      score[slot] = score[slot] + gain;
+      score[min(max(raw, 0), A.cap - 1)] = before + gain;
+    };
+#pragma unroll
+    for (int k = 0; k < kEarly; ++k)
+      if (tid + k * NT < cnt) update(tid + k * NT, slot[k], old[k], ONE ? lg[k] : 0.0f);
+    for (int j = tid + kEarly * NT; j < cnt; j += NT) {
+      const int raw = list[j];
+      update(j, raw, score[min(max(raw, 0), A.cap - 1)], ONE ? ((const gfloat*)A.logits)[at0 * A.lg_stride + j] : 0.0f);
     }
   }
-  if (A.advance && head == 0 && tid == 0) sq.step = sq.step + 1;
+  if (A.advance && head == 0 && tid == 0) sq.step = step + 1;
 }
 
 Mods make_mods(const adsa_params& p, const adsa_mods& m) {
@@ -1416,8 +1568,11 @@ hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStrea
 template <int EB, int D, bool MOD>
 hipError_t shared_launches(const SharedArgs& A, hipStream_t st) {
   constexpr int KW = kKeyWaves<EB, D>;
-  k_shared<EB, D, KW, MOD><<<dim3((unsigned)(A.prompt_blocks + A.n_seq * A.h * A.own_chunks)), KW * kWave, Shape<EB, D, 1, KW, 32>::kLds, st>>>(A);
-  k_shared_finish<EB, D><<<dim3((unsigned)(A.n_seq * A.h)), 256, 0, st>>>(A);
+  const dim3 grid((unsigned)(A.prompt_blocks + A.n_seq * A.h * A.own_chunks));
+  if (A.G == 1) k_shared<EB, D, KW, MOD, true><<<grid, KW * kWave, Shape<EB, D, 1, KW, 32>::kLds, st>>>(A);
+  else k_shared<EB, D, KW, MOD, false><<<grid, KW * kWave, Shape<EB, D, 1, KW, 32>::kLds, st>>>(A);
+  if (A.G == 1) k_shared_finish<EB, D, true><<<dim3((unsigned)(A.n_seq * A.h)), 256, 0, st>>>(A);
+  else k_shared_finish<EB, D, false><<<dim3((unsigned)(A.n_seq * A.h)), 256, 0, st>>>(A);
   return hipGetLastError();
 }
 
@@ -1431,7 +1586,8 @@ hipError_t allow_lds() {
   allow(k_prompt<EB, D, 1, KW, 32, MOD>, Shape<EB, D, 1, KW, 32>::kLds);
   allow(k_prompt<EB, D, 4, 1, KT, MOD>, Shape<EB, D, 4, 1, KT>::kLds);
   allow(k_prompt_mass<EB, D, MOD>, MassLds<EB, D>::kLds);
-  allow(k_shared<EB, D, KW, MOD>, Shape<EB, D, 1, KW, 32>::kLds);
+  allow(k_shared<EB, D, KW, MOD, true>, Shape<EB, D, 1, KW, 32>::kLds);
+  allow(k_shared<EB, D, KW, MOD, false>, Shape<EB, D, 1, KW, 32>::kLds);
   if constexpr (EB == 2) {
     allow(k_prompt_many<D, 4, MOD>, Flow<D, 4, MOD>::kLds);
     allow(k_prompt_many<D, 8, MOD>, Flow<D, 8, MOD>::kLds);
