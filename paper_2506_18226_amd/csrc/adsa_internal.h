@@ -146,7 +146,8 @@ struct PromptWorkspace {
 PromptWorkspace make_prompt_workspace(const adsa_params& p, const adsa_tokens& t, const PromptPlan& plan);
 
 struct SharedPlan {
-  int prompt_tiles;     // tiles of 32 (member, query head) rows per (group, cache head)
+  bool big;             // prompts are met by 128 rows at a time, else by 32
+  int prompt_tiles;     // tiles of so many (member, query head) rows per (group, cache head)
   int prompt_chunks, own_chunks;       // parts that a prompt's slots and a list are split into
 };
 SharedPlan make_shared_plan(const adsa_params& p, const adsa_shared& s);

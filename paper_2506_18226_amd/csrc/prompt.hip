@@ -38,6 +38,12 @@ __device__ __forceinline__ void each(F f, std::integer_sequence<int, I...>) { (f
 template <int N, typename F>
 __device__ __forceinline__ void each(F f) { each(f, std::make_integer_sequence<int, N>()); }
 
+template <int EB>
+__device__ __forceinline__ void store4(gchar* p, float a, float b, float c, float d) {
+  if constexpr (EB == 4) *(ADSA_GLOBAL u32x4*)p = u32x4{__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d)};
+  else *(ADSA_GLOBAL u32x2*)p = u32x2{pack2_bf16(a, b), pack2_bf16(c, d)};
+}
+
 // What is done to scores before the softmax.
 struct Mods {
   const float* slopes;         // per query head, or NULL
@@ -127,9 +133,11 @@ struct Tile {
   using L = Layout<EB, D>;
   using S = Shape<EB, D, WR, WK, KT>;
   static constexpr int NT = S::kThreads, TK = S::TK, CPR = L::CPR, RB = L::RB, SUB = KT / 32, DT = D / 32;
-  static constexpr int RPT = NT / CPR, NL = TK / RPT;                   // rows per round of the threads; rounds
+  // Where the waves split the keys (WR == 1) each stages the rows that it alone reads, and nobody waits for anybody in the loop.
+  static constexpr bool kAlone = WR == 1;
+  static constexpr int RPT = (kAlone ? kWave : NT) / CPR, NL = (kAlone ? KT : TK) / RPT;      // rows per round of those who stage; rounds
   static constexpr int kMine = DT * 16 / WK;                            // output registers of a lane after the waves' merge
-  static_assert(TK % RPT == 0 && NT >= TK && kMine % 4 == 0, "whole rounds");
+  static_assert(NL * RPT == (kAlone ? KT : TK) && NT >= TK && KT <= kWave && kMine % 4 == 0, "whole rounds");
 
   const Mods& mods;
   const Keys& keys;
@@ -150,6 +158,14 @@ struct Tile {
       : mods(mods_), keys(keys_), lds(lds_), tid(threadIdx.x), lane(threadIdx.x % kWave), col(lane % 32), half(lane / 32),
         wr(__builtin_amdgcn_readfirstlane(tid / kWave) % WR), wk(__builtin_amdgcn_readfirstlane(tid / kWave) / WR) {}
 
+  // row number i of the thread among a step's, and the one whose position, document and flag it brings (if `brings`)
+  __device__ __forceinline__ int staged(int i) const { return (kAlone ? wk * KT + lane / CPR : tid / CPR) + i * RPT; }
+  __device__ __forceinline__ bool brings() const { return kAlone ? lane < KT : tid < TK; }
+  __device__ __forceinline__ int brought() const { return kAlone ? wk * KT + lane : tid; }
+  __device__ __forceinline__ void meet() const {
+    if constexpr (!kAlone) __syncthreads();
+  }
+
   __device__ __forceinline__ void load_q(const gchar* q_row) {
 #pragma unroll
     for (int s = 0; s < CPR / 2; ++s) qf[s] = load16(q_row + (2 * s + half) * 16);
@@ -167,22 +183,22 @@ struct Tile {
   __device__ __forceinline__ void load_slots(int base) {
     if constexpr (LIST) {
 #pragma unroll
-      for (int i = 0; i < NL; ++i) slot_next[i] = slot_at(base + tid / CPR + i * RPT);
+      for (int i = 0; i < NL; ++i) slot_next[i] = slot_at(base + staged(i));
     }
   }
   __device__ __forceinline__ void load_rows(int base) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int slot = LIST ? slot_next[i] : slot_at(base + tid / CPR + i * RPT);
+      const int slot = LIST ? slot_next[i] : slot_at(base + staged(i));
       const long long off = (long long)slot * keys.stride_b + (tid % CPR) * 16;
       kr[i] = load16(keys.k + off);
       vr[i] = load16(keys.v + off);
     }
-    if (tid < TK) {
-      const int at = min(base + tid, keys.end - 1);
+    if (brings()) {
+      const int at = min(base + brought(), keys.end - 1);
       if constexpr (LIST) meta_slot = keys.list[at];
       if constexpr (MOD) {
-        const int slot = slot_at(base + tid);
+        const int slot = slot_at(base + brought());
         meta_pos = mods.slopes ? (float)keys.pos[slot] : 0.0f;
         meta_doc = keys.doc ? keys.doc[slot] : 0;
       }
@@ -191,14 +207,14 @@ struct Tile {
   __device__ __forceinline__ void store_rows() {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int r = tid / CPR + i * RPT, c = tid % CPR;
+      const int r = staged(i), c = tid % CPR;
       put16(lds + r * RB + ((c ^ L::swz_k(r)) << 4), kr[i]);
       put16(lds + TK * RB + r * RB + ((c ^ L::swz_v(r)) << 4), vr[i]);
     }
-    if (tid < TK) {
-      ADSA_LDS int* const meta = (ADSA_LDS int*)(lds + S::kMeta);
-      if constexpr (MOD) { meta[tid] = __float_as_int(meta_pos); meta[TK + tid] = meta_doc; }
-      if constexpr (LIST) meta[2 * TK + tid] = meta_slot == keys.skip;
+    if (brings()) {
+      ADSA_LDS int* const meta = (ADSA_LDS int*)(lds + S::kMeta) + brought();
+      if constexpr (MOD) { meta[0] = __float_as_int(meta_pos); meta[TK] = meta_doc; }
+      if constexpr (LIST) meta[2 * TK] = meta_slot == keys.skip;
     }
   }
 
@@ -347,13 +363,14 @@ struct Tile {
         }
     }
     if constexpr (LIST) {
-      if (keys.logits && col < keys.lg_rows) {       // (entries past the list: the row's padding, or the next chunk's, which must stay)
+      if (keys.logits && col < keys.lg_rows) {       // four at a time: a row's padding to a multiple of 4 may get something, too
+        gfloat* const at = keys.logits + (size_t)col * keys.lg_stride;
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int k = base + r0 + u * 32 + (i / 4) * 8 + half * 4 + i % 4;
-            if (k < keys.end) keys.logits[(size_t)col * keys.lg_stride + k] = s[u][i] * scale;
+          for (int i = 0; i < 16; i += 4) {
+            const int k = base + r0 + u * 32 + i * 2 + half * 4;
+            if (k < keys.end) store4<4>((gchar*)(at + k), s[u][i] * scale, s[u][i + 1] * scale, s[u][i + 2] * scale, s[u][i + 3] * scale);
           }
       }
     }
@@ -405,14 +422,15 @@ struct Tile {
     load_rows(keys.begin);
     load_slots(keys.begin + TK);
     for (int base = keys.begin; base < keys.end; base += TK) {
-      __syncthreads();                               // (the step before has been read)
+      const int first = base + wk * KT;
+      if (kAlone && first >= min(hi, keys.end)) break;         // (uniform in the wave; what follows are others' keys)
+      meet();                                        // (the step before has been read)
       store_rows();
-      __syncthreads();
+      meet();
       if (base + TK < keys.end) {
         load_rows(base + TK);
         load_slots(base + 2 * TK);
       }
-      const int first = base + wk * KT;
       if (first < hi) {
         bool masked = first + KT > lo;
         if constexpr (MOD) masked |= keys.doc != nullptr;
@@ -463,11 +481,6 @@ struct Tile {
   }
 };
 
-template <int EB>
-__device__ __forceinline__ void store4(gchar* p, float a, float b, float c, float d) {
-  if constexpr (EB == 4) *(ADSA_GLOBAL u32x4*)p = u32x4{__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d)};
-  else *(ADSA_GLOBAL u32x2*)p = u32x2{pack2_bf16(a, b), pack2_bf16(c, d)};
-}
 
 // Many rows of a bf16 prompt: W waves of 32 rows each, keys in steps of 32, two steps to a tile of K and V in LDS.
 //
@@ -729,6 +742,10 @@ struct Flow {
     for (int i = 0; i < 16; i += 2) p[i / 2] = two_probabilities(i, &sum);
     l += sum;
   }
+
+  // (as a Tile's: outputs r .. r + 3 of the lane are elements from element(r) on)
+  static constexpr int kMine = DT * 16, wk = 0;
+  __device__ __forceinline__ int element(int r) const { return r / 16 * 32 + r % 16 / 4 * 8 + half * 4; }
 
   int lo, hi;                  // keys that all rows of the wave see, and from which on none does
   __device__ __forceinline__ bool masked_at(int first) const {
@@ -1256,7 +1273,8 @@ __device__ __forceinline__ void own_list(const Mods& mods, const Keys& keys, con
   }
 }
 
-template <int EB, int D, int WK, bool MOD, bool ONE>
+// BIG: prompts are met by 128 rows at a time (bf16; groups of more than 32 rows), else by 32 rows and as many waves that split the keys.
+template <int EB, int D, int WK, bool MOD, bool ONE, bool BIG>
 __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(SharedArgs A) {
   extern __shared__ __align__(16) char s_lds[];
   const int hq = A.h * A.G, C = A.prompt_chunks + A.own_chunks;
@@ -1292,7 +1310,8 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(S
     const int chunk = unit % A.prompt_chunks, head = unit / A.prompt_chunks % A.h, g = unit / A.prompt_chunks / A.h;
     const Group gr = group_at(A, g);
     const int rows = (gr.end - gr.first) * A.G;
-    if (gr.n < 0 || tile * 32 >= rows) return;
+    constexpr int kRows = BIG ? 128 : 32;
+    if (gr.n < 0 || tile * kRows >= rows) return;
     const ADSA_GLOBAL adsa_seq& pr = ((const ADSA_GLOBAL adsa_seq*)A.prompts)[g];
     keys.k = (const gchar*)pr.k + head * A.prompt_head_stride_b;
     keys.v = (const gchar*)pr.v + head * A.prompt_head_stride_b;
@@ -1302,17 +1321,25 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(S
     const int per = ((gr.n + A.prompt_chunks - 1) / A.prompt_chunks + 31) / 32 * 32;
     keys.begin = min(gr.n, chunk * per);
     keys.end = min(gr.n, keys.begin + per);
-    Tile<EB, D, 1, WK, 32, MOD, false, true> t(A.mods, keys, (lchar*)s_lds);
-    const int r = tile * 32 + t.col, rr = min(r, rows - 1), b = gr.first + rr / A.G, qh = head * A.G + rr % A.G;
-    const size_t at = (size_t)b * hq + qh;
+    auto attend = [&](auto& t, int r) {
+      const int rr = min(r, rows - 1), b = gr.first + rr / A.G, qh = head * A.G + rr % A.G;
+      const size_t at = (size_t)b * hq + qh;
+      t.row = {keys.end, MOD && A.mods.slopes ? query_pos(b) : 0, 0, MOD && A.mods.slopes ? ((const gfloat*)A.mods.slopes)[qh] * kLog2e : 0.0f};
+      t.load_q((const gchar*)A.q + at * (D * EB));
+      t.run();
+      if (r < rows) store(t, at, chunk);
+    };
     if (keys.begin >= keys.end) {
-      if (threadIdx.x < 32 && r < rows) nothing(at, chunk);
+      for (int r = tile * kRows + threadIdx.x; r < min(rows, (tile + 1) * kRows); r += WK * kWave) nothing((size_t)(gr.first + r / A.G) * hq + head * A.G + r % A.G, chunk);
       return;
     }
-    t.row = {keys.end, MOD && A.mods.slopes ? query_pos(b) : 0, 0, MOD && A.mods.slopes ? ((const gfloat*)A.mods.slopes)[qh] * kLog2e : 0.0f};
-    t.load_q((const gchar*)A.q + at * (D * EB));
-    t.run();
-    if (r < rows) store(t, at, chunk);
+    if constexpr (BIG) {
+      Flow<D, WK, MOD> t(A.mods, keys, (lchar*)s_lds);
+      attend(t, tile * kRows + t.wave * 32 + t.col);
+    } else {
+      Tile<EB, D, 1, WK, 32, MOD, false, true> t(A.mods, keys, (lchar*)s_lds);
+      attend(t, tile * kRows + t.col);
+    }
     return;
   }
   // one sequence's own list
@@ -1565,12 +1592,24 @@ hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStrea
   return hipGetLastError();
 }
 
+template <int EB, int D, bool MOD, bool BIG>
+constexpr int shared_lds = [] {
+  const int own = Shape<EB, D, 1, kKeyWaves<EB, D>, 32>::kLds;
+  if constexpr (BIG) return std::max(own, Flow<D, 4, MOD>::kLds);
+  else return own;
+}();
+
 template <int EB, int D, bool MOD>
-hipError_t shared_launches(const SharedArgs& A, hipStream_t st) {
+hipError_t shared_launches(const SharedArgs& A, const SharedPlan& plan, hipStream_t st) {
   constexpr int KW = kKeyWaves<EB, D>;
   const dim3 grid((unsigned)(A.prompt_blocks + A.n_seq * A.h * A.own_chunks));
-  if (A.G == 1) k_shared<EB, D, KW, MOD, true><<<grid, KW * kWave, Shape<EB, D, 1, KW, 32>::kLds, st>>>(A);
-  else k_shared<EB, D, KW, MOD, false><<<grid, KW * kWave, Shape<EB, D, 1, KW, 32>::kLds, st>>>(A);
+  auto launch = [&](auto one, auto big) {
+    constexpr bool kBig = decltype(big)::value;
+    k_shared<EB, D, KW, MOD, decltype(one)::value, kBig><<<grid, KW * kWave, shared_lds<EB, D, MOD, kBig>, st>>>(A);
+  };
+  auto by_group = [&](auto big) { if (A.G == 1) launch(std::true_type(), big); else launch(std::false_type(), big); };
+  if constexpr (EB == 2) { if (plan.big) by_group(std::true_type()); else by_group(std::false_type()); }
+  else by_group(std::false_type());
   if (A.G == 1) k_shared_finish<EB, D, true><<<dim3((unsigned)(A.n_seq * A.h)), 256, 0, st>>>(A);
   else k_shared_finish<EB, D, false><<<dim3((unsigned)(A.n_seq * A.h)), 256, 0, st>>>(A);
   return hipGetLastError();
@@ -1586,11 +1625,13 @@ hipError_t allow_lds() {
   allow(k_prompt<EB, D, 1, KW, 32, MOD>, Shape<EB, D, 1, KW, 32>::kLds);
   allow(k_prompt<EB, D, 4, 1, KT, MOD>, Shape<EB, D, 4, 1, KT>::kLds);
   allow(k_prompt_mass<EB, D, MOD>, MassLds<EB, D>::kLds);
-  allow(k_shared<EB, D, KW, MOD, true>, Shape<EB, D, 1, KW, 32>::kLds);
-  allow(k_shared<EB, D, KW, MOD, false>, Shape<EB, D, 1, KW, 32>::kLds);
+  allow(k_shared<EB, D, KW, MOD, true, false>, shared_lds<EB, D, MOD, false>);
+  allow(k_shared<EB, D, KW, MOD, false, false>, shared_lds<EB, D, MOD, false>);
   if constexpr (EB == 2) {
     allow(k_prompt_many<D, 4, MOD>, Flow<D, 4, MOD>::kLds);
     allow(k_prompt_many<D, 8, MOD>, Flow<D, 8, MOD>::kLds);
+    allow(k_shared<EB, D, KW, MOD, true, true>, shared_lds<EB, D, MOD, true>);
+    allow(k_shared<EB, D, KW, MOD, false, true>, shared_lds<EB, D, MOD, true>);
   }
   return e;
 }
@@ -1647,11 +1688,13 @@ PromptWorkspace make_prompt_workspace(const adsa_params& p, const adsa_tokens& t
 
 SharedPlan make_shared_plan(const adsa_params& p, const adsa_shared& s) {
   SharedPlan plan;
-  plan.prompt_tiles = (s.max_members * query_group(p) + 31) / 32;
+  const int rows = s.max_members * query_group(p);
+  plan.big = p.dtype == ADSA_BF16 && rows > 32 && s.kv_slot_stride * 2 * 64 < (1ll << 31);       // (see make_prompt_plan)
+  plan.prompt_tiles = (rows + (plan.big ? 127 : 31)) / (plan.big ? 128 : 32);
   auto parts = [](long long groups, int longest) {
     return (int)std::clamp<long long>(std::min<long long>((512 + groups - 1) / groups, (longest + 127) / 128), 1, kMaxChunks);
   };
-  plan.prompt_chunks = parts((long long)s.n_groups * p.n_heads * plan.prompt_tiles, s.max_prompt);
+  plan.prompt_chunks = parts((long long)s.n_groups * p.n_heads * plan.prompt_tiles * 4, s.max_prompt);
   plan.own_chunks = parts((long long)p.n_seq * p.n_heads, p.sel_cap);
   return plan;
 }
@@ -1704,7 +1747,7 @@ hipError_t launch_attend_shared(const adsa_params& p, const adsa_shared& s, cons
   A.prompt_blocks = (s.n_groups * p.n_heads * plan.prompt_chunks + 7) / 8 * 8 * plan.prompt_tiles;
   A.accumulate = accumulate; A.append = append; A.advance = advance; A.new_f32 = new_f32;
   return by_type(p, modded(A.mods), [&](auto eb_, auto d, auto m) {
-    return shared_launches<decltype(eb_)::value, decltype(d)::value, decltype(m)::value>(A, st);
+    return shared_launches<decltype(eb_)::value, decltype(d)::value, decltype(m)::value>(A, plan, st);
   });
 }
 
