@@ -1392,7 +1392,7 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(S
 constexpr int kMaxParts = 2 * kMaxChunks;
 template <int EB, int D, bool ONE>
 __global__ __launch_bounds__(256) void k_shared_finish(SharedArgs A) {
-  constexpr int NT = 256, E = D / kWave, kMaxG = ONE ? 1 : 16, kEarly = 3, kAcc = 4;
+  constexpr int NT = 256, E = D / kWave, kMaxG = ONE ? 1 : 16, kEarly = 3, kAcc = 4, kLg = ONE ? 1 : 8;
   __shared__ float s_w[kMaxG][kMaxParts + 1], s_l[kMaxG][kMaxParts], s_lse[kMaxG], s_new[kMaxG], s_inv[kMaxG];
   __shared__ __attribute__((aligned(16))) float s_v[D];
   __shared__ int s_has;
@@ -1408,11 +1408,14 @@ __global__ __launch_bounds__(256) void k_shared_finish(SharedArgs A) {
   for (int i = 0; i < A.n_groups; i += kWave)          // the sequence's group: the last that begins at or before it
     g += __popcll(__ballot(i + lane < A.n_groups && ((const gint*)A.members)[min(i + lane, A.n_groups - 1)] <= b));
   int slot[kEarly];
-  float old[kEarly], lg[kEarly];
+  float old[kEarly], lg[kEarly][kLg];
 #pragma unroll
   for (int k = 0; k < kEarly; ++k) {
     slot[k] = list[min(tid + k * NT, A.sel_cap - 1)];
-    if (ONE && A.accumulate) lg[k] = ((const gfloat*)A.logits)[at0 * A.lg_stride + min(tid + k * NT, A.sel_cap - 1)];
+    if (A.accumulate) {
+#pragma unroll
+      for (int h = 0; h < kLg; ++h) lg[k][h] = ((const gfloat*)A.logits)[(at0 + min(h, G - 1)) * A.lg_stride + min(tid + k * NT, A.sel_cap - 1)];
+    }
   }
   for (int o = tid; o < G * C; o += NT) {
     const gfloat* const ml = (const gfloat*)A.part_ml + (at0 * C + o) * 2;
@@ -1531,22 +1534,25 @@ __global__ __launch_bounds__(256) void k_shared_finish(SharedArgs A) {
     store4<EB>((gchar*)A.out + ((at0 + h) * D + oe) * EB, x[0] * s_inv[h], x[1] * s_inv[h], x[2] * s_inv[h], x[3] * s_inv[h]);
   }
   if (A.accumulate) {
-    auto update = [&](int j, int raw, float before, float first) {
-      const bool is_new = raw == new_slot && new_slot >= 0;
-      float gain = 0.0f;
-      if constexpr (ONE) gain = fast_exp2((is_new ? s_new[0] : first) - s_lse[0]);
-      else {
-#pragma unroll 4
-        for (int h = 0; h < G; ++h) gain += fast_exp2((is_new ? s_new[h] : ((const gfloat*)A.logits)[(at0 + h) * A.lg_stride + j]) - s_lse[h]);
-      }
-      score[min(max(raw, 0), A.cap - 1)] = before + gain;
-    };
+    auto logit = [&](int j, int h) { return ((const gfloat*)A.logits)[(at0 + h) * A.lg_stride + j]; };
+    auto chance = [&](int raw, int h, float z) { return fast_exp2((raw == new_slot && new_slot >= 0 ? s_new[h] : z) - s_lse[h]); };
+    auto slot_of = [&](int raw) { return min(max(raw, 0), A.cap - 1); };
 #pragma unroll
     for (int k = 0; k < kEarly; ++k)
-      if (tid + k * NT < cnt) update(tid + k * NT, slot[k], old[k], ONE ? lg[k] : 0.0f);
+      if (tid + k * NT < cnt) {
+        float gain = 0.0f;
+#pragma unroll
+        for (int h = 0; h < kLg; ++h)
+          if (h < G) gain += chance(slot[k], h, lg[k][h]);
+        for (int h = kLg; h < G; ++h) gain += chance(slot[k], h, logit(tid + k * NT, h));
+        score[slot_of(slot[k])] = old[k] + gain;
+      }
     for (int j = tid + kEarly * NT; j < cnt; j += NT) {
       const int raw = list[j];
-      update(j, raw, score[min(max(raw, 0), A.cap - 1)], ONE ? ((const gfloat*)A.logits)[at0 * A.lg_stride + j] : 0.0f);
+      const float before = score[slot_of(raw)];
+      float gain = 0.0f;
+      for (int h = 0; h < G; ++h) gain += chance(raw, h, logit(j, h));
+      score[slot_of(raw)] = before + gain;
     }
   }
   if (A.advance && head == 0 && tid == 0) sq.step = step + 1;
