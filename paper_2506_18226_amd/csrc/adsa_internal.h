@@ -131,7 +131,8 @@ static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t
 
 // ---- prompts (prompt_api.hip checks and plans, rotary.hip and prompt.hip launch)
 struct PromptPlan {
-  int rows;             // of a workgroup: 32 (its waves split the keys), 128 or 256 (32 or 64 for each of 4 waves)
+  int rows;             // of a workgroup: 32 (its waves split the keys) or 128 (32 for each of 4 waves)
+  int rows_all;         // of the longest sequence, per cache head
   bool flow;            // k_prompt_many (else k_prompt)
   int tiles;            // row tiles per (sequence, cache head)
   int chunks;           // parts the keys are split into
@@ -140,7 +141,7 @@ PromptPlan make_prompt_plan(const adsa_params& p, const adsa_tokens& t);
 struct PromptWorkspace {
   size_t part_ml_off;   // float [T][hq][chunks][2]   (m, l) of split keys
   size_t part_acc_off;  // float [T][hq][chunks][head_dim]
-  size_t norm_off;      // float [T][hq][2]   (m, 1 / l) of every row, for the attention mass
+  size_t norm_off;      // float [T][hq]   log2 of every row's sum of exponentials, for the attention mass
   size_t total;
 };
 PromptWorkspace make_prompt_workspace(const adsa_params& p, const adsa_tokens& t, const PromptPlan& plan);

@@ -104,10 +104,9 @@ __device__ __forceinline__ bool f32_bad(float x) { return (__float_as_uint(x) & 
 // scores of 16 elements: fp32 sum q.k -> log2 units
 template <int EB>
 __device__ __forceinline__ float capped(float s, const Mods& mods) {
-  const float t = s * mods.cap_in;
-  if constexpr (EB == 4) return mods.cap_out * tanhf(t);
+  if constexpr (EB == 4) return mods.cap_out * tanhf(s * mods.cap_in);
   // tanh t = 1 - 2 / (e^2t + 1): off by 2^-23 of 1, far below the rounding of bf16 inputs
-  return mods.cap_out * fmaf(-2.0f, __builtin_amdgcn_rcpf(fast_exp2(t * (2.0f * kLog2e)) + 1.0f), 1.0f);
+  return fmaf(-2.0f * mods.cap_out, __builtin_amdgcn_rcpf(fast_exp2(s * (mods.cap_in * (2.0f * kLog2e))) + 1.0f), mods.cap_out);
 }
 
 // Two waves share a SIMD's registers, but for fp32 rows of 128, whose steps alone take half of one's.  (Within 256 registers products are formed in
@@ -490,13 +489,17 @@ struct Tile {
 // step j on the vector unit, laid out alternately by hand (a product, then its share of the vector work), since the
 // compiler left alone puts all of one kind before the other.
 // A row's maximum is followed only when it has grown by more than 2^8: P stays below 2^8, and outputs are rescaled next to never.
-template <int D, int W, bool MOD>
+// MODS: kPlain, kCapped (by a tanh, nothing else), or kAny.
+enum : int { kPlain, kCapped, kAny };
+template <int D, int W, int MODS>
 struct Flow {
+  static constexpr bool MOD = MODS == kAny;          // positions and documents are wanted, and what is done is decided at run time
   using L = Layout<2, D>;
   static constexpr int CPR = L::CPR, RB = L::RB, DT = D / 32, KC = D / 16, VC = DT * 2, NC = KC + VC;
   static constexpr int kThreads = W * kWave, kRows = W * 32, TK = 64;
   static constexpr int RPT = kThreads / CPR, NL = TK / RPT;
-  static constexpr int kV = 2 * TK * RB, kMeta = 2 * kV, kLds = kMeta + (MOD ? 3 * 2 * TK * 4 : 0);      // two tiles of K, of V; positions and documents of three
+  static constexpr int kV = 2 * TK * RB, kMeta = 2 * kV, kFlag = kMeta + (MOD ? 3 * 2 * TK * 4 : 0), kLds = kFlag + 16;      // two tiles of K, of V; positions and documents of three;
+                                                     // whether a tile of V holds infinities or NaN
   static constexpr float kGrowth = 8.0f;
 
   const Mods& mods;
@@ -565,9 +568,16 @@ struct Flow {
         meta[TK + tid] = meta_doc;
       }
   }
-  __device__ __forceinline__ void store_v() {
+  // check: some row does not see all of the tile
+  __device__ __forceinline__ void store_v(int t, bool check) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) put16(lds + v_to + i * RPT * RB, vr[i]);
+    if (check) {
+      bool bad = false;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) bad |= bf16_bad(vr[i].x) || bf16_bad(vr[i].y) || bf16_bad(vr[i].z) || bf16_bad(vr[i].w);
+      if (__ballot(bad) != 0) *(ADSA_LDS int*)(lds + kFlag + t % 4 * 4) = t + 1;
+    }
   }
   __device__ __forceinline__ void load_meta(int base) {
     if constexpr (MOD)
@@ -587,16 +597,8 @@ struct Flow {
   }
   __device__ __forceinline__ bf16x8 p_piece(int t) const { return __builtin_bit_cast(bf16x8, u32x4{p[4 * t], p[4 * t + 1], p[4 * t + 2], p[4 * t + 3]}); }
 
-  // Infinities and NaN among V's rows of a step whose keys not every row sees (rare): they must not reach rows that do not see them.
-  __device__ __forceinline__ bool values_bad(int sub) const {
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < 32 * CPR / kWave; ++i) {
-      const uint4 w = lds16(lds + kV + (v_at[0] & (TK * RB)) + sub * 32 * RB + (i * kWave + lane) * 16);
-      bad |= bf16_bad(w.x) || bf16_bad(w.y) || bf16_bad(w.z) || bf16_bad(w.w);
-    }
-    return __ballot(bad) != 0;
-  }
+  // Infinities and NaN among tile t's rows of V (rare) must not reach rows that do not see them.
+  __device__ __forceinline__ bool values_bad(int t) const { return *(const ADSA_LDS int*)(lds + kFlag + t % 4 * 4) == t + 1; }
   // ... and what those give the rows that see their key: where V holds +infinity (and where -infinity, NaN counting as both) the
   // product of ones there with ones for p > 0 says which rows have one among their keys.
   __device__ __forceinline__ void add_bad_values(int sub) {
@@ -621,12 +623,33 @@ struct Flow {
   }
 
   // pieces of the two steps' work
-  __device__ __forceinline__ void bend(int i, const ADSA_LDS int* meta) {                  // cap and distance of one score
-    float z = mods.cap_out != 0.0f ? capped<2>(s[i], mods) : s[i] * mods.scale_log2;
-    if (mods.slopes) z = fmaf(-row.slope, fabsf((float)row.pos - __int_as_float(meta[(i / 4) * 8 + half * 4 + i % 4])), z);
-    s[i] = z;
+  // cap and distance of N scores from number i on
+  template <int N>
+  __device__ __forceinline__ void bend(int i, const ADSA_LDS int* meta) {
+    if (MODS == kCapped || mods.cap_out != 0.0f) {
+#pragma unroll
+      for (int k = i; k < i + N; ++k) s[k] = capped<2>(s[k], mods);
+    } else {
+#pragma unroll
+      for (int k = i; k < i + N; ++k) s[k] *= mods.scale_log2;
+    }
+    if constexpr (MOD)
+      if (mods.slopes) {
+#pragma unroll
+        for (int k = i; k < i + N; ++k) s[k] = fmaf(-row.slope, fabsf((float)row.pos - __int_as_float(meta[(k / 4) * 8 + half * 4 + k % 4])), s[k]);
+      }
   }
-  __device__ __forceinline__ float score_scale() const { return MOD ? 1.0f : mods.scale_log2; }
+  __device__ __forceinline__ void hide(int base, const ADSA_LDS int* meta) {               // what the row does not see of the keys from `base` on
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int k = (i / 4) * 8 + half * 4 + i % 4;
+      bool seen = base + k < row.limit;
+      if constexpr (MOD)
+        if (keys.doc) seen &= meta[TK + k] == row.doc;
+      s[i] = seen ? s[i] : -INFINITY;
+    }
+  }
+  __device__ __forceinline__ float score_scale() const { return MODS != kPlain ? 1.0f : mods.scale_log2; }
   // The step's maximum; where it has grown, what the state so far has to be multiplied by.
   __device__ __forceinline__ bool maximum(float* corr) {
     float mx = s[0];
@@ -659,16 +682,16 @@ struct Flow {
     acc[i / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), p_piece(i % 2), acc[i / 2], 0, 0, 0);
   }
 
-  // One step of keys that every row sees: the scores of K's rows (half SUB of the tile), the softmax of the scores s of the step
+  // One step (HIDE: of keys that not every row sees): the scores of K's rows (half SUB of the tile), the softmax of the scores s of the step
   // before, the outputs of its predecessor's p with V's rows, alternately.
-  template <int SUB>
-  __device__ __forceinline__ void step(const ADSA_LDS int* meta) {
+  template <int SUB, bool HIDE>
+  __device__ __forceinline__ void step(int base, const ADSA_LDS int* meta) {
     f32x16 next = {};
     uint32_t pn[8];
     float corr, sum = 0.0f;
     bool grown = false;
     constexpr int kAhead = 3;                        // pieces fetched ahead of their product
-    constexpr int kMax = MOD ? NC / 2 : 1;           // the maximum stands before this chunk's probabilities
+    constexpr int kMax = MODS != kPlain ? NC / 2 : 1;      // the maximum stands before this chunk's probabilities
     uint4 kp[KC];
     u32x4 vp[VC];
     auto fetch = [&](auto at) {
@@ -682,11 +705,11 @@ struct Flow {
       fetch(std::integral_constant<int, c + kAhead>());
       if constexpr (c < KC) next = score_product(kp[c], c, next);
       else output_product(vp[c - KC], c - KC);
-      if constexpr (MOD && c < kMax) {
-        constexpr int e0 = 16 * c / kMax;
-        each<16 * (c + 1) / kMax - e0>([&](auto o) { bend(e0 + decltype(o)::value, meta); });
+      if constexpr (MODS != kPlain && c < kMax) bend<16 / kMax>(16 / kMax * c, meta);
+      if constexpr (c == kMax) {
+        if constexpr (HIDE) hide(base, meta);
+        grown = maximum(&corr);
       }
-      if constexpr (c == kMax) grown = maximum(&corr);
       if constexpr (c >= kMax) {                     // this chunk's share of the probabilities
         constexpr int kRest = NC - kMax, e0 = 8 * (c - kMax) / kRest;
         each<8 * (c + 1 - kMax) / kRest - e0>([&](auto o) {
@@ -705,8 +728,7 @@ struct Flow {
   }
 
   // The same one after the other: first and last steps (which lack a part), and keys that not every row sees.
-  __device__ __forceinline__ void outputs(int sub, bool masked) {
-    const bool tidy = masked && values_bad(sub);
+  __device__ __forceinline__ void outputs(int sub, bool tidy) {
     if (tidy) add_bad_values(sub);
 #pragma unroll
     for (int i = 0; i < VC; ++i) {
@@ -720,21 +742,9 @@ struct Flow {
 #pragma unroll
     for (int c = 0; c < KC; ++c) s = score_product(k_piece(sub, c), c, s);
   }
-  __device__ __forceinline__ void softmax(int base, const ADSA_LDS int* meta, bool masked) {
-    if constexpr (MOD) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) bend(i, meta);
-    }
-    if (masked) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int k = (i / 4) * 8 + half * 4 + i % 4;
-        bool seen = base + k < row.limit;
-        if constexpr (MOD)
-          if (keys.doc) seen &= meta[TK + k] == row.doc;
-        s[i] = seen ? s[i] : -INFINITY;
-      }
-    }
+  __device__ __forceinline__ void softmax(int base, const ADSA_LDS int* meta) {
+    if constexpr (MODS != kPlain) bend<16>(0, meta);
+    if (hides(base)) hide(base, meta);
     float corr, sum = 0.0f;
     const bool grown = maximum(&corr);
     if (__ballot(grown) != 0) rescale(corr);
@@ -748,7 +758,7 @@ struct Flow {
   __device__ __forceinline__ int element(int r) const { return r / 16 * 32 + r % 16 / 4 * 8 + half * 4; }
 
   int lo, hi;                  // keys that all rows of the wave see, and from which on none does
-  __device__ __forceinline__ bool masked_at(int first) const {
+  __device__ __forceinline__ bool hides(int first) const {            // whether some row does not see all of the 32 keys from `first` on
     bool x = first + 32 > lo;
     if constexpr (MOD) x |= keys.doc != nullptr;
     return x;
@@ -756,21 +766,22 @@ struct Flow {
   // Tile number t (of `mine` that this wave's rows see): the scores of steps 2t and 2t + 1, the softmax of 2t - 1 and 2t, the outputs of 2t - 2
   // and 2t - 1; so K's tile t and V's tile t - 1 are read.
   __device__ __forceinline__ const ADSA_LDS int* meta_of(int t) const { return (const ADSA_LDS int*)(lds + kMeta) + t % 3 * 2 * TK; }
-  __device__ __forceinline__ void tile(int t, int mine) {
+  __device__ __forceinline__ void tile(int t, int mine, bool tidy) {
     if (t > mine || mine == 0) return;
     const int base = keys.begin + t * TK;
     for (int sub = 0; sub < 2; ++sub) {
       if (t > 0) {
-        outputs(sub, masked_at(base - 64 + 32 * sub));
-        if (sub == 0) softmax(base - 32, meta_of(t + 2) + 32, masked_at(base - 32));
+        outputs(sub, tidy);
+        if (sub == 0) softmax(base - 32, meta_of(t + 2) + 32);
       }
       if (t < mine) {
-        if (sub == 1) softmax(base, meta_of(t), masked_at(base));
+        if (sub == 1) softmax(base, meta_of(t));
         scores(sub);
       }
     }
   }
-  __device__ __forceinline__ void run() {
+  // least: no row of the workgroup sees fewer keys
+  __device__ __forceinline__ void run(int least) {
     m = kLowest;
     l = 0.0f;
 #pragma unroll
@@ -784,6 +795,8 @@ struct Flow {
     const int tiles = (keys.end - keys.begin + TK - 1) / TK, mine = max(0, (min(hi, keys.end) - keys.begin + TK - 1) / TK);
     // tiles 1 .. open - 1 have no key that some row does not see
     const int open = MOD && keys.doc ? 1 : min(mine, max(0, lo - 32 - keys.begin) / TK + 1);
+    const int checked = MOD && keys.doc ? 0 : max(0, least - keys.begin) / TK;      // the first tile that some row of the workgroup does not see all of
+    if (tid < 4) ((ADSA_LDS int*)(lds + kFlag))[tid] = 0;
     load_tile(keys.k, keys.begin, kr);
     load_meta(keys.begin);
     store_k(0);
@@ -794,22 +807,28 @@ struct Flow {
     // Between two barriers, tile t's K and tile t - 1's V are read, and tile t + 1's K and tile t's V written, into the other buffers.
     auto next_tile = [&](int t) {
       if (t + 1 < tiles) store_k((t + 1) % 3);
-      store_v();
+      store_v(t, t >= checked);
       __syncthreads();
       change_buffers();
       if (t + 2 < tiles) { load_tile(keys.k, keys.begin + (t + 2) * TK, kr); load_meta(keys.begin + (t + 2) * TK); }
       if (t + 1 < tiles) load_tile(keys.v, keys.begin + (t + 1) * TK, vr);
     };
-    tile(0, mine);
+    tile(0, mine, false);
     next_tile(0);
     int t = 1;
     for (; t < open; ++t) {
-      step<0>(meta_of(t + 2) + 32);
-      step<1>(meta_of(t));
+      step<0, false>(0, meta_of(t + 2) + 32);
+      step<1, false>(0, meta_of(t));
+      next_tile(t);
+    }
+    for (; t < mine && !values_bad(t - 1); ++t) {
+      const int base = keys.begin + t * TK;
+      step<0, true>(base - 32, meta_of(t + 2) + 32);
+      step<1, true>(base, meta_of(t));
       next_tile(t);
     }
     for (; t <= tiles; ++t) {
-      tile(t, mine);
+      tile(t, mine, values_bad(t - 1));
       if (t < tiles) next_tile(t);
     }
     l = xor_sum<32>(l);
@@ -830,6 +849,8 @@ struct PromptArgs {
   Mods mods;
   long long slot_stride_b, head_stride_b;
   int n_seq, n_tokens, max_len, h, G, cap, mask, tiles, chunks, advance;
+  uint32_t inv_G;              // ceil(2^32 / G) for G > 1: row / G is the upper half of a product (rows are less than 2^17, G at most 16)
+  __device__ __forceinline__ int token_of(int row) const { return G == 1 ? row : (int)__umulhi((uint32_t)row, inv_G); }
 };
 
 // A sequence's new tokens: where they stand in the packed rows and in the cache.
@@ -935,7 +956,7 @@ __device__ __forceinline__ void store_part(const PromptArgs& A, const Job& J, si
 __device__ __forceinline__ float inverse(float l) { return l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l; }       // (a NaN stays one)
 __device__ __forceinline__ void store_lse(const PromptArgs& A, size_t at, float m, float l) {
   ((gfloat*)A.lse)[at] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
-  if (A.norm) { ((gfloat*)A.norm)[2 * at] = m; ((gfloat*)A.norm)[2 * at + 1] = inverse(l); }
+  if (A.norm) ((gfloat*)A.norm)[at] = l == 0.0f ? INFINITY : m + __log2f(l);           // (exp2(z - norm): 0 for a row that sees nothing)
 }
 
 template <int EB, int D, int WR, int WK, int KT, bool MOD>
@@ -968,17 +989,17 @@ __global__ __launch_bounds__(WR * WK * kWave, EB == 2 && D == 64 ? 2 : 1) void k
   }
 }
 
-template <int D, int W, bool MOD>
-__global__ __launch_bounds__(W * kWave, 2) void k_prompt_many(PromptArgs A) {
-  using F = Flow<D, W, MOD>;
+template <int D, int W, int MODS>
+__global__ __launch_bounds__(W * kWave, D == 64 ? 3 : 2) void k_prompt_many(PromptArgs A) {
+  using F = Flow<D, W, MODS>;
   extern __shared__ __align__(16) char s_lds[];
   Job J;
   if (!job_of<2, D, F::kRows, F::kThreads>(A, J)) return;
   F f(A.mods, J.keys, (lchar*)s_lds);
   const int r = J.row0 + f.wave * 32 + f.col;
-  const size_t at = row_of<MOD>(A, J, r, f.row);
+  const size_t at = row_of<F::MOD>(A, J, r, f.row);
   f.load_q((const gchar*)A.q + at * (D * 2));
-  f.run();
+  f.run(min(J.keys.end, limit_of(J.pr, J.pr.slot0 + J.row0 / A.G)));       // (the first row's limit is the least: the prefix's are no less than the first's)
   if (r >= J.rows) return;
   if (A.chunks > 1) {
     gfloat* const acc = (gfloat*)A.part_acc + (at * A.chunks + J.chunk) * D;
@@ -1040,17 +1061,19 @@ __global__ __launch_bounds__(256) void k_prompt_finish(PromptArgs A) {
   if (lane == 0) store_lse(A, at, M, L);
 }
 
-// score[head][slot] += sum over rows of the probability they gave the slot.  A wave keeps 32 slots' K rows as the B operand and meets 64
-// rows per step, from the first that can see the slots on; scores come untransposed (a lane's column is a slot), so a lane sums its own.
-constexpr int kMassRows = 64, kMassKeys = 128;
-template <int EB, int D> struct MassLds {
-  static constexpr int kInfo = kMassRows * Layout<EB, D>::RB;          // q rows, then per row: m, 1 / l, limit, slope, position, document
-  static constexpr int kLds = kInfo + 6 * kMassRows * 4;
+// score[head][slot] += sum over rows of the probability they gave the slot.  A wave keeps NB x 32 slots' K rows as the A operand and meets the rows
+// from the first that can see the slots on, 32 at a time; a lane's column is a row, whose normaliser (m + log2 l) it holds, and its registers
+// are slots, which it sums up over its rows: lanes meet once, at the end.  The products of a block of rows run beside the exponentials of
+// the one before.  Two blocks of slots share a fetch of q rows (with one, LDS takes as long as the products).
+template <int EB, int D, bool MOD> struct Mass {      // (slots' positions and documents, or fp32 rows, take the second block's registers)
+  static constexpr int NB = EB == 2 && !MOD ? 2 : 1, kKeys = 4 * 32 * NB, kRows = 64, kTile = kRows * Layout<EB, D>::RB;
+  static constexpr int kLds = 2 * kTile;
 };
 template <int EB, int D, bool MOD>
-__global__ __launch_bounds__(256) void k_prompt_mass(PromptArgs A, int key_tiles) {
+__global__ __launch_bounds__(256, EB == 2 ? 2 : 1) void k_prompt_mass(PromptArgs A, int key_tiles) {
   using L = Layout<EB, D>;
-  constexpr int CPR = L::CPR, RB = L::RB, RPT = 256 / CPR, NL = kMassRows / RPT;
+  using M = Mass<EB, D, MOD>;
+  constexpr int CPR = L::CPR, RB = L::RB, RPT = 256 / CPR, NL = M::kRows / RPT, KC = CPR / 2, NB = M::NB;
   extern __shared__ __align__(16) char s_lds[];
   lchar* const lds = (lchar*)s_lds;
   int pair, tile;
@@ -1059,92 +1082,169 @@ __global__ __launch_bounds__(256) void k_prompt_mass(PromptArgs A, int key_tiles
   const int b = pair / A.h, head = pair % A.h, tid = threadIdx.x, lane = tid % kWave, col = lane % 32, half = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave), hq = A.h * A.G;
   const Prompt pr = prompt_of(A, b);
-  const int n = pr.slot0 + pr.len, key0 = tile * kMassKeys, rows = pr.len * A.G;
+  const int n = pr.slot0 + pr.len, rows = pr.len * A.G, key0 = tile * M::kKeys, mine = key0 + wave * 32 * NB;
   if (pr.status != 0 || pr.len == 0 || key0 >= n) return;
   const ADSA_GLOBAL adsa_seq& sq = ((const ADSA_GLOBAL adsa_seq*)A.seqs)[b];
-  const int key = key0 + wave * 32 + col, slot = min(key, n - 1);
-  const gint* const doc = A.mods.doc ? (const gint*)A.mods.doc + b * A.mods.doc_stride : nullptr;
-  uint4 kf[CPR / 2];
-  const gchar* const krow = (const gchar*)sq.k + head * A.head_stride_b + (long long)slot * A.slot_stride_b;
+  const gint* const pos = (const gint*)sq.pos;
+  const gint* const doc = MOD && A.mods.doc ? (const gint*)A.mods.doc + b * A.mods.doc_stride : nullptr;
+  uint4 kf[NB][KC];
 #pragma unroll
-  for (int c = 0; c < CPR / 2; ++c) kf[c] = load16(krow + (2 * c + half) * 16);
-  const float kpos = MOD && A.mods.slopes ? (float)((const gint*)sq.pos)[slot] : 0.0f;
-  const int kdoc = MOD && doc ? doc[slot] : 0;
+  for (int x = 0; x < NB; ++x) {
+    const gchar* const krow = (const gchar*)sq.k + head * A.head_stride_b + (long long)min(mine + x * 32 + col, n - 1) * A.slot_stride_b;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) kf[x][c] = load16(krow + (2 * c + half) * 16);
+  }
+  // of the slots that this lane's registers stand for
+  auto slot_of = [&](int x, int i) { return min(mine + x * 32 + (i / 4) * 8 + half * 4 + i % 4, n - 1); };
+  float kpos[NB][16];
+  int kdoc[NB][16];
+  if constexpr (MOD) {
+#pragma unroll
+    for (int x = 0; x < NB; ++x)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        kpos[x][i] = A.mods.slopes ? (float)pos[slot_of(x, i)] : 0.0f;
+        kdoc[x][i] = doc ? doc[slot_of(x, i)] : 0;
+      }
+  }
   // the first row that sees the tile: the token of its first slot, or any where the prefix sees itself
-  const int token0 = key0 < pr.prefix ? 0 : max(0, key0 - pr.slot0);
+  const int row0 = (key0 < pr.prefix ? 0 : max(0, key0 - pr.slot0)) * A.G, steps = (rows - row0 + M::kRows - 1) / M::kRows;
   uint4 qr[NL];
-  float info[6];
-  auto load = [&](int base) {
+  const gchar* const q_first = (const gchar*)A.q + ((size_t)pr.from * hq + head * A.G) * RB;         // of the sequence, for this cache head
+  auto load = [&](int t) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int r = min(base + tid / CPR + i * RPT, rows - 1);
-      qr[i] = load16((const gchar*)A.q + ((size_t)(pr.from + r / A.G) * hq + head * A.G + r % A.G) * RB + (tid % CPR) * 16);
-    }
-    if (tid < kMassRows) {
-      const int r = min(base + tid, rows - 1), token = r / A.G, qh = head * A.G + r % A.G, s = pr.slot0 + token;
-      const size_t at = (size_t)(pr.from + token) * hq + qh;
-      info[0] = ((const gfloat*)A.norm)[2 * at];
-      info[1] = ((const gfloat*)A.norm)[2 * at + 1];
-      info[2] = __int_as_float(base + tid < rows ? limit_of(pr, s) : 0);
-      info[3] = MOD && A.mods.slopes ? ((const gfloat*)A.mods.slopes)[qh] * kLog2e : 0.0f;
-      info[4] = MOD && A.mods.slopes ? (float)((const gint*)sq.pos)[s] : 0.0f;
-      info[5] = __int_as_float(MOD && doc ? doc[s] : 0);
-      if (MOD && doc && doc[s] < 0) info[2] = __int_as_float(0);
+      const int r = min(row0 + t * M::kRows + tid / CPR + i * RPT, rows - 1), token = A.token_of(r);
+      qr[i] = load16(q_first + ((uint64_t)(uint32_t)token * (uint32_t)(hq * RB) + (uint32_t)((r - token * A.G) * RB + (tid % CPR) * 16)));
     }
   };
-  float sum = 0.0f;
-  const float scale = MOD ? 1.0f : A.mods.scale_log2;
-  const ADSA_LDS float* const at = (const ADSA_LDS float*)(lds + MassLds<EB, D>::kInfo);
-  load(token0 * A.G);
-  for (int base = token0 * A.G; base < rows; base += kMassRows) {
-    __syncthreads();
+  auto store = [&](int t) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int r = tid / CPR + i * RPT;
-      put16(lds + r * RB + (((tid % CPR) ^ L::swz_k(r)) << 4), qr[i]);
+      put16(lds + (t & 1) * M::kTile + r * RB + (((tid % CPR) ^ L::swz_k(r)) << 4), qr[i]);
     }
-    if (tid < kMassRows) {
+  };
+  // a lane's row of a block: its normaliser, and what it sees (nothing: past the last row)
+  struct Column {
+    float norm, slope, pos;
+    int limit, doc;
+  };
+  const gfloat* const norm_first = (const gfloat*)A.norm + (size_t)pr.from * hq + head * A.G;
+  auto column = [&](int t, int u) {
+    const int r = row0 + t * M::kRows + u * 32 + col, rr = min(r, rows - 1), token = A.token_of(rr), g = rr - token * A.G, qh = head * A.G + g, s = pr.slot0 + token;
+    Column x;
+    x.norm = norm_first[(uint64_t)(uint32_t)token * (uint32_t)hq + (uint32_t)g];
+    x.limit = r < rows ? limit_of(pr, s) : 0;
+    x.slope = MOD && A.mods.slopes ? ((const gfloat*)A.mods.slopes)[qh] * kLog2e : 0.0f;
+    x.pos = MOD && A.mods.slopes ? (float)pos[s] : 0.0f;
+    x.doc = MOD && doc ? doc[s] : 0;
+    if (MOD && doc && x.doc < 0) x.limit = 0;
+    return x;
+  };
+  f32x16 s0[NB], s1[NB];       // scores of a step's first and second block of rows
+  float sum[NB][16];
 #pragma unroll
-      for (int i = 0; i < 6; ++i) ((ADSA_LDS float*)(lds + MassLds<EB, D>::kInfo))[i * kMassRows + tid] = info[i];
+  for (int x = 0; x < NB; ++x)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum[x][i] = 0.0f;
+  const float scale = MOD ? 1.0f : A.mods.scale_log2;
+  auto product = [&](f32x16 (&next)[NB], int x, int c, const uint4& q) {
+    const f32x16 z = {};
+    const f32x16& to = c == 0 ? z : next[x];
+    if constexpr (EB == 2) next[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[x][c]), __builtin_bit_cast(bf16x8, q), to, 0, 0, 0);
+    else {
+      f32x16 y = to;
+      const uint32_t ka[4] = {kf[x][c].x, kf[x][c].y, kf[x][c].z, kf[x][c].w}, qa[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(ka[e]), __uint_as_float(qa[e]), y, 0, 0, 0);
+      next[x] = y;
     }
-    __syncthreads();
-    if (base + kMassRows < rows) load(base + kMassRows);
+  };
+  auto count = [&](const f32x16 (&s)[NB], int e, const Column& y) {         // score number e of the lane's NB * 16
+    const int x = e / 16, i = e % 16;
+    sum[x][i] += fast_exp2(fmaf(s[x][i], scale, -y.norm));
+  };
+  // what comes before the exponentials where not all is seen, or scores are changed
+  auto prepare = [&](f32x16 (&s)[NB], const Column& y) {
+    if constexpr (MOD) {
 #pragma unroll
-    for (int u = 0; u < kMassRows / 32; ++u) {
-      f32x16 s = {};
-      const lchar* const qrow = lds + (u * 32 + col) * RB;
-      const int sw = L::swz_k(u * 32 + col);
+      for (int x = 0; x < NB; ++x)
 #pragma unroll
-      for (int c = 0; c < CPR / 2; ++c) {
-        const uint4 a = lds16(qrow + (((2 * c + half) ^ sw) << 4));
-        if constexpr (EB == 2) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, kf[c]), s, 0, 0, 0);
-        else {
-          const uint32_t qa[4] = {a.x, a.y, a.z, a.w}, ka[4] = {kf[c].x, kf[c].y, kf[c].z, kf[c].w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(qa[e]), __uint_as_float(ka[e]), s, 0, 0, 0);
+        for (int i = 0; i < 16; ++i) {
+          float z = A.mods.cap_out != 0.0f ? capped<EB>(s[x][i], A.mods) : s[x][i] * A.mods.scale_log2;
+          if (A.mods.slopes) z = fmaf(-y.slope, fabsf(y.pos - kpos[x][i]), z);
+          s[x][i] = z;
         }
-      }
+    }
+    const int last = mine + NB * 32;
+    if ((MOD && doc) || __ballot(y.limit < last) != 0) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int r = u * 32 + (i / 4) * 8 + half * 4 + i % 4;
-        float z = s[i];
-        if constexpr (MOD) {
-          z = A.mods.cap_out != 0.0f ? capped<EB>(z, A.mods) : z * A.mods.scale_log2;
-          if (A.mods.slopes) z = fmaf(-at[3 * kMassRows + r], fabsf(at[4 * kMassRows + r] - kpos), z);
+      for (int x = 0; x < NB; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          bool seen = mine + x * 32 + (i / 4) * 8 + half * 4 + i % 4 < y.limit;
+          if constexpr (MOD)
+            if (doc) seen &= kdoc[x][i] == y.doc;
+          s[x][i] = seen ? s[x][i] : -INFINITY;
         }
-        bool seen = key < __float_as_int(at[2 * kMassRows + r]);
-        if constexpr (MOD)
-          if (doc) seen &= __float_as_int(at[5 * kMassRows + r]) == kdoc;
-        const float p = fast_exp2(fmaf(z, scale, -at[r])) * at[kMassRows + r];
-        sum += seen ? p : 0.0f;
+    }
+  };
+  // the products of block u of step t beside the exponentials of the block before (LAST: there is one)
+  auto block = [&](f32x16 (&next)[NB], int t, int u, auto last, f32x16 (&s)[NB], const Column& y) {
+    constexpr bool kLast = decltype(last)::value;
+    if constexpr (kLast) prepare(s, y);
+    const lchar* const qrow = lds + (t & 1) * M::kTile + (u * 32 + col) * RB;
+    const int sw = L::swz_k(col);
+    uint4 q[KC];
+    auto fetch = [&](auto at) {
+      constexpr int c = decltype(at)::value;
+      if constexpr (c < KC) q[c] = lds16(qrow + (((2 * c + half) ^ sw) << 4));
+    };
+    each<2>(fetch);
+    each<KC>([&](auto at) {
+      constexpr int c = decltype(at)::value;
+      fetch(std::integral_constant<int, c + 2>());
+#pragma unroll
+      for (int x = 0; x < NB; ++x) product(next, x, c, q[c]);
+      if constexpr (kLast) {
+        constexpr int e0 = NB * 16 * c / KC, e1 = NB * 16 * (c + 1) / KC;
+        each<e1 - e0>([&](auto o) { count(s, e0 + decltype(o)::value, y); });
       }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  load(0);
+  store(0);
+  Column y0 = column(0, 0), y1;
+  if (steps > 1) load(1);
+  __syncthreads();
+  block(s0, 0, 0, std::false_type(), s1, y0);
+  for (int t = 0; t < steps; ++t) {
+    y1 = column(t, 1);
+    block(s1, t, 1, std::true_type(), s0, y0);
+    if (t + 1 < steps) {
+      store(t + 1);                                  // (the buffer's rows were read before the barrier below, a step ago)
+      y0 = column(t + 1, 0);
+      if (t + 2 < steps) load(t + 2);
+      __syncthreads();
+      block(s0, t + 1, 0, std::true_type(), s1, y1);
     }
   }
-  sum = xor_sum<32>(sum);
-  if (half == 0 && key < n) {
-    gfloat* const score = (gfloat*)sq.score + (size_t)head * A.cap + key;
-    *score = *score + sum;
-  }
+  prepare(s1, y1);
+#pragma unroll
+  for (int e = 0; e < NB * 16; ++e) count(s1, e, y1);
+  // the 32 lanes of a half meet
+  gfloat* const score = (gfloat*)sq.score + (size_t)head * A.cap;
+#pragma unroll
+  for (int x = 0; x < NB; ++x)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float v = row_sum<16>(sum[x][i]);
+      v = xor_sum<16>(v);
+      const int slot = mine + x * 32 + (i / 4) * 8 + half * 4 + i % 4;
+      if (col == i && slot < n) score[slot] = score[slot] + v;
+    }
 }
 
 // ---------------------------------------------------------------------------------------------------- shared prompts
@@ -1326,7 +1426,8 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(S
       const size_t at = (size_t)b * hq + qh;
       t.row = {keys.end, MOD && A.mods.slopes ? query_pos(b) : 0, 0, MOD && A.mods.slopes ? ((const gfloat*)A.mods.slopes)[qh] * kLog2e : 0.0f};
       t.load_q((const gchar*)A.q + at * (D * EB));
-      t.run();
+      if constexpr (BIG) t.run(keys.end);
+      else t.run();
       if (r < rows) store(t, at, chunk);
     };
     if (keys.begin >= keys.end) {
@@ -1334,7 +1435,7 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(S
       return;
     }
     if constexpr (BIG) {
-      Flow<D, WK, MOD> t(A.mods, keys, (lchar*)s_lds);
+      Flow<D, WK, MOD ? kAny : kPlain> t(A.mods, keys, (lchar*)s_lds);
       attend(t, tile * kRows + t.wave * 32 + t.col);
     } else {
       Tile<EB, D, 1, WK, 32, MOD, false, true> t(A.mods, keys, (lchar*)s_lds);
@@ -1575,6 +1676,11 @@ bool modded(const Mods& m) { return m.slopes || m.doc || m.cap_out != 0.0f; }
 template <int EB> constexpr int kStepKeys = EB == 2 ? 64 : 32;
 template <int EB, int D> constexpr int kKeyWaves = EB == 4 && D == 128 ? 2 : 4;
 
+// Workgroups of 8 waves (256 rows), where 4 waves' share of staging a tile leaves too few registers.  us with 4 | 8 waves, 2 x 4352 x 32 x 128 lowered with
+// distance 1281 | 953; elsewhere 4 waves are as fast or faster: 4 x 4352 x 32 x 128 820 | 797, capped ragged prompts of 64 over 8 heads
+// 247 | 267, 16 x 300..600 x 24 x 64 36 | 51.
+template <int D, int MODS> constexpr bool two_sizes = D == 128 && MODS == kAny;
+
 template <int EB, int D, bool MOD>
 hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStream_t st) {
   const unsigned pairs = (unsigned)((A.n_seq * A.h + 7) / 8 * 8);
@@ -1583,8 +1689,20 @@ hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStrea
   if (plan.rows <= 32) k_prompt<EB, D, 1, KW, 32, MOD><<<grid, KW * kWave, Shape<EB, D, 1, KW, 32>::kLds, st>>>(A);
   else if (EB == 2 && plan.flow) {
     if constexpr (EB == 2) {
-      if (plan.rows == 128) k_prompt_many<D, 4, MOD><<<grid, 4 * kWave, Flow<D, 4, MOD>::kLds, st>>>(A);
-      else k_prompt_many<D, 8, MOD><<<grid, 8 * kWave, Flow<D, 8, MOD>::kLds, st>>>(A);
+      auto many = [&](auto mods) {
+        constexpr int M = decltype(mods)::value;
+        if constexpr (two_sizes<D, M>)
+          if (plan.rows_all > 128 && plan.chunks == 1) {
+            PromptArgs B = A;
+            B.tiles = (plan.rows_all + 255) / 256;
+            k_prompt_many<D, 8, M><<<dim3(pairs * (unsigned)B.tiles), 8 * kWave, Flow<D, 8, M>::kLds, st>>>(B);
+            return;
+          }
+        k_prompt_many<D, 4, M><<<grid, 4 * kWave, Flow<D, 4, M>::kLds, st>>>(A);
+      };
+      if constexpr (!MOD) many(std::integral_constant<int, kPlain>());
+      else if (A.mods.slopes || A.mods.doc) many(std::integral_constant<int, kAny>());
+      else many(std::integral_constant<int, kCapped>());
     }
   } else k_prompt<EB, D, 4, 1, KT, MOD><<<grid, 4 * kWave, Shape<EB, D, 4, 1, KT>::kLds, st>>>(A);
   if (plan.chunks > 1) {
@@ -1592,8 +1710,8 @@ hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStrea
     k_prompt_finish<EB, D><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, st>>>(A);
   }
   if (A.norm) {
-    const int key_tiles = (A.cap + kMassKeys - 1) / kMassKeys;
-    k_prompt_mass<EB, D, MOD><<<dim3(pairs * (unsigned)key_tiles), 256, MassLds<EB, D>::kLds, st>>>(A, key_tiles);
+    const int key_tiles = (A.cap + Mass<EB, D, MOD>::kKeys - 1) / Mass<EB, D, MOD>::kKeys;
+    k_prompt_mass<EB, D, MOD><<<dim3(pairs * (unsigned)key_tiles), 256, Mass<EB, D, MOD>::kLds, st>>>(A, key_tiles);
   }
   return hipGetLastError();
 }
@@ -1601,7 +1719,7 @@ hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStrea
 template <int EB, int D, bool MOD, bool BIG>
 constexpr int shared_lds = [] {
   const int own = Shape<EB, D, 1, kKeyWaves<EB, D>, 32>::kLds;
-  if constexpr (BIG) return std::max(own, Flow<D, 4, MOD>::kLds);
+  if constexpr (BIG) return std::max(own, Flow<D, 4, MOD ? kAny : kPlain>::kLds);
   else return own;
 }();
 
@@ -1630,12 +1748,20 @@ hipError_t allow_lds() {
   };
   allow(k_prompt<EB, D, 1, KW, 32, MOD>, Shape<EB, D, 1, KW, 32>::kLds);
   allow(k_prompt<EB, D, 4, 1, KT, MOD>, Shape<EB, D, 4, 1, KT>::kLds);
-  allow(k_prompt_mass<EB, D, MOD>, MassLds<EB, D>::kLds);
+  allow(k_prompt_mass<EB, D, MOD>, Mass<EB, D, MOD>::kLds);
   allow(k_shared<EB, D, KW, MOD, true, false>, shared_lds<EB, D, MOD, false>);
   allow(k_shared<EB, D, KW, MOD, false, false>, shared_lds<EB, D, MOD, false>);
   if constexpr (EB == 2) {
-    allow(k_prompt_many<D, 4, MOD>, Flow<D, 4, MOD>::kLds);
-    allow(k_prompt_many<D, 8, MOD>, Flow<D, 8, MOD>::kLds);
+    auto many = [&](auto mods) {
+      constexpr int M = decltype(mods)::value;
+      allow(k_prompt_many<D, 4, M>, Flow<D, 4, M>::kLds);
+      if constexpr (two_sizes<D, M>) allow(k_prompt_many<D, 8, M>, Flow<D, 8, M>::kLds);
+    };
+    if constexpr (!MOD) many(std::integral_constant<int, kPlain>());
+    else {
+      many(std::integral_constant<int, kCapped>());
+      many(std::integral_constant<int, kAny>());
+    }
     allow(k_shared<EB, D, KW, MOD, true, true>, shared_lds<EB, D, MOD, true>);
     allow(k_shared<EB, D, KW, MOD, false, true>, shared_lds<EB, D, MOD, true>);
   }
@@ -1674,7 +1800,8 @@ PromptPlan make_prompt_plan(const adsa_params& p, const adsa_tokens& t) {
   PromptPlan plan;
   // (a tile's rows are reached with 32-bit offsets from its first)
   plan.flow = p.dtype == ADSA_BF16 && p.kv_slot_stride * 2 * 64 < (1ll << 31);
-  plan.rows = rows <= 32 ? 32 : rows <= 128 || !plan.flow ? 128 : 256;
+  plan.rows = rows <= 32 ? 32 : 128;
+  plan.rows_all = (int)rows;
   plan.tiles = (int)((rows + plan.rows - 1) / plan.rows);
   const long long groups = pairs * plan.tiles;
   plan.chunks = (int)std::clamp<long long>(std::min<long long>((512 + groups - 1) / groups, (p.cap + 255) / 256), 1, kMaxChunks);
@@ -1687,7 +1814,7 @@ PromptWorkspace make_prompt_workspace(const adsa_params& p, const adsa_tokens& t
   w.part_ml_off = 0;
   w.part_acc_off = w.part_ml_off + (plan.chunks > 1 ? up256(rows * plan.chunks * 8) : 0);
   w.norm_off = w.part_acc_off + (plan.chunks > 1 ? up256(rows * plan.chunks * p.head_dim * 4) : 0);
-  w.total = w.norm_off + (p.score_mode == ADSA_SCORE_ATTN_MASS ? up256(rows * 8) : 0);
+  w.total = w.norm_off + (p.score_mode == ADSA_SCORE_ATTN_MASS ? up256(rows * 4) : 0);
   w.total = std::max<size_t>(w.total, 256);
   return w;
 }
@@ -1728,6 +1855,7 @@ hipError_t launch_prefill(const adsa_params& p, const adsa_tokens& t, const adsa
   A.head_stride_b = p.kv_head_stride * elem_bytes(p);
   A.n_seq = p.n_seq; A.n_tokens = t.n_tokens; A.max_len = t.max_len; A.h = p.n_heads; A.G = query_group(p); A.cap = p.cap; A.mask = mods.mask;
   A.tiles = plan.tiles; A.chunks = plan.chunks; A.advance = advance ? 1 : 0;
+  A.inv_G = A.G > 1 ? (uint32_t)(((1ull << 32) + A.G - 1) / A.G) : 0;
   return by_type(p, modded(A.mods), [&](auto eb, auto d, auto m) {
     return prompt_launches<decltype(eb)::value, decltype(d)::value, decltype(m)::value>(A, plan, st);
   });
