@@ -157,14 +157,18 @@ class LayerBatch:
                            self.keep_map, flags, stream)
 
     # ---- prompts
-    def _space(self, need: int, where: str) -> torch.Tensor:
-        """Workspace of at least `need` bytes, kept for the calls to come (the first call of a size allocates: make it before a
-        graph is captured)."""
-        if need == 0:
-            raise B.AdsaError(-2, where + " (invalid parameters)")
-        if self.prompt_workspace is None or self.prompt_workspace.numel() < need:
-            self.prompt_workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
-        return self.prompt_workspace
+    def _with_workspace(self, call, need) -> None:
+        """call(workspace), with a larger one where that is refused as too small.  It is kept for the calls to come: the first call of a
+        size allocates, so make it before a graph is captured."""
+        if self.prompt_workspace is not None:
+            try:
+                return call(self.prompt_workspace)
+            except B.AdsaError as e:
+                if e.code != B.ERR_WORKSPACE:
+                    raise
+        n = need()
+        self.prompt_workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=self.device)
+        call(self.prompt_workspace)
 
     def rotate(self, rope, q, k, q_out, k_out, coords=None, flags: int = 0, stream=None, q_stride: int = 0, k_stride: int = 0):
         B.adsa_rotate(self.params, rope, self.seqs, q, k, q_out, k_out, coords, flags, stream, q_stride, k_stride)
@@ -173,12 +177,13 @@ class LayerBatch:
         B.adsa_append(self.params, tokens, rope, self.seqs, q, k, v, q_out, flags, stream)
 
     def prefill(self, tokens, q, out, lse, mods=None, flags: int = 0, stream=None):
-        ws = self._space(B.adsa_prefill_workspace_bytes(self.params, tokens), "adsa_prefill")
-        B.adsa_prefill(self.params, tokens, mods, self.seqs, q, out, lse, ws, flags, stream)
+        self._with_workspace(lambda ws: B.adsa_prefill(self.params, tokens, mods, self.seqs, q, out, lse, ws, flags, stream),
+                             lambda: B.adsa_prefill_workspace_bytes(self.params, tokens))
 
     def attend_shared(self, shared, q, k_new=None, v_new=None, flags: int = 0, mods=None, stream=None):
-        ws = self._space(B.adsa_shared_workspace_bytes(self.params, shared), "adsa_attend_shared")
-        B.adsa_attend_shared(self.params, shared, mods, self.seqs, q, k_new, v_new, self.sel_idx, self.sel_cnt, self.out, self.lse, ws, flags, stream)
+        self._with_workspace(lambda ws: B.adsa_attend_shared(self.params, shared, mods, self.seqs, q, k_new, v_new, self.sel_idx, self.sel_cnt, self.out,
+                                                             self.lse, ws, flags, stream),
+                             lambda: B.adsa_shared_workspace_bytes(self.params, shared))
 
 
 class ModelBatch(LayerBatch):

@@ -108,6 +108,64 @@ static PyObject* call_static(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   return call_c(a, n, 0);
 }
 
+/* ---- prompts: every argument is a 64-bit integer, a pointer as above, or a host struct (a ctypes Structure, or None) */
+typedef int (*fn_rotate)(const void*, const void*, const void*, const void*, const void*, const void*, int64_t, int64_t, void*, void*, uint32_t, void*);
+typedef int (*fn_append)(const void*, const void*, const void*, void*, const void*, const void*, const void*, void*, uint32_t, void*);
+typedef int (*fn_prefill)(const void*, const void*, const void*, void*, const void*, void*, void*, uint32_t, void*, size_t, void*);
+typedef int (*fn_shared)(const void*, const void*, const void*, void*, const void*, const void*, const void*, const void*, const void*, void*, void*, uint32_t, void*, size_t, void*);
+
+/* the address a host struct's buffer has (structs live as long as the call: the arguments hold them) */
+static int as_struct(PyObject* x, const void** out) {
+  if (x == Py_None) { *out = NULL; return 0; }
+  Py_buffer b;
+  if (PyObject_GetBuffer(x, &b, PyBUF_SIMPLE) < 0) return -1;
+  *out = b.buf;
+  PyBuffer_Release(&b);
+  return 0;
+}
+
+/* call_prompt(which, address of the C function, host structs x 2 or 3, flags, stream, workspace, pointers and strides...) */
+static PyObject* call_prompt(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  (void)self;
+  const long which = n > 0 ? PyLong_AsLong(a[0]) : -1;        /* 0 rotate, 1 append, 2 prefill, 3 attend_shared */
+  static const Py_ssize_t counts[4] = {8, 5, 4, 8};           /* pointers and strides of each */
+  if (PyErr_Occurred()) return NULL;
+  if (which < 0 || which > 3 || n != 8 + counts[which]) {
+    PyErr_SetString(PyExc_TypeError, "wrong number of arguments");
+    return NULL;
+  }
+  void *fn, *stream, *ws, *p[8];
+  const void* h[3];
+  size_t ws_bytes = 0;
+  int64_t stride[2] = {0, 0};
+  if (as_pointer(a[1], &fn) < 0) return NULL;
+  const int typed = params_type ? PyObject_IsInstance(a[2], params_type) : 0;
+  if (typed < 0) return NULL;
+  if (!typed) {
+    PyErr_SetString(PyExc_TypeError, "params: AdsaParams expected");
+    return NULL;
+  }
+  for (int i = 0; i < 3; ++i)
+    if (as_struct(a[2 + i], &h[i]) < 0) return NULL;
+  const unsigned long flags = PyLong_AsUnsignedLongMask(a[5]);
+  if (PyErr_Occurred() || as_pointer(a[6], &stream) < 0 || as_pointer(a[7], &ws) < 0 || as_bytes(a[7], &ws_bytes) < 0) return NULL;
+  for (Py_ssize_t i = 0; i < counts[which]; ++i) {
+    if (which == 0 && i >= 6) {
+      stride[i - 6] = PyLong_AsLongLong(a[8 + i]);
+      if (PyErr_Occurred()) return NULL;
+    } else if (as_pointer(a[8 + i], &p[i]) < 0) return NULL;
+  }
+  const uint32_t f = (uint32_t)flags;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  if (which == 0) rc = ((fn_rotate)fn)(h[0], h[1], p[0], p[1], p[2], p[3], stride[0], stride[1], p[4], p[5], f, stream);
+  else if (which == 1) rc = ((fn_append)fn)(h[0], h[1], h[2], p[0], p[1], p[2], p[3], p[4], f, stream);
+  else if (which == 2) rc = ((fn_prefill)fn)(h[0], h[1], h[2], p[0], p[1], p[2], p[3], f, ws, ws_bytes, stream);
+  else rc = ((fn_shared)fn)(h[0], h[1], h[2], p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], f, ws, ws_bytes, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
 /* the ctypes mirror of adsa_params that the calls take */
 static PyObject* set_params_type(PyObject* self, PyObject* type) {
   (void)self;
@@ -118,7 +176,8 @@ static PyObject* set_params_type(PyObject* self, PyObject* type) {
 
 static PyMethodDef methods[] = {{"set_params_type", set_params_type, METH_O, "The type of the calls' params."},
                                 {"call", (PyCFunction)(void (*)(void))call_entry, METH_FASTCALL, "One C call."},
-                                {"call_static", (PyCFunction)(void (*)(void))call_static, METH_FASTCALL, "One call of adsa_step_static."}, {NULL, NULL, 0, NULL}};
+                                {"call_static", (PyCFunction)(void (*)(void))call_static, METH_FASTCALL, "One call of adsa_step_static."},
+                                {"call_prompt", (PyCFunction)(void (*)(void))call_prompt, METH_FASTCALL, "One call of the prompt side."}, {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_adsa_native", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__adsa_native(void) {

@@ -926,9 +926,31 @@ __device__ __forceinline__ bool job_of(const PromptArgs& A, Job& J) {
   // what the tile's last row sees (a row of the prefix may see more than later rows)
   const int end = min(J.row0 + ROWS, J.rows), last_slot = J.pr.slot0 + (end + A.G - 1) / A.G - 1, first_slot = J.pr.slot0 + J.row0 / A.G;
   const int n = max(limit_of(J.pr, last_slot), limit_of(J.pr, first_slot));
-  const int per = A.chunks == 1 ? n : ((n + A.chunks - 1) / A.chunks + 31) / 32 * 32;
-  keys.begin = min(n, J.chunk * per);
-  keys.end = min(n, keys.begin + per);
+  int first = 0, last = n;
+  if (keys.doc) {                                    // (uniform) only from the first to the last slot of a document that the tile's rows belong to
+    __shared__ int s_doc[4];                         // least and greatest of the rows' documents, first and last slot of one among them
+    if (tid < 4) s_doc[tid] = tid == 0 || tid == 2 ? 0x7FFFFFFF : -1;
+    __syncthreads();
+    const int slots = last_slot - first_slot + 1;
+    for (int i = tid; i < slots; i += THREADS) {
+      const int d = keys.doc[first_slot + i];
+      if (d >= 0) { atomicMin(&s_doc[0], d); atomicMax(&s_doc[1], d); }
+    }
+    __syncthreads();
+    const int least = s_doc[0], most = s_doc[1];
+    int lo = 0x7FFFFFFF, hi = -1;
+    for (int i = tid; i < n; i += THREADS) {
+      const int d = keys.doc[i];
+      if (d >= least && d <= most) { lo = min(lo, i); hi = i; }
+    }
+    if (hi >= 0) { atomicMin(&s_doc[2], lo); atomicMax(&s_doc[3], hi); }
+    __syncthreads();
+    first = s_doc[3] < 0 ? 0 : s_doc[2] / 32 * 32;
+    last = s_doc[3] < 0 ? min(n, 1) : s_doc[3] + 1;  // (none: one key, which nobody sees)
+  }
+  const int m = last - first, per = A.chunks == 1 ? m : ((m + A.chunks - 1) / A.chunks + 31) / 32 * 32;
+  keys.begin = min(last, first + J.chunk * per);
+  keys.end = min(last, keys.begin + per);
   return true;
 }
 // Row number r of the job (past the last one: that one again): its place among the packed rows, and what it sees.

@@ -133,10 +133,38 @@ __device__ __forceinline__ Token append_token(const RotateArgs& A, int t, bool w
 
 template <int EB, int D, bool IN32, bool NEAR, bool APPEND>
 __global__ __launch_bounds__(kRotThreads) void k_rotate(RotateArgs A) {
-  constexpr int kPairs = D / 2, IB = IN32 ? 4 : EB;
+  constexpr int kPairs = D / 2, IB = IN32 ? 4 : EB, kPieces = kPairs / 8;
   __shared__ RotateShared<D> sh;
   const int tid = threadIdx.x, t0 = (int)(blockIdx.x / (unsigned)A.parts) * A.tokens_here, part = (int)(blockIdx.x % (unsigned)A.parts);
   const int n_here = min(A.tokens_here, A.n_tokens - t0);
+  // rows: q heads, k heads, then (append) v heads; a thread takes 8 pairs of a row, as two vectors of 8 elements, from ea and eb on
+  const int q_rows = A.q ? A.hq : 0, rows = q_rows + (APPEND ? 2 : 1) * A.h;
+  const int first = rows * part / A.parts, mine = rows * (part + 1) / A.parts - first, work = n_here * mine * kPieces;
+  const int piece = tid % kPieces, ea = NEAR ? piece * 16 : piece * 8, eb = NEAR ? ea + 8 : ea + kPairs;       // (kRotThreads is a multiple of kPieces)
+  int i = tid / kPieces / mine, r = tid / kPieces - i * mine;        // the thread's token and row of its part
+  struct Place {
+    bool is_q, is_v;
+    int head;
+  };
+  auto place = [&](int row) { return Place{row < q_rows, row >= q_rows + A.h, row < q_rows ? row : row >= q_rows + A.h ? row - q_rows - A.h : row - q_rows}; };
+  float a[8], b[8];
+  auto fetch = [&](int i, int r) {
+    const Place p = place(first + r);
+    const long long t = t0 + i;
+    const gchar* const in = (p.is_q ? (const gchar*)A.q + t * A.q_stride_b : p.is_v ? (const gchar*)A.v + t * A.v_stride_b : (const gchar*)A.k + t * A.k_stride_b) + p.head * (D * IB);
+    load8<IB == 4>(in + ea * IB, a);
+    load8<IB == 4>(in + eb * IB, b);
+  };
+  // ---- on their way together: the thread's first piece, its token and its pair's frequencies
+  if (tid < work) fetch(i, r);
+  const int ai = tid / kPairs, pair = tid % kPairs;                  // the angle that this thread forms
+  const bool turns_one = A.freq && tid < n_here * kPairs;
+  double f[3] = {0.0, 0.0, 0.0};
+  if (turns_one) {
+#pragma unroll
+    for (int x = 0; x < 3; ++x)
+      if (x < A.n_axes) f[x] = ((const ADSA_GLOBAL double*)A.freq)[x * kPairs + pair];
+  }
   if (tid < n_here) {
     const int t = t0 + tid;
     if constexpr (APPEND) sh.token[tid] = append_token(A, t, part == 0);
@@ -147,82 +175,60 @@ __global__ __launch_bounds__(kRotThreads) void k_rotate(RotateArgs A) {
     }
   }
   __syncthreads();
-  if (A.freq && tid < n_here * kPairs) {
-    const int i = tid / kPairs, pair = tid % kPairs, t = t0 + i;
+  if (turns_one) {
     double c[3] = {0.0, 0.0, 0.0};
     if (A.coords) {
 #pragma unroll
-      for (int a = 0; a < 3; ++a)
-        if (a < A.n_axes) c[a] = ((const gint*)A.coords)[(size_t)t * A.n_axes + a];
-    } else if (sh.token[i].ok) {
-      const int pos = sh.token[i].pos, origin = sh.token[i].origin;
+      for (int x = 0; x < 3; ++x)
+        if (x < A.n_axes) c[x] = ((const gint*)A.coords)[(size_t)(t0 + ai) * A.n_axes + x];
+    } else if (sh.token[ai].ok) {
+      const int pos = sh.token[ai].pos, origin = sh.token[ai].origin;
       int col = 0, row = 0;
       if (pos >= origin) row = A.grid.row(pos - origin, &col);
 #pragma unroll
-      for (int a = 0; a < 3; ++a)
-        c[a] = pos < origin ? (double)A.text[a] * pos : (double)A.origin[a] * origin + (double)A.row[a] * row + (double)A.col[a] * col;
+      for (int x = 0; x < 3; ++x)
+        c[x] = pos < origin ? (double)A.text[x] * pos : (double)A.origin[x] * origin + (double)A.row[x] * row + (double)A.col[x] * col;
     }
-    const ADSA_GLOBAL double* const f = (const ADSA_GLOBAL double*)A.freq + pair;
     double angle = 0.0;
 #pragma unroll
-    for (int a = 0; a < 3; ++a)
-      if (a < A.n_axes) angle = fma(c[a], f[a * kPairs], angle);
-    double turns = angle * 0.15915494309189533577;              // 1 / (2 pi)
-    turns = 2.0 * (turns - rint(turns));                        // half turns, -1 .. 1
+    for (int x = 0; x < 3; ++x) angle = fma(c[x], f[x], angle);      // (axes that are not there have 0)
+    double turns = angle * 0.15915494309189533577;                   // 1 / (2 pi)
+    turns = 2.0 * (turns - rint(turns));                             // half turns, -1 .. 1
     const float x = (float)turns, d = (float)(turns - x) * 3.14159265358979f;
     float s, co;
     sincospif(x, &s, &co);
     sh.turn[tid] = make_float2(fmaf(-s, d, co), fmaf(co, d, s));
   }
   __syncthreads();
-  // rows: q heads, k heads, then (append) v heads; a thread takes 8 pairs of a row
-  constexpr int kPieces = kPairs / 8;
-  const int q_rows = A.q ? A.hq : 0, rows = q_rows + (APPEND ? 2 : 1) * A.h;
-  const int first = rows * part / A.parts, mine = rows * (part + 1) / A.parts - first, work = n_here * mine * kPieces;
   for (int w = tid; w < work; w += kRotThreads) {
-    const int piece = w % kPieces, rr = w / kPieces, i = rr / mine, r = first + rr % mine, t = t0 + i;
     const Token tk = sh.token[i];
-    const bool is_q = r < q_rows, is_v = r >= q_rows + A.h;
-    const int head = is_q ? r : is_v ? r - q_rows - A.h : r - q_rows;
-    // the 8 pairs as two vectors of 8: (x, y) of a pair 8 elements apart in memory order of the loads
-    const int ea = NEAR ? piece * 16 : piece * 8, eb = NEAR ? ea + 8 : ea + kPairs;
+    const Place p = place(first + r);
+    float x[8], y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { x[e] = tk.ok ? a[e] : 0.0f; y[e] = tk.ok ? b[e] : 0.0f; }
+    const float2* const turn = sh.turn + i * kPairs + piece * 8;
     gchar* out;
-    if (is_q) out = (gchar*)A.q_out + ((size_t)t * A.hq + head) * (D * EB);
-    else if constexpr (APPEND) out = (is_v ? tk.v : tk.k) + head * A.head_stride_b;
-    else out = (gchar*)A.k_out + ((size_t)t * A.h + head) * (D * EB);
-    float a[8], b[8];
-    if (!tk.ok) {
-      if (APPEND && !is_q) continue;
+    if (p.is_q) out = (gchar*)A.q_out + ((size_t)(t0 + i) * A.hq + p.head) * (D * EB);
+    else if constexpr (APPEND) out = (p.is_v ? tk.v : tk.k) + p.head * A.head_stride_b;
+    else out = (gchar*)A.k_out + ((size_t)(t0 + i) * A.h + p.head) * (D * EB);
+    // the next piece leaves before this one is stored (which nobody else reads or writes)
+    r += kRotThreads / kPieces;
+    while (r >= mine) { r -= mine; ++i; }
+    if (w + kRotThreads < work) fetch(i, r);
+    if (A.freq && !p.is_v && tk.ok) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) a[e] = b[e] = 0.0f;
-    } else {
-      const gchar* const in = is_q ? (const gchar*)A.q + t * A.q_stride_b : is_v ? (const gchar*)A.v + t * A.v_stride_b : (const gchar*)A.k + t * A.k_stride_b;
-      load8<IB == 4>(in + (head * D + ea) * IB, a);
-      load8<IB == 4>(in + (head * D + eb) * IB, b);
-      if (A.freq && !is_v) {
-        const float2* const turn = sh.turn + i * kPairs + piece * 8;
-        if constexpr (NEAR) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float2 cs = turn[e];
-            float* const v = e < 4 ? a + 2 * e : b + 2 * (e - 4);
-            const float x = v[0], y = v[1];
-            v[0] = x * cs.x - y * cs.y;
-            v[1] = y * cs.x + x * cs.y;
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float2 cs = turn[e];
-            const float x = a[e], y = b[e];
-            a[e] = x * cs.x - y * cs.y;
-            b[e] = y * cs.x + x * cs.y;
-          }
-        }
+      for (int e = 0; e < 8; ++e) {
+        const float2 cs = turn[e];
+        float& u = NEAR ? (e < 4 ? x[2 * e] : y[2 * e - 8]) : x[e];
+        float& v = NEAR ? (e < 4 ? x[2 * e + 1] : y[2 * e - 7]) : y[e];
+        const float u0 = u, v0 = v;
+        u = u0 * cs.x - v0 * cs.y;
+        v = v0 * cs.x + u0 * cs.y;
       }
     }
-    store8<EB>(out + ea * EB, a);
-    store8<EB>(out + eb * EB, b);
+    if (APPEND && !tk.ok && !p.is_q) continue;
+    store8<EB>(out + ea * EB, x);
+    store8<EB>(out + eb * EB, y);
   }
 }
 
@@ -247,9 +253,10 @@ hipError_t launch(const adsa_params& p, RotateArgs& A, const adsa_rope* rope, bo
     for (int a = 0; a < ADSA_MAX_AXES; ++a) { A.text[a] = rope->text[a]; A.origin[a] = rope->origin[a]; A.row[a] = rope->row[a]; A.col[a] = rope->col[a]; }
   }
   // Few tokens: a token per workgroup, and its rows in as many parts as there are 256-thread pieces of them, so that every thread
-  // has one piece of work behind the angles.  Many: as many tokens as have their angles formed by one round of the threads.
+  // has one piece of work behind the angles.  Many: about six pieces a thread, the next on its way while one is turned.  us at one token a
+  // workgroup | two | four | eight, 4352 tokens of 24 + 2 x 24 heads x 64: 22 | 18.8 | 16.9 | 18.0 (80 MB); 9216 of 32 + 2 x 32 x 128: - | 93 | 101 | - (453 MB).
   const int rows = (A.q ? A.hq : 0) + (APPEND ? 2 : 1) * A.h;
-  A.tokens_here = std::clamp(A.n_tokens / 512, 1, kRotThreads / pairs);
+  A.tokens_here = std::clamp(std::min(A.n_tokens / 512, 6 * kRotThreads / (rows * (pairs / 8))), 1, kRotThreads / pairs);
   A.parts = A.tokens_here == 1 ? std::clamp(rows * (pairs / 8) / kRotThreads, 1, 8) : 1;
   const dim3 grid((unsigned)((A.n_tokens + A.tokens_here - 1) / A.tokens_here * A.parts));
   const bool near = rope && rope->pairing == ADSA_PAIR_NEIGHBOURS;
