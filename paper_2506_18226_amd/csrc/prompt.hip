@@ -64,11 +64,12 @@ struct Keys {
   gfloat* logits;              // own lists: scores of row 0 of the tile, log2 units; the next row's lg_stride on
   int lg_stride, lg_rows;
   int begin, end, last_slot, skip;     // skip: a slot that is not attended
+  int pos0;                    // positions are taken from here (slopes): fp32 holds near ones whole, whatever the absolute ones are
 };
 
 // A lane's row: what it sees are keys below `limit` (of its document).
 struct Row {
-  int limit, pos, doc;
+  int limit, pos, doc;         // pos: from the keys' pos0
   float slope;                 // log2 units
 };
 
@@ -198,7 +199,7 @@ struct Tile {
       if constexpr (LIST) meta_slot = keys.list[at];
       if constexpr (MOD) {
         const int slot = slot_at(base + brought());
-        meta_pos = mods.slopes ? (float)keys.pos[slot] : 0.0f;
+        meta_pos = mods.slopes ? (float)(keys.pos[slot] - keys.pos0) : 0.0f;
         meta_doc = keys.doc ? keys.doc[slot] : 0;
       }
     }
@@ -583,7 +584,7 @@ struct Flow {
     if constexpr (MOD)
       if (tid < TK) {
         const int slot = min(base + tid, keys.end - 1);
-        meta_pos = mods.slopes ? __float_as_int((float)keys.pos[slot]) : 0;
+        meta_pos = mods.slopes ? __float_as_int((float)(keys.pos[slot] - keys.pos0)) : 0;
         meta_doc = keys.doc ? keys.doc[slot] : 0;
       }
   }
@@ -921,6 +922,7 @@ __device__ __forceinline__ bool job_of(const PromptArgs& A, Job& J) {
   keys.list = nullptr;
   keys.pos = (const gint*)sq.pos;
   keys.doc = A.mods.doc ? (const gint*)A.mods.doc + J.b * A.mods.doc_stride : nullptr;
+  keys.pos0 = A.mods.slopes ? keys.pos[J.pr.slot0 + J.row0 / A.G] : 0;
   keys.logits = nullptr;
   keys.skip = -1;
   // what the tile's last row sees (a row of the prefix may see more than later rows)
@@ -962,7 +964,7 @@ __device__ __forceinline__ size_t row_of(const PromptArgs& A, const Job& J, int 
   row.doc = 0;
   row.slope = 0.0f;
   if constexpr (MOD) {
-    if (A.mods.slopes) { row.pos = J.keys.pos[slot]; row.slope = ((const gfloat*)A.mods.slopes)[qh] * kLog2e; }
+    if (A.mods.slopes) { row.pos = J.keys.pos[slot] - J.keys.pos0; row.slope = ((const gfloat*)A.mods.slopes)[qh] * kLog2e; }
     if (J.keys.doc) {
       row.doc = J.keys.doc[slot];
       if (row.doc < 0) row.limit = 0;
@@ -1109,6 +1111,7 @@ __global__ __launch_bounds__(256, EB == 2 ? 2 : 1) void k_prompt_mass(PromptArgs
   const ADSA_GLOBAL adsa_seq& sq = ((const ADSA_GLOBAL adsa_seq*)A.seqs)[b];
   const gint* const pos = (const gint*)sq.pos;
   const gint* const doc = MOD && A.mods.doc ? (const gint*)A.mods.doc + b * A.mods.doc_stride : nullptr;
+  const int pos0 = MOD && A.mods.slopes ? pos[key0] : 0;       // (see Keys)
   uint4 kf[NB][KC];
 #pragma unroll
   for (int x = 0; x < NB; ++x) {
@@ -1125,7 +1128,7 @@ __global__ __launch_bounds__(256, EB == 2 ? 2 : 1) void k_prompt_mass(PromptArgs
     for (int x = 0; x < NB; ++x)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        kpos[x][i] = A.mods.slopes ? (float)pos[slot_of(x, i)] : 0.0f;
+        kpos[x][i] = A.mods.slopes ? (float)(pos[slot_of(x, i)] - pos0) : 0.0f;
         kdoc[x][i] = doc ? doc[slot_of(x, i)] : 0;
       }
   }
@@ -1159,7 +1162,7 @@ __global__ __launch_bounds__(256, EB == 2 ? 2 : 1) void k_prompt_mass(PromptArgs
     x.norm = norm_first[(uint64_t)(uint32_t)token * (uint32_t)hq + (uint32_t)g];
     x.limit = r < rows ? limit_of(pr, s) : 0;
     x.slope = MOD && A.mods.slopes ? ((const gfloat*)A.mods.slopes)[qh] * kLog2e : 0.0f;
-    x.pos = MOD && A.mods.slopes ? (float)pos[s] : 0.0f;
+    x.pos = MOD && A.mods.slopes ? (float)(pos[s] - pos0) : 0.0f;
     x.doc = MOD && doc ? doc[s] : 0;
     if (MOD && doc && x.doc < 0) x.limit = 0;
     return x;
@@ -1346,7 +1349,7 @@ __device__ __forceinline__ void own_list(const Mods& mods, const Keys& keys, con
       float z = row_sum<LPR>(q.dot(kr[u]));
       if constexpr (MOD) {
         z = mods.cap_out != 0.0f ? capped<EB>(z, mods) : z * mods.scale_log2;
-        if (mods.slopes) z = fmaf(-slope, fabsf((float)q_pos - (float)pos[u]), z);
+        if (mods.slopes) z = fmaf(-slope, fabsf((float)(q_pos - pos[u])), z);
       } else z = Elems<EB>::scaled(z, mods.scale_log2);
       z = ent[u] >= 0 ? z : -INFINITY;
       const int j = first + (i0 + u) * NW * RPW;
@@ -1404,6 +1407,7 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(S
   keys.doc = nullptr;
   keys.logits = nullptr;
   keys.skip = -1;
+  keys.pos0 = 0;
   auto store = [&](auto& t, size_t at, int part) {
     gfloat* const acc = (gfloat*)A.part_acc + (at * C + part) * D;
     using T = std::decay_t<decltype(t)>;
@@ -1446,7 +1450,7 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(S
     auto attend = [&](auto& t, int r) {
       const int rr = min(r, rows - 1), b = gr.first + rr / A.G, qh = head * A.G + rr % A.G;
       const size_t at = (size_t)b * hq + qh;
-      t.row = {keys.end, MOD && A.mods.slopes ? query_pos(b) : 0, 0, MOD && A.mods.slopes ? ((const gfloat*)A.mods.slopes)[qh] * kLog2e : 0.0f};
+      t.row = {keys.end, MOD && A.mods.slopes ? query_pos(b) - keys.pos0 : 0, 0, MOD && A.mods.slopes ? ((const gfloat*)A.mods.slopes)[qh] * kLog2e : 0.0f};
       t.load_q((const gchar*)A.q + at * (D * EB));
       if constexpr (BIG) t.run(keys.end);
       else t.run();
@@ -1456,6 +1460,7 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(S
       for (int r = tile * kRows + threadIdx.x; r < min(rows, (tile + 1) * kRows); r += WK * kWave) nothing((size_t)(gr.first + r / A.G) * hq + head * A.G + r % A.G, chunk);
       return;
     }
+    if (MOD && A.mods.slopes) keys.pos0 = keys.pos[keys.begin];
     if constexpr (BIG) {
       Flow<D, WK, MOD ? kAny : kPlain> t(A.mods, keys, (lchar*)s_lds);
       attend(t, tile * kRows + t.wave * 32 + t.col);
@@ -1504,7 +1509,8 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(S
     return;
   }
   const int qh = head * A.G + min(t.col, A.G - 1);
-  t.row = {keys.end, MOD && A.mods.slopes ? query_pos(b) : 0, 0, MOD && A.mods.slopes ? ((const gfloat*)A.mods.slopes)[qh] * kLog2e : 0.0f};
+  keys.pos0 = MOD && A.mods.slopes ? query_pos(b) : 0;
+  t.row = {keys.end, 0, 0, MOD && A.mods.slopes ? ((const gfloat*)A.mods.slopes)[qh] * kLog2e : 0.0f};
   t.load_q((const gchar*)A.q + at * (D * EB));
   t.run();
   if (t.col < A.G) store(t, at, A.prompt_chunks + chunk);
@@ -1635,7 +1641,7 @@ __global__ __launch_bounds__(256) void k_shared_finish(SharedArgs A) {
     }
     s_w[tid][C] = pn;
     s_inv[tid] = sum == 0.0f ? 0.0f : 1.0f / sum;
-    s_lse[tid] = M + __log2f(sum);
+    s_lse[tid] = sum == 0.0f ? INFINITY : M + __log2f(sum);            // (no finite score: no slot gains anything)
     ((gfloat*)A.lse)[at0 + tid] = sum == 0.0f ? -INFINITY : s_lse[tid] * kLn2;
   }
   __syncthreads();

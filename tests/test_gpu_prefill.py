@@ -141,6 +141,17 @@ def test_infinities_and_nan_behind_the_mask(dtype, D, lens, past):
     assert torch.equal(p.out[:at], clean[:at]) and torch.equal(p.lse[:at], lse[:at]) and p.out[rows].isnan().all()
 
 
+@pytest.mark.parametrize("dtype,D,G", [("bf16", 64, 0), ("bf16", 128, 2), ("f32", 64, 0), ("f32", 128, 0)])
+@pytest.mark.parametrize("lens,past", [([3, 30, 1], 40), ([150, 40, 300], 0)])
+def test_distances_between_far_positions(dtype, D, G, lens, past):
+    """Positions that fp32 does not hold (it counts in steps of 64 there) lie as far apart as near ones."""
+    p = Prompt(lens, past, 2, D, dtype, G)
+    p.batch.pos += 1_000_000_000
+    mods = dict(slopes=torch.tensor([2.0 ** -(i + 1) for i in range(2 * p.G)], device=DEV))
+    p.run(**mods)
+    p.check(**mods)
+
+
 def test_mass_is_left_alone_where_it_is_not_wanted_and_steps_advance():
     p = Prompt([5, 0, 70], [0, 9, 4], 2, 64)
     p.run(flags=B.FLAG_NO_ACCUMULATE | B.FLAG_ADVANCE)

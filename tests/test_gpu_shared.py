@@ -74,7 +74,7 @@ class Shared:
         self.batch.attend_shared(self.shared, self.q, self.kn, self.vn, flags=self.flags | flags, mods=B.make_mods(**mods) if mods else None)
         torch.cuda.synchronize()
 
-    def check(self, softcap=0.0, slopes=None, mass=True, dead=()):
+    def check(self, softcap=0.0, slopes=None, mass=True, dead=(), prompt_from=0):
         K, V, PK, PV, q, out, lse, score = (f64(x) for x in (self.K, self.V, self.PK, self.PV, self.q, self.batch.out, self.batch.lse, self.batch.score))
         kn, vn = f64(self.kn.to(self.batch.tdtype)), f64(self.vn.to(self.batch.tdtype))
         want_score, tol_score = self.score0.copy(), 4 * 2.0 ** -24 * np.abs(self.score0)
@@ -87,7 +87,7 @@ class Shared:
                 s = self.sel[b]
                 if self.pending[b] >= 0:                     # the row is in the cache now
                     assert np.array_equal(K[b, :, self.pending[b]], kn[b]) and np.array_equal(V[b, :, self.pending[b]], vn[b])
-                dist = self.qpos - np.concatenate([np.arange(m), pos[b, s]])
+                dist = self.qpos - np.concatenate([prompt_from + np.arange(m), pos[b, s]])
                 if self.pending[b] >= 0:
                     dist[m + int(np.flatnonzero(s == self.pending[b])[0])] = 0           # its distance to itself
                 for j in range(self.h * self.G):
@@ -127,6 +127,30 @@ def test_scores_capped_and_lowered_with_distance(h, D, dtype, G, cap, slope):
     mods = dict(softcap=cap, slopes=torch.tensor([2.0 ** -(3 + i) for i in range(h * s.G)], device=DEV) if slope else None)
     s.run(**mods)
     s.check(**mods)
+
+
+@pytest.mark.parametrize("h,D,dtype,G", [(2, 64, "bf16", 0), (1, 128, "bf16", 5), (1, 64, "bf16", 16), (2, 64, "f32", 0), (1, 128, "f32", 0)])
+def test_distances_between_far_positions(h, D, dtype, G):
+    """Positions that fp32 does not hold (it counts in steps of 64 there) lie as far apart as near ones."""
+    s = Shared([3, 2], [150, 20], [70, 0, 33, 1, 200], h, D, dtype, G, new_at=4)
+    far = 1_000_000_000
+    s.batch.pos += far
+    s.pb.pos += far
+    s.batch.seqs_host["grid_origin"] += far
+    s.batch.upload_seqs()
+    mods = dict(slopes=torch.tensor([2.0 ** -(3 + i) for i in range(h * s.G)], device=DEV))
+    s.qpos += far
+    s.run(**mods)
+    s.check(**mods, prompt_from=far)
+
+
+def test_scores_of_minus_infinity_gain_nothing():
+    s = Shared([2], [0], [5, 40], 2, 64, append=False)
+    for t in (s.K, s.q.view(2, 2, 1, 64)):
+        t[..., 0] = 1.0
+    s.K[..., 0] = -float("inf")
+    s.run()
+    assert not s.batch.out.any() and (s.batch.lse == -float("inf")).all() and np.array_equal(f64(s.batch.score), s.score0)
 
 
 def test_without_append_and_without_mass():
