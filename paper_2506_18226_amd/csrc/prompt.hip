@@ -114,39 +114,38 @@ __device__ __forceinline__ float capped(float s, const Mods& mods) {
 // those the vector unit works on, too; beyond, scores and outputs would be copied between the two kinds.)
 template <int EB, int D> constexpr int kWavesPerSimd = EB == 4 && D == 128 ? 1 : 2;
 
-template <int EB, int D, int WR, int WK, int KT> struct Shape {
-  static constexpr int kThreads = WR * WK * kWave;
-  static constexpr int kRows = 32 * WR;                // rows of a workgroup's tile
-  static constexpr int TK = WK * KT;                   // keys of a step
+template <int EB, int D, int WK> struct Shape {
+  static constexpr int kThreads = WK * kWave, kRows = 32;      // rows of a workgroup's tile
+  static constexpr int TK = WK * 32;                   // keys of a step
   static constexpr int kMeta = 2 * TK * Layout<EB, D>::RB;             // LDS: K, V, then per key: position (float), document, flag
   static constexpr int kStep = kMeta + 3 * TK * 4;
-  static constexpr int kMerge = WK > 1 ? WK * (D / 32) * 16 * kWave * 4 + 2 * WK * kWave * 4 : 0;       // over the same memory, behind the loop
+  static constexpr int kMerge = WK * (D / 32) * 16 * kWave * 4 + 2 * WK * kWave * 4;       // over the same memory, behind the loop
   static constexpr int kLds = kStep > kMerge ? kStep : kMerge;
 };
 
-// The attention of a workgroup's rows (32 per row wave; a lane's q pieces in qf) over its keys.  Afterwards m, l (of the lane's row, both halves of
-// the wave alike) and the wave's share of the unnormalised outputs: acc[r], r in [0, D / 32 * 16 / WK), are the
-// elements of register r + wk * (...) of the D / 32 transposed 32x32 blocks.
+// The attention of a workgroup's 32 rows (a lane's q pieces in qf) over its keys, which its waves split: each stages the 32 rows of a step that it
+// alone reads, so nobody waits for anybody in the loop.  Afterwards m, l (of the lane's row, both halves of the wave alike) and the wave's
+// share of the unnormalised outputs: acc[r], r in [0, D / 32 * 16 / WK), are the elements of register r + wk * (...) of the D / 32
+// transposed 32x32 blocks.
 // ALL: every row sees every key (but the ones past the end, which repeat the last), so none can hold what must not reach a row.
-template <int EB, int D, int WR, int WK, int KT, bool MOD, bool LIST, bool ALL>
+template <int EB, int D, int WK, bool MOD, bool LIST, bool ALL>
 struct Tile {
   using L = Layout<EB, D>;
-  using S = Shape<EB, D, WR, WK, KT>;
-  static constexpr int NT = S::kThreads, TK = S::TK, CPR = L::CPR, RB = L::RB, SUB = KT / 32, DT = D / 32;
-  // Where the waves split the keys (WR == 1) each stages the rows that it alone reads, and nobody waits for anybody in the loop.
-  static constexpr bool kAlone = WR == 1;
-  static constexpr int RPT = (kAlone ? kWave : NT) / CPR, NL = (kAlone ? KT : TK) / RPT;      // rows per round of those who stage; rounds
+  using S = Shape<EB, D, WK>;
+  static constexpr int KT = 32, TK = S::TK, CPR = L::CPR, RB = L::RB, DT = D / 32;
+  static constexpr int RPT = kWave / CPR, NL = KT / RPT;                // rows per round of a wave; rounds
   static constexpr int kMine = DT * 16 / WK;                            // output registers of a lane after the waves' merge
-  static_assert(NL * RPT == (kAlone ? KT : TK) && NT >= TK && KT <= kWave && kMine % 4 == 0, "whole rounds");
+  static_assert(NL * RPT == KT && kMine % 4 == 0, "whole rounds");
 
   const Mods& mods;
   const Keys& keys;
   lchar* const lds;
-  const int tid, lane, col, half, wr, wk;
+  const int tid, lane, col, half, wk;
   uint4 qf[CPR / 2];
   Row row;
   f32x16 acc[DT];
   float m, l;
+  bool bad;                    // V held infinities or NaN where not every row sees them
   // the next step's rows on their way
   uint4 kr[NL], vr[NL];
   int slot_next[NL];           // LIST: slots of the step after it
@@ -156,15 +155,12 @@ struct Tile {
 
   __device__ __forceinline__ Tile(const Mods& mods_, const Keys& keys_, lchar* lds_)
       : mods(mods_), keys(keys_), lds(lds_), tid(threadIdx.x), lane(threadIdx.x % kWave), col(lane % 32), half(lane / 32),
-        wr(__builtin_amdgcn_readfirstlane(tid / kWave) % WR), wk(__builtin_amdgcn_readfirstlane(tid / kWave) / WR) {}
+        wk(__builtin_amdgcn_readfirstlane(tid / kWave)) {}
 
   // row number i of the thread among a step's, and the one whose position, document and flag it brings (if `brings`)
-  __device__ __forceinline__ int staged(int i) const { return (kAlone ? wk * KT + lane / CPR : tid / CPR) + i * RPT; }
-  __device__ __forceinline__ bool brings() const { return kAlone ? lane < KT : tid < TK; }
-  __device__ __forceinline__ int brought() const { return kAlone ? wk * KT + lane : tid; }
-  __device__ __forceinline__ void meet() const {
-    if constexpr (!kAlone) __syncthreads();
-  }
+  __device__ __forceinline__ int staged(int i) const { return wk * KT + lane / CPR + i * RPT; }
+  __device__ __forceinline__ bool brings() const { return lane < KT; }
+  __device__ __forceinline__ int brought() const { return wk * KT + lane; }
 
   __device__ __forceinline__ void load_q(const gchar* q_row) {
 #pragma unroll
@@ -233,8 +229,7 @@ struct Tile {
     const int key = r0 + (i / 4) * 8 + half * 4 + i % 4;
     return *(const ADSA_LDS float*)(lds + TK * RB + key * RB + (((dt * 8 + col / 4) ^ L::swz_v(key)) << 4) + (col % 4) * 4);
   }
-  // O^T += V^T P^T over the 32 keys from row r0 of the step; TIDY: infinities and NaN of V count as 0
-  template <bool TIDY>
+  // O^T += V^T P^T over the 32 keys from row r0 of the step
   __device__ __forceinline__ void add_values(int r0, const float* p) {
     if constexpr (EB == 2) {
       bf16x8 pb[2];
@@ -248,8 +243,7 @@ struct Tile {
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          u32x4 w = value_piece(r0, dt, t);
-          if constexpr (TIDY) w = u32x4{bf16_finite(w.x), bf16_finite(w.y), bf16_finite(w.z), bf16_finite(w.w)};
+          const u32x4 w = value_piece(r0, dt, t);
           acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pb[t], acc[dt], 0, 0, 0);
         }
     } else {
@@ -257,9 +251,7 @@ struct Tile {
       for (int i = 0; i < 16; ++i)
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
-          float a = value(r0, i, dt);
-          if constexpr (TIDY) a = f32_bad(a) ? 0.0f : a;
-          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[i], acc[dt], 0, 0, 0);
+          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(r0, i, dt), p[i], acc[dt], 0, 0, 0);
         }
     }
   }
@@ -305,80 +297,82 @@ struct Tile {
         __builtin_amdgcn_sched_barrier(0);           // (one after the other: registers matter here, time does not)
       }
   }
+  __device__ __forceinline__ void clear_bad_values(int r0) const {           // (the rows are the wave's own)
+#pragma unroll 1
+    for (int i = 0; i < 32 * CPR / kWave; ++i) {
+      lchar* const at = lds + TK * RB + r0 * RB + (i * kWave + lane) * 16;
+      uint4 w = lds16(at);
+      if constexpr (EB == 2) w = make_uint4(bf16_finite(w.x), bf16_finite(w.y), bf16_finite(w.z), bf16_finite(w.w));
+      else {
+        auto tidy = [](uint32_t x) { return f32_bad(__uint_as_float(x)) ? 0u : x; };
+        w = make_uint4(tidy(w.x), tidy(w.y), tidy(w.z), tidy(w.w));
+      }
+      put16(at, w);
+    }
+  }
 
-  // one step's keys of this wave; masked: some row does not see all of them
-  __device__ __forceinline__ void fold(int base, bool masked) {
+  // scores of one step's keys of this wave, to be multiplied by score_scale(); masked: some row does not see all of them
+  __device__ __forceinline__ float score_scale() const { return MOD ? 1.0f : mods.scale_log2; }
+  __device__ __forceinline__ f32x16 scores(int base, bool masked) const {
     const int r0 = wk * KT;
-    f32x16 s[SUB];
+    f32x16 s = {};
     const lchar* const krow = lds + (r0 + col) * RB;
     const int sw = L::swz_k(r0 + col);
 #pragma unroll
-    for (int u = 0; u < SUB; ++u) {
-      s[u] = f32x16{};
+    for (int c = 0; c < CPR / 2; ++c) {
+      const uint4 a = lds16(krow + (((2 * c + half) ^ sw) << 4));
+      if constexpr (EB == 2) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, qf[c]), s, 0, 0, 0);
+      else {
+        const uint32_t ka[4] = {a.x, a.y, a.z, a.w}, qa[4] = {qf[c].x, qf[c].y, qf[c].z, qf[c].w};
 #pragma unroll
-      for (int c = 0; c < CPR / 2; ++c) {
-        const uint4 a = lds16(krow + u * 32 * RB + (((2 * c + half) ^ sw) << 4));
-        if constexpr (EB == 2) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, qf[c]), s[u], 0, 0, 0);
-        else {
-          const uint32_t ka[4] = {a.x, a.y, a.z, a.w}, qa[4] = {qf[c].x, qf[c].y, qf[c].z, qf[c].w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(ka[e]), __uint_as_float(qa[e]), s[u], 0, 0, 0);
-        }
+        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(ka[e]), __uint_as_float(qa[e]), s, 0, 0, 0);
       }
     }
-    const float scale = MOD ? 1.0f : mods.scale_log2;
     const ADSA_LDS int* const meta = (const ADSA_LDS int*)(lds + S::kMeta) + r0;
+    auto key_of = [&](int i) { return (i / 4) * 8 + half * 4 + i % 4; };      // of the lane's score number i
     if constexpr (MOD) {
       if (mods.cap_out != 0.0f) {
 #pragma unroll
-        for (int u = 0; u < SUB; ++u)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[u][i] = capped<EB>(s[u][i], mods);
+        for (int i = 0; i < 16; ++i) s[i] = capped<EB>(s[i], mods);
       } else {
 #pragma unroll
-        for (int u = 0; u < SUB; ++u)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[u][i] *= mods.scale_log2;
+        for (int i = 0; i < 16; ++i) s[i] *= mods.scale_log2;
       }
       if (mods.slopes) {
         const float here = (float)row.pos;
 #pragma unroll
-        for (int u = 0; u < SUB; ++u)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            s[u][i] = fmaf(-row.slope, fabsf(here - __int_as_float(meta[u * 32 + (i / 4) * 8 + half * 4 + i % 4])), s[u][i]);
+        for (int i = 0; i < 16; ++i) s[i] = fmaf(-row.slope, fabsf(here - __int_as_float(meta[key_of(i)])), s[i]);
       }
     }
     if (masked) {
 #pragma unroll
-      for (int u = 0; u < SUB; ++u)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int k = u * 32 + (i / 4) * 8 + half * 4 + i % 4;
-          bool seen = base + r0 + k < row.limit;
-          if constexpr (LIST) seen &= meta[2 * TK + k] == 0;
-          if constexpr (MOD)
-            if (keys.doc) seen &= meta[TK + k] == row.doc;
-          s[u][i] = seen ? s[u][i] : -INFINITY;
-        }
+      for (int i = 0; i < 16; ++i) {
+        bool seen = base + r0 + key_of(i) < row.limit;
+        if constexpr (LIST) seen &= meta[2 * TK + key_of(i)] == 0;
+        if constexpr (MOD)
+          if (keys.doc) seen &= meta[TK + key_of(i)] == row.doc;
+        s[i] = seen ? s[i] : -INFINITY;
+      }
     }
+    return s;
+  }
+  __device__ __forceinline__ void fold(int base, bool masked) {
+    const int r0 = wk * KT;
+    const float scale = score_scale();
+    const f32x16 s = scores(base, masked);
     if constexpr (LIST) {
       if (keys.logits && col < keys.lg_rows) {       // four at a time: a row's padding to a multiple of 4 may get something, too
         gfloat* const at = keys.logits + (size_t)col * keys.lg_stride;
 #pragma unroll
-        for (int u = 0; u < SUB; ++u)
-#pragma unroll
-          for (int i = 0; i < 16; i += 4) {
-            const int k = base + r0 + u * 32 + i * 2 + half * 4;
-            if (k < keys.end) store4<4>((gchar*)(at + k), s[u][i] * scale, s[u][i + 1] * scale, s[u][i + 2] * scale, s[u][i + 3] * scale);
-          }
+        for (int i = 0; i < 16; i += 4) {
+          const int k = base + r0 + i * 2 + half * 4;
+          if (k < keys.end) store4<4>((gchar*)(at + k), s[i] * scale, s[i + 1] * scale, s[i + 2] * scale, s[i + 3] * scale);
+        }
       }
     }
-    float mx = s[0][0];
+    float mx = s[0];
 #pragma unroll
-    for (int u = 0; u < SUB; ++u)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[u][i]);           // (no asm here: a product's result takes wait states that the compiler counts)
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);     // (no asm here: a product's result takes wait states that the compiler counts)
     mx = xor_max<32>(mx) * scale;
     if (__ballot(mx > m) != 0) {                     // some row's maximum rose: bring every row's state to its new one
       const float m_new = max2(m, mx), corr = fast_exp2(m - m_new);
@@ -389,27 +383,34 @@ struct Tile {
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[dt][i] *= corr;
     }
-    float p[SUB][16], sum = 0.0f;
+    float p[16], sum = 0.0f;
 #pragma unroll
-    for (int u = 0; u < SUB; ++u)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        p[u][i] = fast_exp2(fmaf(s[u][i], scale, -m));
-        sum += p[u][i];
-      }
-    l += sum;
-#pragma unroll
-    for (int u = 0; u < SUB; ++u) {
-      if (!ALL && masked && values_bad(r0 + u * 32)) {
-        add_bad_values(r0 + u * 32, p[u]);
-        add_values<true>(r0 + u * 32, p[u]);
-      } else add_values<false>(r0 + u * 32, p[u]);
+    for (int i = 0; i < 16; ++i) {
+      p[i] = fast_exp2(fmaf(s[i], scale, -m));
+      sum += p[i];
     }
+    l += sum;
+    if (!ALL && masked && values_bad(r0)) {          // as 0 for now
+      clear_bad_values(r0);
+      bad = true;
+    }
+    add_values(r0, p);
+  }
+  // Infinities and NaN of V that not every row of their step saw (rare): another pass over the keys, behind the loop, whose registers have no room for it.
+  __device__ __forceinline__ void fold_bad(int base, bool masked) {
+    const int r0 = wk * KT;
+    if (!masked || !values_bad(r0)) return;
+    const f32x16 s = scores(base, masked);
+    float p[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) p[i] = fast_exp2(fmaf(s[i], score_scale(), -m));
+    add_bad_values(r0, p);
   }
 
   __device__ __forceinline__ void run() {
     m = kLowest;
     l = 0.0f;
+    bad = false;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x16{};
     // keys that all rows of the wave see, and that none sees any more
@@ -418,33 +419,54 @@ struct Tile {
     for (int x = 1; x < 32; x <<= 1) { lo = min(lo, __shfl_xor(lo, x)); hi = max(hi, __shfl_xor(hi, x)); }
     lo = __builtin_amdgcn_readfirstlane(lo);
     hi = __builtin_amdgcn_readfirstlane(hi);
+    int doc_lo = 0x7FFFFFFF, doc_hi = -1;            // of the wave's rows
+    if constexpr (MOD)
+      if (keys.doc) {
+        if (row.doc >= 0) doc_lo = doc_hi = row.doc;
+#pragma unroll
+        for (int x = 1; x < 32; x <<= 1) { doc_lo = min(doc_lo, __shfl_xor(doc_lo, x)); doc_hi = max(doc_hi, __shfl_xor(doc_hi, x)); }
+      }
+    // what the wave is to do about a staged step: nothing, fold it, and whether some row does not see all of it
+    auto judge = [&](int first, bool* masked) {
+      bool wanted = first < hi;
+      *masked = first + KT > lo;
+      if constexpr (MOD)
+        if (keys.doc && wanted) {                    // documents of the rows among the step's? only the rows' one?
+          const int d = ((const ADSA_LDS int*)(lds + S::kMeta))[TK + wk * KT + lane % KT];
+          wanted = __ballot(d >= doc_lo && d <= doc_hi) != 0;
+          *masked |= __ballot(d != doc_lo || d != doc_hi) != 0;
+        }
+      if constexpr (LIST) {
+        if (keys.skip >= 0) {
+          const ADSA_LDS int* const flag = (const ADSA_LDS int*)(lds + S::kMeta) + 2 * TK + wk * KT;
+          *masked |= __ballot(lane < KT && flag[lane % KT] != 0) != 0;
+        }
+      }
+      return wanted;
+    };
+    bool masked;
     load_slots(keys.begin);
     load_rows(keys.begin);
     load_slots(keys.begin + TK);
-    for (int base = keys.begin; base < keys.end; base += TK) {
-      const int first = base + wk * KT;
-      if (kAlone && first >= min(hi, keys.end)) break;         // (uniform in the wave; what follows are others' keys)
-      meet();                                        // (the step before has been read)
+    const int end = min(hi, keys.end);               // (from here on keys are others')
+    for (int base = keys.begin; base + wk * KT < end; base += TK) {
       store_rows();
-      meet();
       if (base + TK < keys.end) {
         load_rows(base + TK);
         load_slots(base + 2 * TK);
       }
-      if (first < hi) {
-        bool masked = first + KT > lo;
-        if constexpr (MOD) masked |= keys.doc != nullptr;
-        if constexpr (LIST) {
-          if (keys.skip >= 0) {
-            const ADSA_LDS int* const flag = (const ADSA_LDS int*)(lds + S::kMeta) + 2 * TK + wk * KT;
-            masked |= __ballot(lane < KT && flag[lane % KT] != 0) != 0;
-          }
-        }
-        fold(base, masked);
-      }
+      if (judge(base + wk * KT, &masked)) fold(base, masked);
     }
+    if constexpr (!ALL)
+      if (bad)                                       // (uniform)
+        for (int base = keys.begin; base + wk * KT < end; base += TK) {
+          load_slots(base);
+          load_rows(base);
+          store_rows();
+          if (judge(base + wk * KT, &masked)) fold_bad(base, masked);
+        }
     l = xor_sum<32>(l);
-    if constexpr (WK > 1) {                          // the waves' states meet in LDS
+    {                                                // the waves' states meet in LDS
       ADSA_LDS float* const a = (ADSA_LDS float*)lds;
       ADSA_LDS float* const ml = a + WK * DT * 16 * kWave;
       __syncthreads();
@@ -476,7 +498,7 @@ struct Tile {
   }
   // first of the 4 consecutive elements that registers r .. r + 3 of the wave's share hold
   __device__ __forceinline__ int element(int r) const {
-    const int i = (WK > 1 ? wk * kMine : 0) + r;
+    const int i = wk * kMine + r;
     return i / 16 * 32 + i % 16 / 4 * 8 + half * 4;
   }
 };
@@ -907,7 +929,10 @@ __device__ __forceinline__ bool job_of(const PromptArgs& A, Job& J) {
     for (long long r = tile; r < J.pr.len; r += A.tiles) {
       const size_t at = ((size_t)(J.pr.from + r) * hq + J.head * A.G);
       for (int o = tid; o < A.G * D * EB / 4; o += THREADS) ((gint*)(A.out + at * D * EB))[o] = 0;
-      for (int o = tid; o < A.G; o += THREADS) ((gfloat*)A.lse)[at + o] = 0.0f;
+      for (int o = tid; o < A.G; o += THREADS) {
+        ((gfloat*)A.lse)[at + o] = 0.0f;
+        if (A.chunks > 1) ((gfloat*)A.part_ml)[(at + o) * A.chunks * 2 + 1] = -1.0f;           // (k_prompt_finish leaves the row alone)
+      }
     }
     return false;
   }
@@ -930,25 +955,33 @@ __device__ __forceinline__ bool job_of(const PromptArgs& A, Job& J) {
   const int n = max(limit_of(J.pr, last_slot), limit_of(J.pr, first_slot));
   int first = 0, last = n;
   if (keys.doc) {                                    // (uniform) only from the first to the last slot of a document that the tile's rows belong to
-    __shared__ int s_doc[4];                         // least and greatest of the rows' documents, first and last slot of one among them
-    if (tid < 4) s_doc[tid] = tid == 0 || tid == 2 ? 0x7FFFFFFF : -1;
-    __syncthreads();
-    const int slots = last_slot - first_slot + 1;
+    // (each wave to one number by itself: lanes' atomics on one word are done one lane after the other, 7 us of a launch where this takes 1)
+    constexpr int NW = THREADS / kWave;
+    __shared__ int s_doc[4][NW];                     // least and greatest of the rows' documents, first and last slot of one among them; a wave's
+    const int lane = tid % kWave, wave = tid / kWave, slots = last_slot - first_slot + 1;
+    auto spread = [&](int lo, int hi, int at) {      // both over the workgroup
+#pragma unroll
+      for (int x = 1; x < kWave; x <<= 1) { lo = min(lo, __shfl_xor(lo, x)); hi = max(hi, __shfl_xor(hi, x)); }
+      if (lane == 0) { s_doc[at][wave] = lo; s_doc[at + 1][wave] = hi; }
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < NW; ++w) { lo = min(lo, s_doc[at][w]); hi = max(hi, s_doc[at + 1][w]); }
+      return int2{lo, hi};
+    };
+    int lo = 0x7FFFFFFF, hi = -1;
     for (int i = tid; i < slots; i += THREADS) {
       const int d = keys.doc[first_slot + i];
-      if (d >= 0) { atomicMin(&s_doc[0], d); atomicMax(&s_doc[1], d); }
+      if (d >= 0) { lo = min(lo, d); hi = max(hi, d); }
     }
-    __syncthreads();
-    const int least = s_doc[0], most = s_doc[1];
-    int lo = 0x7FFFFFFF, hi = -1;
+    const int2 docs = spread(lo, hi, 0);
+    lo = 0x7FFFFFFF, hi = -1;
     for (int i = tid; i < n; i += THREADS) {
       const int d = keys.doc[i];
-      if (d >= least && d <= most) { lo = min(lo, i); hi = i; }
+      if (d >= docs.x && d <= docs.y) { lo = min(lo, i); hi = i; }
     }
-    if (hi >= 0) { atomicMin(&s_doc[2], lo); atomicMax(&s_doc[3], hi); }
-    __syncthreads();
-    first = s_doc[3] < 0 ? 0 : s_doc[2] / 32 * 32;
-    last = s_doc[3] < 0 ? min(n, 1) : s_doc[3] + 1;  // (none: one key, which nobody sees)
+    const int2 at = spread(lo, hi, 2);
+    first = at.y < 0 ? 0 : at.x / 32 * 32;
+    last = at.y < 0 ? min(n, 1) : at.y + 1;          // (none: one key, which nobody sees)
   }
   const int m = last - first, per = A.chunks == 1 ? m : ((m + A.chunks - 1) / A.chunks + 31) / 32 * 32;
   keys.begin = min(last, first + J.chunk * per);
@@ -983,15 +1016,15 @@ __device__ __forceinline__ void store_lse(const PromptArgs& A, size_t at, float 
   if (A.norm) ((gfloat*)A.norm)[at] = l == 0.0f ? INFINITY : m + __log2f(l);           // (exp2(z - norm): 0 for a row that sees nothing)
 }
 
-template <int EB, int D, int WR, int WK, int KT, bool MOD>
-__global__ __launch_bounds__(WR * WK * kWave, EB == 2 && D == 64 ? 2 : 1) void k_prompt(PromptArgs A) {
-  using T = Tile<EB, D, WR, WK, KT, MOD, false, false>;
+template <int EB, int D, int WK, bool MOD>
+__global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_prompt(PromptArgs A) {
+  using T = Tile<EB, D, WK, MOD, false, false>;
   using S = typename T::S;
   extern __shared__ __align__(16) char s_lds[];
   Job J;
   if (!job_of<EB, D, S::kRows, S::kThreads>(A, J)) return;
   T t(A.mods, J.keys, (lchar*)s_lds);
-  const int r = J.row0 + t.wr * 32 + t.col;
+  const int r = J.row0 + t.col;
   const size_t at = row_of<MOD>(A, J, r, t.row);
   t.load_q((const gchar*)A.q + at * (D * EB));
   t.run();
@@ -1048,40 +1081,48 @@ __global__ __launch_bounds__(W * kWave, D == 64 ? 3 : 2) void k_prompt_many(Prom
   if (f.half == 0) store_lse(A, at, f.m, f.l);
 }
 
-// Split keys: a wave joins the parts of one row.
+// Split keys: a wave joins the parts of one row.  Nothing it loads depends on anything but its arguments (bound by one trip to memory): 16 bytes of a
+// part's outputs to a lane, 64 * 4 / D parts side by side, and every part's maximum and sum to a lane of its own.
 template <int EB, int D>
 __global__ __launch_bounds__(256) void k_prompt_finish(PromptArgs A) {
-  const int lane = threadIdx.x % kWave, hq = A.h * A.G;
+  constexpr int LPR = D / 4, kSide = kWave / LPR, kBatch = 4;
+  const int lane = threadIdx.x % kWave, side = lane / LPR, e = lane % LPR * 4, C = A.chunks;
   const size_t at = (size_t)blockIdx.x * (256 / kWave) + threadIdx.x / kWave;
-  if (at >= (size_t)A.n_tokens * hq) return;
-  const int token = (int)(at / hq);
-  // its sequence: the last one that begins at or before the token
-  int lo = 0, hi = A.n_seq;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (((const gint*)A.begin)[mid] <= token) lo = mid; else hi = mid;
-  }
-  const Prompt pr = prompt_of(A, lo);
-  if (pr.status != 0 || token < pr.from || token >= pr.from + pr.len) return;           // (zeros already)
-  const gfloat* const ml = (const gfloat*)A.part_ml + at * A.chunks * 2;
-  const gfloat* const acc = (const gfloat*)A.part_acc + at * A.chunks * D;
-  float M = kLowest, L = 0.0f, x[D / kWave];
-  for (int c = 0; c < A.chunks; ++c) M = fmaxf(M, ml[2 * c]);
+  if (at >= (size_t)A.n_tokens * A.h * A.G || at >= (size_t)((const gint*)A.begin)[A.n_seq] * A.h * A.G) return;
+  const gfloat* const ml = (const gfloat*)A.part_ml + (at * C + min(lane, C - 1)) * 2;
+  const gfloat* const acc = (const gfloat*)A.part_acc + at * C * D + e;
+  u32x4 part[kBatch];
+  auto fetch = [&](int c0) {
 #pragma unroll
-  for (int e = 0; e < D / kWave; ++e) x[e] = 0.0f;
-  for (int c = 0; c < A.chunks; ++c) {
-    const float w = fast_exp2(ml[2 * c] - M);
-    L = fmaf(ml[2 * c + 1], w, L);
+    for (int i = 0; i < kBatch; ++i) part[i] = *(const ADSA_GLOBAL u32x4*)(acc + (size_t)min(c0 + i * kSide + side, C - 1) * D);
+  };
+  fetch(0);
+  const float m = ml[0], l = ml[1];
+  if (__shfl(l, 0) < 0.0f) return;                   // (a sequence that is not attended: zeros already)
+  float M = m;
 #pragma unroll
-    for (int e = 0; e < D / kWave; ++e) x[e] = fmaf(acc[(size_t)c * D + e * kWave + lane], w, x[e]);
+  for (int x = 1; x < kMaxChunks; x <<= 1) M = fmaxf(M, __shfl_xor(M, x));             // (lanes past the last part repeat it)
+  const float w = lane < C ? fast_exp2(m - M) : 0.0f;
+  float L = lane < C ? l * w : 0.0f, x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  L = row_sum<16>(L);
+  for (int c0 = 0; c0 < C; c0 += kBatch * kSide) {
+    if (c0 > 0) fetch(c0);
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int c = c0 + i * kSide + side;
+      const float f = __shfl(w, min(c, kMaxChunks));   // (0 past the last part)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = f != 0.0f ? fmaf(__uint_as_float(part[i][k]), f, x[k]) : x[k];
+    }
   }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if constexpr (kSide == 4) x[k] = xor_sum<16>(x[k]);
+    x[k] = xor_sum<32>(x[k]);
+  }
+  L = __shfl(L, 0);
   const float inv = inverse(L);
-#pragma unroll
-  for (int e = 0; e < D / kWave; ++e) {
-    const size_t o = at * D + e * kWave + lane;
-    if constexpr (EB == 4) ((gfloat*)A.out)[o] = x[e] * inv;
-    else ((ADSA_GLOBAL uint16_t*)A.out)[o] = (uint16_t)f32_to_bf16_rne(x[e] * inv);
-  }
+  if (side == 0) store4<EB>((gchar*)A.out + (at * D + e) * EB, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
   if (lane == 0) store_lse(A, at, M, L);
 }
 
@@ -1465,7 +1506,7 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(S
       Flow<D, WK, MOD ? kAny : kPlain> t(A.mods, keys, (lchar*)s_lds);
       attend(t, tile * kRows + t.wave * 32 + t.col);
     } else {
-      Tile<EB, D, 1, WK, 32, MOD, false, true> t(A.mods, keys, (lchar*)s_lds);
+      Tile<EB, D, WK, MOD, false, true> t(A.mods, keys, (lchar*)s_lds);
       attend(t, tile * kRows + t.col);
     }
     return;
@@ -1501,7 +1542,7 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(S
   }
   keys.lg_stride = A.lg_stride;
   keys.lg_rows = A.G;
-  Tile<EB, D, 1, WK, 32, MOD, true, true> t(A.mods, keys, (lchar*)s_lds);
+  Tile<EB, D, WK, MOD, true, true> t(A.mods, keys, (lchar*)s_lds);
   const size_t at = at0 + min(t.col, A.G - 1);
   // (a part that holds the query token alone has no other row to stand in for it)
   if (keys.begin >= keys.end || (keys.end - keys.begin == 1 && keys.list[keys.begin] == keys.skip)) {
@@ -1700,9 +1741,9 @@ Mods make_mods(const adsa_params& p, const adsa_mods& m) {
 }
 bool modded(const Mods& m) { return m.slopes || m.doc || m.cap_out != 0.0f; }
 
-// Shapes of the launches: many rows, 4 waves of 32 rows each over steps of 64 keys (fp32: 32); few rows, waves that split the keys.
-template <int EB> constexpr int kStepKeys = EB == 2 ? 64 : 32;
+// Waves that split the keys of 32 rows.
 template <int EB, int D> constexpr int kKeyWaves = EB == 4 && D == 128 ? 2 : 4;
+
 
 // Workgroups of 8 waves (256 rows), where 4 waves' share of staging a tile leaves too few registers.  us with 4 | 8 waves, 2 x 4352 x 32 x 128 lowered with
 // distance 1281 | 953; elsewhere 4 waves are as fast or faster: 4 x 4352 x 32 x 128 820 | 797, capped ragged prompts of 64 over 8 heads
@@ -1712,10 +1753,10 @@ template <int D, int MODS> constexpr bool two_sizes = D == 128 && MODS == kAny;
 template <int EB, int D, bool MOD>
 hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStream_t st) {
   const unsigned pairs = (unsigned)((A.n_seq * A.h + 7) / 8 * 8);
-  constexpr int KW = kKeyWaves<EB, D>, KT = kStepKeys<EB>;
+  constexpr int KW = kKeyWaves<EB, D>;
   const dim3 grid(pairs * (unsigned)(plan.tiles * plan.chunks));
-  if (plan.rows <= 32) k_prompt<EB, D, 1, KW, 32, MOD><<<grid, KW * kWave, Shape<EB, D, 1, KW, 32>::kLds, st>>>(A);
-  else if (EB == 2 && plan.flow) {
+  if (!plan.flow) k_prompt<EB, D, KW, MOD><<<grid, KW * kWave, Shape<EB, D, KW>::kLds, st>>>(A);
+  else {
     if constexpr (EB == 2) {
       auto many = [&](auto mods) {
         constexpr int M = decltype(mods)::value;
@@ -1732,7 +1773,7 @@ hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStrea
       else if (A.mods.slopes || A.mods.doc) many(std::integral_constant<int, kAny>());
       else many(std::integral_constant<int, kCapped>());
     }
-  } else k_prompt<EB, D, 4, 1, KT, MOD><<<grid, 4 * kWave, Shape<EB, D, 4, 1, KT>::kLds, st>>>(A);
+  }
   if (plan.chunks > 1) {
     const size_t rows = (size_t)A.n_tokens * A.h * A.G;
     k_prompt_finish<EB, D><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, st>>>(A);
@@ -1746,7 +1787,7 @@ hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStrea
 
 template <int EB, int D, bool MOD, bool BIG>
 constexpr int shared_lds = [] {
-  const int own = Shape<EB, D, 1, kKeyWaves<EB, D>, 32>::kLds;
+  const int own = Shape<EB, D, kKeyWaves<EB, D>>::kLds;
   if constexpr (BIG) return std::max(own, Flow<D, 4, MOD ? kAny : kPlain>::kLds);
   else return own;
 }();
@@ -1769,13 +1810,12 @@ hipError_t shared_launches(const SharedArgs& A, const SharedPlan& plan, hipStrea
 
 template <int EB, int D, bool MOD>
 hipError_t allow_lds() {
-  constexpr int KW = kKeyWaves<EB, D>, KT = kStepKeys<EB>;
+  constexpr int KW = kKeyWaves<EB, D>;
   hipError_t e = hipSuccess;
   auto allow = [&](auto kernel, int bytes) {
     if (e == hipSuccess) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
   };
-  allow(k_prompt<EB, D, 1, KW, 32, MOD>, Shape<EB, D, 1, KW, 32>::kLds);
-  allow(k_prompt<EB, D, 4, 1, KT, MOD>, Shape<EB, D, 4, 1, KT>::kLds);
+  allow(k_prompt<EB, D, KW, MOD>, Shape<EB, D, KW>::kLds);
   allow(k_prompt_mass<EB, D, MOD>, Mass<EB, D, MOD>::kLds);
   allow(k_shared<EB, D, KW, MOD, true, false>, shared_lds<EB, D, MOD, false>);
   allow(k_shared<EB, D, KW, MOD, false, false>, shared_lds<EB, D, MOD, false>);
@@ -1826,13 +1866,14 @@ hipError_t prompt_prepare_kernels() {
 PromptPlan make_prompt_plan(const adsa_params& p, const adsa_tokens& t) {
   const long long rows = (long long)t.max_len * query_group(p), pairs = (long long)p.n_seq * p.n_heads;
   PromptPlan plan;
-  // (a tile's rows are reached with 32-bit offsets from its first)
-  plan.flow = p.dtype == ADSA_BF16 && p.kv_slot_stride * 2 * 64 < (1ll << 31);
-  plan.rows = rows <= 32 ? 32 : 128;
+  auto groups = [&](int tile) { return pairs * ((rows + tile - 1) / tile); };
+  const bool near = p.kv_slot_stride * 2 * 64 < (1ll << 31);       // (k_prompt_many reaches a tile's rows with 32-bit offsets from its first)
+  plan.flow = p.dtype == ADSA_BF16 && rows > 32 && near && !(groups(128) <= 256 && p.cap <= 512);
+  plan.rows = plan.flow ? 128 : 32;
   plan.rows_all = (int)rows;
   plan.tiles = (int)((rows + plan.rows - 1) / plan.rows);
-  const long long groups = pairs * plan.tiles;
-  plan.chunks = (int)std::clamp<long long>(std::min<long long>((512 + groups - 1) / groups, (p.cap + 255) / 256), 1, kMaxChunks);
+  const long long n = groups(plan.rows), most = plan.flow ? (p.cap + 511) / 512 : (p.cap + 255) / 256;
+  plan.chunks = n > 256 ? 1 : (int)std::clamp<long long>(std::min<long long>((plan.flow ? 256 : 512) / n, most), 1, kMaxChunks);
   return plan;
 }
 
