@@ -713,7 +713,7 @@ struct Flow {
     uint32_t pn[8];
     float corr, sum = 0.0f;
     bool grown = false;
-    constexpr int kAhead = 3;                        // pieces fetched ahead of their product
+    constexpr int kAhead = D == 64 ? 2 : 3;          // pieces fetched ahead of their product (three waves a SIMD have registers for two)
     constexpr int kMax = MODS != kPlain ? NC / 2 : 1;      // the maximum stands before this chunk's probabilities
     uint4 kp[KC];
     u32x4 vp[VC];
@@ -1562,7 +1562,7 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(S
 constexpr int kMaxParts = 2 * kMaxChunks;
 template <int EB, int D, bool ONE>
 __global__ __launch_bounds__(256) void k_shared_finish(SharedArgs A) {
-  constexpr int NT = 256, E = D / kWave, kMaxG = ONE ? 1 : 16, kEarly = 3, kAcc = 4, kLg = ONE ? 1 : 8;
+  constexpr int NT = 256, E = D / kWave, kMaxG = ONE ? 1 : 16, kEarly = 3, kAcc = 4, kLg = ONE ? 1 : 8, kQ = ONE ? 1 : 2;
   __shared__ float s_w[kMaxG][kMaxParts + 1], s_l[kMaxG][kMaxParts], s_lse[kMaxG], s_new[kMaxG], s_inv[kMaxG];
   __shared__ __attribute__((aligned(16))) float s_v[D];
   __shared__ int s_has;
@@ -1600,8 +1600,16 @@ __global__ __launch_bounds__(256) void k_shared_finish(SharedArgs A) {
 #pragma unroll
     for (int c = 0; c < kAcc; ++c) parts[c] = part_of(oh, min(c, C - 1));
   }
-  float kn[E], vn[E];
+  float kn[E], vn[E], qn[kQ][E];
+  auto q_of = [&](int h, int e) {
+    const size_t o = (at0 + h) * D + e * kWave + lane;
+    return EB == 4 ? ((const gfloat*)A.q)[o] : __uint_as_float((uint32_t)((const ADSA_GLOBAL uint16_t*)A.q)[o] << 16);
+  };
   if (A.append) {
+#pragma unroll
+    for (int k = 0; k < kQ; ++k)
+#pragma unroll
+      for (int e = 0; e < E; ++e) qn[k][e] = q_of(min(wave + k * (NT / kWave), G - 1), e);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const size_t o = row + e * kWave + lane;
@@ -1618,24 +1626,26 @@ __global__ __launch_bounds__(256) void k_shared_finish(SharedArgs A) {
       }
     }
   }
+  // ---- what depends on that: scores so far, the group's record
+  const bool live = status == 0 && step >= 0;
+  cnt = min(max(cnt, 0), A.sel_cap);
+#pragma unroll
+  for (int k = 0; k < kEarly; ++k) {
+    old[k] = 0.0f;
+    if (A.accumulate && live && tid + k * NT < cnt) old[k] = score[min(max(slot[k], 0), A.cap - 1)];
+  }
   const Group gr = group_at(A, max(g, 0));
-  const bool fits = gr.n >= 0 && gr.first <= b && b < gr.end, live = status == 0 && step >= 0;
+  const bool fits = gr.n >= 0 && gr.first <= b && b < gr.end;
   if (!live || !fits) {
     if (live && head == 0 && tid == 0) sq.status = ADSA_SEQ_BAD_STATE;
     for (int o = tid; o < G * D * EB / 4; o += NT) ((gint*)(A.out + at0 * D * EB))[o] = 0;
     for (int o = tid; o < G; o += NT) ((gfloat*)A.lse)[at0 + o] = 0.0f;
     return;
   }
-  cnt = min(max(cnt, 0), A.sel_cap);
   const int new_slot = A.append && pending >= 0 && pending < A.cap ? pending : -1;
   bool mine = false;
 #pragma unroll
-  for (int k = 0; k < kEarly; ++k) {
-    const bool in = tid + k * NT < cnt;
-    mine |= in && slot[k] == new_slot;
-    old[k] = 0.0f;
-    if (A.accumulate && in) old[k] = score[min(max(slot[k], 0), A.cap - 1)];
-  }
+  for (int k = 0; k < kEarly; ++k) mine |= tid + k * NT < cnt && slot[k] == new_slot;
   for (int j = tid + kEarly * NT; j < cnt; j += NT) mine |= list[j] == new_slot;
   if (tid == 0) s_has = 0;
   __syncthreads();
@@ -1654,19 +1664,19 @@ __global__ __launch_bounds__(256) void k_shared_finish(SharedArgs A) {
         s_v[e * kWave + lane] = vn[e];
       }
     }
-    for (int h = wave; h < G; h += NT / kWave) {     // its score with every query head
+    auto meet = [&](int h, auto q) {                 // its score with a query head
       float z = 0.0f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const size_t o = (at0 + h) * D + e * kWave + lane;
-        const float x = EB == 4 ? ((const gfloat*)A.q)[o] : __uint_as_float((uint32_t)((const ADSA_GLOBAL uint16_t*)A.q)[o] << 16);
-        z = fmaf(x, kn[e], z);
-      }
+      for (int e = 0; e < E; ++e) z = fmaf(q(e), kn[e], z);
       z = row_sum<32>(z);
       z = xor_sum<32>(z);
       z = A.mods.cap_out != 0.0f ? capped<EB>(z, A.mods) : z * A.mods.scale_log2;      // (its distance to itself is 0)
       if (lane == 0) s_new[h] = z;
-    }
+    };
+#pragma unroll
+    for (int k = 0; k < kQ; ++k)
+      if (wave + k * (NT / kWave) < G) meet(wave + k * (NT / kWave), [&](int e) { return qn[k][e]; });
+    for (int h = wave + kQ * (NT / kWave); h < G; h += NT / kWave) meet(h, [&](int e) { return q_of(h, e); });
   }
   __syncthreads();
   const bool has = new_slot >= 0 && s_has != 0;
@@ -1868,10 +1878,16 @@ PromptPlan make_prompt_plan(const adsa_params& p, const adsa_tokens& t) {
   PromptPlan plan;
   auto groups = [&](int tile) { return pairs * ((rows + tile - 1) / tile); };
   const bool near = p.kv_slot_stride * 2 * 64 < (1ll << 31);       // (k_prompt_many reaches a tile's rows with 32-bit offsets from its first)
-  plan.flow = p.dtype == ADSA_BF16 && rows > 32 && near && !(groups(128) <= 256 && p.cap <= 512);
+  // Tiles of 32 rows, whose 4 waves split the keys, or of 128, whose waves share them (bf16).  us with 128 | 32 rows a tile:
+  // short caches that leave CUs idle, 1 x 400 x 24 heads x 64 12.5 | 7.7, 4 x 120 7.9 | 6.2; 64 rows and less, of which 128 leave half empty, behind
+  // 2000 slots 2 x 60 x 24 x 64 19.4 | 14.0, behind 700 slots 16 x 60 x 24 x 64 29 | 18.4.  Elsewhere K and V are read too often: 32 x 60 x 24 x 64
+  // 10.6 | 13.4, 16 x 60 x 32 x 128 behind 700 47 | 52, 2 x 1000 x 32 x 128 41 | 110.
+  const bool idle = groups(128) <= 256, half = rows <= 64 && (idle || (p.head_dim == 64 && p.cap > 512));
+  plan.flow = p.dtype == ADSA_BF16 && near && rows > 32 && !half && !(idle && p.cap <= 512);
   plan.rows = plan.flow ? 128 : 32;
   plan.rows_all = (int)rows;
   plan.tiles = (int)((rows + plan.rows - 1) / plan.rows);
+  // Keys are split where tiles alone leave CUs idle.  (Two parts where 256 tiles fill them: 16 x 1..9 x 24 x 64 behind 700 slots 15.4 -> 21.3 us.)
   const long long n = groups(plan.rows), most = plan.flow ? (p.cap + 511) / 512 : (p.cap + 255) / 256;
   plan.chunks = n > 256 ? 1 : (int)std::clamp<long long>(std::min<long long>((plan.flow ? 256 : 512) / n, most), 1, kMaxChunks);
   return plan;
