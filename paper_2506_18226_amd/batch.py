@@ -158,8 +158,9 @@ class LayerBatch:
 
     # ---- prompts
     def _with_workspace(self, call, need) -> None:
-        """call(workspace), with a larger one where that is refused as too small.  It is kept for the calls to come: the first call of a
-        size allocates, so make it before a graph is captured."""
+        """call(workspace), with a larger one where that is refused as too small.  It is kept for the calls to come, whatever their stream:
+        the first call of a size allocates and waits for the device, since torch orders memory by the stream that was current when it was
+        taken, so make it before a graph is captured."""
         if self.prompt_workspace is not None:
             try:
                 return call(self.prompt_workspace)
@@ -167,6 +168,8 @@ class LayerBatch:
                 if e.code != B.ERR_WORKSPACE:
                     raise
         n = need()
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.synchronize(self.device)
         self.prompt_workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=self.device)
         call(self.prompt_workspace)
 

@@ -204,3 +204,22 @@ def test_wide_strides():
     p.batch.params = params
     p.run()
     p.check()
+
+
+def test_a_workspace_that_grows_on_another_stream():
+    """Calls on a stream of their own, each needing more workspace than the last, leave results that no later use of that memory changes."""
+    want, got = [], []
+    for side in (False, True):
+        stream = torch.cuda.Stream() if side else None
+        batch = None
+        for lens, past in (([2, 1], [700, 900]), ([20, 31], [900, 1400]), ([140, 90], [2000, 1500])):
+            p = Prompt(lens, past, 2, 64, cap=2200)
+            if batch is not None:
+                p.batch.prompt_workspace = batch.prompt_workspace
+            batch = p.batch
+            torch.cuda.synchronize()
+            batch.prefill(p.tokens, p.q, p.out, p.lse, stream=stream)
+            torch.full((batch.prompt_workspace.numel(),), 255, dtype=torch.uint8, device=DEV)
+            torch.cuda.synchronize()
+            (got if side else want).append((p.out, p.lse, batch.score))
+    assert all(torch.equal(a, b) for x, y in zip(want, got) for a, b in zip(x, y))
