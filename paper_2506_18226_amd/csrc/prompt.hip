@@ -511,7 +511,8 @@ struct Tile {
 // So a wave takes whatever is independent at one time: the scores of step j + 1 and the outputs of step j - 1 on the matrix core, the softmax of
 // step j on the vector unit, laid out alternately by hand (a product, then its share of the vector work), since the
 // compiler left alone puts all of one kind before the other.
-// A row's maximum is followed only when it has grown by more than 2^8: P stays below 2^8, and outputs are rescaled next to never.
+// A row's maximum is looked for only where a lane's sum of P passes 2^20 (the first keys', a row's first ones behind a mask, and next to never
+// after that), so no score waits for the others of its step; P is as exact at 2^20 as at 1.  It is followed where it has grown by more than 2^8.
 // MODS: kPlain, kCapped (by a tanh, nothing else), or kAny.
 enum : int { kPlain, kCapped, kAny };
 template <int D, int W, int MODS>
@@ -523,7 +524,7 @@ struct Flow {
   static constexpr int RPT = kThreads / CPR, NL = TK / RPT;
   static constexpr int kV = 2 * TK * RB, kMeta = 2 * kV, kFlag = kMeta + (MOD ? 3 * 2 * TK * 4 : 0), kLds = kFlag + 16;      // two tiles of K, of V; positions and documents of three;
                                                      // whether a tile of V holds infinities or NaN
-  static constexpr float kGrowth = 8.0f;
+  static constexpr float kGrowth = 8.0f, kMost = 1048576.0f;
 
   const Mods& mods;
   const Keys& keys;
@@ -662,9 +663,10 @@ struct Flow {
         for (int k = i; k < i + N; ++k) s[k] = fmaf(-row.slope, fabsf((float)row.pos - __int_as_float(meta[(k / 4) * 8 + half * 4 + k % 4])), s[k]);
       }
   }
-  __device__ __forceinline__ void hide(int base, const ADSA_LDS int* meta) {               // what the row does not see of the keys from `base` on
+  template <int N>
+  __device__ __forceinline__ void hide(int i0, int base, const ADSA_LDS int* meta) {       // what the row does not see of the keys from `base` on
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = i0; i < i0 + N; ++i) {
       const int k = (i / 4) * 8 + half * 4 + i % 4;
       bool seen = base + k < row.limit;
       if constexpr (MOD)
@@ -685,11 +687,17 @@ struct Flow {
     m = m_new;
     return grows;
   }
-  __device__ __forceinline__ uint32_t two_probabilities(int i, float* sum) {
-    const float a = fast_exp2(fmaf(s[i], score_scale(), -m)), d = fast_exp2(fmaf(s[i + 1], score_scale(), -m));
-    *sum += a;
-    *sum += d;
-    return pack2_bf16(a, d);
+  __device__ __forceinline__ float probability(int i) const { return fast_exp2(fmaf(s[i], score_scale(), -m)); }
+  __device__ __forceinline__ float probabilities(uint32_t (&to)[8]) const {            // their sum
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const float a = probability(i), d = probability(i + 1);
+      sum += a;
+      sum += d;
+      to[i / 2] = pack2_bf16(a, d);
+    }
+    return sum;
   }
   __device__ __forceinline__ void rescale(float corr) {
     l *= corr;
@@ -711,10 +719,8 @@ struct Flow {
   __device__ __forceinline__ void step(int base, const ADSA_LDS int* meta) {
     f32x16 next = {};
     uint32_t pn[8];
-    float corr, sum = 0.0f;
-    bool grown = false;
+    float even = 0.0f, sum = 0.0f;
     constexpr int kAhead = D == 64 ? 2 : 3;          // pieces fetched ahead of their product (three waves a SIMD have registers for two)
-    constexpr int kMax = MODS != kPlain ? NC / 2 : 1;      // the maximum stands before this chunk's probabilities
     uint4 kp[KC];
     u32x4 vp[VC];
     auto fetch = [&](auto at) {
@@ -724,26 +730,30 @@ struct Flow {
     };
     each<kAhead>(fetch);
     each<NC>([&](auto at) {
-      constexpr int c = decltype(at)::value;
+      constexpr int c = decltype(at)::value, i0 = 16 * c / NC, n = 16 * (c + 1) / NC - i0;
       fetch(std::integral_constant<int, c + kAhead>());
       if constexpr (c < KC) next = score_product(kp[c], c, next);
       else output_product(vp[c - KC], c - KC);
-      if constexpr (MODS != kPlain && c < kMax) bend<16 / kMax>(16 / kMax * c, meta);
-      if constexpr (c == kMax) {
-        if constexpr (HIDE) hide(base, meta);
-        grown = maximum(&corr);
-      }
-      if constexpr (c >= kMax) {                     // this chunk's share of the probabilities
-        constexpr int kRest = NC - kMax, e0 = 8 * (c - kMax) / kRest;
-        each<8 * (c + 1 - kMax) / kRest - e0>([&](auto o) {
-          constexpr int e = e0 + decltype(o)::value;
-          pn[e] = two_probabilities(2 * e, &sum);
-          asm volatile("" : "+v"(pn[e]), "+v"(sum));           // (here, not where p is used)
-        });
-      }
+      // this chunk's share of the softmax
+      if constexpr (MODS != kPlain) bend<n>(i0, meta);
+      if constexpr (HIDE) hide<n>(i0, base, meta);
+      each<n>([&](auto o) {
+        constexpr int i = i0 + decltype(o)::value;
+        const float x = probability(i);
+        sum += x;
+        if constexpr (i % 2 == 0) even = x;
+        else pn[i / 2] = pack2_bf16(even, x);
+        if constexpr (i % 2 == 0) asm volatile("" : "+v"(even), "+v"(sum));            // (here, not where p is used)
+        else asm volatile("" : "+v"(pn[i / 2]), "+v"(sum));
+      });
       __builtin_amdgcn_sched_barrier(0);
     });
-    if (__ballot(grown) != 0) rescale(corr);
+    if (__ballot(sum > kMost) != 0) {
+      float corr;
+      maximum(&corr);
+      rescale(corr);
+      sum = probabilities(pn);
+    }
     l += sum;
     s = next;
 #pragma unroll
@@ -767,13 +777,11 @@ struct Flow {
   }
   __device__ __forceinline__ void softmax(int base, const ADSA_LDS int* meta) {
     if constexpr (MODS != kPlain) bend<16>(0, meta);
-    if (hides(base)) hide(base, meta);
-    float corr, sum = 0.0f;
+    if (hides(base)) hide<16>(0, base, meta);
+    float corr;
     const bool grown = maximum(&corr);
     if (__ballot(grown) != 0) rescale(corr);
-#pragma unroll
-    for (int i = 0; i < 16; i += 2) p[i / 2] = two_probabilities(i, &sum);
-    l += sum;
+    l += probabilities(p);
   }
 
   // (as a Tile's: outputs r .. r + 3 of the lane are elements from element(r) on)
