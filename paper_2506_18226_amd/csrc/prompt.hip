@@ -513,11 +513,11 @@ struct Tile {
 // compiler left alone puts all of one kind before the other.
 // A row's maximum is looked for only where a lane's sum of P passes 2^20 (the first keys', a row's first ones behind a mask, and next to never
 // after that), so no score waits for the others of its step; P is as exact at 2^20 as at 1.  It is followed where it has grown by more than 2^8.
-// MODS: kPlain, kCapped (by a tanh, nothing else), or kAny.
-enum : int { kPlain, kCapped, kAny };
+// MODS: kPlain, kCapped (by a tanh, nothing else), kAny (distances, documents or both, without a branch for either) or kAnyCapped (the same, capped or not).
+enum : int { kPlain, kCapped, kAny, kAnyCapped };
 template <int D, int W, int MODS>
 struct Flow {
-  static constexpr bool MOD = MODS == kAny;          // positions and documents are wanted, and what is done is decided at run time
+  static constexpr bool MOD = MODS >= kAny;          // keys' positions and documents are wanted (0 where there are none)
   using L = Layout<2, D>;
   static constexpr int CPR = L::CPR, RB = L::RB, DT = D / 32, KC = D / 16, VC = DT * 2, NC = KC + VC;
   static constexpr int kThreads = W * kWave, kRows = W * 32, TK = 64;
@@ -647,32 +647,18 @@ struct Flow {
   }
 
   // pieces of the two steps' work
-  // cap and distance of N scores from number i on
-  template <int N>
-  __device__ __forceinline__ void bend(int i, const ADSA_LDS int* meta) {
-    if (MODS == kCapped || mods.cap_out != 0.0f) {
-#pragma unroll
-      for (int k = i; k < i + N; ++k) s[k] = capped<2>(s[k], mods);
-    } else {
-#pragma unroll
-      for (int k = i; k < i + N; ++k) s[k] *= mods.scale_log2;
-    }
-    if constexpr (MOD)
-      if (mods.slopes) {
-#pragma unroll
-        for (int k = i; k < i + N; ++k) s[k] = fmaf(-row.slope, fabsf((float)row.pos - __int_as_float(meta[(k / 4) * 8 + half * 4 + k % 4])), s[k]);
-      }
+  // positions and documents of the keys of the lane's scores 4 q .. 4 q + 3
+  __device__ __forceinline__ u32x4 quad(const ADSA_LDS int* meta, int q) const { return *(const ADSA_LDS u32x4*)(meta + q * 8 + half * 4); }
+  // cap and distance of score number i
+  __device__ __forceinline__ void bend(int i, const u32x4& pos) {
+    if (MODS == kCapped || (MODS == kAnyCapped && mods.cap_out != 0.0f)) s[i] = capped<2>(s[i], mods);
+    else s[i] *= mods.scale_log2;
+    if constexpr (MOD) s[i] = fmaf(-row.slope, fabsf((float)row.pos - __uint_as_float(pos[i % 4])), s[i]);
   }
-  template <int N>
-  __device__ __forceinline__ void hide(int i0, int base, const ADSA_LDS int* meta) {       // what the row does not see of the keys from `base` on
-#pragma unroll
-    for (int i = i0; i < i0 + N; ++i) {
-      const int k = (i / 4) * 8 + half * 4 + i % 4;
-      bool seen = base + k < row.limit;
-      if constexpr (MOD)
-        if (keys.doc) seen &= meta[TK + k] == row.doc;
-      s[i] = seen ? s[i] : -INFINITY;
-    }
+  __device__ __forceinline__ void hide(int i, int base, const u32x4& doc) {       // if the row does not see its key, one of those from `base` on
+    bool seen = base + (i / 4) * 8 + half * 4 + i % 4 < row.limit;
+    if constexpr (MOD) seen &= (int)doc[i % 4] == row.doc;
+    s[i] = seen ? s[i] : -INFINITY;
   }
   __device__ __forceinline__ float score_scale() const { return MODS != kPlain ? 1.0f : mods.scale_log2; }
   // The step's maximum; where it has grown, what the state so far has to be multiplied by.
@@ -728,17 +714,27 @@ struct Flow {
       if constexpr (c < KC) kp[c] = k_piece(SUB, c);
       else if constexpr (c < NC) vp[c - KC] = v_piece(SUB, c - KC);
     };
+    u32x4 pos[4] = {}, doc[4] = {};
+    auto fetch_quad = [&](auto q) {
+      constexpr int i = decltype(q)::value;
+      if constexpr (MOD && i < 4) {
+        pos[i] = quad(meta, i);
+        if constexpr (HIDE) doc[i] = quad(meta + TK, i);
+      }
+    };
     each<kAhead>(fetch);
+    fetch_quad(std::integral_constant<int, 0>());
     each<NC>([&](auto at) {
       constexpr int c = decltype(at)::value, i0 = 16 * c / NC, n = 16 * (c + 1) / NC - i0;
       fetch(std::integral_constant<int, c + kAhead>());
       if constexpr (c < KC) next = score_product(kp[c], c, next);
       else output_product(vp[c - KC], c - KC);
       // this chunk's share of the softmax
-      if constexpr (MODS != kPlain) bend<n>(i0, meta);
-      if constexpr (HIDE) hide<n>(i0, base, meta);
+      if constexpr (i0 % 4 == 0) fetch_quad(std::integral_constant<int, i0 / 4 + 1>());
       each<n>([&](auto o) {
         constexpr int i = i0 + decltype(o)::value;
+        if constexpr (MODS != kPlain) bend(i, pos[i / 4]);
+        if constexpr (HIDE) hide(i, base, doc[i / 4]);
         const float x = probability(i);
         sum += x;
         if constexpr (i % 2 == 0) even = x;
@@ -776,8 +772,13 @@ struct Flow {
     for (int c = 0; c < KC; ++c) s = score_product(k_piece(sub, c), c, s);
   }
   __device__ __forceinline__ void softmax(int base, const ADSA_LDS int* meta) {
-    if constexpr (MODS != kPlain) bend<16>(0, meta);
-    if (hides(base)) hide<16>(0, base, meta);
+    const bool hidden = hides(base);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const u32x4 none = {};
+      if constexpr (MODS != kPlain) bend(i, MOD ? quad(meta, i / 4) : none);
+      if (hidden) hide(i, base, MOD ? quad(meta + TK, i / 4) : none);
+    }
     float corr;
     const bool grown = maximum(&corr);
     if (__ballot(grown) != 0) rescale(corr);
@@ -1055,7 +1056,7 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_prompt(P
 }
 
 template <int D, int W, int MODS>
-__global__ __launch_bounds__(W * kWave, D == 64 ? 3 : 2) void k_prompt_many(PromptArgs A) {
+__global__ __launch_bounds__(W * kWave, D == 64 && MODS < kAny ? 3 : 2) void k_prompt_many(PromptArgs A) {
   using F = Flow<D, W, MODS>;
   extern __shared__ __align__(16) char s_lds[];
   Job J;
@@ -1511,7 +1512,7 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(S
     }
     if (MOD && A.mods.slopes) keys.pos0 = keys.pos[keys.begin];
     if constexpr (BIG) {
-      Flow<D, WK, MOD ? kAny : kPlain> t(A.mods, keys, (lchar*)s_lds);
+      Flow<D, WK, MOD ? kAnyCapped : kPlain> t(A.mods, keys, (lchar*)s_lds);
       attend(t, tile * kRows + t.wave * 32 + t.col);
     } else {
       Tile<EB, D, WK, MOD, false, true> t(A.mods, keys, (lchar*)s_lds);
@@ -1766,7 +1767,7 @@ template <int EB, int D> constexpr int kKeyWaves = EB == 4 && D == 128 ? 2 : 4;
 // Workgroups of 8 waves (256 rows), where 4 waves' share of staging a tile leaves too few registers.  us with 4 | 8 waves, 2 x 4352 x 32 x 128 lowered with
 // distance 1281 | 953; elsewhere 4 waves are as fast or faster: 4 x 4352 x 32 x 128 820 | 797, capped ragged prompts of 64 over 8 heads
 // 247 | 267, 16 x 300..600 x 24 x 64 36 | 51.
-template <int D, int MODS> constexpr bool two_sizes = D == 128 && MODS == kAny;
+template <int D, int MODS> constexpr bool two_sizes = D == 128 && MODS >= kAny;
 
 template <int EB, int D, bool MOD>
 hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStream_t st) {
@@ -1788,8 +1789,10 @@ hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStrea
         k_prompt_many<D, 4, M><<<grid, 4 * kWave, Flow<D, 4, M>::kLds, st>>>(A);
       };
       if constexpr (!MOD) many(std::integral_constant<int, kPlain>());
-      else if (A.mods.slopes || A.mods.doc) many(std::integral_constant<int, kAny>());
-      else many(std::integral_constant<int, kCapped>());
+      else if (A.mods.slopes || A.mods.doc) {
+        if (A.mods.cap_out != 0.0f) many(std::integral_constant<int, kAnyCapped>());
+        else many(std::integral_constant<int, kAny>());
+      } else many(std::integral_constant<int, kCapped>());
     }
   }
   if (plan.chunks > 1) {
@@ -1806,7 +1809,7 @@ hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStrea
 template <int EB, int D, bool MOD, bool BIG>
 constexpr int shared_lds = [] {
   const int own = Shape<EB, D, kKeyWaves<EB, D>>::kLds;
-  if constexpr (BIG) return std::max(own, Flow<D, 4, MOD ? kAny : kPlain>::kLds);
+  if constexpr (BIG) return std::max(own, Flow<D, 4, MOD ? kAnyCapped : kPlain>::kLds);
   else return own;
 }();
 
@@ -1847,6 +1850,7 @@ hipError_t allow_lds() {
     else {
       many(std::integral_constant<int, kCapped>());
       many(std::integral_constant<int, kAny>());
+      many(std::integral_constant<int, kAnyCapped>());
     }
     allow(k_shared<EB, D, KW, MOD, true, true>, shared_lds<EB, D, MOD, true>);
     allow(k_shared<EB, D, KW, MOD, false, true>, shared_lds<EB, D, MOD, true>);
