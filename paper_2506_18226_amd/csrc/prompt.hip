@@ -148,7 +148,7 @@ struct Tile {
   bool bad;                    // V held infinities or NaN where not every row sees them
   // the next step's rows on their way
   uint4 kr[NL], vr[NL];
-  int slot_next[NL];           // LIST: slots of the step after it
+  int slot_next[NL], meta_next, stand_in;        // LIST: entries of the step after it
   int meta_slot;
   float meta_pos;
   int meta_doc;
@@ -167,34 +167,30 @@ struct Tile {
     for (int s = 0; s < CPR / 2; ++s) qf[s] = load16(q_row + (2 * s + half) * 16);
   }
 
-  // entry of the list, or the key itself, brought into the cache; the slot that is not attended: its neighbour in the list instead
-  // (rows of the cache that hold nothing yet must not reach the sums, not even times 0)
-  __device__ __forceinline__ int slot_at(int key) const {
-    const int at = min(key, keys.end - 1);
-    if constexpr (!LIST) return at;
-    int s = keys.list[at];
-    if (s == keys.skip) s = keys.list[at > keys.begin ? at - 1 : min(at + 1, keys.end - 1)];
-    return min(max(s, 0), keys.last_slot);
-  }
+  // LIST: entries are asked for a step before the rows they name, and looked at only when those are (a look waits for whatever was asked for before it,
+  // the rows of the step ahead among it).  Instead of the slot that is not attended (rows of the cache that hold nothing yet must not reach the sums,
+  // not even times 0): another one of the list.
+  __device__ __forceinline__ int entry(int key) const { return keys.list[min(key, keys.end - 1)]; }
+  __device__ __forceinline__ int slot_of(int entry) const { return min(max(entry == keys.skip ? stand_in : entry, 0), keys.last_slot); }
   __device__ __forceinline__ void load_slots(int base) {
     if constexpr (LIST) {
 #pragma unroll
-      for (int i = 0; i < NL; ++i) slot_next[i] = slot_at(base + staged(i));
+      for (int i = 0; i < NL; ++i) slot_next[i] = entry(base + staged(i));
+      if (brings()) meta_next = entry(base + brought());
     }
   }
   __device__ __forceinline__ void load_rows(int base) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int slot = LIST ? slot_next[i] : slot_at(base + staged(i));
+      const int slot = LIST ? slot_of(slot_next[i]) : min(base + staged(i), keys.end - 1);
       const long long off = (long long)slot * keys.stride_b + (tid % CPR) * 16;
       kr[i] = load16(keys.k + off);
       vr[i] = load16(keys.v + off);
     }
     if (brings()) {
-      const int at = min(base + brought(), keys.end - 1);
-      if constexpr (LIST) meta_slot = keys.list[at];
+      if constexpr (LIST) meta_slot = meta_next;
       if constexpr (MOD) {
-        const int slot = slot_at(base + brought());
+        const int slot = LIST ? slot_of(meta_next) : min(base + brought(), keys.end - 1);
         meta_pos = mods.slopes ? (float)(keys.pos[slot] - keys.pos0) : 0.0f;
         meta_doc = keys.doc ? keys.doc[slot] : 0;
       }
@@ -445,6 +441,10 @@ struct Tile {
       return wanted;
     };
     bool masked;
+    if constexpr (LIST) {
+      stand_in = keys.list[keys.begin];
+      if (stand_in == keys.skip) stand_in = keys.list[min(keys.begin + 1, keys.end - 1)];
+    }
     load_slots(keys.begin);
     load_rows(keys.begin);
     load_slots(keys.begin + TK);
