@@ -150,7 +150,7 @@ struct Tile {
   uint4 kr[NL], vr[NL];
   int slot_next[NL], meta_next, stand_in;        // LIST: entries of the step after it
   int meta_slot;
-  float meta_pos;
+  int meta_pos;
   int meta_doc;
 
   __device__ __forceinline__ Tile(const Mods& mods_, const Keys& keys_, lchar* lds_)
@@ -191,7 +191,7 @@ struct Tile {
       if constexpr (LIST) meta_slot = meta_next;
       if constexpr (MOD) {
         const int slot = LIST ? slot_of(meta_next) : min(base + brought(), keys.end - 1);
-        meta_pos = mods.slopes ? (float)(keys.pos[slot] - keys.pos0) : 0.0f;
+        meta_pos = mods.slopes ? keys.pos[slot] : keys.pos0;       // (not touched before store_rows: a touch waits for the rows)
         meta_doc = keys.doc ? keys.doc[slot] : 0;
       }
     }
@@ -205,7 +205,7 @@ struct Tile {
     }
     if (brings()) {
       ADSA_LDS int* const meta = (ADSA_LDS int*)(lds + S::kMeta) + brought();
-      if constexpr (MOD) { meta[0] = __float_as_int(meta_pos); meta[TK] = meta_doc; }
+      if constexpr (MOD) { meta[0] = __float_as_int((float)(meta_pos - keys.pos0)); meta[TK] = meta_doc; }
       if constexpr (LIST) meta[2 * TK] = meta_slot == keys.skip;
     }
   }
@@ -588,7 +588,7 @@ struct Flow {
     if constexpr (MOD)
       if (tid < TK) {
         ADSA_LDS int* const meta = (ADSA_LDS int*)(lds + kMeta) + third * 2 * TK;
-        meta[tid] = meta_pos;
+        meta[tid] = __float_as_int((float)(meta_pos - keys.pos0));
         meta[TK + tid] = meta_doc;
       }
   }
@@ -607,7 +607,7 @@ struct Flow {
     if constexpr (MOD)
       if (tid < TK) {
         const int slot = min(base + tid, keys.end - 1);
-        meta_pos = mods.slopes ? __float_as_int((float)(keys.pos[slot] - keys.pos0)) : 0;
+        meta_pos = mods.slopes ? keys.pos[slot] : keys.pos0;       // (not touched before store_k: a touch waits for the rows)
         meta_doc = keys.doc ? keys.doc[slot] : 0;
       }
   }
