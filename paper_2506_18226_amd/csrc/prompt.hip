@@ -1025,6 +1025,8 @@ __device__ __forceinline__ void store_lse(const PromptArgs& A, size_t at, float 
   if (A.norm) ((gfloat*)A.norm)[at] = l == 0.0f ? INFINITY : m + __log2f(l);           // (exp2(z - norm): 0 for a row that sees nothing)
 }
 
+// Few rows, or fp32: a Tile.  Bound by dependent trips where keys are few (3 x 2..7 tokens x 20 heads x 64 behind 2011 slots: 10.6 us for 31 MB), by HBM where they are
+// many (16 x 1..9 x 24 x 64 behind 700: 15 us, 4.5 TB/s), in fp32 by the matrix core (8 x 900..1000 x 16 x 64: 203 us, 73 TFLOP/s of whole and part-seen blocks).
 template <int EB, int D, int WK, bool MOD>
 __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_prompt(PromptArgs A) {
   using T = Tile<EB, D, WK, MOD, false, false>;
@@ -1055,6 +1057,9 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_prompt(P
   }
 }
 
+// Many rows of a bf16 cache: a Flow.  4 x 4352 x 32 x 128 causal 690-710 us (0.89 PFLOP/s), 4 x 4352 x 24 x 64 312 us (0.74), capped ragged prompts of 64 heads over 8
+// 226 us (0.53), 2 x 4352 x 32 x 128 lowered with distance 462 us (0.67).  Three waves a SIMD at head size 64, but for distances and documents (16 x 300..600 x 24 x 64 with
+// three | two 92 | 59 us: spills).
 template <int D, int W, int MODS>
 __global__ __launch_bounds__(W * kWave, D == 64 && MODS < kAny ? 3 : 2) void k_prompt_many(PromptArgs A) {
   using F = Flow<D, W, MODS>;
@@ -1091,7 +1096,7 @@ __global__ __launch_bounds__(W * kWave, D == 64 && MODS < kAny ? 3 : 2) void k_p
 }
 
 // Split keys: a wave joins the parts of one row.  Nothing it loads depends on anything but its arguments (bound by one trip to memory): 16 bytes of a
-// part's outputs to a lane, 64 * 4 / D parts side by side, and every part's maximum and sum to a lane of its own.
+// part's outputs to a lane, 64 * 4 / D parts side by side, and every part's maximum and sum to a lane of its own.  3.3 us for 8 parts of 260 rows of 64.
 template <int EB, int D>
 __global__ __launch_bounds__(256) void k_prompt_finish(PromptArgs A) {
   constexpr int LPR = D / 4, kSide = kWave / LPR, kBatch = 4;
@@ -1138,7 +1143,8 @@ __global__ __launch_bounds__(256) void k_prompt_finish(PromptArgs A) {
 // score[head][slot] += sum over rows of the probability they gave the slot.  A wave keeps NB x 32 slots' K rows as the A operand and meets the rows
 // from the first that can see the slots on, 32 at a time; a lane's column is a row, whose normaliser (m + log2 l) it holds, and its registers
 // are slots, which it sums up over its rows: lanes meet once, at the end.  The products of a block of rows run beside the exponentials of
-// the one before.  Two blocks of slots share a fetch of q rows (with one, LDS takes as long as the products).
+// the one before.  Two blocks of slots share a fetch of q rows (with one, LDS takes as long as the products).  4 x 4352 x 32 x 128: 400-430 us, 0.74 PFLOP/s,
+// the vector unit busy 54 % of the time and the matrix core 34.
 template <int EB, int D, bool MOD> struct Mass {      // (slots' positions and documents, or fp32 rows, take the second block's registers)
   static constexpr int NB = EB == 2 && !MOD ? 2 : 1, kKeys = 4 * 32 * NB, kRows = 64, kTile = kRows * Layout<EB, D>::RB;
   static constexpr int kLds = 2 * kTile;
@@ -1361,7 +1367,7 @@ __device__ __forceinline__ Group group_at(const SharedArgs& A, int g) {
 // One query head over a part of its sequence's own list: nothing is shared, so there is no matrix product; bound by the rows' way from HBM.
 // 16 bytes of a row per lane, 64 / (row bytes / 16) tokens ("a unit") per load of a wave; kRing units of K and V are on their way at any time, and
 // a unit's registers are refilled as soon as it is folded into its lanes' softmax states.  Entries that are not attended read the query's
-// row instead (whatever the cache holds there must not reach the sums, not even times 0).
+// row instead (whatever the cache holds there must not reach the sums, not even times 0).  32 x 24 heads x 553 tokens x 64, with prompts of 120: 20.4-22 us for 114 MB.
 template <int EB, int D, int NW, bool MOD>
 __device__ __forceinline__ void own_list(const Mods& mods, const Keys& keys, const gchar* q_row, float slope, int q_pos, gfloat* part_ml, gfloat* part_acc, lchar* lds) {
   constexpr int EPL = Elems<EB>::N, LPR = D / EPL, RPW = kWave / LPR, kRing = 8;
@@ -1448,6 +1454,7 @@ __device__ __forceinline__ void own_list(const Mods& mods, const Keys& keys, con
   }
 }
 
+// Tiles of prompts come first, since they take longest.  64 sequences x 64 heads over 8 x 128, lists of 200..577, four prompts of 2100..4352: 45 us for 159 MB (27 and 25 alone).
 // BIG: prompts are met by 128 rows at a time (bf16; groups of more than 32 rows), else by 32 rows and as many waves that split the keys.
 template <int EB, int D, int WK, bool MOD, bool ONE, bool BIG>
 __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(SharedArgs A) {
@@ -1567,7 +1574,8 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(S
 }
 
 // Joins the parts of a (sequence, cache head)'s rows with the query token, whose row enters the cache, and updates the scores.  Bound by the trips
-// that depend on each other (record; parts, list and scores' logits; scores), so everything leaves as soon as its address is known.
+// that depend on each other (record, parts, list and scores' logits; scores and the group's record), so everything leaves as soon as its address is known.
+// 5.2 us for 768 rows of one head, 10 for 512 x 8 heads with their scores, 7 without.
 constexpr int kMaxParts = 2 * kMaxChunks;
 template <int EB, int D, bool ONE>
 __global__ __launch_bounds__(256) void k_shared_finish(SharedArgs A) {
@@ -1765,8 +1773,8 @@ template <int EB, int D> constexpr int kKeyWaves = EB == 4 && D == 128 ? 2 : 4;
 
 
 // Workgroups of 8 waves (256 rows), where 4 waves' share of staging a tile leaves too few registers.  us with 4 | 8 waves, 2 x 4352 x 32 x 128 lowered with
-// distance 1281 | 953; elsewhere 4 waves are as fast or faster: 4 x 4352 x 32 x 128 820 | 797, capped ragged prompts of 64 over 8 heads
-// 247 | 267, 16 x 300..600 x 24 x 64 36 | 51.
+// distance 828 | 477, by documents 184 | 156; elsewhere 4 waves are as fast or faster: 4 x 4352 x 32 x 128 with its mass 1127 | 1102, capped ragged prompts of 64 over
+// 8 heads 226 | 242, 16 x 300..600 x 24 x 64 lowered with distance 59 | 76.
 template <int D, int MODS> constexpr bool two_sizes = D == 128 && MODS >= kAny;
 
 template <int EB, int D, bool MOD>

@@ -5,6 +5,7 @@
 //    The angle of (token, pair) is one number for all heads: sum over the axes of coordinate * frequency, in 64 bits, brought to a
 //    fraction of a turn there; its sine and cosine go to LDS once and every head's rows are turned with them.
 //    A thread turns 8 pairs: 16 bytes of bf16 on either side of the row (NEAR false), or 32 bytes in a row (NEAR).
+//    Bound by HBM (9216 tokens x 96 rows x 128: 90 us, 5 TB/s; 4352 x 72 x 64: 16.6 us, 4.8 TB/s), few tokens by two trips that depend on each other (3.4 us).
 #include <algorithm>
 
 #include "adsa_device.h"
