@@ -539,19 +539,23 @@ struct Flow {
   int meta_pos, meta_doc;
   // LDS offsets: the lane's pieces of the tile of K and of V that are read, the thread's of those that are written.  Each changes buffers
   // with every tile (K's two lie TK * RB apart, an offset's bit of that value says which; so do V's).
-  int k_at[KC], v_at[DT], k_to, v_to;
-  uint32_t row_at[NL];         // offsets of the thread's rows of a tile from its first
+  // FEW: registers are short (what is asked for ahead would be spilled, which waits for it), and offsets are formed from the first one's, of whose
+  // bits they differ in some.  us without | with: 64 x 8 tokens x 64 heads over 8 x 128 behind 2000 slots, lowered with distance, 213 | 141.
+  static constexpr bool FEW = MOD && D == 128;
+  static constexpr int KA = FEW ? 1 : KC, VA = FEW ? 1 : DT, RA = FEW ? 1 : NL;
+  int k_at[KA], v_at[VA], k_to, v_to;
+  uint32_t row_at[RA];         // offsets of the thread's rows of a tile from its first
 
   __device__ __forceinline__ Flow(const Mods& mods_, const Keys& keys_, lchar* lds_)
       : mods(mods_), keys(keys_), lds(lds_), tid(threadIdx.x), lane(threadIdx.x % kWave), col(lane % 32), half(lane / 32),
         wave(__builtin_amdgcn_readfirstlane(tid / kWave)) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) row_at[i] = (uint32_t)((tid / CPR + i * RPT) * (int)keys.stride_b + (tid % CPR) * 16);
+    for (int i = 0; i < RA; ++i) row_at[i] = (uint32_t)((tid / CPR + i * RPT) * (int)keys.stride_b + (tid % CPR) * 16);
 #pragma unroll
-    for (int c = 0; c < KC; ++c) k_at[c] = col * RB + (((2 * c + half) ^ L::swz_k(col)) << 4);
+    for (int c = 0; c < KA; ++c) k_at[c] = col * RB + (((2 * c + half) ^ L::swz_k(col)) << 4);
     const int vrow = half * 4 + (lane % 16) / 4, vcol = ((lane / 16) & 1) * 16 + (lane % 4) * 4;       // (see Tile::add_values)
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) v_at[dt] = kV + TK * RB + vrow * RB + (vcol % 8) * 2 + (((dt * 4 + vcol / 8) ^ L::swz_v(vrow)) << 4);
+    for (int dt = 0; dt < VA; ++dt) v_at[dt] = kV + TK * RB + vrow * RB + (vcol % 8) * 2 + (((dt * 4 + vcol / 8) ^ L::swz_v(vrow)) << 4);
     const int r = tid / CPR;                         // (rows RPT further on are permuted alike)
     static_assert(RPT % 16 == 0, "swizzles repeat");
     k_to = r * RB + (((tid % CPR) ^ L::swz_k(r)) << 4);
@@ -559,9 +563,9 @@ struct Flow {
   }
   __device__ __forceinline__ void change_buffers() {
 #pragma unroll
-    for (int c = 0; c < KC; ++c) k_at[c] ^= TK * RB;
+    for (int c = 0; c < KA; ++c) k_at[c] ^= TK * RB;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) v_at[dt] ^= TK * RB;
+    for (int dt = 0; dt < VA; ++dt) v_at[dt] ^= TK * RB;
     k_to ^= TK * RB;
     v_to ^= TK * RB;
   }
@@ -576,7 +580,7 @@ struct Flow {
     const int last = keys.end - 1 - base;
     if (last >= TK - 1) {
 #pragma unroll
-      for (int i = 0; i < NL; ++i) r[i] = load16(first + row_at[i]);
+      for (int i = 0; i < NL; ++i) r[i] = FEW ? load16(first + (long long)(i * RPT) * keys.stride_b + row_at[0]) : load16(first + row_at[i % RA]);
     } else {
 #pragma unroll
       for (int i = 0; i < NL; ++i) r[i] = load16(first + (uint32_t)(min(tid / CPR + i * RPT, last) * (int)keys.stride_b + (tid % CPR) * 16));
@@ -612,9 +616,9 @@ struct Flow {
       }
   }
 
-  __device__ __forceinline__ uint4 k_piece(int sub, int c) const { return lds16(lds + k_at[c] + sub * 32 * RB); }
+  __device__ __forceinline__ uint4 k_piece(int sub, int c) const { return lds16(lds + (FEW ? k_at[0] ^ c << 5 : k_at[c % KA]) + sub * 32 * RB); }
   __device__ __forceinline__ u32x4 v_piece(int sub, int i) const {
-    const lchar* const at = lds + v_at[i / 2] + (sub * 32 + 16 * (i % 2)) * RB;
+    const lchar* const at = lds + (FEW ? v_at[0] ^ i / 2 << 6 : v_at[i / 2 % VA]) + (sub * 32 + 16 * (i % 2)) * RB;
     const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ADSA_LDS i16x4*)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ADSA_LDS i16x4*)(at + 8 * RB));
     const u32x2 a = __builtin_bit_cast(u32x2, lo), b = __builtin_bit_cast(u32x2, hi);
     return u32x4{a.x, a.y, b.x, b.y};
@@ -1773,7 +1777,7 @@ template <int EB, int D> constexpr int kKeyWaves = EB == 4 && D == 128 ? 2 : 4;
 
 
 // Workgroups of 8 waves (256 rows), where 4 waves' share of staging a tile leaves too few registers.  us with 4 | 8 waves, 2 x 4352 x 32 x 128 lowered with
-// distance 828 | 477, by documents 184 | 156; elsewhere 4 waves are as fast or faster: 4 x 4352 x 32 x 128 with its mass 1127 | 1102, capped ragged prompts of 64 over
+// distance 558 | 469, by documents 163 | 143; elsewhere 4 waves are as fast or faster: 4 x 4352 x 32 x 128 with its mass 1127 | 1102, capped ragged prompts of 64 over
 // 8 heads 226 | 242, 16 x 300..600 x 24 x 64 lowered with distance 59 | 76.
 template <int D, int MODS> constexpr bool two_sizes = D == 128 && MODS >= kAny;
 
