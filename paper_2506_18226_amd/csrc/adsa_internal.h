@@ -132,7 +132,6 @@ static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t
 // ---- prompts (prompt_api.hip checks and plans, rotary.hip and prompt.hip launch)
 struct PromptPlan {
   int rows;             // of a workgroup: 32 (its waves split the keys) or 128 (32 for each of 4 waves)
-  int rows_all;         // of the longest sequence, per cache head
   bool flow;            // k_prompt_many (else k_prompt)
   int tiles;            // row tiles per (sequence, cache head)
   int chunks;           // parts the keys are split into

@@ -1062,7 +1062,7 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_prompt(P
 }
 
 // Many rows of a bf16 cache: a Flow.  4 x 4352 x 32 x 128 causal 690-710 us (0.89 PFLOP/s), 4 x 4352 x 24 x 64 312 us (0.74), capped ragged prompts of 64 heads over 8
-// 226 us (0.53), 2 x 4352 x 32 x 128 lowered with distance 462 us (0.67).  Three waves a SIMD at head size 64, but for distances and documents (16 x 300..600 x 24 x 64 with
+// 226 us (0.53), 2 x 4352 x 32 x 128 lowered with distance 495 us (0.63).  Three waves a SIMD at head size 64, but for distances and documents (16 x 300..600 x 24 x 64 with
 // three | two 92 | 59 us: spills).
 template <int D, int W, int MODS>
 __global__ __launch_bounds__(W * kWave, D == 64 && MODS < kAny ? 3 : 2) void k_prompt_many(PromptArgs A) {
@@ -1460,8 +1460,10 @@ __device__ __forceinline__ void own_list(const Mods& mods, const Keys& keys, con
 
 // Tiles of prompts come first, since they take longest.  64 sequences x 64 heads over 8 x 128, lists of 200..577, four prompts of 2100..4352: 45 us for 159 MB (27 and 25 alone).
 // BIG: prompts are met by 128 rows at a time (bf16; groups of more than 32 rows), else by 32 rows and as many waves that split the keys.
-template <int EB, int D, int WK, bool MOD, bool ONE, bool BIG>
+// MODS: what is done to scores, as a Flow has it (a Tile tells plain from anything else).
+template <int EB, int D, int WK, int MODS, bool ONE, bool BIG>
 __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(SharedArgs A) {
+  constexpr bool MOD = MODS != kPlain;
   extern __shared__ __align__(16) char s_lds[];
   const int hq = A.h * A.G, C = A.prompt_chunks + A.own_chunks;
   Keys keys;
@@ -1523,7 +1525,7 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(S
     }
     if (MOD && A.mods.slopes) keys.pos0 = keys.pos[keys.begin];
     if constexpr (BIG) {
-      Flow<D, WK, MOD ? kAnyCapped : kPlain> t(A.mods, keys, (lchar*)s_lds);
+      Flow<D, WK, MODS> t(A.mods, keys, (lchar*)s_lds);
       attend(t, tile * kRows + t.wave * 32 + t.col);
     } else {
       Tile<EB, D, WK, MOD, false, true> t(A.mods, keys, (lchar*)s_lds);
@@ -1776,10 +1778,9 @@ bool modded(const Mods& m) { return m.slopes || m.doc || m.cap_out != 0.0f; }
 template <int EB, int D> constexpr int kKeyWaves = EB == 4 && D == 128 ? 2 : 4;
 
 
-// Workgroups of 8 waves (256 rows), where 4 waves' share of staging a tile leaves too few registers.  us with 4 | 8 waves, 2 x 4352 x 32 x 128 lowered with
-// distance 558 | 469, by documents 163 | 143; elsewhere 4 waves are as fast or faster: 4 x 4352 x 32 x 128 with its mass 1127 | 1102, capped ragged prompts of 64 over
-// 8 heads 226 | 242, 16 x 300..600 x 24 x 64 lowered with distance 59 | 76.
-template <int D, int MODS> constexpr bool two_sizes = D == 128 && MODS >= kAny;
+// Rows of a k_prompt_many workgroup: 4 waves' 32 each.  us with 4 | 8 waves: 4 x 4352 x 32 x 128 with its mass 1127 | 1102, lowered with distance 2 x 4352 x 32 x 128 495 | 470,
+// by documents 135 | 144, capped ragged prompts of 64 over 8 heads 226 | 242, 16 x 300..600 x 24 x 64 lowered with distance 59 | 76.
+constexpr int kRowWaves = 4;
 
 template <int EB, int D, bool MOD>
 hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStream_t st) {
@@ -1791,14 +1792,7 @@ hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStrea
     if constexpr (EB == 2) {
       auto many = [&](auto mods) {
         constexpr int M = decltype(mods)::value;
-        if constexpr (two_sizes<D, M>)
-          if (plan.rows_all > 128 && plan.chunks == 1) {
-            PromptArgs B = A;
-            B.tiles = (plan.rows_all + 255) / 256;
-            k_prompt_many<D, 8, M><<<dim3(pairs * (unsigned)B.tiles), 8 * kWave, Flow<D, 8, M>::kLds, st>>>(B);
-            return;
-          }
-        k_prompt_many<D, 4, M><<<grid, 4 * kWave, Flow<D, 4, M>::kLds, st>>>(A);
+        k_prompt_many<D, kRowWaves, M><<<grid, kRowWaves * kWave, Flow<D, kRowWaves, M>::kLds, st>>>(A);
       };
       if constexpr (!MOD) many(std::integral_constant<int, kPlain>());
       else if (A.mods.slopes || A.mods.doc) {
@@ -1818,10 +1812,10 @@ hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStrea
   return hipGetLastError();
 }
 
-template <int EB, int D, bool MOD, bool BIG>
+template <int EB, int D, int MODS, bool BIG>
 constexpr int shared_lds = [] {
   const int own = Shape<EB, D, kKeyWaves<EB, D>>::kLds;
-  if constexpr (BIG) return std::max(own, Flow<D, 4, MOD ? kAnyCapped : kPlain>::kLds);
+  if constexpr (BIG) return std::max(own, Flow<D, 4, MODS>::kLds);
   else return own;
 }();
 
@@ -1829,13 +1823,23 @@ template <int EB, int D, bool MOD>
 hipError_t shared_launches(const SharedArgs& A, const SharedPlan& plan, hipStream_t st) {
   constexpr int KW = kKeyWaves<EB, D>;
   const dim3 grid((unsigned)(A.prompt_blocks + A.n_seq * A.h * A.own_chunks));
-  auto launch = [&](auto one, auto big) {
+  auto launch = [&](auto mods, auto big) {
+    constexpr int M = decltype(mods)::value;
     constexpr bool kBig = decltype(big)::value;
-    k_shared<EB, D, KW, MOD, decltype(one)::value, kBig><<<grid, KW * kWave, shared_lds<EB, D, MOD, kBig>, st>>>(A);
+    if (A.G == 1) k_shared<EB, D, KW, M, true, kBig><<<grid, KW * kWave, shared_lds<EB, D, M, kBig>, st>>>(A);
+    else k_shared<EB, D, KW, M, false, kBig><<<grid, KW * kWave, shared_lds<EB, D, M, kBig>, st>>>(A);
   };
-  auto by_group = [&](auto big) { if (A.G == 1) launch(std::true_type(), big); else launch(std::false_type(), big); };
-  if constexpr (EB == 2) { if (plan.big) by_group(std::true_type()); else by_group(std::false_type()); }
-  else by_group(std::false_type());
+  using std::integral_constant;
+  constexpr int kAll = MOD ? kAnyCapped : kPlain;
+  bool done = false;
+  if constexpr (EB == 2)
+    if (plan.big) {
+      done = true;
+      if (MOD && !A.mods.slopes) launch(integral_constant<int, MOD ? kCapped : kPlain>(), std::true_type());
+      else if (MOD && A.mods.cap_out == 0.0f) launch(integral_constant<int, MOD ? kAny : kPlain>(), std::true_type());
+      else launch(integral_constant<int, kAll>(), std::true_type());
+    }
+  if (!done) launch(integral_constant<int, kAll>(), std::false_type());
   if (A.G == 1) k_shared_finish<EB, D, true><<<dim3((unsigned)(A.n_seq * A.h)), 256, 0, st>>>(A);
   else k_shared_finish<EB, D, false><<<dim3((unsigned)(A.n_seq * A.h)), 256, 0, st>>>(A);
   return hipGetLastError();
@@ -1850,22 +1854,26 @@ hipError_t allow_lds() {
   };
   allow(k_prompt<EB, D, KW, MOD>, Shape<EB, D, KW>::kLds);
   allow(k_prompt_mass<EB, D, MOD>, Mass<EB, D, MOD>::kLds);
-  allow(k_shared<EB, D, KW, MOD, true, false>, shared_lds<EB, D, MOD, false>);
-  allow(k_shared<EB, D, KW, MOD, false, false>, shared_lds<EB, D, MOD, false>);
+  auto shared = [&](auto mods, auto big) {
+    constexpr int M = decltype(mods)::value;
+    constexpr bool kBig = decltype(big)::value;
+    allow(k_shared<EB, D, KW, M, true, kBig>, shared_lds<EB, D, M, kBig>);
+    allow(k_shared<EB, D, KW, M, false, kBig>, shared_lds<EB, D, M, kBig>);
+  };
+  using std::integral_constant;
+  shared(integral_constant<int, MOD ? kAnyCapped : kPlain>(), std::false_type());
   if constexpr (EB == 2) {
     auto many = [&](auto mods) {
       constexpr int M = decltype(mods)::value;
-      allow(k_prompt_many<D, 4, M>, Flow<D, 4, M>::kLds);
-      if constexpr (two_sizes<D, M>) allow(k_prompt_many<D, 8, M>, Flow<D, 8, M>::kLds);
+      allow(k_prompt_many<D, kRowWaves, M>, Flow<D, kRowWaves, M>::kLds);
     };
-    if constexpr (!MOD) many(std::integral_constant<int, kPlain>());
+    auto both = [&](auto mods) { many(mods); shared(mods, std::true_type()); };
+    if constexpr (!MOD) both(integral_constant<int, kPlain>());
     else {
-      many(std::integral_constant<int, kCapped>());
-      many(std::integral_constant<int, kAny>());
-      many(std::integral_constant<int, kAnyCapped>());
+      both(integral_constant<int, kCapped>());
+      both(integral_constant<int, kAny>());
+      both(integral_constant<int, kAnyCapped>());
     }
-    allow(k_shared<EB, D, KW, MOD, true, true>, shared_lds<EB, D, MOD, true>);
-    allow(k_shared<EB, D, KW, MOD, false, true>, shared_lds<EB, D, MOD, true>);
   }
   return e;
 }
@@ -1909,7 +1917,6 @@ PromptPlan make_prompt_plan(const adsa_params& p, const adsa_tokens& t) {
   const bool idle = groups(128) <= 256, half = rows <= 64 && (idle || (p.head_dim == 64 && p.cap > 512));
   plan.flow = p.dtype == ADSA_BF16 && near && rows > 32 && !half && !(idle && p.cap <= 512);
   plan.rows = plan.flow ? 128 : 32;
-  plan.rows_all = (int)rows;
   plan.tiles = (int)((rows + plan.rows - 1) / plan.rows);
   // Keys are split where tiles alone leave CUs idle.  (Two parts where 256 tiles fill them: 16 x 1..9 x 24 x 64 behind 700 slots 15.4 -> 21.3 us.)
   const long long n = groups(plan.rows), most = plan.flow ? (p.cap + 511) / 512 : (p.cap + 255) / 256;
