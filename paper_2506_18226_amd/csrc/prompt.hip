@@ -423,7 +423,7 @@ struct Tile {
         for (int x = 1; x < 32; x <<= 1) { doc_lo = min(doc_lo, __shfl_xor(doc_lo, x)); doc_hi = max(doc_hi, __shfl_xor(doc_hi, x)); }
       }
     // what the wave is to do about a staged step: nothing, fold it, and whether some row does not see all of it
-    auto judge = [&](int first, bool* masked) {
+    auto examine = [&](int first, bool* masked) {
       bool wanted = first < hi;
       *masked = first + KT > lo;
       if constexpr (MOD)
@@ -455,7 +455,7 @@ struct Tile {
         load_rows(base + TK);
         load_slots(base + 2 * TK);
       }
-      if (judge(base + wk * KT, &masked)) fold(base, masked);
+      if (examine(base + wk * KT, &masked)) fold(base, masked);
     }
     if constexpr (!ALL)
       if (bad)                                       // (uniform)
@@ -463,7 +463,7 @@ struct Tile {
           load_slots(base);
           load_rows(base);
           store_rows();
-          if (judge(base + wk * KT, &masked)) fold_bad(base, masked);
+          if (examine(base + wk * KT, &masked)) fold_bad(base, masked);
         }
     l = xor_sum<32>(l);
     {                                                // the waves' states meet in LDS

@@ -144,6 +144,21 @@ def test_distances_between_far_positions(h, D, dtype, G):
     s.check(**mods, prompt_from=far)
 
 
+@pytest.mark.parametrize("h,D,G", [(2, 64, 0), (1, 128, 0), (1, 128, 5), (2, 64, 2)])
+@pytest.mark.parametrize("cap,slope,far", [(4.0, False, 0), (0.0, True, 0), (15.0, True, 0), (0.0, True, 1_000_000_000)])
+def test_many_rows_capped_and_lowered_with_distance(h, D, G, cap, slope, far):
+    """Groups of more than 32 rows, which meet their prompt 128 at a time."""
+    s = Shared([40, 3], [150, 333], [(7 * i) % 65 for i in range(43)], h, D, "bf16", G, q_scale=4.0)
+    s.batch.pos += far
+    s.pb.pos += far
+    s.batch.seqs_host["grid_origin"] += far
+    s.batch.upload_seqs()
+    s.qpos += far
+    mods = dict(softcap=cap, slopes=torch.tensor([2.0 ** -(3 + i) for i in range(h * s.G)], device=DEV) if slope else None)
+    s.run(**mods)
+    s.check(**mods, prompt_from=far)
+
+
 def test_scores_of_minus_infinity_gain_nothing():
     s = Shared([2], [0], [5, 40], 2, 64, append=False)
     for t in (s.K, s.q.view(2, 2, 1, 64)):
