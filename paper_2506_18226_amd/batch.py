@@ -81,6 +81,7 @@ class LayerBatch:
         self.workspace = torch.empty(ws, dtype=torch.uint8, device=dev)
         B.adsa_workspace_init(p, self.workspace)
         self.prompt_workspace = None
+        self._outgrown = []
 
     # ---- host -> device
     def set_sequence(self, b: int, *, k: np.ndarray, v: np.ndarray, pos: np.ndarray,
@@ -160,17 +161,20 @@ class LayerBatch:
     def _with_workspace(self, call, need) -> None:
         """call(workspace), with a larger one where that is refused as too small.  It is kept for the calls to come, whatever their stream:
         the first call of a size allocates and waits for the device, since torch orders memory by the stream that was current when it was
-        taken, so make it before a graph is captured."""
-        if self.prompt_workspace is not None:
+        taken.  A workspace that has become too small is kept as long as the batch: graphs may hold its address."""
+        ws = self.prompt_workspace
+        if ws is not None:
             try:
-                return call(self.prompt_workspace)
+                return call(ws)
             except B.AdsaError as e:
                 if e.code != B.ERR_WORKSPACE:
                     raise
-        n = need()
+            self._outgrown.append(ws)
+        n = max(need(), 256)
         if not torch.cuda.is_current_stream_capturing():
             torch.cuda.synchronize(self.device)
-        self.prompt_workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=self.device)
+        # (twice the last one at least: what is kept stays below what is used)
+        self.prompt_workspace = torch.empty(n if ws is None else max(n, 2 * ws.numel()), dtype=torch.uint8, device=self.device)
         call(self.prompt_workspace)
 
     def rotate(self, rope, q, k, q_out, k_out, coords=None, flags: int = 0, stream=None, q_stride: int = 0, k_stride: int = 0):
