@@ -286,7 +286,8 @@ int adsa_step_static(const adsa_params* p, adsa_seq* seqs, const void* q, const 
 /* ---------------------------------------------------------------------------------------------------------------------------------
  * Prompts: rotary positions, tokens that enter the caches many at a time, their attention, and decode attention for sequences that
  * share a prompt.  The entry points below take the same parameters and records as those above, one layer per call; sel_groups != 1
- * is ADSA_ERR_UNSUPPORTED in all of them.
+ * is ADSA_ERR_UNSUPPORTED in all of them.  A workspace of adsa_prefill or adsa_attend_shared holds partial results between the launches of
+ * one call: calls that may run at the same time (on streams without an order between them, or replays of graphs) need one each.
  */
 #define ADSA_MAX_AXES 3
 

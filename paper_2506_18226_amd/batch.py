@@ -80,7 +80,8 @@ class LayerBatch:
             raise B.AdsaError(-2, "adsa_workspace_bytes (invalid parameters)")
         self.workspace = torch.empty(ws, dtype=torch.uint8, device=dev)
         B.adsa_workspace_init(p, self.workspace)
-        self.prompt_workspace = None
+        self.prompt_workspace = None            # that of the last prompt call
+        self._prompt_workspaces = {}            # (entry point, stream) -> its workspace
         self._outgrown = []
 
     # ---- host -> device
@@ -158,14 +159,17 @@ class LayerBatch:
                            self.keep_map, flags, stream)
 
     # ---- prompts
-    def _with_workspace(self, call, need) -> None:
-        """call(workspace), with a larger one where that is refused as too small.  It is kept for the calls to come, whatever their stream:
-        the first call of a size allocates and waits for the device, since torch orders memory by the stream that was current when it was
+    def _with_workspace(self, name, stream, call, need) -> None:
+        """call(workspace, stream), with a larger workspace where that is refused as too small.  Each entry point has one for every stream it is
+        called on, so calls on different streams share none; replays of graphs captured on one stream are to be ordered as calls on it.
+        The first call of a size allocates and waits for the device, since torch orders memory by the stream that was current when it was
         taken.  A workspace that has become too small is kept as long as the batch: graphs may hold its address."""
-        ws = self.prompt_workspace
+        stream = B._stream(stream)
+        ws = self._prompt_workspaces.get((name, stream))
         if ws is not None:
+            self.prompt_workspace = ws
             try:
-                return call(ws)
+                return call(ws, stream)
             except B.AdsaError as e:
                 if e.code != B.ERR_WORKSPACE:
                     raise
@@ -174,8 +178,9 @@ class LayerBatch:
         if not torch.cuda.is_current_stream_capturing():
             torch.cuda.synchronize(self.device)
         # (twice the last one at least: what is kept stays below what is used)
-        self.prompt_workspace = torch.empty(n if ws is None else max(n, 2 * ws.numel()), dtype=torch.uint8, device=self.device)
-        call(self.prompt_workspace)
+        ws = torch.empty(n if ws is None else max(n, 2 * ws.numel()), dtype=torch.uint8, device=self.device)
+        self._prompt_workspaces[name, stream] = self.prompt_workspace = ws
+        call(ws, stream)
 
     def rotate(self, rope, q, k, q_out, k_out, coords=None, flags: int = 0, stream=None, q_stride: int = 0, k_stride: int = 0):
         B.adsa_rotate(self.params, rope, self.seqs, q, k, q_out, k_out, coords, flags, stream, q_stride, k_stride)
@@ -184,12 +189,13 @@ class LayerBatch:
         B.adsa_append(self.params, tokens, rope, self.seqs, q, k, v, q_out, flags, stream)
 
     def prefill(self, tokens, q, out, lse, mods=None, flags: int = 0, stream=None):
-        self._with_workspace(lambda ws: B.adsa_prefill(self.params, tokens, mods, self.seqs, q, out, lse, ws, flags, stream),
+        self._with_workspace("adsa_prefill", stream, lambda ws, st: B.adsa_prefill(self.params, tokens, mods, self.seqs, q, out, lse, ws, flags, st),
                              lambda: B.adsa_prefill_workspace_bytes(self.params, tokens))
 
     def attend_shared(self, shared, q, k_new=None, v_new=None, flags: int = 0, mods=None, stream=None):
-        self._with_workspace(lambda ws: B.adsa_attend_shared(self.params, shared, mods, self.seqs, q, k_new, v_new, self.sel_idx, self.sel_cnt, self.out,
-                                                             self.lse, ws, flags, stream),
+        self._with_workspace("adsa_attend_shared", stream,
+                             lambda ws, st: B.adsa_attend_shared(self.params, shared, mods, self.seqs, q, k_new, v_new, self.sel_idx, self.sel_cnt, self.out,
+                                                                 self.lse, ws, flags, st),
                              lambda: B.adsa_shared_workspace_bytes(self.params, shared))
 
 

@@ -1,4 +1,4 @@
-"""Workspaces of the prompt calls of a batch: none is given up once a call has had it, since a captured
+"""Workspaces of the prompt calls of a batch: one for each entry point and stream, and none is given up once a call has had it, since a captured
 graph may hold its address.  (No GPU: tensors are the host's, and calls do what the library does about a workspace that is too small.)"""
 import gc
 import weakref
@@ -29,7 +29,7 @@ def batch(monkeypatch):
     b.device, b.params, b.seqs = torch.device("cpu"), B.make_params(n_seq=2, n_heads=1, head_dim=64, grid_h=4, grid_w=4, win_rows_back=1, win_col_radius=1, dtype=B.F32,
                                                                     score_mode=B.SCORE_ATTN_MASS, cap=40), None
     b.sel_idx = b.sel_cnt = b.out = b.lse = b.prompt_workspace = None
-    b._outgrown = []
+    b._prompt_workspaces, b._outgrown = {}, []
     q, mods = torch.zeros(2, 1, 64), None
     tokens = B.make_tokens(torch.tensor([0, 1, 2], dtype=torch.int32), torch.zeros(2, dtype=torch.int32), 2, 1)
     shared = B.AdsaShared()
@@ -53,6 +53,13 @@ def test_a_workspace_that_a_graph_may_hold_is_kept(batch, call):
     for at, ref in held:
         assert ref() is not None and ref().data_ptr() == at
     assert sum(w.numel() for w in batch._outgrown) <= batch.prompt_workspace.numel() + 1000
+
+
+def test_calls_that_may_run_at_one_time_share_no_workspace(batch):
+    places = {(call, stream): batch.run(call, 700, stream)[0] for call in ("prefill", "shared") for stream in (1, 2)}
+    assert len(set(places.values())) == 4
+    for (call, stream), at in places.items():                # ... and each finds its own again
+        assert batch.run(call, 600, stream)[0] == at and batch.prompt_workspace.data_ptr() == at
 
 
 def test_other_errors_pass_through(batch, monkeypatch):
