@@ -54,10 +54,13 @@ class AdsaParams(C.Structure):
 
 
 class _HostStruct(C.Structure):
-    """A host struct of device pointers: it keeps the tensors they belong to alive."""
+    """A host struct of device pointers: it keeps the tensors they belong to alive, and what their shapes say for the checks of the calls
+    (nothing where a field was filled with a raw pointer)."""
+    sizes = ()                     # (name, elements along the first axis); see _check_sizes
+    width = None                   # elements along the second axis of what has one
 
-    def _hold(self, *tensors):
-        self.held = tensors
+    def _hold(self, *tensors, sizes=(), width=None):
+        self.held, self.sizes, self.width = tensors, tuple((name, n) for name, n in sizes if n is not None), width
         return self
 
 
@@ -80,6 +83,7 @@ class AdsaMods(_HostStruct):
 
 class AdsaShared(_HostStruct):
     """Mirror of `adsa_shared` (host struct)."""
+    rows = None                    # (heads, head_dim, dtype) of the prompts' caches
     _fields_ = [("n_groups", C.c_int32), ("max_prompt", C.c_int32), ("max_members", C.c_int32), ("reserved", C.c_int32),
                 ("prompts", C.c_void_p), ("members", C.c_void_p), ("kv_slot_stride", C.c_int64), ("kv_head_stride", C.c_int64)]
 
@@ -319,6 +323,28 @@ def _expect(name, x, dtype, *shape):
         raise ValueError(f"{name}: a contiguous {dtype} tensor{' of shape ' + str(shape) if shape else ''} expected")
 
 
+def _length(x):
+    """Elements of a tensor along its first axis; None of a raw pointer, whose shape nobody knows."""
+    return None if x is None or isinstance(x, int) else x.shape[0] if x.dim() else 1
+
+
+def _check_sizes(struct, **least) -> None:
+    """What a call reads of a host struct's tensors has to be there."""
+    if struct is not None:
+        for name, n in struct.sizes:
+            if n < least.get(name, 0):
+                raise ValueError(f"{name}: {least[name]} expected along the first axis, {n} there")
+
+
+def _check_rope(params, rope, coords_width) -> None:
+    if rope is None:
+        return
+    if rope.width not in (None, params.head_dim // 2):
+        raise ValueError(f"freq: [axes][{params.head_dim // 2}] expected, {rope.width} there")
+    if coords_width not in (None, rope.n_axes):
+        raise ValueError(f"coords: one number for each of {rope.n_axes} axes expected, {coords_width} there")
+
+
 def make_rope(freq, *, pairing="halves", text, origin, row, col) -> AdsaRope:
     """Fill `adsa_rope`.  freq: fp64 device tensor [axes][head_dim / 2], radians by which one unit of each axis turns each pair; the other
     arguments hold one integer per axis (see include/adsa.h for the rule from position to coordinates)."""
@@ -327,29 +353,38 @@ def make_rope(freq, *, pairing="halves", text, origin, row, col) -> AdsaRope:
         raise ValueError(f"freq: [1..{MAX_AXES}][head_dim / 2] expected")
     n = freq.shape[0]
     return AdsaRope(_ptr(freq), n, PAIRINGS[pairing], _axes("text", text, n), _axes("origin", origin, n), _axes("row", row, n),
-                    _axes("col", col, n))._hold(freq)
+                    _axes("col", col, n))._hold(freq, width=freq.shape[1])
 
 
 def make_tokens(begin, slot0, n_tokens, max_len, *, pos0=None, coords=None, q_stride=0, k_stride=0, v_stride=0) -> AdsaTokens:
     """Fill `adsa_tokens`: int32 device tensors begin [n_seq + 1], slot0 and pos0 [n_seq], coords [n_tokens][axes]."""
     for name, x in (("begin", begin), ("slot0", slot0), ("pos0", pos0), ("coords", coords)):
         _expect(name, x, "int32")
+    if _length(coords) is not None and (coords.dim() != 2 or coords.shape[0] < n_tokens):
+        raise ValueError(f"coords: [{n_tokens}][axes] expected")
     return AdsaTokens(n_tokens, max_len, _ptr(begin), _ptr(slot0), _ptr(pos0), _ptr(coords), q_stride, k_stride, v_stride)._hold(
-        begin, slot0, pos0, coords)
+        begin, slot0, pos0, coords, sizes=(("begin", _length(begin)), ("slot0", _length(slot0)), ("pos0", _length(pos0))),
+        width=None if _length(coords) is None else coords.shape[1])
 
 
 def make_mods(*, softcap=0.0, mask=MASK_CAUSAL, slopes=None, doc=None) -> AdsaMods:
     """Fill `adsa_mods`: slopes float32 [query heads], doc int32 [n_seq][>= cap], both on the device."""
     _expect("slopes", slopes, "float32")
     _expect("doc", doc, "int32")
-    return AdsaMods(softcap, mask, _ptr(slopes), _ptr(doc), 0 if doc is None else doc.shape[-1])._hold(slopes, doc)
+    stride = 0 if doc is None else doc.shape[-1]
+    return AdsaMods(softcap, mask, _ptr(slopes), _ptr(doc), stride)._hold(
+        slopes, doc, sizes=(("slopes", _length(slopes)), ("doc", None if doc is None else doc.numel() // max(stride, 1))))
 
 
 def make_shared(prompt_params, prompts, members, *, max_members) -> AdsaShared:
     """Fill `adsa_shared`: the records `prompts` (one per group) of caches made for prompt_params, and int32 members [n_groups + 1]."""
     _expect("members", members, "int32")
     p = prompt_params
-    return AdsaShared(p.n_seq, p.cap, max_members, 0, _ptr(prompts), _ptr(members), p.kv_slot_stride, p.kv_head_stride)._hold(prompts, members)
+    shared = AdsaShared(p.n_seq, p.cap, max_members, 0, _ptr(prompts), _ptr(members), p.kv_slot_stride, p.kv_head_stride)._hold(
+        prompts, members, sizes=(("members", _length(members)), ("prompts", None if _length(prompts) is None else _nbytes(prompts) // SEQ_DTYPE.itemsize)))
+    _check_sizes(shared, members=p.n_seq + 1, prompts=p.n_seq)
+    shared.rows = p.n_heads, p.head_dim, p.dtype
+    return shared
 
 
 def _host(x):
@@ -375,11 +410,35 @@ def _prompt_call(name, params, second, third, flags, stream, workspace, *rest) -
 
 
 def adsa_rotate(params, rope, seqs, q, k, q_out, k_out, coords=None, flags=0, stream=None, q_stride=0, k_stride=0) -> None:
-    _prompt_call("adsa_rotate", params, _struct(rope, AdsaRope, "rope"), None, flags, stream, None, seqs, coords, q, k, q_out, k_out, q_stride, k_stride)
+    _struct(rope, AdsaRope, "rope")
+    width = None
+    if not (coords is None or isinstance(coords, (int, tuple))):
+        _expect("coords", coords, "int32")
+        if coords.dim() != 2 or coords.shape[0] < params.n_seq:
+            raise ValueError(f"coords: [{params.n_seq}][axes] expected")
+        width = coords.shape[1]
+    _check_rope(params, rope, width)
+    _prompt_call("adsa_rotate", params, rope, None, flags, stream, None, seqs, coords, q, k, q_out, k_out, q_stride, k_stride)
+
+
+def _tokens(params, tokens):
+    _struct(tokens, AdsaTokens, "tokens")
+    _check_sizes(tokens, begin=params.n_seq + 1, slot0=params.n_seq, pos0=params.n_seq)
+    return tokens
+
+
+def _mods(params, mods, docs):
+    _struct(mods, AdsaMods, "mods")
+    if mods is not None:
+        _check_sizes(mods, slopes=query_heads(params), doc=docs)
+    return mods
 
 
 def adsa_append(params, tokens, rope, seqs, q, k, v, q_out, flags=0, stream=None) -> None:
-    _prompt_call("adsa_append", params, _struct(tokens, AdsaTokens, "tokens"), _struct(rope, AdsaRope, "rope"), flags, stream, None, seqs, q, k, v, q_out)
+    _struct(rope, AdsaRope, "rope")
+    _tokens(params, tokens)
+    _check_rope(params, rope, None if tokens is None else tokens.width)
+    _prompt_call("adsa_append", params, tokens, rope, flags, stream, None, seqs, q, k, v, q_out)
 
 
 def adsa_prefill_workspace_bytes(params, tokens) -> int:
@@ -387,7 +446,7 @@ def adsa_prefill_workspace_bytes(params, tokens) -> int:
 
 
 def adsa_prefill(params, tokens, mods, seqs, q, out, lse, workspace, flags=0, stream=None) -> None:
-    _prompt_call("adsa_prefill", params, _struct(tokens, AdsaTokens, "tokens"), _struct(mods, AdsaMods, "mods"), flags, stream, workspace, seqs, q, out, lse)
+    _prompt_call("adsa_prefill", params, _tokens(params, tokens), _mods(params, mods, params.n_seq), flags, stream, workspace, seqs, q, out, lse)
 
 
 def adsa_shared_workspace_bytes(params, shared) -> int:
@@ -395,7 +454,10 @@ def adsa_shared_workspace_bytes(params, shared) -> int:
 
 
 def adsa_attend_shared(params, shared, mods, seqs, q, k_new, v_new, sel_idx, sel_cnt, out, lse, workspace, flags=0, stream=None) -> None:
-    _prompt_call("adsa_attend_shared", params, _struct(shared, AdsaShared, "shared"), _struct(mods, AdsaMods, "mods"), flags, stream, workspace, seqs, q,
+    _struct(shared, AdsaShared, "shared")
+    if shared is not None and shared.rows not in (None, (params.n_heads, params.head_dim, params.dtype)):
+        raise ValueError(f"shared: prompts of (heads, head_dim, dtype) {shared.rows}, sequences of {(params.n_heads, params.head_dim, params.dtype)}")
+    _prompt_call("adsa_attend_shared", params, shared, _mods(params, mods, 0), flags, stream, workspace, seqs, q,
                  k_new, v_new, sel_idx, sel_cnt, out, lse)
 
 
