@@ -137,6 +137,14 @@ __device__ __forceinline__ float xor_max(float x) {
   }
 }
 
+// Lanes of one wave hand data to each other through LDS: LDS instructions of a wave execute in
+// issue order, so only the compiler has to be kept from moving accesses across this point.
+__device__ __forceinline__ void wave_lds_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Sum over the LPR consecutive lanes that hold one row; every lane of the group gets the sum.
 template <int LPR>
 __device__ __forceinline__ float row_sum(float x) {

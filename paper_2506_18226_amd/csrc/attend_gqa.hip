@@ -53,14 +53,6 @@ __device__ __forceinline__ f32x4 mfma_bf16(s16x4 a, s16x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, b, c, 0, 0, 0);
 }
 
-// Lanes of one wave hand data to each other through LDS: LDS instructions of a wave execute in
-// issue order, so only the compiler has to be kept from moving accesses across this point.
-__device__ __forceinline__ void wave_lds_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // c ? a : b by components (a ternary on the structs themselves would select between their ADDRESSES and
 // keep both in memory)
 __device__ __forceinline__ uint4 pick16(bool c, const uint4& a, const uint4& b) {

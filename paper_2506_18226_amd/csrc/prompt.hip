@@ -124,7 +124,7 @@ template <int EB, int D, int WK> struct Shape {
 };
 
 // The attention of a workgroup's 32 rows (a lane's q pieces in qf) over its keys, which its waves split: each stages the 32 rows of a step that it
-// alone reads, so nobody waits for anybody in the loop.  Afterwards m, l (of the lane's row, both halves of the wave alike) and the wave's
+// alone reads, so nobody waits for anybody in the loop (its own lanes' hand-over apart).  Afterwards m, l (of the lane's row, both halves of the wave alike) and the wave's
 // share of the unnormalised outputs: acc[r], r in [0, D / 32 * 16 / WK), are the elements of register r + wk * (...) of the D / 32
 // transposed 32x32 blocks.
 // ALL: every row sees every key (but the ones past the end, which repeat the last), so none can hold what must not reach a row.
@@ -388,6 +388,7 @@ struct Tile {
     l += sum;
     if (!ALL && masked && values_bad(r0)) {          // as 0 for now
       clear_bad_values(r0);
+      wave_lds_sync();
       bad = true;
     }
     add_values(r0, p);
@@ -450,7 +451,9 @@ struct Tile {
     load_slots(keys.begin + TK);
     const int end = min(hi, keys.end);               // (from here on keys are others')
     for (int base = keys.begin; base + wk * KT < end; base += TK) {
+      wave_lds_sync();                               // (the step before has been read)
       store_rows();
+      wave_lds_sync();
       if (base + TK < keys.end) {
         load_rows(base + TK);
         load_slots(base + 2 * TK);
@@ -462,7 +465,9 @@ struct Tile {
         for (int base = keys.begin; base + wk * KT < end; base += TK) {
           load_slots(base);
           load_rows(base);
+          wave_lds_sync();
           store_rows();
+          wave_lds_sync();
           if (examine(base + wk * KT, &masked)) fold_bad(base, masked);
         }
     l = xor_sum<32>(l);
