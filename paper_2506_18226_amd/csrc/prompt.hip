@@ -896,7 +896,7 @@ struct PromptArgs {
 
 // A sequence's new tokens: where they stand in the packed rows and in the cache.
 struct Prompt {
-  int from, len, slot0, prefix, status;      // status: 0, or why the record does not fit
+  int from, len, slot0, prefix, status;      // status: 0, or why the record does not fit (one without new tokens does)
 };
 __device__ __forceinline__ Prompt prompt_of(const PromptArgs& A, int b) {
   const ADSA_GLOBAL adsa_seq& sq = ((const ADSA_GLOBAL adsa_seq*)A.seqs)[b];
@@ -908,7 +908,7 @@ __device__ __forceinline__ Prompt prompt_of(const PromptArgs& A, int b) {
   const int n_res = sq.n_res;
   pr.prefix = A.mask == ADSA_MASK_PREFIX ? sq.n_keep_prefix : 0;
   if (pr.from < 0 || pr.len < 0 || pr.len > A.n_tokens || pr.from > A.n_tokens - pr.len) pr.len = 0;        // (begin[] is not what it should be)
-  if (pr.status == 0 && (n_res < 0 || n_res > A.cap || pr.slot0 < 0 || pr.len > A.max_len || pr.slot0 > n_res - pr.len)) pr.status = ADSA_SEQ_BAD_STATE;
+  if (pr.status == 0 && pr.len > 0 && (n_res < 0 || n_res > A.cap || pr.slot0 < 0 || pr.len > A.max_len || pr.slot0 > n_res - pr.len)) pr.status = ADSA_SEQ_BAD_STATE;
   return pr;
 }
 // keys below this are seen by the token in slot s
