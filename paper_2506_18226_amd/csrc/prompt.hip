@@ -127,7 +127,8 @@ template <int EB, int D, int WK> struct Shape {
 // alone reads, so nobody waits for anybody in the loop (its own lanes' hand-over apart).  Afterwards m, l (of the lane's row, both halves of the wave alike) and the wave's
 // share of the unnormalised outputs: acc[r], r in [0, D / 32 * 16 / WK), are the elements of register r + wk * (...) of the D / 32
 // transposed 32x32 blocks.
-// ALL: every row sees every key (but the ones past the end, which repeat the last), so none can hold what must not reach a row.
+// ALL: every row sees every key of the list or prompt, so none can hold what must not reach a row.  What stands in for others (past the end, or
+// for the query token) counts as 0 in V: its probability is 0, but 0 times an infinity is not.
 template <int EB, int D, int WK, bool MOD, bool LIST, bool ALL>
 struct Tile {
   using L = Layout<EB, D>;
@@ -196,7 +197,14 @@ struct Tile {
       }
     }
   }
-  __device__ __forceinline__ void store_rows() {
+  __device__ __forceinline__ void store_rows(int base) {
+    if (ALL && base + wk * KT + KT > keys.end) {     // (uniform: the wave's last step)
+      int past = base + staged(0) - keys.end;
+      asm volatile("" : "+v"(past));                 // (formed here: no registers in the loop)
+#pragma unroll
+      for (int i = 0; i < NL; ++i)
+        if (past + i * RPT >= 0) vr[i] = make_uint4(0, 0, 0, 0);
+    }
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int r = staged(i), c = tid % CPR;
@@ -436,7 +444,15 @@ struct Tile {
       if constexpr (LIST) {
         if (keys.skip >= 0) {
           const ADSA_LDS int* const flag = (const ADSA_LDS int*)(lds + S::kMeta) + 2 * TK + wk * KT;
-          *masked |= __ballot(lane < KT && flag[lane % KT] != 0) != 0;
+          const uint64_t hit = __ballot(lane < KT && flag[lane % KT] != 0);
+          *masked |= hit != 0;
+          if (hit != 0) {                            // (a list names a slot once)
+            int piece = lane;
+            uint32_t zero = 0;
+            asm volatile("" : "+v"(piece), "+v"(zero));          // (as in store_rows)
+            if (piece < CPR) put16(lds + TK * RB + (wk * KT + __builtin_ctzll(hit)) * RB + piece * 16, make_uint4(zero, zero, zero, zero));
+            wave_lds_sync();
+          }
         }
       }
       return wanted;
@@ -445,6 +461,7 @@ struct Tile {
     if constexpr (LIST) {
       stand_in = keys.list[keys.begin];
       if (stand_in == keys.skip) stand_in = keys.list[min(keys.begin + 1, keys.end - 1)];
+      stand_in = __builtin_amdgcn_readfirstlane(stand_in);
     }
     load_slots(keys.begin);
     load_rows(keys.begin);
@@ -452,7 +469,7 @@ struct Tile {
     const int end = min(hi, keys.end);               // (from here on keys are others')
     for (int base = keys.begin; base + wk * KT < end; base += TK) {
       wave_lds_sync();                               // (the step before has been read)
-      store_rows();
+      store_rows(base);
       wave_lds_sync();
       if (base + TK < keys.end) {
         load_rows(base + TK);
@@ -466,7 +483,7 @@ struct Tile {
           load_slots(base);
           load_rows(base);
           wave_lds_sync();
-          store_rows();
+          store_rows(base);
           wave_lds_sync();
           if (examine(base + wk * KT, &masked)) fold_bad(base, masked);
         }
