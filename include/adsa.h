@@ -328,7 +328,7 @@ typedef enum { ADSA_MASK_CAUSAL = 0,       /* a token sees itself and the slots 
 
 /* [host] What is done to scaled scores z = q.k * softmax_scale before the softmax; NULL: nothing, causal. */
 typedef struct adsa_mods {
-  float softcap;               /* > 0: z <- softcap * tanh(z / softcap); 0: not */
+  float softcap;               /* > 0: z <- softcap * tanh(z / softcap); 0: not.  softmax_scale / softcap and 1.45 softcap have to be normal fp32 numbers */
   int32_t mask;                /* adsa_mask (adsa_prefill) */
   const float* slopes;         /* device, one per query head: z <- z - slopes[head] * |difference of absolute positions|, after the cap; or NULL */
   const int32_t* doc;          /* device [n_seq][doc_stride]: document of every slot; a token sees only its own document's slots, and a

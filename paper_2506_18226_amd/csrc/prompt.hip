@@ -50,6 +50,7 @@ struct Mods {
   const int32_t* doc;          // [n_seq][doc_stride], or NULL
   long long doc_stride;
   float cap_in, cap_out;       // softmax scale / cap, cap * log2(e); cap_out 0: no cap
+  bool wide;                   // a cap so far off that scores near 0 need more than capped<2> keeps of them (bf16)
   float scale_log2;            // softmax scale * log2(e)
 };
 
@@ -102,12 +103,27 @@ __device__ __forceinline__ uint32_t ones_at(uint32_t w, bool negative) {
 }
 __device__ __forceinline__ bool f32_bad(float x) { return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u; }
 
-// scores of 16 elements: fp32 sum q.k -> log2 units
+// Capped score: fp32 sum q.k -> log2 units.  bf16: tanh t = 1 - 2 / (e^2t + 1), three instructions of which two are transcendental.  What it is off
+// by does not shrink with t: about 2^-22 of the cap, 6e-5 of a score's unit at kWideCap, which bf16 probabilities (2^-9) and lse hide.
+constexpr float kWideCap = 256.0f;
 template <int EB>
 __device__ __forceinline__ float capped(float s, const Mods& mods) {
   if constexpr (EB == 4) return mods.cap_out * tanhf(s * mods.cap_in);
-  // tanh t = 1 - 2 / (e^2t + 1): off by 2^-23 of 1, far below the rounding of bf16 inputs
   return fmaf(-2.0f * mods.cap_out, __builtin_amdgcn_rcpf(fast_exp2(s * (mods.cap_in * (2.0f * kLog2e))) + 1.0f), mods.cap_out);
+}
+// ... beyond kWideCap: within 2^-20 of the score itself, by tanh's series (to t^11; the next term is 1e-8 of t at 0.35) and, further out, by
+// (1 - e^-2t) / (1 + e^-2t).
+__device__ __forceinline__ float capped_wide(float s, const Mods& mods) {
+  const float t = s * mods.cap_in, a = fabsf(t), x = t * t, u = fast_exp2(a * (-2.0f * kLog2e));
+  const float near = fmaf(x, fmaf(x, fmaf(x, fmaf(x, fmaf(x, -1382.0f / 155925.0f, 62.0f / 2835.0f), -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), 1.0f) * t;
+  const float far = copysignf((1.0f - u) * __builtin_amdgcn_rcpf(1.0f + u), t);
+  return mods.cap_out * (a < 0.35f ? near : far);
+}
+template <int EB>
+__device__ __forceinline__ float capped_any(float s, const Mods& mods) {
+  if constexpr (EB == 2)
+    if (mods.wide) return capped_wide(s, mods);
+  return capped<EB>(s, mods);
 }
 
 // Two waves share a SIMD's registers, but for fp32 rows of 128, whose steps alone take half of one's.  (Within 256 registers products are formed in
@@ -177,7 +193,9 @@ struct Tile {
     if constexpr (LIST) {
 #pragma unroll
       for (int i = 0; i < NL; ++i) slot_next[i] = entry(base + staged(i));
-      if (brings()) meta_next = entry(base + brought());
+      int first = base + wk * KT;                    // (a sum with the lane that is kept would be spilled, and its reload waits for the rows asked for)
+      asm volatile("" : "+s"(first));
+      if (brings()) meta_next = entry(first + lane);
     }
   }
   __device__ __forceinline__ void load_rows(int base) {
@@ -335,7 +353,13 @@ struct Tile {
     const ADSA_LDS int* const meta = (const ADSA_LDS int*)(lds + S::kMeta) + r0;
     auto key_of = [&](int i) { return (i / 4) * 8 + half * 4 + i % 4; };      // of the lane's score number i
     if constexpr (MOD) {
-      if (mods.cap_out != 0.0f) {
+      if (EB == 2 && mods.wide) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[i] = capped_wide(s[i], mods);
+          __builtin_amdgcn_sched_barrier(0);         // (registers matter here)
+        }
+      } else if (mods.cap_out != 0.0f) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = capped<EB>(s[i], mods);
       } else {
@@ -535,7 +559,8 @@ struct Tile {
 // compiler left alone puts all of one kind before the other.
 // A row's maximum is looked for only where a lane's sum of P passes 2^20 (the first keys', a row's first ones behind a mask, and next to never
 // after that), so no score waits for the others of its step; P is as exact at 2^20 as at 1.  It is followed where it has grown by more than 2^8.
-// MODS: kPlain, kCapped (by a tanh, nothing else), kAny (distances, documents or both, without a branch for either) or kAnyCapped (the same, capped or not).
+// MODS: kPlain, kCapped (by a tanh, nothing else), kAny (distances, documents or both, without a branch for either) or kAnyCapped (the same, capped; also caps
+// beyond kWideCap; the cap is looked for at every score, which leaves little of the alternation).
 enum : int { kPlain, kCapped, kAny, kAnyCapped };
 template <int D, int W, int MODS>
 struct Flow {
@@ -675,9 +700,11 @@ struct Flow {
   // pieces of the two steps' work
   // positions and documents of the keys of the lane's scores 4 q .. 4 q + 3
   __device__ __forceinline__ u32x4 quad(const ADSA_LDS int* meta, int q) const { return *(const ADSA_LDS u32x4*)(meta + q * 8 + half * 4); }
-  // cap and distance of score number i
+  // cap and distance of score number i (WIDE: a cap beyond kWideCap)
+  template <bool WIDE = false>
   __device__ __forceinline__ void bend(int i, const u32x4& pos) {
-    if (MODS == kCapped || (MODS == kAnyCapped && mods.cap_out != 0.0f)) s[i] = capped<2>(s[i], mods);
+    if constexpr (WIDE) s[i] = capped_wide(s[i], mods);
+    else if (MODS == kCapped || (MODS == kAnyCapped && mods.cap_out != 0.0f)) s[i] = capped<2>(s[i], mods);
     else s[i] *= mods.scale_log2;
     if constexpr (MOD) s[i] = fmaf(-row.slope, fabsf((float)row.pos - __uint_as_float(pos[i % 4])), s[i]);
   }
@@ -799,10 +826,20 @@ struct Flow {
   }
   __device__ __forceinline__ void softmax(int base, const ADSA_LDS int* meta) {
     const bool hidden = hides(base);
+    auto bend_all = [&](auto wide) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        bend<decltype(wide)::value>(i, MOD ? quad(meta, i / 4) : u32x4{});
+        if (decltype(wide)::value) __builtin_amdgcn_sched_barrier(0);                  // (registers matter here)
+      }
+    };
+    if constexpr (MODS == kAnyCapped) {
+      if (mods.wide) bend_all(std::true_type());
+      else bend_all(std::false_type());
+    } else if constexpr (MODS != kPlain) bend_all(std::false_type());
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const u32x4 none = {};
-      if constexpr (MODS != kPlain) bend(i, MOD ? quad(meta, i / 4) : none);
       if (hidden) hide(i, base, MOD ? quad(meta + TK, i / 4) : none);
     }
     float corr;
@@ -874,12 +911,13 @@ struct Flow {
     tile(0, mine, false);
     next_tile(0);
     int t = 1;
-    for (; t < open; ++t) {
+    const bool wide = MODS == kAnyCapped && mods.wide;                                 // (rare: one after the other throughout)
+    for (; t < open && !wide; ++t) {
       step<0, false>(0, meta_of(t + 2) + 32);
       step<1, false>(0, meta_of(t));
       next_tile(t);
     }
-    for (; t < mine && !values_bad(t - 1); ++t) {
+    for (; t < mine && !wide && !values_bad(t - 1); ++t) {
       const int base = keys.begin + t * TK;
       step<0, true>(base - 32, meta_of(t + 2) + 32);
       step<1, true>(base, meta_of(t));
@@ -1275,14 +1313,16 @@ __global__ __launch_bounds__(256, EB == 2 ? 2 : 1) void k_prompt_mass(PromptArgs
   // what comes before the exponentials where not all is seen, or scores are changed
   auto prepare = [&](f32x16 (&s)[NB], const Column& y) {
     if constexpr (MOD) {
+      auto each_score = [&](auto f) {
 #pragma unroll
-      for (int x = 0; x < NB; ++x)
+        for (int x = 0; x < NB; ++x)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float z = A.mods.cap_out != 0.0f ? capped<EB>(s[x][i], A.mods) : s[x][i] * A.mods.scale_log2;
-          if (A.mods.slopes) z = fmaf(-y.slope, fabsf(y.pos - kpos[x][i]), z);
-          s[x][i] = z;
-        }
+          for (int i = 0; i < 16; ++i) s[x][i] = f(s[x][i], kpos[x][i]);
+      };
+      if (EB == 2 && A.mods.wide) each_score([&](float z, float) { return capped_wide(z, A.mods); });
+      else if (A.mods.cap_out != 0.0f) each_score([&](float z, float) { return capped<EB>(z, A.mods); });
+      else each_score([&](float z, float) { return z * A.mods.scale_log2; });
+      if (A.mods.slopes) each_score([&](float z, float p) { return fmaf(-y.slope, fabsf(y.pos - p), z); });
     }
     const int last = mine + NB * 32;
     if ((MOD && doc) || __ballot(y.limit < last) != 0) {
@@ -1430,7 +1470,7 @@ __device__ __forceinline__ void own_list(const Mods& mods, const Keys& keys, con
       if (i0 + u >= n) break;                        // (uniform)
       float z = row_sum<LPR>(q.dot(kr[u]));
       if constexpr (MOD) {
-        z = mods.cap_out != 0.0f ? capped<EB>(z, mods) : z * mods.scale_log2;
+        z = mods.cap_out != 0.0f ? capped_any<EB>(z, mods) : z * mods.scale_log2;
         if (mods.slopes) z = fmaf(-slope, fabsf((float)(q_pos - pos[u])), z);
       } else z = Elems<EB>::scaled(z, mods.scale_log2);
       z = ent[u] >= 0 ? z : -INFINITY;
@@ -1715,7 +1755,7 @@ __global__ __launch_bounds__(256) void k_shared_finish(SharedArgs A) {
       for (int e = 0; e < E; ++e) z = fmaf(q(e), kn[e], z);
       z = row_sum<32>(z);
       z = xor_sum<32>(z);
-      z = A.mods.cap_out != 0.0f ? capped<EB>(z, A.mods) : z * A.mods.scale_log2;      // (its distance to itself is 0)
+      z = A.mods.cap_out != 0.0f ? capped_any<EB>(z, A.mods) : z * A.mods.scale_log2;      // (its distance to itself is 0)
       if (lane == 0) s_new[h] = z;
     };
 #pragma unroll
@@ -1791,6 +1831,7 @@ Mods make_mods(const adsa_params& p, const adsa_mods& m) {
   o.doc_stride = m.doc_stride;
   o.cap_in = m.softcap > 0.0f ? scale / m.softcap : 0.0f;
   o.cap_out = m.softcap > 0.0f ? m.softcap * kLog2e : 0.0f;
+  o.wide = p.dtype == ADSA_BF16 && m.softcap > kWideCap;
   o.scale_log2 = scale * kLog2e;
   return o;
 }
@@ -1817,7 +1858,7 @@ hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStrea
         k_prompt_many<D, kRowWaves, M><<<grid, kRowWaves * kWave, Flow<D, kRowWaves, M>::kLds, st>>>(A);
       };
       if constexpr (!MOD) many(std::integral_constant<int, kPlain>());
-      else if (A.mods.slopes || A.mods.doc) {
+      else if (A.mods.slopes || A.mods.doc || A.mods.wide) {
         if (A.mods.cap_out != 0.0f) many(std::integral_constant<int, kAnyCapped>());
         else many(std::integral_constant<int, kAny>());
       } else many(std::integral_constant<int, kCapped>());
@@ -1857,7 +1898,7 @@ hipError_t shared_launches(const SharedArgs& A, const SharedPlan& plan, hipStrea
   if constexpr (EB == 2)
     if (plan.big) {
       done = true;
-      if (MOD && !A.mods.slopes) launch(integral_constant<int, MOD ? kCapped : kPlain>(), std::true_type());
+      if (MOD && !A.mods.slopes && !A.mods.wide) launch(integral_constant<int, MOD ? kCapped : kPlain>(), std::true_type());
       else if (MOD && A.mods.cap_out == 0.0f) launch(integral_constant<int, MOD ? kAny : kPlain>(), std::true_type());
       else launch(integral_constant<int, kAll>(), std::true_type());
     }

@@ -42,6 +42,10 @@ int check_tokens(const adsa_params& p, const adsa_tokens* t) {
 
 int check_mods(const adsa_params& p, const adsa_mods& m, bool prompt) {
   if (!(m.softcap >= 0.0f) || std::isinf(m.softcap)) return ADSA_ERR_SHAPE;
+  if (m.softcap > 0.0f) {                            // the kernels' constants are fp32, too
+    const float scale = p.softmax_scale > 0.0f ? p.softmax_scale : 1.0f / std::sqrt((float)p.head_dim);
+    if (!std::isnormal(scale / m.softcap) || !std::isnormal(m.softcap * 1.4426950408889634f)) return ADSA_ERR_SHAPE;
+  }
   if (!prompt) return ADSA_OK;
   if (m.mask != ADSA_MASK_CAUSAL && m.mask != ADSA_MASK_PREFIX) return ADSA_ERR_DTYPE;
   if (m.doc && m.doc_stride < p.cap) return ADSA_ERR_SHAPE;
