@@ -12,7 +12,10 @@
 // and P^T is, register by register, the B operand of O^T = V^T P^T; the order of keys that this fixes within an instruction
 // is met on the other side by how V^T is fetched, bf16 by transposing LDS loads, so P never goes through memory.
 // Scores are held in fp32 and in units of log 2 (exp2 is the hardware's); so are sums, maxima and outputs until the end.  P enters the second
-// product in the cache's type: for bf16 that rounds each probability by 2^-9 at most, as much as the output's own rounding.
+// product in the cache's type.  For bf16 prompts (k_prompt, k_prompt_many) that rounds each probability by half a step, 2^-8 of it at most, as much as
+// the output's own rounding, for two thirds of the products.  Decode attention (k_shared) is as exact as adsa_attend: P as a bf16 and what that leaves
+// of it as another, 2^-16 together, half as many products again.  us with one | with two: 64 sequences x 64 heads over 8 x 128 with four prompts 51.6 | 56.2 (capped
+// 53.7 | 61.8, with distances 66.8 | 70.7); 64 x 18 heads over 9 x 64, 553 tokens each 31.7 | 32.9; one query head's own list has fp32 products either way.
 #include <algorithm>
 #include <type_traits>
 #include <utility>
@@ -32,6 +35,14 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 #define ADSA_LDS __attribute__((address_space(3)))
 typedef ADSA_LDS char lchar;
 
+// A pointer that all lanes hold alike, in scalar registers.
+template <typename T>
+__device__ __forceinline__ T* scalar(T* p) {
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
+  const uint32_t lower = (uint32_t)__builtin_amdgcn_readfirstlane((int)x), upper = (uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32));
+  return reinterpret_cast<T*>((uint64_t)upper << 32 | lower);          // (halves without a sign)
+}
+
 // f(0) .. f(N - 1), each a constant of the program
 template <typename F, int... I>
 __device__ __forceinline__ void each(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>()), ...); }
@@ -42,6 +53,17 @@ template <int EB>
 __device__ __forceinline__ void store4(gchar* p, float a, float b, float c, float d) {
   if constexpr (EB == 4) *(ADSA_GLOBAL u32x4*)p = u32x4{__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d)};
   else *(ADSA_GLOBAL u32x2*)p = u32x2{pack2_bf16(a, b), pack2_bf16(c, d)};
+}
+
+// What a bf16 pair leaves of two fp32 values, as another pair: the two hold 16 bits of each.  (A dot product with -1 and 0 takes one of a pair.  The
+// constants come in registers: the compiler writes -1 in one half as the inline constant -1.0, which gave wrong results.)
+__device__ __forceinline__ uint32_t rest2_bf16(uint32_t pair, float a, float b) {
+  const bf16x2 x = __builtin_bit_cast(bf16x2, pair);
+  uint32_t lower = 0x0000BF80u, upper = 0xBF800000u;
+  asm("" : "+s"(lower));
+  asm("" : "+s"(upper));
+  return pack2_bf16(__builtin_amdgcn_fdot2_f32_bf16(x, __builtin_bit_cast(bf16x2, lower), a, false),
+                    __builtin_amdgcn_fdot2_f32_bf16(x, __builtin_bit_cast(bf16x2, upper), b, false));
 }
 
 // What is done to scores before the softmax.
@@ -95,6 +117,16 @@ __device__ __forceinline__ uint32_t bf16_finite(uint32_t w) {            // infi
   if ((w & 0x7F80u) == 0x7F80u) w &= 0xFFFF0000u;
   if ((w & 0x7F800000u) == 0x7F800000u) w &= 0xFFFFu;
   return w;
+}
+// whether one of N 16-byte pieces of bf16 values holds an infinity or a NaN
+template <int N>
+__device__ __forceinline__ bool bf16_bad_among(const uint4 (&r)[N]) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  u16x2 most = {0, 0};
+  auto meet = [&](uint32_t w) { most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu)); };
+#pragma unroll
+  for (int i = 0; i < N; ++i) { meet(r[i].x); meet(r[i].y); meet(r[i].z); meet(r[i].w); }
+  return most.x >= 0x7F80 || most.y >= 0x7F80;
 }
 // ones (bf16) where w's values are +infinity or -infinity; a NaN counts as both
 __device__ __forceinline__ uint32_t ones_at(uint32_t w, bool negative) {
@@ -152,6 +184,7 @@ struct Tile {
   static constexpr int KT = 32, TK = S::TK, CPR = L::CPR, RB = L::RB, DT = D / 32;
   static constexpr int RPT = kWave / CPR, NL = KT / RPT;                // rows per round of a wave; rounds
   static constexpr int kMine = DT * 16 / WK;                            // output registers of a lane after the waves' merge
+  static constexpr bool SPLIT = ALL && EB == 2;                         // probabilities in two bf16, which hold 16 bits of them
   static_assert(NL * RPT == KT && kMine % 4 == 0, "whole rounds");
 
   const Mods& mods;
@@ -162,7 +195,9 @@ struct Tile {
   Row row;
   f32x16 acc[DT];
   float m, l;
-  bool bad;                    // V held infinities or NaN where not every row sees them
+  bool bad;                    // V held infinities or NaN where not every row sees them (SPLIT: anywhere; times what is left of a probability they
+                               // may be anything)
+  bool bad_here;               // SPLIT: in the wave's staged rows
   // the next step's rows on their way
   uint4 kr[NL], vr[NL];
   int slot_next[NL], meta_next, stand_in;        // LIST: entries of the step after it
@@ -216,6 +251,7 @@ struct Tile {
     }
   }
   __device__ __forceinline__ void store_rows(int base) {
+    if constexpr (SPLIT) bad_here = __ballot(bf16_bad_among(vr)) != 0;
     if (ALL && base + wk * KT + KT > keys.end) {     // (uniform: the wave's last step)
       int past = base + staged(0) - keys.end;
       asm volatile("" : "+v"(past));                 // (formed here: no registers in the loop)
@@ -254,12 +290,17 @@ struct Tile {
   // O^T += V^T P^T over the 32 keys from row r0 of the step
   __device__ __forceinline__ void add_values(int r0, const float* p) {
     if constexpr (EB == 2) {
-      bf16x8 pb[2];
+      bf16x8 pb[2], pr[2];                           // pr (SPLIT): what pb leaves of the probabilities
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const u32x4 w = {pack2_bf16(p[8 * t], p[8 * t + 1]), pack2_bf16(p[8 * t + 2], p[8 * t + 3]), pack2_bf16(p[8 * t + 4], p[8 * t + 5]),
-                         pack2_bf16(p[8 * t + 6], p[8 * t + 7])};
+        u32x4 w, rest = {};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          w[i] = pack2_bf16(p[8 * t + 2 * i], p[8 * t + 2 * i + 1]);
+          if constexpr (SPLIT) rest[i] = rest2_bf16(w[i], p[8 * t + 2 * i], p[8 * t + 2 * i + 1]);
+        }
         pb[t] = __builtin_bit_cast(bf16x8, w);
+        pr[t] = __builtin_bit_cast(bf16x8, rest);
       }
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
@@ -267,6 +308,7 @@ struct Tile {
         for (int t = 0; t < 2; ++t) {
           const u32x4 w = value_piece(r0, dt, t);
           acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pb[t], acc[dt], 0, 0, 0);
+          if constexpr (SPLIT) acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pr[t], acc[dt], 0, 0, 0);
         }
     } else {
 #pragma unroll
@@ -418,7 +460,7 @@ struct Tile {
       sum += p[i];
     }
     l += sum;
-    if (!ALL && masked && values_bad(r0)) {          // as 0 for now
+    if (SPLIT ? bad_here : !ALL && masked && values_bad(r0)) {                 // as 0 for now
       clear_bad_values(r0);
       wave_lds_sync();
       bad = true;
@@ -428,7 +470,7 @@ struct Tile {
   // Infinities and NaN of V that not every row of their step saw (rare): another pass over the keys, behind the loop, whose registers have no room for it.
   __device__ __forceinline__ void fold_bad(int base, bool masked) {
     const int r0 = wk * KT;
-    if (!masked || !values_bad(r0)) return;
+    if ((!ALL && !masked) || !values_bad(r0)) return;
     const f32x16 s = scores(base, masked);
     float p[16];
 #pragma unroll
@@ -467,8 +509,9 @@ struct Tile {
         }
       if constexpr (LIST) {
         if (keys.skip >= 0) {
-          const ADSA_LDS int* const flag = (const ADSA_LDS int*)(lds + S::kMeta) + 2 * TK + wk * KT;
-          const uint64_t hit = __ballot(lane < KT && flag[lane % KT] != 0);
+          int at = lane;
+          asm volatile("" : "+v"(at));               // (as in store_rows)
+          const uint64_t hit = __ballot(at < KT && ((const ADSA_LDS int*)(lds + S::kMeta))[2 * TK + wk * KT + at % KT] != 0);
           *masked |= hit != 0;
           if (hit != 0) {                            // (a list names a slot once)
             int piece = lane;
@@ -501,7 +544,7 @@ struct Tile {
       }
       if (examine(base + wk * KT, &masked)) fold(base, masked);
     }
-    if constexpr (!ALL)
+    if constexpr (!ALL || SPLIT)
       if (bad)                                       // (uniform)
         for (int base = keys.begin; base + wk * KT < end; base += TK) {
           load_slots(base);
@@ -562,9 +605,11 @@ struct Tile {
 // MODS: kPlain, kCapped (by a tanh, nothing else), kAny (distances, documents or both, without a branch for either) or kAnyCapped (the same, capped; also caps
 // beyond kWideCap; the cap is looked for at every score, which leaves little of the alternation).
 enum : int { kPlain, kCapped, kAny, kAnyCapped };
-template <int D, int W, int MODS>
+// SPLIT: probabilities in two bf16, which hold 16 bits of them, and half as many products again.
+template <int D, int W, int MODS, bool SPLIT = false>
 struct Flow {
   static constexpr bool MOD = MODS >= kAny;          // keys' positions and documents are wanted (0 where there are none)
+  static constexpr bool DOCS = MOD && !SPLIT;        // (shared prompts have no documents)
   using L = Layout<2, D>;
   static constexpr int CPR = L::CPR, RB = L::RB, DT = D / 32, KC = D / 16, VC = DT * 2, NC = KC + VC;
   static constexpr int kThreads = W * kWave, kRows = W * 32, TK = 64;
@@ -580,7 +625,8 @@ struct Flow {
   uint4 qf[KC];
   Row row;
   f32x16 acc[DT], s;
-  uint32_t p[8];           // probabilities of the step before, two to a word
+  static constexpr int PW = SPLIT ? 16 : 8;
+  uint32_t p[PW];          // probabilities of the step before, two to a word (SPLIT: then what those leave of them)
   float m, l;
   uint4 kr[NL], vr[NL];
   int meta_pos, meta_doc;
@@ -588,7 +634,7 @@ struct Flow {
   // with every tile (K's two lie TK * RB apart, an offset's bit of that value says which; so do V's).
   // FEW: registers are short (what is asked for ahead would be spilled, which waits for it), and offsets are formed from the first one's, of whose
   // bits they differ in some.  us without | with: 64 x 8 tokens x 64 heads over 8 x 128 behind 2000 slots, lowered with distance, 213 | 141.
-  static constexpr bool FEW = MOD && D == 128;
+  static constexpr bool FEW = (MOD || SPLIT) && D == 128;
   static constexpr int KA = FEW ? 1 : KC, VA = FEW ? 1 : DT, RA = FEW ? 1 : NL;
   int k_at[KA], v_at[VA], k_to, v_to;
   uint32_t row_at[RA];         // offsets of the thread's rows of a tile from its first
@@ -640,18 +686,15 @@ struct Flow {
       if (tid < TK) {
         ADSA_LDS int* const meta = (ADSA_LDS int*)(lds + kMeta) + third * 2 * TK;
         meta[tid] = __float_as_int((float)(meta_pos - keys.pos0));
-        meta[TK + tid] = meta_doc;
+        if constexpr (DOCS) meta[TK + tid] = meta_doc;
       }
   }
-  // check: some row does not see all of the tile
+  // check: some row does not see all of the tile (SPLIT: infinities and NaN of V times what is left of a probability may be anything, so all are looked at)
   __device__ __forceinline__ void store_v(int t, bool check) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) put16(lds + v_to + i * RPT * RB, vr[i]);
-    if (check) {
-      bool bad = false;
-#pragma unroll
-      for (int i = 0; i < NL; ++i) bad |= bf16_bad(vr[i].x) || bf16_bad(vr[i].y) || bf16_bad(vr[i].z) || bf16_bad(vr[i].w);
-      if (__ballot(bad) != 0) *(ADSA_LDS int*)(lds + kFlag + t % 4 * 4) = t + 1;
+    if (SPLIT || check) {
+      if (__ballot(bf16_bad_among(vr)) != 0) *(ADSA_LDS int*)(lds + kFlag + t % 4 * 4) = t + 1;
     }
   }
   __device__ __forceinline__ void load_meta(int base) {
@@ -659,7 +702,7 @@ struct Flow {
       if (tid < TK) {
         const int slot = min(base + tid, keys.end - 1);
         meta_pos = mods.slopes ? keys.pos[slot] : keys.pos0;       // (not touched before store_k: a touch waits for the rows)
-        meta_doc = keys.doc ? keys.doc[slot] : 0;
+        if constexpr (DOCS) meta_doc = keys.doc ? keys.doc[slot] : 0;
       }
   }
 
@@ -710,7 +753,7 @@ struct Flow {
   }
   __device__ __forceinline__ void hide(int i, int base, const u32x4& doc) {       // if the row does not see its key, one of those from `base` on
     bool seen = base + (i / 4) * 8 + half * 4 + i % 4 < row.limit;
-    if constexpr (MOD) seen &= (int)doc[i % 4] == row.doc;
+    if constexpr (DOCS) seen &= (int)doc[i % 4] == row.doc;
     s[i] = seen ? s[i] : -INFINITY;
   }
   __device__ __forceinline__ float score_scale() const { return MODS != kPlain ? 1.0f : mods.scale_log2; }
@@ -727,7 +770,7 @@ struct Flow {
     return grows;
   }
   __device__ __forceinline__ float probability(int i) const { return fast_exp2(fmaf(s[i], score_scale(), -m)); }
-  __device__ __forceinline__ float probabilities(uint32_t (&to)[8]) const {            // their sum
+  __device__ __forceinline__ float probabilities(uint32_t (&to)[PW]) const {           // their sum
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
@@ -735,6 +778,7 @@ struct Flow {
       sum += a;
       sum += d;
       to[i / 2] = pack2_bf16(a, d);
+      if constexpr (SPLIT) to[8 + i / 2] = rest2_bf16(to[i / 2], a, d);
     }
     return sum;
   }
@@ -750,6 +794,7 @@ struct Flow {
   }
   __device__ __forceinline__ void output_product(const u32x4& v, int i) {
     acc[i / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), p_piece(i % 2), acc[i / 2], 0, 0, 0);
+    if constexpr (SPLIT) acc[i / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), p_piece(2 + i % 2), acc[i / 2], 0, 0, 0);
   }
 
   // One step (HIDE: of keys that not every row sees): the scores of K's rows (half SUB of the tile), the softmax of the scores s of the step
@@ -757,9 +802,9 @@ struct Flow {
   template <int SUB, bool HIDE>
   __device__ __forceinline__ void step(int base, const ADSA_LDS int* meta) {
     f32x16 next = {};
-    uint32_t pn[8];
+    uint32_t pn[PW];
     float even = 0.0f, sum = 0.0f;
-    constexpr int kAhead = D == 64 ? 2 : 3;          // pieces fetched ahead of their product (three waves a SIMD have registers for two)
+    constexpr int kAhead = D == 64 || (MOD && SPLIT) ? 2 : 3;        // pieces fetched ahead of their product (as registers allow)
     uint4 kp[KC];
     u32x4 vp[VC];
     auto fetch = [&](auto at) {
@@ -772,7 +817,7 @@ struct Flow {
       constexpr int i = decltype(q)::value;
       if constexpr (MOD && i < 4) {
         pos[i] = quad(meta, i);
-        if constexpr (HIDE) doc[i] = quad(meta + TK, i);
+        if constexpr (HIDE && DOCS) doc[i] = quad(meta + TK, i);
       }
     };
     each<kAhead>(fetch);
@@ -791,8 +836,12 @@ struct Flow {
         const float x = probability(i);
         sum += x;
         if constexpr (i % 2 == 0) even = x;
-        else pn[i / 2] = pack2_bf16(even, x);
+        else {
+          pn[i / 2] = pack2_bf16(even, x);
+          if constexpr (SPLIT) pn[8 + i / 2] = rest2_bf16(pn[i / 2], even, x);
+        }
         if constexpr (i % 2 == 0) asm volatile("" : "+v"(even), "+v"(sum));            // (here, not where p is used)
+        else if constexpr (SPLIT) asm volatile("" : "+v"(pn[i / 2]), "+v"(pn[8 + i / 2]), "+v"(sum));
         else asm volatile("" : "+v"(pn[i / 2]), "+v"(sum));
       });
       __builtin_amdgcn_sched_barrier(0);
@@ -806,7 +855,7 @@ struct Flow {
     l += sum;
     s = next;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) p[i] = pn[i];
+    for (int i = 0; i < PW; ++i) p[i] = pn[i];
   }
 
   // The same one after the other: first and last steps (which lack a part), and keys that not every row sees.
@@ -840,7 +889,7 @@ struct Flow {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const u32x4 none = {};
-      if (hidden) hide(i, base, MOD ? quad(meta + TK, i / 4) : none);
+      if (hidden) hide(i, base, DOCS ? quad(meta + TK, i / 4) : none);
     }
     float corr;
     const bool grown = maximum(&corr);
@@ -855,7 +904,7 @@ struct Flow {
   int lo, hi;                  // keys that all rows of the wave see, and from which on none does
   __device__ __forceinline__ bool hides(int first) const {            // whether some row does not see all of the 32 keys from `first` on
     bool x = first + 32 > lo;
-    if constexpr (MOD) x |= keys.doc != nullptr;
+    if constexpr (DOCS) x |= keys.doc != nullptr;
     return x;
   }
   // Tile number t (of `mine` that this wave's rows see): the scores of steps 2t and 2t + 1, the softmax of 2t - 1 and 2t, the outputs of 2t - 2
@@ -889,8 +938,8 @@ struct Flow {
     hi = __builtin_amdgcn_readfirstlane(hi);
     const int tiles = (keys.end - keys.begin + TK - 1) / TK, mine = max(0, (min(hi, keys.end) - keys.begin + TK - 1) / TK);
     // tiles 1 .. open - 1 have no key that some row does not see
-    const int open = MOD && keys.doc ? 1 : min(mine, max(0, lo - 32 - keys.begin) / TK + 1);
-    const int checked = MOD && keys.doc ? 0 : max(0, least - keys.begin) / TK;      // the first tile that some row of the workgroup does not see all of
+    const int open = DOCS && keys.doc ? 1 : min(mine, max(0, lo - 32 - keys.begin) / TK + 1);
+    const int checked = DOCS && keys.doc ? 0 : max(0, least - keys.begin) / TK;      // the first tile that some row of the workgroup does not see all of
     if (tid < 4) ((ADSA_LDS int*)(lds + kFlag))[tid] = 0;
     load_tile(keys.k, keys.begin, kr);
     load_meta(keys.begin);
@@ -912,7 +961,7 @@ struct Flow {
     next_tile(0);
     int t = 1;
     const bool wide = MODS == kAnyCapped && mods.wide;                                 // (rare: one after the other throughout)
-    for (; t < open && !wide; ++t) {
+    for (; t < open && !wide && !(SPLIT && values_bad(t - 1)); ++t) {
       step<0, false>(0, meta_of(t + 2) + 32);
       step<1, false>(0, meta_of(t));
       next_tile(t);
@@ -1523,8 +1572,9 @@ __device__ __forceinline__ void own_list(const Mods& mods, const Keys& keys, con
 // Tiles of prompts come first, since they take longest.  64 sequences x 64 heads over 8 x 128, lists of 200..577, four prompts of 2100..4352: 45 us for 159 MB (27 and 25 alone).
 // BIG: prompts are met by 128 rows at a time (bf16; groups of more than 32 rows), else by 32 rows and as many waves that split the keys.
 // MODS: what is done to scores, as a Flow has it (a Tile tells plain from anything else).
+// Three waves a SIMD where 64 elements of 32 rows leave registers for them (64 x 18 heads over 9 x 64, lists of 553: two | three 38.6 | 32.9 us).
 template <int EB, int D, int WK, int MODS, bool ONE, bool BIG>
-__global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(SharedArgs A) {
+__global__ __launch_bounds__(WK * kWave, (EB == 2 && D == 64 && !BIG ? 3 : kWavesPerSimd<EB, D>)) void k_shared(SharedArgs A) {
   constexpr bool MOD = MODS != kPlain;
   extern __shared__ __align__(16) char s_lds[];
   const int hq = A.h * A.G, C = A.prompt_chunks + A.own_chunks;
@@ -1568,7 +1618,7 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(S
     keys.v = (const gchar*)pr.v + head * A.prompt_head_stride_b;
     keys.stride_b = A.prompt_slot_stride_b;
     keys.list = nullptr;
-    keys.pos = (const gint*)pr.pos;
+    keys.pos = scalar((const gint*)pr.pos);
     const int per = ((gr.n + A.prompt_chunks - 1) / A.prompt_chunks + 31) / 32 * 32;
     keys.begin = min(gr.n, chunk * per);
     keys.end = min(gr.n, keys.begin + per);
@@ -1587,7 +1637,7 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(S
     }
     if (MOD && A.mods.slopes) keys.pos0 = keys.pos[keys.begin];
     if constexpr (BIG) {
-      Flow<D, WK, MODS> t(A.mods, keys, (lchar*)s_lds);
+      Flow<D, WK, MODS, true> t(A.mods, keys, (lchar*)s_lds);
       attend(t, tile * kRows + t.wave * 32 + t.col);
     } else {
       Tile<EB, D, WK, MOD, false, true> t(A.mods, keys, (lchar*)s_lds);
@@ -1604,7 +1654,7 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_shared(S
   keys.v = (const gchar*)sq.v + head * A.head_stride_b;
   keys.stride_b = A.slot_stride_b;
   keys.list = (const gint*)A.sel_idx + (size_t)b * A.sel_cap;
-  keys.pos = (const gint*)sq.pos;
+  keys.pos = scalar((const gint*)sq.pos);
   keys.last_slot = A.cap - 1;
   const int pending = A.append ? sq.pending_slot : -1;
   keys.skip = pending >= 0 && pending < A.cap ? pending : -1;
