@@ -189,14 +189,19 @@ class LayerBatch:
         B.adsa_append(self.params, tokens, rope, self.seqs, q, k, v, q_out, flags, stream)
 
     def prefill(self, tokens, q, out, lse, mods=None, flags: int = 0, stream=None):
-        self._with_workspace("adsa_prefill", stream, lambda ws, st: B.adsa_prefill(self.params, tokens, mods, self.seqs, q, out, lse, ws, flags, st),
-                             lambda: B.adsa_prefill_workspace_bytes(self.params, tokens))
+        self._prefill(self.params, self.seqs, tokens, q, out, lse, mods, flags, stream)
+
+    def _prefill(self, params, seqs, tokens, q, out, lse, mods, flags, stream):
+        self._with_workspace("adsa_prefill", stream, lambda ws, st: B.adsa_prefill(params, tokens, mods, seqs, q, out, lse, ws, flags, st),
+                             lambda: B.adsa_prefill_workspace_bytes(params, tokens))
 
     def attend_shared(self, shared, q, k_new=None, v_new=None, flags: int = 0, mods=None, stream=None):
+        self._attend_shared(self.params, self.seqs, self.sel_idx, self.sel_cnt, self.out, self.lse, shared, q, k_new, v_new, flags, mods, stream)
+
+    def _attend_shared(self, params, seqs, idx, cnt, out, lse, shared, q, k_new, v_new, flags, mods, stream):
         self._with_workspace("adsa_attend_shared", stream,
-                             lambda ws, st: B.adsa_attend_shared(self.params, shared, mods, self.seqs, q, k_new, v_new, self.sel_idx, self.sel_cnt, self.out,
-                                                                 self.lse, ws, flags, st),
-                             lambda: B.adsa_shared_workspace_bytes(self.params, shared))
+                             lambda ws, st: B.adsa_attend_shared(params, shared, mods, seqs, q, k_new, v_new, idx, cnt, out, lse, ws, flags, st),
+                             lambda: B.adsa_shared_workspace_bytes(params, shared))
 
 
 class ModelBatch(LayerBatch):
@@ -234,3 +239,26 @@ class ModelBatch(LayerBatch):
         seqs, idx, cnt, out, lse = self._layer_offsets[layer]
         B.adsa_attend(self.layer_params, (self.seqs, seqs), q, (self.sel_idx, idx), (self.sel_cnt, cnt), (self.out, out),
                       (self.lse, lse), self.layer_workspace, flags, k_new, v_new, stream)
+
+    # ---- prompts, a layer at a time: arguments as in LayerBatch, for the n_per_layer sequences of the layer
+    def _layer(self, layer: int, where: str):
+        """seqs, sel_idx, sel_cnt, out, lse of a layer."""
+        if not 0 <= layer < self.n_layers:
+            raise B.AdsaError(-1, where)
+        return tuple(zip((self.seqs, self.sel_idx, self.sel_cnt, self.out, self.lse), self._layer_offsets[layer]))
+
+    def records(self, layer: int):
+        """The layer's records, as make_shared takes a group's prompts."""
+        return self._layer(layer, "records")[0]
+
+    def rotate_layer(self, layer: int, rope, q, k, q_out, k_out, coords=None, flags: int = 0, stream=None, q_stride: int = 0, k_stride: int = 0):
+        B.adsa_rotate(self.layer_params, rope, self._layer(layer, "adsa_rotate")[0], q, k, q_out, k_out, coords, flags, stream, q_stride, k_stride)
+
+    def append_layer(self, layer: int, tokens, rope, q, k, v, q_out, flags: int = 0, stream=None):
+        B.adsa_append(self.layer_params, tokens, rope, self._layer(layer, "adsa_append")[0], q, k, v, q_out, flags, stream)
+
+    def prefill_layer(self, layer: int, tokens, q, out, lse, mods=None, flags: int = 0, stream=None):
+        self._prefill(self.layer_params, self._layer(layer, "adsa_prefill")[0], tokens, q, out, lse, mods, flags, stream)
+
+    def attend_shared_layer(self, layer: int, shared, q, k_new=None, v_new=None, flags: int = 0, mods=None, stream=None):
+        self._attend_shared(self.layer_params, *self._layer(layer, "adsa_attend_shared"), shared, q, k_new, v_new, flags, mods, stream)

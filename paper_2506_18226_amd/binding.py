@@ -197,7 +197,9 @@ def _enqueue(name: str, params, flags, workspace, stream, *pointers) -> None:
 
 
 def _ptr(x) -> Optional[int]:
-    """Device pointer of a torch tensor, or the integer itself, or None."""
+    """Device pointer of a torch tensor, the integer itself, one of these with a byte offset, or None."""
+    if isinstance(x, tuple):
+        return _ptr(x[0]) + x[1]
     return x if x is None or isinstance(x, int) else x.data_ptr()
 
 
@@ -377,11 +379,14 @@ def make_mods(*, softcap=0.0, mask=MASK_CAUSAL, slopes=None, doc=None) -> AdsaMo
 
 
 def make_shared(prompt_params, prompts, members, *, max_members) -> AdsaShared:
-    """Fill `adsa_shared`: the records `prompts` (one per group) of caches made for prompt_params, and int32 members [n_groups + 1]."""
+    """Fill `adsa_shared`: the records `prompts` (one per group; a tensor, or one and a byte offset) of caches made for prompt_params, and int32
+    members [n_groups + 1]."""
     _expect("members", members, "int32")
     p = prompt_params
+    records, skipped = prompts if isinstance(prompts, tuple) else (prompts, 0)
+    there = None if records is None or isinstance(records, int) else (_nbytes(records) - skipped) // SEQ_DTYPE.itemsize
     shared = AdsaShared(p.n_seq, p.cap, max_members, 0, _ptr(prompts), _ptr(members), p.kv_slot_stride, p.kv_head_stride)._hold(
-        prompts, members, sizes=(("members", _length(members)), ("prompts", None if _length(prompts) is None else _nbytes(prompts) // SEQ_DTYPE.itemsize)))
+        prompts, members, sizes=(("members", _length(members)), ("prompts", there)))
     _check_sizes(shared, members=p.n_seq + 1, prompts=p.n_seq)
     shared.rows = p.n_heads, p.head_dim, p.dtype
     return shared

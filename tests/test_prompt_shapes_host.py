@@ -78,3 +78,12 @@ def test_others_are_refused(calls, call, bad):
     with pytest.raises(ValueError):
         calls[call](*bad())
     assert not calls["reached"]
+
+
+def test_records_behind_others():
+    """Prompts of a later layer: what lies in front of them counts for nothing."""
+    records = torch.zeros(96 * 6, dtype=torch.uint8)
+    p = params(n_seq=2)
+    assert B.make_shared(p, (records, 96 * 4), ints(3), max_members=2).prompts == records.data_ptr() + 96 * 4
+    with pytest.raises(ValueError):
+        B.make_shared(p, (records, 96 * 5), ints(3), max_members=2)
