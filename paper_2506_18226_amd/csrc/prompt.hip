@@ -1360,7 +1360,7 @@ __global__ __launch_bounds__(256, EB == 2 ? 2 : 1) void k_prompt_mass(PromptArgs
     sum[x][i] += fast_exp2(fmaf(s[x][i], scale, -y.norm));
   };
   // what comes before the exponentials where not all is seen, or scores are changed
-  auto prepare = [&](f32x16 (&s)[NB], const Column& y) {
+  auto prepare = [&](f32x16 (&s)[NB], Column& y) {
     if constexpr (MOD) {
       auto each_score = [&](auto f) {
 #pragma unroll
@@ -1375,6 +1375,8 @@ __global__ __launch_bounds__(256, EB == 2 ? 2 : 1) void k_prompt_mass(PromptArgs
     }
     const int last = mine + NB * 32;
     if ((MOD && doc) || __ballot(y.limit < last) != 0) {
+      const float spoils = y.norm != y.norm ? y.norm : 0.0f;                 // a row whose normaliser is NaN gives that to the slots it sees, and to no others
+      y.norm = y.norm != y.norm ? 0.0f : y.norm;
 #pragma unroll
       for (int x = 0; x < NB; ++x)
 #pragma unroll
@@ -1382,12 +1384,12 @@ __global__ __launch_bounds__(256, EB == 2 ? 2 : 1) void k_prompt_mass(PromptArgs
           bool seen = mine + x * 32 + (i / 4) * 8 + half * 4 + i % 4 < y.limit;
           if constexpr (MOD)
             if (doc) seen &= kdoc[x][i] == y.doc;
-          s[x][i] = seen ? s[x][i] : -INFINITY;
+          s[x][i] = seen ? s[x][i] + spoils : -INFINITY;
         }
     }
   };
   // the products of block u of step t beside the exponentials of the block before (LAST: there is one)
-  auto block = [&](f32x16 (&next)[NB], int t, int u, auto last, f32x16 (&s)[NB], const Column& y) {
+  auto block = [&](f32x16 (&next)[NB], int t, int u, auto last, f32x16 (&s)[NB], Column& y) {
     constexpr bool kLast = decltype(last)::value;
     if constexpr (kLast) prepare(s, y);
     const lchar* const qrow = lds + (t & 1) * M::kTile + (u * 32 + col) * RB;
