@@ -382,6 +382,7 @@ int adsa_append(const adsa_params* p, const adsa_tokens* tokens, const adsa_rope
  * A row that sees nothing gives zeros and lse = -INFINITY; what masked slots hold, infinities and NaN included, changes nothing.
  * For ADSA_SCORE_ATTN_MASS and unless ADSA_FLAG_NO_ACCUMULATE is set, score[h][slot] gains the probability that the tokens' query
  * heads of cache head h gave the slot.  Sums are taken in the same order whatever the launch does: results repeat bit by bit.
+ * (bf16 caches: probabilities are rounded to bf16 before they meet V, unlike adsa_attend's and adsa_attend_shared's.)
  * A sequence with a status or without those slots (ADSA_SEQ_BAD_STATE) gets zeros; one without new tokens is left alone.
  * flags: ADSA_FLAG_NO_ACCUMULATE, ADSA_FLAG_ADVANCE (step += 1 for every sequence with new tokens, where adsa_append did not).
  */

@@ -467,7 +467,7 @@ struct Tile {
     }
     add_values(r0, p);
   }
-  // Infinities and NaN of V that not every row of their step saw (rare): another pass over the keys, behind the loop, whose registers have no room for it.
+  // Infinities and NaN of V that not every row of their step saw, or (SPLIT) any (rare): another pass over the keys, behind the loop, whose registers have no room for it.
   __device__ __forceinline__ void fold_bad(int base, bool masked) {
     const int r0 = wk * KT;
     if ((!ALL && !masked) || !values_bad(r0)) return;
@@ -1140,6 +1140,7 @@ __device__ __forceinline__ void store_lse(const PromptArgs& A, size_t at, float 
 
 // Few rows, or fp32: a Tile.  Bound by dependent trips where keys are few (3 x 2..7 tokens x 20 heads x 64 behind 2011 slots: 10.6 us for 31 MB), by HBM where they are
 // many (16 x 1..9 x 24 x 64 behind 700: 15 us, 4.5 TB/s), in fp32 by the matrix core (8 x 900..1000 x 16 x 64: 203 us, 73 TFLOP/s of whole and part-seen blocks).
+// (Caps, distances and documents of bf16 rows of 128 spill 14 words, two reloaded in the loop; fp32 rows of 64 six, outside it.)
 template <int EB, int D, int WK, bool MOD>
 __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_prompt(PromptArgs A) {
   using T = Tile<EB, D, WK, MOD, false, false>;
@@ -1171,7 +1172,9 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_prompt(P
 }
 
 // Many rows of a bf16 cache: a Flow.  4 x 4352 x 32 x 128 causal 690-710 us (0.89 PFLOP/s), 4 x 4352 x 24 x 64 312 us (0.74), capped ragged prompts of 64 heads over 8
-// 226 us (0.53), 2 x 4352 x 32 x 128 lowered with distance 495 us (0.63).  Three waves a SIMD at head size 64, but for distances and documents (16 x 300..600 x 24 x 64 with
+// 226-231 us (0.53; vector unit 58 % of the time and matrix core 24, so the two add up there: prompts of some 580 keys are few tiles a workgroup, and the first
+// and last are not interleaved), 2 x 4352 x 32 x 128 lowered with distance 488 us (0.64).  At head size 128 distances and documents need more than the 256 registers: 18 words are spilled (35 with a cap), and
+// some reloaded in the loops; plain and capped forms spill 4 outside theirs.  Three waves a SIMD at head size 64, but for distances and documents (16 x 300..600 x 24 x 64 with
 // three | two 92 | 59 us: spills).
 template <int D, int W, int MODS>
 __global__ __launch_bounds__(W * kWave, D == 64 && MODS < kAny ? 3 : 2) void k_prompt_many(PromptArgs A) {
@@ -1571,7 +1574,7 @@ __device__ __forceinline__ void own_list(const Mods& mods, const Keys& keys, con
   }
 }
 
-// Tiles of prompts come first, since they take longest.  64 sequences x 64 heads over 8 x 128, lists of 200..577, four prompts of 2100..4352: 45 us for 159 MB (27 and 25 alone).
+// Tiles of prompts come first, since they take longest.  64 sequences x 64 heads over 8 x 128, lists of 200..577, four prompts of 2100..4352: 51 us for 159 MB (37 and 28 alone).
 // BIG: prompts are met by 128 rows at a time (bf16; groups of more than 32 rows), else by 32 rows and as many waves that split the keys.
 // MODS: what is done to scores, as a Flow has it (a Tile tells plain from anything else).
 // Three waves a SIMD where 64 elements of 32 rows leave registers for them (64 x 18 heads over 9 x 64, lists of 553: two | three 38.6 | 32.9 us).
@@ -2025,7 +2028,8 @@ PromptPlan make_prompt_plan(const adsa_params& p, const adsa_tokens& t) {
   PromptPlan plan;
   auto groups = [&](int tile) { return pairs * ((rows + tile - 1) / tile); };
   const bool near = p.kv_slot_stride * 2 * 64 < (1ll << 31);       // (k_prompt_many reaches a tile's rows with 32-bit offsets from its first)
-  // Tiles of 32 rows, whose 4 waves split the keys, or of 128, whose waves share them (bf16).  us with 128 | 32 rows a tile:
+  // Tiles of 32 rows, whose 4 waves split the keys, or of 128, whose waves share them (bf16).  The host does not know how many keys there are, so the
+  // capacity stands for them, and a short prompt in a long cache takes the long ones' form (1 x 400 x 24 x 64 in 512 | 600 slots 7.8 | 16).  us with 128 | 32 rows a tile:
   // short caches that leave CUs idle, 1 x 400 x 24 heads x 64 12.5 | 7.7, 4 x 120 7.9 | 6.2; 64 rows and less, of which 128 leave half empty, behind
   // 2000 slots 2 x 60 x 24 x 64 19.4 | 14.0, behind 700 slots 16 x 60 x 24 x 64 29 | 18.4.  Elsewhere K and V are read too often: 32 x 60 x 24 x 64
   // 10.6 | 13.4, 16 x 60 x 32 x 128 behind 700 47 | 52, 2 x 1000 x 32 x 128 41 | 110.
