@@ -103,7 +103,7 @@ typedef enum {
 #define ADSA_SEQ_BAD_STATE     2   /* n_res/step out of range, or an entry newer than the query */
 #define ADSA_SEQ_SEL_OVERFLOW  4   /* attended set larger than sel_cap */
 
-/* Flags of adsa_select / adsa_attend / adsa_compact / adsa_step. */
+/* Flags of adsa_select / adsa_attend / adsa_compact / adsa_step and of the prompt side. */
 #define ADSA_FLAG_NO_COMPACT    1u  /* caller guarantees no sequence closes a grid row in this step */
 #define ADSA_FLAG_NO_ACCUMULATE 2u  /* adsa_attend: do not add attention mass to score[] */
 #define ADSA_FLAG_PLAN_APPEND   4u  /* adsa_select: reserve slot n_res for the query token (pos, zero score,
@@ -118,6 +118,11 @@ typedef enum {
 #define ADSA_FLAG_ADVANCE      16u  /* adsa_attend / adsa_compact: step += 1 for every active sequence when
                                        the call is done; give it to the LAST call of a decode step only
                                        (adsa_compact tests the row end on the step before the increment) */
+
+#define ADSA_FLAG_SPLIT_P      64u  /* adsa_prefill with a bf16 cache: probabilities meet V with 16 bits in calls of any size, as
+                                       those of the other calls do, for half as many products again.  Without it
+                                       they may be rounded to bf16, by 2^-8 of themselves at most (calls of more
+                                       than 32 rows a cache head).  No effect with an fp32 cache */
 
 /* [host] Launch-wide parameters (Section 4.1's n, m, K and the problem shape). */
 typedef struct adsa_params {
@@ -382,9 +387,8 @@ int adsa_append(const adsa_params* p, const adsa_tokens* tokens, const adsa_rope
  * A row that sees nothing gives zeros and lse = -INFINITY; what masked slots hold, infinities and NaN included, changes nothing.
  * For ADSA_SCORE_ATTN_MASS and unless ADSA_FLAG_NO_ACCUMULATE is set, score[h][slot] gains the probability that the tokens' query
  * heads of cache head h gave the slot.  Sums are taken in the same order whatever the launch does: results repeat bit by bit.
- * (bf16 caches: probabilities are rounded to bf16 before they meet V, unlike adsa_attend's and adsa_attend_shared's.)
  * A sequence with a status or without those slots (ADSA_SEQ_BAD_STATE) gets zeros; one without new tokens is left alone.
- * flags: ADSA_FLAG_NO_ACCUMULATE, ADSA_FLAG_ADVANCE (step += 1 for every sequence with new tokens, where adsa_append did not).
+ * flags: ADSA_FLAG_NO_ACCUMULATE, ADSA_FLAG_SPLIT_P, ADSA_FLAG_ADVANCE (step += 1 for every sequence with new tokens, where adsa_append did not).
  */
 int adsa_prefill(const adsa_params* p, const adsa_tokens* tokens, const adsa_mods* mods, adsa_seq* seqs, const void* q,
                  void* out, float* lse, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);

@@ -165,7 +165,7 @@ hipError_t launch_rotate(const adsa_params& p, const adsa_rope& rope, const adsa
 hipError_t launch_append(const adsa_params& p, const adsa_tokens& t, const adsa_rope* rope, adsa_seq* seqs, const void* q, const void* k, const void* v,
                          void* q_out, bool in_f32, bool advance, hipStream_t st);
 hipError_t launch_prefill(const adsa_params& p, const adsa_tokens& t, const adsa_mods& mods, const PromptPlan& plan, adsa_seq* seqs, const void* q, void* out,
-                          float* lse, char* ws, const PromptWorkspace& w, bool accumulate, bool advance, hipStream_t st);
+                          float* lse, char* ws, const PromptWorkspace& w, bool accumulate, bool advance, bool split, hipStream_t st);
 hipError_t launch_attend_shared(const adsa_params& p, const adsa_shared& s, const adsa_mods& mods, const SharedPlan& plan, adsa_seq* seqs, const void* q,
                                 const void* k_new, const void* v_new, const int32_t* sel_idx, const int32_t* sel_cnt, void* out, float* lse, char* ws,
                                 const SharedWorkspace& w, bool accumulate, bool append, bool advance, bool new_f32, hipStream_t st);

@@ -12,10 +12,11 @@
 // and P^T is, register by register, the B operand of O^T = V^T P^T; the order of keys that this fixes within an instruction
 // is met on the other side by how V^T is fetched, bf16 by transposing LDS loads, so P never goes through memory.
 // Scores are held in fp32 and in units of log 2 (exp2 is the hardware's); so are sums, maxima and outputs until the end.  P enters the second
-// product in the cache's type.  For bf16 prompts (k_prompt, k_prompt_many) that rounds each probability by half a step, 2^-8 of it at most, as much as
-// the output's own rounding, for two thirds of the products.  Decode attention (k_shared) is as exact as adsa_attend: P as a bf16 and what that leaves
-// of it as another, 2^-16 together, half as many products again.  us with one | with two: 64 sequences x 64 heads over 8 x 128 with four prompts 51.6 | 56.2 (capped
-// 53.7 | 61.8, with distances 66.8 | 70.7); 64 x 18 heads over 9 x 64, 553 tokens each 31.7 | 32.9; one query head's own list has fp32 products either way.
+// product in the cache's type: for bf16 as one value and what that leaves of it as another, 16 bits together, as exact as adsa_attend, for half as many products again.  us
+// with one | with two: 64 sequences x 64 heads over 8 x 128 with four prompts 51.6 | 56.2 (capped 53.7 | 61.8, with distances 66.8 | 70.7), 64 x 18 heads over 9 x 64 with lists
+// of 553 31.7 | 32.9, 3 x 2..7 tokens x 20 x 64 behind 2011 slots 12.2 either way, 16 x 1..9 x 24 x 64 behind 700 16.1 | 16.4.  Prompts of many rows (k_prompt_many) are bound by their
+// products and round P to one bf16, by 2^-8 of it at most, as much as the output's own rounding, unless ADSA_FLAG_SPLIT_P asks for two: 2 x 4352 x 32 x 128 364 | 511 us, lowered
+// with distance 487 | 699, by documents 131 | 160, capped ragged prompts of 64 heads over 8 226 | 271, 32 x 120 x 24 x 64 14.2 | 16.9.
 #include <algorithm>
 #include <type_traits>
 #include <utility>
@@ -184,7 +185,7 @@ struct Tile {
   static constexpr int KT = 32, TK = S::TK, CPR = L::CPR, RB = L::RB, DT = D / 32;
   static constexpr int RPT = kWave / CPR, NL = KT / RPT;                // rows per round of a wave; rounds
   static constexpr int kMine = DT * 16 / WK;                            // output registers of a lane after the waves' merge
-  static constexpr bool SPLIT = ALL && EB == 2;                         // probabilities in two bf16, which hold 16 bits of them
+  static constexpr bool SPLIT = EB == 2;                                // probabilities in two bf16, which hold 16 bits of them
   static_assert(NL * RPT == KT && kMine % 4 == 0, "whole rounds");
 
   const Mods& mods;
@@ -470,7 +471,7 @@ struct Tile {
   // Infinities and NaN of V that not every row of their step saw, or (SPLIT) any (rare): another pass over the keys, behind the loop, whose registers have no room for it.
   __device__ __forceinline__ void fold_bad(int base, bool masked) {
     const int r0 = wk * KT;
-    if ((!ALL && !masked) || !values_bad(r0)) return;
+    if ((!SPLIT && !masked) || !values_bad(r0)) return;
     const f32x16 s = scores(base, masked);
     float p[16];
 #pragma unroll
@@ -605,11 +606,10 @@ struct Tile {
 // MODS: kPlain, kCapped (by a tanh, nothing else), kAny (distances, documents or both, without a branch for either) or kAnyCapped (the same, capped; also caps
 // beyond kWideCap; the cap is looked for at every score, which leaves little of the alternation).
 enum : int { kPlain, kCapped, kAny, kAnyCapped };
-// SPLIT: probabilities in two bf16, which hold 16 bits of them, and half as many products again.
-template <int D, int W, int MODS, bool SPLIT = false>
+// SPLIT: probabilities in two bf16, which hold 16 bits of them, and half as many products again.  DOCS: keys may have documents.
+template <int D, int W, int MODS, bool SPLIT, bool DOCS>
 struct Flow {
   static constexpr bool MOD = MODS >= kAny;          // keys' positions and documents are wanted (0 where there are none)
-  static constexpr bool DOCS = MOD && !SPLIT;        // (shared prompts have no documents)
   using L = Layout<2, D>;
   static constexpr int CPR = L::CPR, RB = L::RB, DT = D / 32, KC = D / 16, VC = DT * 2, NC = KC + VC;
   static constexpr int kThreads = W * kWave, kRows = W * 32, TK = 64;
@@ -1171,14 +1171,15 @@ __global__ __launch_bounds__(WK * kWave, (kWavesPerSimd<EB, D>)) void k_prompt(P
   }
 }
 
+template <int D, int W, int MODS, bool SPLIT> using PromptFlow = Flow<D, W, MODS, SPLIT, (MODS >= kAny)>;
 // Many rows of a bf16 cache: a Flow.  4 x 4352 x 32 x 128 causal 690-710 us (0.89 PFLOP/s), 4 x 4352 x 24 x 64 312 us (0.74), capped ragged prompts of 64 heads over 8
 // 226-231 us (0.53; vector unit 58 % of the time and matrix core 24, so the two add up there: prompts of some 580 keys are few tiles a workgroup, and the first
 // and last are not interleaved), 2 x 4352 x 32 x 128 lowered with distance 488 us (0.64).  At head size 128 distances and documents need more than the 256 registers: 18 words are spilled (35 with a cap), and
 // some reloaded in the loops; plain and capped forms spill 4 outside theirs.  Three waves a SIMD at head size 64, but for distances and documents (16 x 300..600 x 24 x 64 with
 // three | two 92 | 59 us: spills).
-template <int D, int W, int MODS>
-__global__ __launch_bounds__(W * kWave, D == 64 && MODS < kAny ? 3 : 2) void k_prompt_many(PromptArgs A) {
-  using F = Flow<D, W, MODS>;
+template <int D, int W, int MODS, bool SPLIT>
+__global__ __launch_bounds__(W * kWave, D == 64 && MODS < kAny && !SPLIT ? 3 : 2) void k_prompt_many(PromptArgs A) {
+  using F = PromptFlow<D, W, MODS, SPLIT>;
   extern __shared__ __align__(16) char s_lds[];
   Job J;
   if (!job_of<2, D, F::kRows, F::kThreads>(A, J)) return;
@@ -1574,6 +1575,7 @@ __device__ __forceinline__ void own_list(const Mods& mods, const Keys& keys, con
   }
 }
 
+template <int D, int W, int MODS> using SharedFlow = Flow<D, W, MODS, true, false>;
 // Tiles of prompts come first, since they take longest.  64 sequences x 64 heads over 8 x 128, lists of 200..577, four prompts of 2100..4352: 51 us for 159 MB (37 and 28 alone).
 // BIG: prompts are met by 128 rows at a time (bf16; groups of more than 32 rows), else by 32 rows and as many waves that split the keys.
 // MODS: what is done to scores, as a Flow has it (a Tile tells plain from anything else).
@@ -1642,7 +1644,7 @@ __global__ __launch_bounds__(WK * kWave, (EB == 2 && D == 64 && !BIG ? 3 : kWave
     }
     if (MOD && A.mods.slopes) keys.pos0 = keys.pos[keys.begin];
     if constexpr (BIG) {
-      Flow<D, WK, MODS, true> t(A.mods, keys, (lchar*)s_lds);
+      SharedFlow<D, WK, MODS> t(A.mods, keys, (lchar*)s_lds);
       attend(t, tile * kRows + t.wave * 32 + t.col);
     } else {
       Tile<EB, D, WK, MOD, false, true> t(A.mods, keys, (lchar*)s_lds);
@@ -1901,17 +1903,19 @@ template <int EB, int D> constexpr int kKeyWaves = EB == 4 && D == 128 ? 2 : 4;
 constexpr int kRowWaves = 4;
 
 template <int EB, int D, bool MOD>
-hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStream_t st) {
+hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, bool split, hipStream_t st) {
   const unsigned pairs = (unsigned)((A.n_seq * A.h + 7) / 8 * 8);
   constexpr int KW = kKeyWaves<EB, D>;
   const dim3 grid(pairs * (unsigned)(plan.tiles * plan.chunks));
   if (!plan.flow) k_prompt<EB, D, KW, MOD><<<grid, KW * kWave, Shape<EB, D, KW>::kLds, st>>>(A);
   else {
     if constexpr (EB == 2) {
-      auto many = [&](auto mods) {
+      auto launch = [&](auto mods, auto two) {
         constexpr int M = decltype(mods)::value;
-        k_prompt_many<D, kRowWaves, M><<<grid, kRowWaves * kWave, Flow<D, kRowWaves, M>::kLds, st>>>(A);
+        constexpr bool kSplit = decltype(two)::value;
+        k_prompt_many<D, kRowWaves, M, kSplit><<<grid, kRowWaves * kWave, PromptFlow<D, kRowWaves, M, kSplit>::kLds, st>>>(A);
       };
+      auto many = [&](auto mods) { split ? launch(mods, std::true_type()) : launch(mods, std::false_type()); };
       if constexpr (!MOD) many(std::integral_constant<int, kPlain>());
       else if (A.mods.slopes || A.mods.doc || A.mods.wide) {
         if (A.mods.cap_out != 0.0f) many(std::integral_constant<int, kAnyCapped>());
@@ -1933,7 +1937,7 @@ hipError_t prompt_launches(const PromptArgs& A, const PromptPlan& plan, hipStrea
 template <int EB, int D, int MODS, bool BIG>
 constexpr int shared_lds = [] {
   const int own = Shape<EB, D, kKeyWaves<EB, D>>::kLds;
-  if constexpr (BIG) return std::max(own, Flow<D, 4, MODS>::kLds);
+  if constexpr (BIG) return std::max(own, SharedFlow<D, 4, MODS>::kLds);
   else return own;
 }();
 
@@ -1983,7 +1987,8 @@ hipError_t allow_lds() {
   if constexpr (EB == 2) {
     auto many = [&](auto mods) {
       constexpr int M = decltype(mods)::value;
-      allow(k_prompt_many<D, kRowWaves, M>, Flow<D, kRowWaves, M>::kLds);
+      allow(k_prompt_many<D, kRowWaves, M, false>, PromptFlow<D, kRowWaves, M, false>::kLds);
+      allow(k_prompt_many<D, kRowWaves, M, true>, PromptFlow<D, kRowWaves, M, true>::kLds);
     };
     auto both = [&](auto mods) { many(mods); shared(mods, std::true_type()); };
     if constexpr (!MOD) both(integral_constant<int, kPlain>());
@@ -2079,7 +2084,7 @@ SharedWorkspace make_shared_workspace(const adsa_params& p, const SharedPlan& pl
 }
 
 hipError_t launch_prefill(const adsa_params& p, const adsa_tokens& t, const adsa_mods& mods, const PromptPlan& plan, adsa_seq* seqs, const void* q, void* out,
-                          float* lse, char* ws, const PromptWorkspace& w, bool accumulate, bool advance, hipStream_t st) {
+                          float* lse, char* ws, const PromptWorkspace& w, bool accumulate, bool advance, bool split, hipStream_t st) {
   PromptArgs A = {};
   A.seqs = seqs; A.begin = t.begin; A.slot0 = t.slot0; A.q = (const char*)q; A.out = (char*)out; A.lse = lse;
   A.part_ml = (float*)(ws + w.part_ml_off);
@@ -2092,7 +2097,7 @@ hipError_t launch_prefill(const adsa_params& p, const adsa_tokens& t, const adsa
   A.tiles = plan.tiles; A.chunks = plan.chunks; A.advance = advance ? 1 : 0;
   A.inv_G = A.G > 1 ? (uint32_t)(((1ull << 32) + A.G - 1) / A.G) : 0;
   return by_type(p, modded(A.mods), [&](auto eb, auto d, auto m) {
-    return prompt_launches<decltype(eb)::value, decltype(d)::value, decltype(m)::value>(A, plan, st);
+    return prompt_launches<decltype(eb)::value, decltype(d)::value, decltype(m)::value>(A, plan, split, st);
   });
 }
 

@@ -162,7 +162,7 @@ int adsa_prefill(const adsa_params* p, const adsa_tokens* tokens, const adsa_mod
   if (rc) return rc;
   const bool accumulate = eff.score_mode == ADSA_SCORE_ATTN_MASS && !(flags & ADSA_FLAG_NO_ACCUMULATE);
   if (launch_prefill(eff, *tokens, m, plan, seqs, q, out, lse, (char*)workspace, w, accumulate, (flags & ADSA_FLAG_ADVANCE) != 0,
-                     reinterpret_cast<hipStream_t>(stream)) != hipSuccess)
+                     (flags & ADSA_FLAG_SPLIT_P) != 0, reinterpret_cast<hipStream_t>(stream)) != hipSuccess)
     return ADSA_ERR_LAUNCH;
   return ADSA_OK;
 }

@@ -34,7 +34,8 @@ def kernels(tmp_path_factory):
 
 # mangled name and template arguments, waves per SIMD, spilled words at most
 @pytest.mark.parametrize("kernel,waves,spilled", [
-    (r"k_prompt_manyILi64ELi4ELi[01]E", 3, 5), (r"k_prompt_manyILi64ELi4ELi[23]E", 2, 0), (r"k_prompt_manyILi128ELi4ELi[01]E", 2, 4), (r"k_prompt_manyILi128ELi4ELi[23]E", 2, 35),
+    (r"k_prompt_manyILi64ELi4ELi[01]ELb0E", 3, 5), (r"k_prompt_manyILi64ELi4ELi([23]ELb0|[0123]ELb1)E", 2, 0), (r"k_prompt_manyILi128ELi4ELi[01]E", 2, 4), (r"k_prompt_manyILi128ELi4ELi[23]ELb0E", 2, 35),
+    (r"k_prompt_manyILi128ELi4ELi[23]ELb1E", 2, 109),
     (r"k_promptILi2ELi64ELi4ELb[01]E", 2, 0), (r"k_promptILi2ELi128ELi4ELb0E", 2, 0), (r"k_promptILi2ELi128ELi4ELb1E", 2, 14), (r"k_promptILi4ELi64ELi4ELb[01]E", 2, 6),
     (r"k_promptILi4ELi128ELi2ELb[01]E", 1, 2), (r"k_prompt_massILi2E", 2, 0), (r"k_prompt_massILi4E", 1, 0), (r"k_sharedILi2ELi64ELi4ELi[03]ELb[01]ELb0E", 3, 3),
     (r"k_sharedILi2ELi64ELi4ELi[0123]ELb[01]ELb1E", 2, 0), (r"k_sharedILi2ELi128E", 2, 6), (r"k_sharedILi4ELi64E", 2, 0), (r"k_sharedILi4ELi128E", 1, 0),
