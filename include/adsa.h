@@ -47,6 +47,8 @@ extern "C" {
 #define ADSA_VERSION 1
 #define ADSA_MAX_CAP 8192      /* largest `cap` (slots per sequence) the select/compact kernels accept */
 #define ADSA_STATIC_SCRATCH_BYTES (4u << 20)   /* built-in scratch of adsa_step_static, per GPU */
+#define ADSA_MIN_PAGE 16       /* smallest `page_size` of a paged cache */
+#define ADSA_MAX_VOCAB (1 << 18)               /* most logits of a row of adsa_sample */
 
 typedef enum {
   ADSA_OK = 0,
@@ -406,6 +408,80 @@ int adsa_attend_shared(const adsa_params* p, const adsa_shared* shared, const ad
                        const void* k_new, const void* v_new, const int32_t* sel_idx, const int32_t* sel_cnt, void* out,
                        float* lse, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
 size_t adsa_shared_workspace_bytes(const adsa_params* p, const adsa_shared* shared);    /* 0 if the parameters are invalid */
+
+/* ---------------------------------------------------------------------------------------------------------------------------------
+ * Caches in pages: the K and V rows of all sequences of a launch lie in two pools of equal pages, and a table says which page holds which
+ * slots.  pos, score and the counters of a sequence stay in its record, so adsa_select, which reads no cache row, works as it is; a
+ * record's k and v are not used and may be NULL, nor are kv_slot_stride and kv_head_stride of the parameters (they have to be valid).
+ * ADSA_SCORE_VCOS and ADSA_SCORE_VCOS_FUSED, which rank by V, and sel_groups != 1 are ADSA_ERR_UNSUPPORTED in the calls below.
+ * Table entries of slots a sequence does not have are not read as pages; a sequence with resident slots on an entry that is no page of
+ * the pool gets ADSA_SEQ_BAD_STATE and zeros (adsa_append_paged: ADSA_SEQ_CACHE_FULL where it is the new tokens' slots), and its pages stay
+ * as they are.  A page may be in several sequences' tables as long as no call writes to it: pinned prefixes do not move.
+ */
+typedef struct adsa_pages {    /* [host] */
+  void* k;                     /* device: page 0 of the pool of K (dtype elements); 16-byte aligned, as is v */
+  void* v;                     /* ... of V; may be the same memory as k, with strides that keep them apart */
+  const int32_t* table;        /* device [n_seq][table_stride]: entry i of a row is the page of slots i * page_size .. + page_size - 1 */
+  int64_t page_stride;         /* elements from a page to the next, from a slot's row to the next slot's in a page, and from a */
+  int64_t slot_stride;         /* head's row to the next head's; multiples of 16 bytes, nested [page][head][slot][D] or */
+  int64_t head_stride;         /* [page][slot][head][D] */
+  int32_t page_size;           /* slots of a page: a power of two from ADSA_MIN_PAGE to ADSA_MAX_CAP */
+  int32_t n_pages;             /* pages of a pool; n_pages * page_stride, in units of the largest power of two (16 bytes at least) that divides the
+                                  three strides, below 2^31 (rows of 128 bytes, one behind the other: 256 GiB), else ADSA_ERR_UNSUPPORTED */
+  int32_t table_stride;        /* entries of a row: at least cap / page_size, rounded up; at most 65535 */
+  int32_t reserved;
+} adsa_pages;
+
+/* adsa_append, adsa_prefill, adsa_attend and adsa_compact over pages: what those say holds, but for where rows lie. */
+int adsa_append_paged(const adsa_params* p, const adsa_pages* pages, const adsa_tokens* tokens, const adsa_rope* rope, adsa_seq* seqs, const void* q,
+                      const void* k, const void* v, void* q_out, uint32_t flags, void* stream);
+int adsa_prefill_paged(const adsa_params* p, const adsa_pages* pages, const adsa_tokens* tokens, const adsa_mods* mods, adsa_seq* seqs, const void* q,
+                       void* out, float* lse, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
+size_t adsa_prefill_paged_workspace_bytes(const adsa_params* p, const adsa_pages* pages, const adsa_tokens* tokens);   /* 0 if something is invalid */
+/* Listed slots have to be resident.  flags: ADSA_FLAG_NO_ACCUMULATE, ADSA_FLAG_APPEND, ADSA_FLAG_NEW_F32, ADSA_FLAG_ADVANCE. */
+int adsa_attend_paged(const adsa_params* p, const adsa_pages* pages, adsa_seq* seqs, const void* q, const void* k_new, const void* v_new,
+                      const int32_t* sel_idx, const int32_t* sel_cnt, void* out, float* lse, uint32_t flags, void* workspace, size_t workspace_bytes,
+                      void* stream);
+/* The table is not changed: pages behind the new n_res are the caller's to give to others. */
+int adsa_compact_paged(const adsa_params* p, const adsa_pages* pages, adsa_seq* seqs, int32_t* keep_map, uint32_t flags, void* workspace,
+                       size_t workspace_bytes, void* stream);
+size_t adsa_paged_workspace_bytes(const adsa_params* p);       /* of adsa_attend_paged and adsa_compact_paged; 0 if the parameters are invalid */
+
+/* ---------------------------------------------------------------------------------------------------------------------------------
+ * The next token of every row of logits, from random numbers that the caller brings.
+ *   z[i]   the logit; guided: fp32(u + guidance * (c - u)), formed in 64 bits, of the conditional row's c and its partner's u
+ *   w[i]   exp((z[i] - max z) / temperature)
+ * In descending order of z (equal ones: the lower index first) the candidates are the first top_k, of these as few as have together top_p of
+ * their sum of w, and of these those with w >= min_p (relative to the largest, whose w is 1).  The token is the first candidate in ascending
+ * order of index at which the running sum of the candidates' w exceeds uniform times their whole sum; logprob the natural logarithm of its share.
+ * Temperature 0: the largest (the first of several), logprob 0.  A NaN counts as -infinity; where +infinities are, only these are
+ * candidates; a row without a logit above -infinity gets token -1 and logprob -infinity.  Weights are summed as whole numbers of 2^-44, whatever
+ * the order, so results repeat bit by bit; a w below that is 0.
+ */
+typedef struct adsa_sampling { /* [host] */
+  int32_t n_rows;              /* tokens to draw: 1..2^20 */
+  int32_t vocab;               /* logits of a row: 1..ADSA_MAX_VOCAB */
+  int32_t dtype;               /* adsa_dtype of the logits */
+  int32_t guided;              /* 0: n_rows rows of logits.  1: 2 * n_rows, row n_rows + r being the unconditional partner of row r */
+  int64_t row_stride;          /* elements from a row of logits to the next; 0: vocab.  Any alignment of elements */
+  float   guidance;            /* finite; 1: the conditional row alone */
+  float   temperature;         /* >= 0, finite */
+  int32_t top_k;               /* <= 0, or vocab and more: not limited */
+  float   top_p;               /* 1 and more: not limited; 0 and less: the largest alone */
+  float   min_p;               /* 0 and less: not limited; more than 1 counts as 1 */
+  int32_t reserved;
+  const float* temperatures;   /* device [n_rows], or NULL: the number above for every row (negative or NaN counts as 0) */
+  const int32_t* top_ks;       /* the same for the others (a NaN: not limited) */
+  const float* top_ps;
+  const float* min_ps;
+} adsa_sampling;
+
+/*
+ *   logits   dtype rows, aligned to their elements      uniform  float [n_rows] in [0, 1) (outside: the nearest that is)
+ *   token    int32 [n_rows], guided [2 * n_rows]: the partner gets the same token      logprob  float [n_rows], or NULL
+ *   seqs     NULL, or as many records as token has numbers: a row whose record is inactive (step < 0 or a status) gets token -1 and logprob 0
+ */
+int adsa_sample(const adsa_sampling* s, const adsa_seq* seqs, const void* logits, const float* uniform, int32_t* token, float* logprob, void* stream);
 
 /* Timing hook for benchmarks: when enabled, adsa_attend/adsa_step attach a start and a stop HIP
    event to every attention-kernel dispatch on the caller's stream (in adsa_step, where that kernel ranks for itself or plans

@@ -46,9 +46,7 @@ class LayerBatch:
         else:
             raise ValueError("LayerBatch allocates dense [head][slot][D] or [slot][head][D] caches only")
         dev = self.device
-        shape = (n, h, cap, D) if self.head_major else (n, cap, h, D)
-        self.K = torch.zeros(shape, dtype=self.tdtype, device=dev)
-        self.V = torch.zeros(shape, dtype=self.tdtype, device=dev)
+        self._allocate_caches()
         self.pos = torch.zeros((n, cap), dtype=torch.int32, device=dev)
         self.rows = B.score_rows(p)
         self.score = torch.zeros((n, self.rows, cap), dtype=torch.float32, device=dev)
@@ -59,8 +57,9 @@ class LayerBatch:
         elem = self.K.element_size()
         for b in range(n):
             s = self.seqs_host[b]
-            s["k"] = self.K.data_ptr() + b * cap * h * D * elem
-            s["v"] = self.V.data_ptr() + b * cap * h * D * elem
+            if self.dense:
+                s["k"] = self.K.data_ptr() + b * cap * h * D * elem
+                s["v"] = self.V.data_ptr() + b * cap * h * D * elem
             s["pos"] = self.pos.data_ptr() + b * cap * 4
             s["score"] = self.score.data_ptr() + b * self.rows * cap * 4
             s["step"] = -1
@@ -78,11 +77,31 @@ class LayerBatch:
         ws = B.adsa_workspace_bytes(p)
         if ws == 0:
             raise B.AdsaError(-2, "adsa_workspace_bytes (invalid parameters)")
+        if not self.dense:
+            ws = max(ws, B.adsa_paged_workspace_bytes(p))
         self.workspace = torch.empty(ws, dtype=torch.uint8, device=dev)
         B.adsa_workspace_init(p, self.workspace)
         self.prompt_workspace = None            # that of the last prompt call
         self._prompt_workspaces = {}            # (entry point, stream) -> its workspace
         self._outgrown = []
+
+    dense = True                                # every sequence has a cache of its own, cap slots long
+
+    def _allocate_caches(self) -> None:
+        p = self.params
+        shape = (p.n_seq, p.n_heads, p.cap, p.head_dim) if self.head_major else (p.n_seq, p.cap, p.n_heads, p.head_dim)
+        self.K = torch.zeros(shape, dtype=self.tdtype, device=self.device)
+        self.V = torch.zeros(shape, dtype=self.tdtype, device=self.device)
+
+    def _put_rows(self, b: int, k: torch.Tensor, v: torch.Tensor) -> None:
+        """k, v: [n][h][D], the rows of slots 0 .. n - 1 of sequence b."""
+        n = len(k)
+        if self.head_major:
+            self.K[b, :, :n] = k.transpose(0, 1)
+            self.V[b, :, :n] = v.transpose(0, 1)
+        else:
+            self.K[b, :n] = k
+            self.V[b, :n] = v
 
     # ---- host -> device
     def set_sequence(self, b: int, *, k: np.ndarray, v: np.ndarray, pos: np.ndarray,
@@ -96,13 +115,7 @@ class LayerBatch:
         if n > p.cap:
             raise ValueError("more resident slots than cap")
         if n:
-            kd, vd = to_device(k[:n], p.dtype, self.device), to_device(v[:n], p.dtype, self.device)
-            if self.head_major:
-                self.K[b, :, :n] = kd.transpose(0, 1)
-                self.V[b, :, :n] = vd.transpose(0, 1)
-            else:
-                self.K[b, :n] = kd
-                self.V[b, :n] = vd
+            self._put_rows(b, to_device(k[:n], p.dtype, self.device), to_device(v[:n], p.dtype, self.device))
             self.pos[b, :n] = torch.from_numpy(np.ascontiguousarray(pos[:n], dtype=np.int32)).to(self.device)
             self.score[b].zero_()
             if score is not None:
@@ -262,3 +275,121 @@ class ModelBatch(LayerBatch):
 
     def attend_shared_layer(self, layer: int, shared, q, k_new=None, v_new=None, flags: int = 0, mods=None, stream=None):
         self._attend_shared(self.layer_params, *self._layer(layer, "adsa_attend_shared"), shared, q, k_new, v_new, flags, mods, stream)
+
+
+class PagedBatch(LayerBatch):
+    """A layer batch whose K and V rows lie in pages of two pools: K, V [n_pages][h][page_size][D] or, for parameters made with layout
+    "slot_major", [n_pages][page_size][h][D]; table int32 [n_seq][ceil(cap / page_size)] on the device, -1 where a sequence has no page.
+    Which page is whose is kept on the host: reserve() gives a sequence pages, release() takes them back; the device's table is brought up to
+    date by upload_table(), on the current stream.  (A caller with an allocator of its own may fill `table` and leave those alone.)
+    The calls are those of LayerBatch; several batches (the layers of a model) may share one table where all of them keep as many tokens."""
+
+    dense = False
+
+    def __init__(self, params: B.AdsaParams, n_pages: int, page_size: int = 64, device: str = "cuda:0"):
+        self.page_size, self.n_pages = page_size, n_pages
+        super().__init__(params, device)
+
+    def _allocate_caches(self) -> None:
+        p = self.params
+        shape = (self.n_pages, p.n_heads, self.page_size, p.head_dim) if self.head_major else (self.n_pages, self.page_size, p.n_heads, p.head_dim)
+        self.K = torch.zeros(shape, dtype=self.tdtype, device=self.device)
+        self.V = torch.zeros(shape, dtype=self.tdtype, device=self.device)
+        self.table_host = np.full((p.n_seq, -(-p.cap // self.page_size)), -1, dtype=np.int32)
+        self.table = torch.from_numpy(self.table_host).to(self.device)
+        self.free_pages = list(range(self.n_pages - 1, -1, -1))                # the last is taken first
+        self.pages = B.make_pages(self.K, self.V, self.table, page_size=self.page_size, layout="head_major" if self.head_major else "slot_major")
+
+    # ---- pages, on the host
+    def reserve(self, b: int, slots: int) -> None:
+        """Pages for the first `slots` slots of sequence b; nothing changes if there are not as many."""
+        row = self.table_host[b]
+        need = -(-slots // self.page_size)
+        if not 0 <= slots <= self.params.cap:
+            raise ValueError(f"slots: 0..{self.params.cap} expected, {slots} given")
+        missing = [i for i in range(need) if row[i] < 0]
+        if len(missing) > len(self.free_pages):
+            raise MemoryError(f"{len(missing)} pages wanted, {len(self.free_pages)} free")
+        for i in missing:
+            row[i] = self.free_pages.pop()
+
+    def release(self, b: int, slots: int = 0) -> None:
+        """Gives back the pages of sequence b that hold none of its first `slots` slots."""
+        row = self.table_host[b]
+        for i in range(len(row) - 1, -(-slots // self.page_size) - 1, -1):
+            if row[i] >= 0:
+                self.free_pages.append(int(row[i]))
+                row[i] = -1
+
+    def upload_table(self) -> None:
+        self.table.copy_(torch.from_numpy(self.table_host))
+
+    def _slots(self, b: int, n: int):
+        """Page and place in it of slots 0 .. n - 1 of sequence b."""
+        slot = torch.arange(n, device=self.device)
+        return self.table[b].long()[slot // self.page_size], slot % self.page_size
+
+    def _put_rows(self, b, k, v):
+        page, place = self._slots(b, len(k))
+        for pool, rows in ((self.K, k), (self.V, v)):
+            if self.head_major:
+                pool[page, :, place] = rows
+            else:
+                pool[page, place] = rows
+
+    def cache_rows(self, pool: torch.Tensor, b: int, n: int) -> torch.Tensor:
+        """[n][h][D]: the rows of slots 0 .. n - 1 of sequence b."""
+        page, place = self._slots(b, n)
+        return pool[page, :, place] if self.head_major else pool[page, place]
+
+    def k_host(self):
+        raise TypeError("a paged batch has no dense caches: cache_rows(K, sequence, slots)")
+
+    v_host = k_host
+
+    # ---- thin forwards to the C ABI
+    def attend(self, q: torch.Tensor, flags: int = 0, k_new=None, v_new=None, stream=None):
+        B.adsa_attend_paged(self.params, self.pages, self.seqs, q, self.sel_idx, self.sel_cnt, self.out, self.lse, self.workspace, flags, k_new, v_new, stream)
+
+    def compact(self, flags: int = 0, stream=None):
+        B.adsa_compact_paged(self.params, self.pages, self.seqs, self.keep_map, self.workspace, flags, stream)
+
+    def step(self, q, k_new, v_new, flags: int = 0, stream=None):
+        """One decode step: select with the append planned, attend, and unless FLAG_NO_COMPACT is given compact, the last of them advancing (streaming
+        eviction policies evict first, as adsa_step does)."""
+        streaming = self.params.evict_policy != B.EVICT_ROW_END
+        evicts = not flags & B.FLAG_NO_COMPACT
+        if streaming and evicts:
+            self.compact(0, stream)
+        self.select(B.FLAG_PLAN_APPEND, stream)
+        last = streaming or not evicts
+        self.attend(q, B.FLAG_APPEND | (flags & (B.FLAG_NEW_F32 | B.FLAG_NO_ACCUMULATE)) | (B.FLAG_ADVANCE if last else 0), k_new, v_new, stream)
+        if not last:
+            self.compact(B.FLAG_ADVANCE, stream)
+
+    def step_static(self, *args, **kw):
+        raise TypeError("adsa_step_static works on dense caches")
+
+    def append(self, tokens, rope, q, k, v, q_out, flags: int = 0, stream=None):
+        B.adsa_append_paged(self.params, self.pages, tokens, rope, self.seqs, q, k, v, q_out, flags, stream)
+
+    def prefill(self, tokens, q, out, lse, mods=None, flags: int = 0, stream=None):
+        self._with_workspace("adsa_prefill_paged", stream, lambda ws, st: B.adsa_prefill_paged(self.params, self.pages, tokens, mods, self.seqs, q, out, lse, ws, flags, st),
+                             lambda: B.adsa_prefill_paged_workspace_bytes(self.params, self.pages, tokens))
+
+    def attend_shared(self, *args, **kw):
+        raise TypeError("adsa_attend_shared works on dense caches")
+
+
+class Sampler:
+    """What a program keeps to draw tokens with: settings (see binding.make_sampling), token int32 [n_rows] (guided: [2 * n_rows], the partners'
+    behind) and logprob float32 [n_rows]."""
+
+    def __init__(self, n_rows: int, vocab: int, dtype: int, *, device: str = "cuda:0", **settings):
+        self.sampling = B.make_sampling(n_rows, vocab, dtype, **settings)
+        self.token = torch.full((n_rows * (2 if self.sampling.guided else 1),), -1, dtype=torch.int32, device=device)
+        self.logprob = torch.zeros(n_rows, dtype=torch.float32, device=device)
+
+    def sample(self, logits: torch.Tensor, uniform: torch.Tensor, seqs=None, stream=None) -> None:
+        """seqs: the records (a batch's `seqs`) whose inactive ones get no token."""
+        B.adsa_sample(self.sampling, logits, uniform, self.token, self.logprob, seqs, stream)

@@ -24,6 +24,8 @@ SEQ_CACHE_FULL, SEQ_BAD_STATE, SEQ_SEL_OVERFLOW = 1, 2, 4
 MAX_CAP = 8192
 EVICT_ROW_END, EVICT_WHEN_FULL, EVICT_REUSE_SLOT = 0, 1, 2
 MAX_AXES = 3
+MIN_PAGE = 16
+MAX_VOCAB = 1 << 18
 PAIRINGS = {"halves": 0, "neighbours": 1}
 MASK_CAUSAL, MASK_PREFIX = 0, 1
 
@@ -35,7 +37,8 @@ STATIC_SCRATCH_BYTES = 4 << 20
 
 EXPORTS = ["adsa_workspace_bytes", "adsa_workspace_init", "adsa_select", "adsa_attend", "adsa_compact", "adsa_step",
            "adsa_step_static", "adsa_rotate", "adsa_append", "adsa_prefill", "adsa_prefill_workspace_bytes", "adsa_attend_shared",
-           "adsa_shared_workspace_bytes",
+           "adsa_shared_workspace_bytes", "adsa_append_paged", "adsa_prefill_paged", "adsa_prefill_paged_workspace_bytes", "adsa_attend_paged",
+           "adsa_compact_paged", "adsa_paged_workspace_bytes", "adsa_sample",
            "adsa_profile_enable", "adsa_profile_read", "adsa_strerror", "adsa_version"]
 
 
@@ -86,6 +89,20 @@ class AdsaShared(_HostStruct):
     rows = None                    # (heads, head_dim, dtype) of the prompts' caches
     _fields_ = [("n_groups", C.c_int32), ("max_prompt", C.c_int32), ("max_members", C.c_int32), ("reserved", C.c_int32),
                 ("prompts", C.c_void_p), ("members", C.c_void_p), ("kv_slot_stride", C.c_int64), ("kv_head_stride", C.c_int64)]
+
+
+class AdsaPages(_HostStruct):
+    """Mirror of `adsa_pages` (host struct)."""
+    rows = None                    # (heads, head_dim, dtype) of the pools
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("table", C.c_void_p), ("page_stride", C.c_int64), ("slot_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("table_stride", C.c_int32), ("reserved", C.c_int32)]
+
+
+class AdsaSampling(_HostStruct):
+    """Mirror of `adsa_sampling` (host struct)."""
+    _fields_ = [("n_rows", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32), ("guided", C.c_int32), ("row_stride", C.c_int64), ("guidance", C.c_float),
+                ("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float), ("reserved", C.c_int32),
+                ("temperatures", C.c_void_p), ("top_ks", C.c_void_p), ("top_ps", C.c_void_p), ("min_ps", C.c_void_p)]
 
 
 # Mirror of `adsa_seq` (device struct array), 96 bytes per entry.
@@ -154,6 +171,21 @@ def load_library() -> C.CDLL:
         lib.adsa_attend_shared.argtypes = [pp, sp, mp, vp, vp, vp, vp, i32p, i32p, vp, f32p, C.c_uint32, vp, C.c_size_t, vp]
         lib.adsa_shared_workspace_bytes.restype = C.c_size_t
         lib.adsa_shared_workspace_bytes.argtypes = [pp, sp]
+        gp, ap = C.POINTER(AdsaPages), C.POINTER(AdsaSampling)
+        lib.adsa_append_paged.restype = C.c_int
+        lib.adsa_append_paged.argtypes = [pp, gp, tp, rp, vp, vp, vp, vp, vp, C.c_uint32, vp]
+        lib.adsa_prefill_paged.restype = C.c_int
+        lib.adsa_prefill_paged.argtypes = [pp, gp, tp, mp, vp, vp, vp, f32p, C.c_uint32, vp, C.c_size_t, vp]
+        lib.adsa_prefill_paged_workspace_bytes.restype = C.c_size_t
+        lib.adsa_prefill_paged_workspace_bytes.argtypes = [pp, gp, tp]
+        lib.adsa_attend_paged.restype = C.c_int
+        lib.adsa_attend_paged.argtypes = [pp, gp, vp, vp, vp, vp, i32p, i32p, vp, f32p, C.c_uint32, vp, C.c_size_t, vp]
+        lib.adsa_compact_paged.restype = C.c_int
+        lib.adsa_compact_paged.argtypes = [pp, gp, vp, i32p, C.c_uint32, vp, C.c_size_t, vp]
+        lib.adsa_paged_workspace_bytes.restype = C.c_size_t
+        lib.adsa_paged_workspace_bytes.argtypes = [pp]
+        lib.adsa_sample.restype = C.c_int
+        lib.adsa_sample.argtypes = [ap, vp, vp, f32p, i32p, f32p, vp]
         lib.adsa_profile_enable.restype = C.c_int
         lib.adsa_profile_enable.argtypes = [C.c_int]
         lib.adsa_profile_read.restype = C.c_int
@@ -166,12 +198,12 @@ def load_library() -> C.CDLL:
     return _lib
 
 
-_call = _call_static = _call_prompt = None       # the CPython module's functions
+_call = _call_static = _call_prompt = _call_paged = None       # the CPython module's functions
 _entry = {}                       # C entry point -> its address
 
 
 def _load_native():
-    global _call, _call_static, _call_prompt
+    global _call, _call_static, _call_prompt, _call_paged
     lib, path = load_library(), _build.NATIVE_PATH
     if not os.path.exists(path):
         raise FileNotFoundError(f"{path} is missing: run `python -m paper_2506_18226_amd.build` (or __graft_entry__.build()) first; "
@@ -180,10 +212,10 @@ def _load_native():
     module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_adsa_native", loader))
     loader.exec_module(module)
     for name in ("adsa_select", "adsa_attend", "adsa_compact", "adsa_step", "adsa_step_static", "adsa_rotate", "adsa_append", "adsa_prefill",
-                 "adsa_attend_shared"):
+                 "adsa_attend_shared", "adsa_append_paged", "adsa_prefill_paged", "adsa_attend_paged", "adsa_compact_paged", "adsa_sample"):
         _entry[name] = C.cast(getattr(lib, name), C.c_void_p).value
     module.set_params_type(AdsaParams)
-    _call_static, _call_prompt = module.call_static, module.call_prompt
+    _call_static, _call_prompt, _call_paged = module.call_static, module.call_prompt, module.call_paged
     _call = module.call
 
 
@@ -464,6 +496,115 @@ def adsa_attend_shared(params, shared, mods, seqs, q, k_new, v_new, sel_idx, sel
         raise ValueError(f"shared: prompts of (heads, head_dim, dtype) {shared.rows}, sequences of {(params.n_heads, params.head_dim, params.dtype)}")
     _prompt_call("adsa_attend_shared", params, shared, _mods(params, mods, 0), flags, stream, workspace, seqs, q,
                  k_new, v_new, sel_idx, sel_cnt, out, lse)
+
+
+# ---- caches in pages
+def make_pages(k, v, table, *, page_size, layout="head_major", dtype=None, strides=None, n_heads=None, head_dim=None, n_pages=None) -> AdsaPages:
+    """Fill `adsa_pages`: int32 table [n_seq][entries] and the pools k and v, device tensors [n_pages][heads][page_size][head_dim] (layout
+    "head_major") or [n_pages][page_size][heads][head_dim] ("slot_major"), whose last axis has no gaps and whose other strides are taken as they
+    are.  Where the pools are raw pointers, strides = (page, slot, head) in elements and n_pages say what tensors would."""
+    _expect("table", table, "int32")
+    if not isinstance(k, int):
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1 or k.dtype != v.dtype:
+            raise ValueError("k and v: pools of four axes expected, of the same shape, strides and type, and without gaps along the last")
+        heads, slots = (1, 2) if layout == "head_major" else (2, 1)
+        if k.shape[slots] != page_size:
+            raise ValueError(f"k: pages of {page_size} slots expected, {k.shape[slots]} there")
+        strides = k.stride(0), k.stride(slots), k.stride(heads)
+        n_pages, n_heads, head_dim = k.shape[0], k.shape[heads], k.shape[3]
+        dtype = {"torch.float32": F32, "torch.bfloat16": BF16}.get(str(k.dtype), -1)
+    width = table.shape[-1] if not isinstance(table, int) else None
+    if width is None:
+        raise ValueError("table: an int32 tensor expected")
+    pages = AdsaPages(_ptr(k), _ptr(v), _ptr(table), *strides, page_size, n_pages, width, 0)._hold(k, v, table, sizes=(("table", table.numel() // max(width, 1)),))
+    pages.rows = None if n_heads is None else (n_heads, head_dim, dtype)
+    return pages
+
+
+def _pages(params, pages):
+    _struct(pages, AdsaPages, "pages")
+    if pages is not None:
+        if pages.rows not in (None, (params.n_heads, params.head_dim, params.dtype)):
+            raise ValueError(f"pages: pools of (heads, head_dim, dtype) {pages.rows}, sequences of {(params.n_heads, params.head_dim, params.dtype)}")
+        _check_sizes(pages, table=params.n_seq)
+    return pages
+
+
+_PAGED_CALLS = {"adsa_append_paged": 0, "adsa_prefill_paged": 1, "adsa_attend_paged": 2, "adsa_compact_paged": 3, "adsa_sample": 4}
+
+
+def _paged_call(name, params, pages, third, fourth, flags, stream, workspace, *pointers) -> None:
+    if _call_paged is None:
+        _load_native()
+    rc = _call_paged(_PAGED_CALLS[name], _entry[name], params, pages, third, fourth, flags, _current_stream() if stream is None else _stream(stream),
+                     workspace, *pointers)
+    if rc != 0:
+        raise AdsaError(rc, name)
+
+
+def adsa_append_paged(params, pages, tokens, rope, seqs, q, k, v, q_out, flags=0, stream=None) -> None:
+    _struct(rope, AdsaRope, "rope")
+    _tokens(params, tokens)
+    _check_rope(params, rope, None if tokens is None else tokens.width)
+    _paged_call("adsa_append_paged", params, _pages(params, pages), tokens, rope, flags, stream, None, seqs, q, k, v, q_out)
+
+
+def adsa_prefill_paged_workspace_bytes(params, pages, tokens) -> int:
+    return int(load_library().adsa_prefill_paged_workspace_bytes(_host(params), _host(pages), _host(tokens)))
+
+
+def adsa_prefill_paged(params, pages, tokens, mods, seqs, q, out, lse, workspace, flags=0, stream=None) -> None:
+    _paged_call("adsa_prefill_paged", params, _pages(params, pages), _tokens(params, tokens), _mods(params, mods, params.n_seq), flags, stream, workspace,
+                seqs, q, out, lse)
+
+
+def adsa_paged_workspace_bytes(params) -> int:
+    return int(load_library().adsa_paged_workspace_bytes(_host(params)))
+
+
+def adsa_attend_paged(params, pages, seqs, q, sel_idx, sel_cnt, out, lse, workspace, flags=0, k_new=None, v_new=None, stream=None) -> None:
+    _paged_call("adsa_attend_paged", params, _pages(params, pages), None, None, flags, stream, workspace, seqs, q, k_new, v_new, sel_idx, sel_cnt, out, lse)
+
+
+def adsa_compact_paged(params, pages, seqs, keep_map, workspace, flags=0, stream=None) -> None:
+    _paged_call("adsa_compact_paged", params, _pages(params, pages), None, None, flags, stream, workspace, seqs, keep_map)
+
+
+# ---- sampling
+def make_sampling(n_rows, vocab, dtype, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, guidance=None, row_stride=0) -> AdsaSampling:
+    """Fill `adsa_sampling`.  temperature, top_k, top_p and min_p are numbers, or device tensors [n_rows] (int32 top_k, float32 the others) with one for
+    every row; guidance: None, or how far guided pairs go."""
+    one, many, sizes = {}, {}, []
+    for name, x, kind in (("temperature", temperature, "float32"), ("top_k", top_k, "int32"), ("top_p", top_p, "float32"), ("min_p", min_p, "float32")):
+        rows = hasattr(x, "data_ptr")
+        if rows:
+            _expect(name, x, kind)
+            sizes.append((name, _length(x)))
+        one[name], many[name] = (0 if rows else x), (x if rows else None)
+    s = AdsaSampling(n_rows, vocab, dtype, 0 if guidance is None else 1, row_stride, 1.0 if guidance is None else guidance, one["temperature"], one["top_k"], one["top_p"],
+                     one["min_p"], 0, *(_ptr(many[name]) for name in ("temperature", "top_k", "top_p", "min_p")))._hold(*many.values(), sizes=sizes)
+    _check_sizes(s, **{name: n_rows for name, _ in sizes})
+    return s
+
+
+def adsa_sample(sampling, logits, uniform, token, logprob=None, seqs=None, stream=None) -> None:
+    _struct(sampling, AdsaSampling, "sampling")
+    if sampling is None:
+        raise AdsaError(-1, "adsa_sample")
+    s, rows = sampling, sampling.n_rows * (2 if sampling.guided else 1)
+    if hasattr(logits, "data_ptr"):
+        kind = "float32" if s.dtype == F32 else "bfloat16"
+        last = (rows - 1) * (s.row_stride or s.vocab) + s.vocab
+        if str(logits.dtype) != f"torch.{kind}" or logits.dim() != 2 or logits.shape[0] < rows or logits.shape[1] != s.vocab or logits.stride(1) != 1 or (
+                rows > 1 and logits.stride(0) != (s.row_stride or s.vocab)):
+            raise ValueError(f"logits: {kind} [{rows}][{s.vocab}] expected, rows {s.row_stride or s.vocab} elements apart ({last} of them in all)")
+    for name, x, kind, least in (("uniform", uniform, "float32", s.n_rows), ("token", token, "int32", rows), ("logprob", logprob, "float32", s.n_rows)):
+        _expect(name, x, kind)
+        if _length(x) is not None and x.numel() < least:
+            raise ValueError(f"{name}: {least} expected, {x.numel()} there")
+    if hasattr(seqs, "data_ptr") and _nbytes(seqs) < rows * SEQ_DTYPE.itemsize:
+        raise ValueError(f"seqs: {rows} records expected")
+    _paged_call("adsa_sample", s, None, None, None, 0, stream, None, seqs, logits, uniform, token, logprob)
 
 
 def adsa_profile_enable(on: bool) -> None:

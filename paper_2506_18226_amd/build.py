@@ -11,7 +11,7 @@ LIB_DIR = os.path.join(_HERE, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libadsa_hip.so")
 NATIVE_PATH = os.path.join(LIB_DIR, "_adsa_native.so")       # CPython side of binding.py
 CEILING_PATH = os.path.join(LIB_DIR, "read_ceiling")
-SOURCES = ["api.hip", "select_compact.hip", "attend.hip", "attend_gqa.hip", "vcos.hip", "prompt_api.hip", "rotary.hip", "prompt.hip"]
+SOURCES = ["api.hip", "select_compact.hip", "attend.hip", "attend_gqa.hip", "vcos.hip", "prompt_api.hip", "rotary.hip", "prompt.hip", "prompt_paged.hip", "paged_api.hip", "sample.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

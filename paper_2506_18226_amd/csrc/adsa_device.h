@@ -56,6 +56,29 @@ struct SlotList {
   __device__ __forceinline__ int operator[](int i) const { return (int)__builtin_amdgcn_raw_buffer_load_b32(row, i * 4, 0, 0); }
 };
 
+// One sequence's row of a page table in LDS, in units (see PageArgs): where each page begins, -1 where an entry is no page.
+// Loads leave at once (entries); put() says whether the thread's entries of the first `need` are pages.
+template <int THREADS>
+struct PageEntries {
+  static constexpr int N = kMostEntries / THREADS > 1 ? kMostEntries / THREADS : 1;
+  int entry[N];
+  __device__ __forceinline__ PageEntries(const SlotList& row) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) entry[k] = row[threadIdx.x + k * THREADS];
+  }
+  __device__ __forceinline__ bool put(int* units, int n_pages, uint32_t page_units, int need) const {
+    bool good = true;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int i = threadIdx.x + k * THREADS;
+      const bool page = (uint32_t)entry[k] < (uint32_t)n_pages;
+      if (i < kMostEntries) units[i] = page ? (int)((uint32_t)entry[k] * page_units) : -1;
+      good &= page || i >= need;
+    }
+    return good;
+  }
+};
+
 // Rows of a cache within 32-bit offsets of a uniform address: 16-byte streaming loads that read zeros, without an access, at any
 // offset from kRowBufferBytes on.  ~(slot + ADSA_MAX_CAP), as an unsigned number, is such an offset for every slot of a cache, and the
 // 16 bytes from there on don't reach the end of the 32 bits.

@@ -171,6 +171,39 @@ hipError_t launch_attend_shared(const adsa_params& p, const adsa_shared& s, cons
                                 const SharedWorkspace& w, bool accumulate, bool append, bool advance, bool new_f32, hipStream_t st);
 hipError_t prompt_prepare_kernels();
 
+// ---- caches in pages (paged_api.hip checks; the kernels are those of the dense caches with another way from a slot to its row)
+// A row's place in a pool is a 31-bit number of units from the pool's first byte, so that a staged list entry holds it whole.
+struct PageArgs {
+  const int32_t* table;
+  char* k;
+  char* v;
+  long long page_stride_b, slot_stride_b, head_stride_b;
+  int n_pages, shift, table_stride, unit_shift;      // page_size = 1 << shift; a unit is 1 << unit_shift bytes
+  uint32_t page_units, slot_units;
+};
+constexpr int kMostEntries = ADSA_MAX_CAP / ADSA_MIN_PAGE;       // of a table's row that a sequence can use
+
+hipError_t launch_append_paged(const adsa_params& p, const PageArgs& pages, const adsa_tokens& t, const adsa_rope* rope, adsa_seq* seqs, const void* q,
+                               const void* k, const void* v, void* q_out, bool in_f32, bool advance, hipStream_t st);
+hipError_t launch_prefill_paged(const adsa_params& p, const PageArgs& pages, const adsa_tokens& t, const adsa_mods& mods, const PromptPlan& plan, adsa_seq* seqs,
+                                const void* q, void* out, float* lse, char* ws, const PromptWorkspace& w, bool accumulate, bool advance, bool split,
+                                hipStream_t st);
+hipError_t paged_prompt_prepare_kernels();
+hipError_t launch_attend_paged(const adsa_params& p, const PageArgs& pages, const AttendPlan& plan, adsa_seq* seqs, const void* q, const void* k_new,
+                               const void* v_new, const int32_t* sel_idx, const int32_t* sel_cnt, void* out, float* lse, char* ws, const Workspace& w,
+                               bool accumulate, bool append, int advance, bool new_f32, hipStream_t st);
+hipError_t launch_attend_gqa_paged(const adsa_params& p, const PageArgs& pages, const AttendPlan& plan, adsa_seq* seqs, const void* q, const void* k_new,
+                                   const void* v_new, const int32_t* sel_idx, const int32_t* sel_cnt, void* out, float* lse, char* ws, const Workspace& w,
+                                   bool accumulate, bool append, int advance, bool new_f32, hipStream_t st);
+hipError_t launch_compact_paged(const adsa_params& p, const PageArgs& pages, adsa_seq* seqs, int32_t* keep_map, char* ws, const Workspace& w, bool advance_step,
+                                hipStream_t st);
+
+// ---- sampling (sample.hip)
+hipError_t launch_sample(const adsa_sampling& s, const adsa_seq* seqs, const void* logits, const float* uniform, int32_t* token, float* logprob, hipStream_t st);
+
+// What a paged call runs with: parameters with the strides of a dense cache (nobody reads them as strides), and the pools (paged_api.hip).
+int resolve_paged(const adsa_params* p, const adsa_pages* pages, adsa_params* eff, PageArgs* args);
+
 }  // namespace adsa
 
 // What the launch rules decide for parameters p, for tests that have to know which way a call goes (host only; not in adsa.h).

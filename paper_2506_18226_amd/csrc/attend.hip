@@ -176,6 +176,18 @@ __device__ __forceinline__ void plan_row_end(RankShared& sh, ADSA_GLOBAL adsa_se
   }
 }
 
+// The same for a launch over caches in pages (PAGED): two blocks, one dword per lane of a 32-lane half.
+struct PagedTail {
+  AttendTail a;
+  char* k;
+  char* v;
+  long long head_stride_b;
+  uint32_t page_units, slot_units;      // see PageArgs
+  int n_pages, unit_shift;
+  int unused[6];
+};
+static_assert(sizeof(PagedTail) == 128 && offsetof(PagedTail, k) == 64, "one dword per lane of a 32-lane half");
+
 // DIRECT: the list of a (sequence, head) is not split (grid.x == 1): the workgroup finishes its heads alone.
 // The build asks for leading kernel arguments to be preloaded into scalar registers at wave launch, and 14 dwords of them are.
 // Everything up to the sums is in those 14 (addresses have 48 bits, so six of them take 9 dwords): the first round trip is then
@@ -195,11 +207,14 @@ __device__ __forceinline__ void plan_row_end(RankShared& sh, ADSA_GLOBAL adsa_se
 // nobody waits.  A score's store and load with scope agent meet behind the L2s; the store has been acknowledged (vmcnt) before the ticket is
 // drawn, and the loads leave after the last ticket has come back, so no cache is written back or invalidated for it.
 // The record's step stays, since workgroups that start later tell a row end from it: the next kernel advances it.
-template <int EB, int D, int HT, int U, int NW, bool VF, bool DIRECT, bool WIDE, int RANK = 0, int PLAN = 0>
+// PAGED: rows lie in pages.  The sequence's row of the table goes to LDS with the first trip, and the staged list holds, instead of slots, where their
+// rows begin in the pool (in units: see PageArgs), so the loop looks nothing up; rows are reached with 64-bit addresses and masked as with WIDE.  The arguments
+// stride24 and head_stride16 are the table's address and the entries of a row, the head stride's bits of heads_flags the page size.
+template <int EB, int D, int HT, int U, int NW, bool VF, bool DIRECT, bool WIDE, int RANK = 0, int PLAN = 0, bool PAGED = false>
 __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_t idx_lo, uint32_t cnt_lo, uint32_t q_lo, uint32_t kn_lo,
                                                       uint32_t vn_lo, uint32_t seqs_idx_hi, uint32_t cnt_q_hi, uint32_t kn_vn_hi,
                                                       uint32_t heads_flags, uint32_t caps, uint32_t stride24, uint32_t head_stride16,
-                                                      float scale_log2, std::conditional_t<(RANK > 0), RankTail, std::conditional_t<(PLAN > 0), PlanTail, AttendTail>> T) {
+                                                      float scale_log2, std::conditional_t<PAGED, PagedTail, std::conditional_t<(RANK > 0), RankTail, std::conditional_t<(PLAN > 0), PlanTail, AttendTail>>> T) {
   constexpr int kAttThreads = NW * kWave;           // the waves of the workgroup share one token chunk
   constexpr int EPL = Elems<EB>::N;                 // elements per lane
   constexpr int LPR = D / EPL;                      // lanes per row
@@ -207,6 +222,8 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
   static_assert(HT == 1 || (DIRECT && !VF && RPW * HT * LPR == kWave), "several heads: whole lists only");
   static_assert(RANK == 0 || (HT == 1 && DIRECT && !VF && !WIDE), "ranking: whole lists of one head");
   static_assert(PLAN == 0 || (RANK == 0 && HT == 1 && DIRECT && !VF && !WIDE), "plans: whole lists of one head");
+  static_assert(!PAGED || (RANK == 0 && PLAN == 0 && HT == 1 && !VF && !WIDE), "pages: one head, a list that is there");
+  constexpr bool MASKED = WIDE || PAGED;            // what is not attended reads some row, and is masked when it is folded
   constexpr int kSlots = RANK > 0 ? RANK : 1;       // slots per thread of the ranking
   constexpr int PF = 4;                             // list entries a thread fetches, and score read-modify-writes it starts, early
   constexpr int kRev = NW * U * RPW;                // tokens of one ring revolution of the workgroup
@@ -244,7 +261,7 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
   const gint* const pos = RANK > 0 ? (const gint*)sqp->pos : nullptr;
   const BudgetOf budget(*sqp);
   const int n_keep_prefix = RANK > 0 ? sqp->n_keep_prefix : 0;
-  int n_res = RANK > 0 ? sqp->n_res : 0;
+  int n_res = RANK > 0 || PAGED ? sqp->n_res : 0;
   gfloat* const u_state = VF ? (gfloat*)sqp->vcos_u : nullptr;
   __builtin_amdgcn_sched_barrier(0);                // (the scalar loads leave first: the rows need them and the first slots)
   const gint* const idx_row = (const gint*)address(idx_lo, seqs_idx_hi >> 16) + (size_t)b * sel_cap;
@@ -259,12 +276,19 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
   const int unit0 = wave * RPW + ts;                // this lane's token of the wave's first unit
   uint32_t tail = 0u;                               // lane i (modulo 16): dword i of T
   auto load_tail = [&] {
-    tail = ((const ADSA_GLOBAL uint32_t*)((const char __attribute__((address_space(4)))*)__builtin_amdgcn_kernarg_segment_ptr() + kLeadBytes))[lane % 16];
+    tail = ((const ADSA_GLOBAL uint32_t*)((const char __attribute__((address_space(4)))*)__builtin_amdgcn_kernarg_segment_ptr() + kLeadBytes))[lane % (PAGED ? 32 : 16)];
   };
   auto tail_word = [&](int i) { return (uint32_t)__builtin_amdgcn_readlane((int)tail, i); };
   auto tail_address = [&](size_t at) { return address(tail_word(at / 4), tail_word(at / 4 + 1)); };
-  if constexpr (RANK > 0) load_tail();
-  else if constexpr (DIRECT) {
+  if constexpr (RANK > 0 || PAGED) load_tail();
+  const int page_shift = PAGED ? (int)(heads_flags >> 19 & 0x1F) : 0, table_stride = PAGED ? (int)(head_stride16 >> 16) : 0;
+  std::conditional_t<PAGED, PageEntries<kAttThreads>, int> page_entries = [&] {
+    if constexpr (PAGED) {
+      const gint* const table = (const gint*)address(stride24, head_stride16 & 0xFFFF) + (size_t)b * table_stride;
+      return PageEntries<kAttThreads>(SlotList(table, min(table_stride, kMostEntries)));
+    } else return 0;
+  }();
+  if constexpr (RANK == 0 && DIRECT) {
 #pragma unroll
     for (int u = 0; u < U; ++u) slot_a[u] = list[unit0 + u * NW * RPW];
     __builtin_amdgcn_sched_barrier(0);
@@ -284,7 +308,10 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
     if constexpr (EB == 2)
       if (new_f32) { nk[1] = load16(k_new_g + 16); nv[1] = load16(v_new_g + 16); }
   }
-  pin_uniform(cnt); pin_uniform(k_base); pin_uniform(v_base); pin_uniform(score); pin_uniform(pending);
+  pin_uniform(cnt);
+  if constexpr (PAGED) pin_uniform(n_res);
+  else { pin_uniform(k_base); pin_uniform(v_base); }
+  pin_uniform(score); pin_uniform(pending);
   if constexpr (VF) pin_uniform(u_state);
 
   cnt = min(cnt, sel_cap);
@@ -373,18 +400,48 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
       if (!active || reject != 0) sqp->pending_slot = -1;
     }
   }
+  const auto& block = [&]() -> const auto& {        // the first block of the tail
+    if constexpr (PAGED) return T.a;
+    else return T;
+  }();
   if (cnt <= 0) {                                   // inactive or rejected sequence: zero-filled row
     if (chunk == 0) {
       const size_t row = (size_t)b * n_heads + head0;
       for (int o = tid; o < heads_here * D; o += kAttThreads) {
-        if (EB == 4) ((gfloat*)T.out)[row * D + o] = 0.0f;
-        else ((ADSA_GLOBAL uint16_t*)T.out)[row * D + o] = 0;
-        if (o % D == 0) ((gfloat*)T.lse)[row + o / D] = 0.0f;
+        if (EB == 4) ((gfloat*)block.out)[row * D + o] = 0.0f;
+        else ((ADSA_GLOBAL uint16_t*)block.out)[row * D + o] = 0;
+        if (o % D == 0) ((gfloat*)block.lse)[row + o / D] = 0.0f;
       }
       if constexpr (RANK == 0)
-        if (head0 == 0 && tid == 0) advance_empty(sqp, T.advance);
+        if (head0 == 0 && tid == 0) advance_empty(sqp, block.advance);
     }
     return;
+  }
+  __shared__ int s_units[PAGED ? kMostEntries : 1];
+  __shared__ int s_good[NW];
+  int last_slot = cap - 1;
+  if constexpr (PAGED) {
+    const int need = n_res >= 1 && n_res <= cap ? ((n_res - 1) >> page_shift) + 1 : kMostEntries + 1;      // (a count that cannot be is no good either)
+    const bool good = page_entries.put(s_units, (int)tail_word(offsetof(PagedTail, n_pages) / 4), tail_word(offsetof(PagedTail, page_units) / 4), need);
+    const bool wave_good = __ballot(!good) == 0 && need <= kMostEntries;
+    if (lane == 0) s_good[wave] = wave_good;
+    __syncthreads();
+    bool all = true;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) all &= s_good[w] != 0;
+    last_slot = n_res - 1;
+    if (!all) {                                     // (every workgroup of the sequence finds the same)
+      if (chunk == 0) {
+        const size_t row = (size_t)b * n_heads + head0;
+        for (int o = tid; o < D; o += kAttThreads) {
+          if (EB == 4) ((gfloat*)tail_address(offsetof(AttendTail, out)))[row * D + o] = 0.0f;
+          else ((ADSA_GLOBAL uint16_t*)tail_address(offsetof(AttendTail, out)))[row * D + o] = 0;
+        }
+        if (tid == 0) ((gfloat*)tail_address(offsetof(AttendTail, lse)))[row] = 0.0f;
+        if (head0 == 0 && tid == 0) sqp->status = sqp->status | ADSA_SEQ_BAD_STATE;
+      }
+      return;
+    }
   }
   const int t_begin = DIRECT ? 0 : chunk_begin(cnt, chunk, n_chunks);
   const int t_end = DIRECT ? cnt : chunk_begin(cnt, chunk + 1, n_chunks);
@@ -401,15 +458,24 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
     for (int k = 0; k < PF; ++k) pf_slot[k] = list[t_begin + tid + k * kAttThreads];
   }
   // the slot adsa_select reserved for the query token (Section 4.2 append), if this launch fills it
-  const int new_slot = (append && pending < cap) ? pending : -1;
+  const int new_slot = (append && pending <= last_slot) ? pending : -1;
+  // PAGED: where a slot's row begins in its pool
+  const uint32_t slot_units = PAGED ? tail_word(offsetof(PagedTail, slot_units) / 4) : 0u;
+  const int unit_shift = PAGED ? (int)tail_word(offsetof(PagedTail, unit_shift) / 4) : 0;
+  auto units_of = [&](int slot) {
+    if constexpr (PAGED) return s_units[slot >> page_shift] + (int)__umul24((uint32_t)slot & ((1u << page_shift) - 1u), slot_units);
+    else return slot;
+  };
 
   const Elems<EB> qv(qr, scale_log2);
   long long stride_b = (long long)stride24;
-  if constexpr (WIDE) stride_b = T.slot_stride_b;
-  const long long head_stride_b = (long long)address(head_stride16, (heads_flags >> 19) & 0x1F) * 16;
+  if constexpr (WIDE) stride_b = block.slot_stride_b;
+  const long long head_stride_b = PAGED ? (long long)tail_address(offsetof(PagedTail, head_stride_b)) : (long long)address(head_stride16, (heads_flags >> 19) & 0x1F) * 16;
   const long long lane_off = (long long)head * head_stride_b + dl * 16;
-  gchar* const kb = k_base + lane_off;
-  gchar* const vb = v_base + lane_off;
+  gchar *kb = k_base, *vb = v_base;
+  if constexpr (PAGED) { kb = (gchar*)tail_address(offsetof(PagedTail, k)); vb = (gchar*)tail_address(offsetof(PagedTail, v)); }
+  kb += lane_off;
+  vb += lane_off;
   // VF: this lane's columns of u for its head, and the two score rows of the head
   float uf[EPL];
   gfloat* vrows = nullptr;
@@ -454,10 +520,15 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
     const RowBuffer ku(k_base + (long long)head0 * head_stride_b), vu(v_base + (long long)head0 * head_stride_b);       // uniform
     const uint32_t lane32 = (uint32_t)(head - head0) * (uint32_t)head_stride_b + (uint32_t)dl * 16u;
     auto load = [&](const RowBuffer& rows, const gchar* own, int e) -> uint4 {
-      if constexpr (!WIDE) return rows[max(__umul24((uint32_t)e, stride24) + lane32, (uint32_t)e)];
+      if constexpr (PAGED) return load_stream16(own + ((uint64_t)(uint32_t)max(e, 0) << unit_shift));
+      else if constexpr (!WIDE) return rows[max(__umul24((uint32_t)e, stride24) + lane32, (uint32_t)e)];
       else return load_stream16(own + (long long)max(e, 0) * stride_b);
     };
-    auto entry = [&](int j, int slot) { return list_entry(slot, j < len && slot != new_slot); };
+    auto entry = [&](int j, int slot) {
+      const bool attended = j < len && slot != new_slot;
+      if constexpr (PAGED) return attended ? units_of(slot) : -1;
+      else return list_entry(slot, attended);
+    };
     if constexpr (RANK > 0) {                      // the list is in LDS already, but for the entries of no token
       for (int j = cnt + tid; j < n_ent; j += kAttThreads) s_ent[j] = list_entry(0, false);
       __syncthreads();
@@ -469,7 +540,7 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
     for (int u = 0; u < U; u += 2) {
 #pragma unroll
       for (int i = u; i < u + 2; ++i) {
-        ent[i] = RANK > 0 ? slot_a[i] : entry(unit0 + i * NW * RPW, clamp_slot(slot_a[i], cap - 1));
+        ent[i] = RANK > 0 ? slot_a[i] : entry(unit0 + i * NW * RPW, clamp_slot(slot_a[i], last_slot));
       }
       kr[u] = load(ku, kb, ent[u]);
       kr[u + 1] = load(ku, kb, ent[u + 1]);
@@ -480,7 +551,7 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
     }
     // ... and while these rows are on their way the chunk's slot list goes to LDS
     if constexpr (RANK == 0) {
-      load_tail();
+      if constexpr (!PAGED) load_tail();
       int new_at = 0;                               // 1 + list position of the query token's slot, if this thread stages it
       auto stage = [&](int j, int slot) {
         s_ent[j] = entry(j, slot);
@@ -490,10 +561,10 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
       for (int k = 0; k < PF; ++k)
         if (k * kAttThreads < n_ent) {                // (uniform; n_ent is a multiple of the revolution, not of the threads)
           const int j = tid + k * kAttThreads;
-          pf_slot[k] = clamp_slot(pf_slot[k], cap - 1);
+          pf_slot[k] = clamp_slot(pf_slot[k], last_slot);
           if (j < n_ent) stage(j, pf_slot[k]);
         }
-      for (int j = tid + PF * kAttThreads; j < n_ent; j += kAttThreads) stage(j, clamp_slot(list[t_begin + j], cap - 1));
+      for (int j = tid + PF * kAttThreads; j < n_ent; j += kAttThreads) stage(j, clamp_slot(list[t_begin + j], last_slot));
       if (new_slot >= 0) {                          // (uniform)
         const unsigned long long who = __ballot(new_at != 0);
         const int at = who ? __builtin_amdgcn_readlane(new_at, __ffsll((long long)who) - 1) : 0;
@@ -527,7 +598,7 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
       }
       const bool mine = ts == 0;
       if (mine && hs < heads_here && chunk == n_chunks - 1) {
-        const long long off = (long long)new_slot * stride_b;
+        const long long off = PAGED ? (long long)((uint64_t)(uint32_t)units_of(new_slot) << unit_shift) : (long long)new_slot * stride_b;
         store16(kb + off, nk[0]);
         store16(vb + off, nv[0]);
       }
@@ -580,7 +651,7 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
       m = m_new;
       l = fmaf(l, corr, pa + pb);
       uint4 xa = vr[u], xb = vr[u + 1];
-      if constexpr (WIDE) {                         // (what a masked entry read may be anything: 0 times it need not be 0)
+      if constexpr (MASKED) {                       // (what a masked entry read may be anything: 0 times it need not be 0)
         xa = make_uint4(on_a ? xa.x : 0u, on_a ? xa.y : 0u, on_a ? xa.z : 0u, on_a ? xa.w : 0u);
         xb = make_uint4(on_b ? xb.x : 0u, on_b ? xb.y : 0u, on_b ? xb.z : 0u, on_b ? xb.w : 0u);
       }
@@ -815,7 +886,8 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
         int slot[B];
 #pragma unroll
         for (int k = 0; k < B; ++k) {
-          slot[k] = slot_of(s_ent[min(i0 + k * kAttThreads, len - 1)]);
+          const int j = min(i0 + k * kAttThreads, len - 1);
+          slot[k] = PAGED ? clamp_slot(list[j], last_slot) : slot_of(s_ent[j]);
           old[k] = srow[slot[k]];
         }
 #pragma unroll
@@ -868,7 +940,8 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
 // normaliser from the chunks' (m, l), in chunk order; slice 0 merges the partial outputs and writes out / lse; every
 // slice adds the probabilities of its kFinishTokens tokens to the head's score row.
 constexpr int kFinishThreads = 256, kFinishTokens = 4 * kFinishThreads;
-template <int EB, int D>
+// (PAGED: a sequence whose pages were not in order has its zeros already.)
+template <int EB, int D, bool PAGED = false>
 __global__ __launch_bounds__(kFinishThreads) void k_attend_finish(
     uint32_t seqs_lo, uint32_t idx_lo, uint32_t cnt_lo, uint32_t out_lo, uint32_t lse_lo, uint32_t lg_lo, uint32_t ml_lo, uint32_t acc_lo,
     uint32_t seqs_idx_hi, uint32_t cnt_out_hi, uint32_t lse_lg_hi, uint32_t ml_acc_hi, uint32_t caps, uint32_t flags) {
@@ -879,7 +952,8 @@ __global__ __launch_bounds__(kFinishThreads) void k_attend_finish(
   const int cnt = min(((const gint*)address(cnt_lo, cnt_out_hi & 0xFFFF))[b], sel_cap);
   gfloat* const score = (gfloat*)sqp->score;
   gfloat* const u_state = vcos_fused ? (gfloat*)sqp->vcos_u : nullptr;
-  if (cnt <= 0 || slice * kFinishTokens >= cnt) return;      // (inactive sequences: zero rows, already written)
+  const int status = PAGED ? sqp->status : 0;
+  if (cnt <= 0 || slice * kFinishTokens >= cnt || status != 0) return;       // (inactive sequences: zero rows, already written)
   const size_t row = (size_t)b * n_heads + head;
   const gfloat* const ml = (const gfloat*)address(ml_lo, ml_acc_hi & 0xFFFF) + row * n_chunks * 2;
   const gfloat* const acc = (const gfloat*)address(acc_lo, ml_acc_hi >> 16) + row * n_chunks * D;
@@ -984,6 +1058,30 @@ hipError_t launch_attend_w(const AttendArgs& A, const AttendPlan& plan, int n_se
       finish([&](auto... args) { hipExtLaunchKernelGGL((k_attend_finish<EB, D>), fgrid, dim3(kFinishThreads), 0, st, nullptr, ev_stop, 0, args...); });
     else
       finish([&](auto... args) { hipLaunchKernelGGL((k_attend_finish<EB, D>), fgrid, dim3(kFinishThreads), 0, st, args...); });
+  }
+  return hipGetLastError();
+}
+
+// The same over pages, one head a workgroup.
+template <int EB, int D, int NW, bool DIRECT>
+hipError_t launch_paged_w(const AttendArgs& A, const PageArgs& pages, const AttendPlan& plan, int n_seq, hipStream_t st) {
+  constexpr int U = 4, kRev = NW * U * (kWave * 16 / (D * EB));
+  const size_t entries = (size_t)((plan.chunk_max - 1 + kRev - 1) / kRev + 1) * kRev, lds = 2 * entries * sizeof(float);
+  const uint32_t flags = A.n_heads | (A.append ? 0x10000 : 0) | (A.new_f32 ? 0x20000 : 0) | (A.accumulate ? 0x40000 : 0) | (uint32_t)pages.shift << 19 | plan.n_chunks << 24;
+  const PagedTail T = {{A.out, A.lse, A.logits, A.part_ml, A.part_acc, A.lg_stride, A.advance, 0, 0}, pages.k, pages.v, pages.head_stride_b, pages.page_units, pages.slot_units,
+                       pages.n_pages, pages.unit_shift, {}};
+  const uint32_t table_hi = (uint32_t)(reinterpret_cast<uintptr_t>(pages.table) >> 32 & 0xFFFF) | (uint32_t)pages.table_stride << 16;
+  hipLaunchKernelGGL((k_attend<EB, D, 1, U, NW, false, DIRECT, false, 0, 0, true>), dim3(plan.n_chunks, A.n_heads, n_seq), dim3(NW * kWave), lds, st, lo32(A.seqs), lo32(A.sel_idx),
+                     lo32(A.sel_cnt), lo32(A.q), lo32(A.k_new), lo32(A.v_new), hi16s(A.seqs, A.sel_idx), hi16s(A.sel_cnt, A.q), hi16s(A.k_new, A.v_new), flags,
+                     (uint32_t)A.cap | (uint32_t)A.sel_cap << 16, lo32(pages.table), table_hi, A.scale_log2, T);
+  if constexpr (!DIRECT) {
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const dim3 fgrid(A.accumulate ? (A.sel_cap + kFinishTokens - 1) / kFinishTokens : 1, A.n_heads, n_seq);
+    const uint32_t fflags = A.n_heads | (A.accumulate ? 0x10000 : 0) | (uint32_t)A.advance << 18 | plan.n_chunks << 24;
+    hipLaunchKernelGGL((k_attend_finish<EB, D, true>), fgrid, dim3(kFinishThreads), 0, st, lo32(A.seqs), lo32(A.sel_idx), lo32(A.sel_cnt), lo32(A.out), lo32(A.lse), lo32(A.logits),
+                       lo32(A.part_ml), lo32(A.part_acc), hi16s(A.seqs, A.sel_idx), hi16s(A.sel_cnt, A.out), hi16s(A.lse, A.logits), hi16s(A.part_ml, A.part_acc),
+                       (uint32_t)A.cap | (uint32_t)A.sel_cap << 16, fflags);
   }
   return hipGetLastError();
 }
@@ -1242,6 +1340,26 @@ hipError_t launch_attend(const adsa_params& p, const AttendPlan& plan, adsa_seq*
   if (key == 4064) return launch_attend_t<4, 64>(A, plan, p.n_seq, st, ev_start, ev_stop);
   if (key == 4128) return launch_attend_t<4, 128>(A, plan, p.n_seq, st, ev_start, ev_stop);
   return hipErrorInvalidValue;
+}
+
+hipError_t launch_attend_paged(const adsa_params& p, const PageArgs& pages, const AttendPlan& plan, adsa_seq* seqs, const void* q, const void* k_new,
+                               const void* v_new, const int32_t* sel_idx, const int32_t* sel_cnt, void* out, float* lse, char* ws, const Workspace& w,
+                               bool accumulate, bool append, int advance, bool new_f32, hipStream_t st) {
+  if (p.q_per_kv > 1) return launch_attend_gqa_paged(p, pages, plan, seqs, q, k_new, v_new, sel_idx, sel_cnt, out, lse, ws, w, accumulate, append, advance, new_f32, st);
+  const AttendArgs A = attend_args(p, plan, seqs, q, k_new, v_new, sel_idx, sel_cnt, out, lse, ws, w, accumulate, append, advance, new_f32);
+  auto go = [&](auto eb, auto d) {
+    constexpr int EB = decltype(eb)::value, D = decltype(d)::value;
+    if (plan.n_chunks > 1) return launch_paged_w<EB, D, 8, false>(A, pages, plan, p.n_seq, st);
+    if (plan.waves == 8) return launch_paged_w<EB, D, 8, true>(A, pages, plan, p.n_seq, st);
+    return launch_paged_w<EB, D, 4, true>(A, pages, plan, p.n_seq, st);
+  };
+  using std::integral_constant;
+  const integral_constant<int, 2> bf16;
+  const integral_constant<int, 4> f32;
+  const integral_constant<int, 64> narrow;
+  const integral_constant<int, 128> broad;
+  if (p.dtype == ADSA_BF16) return p.head_dim == 64 ? go(bf16, narrow) : go(bf16, broad);
+  return p.head_dim == 64 ? go(f32, narrow) : go(f32, broad);
 }
 
 // Whether adsa_step's ranking, attention and eviction are two launches (k_attend with RANK, k_step_finish) instead of three.  The

@@ -119,6 +119,18 @@ struct GqaTail {
 };
 static_assert(sizeof(GqaTail) == 64, "one dword per lane of a 16-lane row");
 
+// The same for a launch over caches in pages (PAGED): two blocks, one dword per lane of a 32-lane half.
+struct PagedGqaTail {
+  GqaTail a;
+  char* k;
+  char* v;
+  long long head_stride_b;
+  uint32_t page_units, slot_units;      // see PageArgs
+  int n_pages, unit_shift;
+  int unused[6];
+};
+static_assert(sizeof(PagedGqaTail) == 128 && offsetof(PagedGqaTail, k) == 64, "one dword per lane of a 32-lane half");
+
 // Everything up to the sums is in the 14 dwords of leading arguments that are preloaded into scalar registers at wave launch (see
 // k_attend): heads_flags: heads | G << 9 | append << 16 | fp32 rows << 17 | accumulate << 18 | upper 5 bits of the head stride << 19
 // | chunks << 24;  caps: cap | sel_cap << 16.
@@ -126,11 +138,14 @@ static_assert(sizeof(GqaTail) == 64, "one dword per lane of a 16-lane row");
 // each; every workgroup leaves a partial and its logits in the workspace and k_gqa_finish merges them in chunk order.
 // R: tiles in flight per wave (a ring: the oldest is multiplied, then refilled).
 // (held to the 128 registers that let two 8-wave workgroups share a CU, but for the deep rings)
-template <int D, int NW, bool SPLIT, int R>
+// PAGED: rows lie in pages.  The sequence's row of the table goes to LDS with the first trip, and the staged list holds, instead of slots, where their
+// rows begin in the pool (in units: see PageArgs).  The arguments stride32 and head_stride16 are the table's address and the entries of a row,
+// the head stride's bits of heads_flags the page size.
+template <int D, int NW, bool SPLIT, int R, bool PAGED = false>
 __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(uint32_t seqs_lo, uint32_t idx_lo, uint32_t cnt_lo, uint32_t q_lo,
                                                           uint32_t kn_lo, uint32_t vn_lo, uint32_t seqs_idx_hi, uint32_t cnt_q_hi,
                                                           uint32_t kn_vn_hi, uint32_t heads_flags, uint32_t caps, uint32_t stride32,
-                                                          uint32_t head_stride16, float scale_log2, GqaTail T) {
+                                                          uint32_t head_stride16, float scale_log2, std::conditional_t<PAGED, PagedGqaTail, GqaTail> T) {
   constexpr int kThreads = NW * kWave;
   constexpr int ROWB = D * 2 + 16;          // bytes of a staged K row (padded against bank conflicts)
   constexpr int LPR = D / 8;                // lanes per K row with 16-byte loads
@@ -161,7 +176,7 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
   gchar* const k_rec = (gchar*)sqp->k;
   gchar* const v_rec = (gchar*)sqp->v;
   gfloat* const score_rec = (gfloat*)sqp->score;
-  const int pending = sqp->pending_slot;
+  const int pending = sqp->pending_slot, n_res = PAGED ? sqp->n_res : 0;
   __builtin_amdgcn_sched_barrier(0);                       // (the scalar loads leave first)
   const gint* const idx = (const gint*)address(idx_lo, seqs_idx_hi >> 16) + (size_t)b * sel_cap;
   const SlotList list(idx, sel_cap);
@@ -177,6 +192,20 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
   const int ld_row = lane / LPR, ld_piece = lane - ld_row * LPR;
   const int first_at = (wave + kg * NW) * 16 + r;            // list position of this lane's token
   int slot_first = 0, pf_slot[PF];
+  uint32_t tail = 0u;                                // lane i (modulo 16; PAGED: 32): dword i of T
+  auto load_tail = [&] {
+    tail = ((const ADSA_GLOBAL uint32_t*)((const char __attribute__((address_space(4)))*)__builtin_amdgcn_kernarg_segment_ptr() + kLeadBytes))[lane % (PAGED ? 32 : 16)];
+  };
+  auto tail_word = [&](int i) { return (uint32_t)__builtin_amdgcn_readlane((int)tail, i); };
+  auto tail_address = [&](size_t at) { return address(tail_word(at / 4), tail_word(at / 4 + 1)); };
+  const int page_shift = PAGED ? (int)(heads_flags >> 19 & 0x1F) : 0, table_stride = PAGED ? (int)(head_stride16 >> 16) : 0;
+  if constexpr (PAGED) load_tail();
+  std::conditional_t<PAGED, PageEntries<kThreads>, int> page_entries = [&] {
+    if constexpr (PAGED) {
+      const gint* const table = (const gint*)address(stride32, head_stride16 & 0xFFFF) + (size_t)b * table_stride;
+      return PageEntries<kThreads>(SlotList(table, min(table_stride, kMostEntries)));
+    } else return 0;
+  }();
   if constexpr (!SPLIT) {
     slot_first = list[first_at];
 #pragma unroll
@@ -207,23 +236,53 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
       vload<VW, false>(vn + new_row * 2 + r * (EV * 2), nv);
     }
   }
-  pin_uniform(cnt_raw); pin_uniform(k_rec); pin_uniform(v_rec); pin_uniform(score_rec); pin_uniform(pending);
-  const long long head_stride_b = (long long)address(head_stride16, (heads_flags >> 19) & 0x1F) * 16;
-  gchar* const k_base = k_rec + hk * head_stride_b;
-  gchar* const v_base = v_rec + hk * head_stride_b;
+  pin_uniform(cnt_raw);
+  if constexpr (PAGED) pin_uniform(n_res);
+  else { pin_uniform(k_rec); pin_uniform(v_rec); }
+  pin_uniform(score_rec); pin_uniform(pending);
+  const long long head_stride_b = PAGED ? (long long)tail_address(offsetof(PagedGqaTail, head_stride_b)) : (long long)address(head_stride16, (heads_flags >> 19) & 0x1F) * 16;
+  gchar* const k_base = (PAGED ? (gchar*)tail_address(offsetof(PagedGqaTail, k)) : k_rec) + hk * head_stride_b;
+  gchar* const v_base = (PAGED ? (gchar*)tail_address(offsetof(PagedGqaTail, v)) : v_rec) + hk * head_stride_b;
   gfloat* const score = score_rec + (size_t)hk * cap;
 
   const int cnt = min(cnt_raw, sel_cap);
+  const GqaTail& block = [&]() -> const GqaTail& {
+    if constexpr (PAGED) return T.a;
+    else return T;
+  }();
   if (cnt <= 0) {                                    // inactive or rejected sequence: zero-filled rows
     if (chunk == 0) {
       const size_t row = (size_t)b * HQ + (size_t)hk * G;
       for (int o = tid; o < G * D; o += kThreads) {
-        ((ADSA_GLOBAL uint16_t*)T.out)[row * D + o] = 0;
-        if (o % D == 0) ((gfloat*)T.lse)[row + o / D] = 0.0f;
+        ((ADSA_GLOBAL uint16_t*)block.out)[row * D + o] = 0;
+        if (o % D == 0) ((gfloat*)block.lse)[row + o / D] = 0.0f;
       }
-      if (hk == 0 && tid == 0) advance_empty(sqp, T.advance);
+      if (hk == 0 && tid == 0) advance_empty(sqp, block.advance);
     }
     return;
+  }
+  __shared__ int s_units[PAGED ? kMostEntries : 1];
+  __shared__ int s_good[NW];
+  int last_slot = cap - 1;
+  if constexpr (PAGED) {                             // (as in k_attend)
+    const int need = n_res >= 1 && n_res <= cap ? ((n_res - 1) >> page_shift) + 1 : kMostEntries + 1;
+    const bool good = page_entries.put(s_units, (int)tail_word(offsetof(PagedGqaTail, n_pages) / 4), tail_word(offsetof(PagedGqaTail, page_units) / 4), need);
+    const bool wave_good = __ballot(!good) == 0 && need <= kMostEntries;
+    if (lane == 0) s_good[wave] = wave_good;
+    __syncthreads();
+    bool all = true;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) all &= s_good[w] != 0;
+    last_slot = n_res - 1;
+    if (!all) {
+      if (chunk == 0) {
+        const size_t row = (size_t)b * HQ + (size_t)hk * G;
+        for (int o = tid; o < G * D; o += kThreads) ((ADSA_GLOBAL uint16_t*)tail_address(offsetof(GqaTail, out)))[row * D + o] = 0;
+        if (tid < G) ((gfloat*)tail_address(offsetof(GqaTail, lse)))[row + tid] = 0.0f;
+        if (hk == 0 && tid == 0) sqp->status = sqp->status | ADSA_SEQ_BAD_STATE;
+      }
+      return;
+    }
   }
   // this workgroup's tiles of the list: all of them, or chunk `chunk` of n_chunks (whole tiles; the last chunk is
   // never empty, chunks beyond the number of tiles are)
@@ -246,7 +305,19 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
     qb[2 * c2] = as_bf16x4(x.x, x.y);
     qb[2 * c2 + 1] = as_bf16x4(x.z, x.w);
   }
-  const int new_slot = (append && pending >= 0 && pending < cap) ? pending : -1;
+  const int new_slot = (append && pending >= 0 && pending <= last_slot) ? pending : -1;
+  // PAGED: where a slot's row begins in its pool; the list is staged as these, and the query token's row is known by its own
+  const uint32_t slot_units = PAGED ? tail_word(offsetof(PagedGqaTail, slot_units) / 4) : 0u;
+  const int unit_shift = PAGED ? (int)tail_word(offsetof(PagedGqaTail, unit_shift) / 4) : 0;
+  auto place_of = [&](int slot) {
+    if constexpr (PAGED) return s_units[slot >> page_shift] + (int)__umul24((uint32_t)slot & ((1u << page_shift) - 1u), slot_units);
+    else return slot;
+  };
+  const int new_place = PAGED && new_slot >= 0 ? place_of(new_slot) : new_slot;
+  auto row_at = [&](const gchar* base, int place, uint32_t lane_off) {
+    if constexpr (PAGED) return base + (((uint64_t)(uint32_t)place << unit_shift) + lane_off);
+    else return base + ((uint32_t)place * stride32 + lane_off);
+  };
 
   char* const stage = s_stage + wave * stage_b;      // LDS this wave owns
 
@@ -272,8 +343,8 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
     uint32_t f = 0u;
 #pragma unroll
     for (int l = 0; l < LT; ++l) {
-      kr[u][l] = load_stream16(k_base + ((uint32_t)sk[l] * stride32 + k_lane_off));
-      f |= sk[l] == new_slot ? (1u << l) : 0u;
+      kr[u][l] = load_stream16(row_at(k_base, sk[l], k_lane_off));
+      f |= sk[l] == new_place ? (1u << l) : 0u;
     }
     fresh_k[u] = f;
     in_order();
@@ -282,8 +353,8 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
     uint32_t f = 0u;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      vload<VW, true>(v_base + ((uint32_t)sv[i] * stride32 + v_lane_off), vr[u][i]);
-      f |= sv[i] == new_slot ? (1u << i) : 0u;
+      vload<VW, true>(row_at(v_base, sv[i], v_lane_off), vr[u][i]);
+      f |= sv[i] == new_place ? (1u << i) : 0u;
     }
     fresh_v[u] = f;
     in_order();
@@ -297,7 +368,6 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
     for (int i = 0; i < 4; ++i) sv[i] = s_slot[min(tile * 16 + 4 * kg + i, len - 1)];
   };
 
-  uint32_t tail = 0u;                                // lane i (modulo 16): dword i of T
   float m_run = -INFINITY, l_lane = 0.0f;            // online softmax of query g = r (l: this lane's tokens only)
   f32x4 acc[EV];                                     // acc[j][i] = partial out[g = 4*kg + i][d = EV*r + j]
 #pragma unroll
@@ -396,7 +466,7 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
         const int end = __builtin_amdgcn_readlane(slot_first, 16 * u + min(max(len - 1 - (wave + u * NW) * 16, 0), 15));
         slot_first = kg == u && first_at >= len ? end : slot_first;
       }
-      slot_first = min(max(slot_first, 0), cap - 1);
+      slot_first = place_of(min(max(slot_first, 0), last_slot));
       int sk[R][LT], sv[R][4];
 #pragma unroll
       for (int u = 0; u < R; ++u) {
@@ -413,14 +483,14 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
 #pragma unroll
     for (int k = 0; k < PF; ++k) {
       const int j = tid + k * kThreads;
-      if (j < len) s_slot[j] = min(max(pf_slot[k], 0), cap - 1);
+      if (j < len) s_slot[j] = place_of(min(max(pf_slot[k], 0), last_slot));
     }
-    for (int j = tid + PF * kThreads; j < len; j += kThreads) s_slot[j] = min(max(idx[j], 0), cap - 1);
+    for (int j = tid + PF * kThreads; j < len; j += kThreads) s_slot[j] = place_of(min(max(idx[j], 0), last_slot));
   } else {
-    for (int j = tid; j < len; j += kThreads) s_slot[j] = min(max(idx[t_begin + j], 0), cap - 1);
+    for (int j = tid; j < len; j += kThreads) s_slot[j] = place_of(min(max(idx[t_begin + j], 0), last_slot));
   }
     // (a vector load behind the first rows': its scalar form would be waited for with the record)
-    tail = ((const ADSA_GLOBAL uint32_t*)((const char __attribute__((address_space(4)))*)__builtin_amdgcn_kernarg_segment_ptr() + kLeadBytes))[lane % 16];
+    if constexpr (!PAGED) load_tail();
     __syncthreads();
     if constexpr (SPLIT) {
 #pragma unroll
@@ -472,8 +542,6 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
   }
   const float lse2 = M + __log2f(L), inv_l = 1.0f / L;
   const size_t hq0 = (size_t)b * HQ + (size_t)hk * G;           // first query head of this cache head
-  auto tail_word = [&](int i) { return (uint32_t)__builtin_amdgcn_readlane((int)tail, i); };
-  auto tail_address = [&](size_t at) { return address(tail_word(at / 4), tail_word(at / 4 + 1)); };
   ADSA_GLOBAL uint16_t* const out = (ADSA_GLOBAL uint16_t*)tail_address(offsetof(GqaTail, out)) + hq0 * D;
   gfloat* const lse = (gfloat*)tail_address(offsetof(GqaTail, lse)) + hq0;
   gfloat* const part_acc = (gfloat*)tail_address(offsetof(GqaTail, part_acc));
@@ -495,7 +563,7 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
   }
   // Section 4.2 append: this cache head's rows of the new token, from the registers that attended them
   if (new_slot >= 0 && wave == 0 && chunk == n_chunks - 1) {
-    const long long off = (long long)new_slot * stride32;
+    const long long off = PAGED ? (long long)((uint64_t)(uint32_t)new_place << unit_shift) : (long long)new_slot * stride32;
     if (ld_row == 0) store16(k_base + off + ld_piece * 16, nk);
     if (kg == 0) {
       if constexpr (VW == 4) store16(v_base + off + r * 16, make_uint4(nv[0], nv[1], nv[2], nv[3]));
@@ -522,7 +590,7 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
           for (int k = 0; k < 8; ++k)
             if (g0 + k < G) inc += fast_exp2(z[k] - lane_f(lse2, g0 + k));
         }
-        unsafeAtomicAdd((float*)(score + s_slot[t]), inc);
+        unsafeAtomicAdd((float*)(score + (PAGED ? min(max(idx[t], 0), last_slot) : s_slot[t])), inc);
       }
     }
     if (hk == 0 && tid == 0) advance_step(sqp, advance);     // no other workgroup reads step
@@ -545,7 +613,8 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
 // the queries in ascending order, to the cache head's score row.
 constexpr int kFinishThreads = 256, kFinishTokens = 2 * kFinishThreads;
 static_assert(kMaxChunks == 16 && kFinishThreads == 16 * 16, "one thread per (query, chunk), a query's chunks in one 16-lane row");
-template <int D>
+// (PAGED: a sequence whose pages were not in order has its zeros already.)
+template <int D, bool PAGED = false>
 __global__ __launch_bounds__(kFinishThreads) void k_gqa_finish(
     uint32_t seqs_lo, uint32_t idx_lo, uint32_t cnt_lo, uint32_t out_lo, uint32_t lse_lo, uint32_t lg_lo, uint32_t ml_lo, uint32_t acc_lo,
     uint32_t seqs_idx_hi, uint32_t cnt_out_hi, uint32_t lse_lg_hi, uint32_t ml_acc_hi, uint32_t caps, uint32_t flags) {
@@ -556,7 +625,8 @@ __global__ __launch_bounds__(kFinishThreads) void k_gqa_finish(
   const int slice = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
   ADSA_GLOBAL adsa_seq* const sqp = (ADSA_GLOBAL adsa_seq*)address(seqs_lo, seqs_idx_hi & 0xFFFF) + b;
   const int cnt = min(((const gint*)address(cnt_lo, cnt_out_hi & 0xFFFF))[b], sel_cap);
-  if (cnt <= 0 || slice * kFinishTokens >= cnt) return;      // (inactive sequences: zero rows, already written)
+  const int status = PAGED ? sqp->status : 0;
+  if (cnt <= 0 || slice * kFinishTokens >= cnt || status != 0) return;       // (inactive sequences: zero rows, already written)
   const size_t hq0 = ((size_t)b * n_heads + hk) * G;
   const unsigned tiles = (unsigned)(cnt + 15) / 16;
   auto on = [&](int c) {                                     // chunks without a tile hold nothing (their workspace words are stale)
@@ -655,6 +725,36 @@ hipError_t launch_gqa_w(const GqaArgs& A, int n_seq, int n_chunks, size_t lds, h
   return hipGetLastError();
 }
 
+// The same over pages.
+template <int D, int NW, bool SPLIT, int R>
+hipError_t launch_gqa_paged_w(const GqaArgs& A, const PageArgs& pages, int n_seq, int n_chunks, size_t lds, hipStream_t st) {
+  const uint32_t flags = A.n_heads | A.G << 9 | (A.append ? 0x10000 : 0) | (A.new_f32 ? 0x20000 : 0) | (A.accumulate ? 0x40000 : 0) | (uint32_t)pages.shift << 19 | n_chunks << 24;
+  const PagedGqaTail T = {{A.out, A.lse, A.logits, A.part_ml, A.part_acc, A.lg_global, A.advance, {}}, pages.k, pages.v, pages.head_stride_b, pages.page_units, pages.slot_units,
+                          pages.n_pages, pages.unit_shift, {}};
+  const uint32_t table_hi = (uint32_t)(reinterpret_cast<uintptr_t>(pages.table) >> 32 & 0xFFFF) | (uint32_t)pages.table_stride << 16;
+  hipLaunchKernelGGL((k_attend_gqa<D, NW, SPLIT, R, true>), dim3(A.n_heads, n_seq, n_chunks), dim3(NW * kWave), lds, st, lo32(A.seqs), lo32(A.sel_idx), lo32(A.sel_cnt), lo32(A.q),
+                     lo32(A.k_new), lo32(A.v_new), hi16s(A.seqs, A.sel_idx), hi16s(A.sel_cnt, A.q), hi16s(A.k_new, A.v_new), flags, (uint32_t)A.cap | (uint32_t)A.sel_cap << 16,
+                     lo32(pages.table), table_hi, A.scale_log2, T);
+  if constexpr (SPLIT) {
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const dim3 fgrid(A.accumulate ? (A.sel_cap + kFinishTokens - 1) / kFinishTokens : 1, A.n_heads, n_seq);
+    const uint32_t fflags = A.n_heads | A.G << 9 | (A.accumulate ? 0x10000 : 0) | (uint32_t)A.advance << 18 | n_chunks << 24;
+    hipLaunchKernelGGL((k_gqa_finish<D, true>), fgrid, dim3(kFinishThreads), 0, st, lo32(A.seqs), lo32(A.sel_idx), lo32(A.sel_cnt), lo32(A.out), lo32(A.lse), lo32(A.logits),
+                       lo32(A.part_ml), lo32(A.part_acc), hi16s(A.seqs, A.sel_idx), hi16s(A.sel_cnt, A.out), hi16s(A.lse, A.logits), hi16s(A.part_ml, A.part_acc),
+                       (uint32_t)A.cap | (uint32_t)A.sel_cap << 16, fflags);
+  }
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_gqa_paged_d(const GqaArgs& A, const PageArgs& pages, const AttendPlan& plan, int n_seq, size_t lds, hipStream_t st) {
+  if (plan.n_chunks > 1) return launch_gqa_paged_w<D, 4, true, ring(D)>(A, pages, n_seq, plan.n_chunks, lds, st);
+  if (plan.waves == 8) return launch_gqa_paged_w<D, 8, false, ring(D)>(A, pages, n_seq, 1, lds, st);
+  if (!gqa_two_fit(lds)) return launch_gqa_paged_w<D, 4, false, deep_ring(D)>(A, pages, n_seq, 1, lds, st);
+  return launch_gqa_paged_w<D, 4, false, ring(D)>(A, pages, n_seq, 1, lds, st);
+}
+
 template <int D>
 hipError_t launch_gqa_d(const GqaArgs& A, const AttendPlan& plan, int n_seq, size_t lds, hipStream_t st, hipEvent_t e0,
                         hipEvent_t e1) {
@@ -670,11 +770,11 @@ hipError_t launch_gqa_d(const GqaArgs& A, const AttendPlan& plan, int n_seq, siz
 // here, at the library's first use of a device, not next to a launch (where it would also sit inside a captured graph).
 hipError_t gqa_prepare_kernels() {
   const int lim = (int)kGqaMaxLds;
-  const void* kernels[] = {
-      reinterpret_cast<const void*>(&k_attend_gqa<64, 4, false, ring(64)>), reinterpret_cast<const void*>(&k_attend_gqa<64, 8, false, ring(64)>),
-      reinterpret_cast<const void*>(&k_attend_gqa<128, 4, false, ring(128)>), reinterpret_cast<const void*>(&k_attend_gqa<128, 8, false, ring(128)>),
-      reinterpret_cast<const void*>(&k_attend_gqa<64, 4, false, deep_ring(64)>), reinterpret_cast<const void*>(&k_attend_gqa<128, 4, false, deep_ring(128)>),
-      reinterpret_cast<const void*>(&k_attend_gqa<64, 4, true, ring(64)>), reinterpret_cast<const void*>(&k_attend_gqa<128, 4, true, ring(128)>)};
+#define ADSA_GQA(D, ...) reinterpret_cast<const void*>(&k_attend_gqa<D, __VA_ARGS__>), reinterpret_cast<const void*>(&k_attend_gqa<D, __VA_ARGS__, true>)
+  const void* kernels[] = {ADSA_GQA(64, 4, false, ring(64)),      ADSA_GQA(64, 8, false, ring(64)),        ADSA_GQA(128, 4, false, ring(128)),
+                           ADSA_GQA(128, 8, false, ring(128)),    ADSA_GQA(64, 4, false, deep_ring(64)),   ADSA_GQA(128, 4, false, deep_ring(128)),
+                           ADSA_GQA(64, 4, true, ring(64)),       ADSA_GQA(128, 4, true, ring(128))};
+#undef ADSA_GQA
   for (const void* k : kernels) {
     const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, lim);
     if (e != hipSuccess) return e;
@@ -702,13 +802,8 @@ size_t gqa_lds_bytes(const adsa_params& p, int waves, int n_chunks) {
   return ((size_t)p.q_per_kv + 1) * lgs * sizeof(float) + (size_t)waves * gqa_stage_bytes(p);
 }
 
-hipError_t launch_attend_gqa(const adsa_params& p, const AttendPlan& plan, adsa_seq* seqs, const void* q,
-                             const void* k_new, const void* v_new, const int32_t* sel_idx,
-                             const int32_t* sel_cnt, void* out, float* lse, char* ws, const Workspace& w,
-                             bool accumulate, bool append, int advance, bool new_f32, hipStream_t st,
-                             hipEvent_t ev_start, hipEvent_t ev_stop) {
-  if (p.dtype != ADSA_BF16 || p.q_per_kv < 2 || p.q_per_kv > 16) return hipErrorInvalidValue;
-  if (plan.n_chunks < 1 || plan.n_chunks > kMaxChunks) return hipErrorInvalidValue;
+static GqaArgs gqa_args(const adsa_params& p, adsa_seq* seqs, const void* q, const void* k_new, const void* v_new, const int32_t* sel_idx, const int32_t* sel_cnt,
+                        void* out, float* lse, char* ws, const Workspace& w, bool accumulate, bool append, int advance, bool new_f32) {
   GqaArgs A;
   A.seqs = seqs; A.q = (const char*)q; A.k_new = (const char*)k_new; A.v_new = (const char*)v_new;
   A.sel_idx = sel_idx; A.sel_cnt = sel_cnt; A.out = (char*)out; A.lse = lse;
@@ -723,11 +818,33 @@ hipError_t launch_attend_gqa(const adsa_params& p, const AttendPlan& plan, adsa_
   A.head_stride_b = (long long)p.kv_head_stride * 2;
   const float scale = p.softmax_scale != 0.0f ? p.softmax_scale : 1.0f / sqrtf((float)p.head_dim);
   A.scale_log2 = scale * kLog2e;
+  return A;
+}
+
+hipError_t launch_attend_gqa(const adsa_params& p, const AttendPlan& plan, adsa_seq* seqs, const void* q,
+                             const void* k_new, const void* v_new, const int32_t* sel_idx,
+                             const int32_t* sel_cnt, void* out, float* lse, char* ws, const Workspace& w,
+                             bool accumulate, bool append, int advance, bool new_f32, hipStream_t st,
+                             hipEvent_t ev_start, hipEvent_t ev_stop) {
+  if (p.dtype != ADSA_BF16 || p.q_per_kv < 2 || p.q_per_kv > 16) return hipErrorInvalidValue;
+  if (plan.n_chunks < 1 || plan.n_chunks > kMaxChunks) return hipErrorInvalidValue;
+  const GqaArgs A = gqa_args(p, seqs, q, k_new, v_new, sel_idx, sel_cnt, out, lse, ws, w, accumulate, append, advance, new_f32);
   const size_t lds = gqa_lds_bytes(p, plan.waves, plan.n_chunks);
   if (lds > kGqaMaxLds) return hipErrorInvalidValue;
   if (p.head_dim == 64) return launch_gqa_d<64>(A, plan, p.n_seq, lds, st, ev_start, ev_stop);
   if (p.head_dim == 128) return launch_gqa_d<128>(A, plan, p.n_seq, lds, st, ev_start, ev_stop);
   return hipErrorInvalidValue;
+}
+
+hipError_t launch_attend_gqa_paged(const adsa_params& p, const PageArgs& pages, const AttendPlan& plan, adsa_seq* seqs, const void* q, const void* k_new,
+                                   const void* v_new, const int32_t* sel_idx, const int32_t* sel_cnt, void* out, float* lse, char* ws, const Workspace& w,
+                                   bool accumulate, bool append, int advance, bool new_f32, hipStream_t st) {
+  if (p.dtype != ADSA_BF16 || p.q_per_kv < 2 || p.q_per_kv > 16) return hipErrorInvalidValue;
+  if (plan.n_chunks < 1 || plan.n_chunks > kMaxChunks) return hipErrorInvalidValue;
+  const GqaArgs A = gqa_args(p, seqs, q, k_new, v_new, sel_idx, sel_cnt, out, lse, ws, w, accumulate, append, advance, new_f32);
+  const size_t lds = gqa_lds_bytes(p, plan.waves, plan.n_chunks);
+  if (lds > kGqaMaxLds) return hipErrorInvalidValue;
+  return p.head_dim == 64 ? launch_gqa_paged_d<64>(A, pages, plan, p.n_seq, lds, st) : launch_gqa_paged_d<128>(A, pages, plan, p.n_seq, lds, st);
 }
 
 }  // namespace adsa

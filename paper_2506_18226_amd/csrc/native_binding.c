@@ -166,6 +166,52 @@ static PyObject* call_prompt(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(rc);
 }
 
+/* ---- caches in pages, and sampling */
+typedef int (*fn_append_paged)(const void*, const void*, const void*, const void*, void*, const void*, const void*, const void*, void*, uint32_t, void*);
+typedef int (*fn_prefill_paged)(const void*, const void*, const void*, const void*, void*, const void*, void*, void*, uint32_t, void*, size_t, void*);
+typedef int (*fn_attend_paged)(const void*, const void*, void*, const void*, const void*, const void*, const void*, const void*, void*, void*, uint32_t, void*, size_t, void*);
+typedef int (*fn_compact_paged)(const void*, const void*, void*, void*, uint32_t, void*, size_t, void*);
+typedef int (*fn_sample)(const void*, const void*, const void*, const void*, void*, void*, void*);
+
+/* call_paged(which, address of the C function, host structs x 4 (params first; sampling alone where that is the call), flags, stream, workspace,
+ * pointers...) */
+static PyObject* call_paged(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  (void)self;
+  const long which = n > 0 ? PyLong_AsLong(a[0]) : -1;        /* 0 append, 1 prefill, 2 attend, 3 compact, 4 sample */
+  static const Py_ssize_t counts[5] = {5, 4, 8, 2, 5};        /* pointers of each */
+  if (PyErr_Occurred()) return NULL;
+  if (which < 0 || which > 4 || n != 9 + counts[which]) {
+    PyErr_SetString(PyExc_TypeError, "wrong number of arguments");
+    return NULL;
+  }
+  void *fn, *stream, *ws, *p[8];
+  const void* h[4];
+  size_t ws_bytes = 0;
+  if (as_pointer(a[1], &fn) < 0) return NULL;
+  const int typed = which < 4 && params_type ? PyObject_IsInstance(a[2], params_type) : which == 4;
+  if (typed < 0) return NULL;
+  if (!typed) {
+    PyErr_SetString(PyExc_TypeError, "params: AdsaParams expected");
+    return NULL;
+  }
+  for (int i = 0; i < 4; ++i)
+    if (as_struct(a[2 + i], &h[i]) < 0) return NULL;
+  const unsigned long flags = PyLong_AsUnsignedLongMask(a[6]);
+  if (PyErr_Occurred() || as_pointer(a[7], &stream) < 0 || as_pointer(a[8], &ws) < 0 || as_bytes(a[8], &ws_bytes) < 0) return NULL;
+  for (Py_ssize_t i = 0; i < counts[which]; ++i)
+    if (as_pointer(a[9 + i], &p[i]) < 0) return NULL;
+  const uint32_t f = (uint32_t)flags;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  if (which == 0) rc = ((fn_append_paged)fn)(h[0], h[1], h[2], h[3], p[0], p[1], p[2], p[3], p[4], f, stream);
+  else if (which == 1) rc = ((fn_prefill_paged)fn)(h[0], h[1], h[2], h[3], p[0], p[1], p[2], p[3], f, ws, ws_bytes, stream);
+  else if (which == 2) rc = ((fn_attend_paged)fn)(h[0], h[1], p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], f, ws, ws_bytes, stream);
+  else if (which == 3) rc = ((fn_compact_paged)fn)(h[0], h[1], p[0], p[1], f, ws, ws_bytes, stream);
+  else rc = ((fn_sample)fn)(h[0], p[0], p[1], p[2], p[3], p[4], stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
 /* the ctypes mirror of adsa_params that the calls take */
 static PyObject* set_params_type(PyObject* self, PyObject* type) {
   (void)self;
@@ -177,7 +223,8 @@ static PyObject* set_params_type(PyObject* self, PyObject* type) {
 static PyMethodDef methods[] = {{"set_params_type", set_params_type, METH_O, "The type of the calls' params."},
                                 {"call", (PyCFunction)(void (*)(void))call_entry, METH_FASTCALL, "One C call."},
                                 {"call_static", (PyCFunction)(void (*)(void))call_static, METH_FASTCALL, "One call of adsa_step_static."},
-                                {"call_prompt", (PyCFunction)(void (*)(void))call_prompt, METH_FASTCALL, "One call of the prompt side."}, {NULL, NULL, 0, NULL}};
+                                {"call_prompt", (PyCFunction)(void (*)(void))call_prompt, METH_FASTCALL, "One call of the prompt side."},
+                                {"call_paged", (PyCFunction)(void (*)(void))call_paged, METH_FASTCALL, "One call over pages, or a sampling call."}, {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_adsa_native", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__adsa_native(void) {

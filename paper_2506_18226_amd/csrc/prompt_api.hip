@@ -1,4 +1,4 @@
-// C ABI of the prompt side (adsa_rotate, adsa_append, adsa_prefill, adsa_attend_shared): host-side argument checks and launch order.
+// C ABI of the prompt side (adsa_rotate, adsa_append, adsa_prefill and the two over pages, adsa_attend_shared): host-side argument checks and launch order.
 #include <algorithm>
 #include <cmath>
 
@@ -92,6 +92,55 @@ int plan_shared(const adsa_params& p, const adsa_shared* s, SharedPlan* plan, Sh
   return ADSA_OK;
 }
 
+// pages: NULL for dense caches
+int append(const adsa_params& eff, const PageArgs* pages, const adsa_tokens* tokens, const adsa_rope* rope, adsa_seq* seqs, const void* q, const void* k,
+           const void* v, void* q_out, uint32_t flags, void* stream) {
+  if (!seqs || !k || !v || (q == nullptr) != (q_out == nullptr)) return ADSA_ERR_NULL;
+  int rc = check_tokens(eff, tokens);
+  if (rc) return rc;
+  if (rope && (rc = check_rope(rope))) return rc;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out)) return ADSA_ERR_ALIGN;
+  const bool in_f32 = f32_rows(eff, flags);
+  if ((rc = check_row_stride(tokens->q_stride, query_heads(eff), eff, in_f32)) || (rc = check_row_stride(tokens->k_stride, eff.n_heads, eff, in_f32)) ||
+      (rc = check_row_stride(tokens->v_stride, eff.n_heads, eff, in_f32)))
+    return rc;
+  const bool advance = (flags & ADSA_FLAG_ADVANCE) != 0;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  const hipError_t e = pages ? launch_append_paged(eff, *pages, *tokens, rope, seqs, q, k, v, q_out, in_f32, advance, st)
+                             : launch_append(eff, *tokens, rope, seqs, q, k, v, q_out, in_f32, advance, st);
+  return e == hipSuccess ? ADSA_OK : ADSA_ERR_LAUNCH;
+}
+
+// The plan of a prompt call goes by the distance of rows, which within a page is the page's.
+adsa_params paged_rows(adsa_params eff, const PageArgs& pages) {
+  eff.kv_slot_stride = pages.slot_stride_b / elem_bytes(eff);
+  return eff;
+}
+
+int prefill(const adsa_params& eff, const PageArgs* pages, const adsa_tokens* tokens, const adsa_mods* mods, adsa_seq* seqs, const void* q, void* out,
+            float* lse, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!seqs || !q || !out || !lse) return ADSA_ERR_NULL;
+  PromptPlan plan;
+  PromptWorkspace w;
+  int rc = plan_prompt(eff, tokens, &plan, &w);
+  if (rc) return rc;
+  const adsa_mods none = {};
+  const adsa_mods& m = mods ? *mods : none;
+  rc = check_mods(eff, m, true);
+  if (rc) return rc;
+  if (!aligned16(q) || !aligned16(out)) return ADSA_ERR_ALIGN;
+  rc = check_space(workspace, workspace_bytes, w.total);
+  if (rc) return rc;
+  rc = ensure_device_ready();
+  if (rc) return rc;
+  const bool accumulate = eff.score_mode == ADSA_SCORE_ATTN_MASS && !(flags & ADSA_FLAG_NO_ACCUMULATE);
+  const bool advance = (flags & ADSA_FLAG_ADVANCE) != 0, split = (flags & ADSA_FLAG_SPLIT_P) != 0;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  const hipError_t e = pages ? launch_prefill_paged(eff, *pages, *tokens, m, plan, seqs, q, out, lse, (char*)workspace, w, accumulate, advance, split, st)
+                             : launch_prefill(eff, *tokens, m, plan, seqs, q, out, lse, (char*)workspace, w, accumulate, advance, split, st);
+  return e == hipSuccess ? ADSA_OK : ADSA_ERR_LAUNCH;
+}
+
 }  // namespace
 }  // namespace adsa
 
@@ -118,20 +167,16 @@ int adsa_rotate(const adsa_params* p, const adsa_rope* rope, const adsa_seq* seq
 int adsa_append(const adsa_params* p, const adsa_tokens* tokens, const adsa_rope* rope, adsa_seq* seqs, const void* q, const void* k, const void* v,
                 void* q_out, uint32_t flags, void* stream) {
   adsa_params eff;
-  int rc = resolve(p, &eff);
-  if (rc) return rc;
-  if (!seqs || !k || !v || (q == nullptr) != (q_out == nullptr)) return ADSA_ERR_NULL;
-  rc = check_tokens(eff, tokens);
-  if (rc) return rc;
-  if (rope && (rc = check_rope(rope))) return rc;
-  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out)) return ADSA_ERR_ALIGN;
-  const bool in_f32 = f32_rows(eff, flags);
-  if ((rc = check_row_stride(tokens->q_stride, query_heads(eff), eff, in_f32)) || (rc = check_row_stride(tokens->k_stride, eff.n_heads, eff, in_f32)) ||
-      (rc = check_row_stride(tokens->v_stride, eff.n_heads, eff, in_f32)))
-    return rc;
-  if (launch_append(eff, *tokens, rope, seqs, q, k, v, q_out, in_f32, (flags & ADSA_FLAG_ADVANCE) != 0, reinterpret_cast<hipStream_t>(stream)) != hipSuccess)
-    return ADSA_ERR_LAUNCH;
-  return ADSA_OK;
+  const int rc = resolve(p, &eff);
+  return rc ? rc : append(eff, nullptr, tokens, rope, seqs, q, k, v, q_out, flags, stream);
+}
+
+int adsa_append_paged(const adsa_params* p, const adsa_pages* pages, const adsa_tokens* tokens, const adsa_rope* rope, adsa_seq* seqs, const void* q,
+                      const void* k, const void* v, void* q_out, uint32_t flags, void* stream) {
+  adsa_params eff;
+  PageArgs args;
+  const int rc = resolve_paged(p, pages, &eff, &args);
+  return rc ? rc : append(eff, &args, tokens, rope, seqs, q, k, v, q_out, flags, stream);
 }
 
 size_t adsa_prefill_workspace_bytes(const adsa_params* p, const adsa_tokens* tokens) {
@@ -144,27 +189,24 @@ size_t adsa_prefill_workspace_bytes(const adsa_params* p, const adsa_tokens* tok
 int adsa_prefill(const adsa_params* p, const adsa_tokens* tokens, const adsa_mods* mods, adsa_seq* seqs, const void* q, void* out, float* lse,
                  uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
   adsa_params eff;
-  int rc = resolve(p, &eff);
-  if (rc) return rc;
-  if (!seqs || !q || !out || !lse) return ADSA_ERR_NULL;
+  const int rc = resolve(p, &eff);
+  return rc ? rc : prefill(eff, nullptr, tokens, mods, seqs, q, out, lse, flags, workspace, workspace_bytes, stream);
+}
+
+size_t adsa_prefill_paged_workspace_bytes(const adsa_params* p, const adsa_pages* pages, const adsa_tokens* tokens) {
+  adsa_params eff;
+  PageArgs args;
   PromptPlan plan;
   PromptWorkspace w;
-  rc = plan_prompt(eff, tokens, &plan, &w);
-  if (rc) return rc;
-  const adsa_mods none = {};
-  const adsa_mods& m = mods ? *mods : none;
-  rc = check_mods(eff, m, true);
-  if (rc) return rc;
-  if (!aligned16(q) || !aligned16(out)) return ADSA_ERR_ALIGN;
-  rc = check_space(workspace, workspace_bytes, w.total);
-  if (rc) return rc;
-  rc = ensure_device_ready();
-  if (rc) return rc;
-  const bool accumulate = eff.score_mode == ADSA_SCORE_ATTN_MASS && !(flags & ADSA_FLAG_NO_ACCUMULATE);
-  if (launch_prefill(eff, *tokens, m, plan, seqs, q, out, lse, (char*)workspace, w, accumulate, (flags & ADSA_FLAG_ADVANCE) != 0,
-                     (flags & ADSA_FLAG_SPLIT_P) != 0, reinterpret_cast<hipStream_t>(stream)) != hipSuccess)
-    return ADSA_ERR_LAUNCH;
-  return ADSA_OK;
+  return resolve_paged(p, pages, &eff, &args) == ADSA_OK && plan_prompt(paged_rows(eff, args), tokens, &plan, &w) == ADSA_OK ? w.total : 0;
+}
+
+int adsa_prefill_paged(const adsa_params* p, const adsa_pages* pages, const adsa_tokens* tokens, const adsa_mods* mods, adsa_seq* seqs, const void* q,
+                       void* out, float* lse, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
+  adsa_params eff;
+  PageArgs args;
+  const int rc = resolve_paged(p, pages, &eff, &args);
+  return rc ? rc : prefill(paged_rows(eff, args), &args, tokens, mods, seqs, q, out, lse, flags, workspace, workspace_bytes, stream);
 }
 
 size_t adsa_shared_workspace_bytes(const adsa_params* p, const adsa_shared* shared) {

@@ -7,6 +7,7 @@
 //    A thread turns 8 pairs: 16 bytes of bf16 on either side of the row (NEAR false), or 32 bytes in a row (NEAR).
 //    Bound by HBM (9216 tokens x 96 rows x 128: 90 us, 5 TB/s; 4352 x 72 x 64: 16.6 us, 4.8 TB/s), few tokens by two trips that depend on each other (3.4 us).
 #include <algorithm>
+#include <type_traits>
 
 #include "adsa_device.h"
 #include "adsa_partition.h"
@@ -34,6 +35,9 @@ struct RotateArgs {
   int tokens_here, parts;          // tokens per workgroup; workgroups that share a token's rows
   int text[3], origin[3], row[3], col[3];
   GridWidth grid;
+};
+struct PagedRotateArgs : RotateArgs {
+  PageArgs pages;
 };
 
 // What a workgroup knows of a token.
@@ -88,7 +92,9 @@ __device__ __forceinline__ int sequence_of(const gint* begin, int n_seq, int t) 
 // pos, score and, for a sequence's first token, the record up to date.  The other workgroups of the sequence may be reading the
 // record meanwhile: what decides here is either not written by this launch, or decides the same way before and after (n_res >= slot0
 // holds for the old n_res and for slot0 + len; a status that is set belongs to a record that everybody finds unfit).
-__device__ __forceinline__ Token append_token(const RotateArgs& A, int t, bool writes) {
+// no_page (pages): the sequence's new slots that lack a page.  rows: where the rows of a slot's head 0 lie.
+template <typename Rows>
+__device__ __forceinline__ Token append_token(const RotateArgs& A, int t, bool writes, bool no_page, Rows rows) {
   Token tk = {nullptr, nullptr, 0, 0, 0};
   const gint* const begin = (const gint*)A.begin;
   const int b = sequence_of(begin, A.n_seq, t), from = begin[b], len = begin[b + 1] - from, j = t - from;
@@ -103,13 +109,13 @@ __device__ __forceinline__ Token append_token(const RotateArgs& A, int t, bool w
     pos0 = A.pos0 ? ((const gint*)A.pos0)[b] : slot0 > 0 ? (long long)((const gint*)sq.pos)[slot0 - 1] + 1 : 0;
     if (pos0 < 0 || pos0 + len > 0x7FFFFFFF || pos0 + len - P > A.total) reject = ADSA_SEQ_BAD_STATE;
   }
+  if (reject == 0 && no_page) reject = ADSA_SEQ_CACHE_FULL;
   if (status != 0 || reject != 0) {
     if (writes && status == 0 && j == 0) sq.status = reject;
     return tk;
   }
   const int slot = slot0 + j;
-  tk.k = (gchar*)sq.k + slot * A.slot_stride_b;
-  tk.v = (gchar*)sq.v + slot * A.slot_stride_b;
+  rows(b, slot, tk);
   tk.pos = (int)pos0 + j;
   tk.origin = P;
   tk.ok = 1;
@@ -132,8 +138,32 @@ __device__ __forceinline__ Token append_token(const RotateArgs& A, int t, bool w
   return tk;
 }
 
-template <int EB, int D, bool IN32, bool NEAR, bool APPEND>
-__global__ __launch_bounds__(kRotThreads) void k_rotate(RotateArgs A) {
+// Pages: whether the new tokens t0 .. t0 + n_here - 1 belong to sequences whose new slots all have a page, a bit each.  Every workgroup looks at all of
+// a sequence's new pages, so all decide alike (slots that cannot be are append_token's to refuse).
+template <typename Shared>
+__device__ __forceinline__ void find_pages(const PagedRotateArgs& A, int t0, int n_here, Shared& no_page) {
+  const gint* const begin = (const gint*)A.begin;
+  if (threadIdx.x < n_here) no_page[threadIdx.x] = 0;
+  __syncthreads();
+  int b = -1;
+  for (int i = 0; i < n_here; ++i) {                 // (uniform)
+    const int before = b;
+    b = sequence_of(begin, A.n_seq, t0 + i);
+    const int slot0 = ((const gint*)A.slot0)[b], len = begin[b + 1] - begin[b];
+    if (b == before) {                               // as the token before: looked at below
+      continue;
+    }
+    if (slot0 < 0 || len < 1 || len > A.cap || slot0 > A.cap - len) continue;
+    const gint* const table = (const gint*)A.pages.table + (size_t)b * A.pages.table_stride;
+    bool bad = false;
+    for (int e = (slot0 >> A.pages.shift) + (int)threadIdx.x; e <= (slot0 + len - 1) >> A.pages.shift; e += kRotThreads) bad |= (uint32_t)table[e] >= (uint32_t)A.pages.n_pages;
+    if (bad) no_page[i] = 1;                         // (whoever stores stores the same)
+  }
+  __syncthreads();
+}
+
+template <int EB, int D, bool IN32, bool NEAR, bool APPEND, bool PAGED = false>
+__global__ __launch_bounds__(kRotThreads) void k_rotate(std::conditional_t<PAGED, PagedRotateArgs, RotateArgs> A) {
   constexpr int kPairs = D / 2, IB = IN32 ? 4 : EB, kPieces = kPairs / 8;
   __shared__ RotateShared<D> sh;
   const int tid = threadIdx.x, t0 = (int)(blockIdx.x / (unsigned)A.parts) * A.tokens_here, part = (int)(blockIdx.x % (unsigned)A.parts);
@@ -166,9 +196,29 @@ __global__ __launch_bounds__(kRotThreads) void k_rotate(RotateArgs A) {
     for (int x = 0; x < 3; ++x)
       if (x < A.n_axes) f[x] = ((const ADSA_GLOBAL double*)A.freq)[x * kPairs + pair];
   }
-  if (tid < n_here) {
+  if constexpr (PAGED) {
+    __shared__ int s_no_page[kRotThreads / kPairs];
+    find_pages(A, t0, n_here, s_no_page);
+    if (tid < n_here) {
+      const gint* const begin = (const gint*)A.begin;
+      int first = tid;                               // the first token here of the same sequence
+      const int b = sequence_of(begin, A.n_seq, t0 + tid);
+      first = max(0, begin[b] - t0);
+      sh.token[tid] = append_token(A, t0 + tid, part == 0, s_no_page[min(first, tid)] != 0, [&](int seq, int slot, Token& tk) {
+        const long long page = ((const gint*)A.pages.table)[(size_t)seq * A.pages.table_stride + (slot >> A.pages.shift)];
+        const long long off = page * A.pages.page_stride_b + (slot & ((1 << A.pages.shift) - 1)) * A.slot_stride_b;
+        tk.k = (gchar*)A.pages.k + off;
+        tk.v = (gchar*)A.pages.v + off;
+      });
+    }
+  } else if (tid < n_here) {
     const int t = t0 + tid;
-    if constexpr (APPEND) sh.token[tid] = append_token(A, t, part == 0);
+    if constexpr (APPEND)
+      sh.token[tid] = append_token(A, t, part == 0, false, [&](int b, int slot, Token& tk) {
+        const ADSA_GLOBAL adsa_seq& sq = ((const ADSA_GLOBAL adsa_seq*)A.seqs)[b];
+        tk.k = (gchar*)sq.k + slot * A.slot_stride_b;
+        tk.v = (gchar*)sq.v + slot * A.slot_stride_b;
+      });
     else {
       const ADSA_GLOBAL adsa_seq& sq = ((const ADSA_GLOBAL adsa_seq*)A.seqs)[t];
       const int step = sq.step;
@@ -233,8 +283,8 @@ __global__ __launch_bounds__(kRotThreads) void k_rotate(RotateArgs A) {
   }
 }
 
-template <bool APPEND>
-hipError_t launch(const adsa_params& p, RotateArgs& A, const adsa_rope* rope, bool in_f32, hipStream_t st) {
+template <bool APPEND, bool PAGED = false>
+hipError_t launch(const adsa_params& p, std::conditional_t<PAGED, PagedRotateArgs, RotateArgs>& A, const adsa_rope* rope, bool in_f32, hipStream_t st) {
   const int D = p.head_dim, eb = elem_bytes(p), ib = in_f32 ? 4 : eb, pairs = D / 2;
   A.h = p.n_heads;
   A.hq = p.n_heads * (p.q_per_kv > 1 ? p.q_per_kv : 1);
@@ -244,6 +294,7 @@ hipError_t launch(const adsa_params& p, RotateArgs& A, const adsa_rope* rope, bo
   A.grid = {p.grid_w, 1.0f / (float)p.grid_w};
   A.slot_stride_b = p.kv_slot_stride * eb;
   A.head_stride_b = p.kv_head_stride * eb;
+  if constexpr (PAGED) { A.slot_stride_b = A.pages.slot_stride_b; A.head_stride_b = A.pages.head_stride_b; }
   auto stride = [&](long long elements, int heads) { return (elements ? elements : (long long)heads * D) * ib; };
   A.q_stride_b = stride(A.q_stride_b, A.hq);
   A.k_stride_b = stride(A.k_stride_b, A.h);
@@ -262,7 +313,7 @@ hipError_t launch(const adsa_params& p, RotateArgs& A, const adsa_rope* rope, bo
   const dim3 grid((unsigned)((A.n_tokens + A.tokens_here - 1) / A.tokens_here * A.parts));
   const bool near = rope && rope->pairing == ADSA_PAIR_NEIGHBOURS;
 #define ADSA_ROTATE(EB, IN32, NEAR)                                                                    \
-  (D == 64 ? k_rotate<EB, 64, IN32, NEAR, APPEND><<<grid, kRotThreads, 0, st>>>(A) : k_rotate<EB, 128, IN32, NEAR, APPEND><<<grid, kRotThreads, 0, st>>>(A))
+  (D == 64 ? k_rotate<EB, 64, IN32, NEAR, APPEND, PAGED><<<grid, kRotThreads, 0, st>>>(A) : k_rotate<EB, 128, IN32, NEAR, APPEND, PAGED><<<grid, kRotThreads, 0, st>>>(A))
   if (eb == 4) { if (near) ADSA_ROTATE(4, true, true); else ADSA_ROTATE(4, true, false); }
   else if (in_f32) { if (near) ADSA_ROTATE(2, true, true); else ADSA_ROTATE(2, true, false); }
   else { if (near) ADSA_ROTATE(2, false, true); else ADSA_ROTATE(2, false, false); }
@@ -283,9 +334,8 @@ hipError_t launch_rotate(const adsa_params& p, const adsa_rope& rope, const adsa
   return launch<false>(p, A, &rope, in_f32, st);
 }
 
-hipError_t launch_append(const adsa_params& p, const adsa_tokens& t, const adsa_rope* rope, adsa_seq* seqs, const void* q, const void* k, const void* v,
-                         void* q_out, bool in_f32, bool advance, hipStream_t st) {
-  RotateArgs A = {};
+static void fill_append_args(RotateArgs& A, const adsa_params& p, const adsa_tokens& t, adsa_seq* seqs, const void* q, const void* k, const void* v, void* q_out,
+                             bool advance) {
   A.q = (const char*)q; A.k = (const char*)k; A.v = (const char*)v; A.q_out = (char*)q_out;
   A.seqs = seqs;
   A.coords = t.coords; A.begin = t.begin; A.slot0 = t.slot0; A.pos0 = t.pos0;
@@ -294,7 +344,21 @@ hipError_t launch_append(const adsa_params& p, const adsa_tokens& t, const adsa_
   A.score_rows = score_rows(p);
   A.advance = advance ? 1 : 0;
   A.tags_at = p.score_mode == ADSA_SCORE_VCOS_FUSED ? p.n_heads * p.head_dim : 0;
+}
+
+hipError_t launch_append(const adsa_params& p, const adsa_tokens& t, const adsa_rope* rope, adsa_seq* seqs, const void* q, const void* k, const void* v,
+                         void* q_out, bool in_f32, bool advance, hipStream_t st) {
+  RotateArgs A = {};
+  fill_append_args(A, p, t, seqs, q, k, v, q_out, advance);
   return launch<true>(p, A, rope, in_f32, st);
+}
+
+hipError_t launch_append_paged(const adsa_params& p, const PageArgs& pages, const adsa_tokens& t, const adsa_rope* rope, adsa_seq* seqs, const void* q,
+                               const void* k, const void* v, void* q_out, bool in_f32, bool advance, hipStream_t st) {
+  PagedRotateArgs A = {};
+  fill_append_args(A, p, t, seqs, q, k, v, q_out, advance);
+  A.pages = pages;
+  return launch<true, true>(p, A, rope, in_f32, st);
 }
 
 }  // namespace adsa

@@ -205,11 +205,14 @@ __device__ __forceinline__ void move_scores(gfloat* score, gint* pos, int rows, 
 // 512 x 24 x 696 1.01.  (One in 20 at a row end: the move is ahead everywhere, by 1.02 to 1.2.)
 constexpr int kMovedWithCache = 12, kPlanRowsCap = 128, kPlanRowsSeqs = 128, kManyRows = 24;
 
+struct NoPages {};
+
 // plan[b] = { old n_res, first slot that moves, did compact, new n_res }
-template <int NT, int S, int RB = rank_batch(S)>
+// PAGED: a sequence that evicts has its rows in pages, all of which have to be pages of the pool.
+template <int NT, int S, int RB = rank_batch(S), bool PAGED = false>
 __global__ __launch_bounds__(NT, S == 1 ? 7 : 1) void k_compact_plan(
     uint32_t seqs_lo, uint32_t map_lo, uint32_t plan_lo, uint32_t vs_lo, uint32_t seqs_map_hi, uint32_t plan_vs_hi, uint32_t cap_arg, uint32_t flags,
-    int total, int W, int R, int recent_m, float inv_w, int dim) {
+    int total, int W, int R, int recent_m, float inv_w, int dim, std::conditional_t<PAGED, PageArgs, NoPages> pages) {
   __shared__ __align__(16) RankShared sh;
   constexpr int NW = NT / kWave;
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & (kWave - 1), cap = (int)cap_arg;
@@ -229,6 +232,21 @@ __global__ __launch_bounds__(NT, S == 1 ? 7 : 1) void k_compact_plan(
   const bool row_end = active && n >= 0 && n <= cap &&
                        (streaming ? (s >= 1 && s <= total && n == cap && !(reuse && sq.hole != 0))
                                   : is_row_end(cell, s, total));
+  if constexpr (PAGED) {
+    if (row_end && n > 0) {                                  // (uniform)
+      const gint* const table = (const gint*)pages.table + (size_t)b * pages.table_stride;
+      bool bad = false;
+      for (int i = tid; i <= (n - 1) >> pages.shift; i += NT) bad |= (uint32_t)elem(table, i) >= (uint32_t)pages.n_pages;
+      if (__syncthreads_or(bad)) {
+        if (tid == 0) {
+          plan[4 * b + 0] = 0; plan[4 * b + 1] = 0; plan[4 * b + 2] = 0; plan[4 * b + 3] = n;
+          sq.compacted = 0;
+          sq.status = ADSA_SEQ_BAD_STATE;
+        }
+        return;
+      }
+    }
+  }
   if (!row_end) {
     if (tid == 0) {
       plan[4 * b + 0] = 0; plan[4 * b + 1] = 0; plan[4 * b + 2] = 0; plan[4 * b + 3] = n;
@@ -374,14 +392,17 @@ __global__ __launch_bounds__(NT, S == 1 ? 7 : 1) void k_compact_plan(
 // alone: with nothing to move, 512 sequences x 24 rows x 696 slots 18.9 | 18.0, 300 x 24 x 1000 14.4 | 13.9, 261 x 48 x 435 20.2 | 19.0.
 constexpr int kSliceLanes = 8;
 struct MoveStrides { long long slot_b, head_b; };
-template <int ROWS, bool SCORES, bool ADVANCE>
-__global__ __launch_bounds__(kMoveThreads) void k_compact_move(const adsa_seq* seqs, const int32_t* keep_map, const int32_t* plan,
-                                                              int part_bits, int cap, MoveStrides stride) {
+// PAGED: rows lie in pages; the sequence's row of the table is in LDS before the first row is asked for.
+template <int ROWS, bool SCORES, bool ADVANCE, bool PAGED>
+__device__ __forceinline__ void compact_move(const adsa_seq* seqs, const int32_t* keep_map, const int32_t* plan, int part_bits, int cap,
+                                             std::conditional_t<PAGED, PageArgs, MoveStrides> stride) {
   constexpr int kPass = kMoveThreads / kSliceLanes;
   const int b = blockIdx.z, head = blockIdx.x >> part_bits, part = blockIdx.x & ((1 << part_bits) - 1);
   const int4 pl = reinterpret_cast<const int4*>(plan)[b];
   gseq& sq = ((gseq*)seqs)[b];
-  gchar* const cache = (gchar*)(blockIdx.y == 0 ? sq.k : sq.v);
+  gchar* cache;
+  if constexpr (PAGED) cache = (gchar*)(blockIdx.y == 0 ? stride.k : stride.v);
+  else cache = (gchar*)(blockIdx.y == 0 ? sq.k : sq.v);
   const int step = ADVANCE ? sq.step : -1, status = ADVANCE ? sq.status : 0;
   asm volatile("" : : "s"(cache));                           // (asked for together with the plan's words, not after them)
   if constexpr (ADVANCE) asm volatile("" : : "s"(step), "s"(status));
@@ -392,7 +413,21 @@ __global__ __launch_bounds__(kMoveThreads) void k_compact_move(const adsa_seq* s
   }
   if (pl.z == 0 || first >= n_old) return;
   const int row_in_pass = threadIdx.x / kSliceLanes, lane = threadIdx.x % kSliceLanes;
-  gchar* const base = cache + (long long)head * stride.head_b + (part * kSliceLanes + lane) * 16;
+  __shared__ int s_units[PAGED ? kMostEntries : 1];
+  long long head_b;
+  if constexpr (PAGED) {
+    head_b = stride.head_stride_b;
+    const PageEntries<kMoveThreads> entries(SlotList((const gint*)stride.table + (size_t)b * stride.table_stride, min(stride.table_stride, kMostEntries)));
+    (void)entries.put(s_units, stride.n_pages, stride.page_units, 0);          // (looked at by the plan)
+    __syncthreads();
+  } else head_b = stride.head_b;
+  gchar* const base = cache + (long long)head * head_b + (part * kSliceLanes + lane) * 16;
+  auto row_at = [&](int slot) {
+    if constexpr (PAGED) {
+      const int units = s_units[slot >> stride.shift] + (int)__umul24((uint32_t)slot & ((1u << stride.shift) - 1u), stride.slot_units);
+      return base + ((uint64_t)(uint32_t)units << stride.unit_shift);
+    } else return base + (long long)slot * stride.slot_b;
+  };
   const gint* const map = (const gint*)keep_map + (size_t)b * cap;
   // one workgroup per head also moves the head's score row (attention mass: a row per cache head), where the plan leaves it: see kMovedWithCache
   constexpr int kTile = kPass * ROWS, SLOTS = (kTile + kMoveThreads - 1) / kMoveThreads;
@@ -417,19 +452,29 @@ __global__ __launch_bounds__(kMoveThreads) void k_compact_move(const adsa_seq* s
     for (int u = 0; u < ROWS; ++u) {
       const int i = t0 + u * kPass + row_in_pass;
       if (i >= n_old || dst[u] == i) dst[u] = -1;            // (past the end, or stays where it is)
-      if (dst[u] >= 0) val[u] = load_stream16(base + (long long)i * stride.slot_b);
+      if (dst[u] >= 0) val[u] = load_stream16(row_at(i));
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // this thread's rows are in registers ...
     __syncthreads();                                         // ... and so are everybody's, before any of them is overwritten
 #pragma unroll
     for (int u = 0; u < ROWS; ++u)
-      if (dst[u] >= 0) store_stream16(base + (long long)dst[u] * stride.slot_b, val[u]);
+      if (dst[u] >= 0) store_stream16(row_at(dst[u]), val[u]);
     if (scores) {
 #pragma unroll
       for (int u = 0; u < SLOTS; ++u)
         if (sdst[u] >= 0) elem(score, (uint32_t)sdst[u]) = sval[u];
     }
   }
+}
+
+template <int ROWS, bool SCORES, bool ADVANCE>
+__global__ __launch_bounds__(kMoveThreads) void k_compact_move(const adsa_seq* seqs, const int32_t* keep_map, const int32_t* plan,
+                                                              int part_bits, int cap, MoveStrides stride) {
+  compact_move<ROWS, SCORES, ADVANCE, false>(seqs, keep_map, plan, part_bits, cap, stride);
+}
+template <int ROWS, bool SCORES>
+__global__ __launch_bounds__(kMoveThreads) void k_paged_move(const adsa_seq* seqs, const int32_t* keep_map, const int32_t* plan, int part_bits, int cap, PageArgs pages) {
+  compact_move<ROWS, SCORES, false, true>(seqs, keep_map, plan, part_bits, cap, pages);
 }
 
 // This workgroup's column slice (blockIdx.x: those of K, then those of V) of the rows first .. n, moved in place by the map in LDS.
@@ -716,7 +761,7 @@ static hipError_t launch_compact_plan(const adsa_params& p, adsa_seq* seqs, int3
 #define ADSA_PLAN(...)                                                                                                                          \
   ADSA_RANK_LAUNCH(k_compact_plan, ADSA_SHAPE(__VA_ARGS__), lo32(seqs), lo32(keep_map), lo32(plan), lo32(vcos_s), hi16s(seqs, keep_map),          \
                    hi16s(plan, vcos_s), (uint32_t)p.cap, rank_flags(p, advance_step, moved_with_cache(p)), p.grid_h * p.grid_w, p.grid_w, p.win_rows_back, \
-                   p.win_recent_m, inv_width(p), p.n_heads * p.head_dim)
+                   p.win_recent_m, inv_width(p), p.n_heads * p.head_dim, NoPages{})
   if (p.cap <= 256) ADSA_PLAN(256, 1);
   if (p.cap <= 512) ADSA_PLAN(256, 2);
   if (p.cap <= 768) ADSA_PLAN(256, 3, 12);
@@ -778,6 +823,27 @@ hipError_t launch_step_finish(const adsa_params& p, adsa_seq* seqs, int32_t* kee
   return hipErrorInvalidValue;
 }
 
+// The same over pages (no ranking by V there).
+static hipError_t launch_paged_plan(const adsa_params& p, const PageArgs& pages, adsa_seq* seqs, int32_t* keep_map, int32_t* plan, bool advance_step, hipStream_t st) {
+  const float* const none = nullptr;
+#define ADSA_PAGED_PLAN(NT, S, RB)                                                                                                              \
+  do {                                                                                                                                          \
+    hipLaunchKernelGGL((k_compact_plan<NT, S, RB, true>), dim3(p.n_seq), dim3(NT), 0, st, lo32(seqs), lo32(keep_map), lo32(plan), lo32(none),     \
+                       hi16s(seqs, keep_map), hi16s(plan, none), (uint32_t)p.cap, rank_flags(p, advance_step, moved_with_cache(p)),               \
+                       p.grid_h * p.grid_w, p.grid_w, p.win_rows_back, p.win_recent_m, inv_width(p), p.n_heads * p.head_dim, pages);              \
+    return hipGetLastError();                                                                                                                   \
+  } while (0)
+  if (p.cap <= 256) ADSA_PAGED_PLAN(256, 1, rank_batch(1));
+  if (p.cap <= 512) ADSA_PAGED_PLAN(256, 2, rank_batch(2));
+  if (p.cap <= 768) ADSA_PAGED_PLAN(256, 3, 12);
+  if (p.cap <= 1024) ADSA_PAGED_PLAN(512, 2, rank_batch(2));
+  if (p.cap <= 2048) ADSA_PAGED_PLAN(512, 4, rank_batch(4));
+  if (p.cap <= 3072) ADSA_PAGED_PLAN(512, 6, rank_batch(6));
+  if (p.cap <= 4096) ADSA_PAGED_PLAN(1024, 4, rank_batch(4));
+  if (p.cap <= 6144) ADSA_PAGED_PLAN(1024, 6, rank_batch(6));
+  ADSA_PAGED_PLAN(1024, 8, rank_batch(8));
+}
+
 static hipError_t launch_move(const adsa_params& p, const adsa_seq* seqs, const int32_t* keep_map, const int32_t* plan, bool scores, bool advance, hipStream_t st) {
   const dim3 grid(p.n_heads << slice_bits(p), 2, p.n_seq);
   constexpr int rows_per_pass = kMoveThreads / kSliceLanes;
@@ -804,6 +870,24 @@ hipError_t launch_compact(const adsa_params& p, adsa_seq* seqs, int32_t* keep_ma
   hipError_t e = launch_compact_plan(p, seqs, keep_map, plan, advance_step, vcos_s, st);
   if (e != hipSuccess || p.evict_policy == ADSA_EVICT_REUSE_SLOT) return e;     // slot reuse moves no row
   return launch_move(p, seqs, keep_map, plan, moved_with_cache(p), false, st);
+}
+
+hipError_t launch_compact_paged(const adsa_params& p, const PageArgs& pages, adsa_seq* seqs, int32_t* keep_map, char* ws, const Workspace& w, bool advance_step,
+                                hipStream_t st) {
+  int32_t* const plan = reinterpret_cast<int32_t*>(ws + w.plan_off);
+  const hipError_t e = launch_paged_plan(p, pages, seqs, keep_map, plan, advance_step, st);
+  if (e != hipSuccess || p.evict_policy == ADSA_EVICT_REUSE_SLOT) return e;     // slot reuse moves no row
+  const dim3 grid(p.n_heads << slice_bits(p), 2, p.n_seq);
+  constexpr int rows_per_pass = kMoveThreads / kSliceLanes;
+  auto of_rows = [&](auto with_scores) {             // (see launch_move)
+    constexpr bool S = decltype(with_scores)::value;
+    constexpr int kLeast = S ? 8 : 4;
+    return p.cap <= kLeast * rows_per_pass ? k_paged_move<kLeast, S> : p.cap <= 8 * rows_per_pass ? k_paged_move<8, S>
+         : p.cap <= 16 * rows_per_pass ? k_paged_move<16, S> : k_paged_move<24, S>;
+  };
+  auto move = moved_with_cache(p) ? of_rows(std::true_type()) : of_rows(std::false_type());
+  hipLaunchKernelGGL(move, grid, dim3(kMoveThreads), 0, st, seqs, keep_map, plan, slice_bits(p), p.cap, pages);
+  return hipGetLastError();
 }
 
 hipError_t launch_step_move(const adsa_params& p, adsa_seq* seqs, const int32_t* keep_map, char* ws, const Workspace& w, hipStream_t st) {
