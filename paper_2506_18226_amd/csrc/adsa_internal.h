@@ -199,6 +199,7 @@ hipError_t launch_compact_paged(const adsa_params& p, const PageArgs& pages, ads
                                 hipStream_t st);
 
 // ---- sampling (sample.hip)
+hipError_t sample_prepare_kernels();
 hipError_t launch_sample(const adsa_sampling& s, const adsa_seq* seqs, const void* logits, const float* uniform, int32_t* token, float* logprob, hipStream_t st);
 
 // What a paged call runs with: parameters with the strides of a dense cache (nobody reads them as strides), and the pools (paged_api.hip).

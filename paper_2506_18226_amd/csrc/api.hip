@@ -88,7 +88,9 @@ int ensure_device_ready() {
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return ADSA_ERR_LAUNCH;
   if (!g_device_ready[dev]) {
-    if (gqa_prepare_kernels() != hipSuccess || vcos_prepare_kernels() != hipSuccess || prompt_prepare_kernels() != hipSuccess) return ADSA_ERR_LAUNCH;
+    if (gqa_prepare_kernels() != hipSuccess || vcos_prepare_kernels() != hipSuccess || prompt_prepare_kernels() != hipSuccess ||
+        sample_prepare_kernels() != hipSuccess)
+      return ADSA_ERR_LAUNCH;
     g_device_ready[dev] = true;
   }
   return ADSA_OK;

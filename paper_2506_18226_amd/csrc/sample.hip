@@ -1,13 +1,15 @@
 // The next token of every row of logits (adsa_sample): temperature, top-k, top-p and min-p, from a random number that the caller brings.
 //
-//  k_sample<EB, NT, VEC>: a workgroup takes a row, and reads it again in every pass over it.
-//  What is kept of a row is always the front of its descending order, so it is known by its last one: (z, index), and a logit is in if its z is
+//  k_sample<EB, NT, BINS, VEC>: a workgroup takes a row.  It reads it once and keeps it in LDS as far as that goes (28672 logits); what is beyond is read again in every pass.
+//  What is kept of a row by top-k and top-p is the front of its descending order, so it is known by its last one: (z, index), and a logit is in if its z is
 //  larger, or the same and its index no larger.  That last one is found without sorting: logits are counted, and their weights summed, by
-//  kBins steps of z below the largest; the bin in which a limit falls is looked at logit by logit.  A bin that holds more than kList of them (many
-//  equal ones) is narrowed bit by bit instead.
+//  BINS steps of z below the largest; running sums over the bins say in which bin a limit falls (for top-p behind top-k between which ones, since the sum
+//  it is a share of is known to a bin's weight by then), and those bins' logits, some dozens, are listed in one more pass and ranked against each other.  Where
+//  they are more than kList (many equal ones), the last one is found bit by bit instead.
 //  Weights are whole numbers of 2^-44 of the largest one's: their sums do not depend on an order, and what is less than half of that is nothing.  They are formed in 64
 //  bits, since a token is decided by where a random number falls among up to 2^18 of them: with weights good to 2^-24 every thousandth row of a large
 //  vocabulary would get its neighbour.
+//  The passes: the largest; bins (rows with top-k or top-p); lists; the candidates' weight by groups of 256; the group that the random number falls in.
 #include <type_traits>
 
 #include "adsa_device.h"
@@ -26,11 +28,12 @@ struct SampleArgs {
   const float *temperatures, *top_ps, *min_ps;       // or NULL
   const int32_t* top_ks;
   long long stride_b;
-  int n_rows, vocab, guided, top_k;
+  int n_rows, vocab, guided, top_k, held;            // held: groups of a wave that stay in LDS
   float guidance, temperature, top_p, min_p;
 };
 
-constexpr int kBins = 1024, kList = 1024;
+constexpr int kGroup = 4 * kWave;        // logits of a group: 4 consecutive ones to a lane
+constexpr int kList = 512;
 constexpr float kReach = 31.25f;         // e^-31.25 < 2^-45: what is further below the largest (in temperatures) weighs nothing
 constexpr double kOne = 17592186044416.0;            // 2^44
 
@@ -39,26 +42,20 @@ __device__ __forceinline__ uint32_t order_of(float z) {            // ascending 
   return u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u);
 }
 
-// exp((z - top) / T) in 64 bits, by 2^(j / 32) from a table and a polynomial: off by some 2^-51 of it.
+// exp((z - top) / T) in 64 bits, by 2^(j / 32) from a table and a polynomial: off by some 2^-49 of it.  (z: live, see k_sample)
 struct Weigh {
   const double* table;         // 2^(j / 32), LDS
-  double inv;                  // 32 log2(e) / T
-  float top;
-  __device__ __forceinline__ double share(float z, int* steps) const {     // share * 2^(steps / 32)
-    const double x = z == top ? 0.0 : fmax(((double)z - (double)top) * inv, -2048.0);
-    const double n = __builtin_rint(x), r = (x - n) * (0.69314718055994530942 / 32.0);
-    *steps = (int)n;
-    return table[*steps & 31] * fma(r, fma(r, fma(r, fma(r, fma(r, 1.0 / 120.0, 1.0 / 24.0), 1.0 / 6.0), 0.5), 1.0), 1.0);
+  double inv, top;             // 32 log2(e) / T; the largest logit
+  __device__ __forceinline__ double operator()(float z) const {
+    const double x = ((double)z - top) * inv, n = __builtin_rint(x), r = x - n;
+    constexpr double a = 0.69314718055994530942 / 32.0;            // ln(2) / 32
+    const int steps = (int)n;
+    const double p = fma(r, fma(r, fma(r, fma(r, fma(r, a * a * a * a * a / 120.0, a * a * a * a / 24.0), a * a * a / 6.0), a * a / 2.0), a), 1.0);
+    return __builtin_ldexp(table[steps & 31] * p, steps >> 5);
   }
-  __device__ __forceinline__ double exact(float z) const {
-    int n;
-    const double s = share(z, &n);
-    return __builtin_ldexp(s, n >> 5);
-  }
-  static __device__ __forceinline__ u64 whole(double w) {                  // rounded to a whole number of 2^-44
+  static __device__ __forceinline__ u64 whole(double w) {          // rounded to a whole number of 2^-44
     return (u64)__double_as_longlong(fma(w, kOne, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
   }
-  __device__ __forceinline__ u64 operator()(float z) const { return whole(exact(z)); }
 };
 
 template <int X, typename T>
@@ -79,23 +76,28 @@ __device__ __forceinline__ T wave_sum(T x) {
   return x;
 }
 
-template <int NT>
+template <int NT, int BINS>
 struct SampleShared {
   static constexpr int NW = NT / kWave;
   double table[32];
-  u64 weight[kBins];           // of a bin, then of it and those before
+  union {
+    u64 weight[BINS];          // of a bin
+    u64 group_weight[NT];      // of a group
+  };
   u64 list_weight[kList];
   u64 wave_weight[2][NW];
-  uint32_t count[kBins];
+  uint32_t count[BINS];
   uint32_t list_key[kList];
-  int list_index[kList];
+  int list_index[kList], list_bin[kList];
   uint32_t wave_count[2][NW];
-  float wave_top[NW];
-  u64 above_weight;            // what comes before the bin that a limit falls in
-  uint32_t above_count, n_list;
-  int bin, last_index, token;
-  uint32_t last_key;
-  float token_z;
+  float wave_top[NW], wave_least[NW];
+  // the bins that limits fall in: top-k's; the first and the last that top-p's can be; what comes before them
+  uint32_t above_count, k_count;
+  u64 above_weight, k_weight, p_above;
+  int k_bin, p_first, p_last;
+  uint32_t n_listed, n_list, last_key;
+  int last_index, token, group;
+  u64 left;
 };
 
 // Where a row's candidates end: the last one in descending order.  Nothing set: key 0, and every index.
@@ -105,10 +107,11 @@ struct Last {
   __device__ __forceinline__ bool holds(uint32_t k, int i) const { return k > key || (k == key && i <= index); }
 };
 
-template <int EB, int NT, bool VEC>
+template <int EB, int NT, int BINS, bool VEC>
 __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
   constexpr int NW = NT / kWave;
-  __shared__ SampleShared<NT> sh;
+  extern __shared__ __align__(16) float s_held[];    // [group of a wave][NT][4]
+  __shared__ SampleShared<NT, BINS> sh;
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), r = blockIdx.x, V = A.vocab;
   const bool guided = A.guided != 0;
   if (A.seqs) {
@@ -122,14 +125,13 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
       return;
     }
   }
-  if (tid < 32) sh.table[tid] = exp2((double)tid / 32.0);
-  for (int i = tid; i < kBins; i += NT) { sh.weight[i] = 0; sh.count[i] = 0; }
   const float T = A.temperatures ? A.temperatures[r] : A.temperature, top_p = A.top_ps ? A.top_ps[r] : A.top_p, min_p = A.min_ps ? A.min_ps[r] : A.min_p;
+  const float u = A.uniform[r];
   const int top_k = A.top_ks ? A.top_ks[r] : A.top_k;
   const gchar* const row = (const gchar*)A.logits + (long long)r * A.stride_b;
   const gchar* const partner = row + (long long)A.n_rows * A.stride_b;
-  // ---- logits: a wave takes consecutive ones, a group 256 of them, a lane 4
-  const int groups = (V + NT * 4 - 1) / (NT * 4), first = wave * groups * 256 + lane * 4;
+  // ---- logits: a wave takes consecutive ones, group by group
+  const int groups = (V + NT * 4 - 1) / (NT * 4), held = min(A.held, groups), first = wave * groups * kGroup + lane * 4;
   auto read4 = [&](const gchar* from, int i, float (&f)[4]) {
     if constexpr (VEC) {
       if (i < V) {                                   // (V is a multiple of 4)
@@ -150,41 +152,42 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
       }
     }
   };
-  auto read_group = [&](int g, float (&z)[4]) {
-    const int i = first + g * 256;
+  auto read_group = [&](int g, float (&z)[4]) {      // from memory
+    const int i = first + g * kGroup;
     read4(row, i, z);
     if (guided) {
-      float u[4];
-      read4(partner, i, u);
+      float f4[4];
+      read4(partner, i, f4);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
 #pragma clang fp contract(off)
-        const double c = z[e], f = u[e], step = c - f, far = (double)A.guidance * step;
+        const double c = z[e], f = f4[e], step = c - f, far = (double)A.guidance * step;
         z[e] = i + e < V ? (float)(f + far) : -INFINITY;
       }
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) z[e] = z[e] != z[e] ? -INFINITY : z[e];
   };
-  // f(logit, index) for each of the thread's, in ascending order
-  auto each_logit = [&](auto f) {
-    for (int g = 0; g < groups; ++g) {
-      float z[4];
-      read_group(g, z);
+  // ---- the largest, and the least that is finite
+  float top = -INFINITY, least_z = INFINITY;
+#pragma unroll 4
+  for (int g = 0; g < groups; ++g) {
+    float z[4];
+    read_group(g, z);
+    if (g < held) *reinterpret_cast<float4*>(s_held + (g * NT + tid) * 4) = make_float4(z[0], z[1], z[2], z[3]);
+    top = fmaxf(fmaxf(top, fmaxf(z[0], z[1])), fmaxf(z[2], z[3]));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) f(z[e], first + g * 256 + e);
-    }
-  };
-  // ---- the largest
-  float top = -INFINITY;
-  each_logit([&](float z, int) { top = fmaxf(top, z); });
+    for (int e = 0; e < 4; ++e) least_z = fminf(least_z, z[e] == -INFINITY ? INFINITY : z[e]);
+  }
 #pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-  if (lane == 0) sh.wave_top[wave] = top;
-  if (tid == 0) { sh.token = V; sh.n_list = 0; }
+  for (int d = 1; d < kWave; d <<= 1) { top = fmaxf(top, __shfl_xor(top, d)); least_z = fminf(least_z, __shfl_xor(least_z, d)); }
+  if (lane == 0) { sh.wave_top[wave] = top; sh.wave_least[wave] = least_z; }
+  if (tid < 32) sh.table[tid] = exp2((double)tid / 32.0);
+  for (int i = tid; i < BINS; i += NT) { sh.weight[i] = 0; sh.count[i] = 0; }
+  if (tid == 0) { sh.token = V; sh.n_list = 0; sh.n_listed = 0; }
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < NW; ++w) top = fmaxf(top, sh.wave_top[w]);
+  for (int w = 0; w < NW; ++w) { top = fmaxf(top, sh.wave_top[w]); least_z = fminf(least_z, sh.wave_least[w]); }
   auto finish = [&](int token, float logprob) {
     A.token[r] = token;
     if (guided) A.token[A.n_rows + r] = token;
@@ -194,6 +197,28 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
     if (tid == 0) finish(-1, -INFINITY);
     return;
   }
+  const bool infinite = top == INFINITY;             // then only the infinities are candidates: as 0, and the others as -infinity
+  top = infinite ? 0.0f : top;
+  auto group_of = [&](int g, float (&z)[4]) {
+    if (g < held) {
+      const float4 x = *reinterpret_cast<const float4*>(s_held + (g * NT + tid) * 4);
+      z[0] = x.x; z[1] = x.y; z[2] = x.z; z[3] = x.w;
+    } else read_group(g, z);
+    if (infinite) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[e] = z[e] == INFINITY ? 0.0f : -INFINITY;
+    }
+  };
+  // f(logit, index) for each of the thread's, in ascending order
+  auto each_logit = [&](auto f) {
+#pragma unroll 2
+    for (int g = 0; g < groups; ++g) {
+      float z[4];
+      group_of(g, z);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f(z[e], first + g * kGroup + e);
+    }
+  };
   if (!(T > 0.0f)) {
     int at = V;
     each_logit([&](float z, int i) { at = z == top ? min(at, i) : at; });
@@ -204,11 +229,11 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
     if (tid == 0) finish(sh.token, 0.0f);
     return;
   }
-  const Weigh weigh = {sh.table, 46.166241308446830 / (double)T, top};                 // 32 log2(e)
-  const float reach = fminf(kReach * T, 1e38f), per_bin = (float)kBins / reach;
-  auto below = [&](float z) { return z == top ? 0.0f : top - z; };
-  auto live = [&](float z) { return below(z) <= reach; };
-  auto bin_of = [&](float z) { return min((int)(below(z) * per_bin), kBins - 1); };
+  const double inv = 46.166241308446828384 / (double)T;                    // 32 log2(e) / T
+  const Weigh weigh = {sh.table, inv, (double)top};
+  const float reach = fminf(kReach * T, 1e38f), range = fminf(reach, infinite ? 1.0f : top - least_z), per_bin = range > 0.0f ? (float)BINS / range : 0.0f;
+  auto live = [&](float z) { return top - z <= reach; };
+  auto bin_of = [&](float z) { return min((int)((top - z) * per_bin), BINS - 1); };
   const bool by_count = top_k > 0 && top_k < V, by_sum = top_p < 1.0f;
   Last last = {0u, 0x7FFFFFFF};
   // sums of a count and a weight over the workgroup
@@ -224,24 +249,30 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
     for (int k = 0; k < NW; ++k) { *all_n += sh.wave_count[turn][k]; *all_w += sh.wave_weight[turn][k]; }
     turn ^= 1;                                       // (the next sum writes elsewhere: one barrier each)
   };
+  auto enough_of = [&](u64 total) {                  // the least whole number that reaches top_p's share, 1 at least
+    const double share = (double)fmaxf(top_p, 0.0f) * (double)total;
+    u64 e = (u64)share;
+    if ((double)e < share) ++e;
+    return e < 1 ? (u64)1 : e > total ? total : e;
+  };
   if (by_count || by_sum) {
     each_logit([&](float z, int) {
       if (live(z)) {
         const int b = bin_of(z);
         atomicAdd(&sh.count[b], 1u);
-        atomicAdd(&sh.weight[b], weigh(z));
+        if (by_sum) atomicAdd(&sh.weight[b], Weigh::whole(weigh(z)));
       }
     });
     __syncthreads();
     // running sums over the bins, PB of them a thread
-    constexpr int PB = kBins / NT > 1 ? kBins / NT : 1;
+    constexpr int PB = BINS / NT;
+    static_assert(PB * NT == BINS, "whole bins");
     uint32_t n[PB], n_sum = 0;
     u64 w[PB], w_sum = 0;
-    const bool scans = tid * PB < kBins;
 #pragma unroll
     for (int k = 0; k < PB; ++k) {
-      n[k] = scans ? sh.count[tid * PB + k] : 0u;
-      w[k] = scans ? sh.weight[tid * PB + k] : 0ull;
+      n[k] = sh.count[tid * PB + k];
+      w[k] = sh.weight[tid * PB + k];
       n_sum += n[k];
       w_sum += w[k];
     }
@@ -258,174 +289,222 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
       total += sh.wave_weight[0][k];
     }
     turn = 1;
-    // The last one before which fewer than `most` logits lie (by_n), or less than `enough` of weight, among those that `last` holds.  The bin in which
-    // that falls is found from the running sums; its own logits, few as a rule, are ranked against each other.
-    auto cut = [&](bool by_n, uint32_t most, u64 enough) {
+    const bool counts = by_count && (uint32_t)top_k < n_live;
+    auto each_bin = [&](auto f) {                    // f(bin, count before it, count, weight before it, weight)
       uint32_t nb = n_at;
       u64 wb = w_at;
-      __syncthreads();                               // (the list and the words below have been read)
-      if (tid == 0) sh.n_list = 0;
 #pragma unroll
       for (int k = 0; k < PB; ++k) {
-        const bool here = by_n ? nb < most && most <= nb + n[k] : wb < enough && enough <= wb + w[k];
-        if (here) { sh.bin = tid * PB + k; sh.above_count = nb; sh.above_weight = wb; }
+        f(tid * PB + k, nb, n[k], wb, w[k]);
         nb += n[k];
         wb += w[k];
       }
+    };
+    if (counts) {
+      each_bin([&](int bin, uint32_t nb, uint32_t c, u64 wb, u64 s) {
+        if (nb < (uint32_t)top_k && (uint32_t)top_k <= nb + c) { sh.k_bin = bin; sh.above_count = nb; sh.k_count = c; sh.above_weight = wb; sh.k_weight = s; }
+      });
       __syncthreads();
-      const int bin = sh.bin;
-      const uint32_t above_n = sh.above_count;
-      const u64 above_w = sh.above_weight;
-      const uint32_t in_bin = sh.count[bin];
-      if (in_bin <= (uint32_t)kList) {               // (uniform)
-        each_logit([&](float z, int i) {
-          if (live(z) && bin_of(z) == bin && last.holds(order_of(z), i)) {
-            const uint32_t at = atomicAdd(&sh.n_list, 1u);
-            sh.list_key[at] = order_of(z);
-            sh.list_index[at] = i;
-            sh.list_weight[at] = weigh(z);
-          }
-        });
-        __syncthreads();
-        const int m = (int)sh.n_list;
+    }
+    const int k_bin = counts ? sh.k_bin : -1;
+    int p_first = -1, p_last = -1;
+    if (by_sum) {                                    // the sum that top_p is a share of is between these two
+      const u64 least = counts ? sh.above_weight : total, most = counts ? least + sh.k_weight : total;
+      const u64 lo = enough_of(least), hi = enough_of(most);
+      each_bin([&](int bin, uint32_t, uint32_t, u64 wb, u64 s) {
+        if (wb < lo && lo <= wb + s) { sh.p_first = bin; sh.p_above = wb; }
+        if (wb < hi && hi <= wb + s) sh.p_last = bin;
+      });
+      __syncthreads();
+      p_first = sh.p_first;
+      p_last = sh.p_last;
+    }
+    auto listed = [&](int bin) { return bin == k_bin || (bin >= p_first && bin <= p_last); };
+    each_bin([&](int bin, uint32_t, uint32_t c, u64, u64) {
+      if (listed(bin) && c != 0) atomicAdd(&sh.n_listed, c);
+    });
+    __syncthreads();
+    const int m = (int)sh.n_listed;                  // (none: no limit cuts anything off)
+    if (m > 0 && m <= kList) {
+      each_logit([&](float z, int i) {
+        if (live(z) && listed(bin_of(z))) {
+          const uint32_t at = atomicAdd(&sh.n_list, 1u);
+          sh.list_key[at] = order_of(z);
+          sh.list_index[at] = i;
+          sh.list_bin[at] = bin_of(z);
+          if (by_sum) sh.list_weight[at] = Weigh::whole(weigh(z));
+        }
+      });
+      __syncthreads();
+      if (counts) {                                  // the one behind which top_k logits end, of its bin
+        const uint32_t wanted = (uint32_t)top_k - sh.above_count;
         for (int i = tid; i < m; i += NT) {
           const Last me = {sh.list_key[i], sh.list_index[i]};
-          uint32_t before_n = above_n;
-          u64 before_w = above_w;
-          for (int j = 0; j < m; ++j)
-            if (j != i && me.holds(sh.list_key[j], sh.list_index[j])) { ++before_n; before_w += sh.list_weight[j]; }
-          const bool ends = by_n ? before_n == most - 1 : before_w < enough && enough <= before_w + sh.list_weight[i];
-          if (ends) { sh.last_key = me.key; sh.last_index = me.index; }
+          uint32_t rank = 0;                         // itself included
+          for (int j = 0; j < m; ++j) rank += sh.list_bin[j] == k_bin && me.holds(sh.list_key[j], sh.list_index[j]);
+          if (sh.list_bin[i] == k_bin && rank == wanted) { sh.last_key = me.key; sh.last_index = me.index; }
         }
         __syncthreads();
-      } else {
-        // the largest key from which on there is enough, then, among its logits, the lowest index up to which
+        last = {sh.last_key, sh.last_index};
+      }
+      if (by_sum) {                                  // the one behind which there is enough of what that leaves
+        if (counts) {
+          total = sh.above_weight;
+          for (int j = 0; j < m; ++j)
+            if (sh.list_bin[j] == k_bin && last.holds(sh.list_key[j], sh.list_index[j])) total += sh.list_weight[j];
+        }
+        const u64 enough = enough_of(total), above = sh.p_above;
+        __syncthreads();                             // (last_key and last_index have been read)
+        for (int i = tid; i < m; i += NT) {
+          const Last me = {sh.list_key[i], sh.list_index[i]};
+          u64 upto = above;                          // itself included
+          for (int j = 0; j < m; ++j)
+            if (sh.list_bin[j] <= p_last && me.holds(sh.list_key[j], sh.list_index[j])) upto += sh.list_weight[j];
+          if (sh.list_bin[i] <= p_last && upto >= enough && upto - sh.list_weight[i] < enough) { sh.last_key = me.key; sh.last_index = me.index; }
+        }
+        __syncthreads();
+        last = {sh.last_key, sh.last_index};
+      }
+    } else if (m > 0) {
+      // Many equal logits: the largest key from which on there is enough, then, among that key's logits, the lowest index up to which.
+      auto cut = [&](bool by_n, uint32_t most, u64 enough) {
         const Last held_by = last;
-        uint32_t key = 0, cn;
-        u64 cw;
+        auto sum = [&](auto in, uint32_t* all_n, u64* all_w) {
+          uint32_t c = 0;
+          u64 x = 0;
+          each_logit([&](float z, int i) {
+            const uint32_t k = order_of(z);
+            if (live(z) && held_by.holds(k, i) && in(k, i)) { ++c; x += by_n ? 0 : Weigh::whole(weigh(z)); }
+          });
+          block_sum(c, x, all_n, all_w);
+        };
+        uint32_t key = 0, cn, on;
+        u64 cw, ow;
         for (int bit = 31; bit >= 0; --bit) {
           const uint32_t from = key | 1u << bit;
-          uint32_t c = 0;
-          u64 s = 0;
-          each_logit([&](float z, int i) {
-            const uint32_t k = order_of(z);
-            if (live(z) && k >= from && held_by.holds(k, i)) { ++c; s += weigh(z); }
-          });
-          block_sum(c, s, &cn, &cw);
+          sum([&](uint32_t k, int) { return k >= from; }, &cn, &cw);
           if (by_n ? cn >= most : cw >= enough) key = from;
         }
-        int index = -1;                              // fewer than enough up to here
-        uint32_t c = 0;
-        u64 s = 0;
-        each_logit([&](float z, int i) {
-          const uint32_t k = order_of(z);
-          if (live(z) && k > key && held_by.holds(k, i)) { ++c; s += weigh(z); }
-        });
-        uint32_t on;
-        u64 ow;
-        block_sum(c, s, &on, &ow);
+        sum([&](uint32_t k, int) { return k > key; }, &on, &ow);
+        int index = -1;                              // not enough up to here
         for (int bit = 17; bit >= 0; --bit) {
           const int upto = index + (1 << bit);
-          c = 0;
-          s = 0;
-          each_logit([&](float z, int i) {
-            const uint32_t k = order_of(z);
-            if (live(z) && k == key && i <= upto && held_by.holds(k, i)) { ++c; s += weigh(z); }
-          });
-          block_sum(c, s, &cn, &cw);
+          sum([&](uint32_t k, int i) { return k == key && i <= upto; }, &cn, &cw);
           if (!(by_n ? on + cn >= most : ow + cw >= enough)) index = upto;
         }
-        __syncthreads();
-        if (tid == 0) { sh.last_key = key; sh.last_index = index + 1; }
-        __syncthreads();
+        last = {key, index + 1};
+      };
+      if (counts) {
+        cut(true, (uint32_t)top_k, 0);
+        if (by_sum) {
+          uint32_t c;
+          u64 mine = 0;
+          each_logit([&](float z, int i) { mine += live(z) && last.holds(order_of(z), i) ? Weigh::whole(weigh(z)) : 0; });
+          block_sum(0, mine, &c, &total);
+        }
       }
-      last.key = sh.last_key;
-      last.index = sh.last_index;
-    };
-    if (by_count && (uint32_t)top_k < n_live) {
-      cut(true, (uint32_t)top_k, 0);
-      if (by_sum) {
-        uint32_t c = 0, all;
-        u64 s = 0;
-        each_logit([&](float z, int i) {
-          if (live(z) && last.holds(order_of(z), i)) { ++c; s += weigh(z); }
-        });
-        block_sum(c, s, &all, &total);
-      }
+      if (by_sum) cut(false, 0, enough_of(total));
     }
-    if (by_sum) {
-      const double share = (double)fmaxf(top_p, 0.0f) * (double)total;
-      u64 enough = (u64)share;
-      if ((double)enough < share) ++enough;          // as few as reach it
-      cut(false, 0, enough < 1 ? 1 : enough > total ? total : enough);
-    }
+    __syncthreads();                                 // (the bins, whose place the groups take, and the sums have been read)
   }
-  // ---- the candidates' whole weight, by waves, and where the random number falls
+  // ---- the candidates' weight by groups, and the group that the random number falls in
   const double least = min_p > 0.0f ? (double)fminf(min_p, 1.0f) : 0.0;
   auto weight_of = [&](float z, int i) -> u64 {
     if (!live(z) || !last.holds(order_of(z), i)) return 0;
-    const double w = weigh.exact(z);
+    const double w = weigh(z);
     return w >= least ? Weigh::whole(w) : 0;
-  };
-  u64 mine = 0;
-  each_logit([&](float z, int i) { mine += weight_of(z, i); });
-  mine = wave_sum(mine);
-  __syncthreads();
-  if (lane == 0) sh.wave_weight[0][wave] = mine;
-  __syncthreads();
-  u64 all = 0;
-#pragma unroll
-  for (int k = 0; k < NW; ++k) all += sh.wave_weight[0][k];
-  const float u = A.uniform[r];
-  const double at = (u >= 0.0f ? (double)fminf(u, 0.99999994f) : 0.0) * (double)all;
-  u64 target = (u64)at;
-  target = target < all ? target : all - 1;
-  u64 before = 0;
-#pragma unroll
-  for (int k = 0; k < NW; ++k)
-    if (k < wave) before += sh.wave_weight[0][k];
-  if (target < before || target - before >= mine) return;            // (uniform in the wave: the one it falls in goes on)
-  u64 left = target - before;
-  auto find = [&](float (&z)[4], int g) {            // whether it is in group g
-    const int i = first + g * 256;
-    u64 w[4], sum = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) { w[e] = weight_of(z[e], i + e); sum += w[e]; }
-    const u64 upto = wave_scan(sum), group = __shfl(upto, kWave - 1);
-    if (left >= group) { left -= group; return false; }
-    u64 from = upto - sum;
-    if (left >= from && left < upto) {
-      int e = 0;
-#pragma unroll
-      for (int k = 0; k < 3; ++k)
-        if (e == k && left - from >= w[k]) { from += w[k]; ++e; }
-      const float ze = e == 0 ? z[0] : e == 1 ? z[1] : e == 2 ? z[2] : z[3];
-      const double d = ze == top ? 0.0 : ((double)ze - (double)top) / (double)T;
-      finish(i + e, (float)(d - log((double)all * (1.0 / kOne))));
-    }
-    return true;
   };
   for (int g = 0; g < groups; ++g) {
     float z[4];
-    read_group(g, z);
-    if (find(z, g)) break;
+    group_of(g, z);
+    u64 sum = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum += weight_of(z[e], first + g * kGroup + e);
+    if (__ballot(sum != 0) != 0) sum = wave_sum(sum);
+    if (lane == 0) sh.group_weight[wave * groups + g] = sum;
+  }
+  __syncthreads();
+  {
+    const u64 mine = tid < NW * groups ? sh.group_weight[tid] : 0, upto = wave_scan(mine);
+    if (lane == kWave - 1) sh.wave_weight[0][wave] = upto;
+    __syncthreads();
+    u64 before = upto - mine, all = 0;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) {
+      before += k < wave ? sh.wave_weight[0][k] : 0;
+      all += sh.wave_weight[0][k];
+    }
+    u64 target = (u64)((u >= 0.0f ? (double)fminf(u, 0.99999994f) : 0.0) * (double)all);
+    target = target < all ? target : all - 1;
+    if (target >= before && target - before < mine) { sh.group = tid; sh.left = target - before; sh.above_weight = all; }
+    __syncthreads();
+  }
+  // ---- its own logits
+  if (wave != sh.group / groups) return;
+  const u64 left = sh.left;
+  float z[4];
+  group_of(sh.group % groups, z);
+  const int i = first + sh.group % groups * kGroup;
+  u64 w[4], sum = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) { w[e] = weight_of(z[e], i + e); sum += w[e]; }
+  const u64 upto = wave_scan(sum);
+  u64 from = upto - sum;
+  if (left >= from && left < upto) {
+    int e = 0;
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (e == k && left - from >= w[k]) { from += w[k]; ++e; }
+    const float ze = e == 0 ? z[0] : e == 1 ? z[1] : e == 2 ? z[2] : z[3];
+    finish(i + e, (float)(((double)ze - (double)top) / (double)T - log((double)sh.above_weight * (1.0 / kOne))));
   }
 }
 
-template <int EB, int NT>
-hipError_t launch_n(const SampleArgs& A, bool vec, hipStream_t st) {
-  if (vec) k_sample<EB, NT, true><<<dim3((unsigned)A.n_rows), NT, 0, st>>>(A);
-  else k_sample<EB, NT, false><<<dim3((unsigned)A.n_rows), NT, 0, st>>>(A);
+// Threads, bins and logits in LDS by the vocabulary: bins as many as leave some 200 logits of a row's densest part to one, LDS beside them for logits.
+template <int NT, int BINS>
+constexpr int kHeld = (160 * 1024 - 256 - (int)sizeof(SampleShared<NT, BINS>)) / (NT * 16);       // groups of a wave
+
+template <int EB, int NT, int BINS>
+hipError_t launch_n(SampleArgs A, bool vec, hipStream_t st) {
+  A.held = (A.vocab + NT * 4 - 1) / (NT * 4);
+  const int most = kHeld<NT, BINS>;
+  A.held = A.held < most ? A.held : most;
+  const size_t lds = (size_t)A.held * NT * 16;
+  if (vec) k_sample<EB, NT, BINS, true><<<dim3((unsigned)A.n_rows), NT, lds, st>>>(A);
+  else k_sample<EB, NT, BINS, false><<<dim3((unsigned)A.n_rows), NT, lds, st>>>(A);
   return hipGetLastError();
 }
 
 template <int EB>
 hipError_t launch_e(const SampleArgs& A, hipStream_t st) {
   const bool vec = A.vocab % 4 == 0 && reinterpret_cast<uintptr_t>(A.logits) % (4 * EB) == 0 && A.stride_b % (4 * EB) == 0;
-  return A.vocab <= 4096 ? launch_n<EB, 256>(A, vec, st) : launch_n<EB, 1024>(A, vec, st);
+  if (A.vocab <= 4096) return launch_n<EB, 256, 1024>(A, vec, st);
+  if (A.vocab <= 65536) return launch_n<EB, 1024, 2048>(A, vec, st);
+  return launch_n<EB, 1024, 8192>(A, vec, st);
 }
 
 }  // namespace
+
+hipError_t sample_prepare_kernels() {
+  hipError_t e = hipSuccess;
+  auto allow = [&](auto kernel, int bytes) {
+    if (e == hipSuccess) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  };
+  auto both = [&](auto eb, auto nt, auto bins) {
+    constexpr int EB = decltype(eb)::value, NT = decltype(nt)::value, BINS = decltype(bins)::value;
+    allow(k_sample<EB, NT, BINS, true>, kHeld<NT, BINS> * NT * 16);
+    allow(k_sample<EB, NT, BINS, false>, kHeld<NT, BINS> * NT * 16);
+  };
+  auto sizes = [&](auto eb) {
+    using std::integral_constant;
+    both(eb, integral_constant<int, 256>(), integral_constant<int, 1024>());
+    both(eb, integral_constant<int, 1024>(), integral_constant<int, 2048>());
+    both(eb, integral_constant<int, 1024>(), integral_constant<int, 8192>());
+  };
+  sizes(std::integral_constant<int, 2>());
+  sizes(std::integral_constant<int, 4>());
+  return e;
+}
 
 hipError_t launch_sample(const adsa_sampling& s, const adsa_seq* seqs, const void* logits, const float* uniform, int32_t* token, float* logprob, hipStream_t st) {
   SampleArgs A = {};
