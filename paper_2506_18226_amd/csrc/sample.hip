@@ -3,13 +3,13 @@
 //  k_sample<EB, NT, BINS, VEC>: a workgroup takes a row.  It reads it once and keeps it in LDS as far as that goes (28672 logits); what is beyond is read again in every pass.
 //  What is kept of a row by top-k and top-p is the front of its descending order, so it is known by its last one: (z, index), and a logit is in if its z is
 //  larger, or the same and its index no larger.  That last one is found without sorting: logits are counted, and their weights summed, by
-//  BINS steps of z below the largest; running sums over the bins say in which bin a limit falls (for top-p behind top-k between which ones, since the sum
-//  it is a share of is known to a bin's weight by then), and those bins' logits, some dozens, are listed in one more pass and ranked against each other.  Where
-//  they are more than kList (many equal ones), the last one is found bit by bit instead.
+//  BINS steps of z below the largest; running sums over the bins say in which bin a limit falls, and that bin's logits, some dozens, are listed in one more
+//  pass and ranked against each other.  Where they are more than kList (many equal ones), the last one is found bit by bit instead.
 //  Weights are whole numbers of 2^-44 of the largest one's: their sums do not depend on an order, and what is less than half of that is nothing.  They are formed in 64
 //  bits, since a token is decided by where a random number falls among up to 2^18 of them: with weights good to 2^-24 every thousandth row of a large
 //  vocabulary would get its neighbour.
-//  The passes: the largest; bins (rows with top-k or top-p); lists; the candidates' weight by groups of 256; the group that the random number falls in.
+//  The passes: the largest; bins (rows with top-k or top-p); a list for each limit; the candidates' weight by runs of 1024; the run that the random number falls in.
+//  What bounds it: memory for the first pass, from then on what the vector unit issues, about 18 instructions a weight, twice a logit.
 #include <type_traits>
 
 #include "adsa_device.h"
@@ -33,6 +33,7 @@ struct SampleArgs {
 };
 
 constexpr int kGroup = 4 * kWave;        // logits of a group: 4 consecutive ones to a lane
+constexpr int kRun = 4;                  // groups of a run, whose weight is kept
 constexpr int kList = 512;
 constexpr float kReach = 31.25f;         // e^-31.25 < 2^-45: what is further below the largest (in temperatures) weighs nothing
 constexpr double kOne = 17592186044416.0;            // 2^44
@@ -42,62 +43,56 @@ __device__ __forceinline__ uint32_t order_of(float z) {            // ascending 
   return u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u);
 }
 
-// exp((z - top) / T) in 64 bits, by 2^(j / 32) from a table and a polynomial: off by some 2^-49 of it.  (z: live, see k_sample)
+// The weight of a live logit (see k_sample): exp((z - top) / T) * 2^44, by 2^(j / 32) from a table and a polynomial of degree 5, off by some 2^-49 of it, rounded
+// to a whole number.  Sums' low bits do the rounding: x + kRound holds the nearest whole number of x in its low bits, and w + 2^52 that of w.
 struct Weigh {
-  const double* table;         // 2^(j / 32), LDS
+  static constexpr double kRound = 6755399441055744.0;             // 1.5 * 2^52
+  const double* table;         // 2^(44 + j / 32), LDS
   double inv, top;             // 32 log2(e) / T; the largest logit
-  __device__ __forceinline__ double operator()(float z) const {
-    const double x = ((double)z - top) * inv, n = __builtin_rint(x), r = x - n;
+  __device__ __forceinline__ u64 operator()(float z) const {
     constexpr double a = 0.69314718055994530942 / 32.0;            // ln(2) / 32
-    const int steps = (int)n;
+    const double d = (double)z - top, t = fma(d, inv, kRound), r = fma(d, inv, kRound - t);
+    const int steps = (int)(uint32_t)__double_as_longlong(t);
     const double p = fma(r, fma(r, fma(r, fma(r, fma(r, a * a * a * a * a / 120.0, a * a * a * a / 24.0), a * a * a / 6.0), a * a / 2.0), a), 1.0);
-    return __builtin_ldexp(table[steps & 31] * p, steps >> 5);
-  }
-  static __device__ __forceinline__ u64 whole(double w) {          // rounded to a whole number of 2^-44
-    return (u64)__double_as_longlong(fma(w, kOne, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
+    const u64 power = (u64)__double_as_longlong(table[steps & 31]) + ((u64)(uint32_t)(steps >> 5) << 52);         // (2^-2 at least: an exponent that there is)
+    return (u64)__double_as_longlong(fma(__longlong_as_double((long long)power), p, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
   }
 };
 
-template <int X, typename T>
-__device__ __forceinline__ T from_below(T x, T none) {            // of lane - X
-  const T y = __shfl_up(x, X);
-  return (int)(threadIdx.x % kWave) >= X ? y : none;
-}
+// x of the lane that CTRL names, 0 where there is none; of the rows of lanes in ROWS only
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t moved(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xF, true); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 moved(u64 x) { return (u64)moved<CTRL, ROWS>((uint32_t)(x >> 32)) << 32 | moved<CTRL, ROWS>((uint32_t)x); }
+// running sums over the wave: within rows of 16, then the row before, then the lower half
 template <typename T>
 __device__ __forceinline__ T wave_scan(T x) {
-  x += from_below<1>(x, (T)0); x += from_below<2>(x, (T)0); x += from_below<4>(x, (T)0);
-  x += from_below<8>(x, (T)0); x += from_below<16>(x, (T)0); x += from_below<32>(x, (T)0);
+  x += moved<0x111, 0xF>(x); x += moved<0x112, 0xF>(x); x += moved<0x114, 0xF>(x); x += moved<0x118, 0xF>(x);          // row_shr
+  x += moved<0x142, 0xA>(x);                         // row_bcast:15 to rows 1 and 3
+  x += moved<0x143, 0xC>(x);                         // row_bcast:31 to rows 2 and 3
   return x;
 }
+__device__ __forceinline__ uint32_t lane_of(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
+__device__ __forceinline__ u64 lane_of(u64 x, int lane) { return (u64)lane_of((uint32_t)(x >> 32), lane) << 32 | lane_of((uint32_t)x, lane); }
 template <typename T>
-__device__ __forceinline__ T wave_sum(T x) {
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) x += __shfl_xor(x, d);
-  return x;
-}
+__device__ __forceinline__ T wave_sum(T x) { return lane_of(wave_scan(x), kWave - 1); }
 
 template <int NT, int BINS>
 struct SampleShared {
   static constexpr int NW = NT / kWave;
   double table[32];
-  union {
-    u64 weight[BINS];          // of a bin
-    u64 group_weight[NT];      // of a group
-  };
+  u64 weight[BINS];            // of a bin
   u64 list_weight[kList];
+  u64 run_weight[NT / kRun];
   u64 wave_weight[2][NW];
+  u64 above_weight, left;      // weight before the bin that a limit falls in; of a run before the random number
   uint32_t count[BINS];
   uint32_t list_key[kList];
-  int list_index[kList], list_bin[kList];
+  int list_index[kList];
   uint32_t wave_count[2][NW];
   float wave_top[NW], wave_least[NW];
-  // the bins that limits fall in: top-k's; the first and the last that top-p's can be; what comes before them
-  uint32_t above_count, k_count;
-  u64 above_weight, k_weight, p_above;
-  int k_bin, p_first, p_last;
-  uint32_t n_listed, n_list, last_key;
-  int last_index, token, group;
-  u64 left;
+  uint32_t above_count, n_list, last_key;
+  int bin, last_index, token, run;
 };
 
 // Where a row's candidates end: the last one in descending order.  Nothing set: key 0, and every index.
@@ -131,7 +126,7 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
   const gchar* const row = (const gchar*)A.logits + (long long)r * A.stride_b;
   const gchar* const partner = row + (long long)A.n_rows * A.stride_b;
   // ---- logits: a wave takes consecutive ones, group by group
-  const int groups = (V + NT * 4 - 1) / (NT * 4), held = min(A.held, groups), first = wave * groups * kGroup + lane * 4;
+  const int groups = (V + NT * 4 - 1) / (NT * 4), runs = (groups + kRun - 1) / kRun, held = min(A.held, groups), first = wave * groups * kGroup + lane * 4;
   auto read4 = [&](const gchar* from, int i, float (&f)[4]) {
     if constexpr (VEC) {
       if (i < V) {                                   // (V is a multiple of 4)
@@ -182,9 +177,9 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
 #pragma unroll
   for (int d = 1; d < kWave; d <<= 1) { top = fmaxf(top, __shfl_xor(top, d)); least_z = fminf(least_z, __shfl_xor(least_z, d)); }
   if (lane == 0) { sh.wave_top[wave] = top; sh.wave_least[wave] = least_z; }
-  if (tid < 32) sh.table[tid] = exp2((double)tid / 32.0);
+  if (tid < 32) sh.table[tid] = exp2((double)tid / 32.0) * kOne;
   for (int i = tid; i < BINS; i += NT) { sh.weight[i] = 0; sh.count[i] = 0; }
-  if (tid == 0) { sh.token = V; sh.n_list = 0; sh.n_listed = 0; }
+  if (tid == 0) { sh.token = V; sh.n_list = 0; }
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < NW; ++w) { top = fmaxf(top, sh.wave_top[w]); least_z = fminf(least_z, sh.wave_least[w]); }
@@ -233,7 +228,7 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
   const Weigh weigh = {sh.table, inv, (double)top};
   const float reach = fminf(kReach * T, 1e38f), range = fminf(reach, infinite ? 1.0f : top - least_z), per_bin = range > 0.0f ? (float)BINS / range : 0.0f;
   auto live = [&](float z) { return top - z <= reach; };
-  auto bin_of = [&](float z) { return min((int)((top - z) * per_bin), BINS - 1); };
+  auto bin_of = [&](float below) { return min((int)(below * per_bin), BINS - 1); };            // below the largest
   const bool by_count = top_k > 0 && top_k < V, by_sum = top_p < 1.0f;
   Last last = {0u, 0x7FFFFFFF};
   // sums of a count and a weight over the workgroup
@@ -257,10 +252,11 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
   };
   if (by_count || by_sum) {
     each_logit([&](float z, int) {
-      if (live(z)) {
-        const int b = bin_of(z);
+      const float below = top - z;
+      if (below <= reach) {
+        const int b = bin_of(below);
         atomicAdd(&sh.count[b], 1u);
-        if (by_sum) atomicAdd(&sh.weight[b], Weigh::whole(weigh(z)));
+        if (by_sum) atomicAdd(&sh.weight[b], weigh(z));
       }
     });
     __syncthreads();
@@ -289,143 +285,132 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
       total += sh.wave_weight[0][k];
     }
     turn = 1;
-    const bool counts = by_count && (uint32_t)top_k < n_live;
-    auto each_bin = [&](auto f) {                    // f(bin, count before it, count, weight before it, weight)
-      uint32_t nb = n_at;
-      u64 wb = w_at;
-#pragma unroll
-      for (int k = 0; k < PB; ++k) {
-        f(tid * PB + k, nb, n[k], wb, w[k]);
-        nb += n[k];
-        wb += w[k];
-      }
+    // (what can be in the bin lies between `from` and `to`, a bin's width to either side: two comparisons for nearly all)
+    const float width = range / (float)BINS;
+    auto in_bin = [&](float z, int bin) {
+      const float below = top - z, from = ((float)bin - 1.0f) * width, to = bin == BINS - 1 || per_bin == 0.0f ? INFINITY : ((float)bin + 2.0f) * width;
+      return below >= from && below < to && below <= reach && bin_of(below) == bin;
     };
-    if (counts) {
-      each_bin([&](int bin, uint32_t nb, uint32_t c, u64 wb, u64 s) {
-        if (nb < (uint32_t)top_k && (uint32_t)top_k <= nb + c) { sh.k_bin = bin; sh.above_count = nb; sh.k_count = c; sh.above_weight = wb; sh.k_weight = s; }
-      });
-      __syncthreads();
-    }
-    const int k_bin = counts ? sh.k_bin : -1;
-    int p_first = -1, p_last = -1;
-    if (by_sum) {                                    // the sum that top_p is a share of is between these two
-      const u64 least = counts ? sh.above_weight : total, most = counts ? least + sh.k_weight : total;
-      const u64 lo = enough_of(least), hi = enough_of(most);
-      each_bin([&](int bin, uint32_t, uint32_t, u64 wb, u64 s) {
-        if (wb < lo && lo <= wb + s) { sh.p_first = bin; sh.p_above = wb; }
-        if (wb < hi && hi <= wb + s) sh.p_last = bin;
-      });
-      __syncthreads();
-      p_first = sh.p_first;
-      p_last = sh.p_last;
-    }
-    auto listed = [&](int bin) { return bin == k_bin || (bin >= p_first && bin <= p_last); };
-    each_bin([&](int bin, uint32_t, uint32_t c, u64, u64) {
-      if (listed(bin) && c != 0) atomicAdd(&sh.n_listed, c);
-    });
-    __syncthreads();
-    const int m = (int)sh.n_listed;                  // (none: no limit cuts anything off)
-    if (m > 0 && m <= kList) {
-      each_logit([&](float z, int i) {
-        if (live(z) && listed(bin_of(z))) {
-          const uint32_t at = atomicAdd(&sh.n_list, 1u);
-          sh.list_key[at] = order_of(z);
-          sh.list_index[at] = i;
-          sh.list_bin[at] = bin_of(z);
-          if (by_sum) sh.list_weight[at] = Weigh::whole(weigh(z));
+    // The last one up to which there are `most` logits, or `enough` of weight, among those that `last` holds.
+    auto cut = [&](bool by_n, uint32_t most, u64 enough) {
+      {
+        uint32_t nb = n_at;
+        u64 wb = w_at;
+#pragma unroll
+        for (int k = 0; k < PB; ++k) {
+          if (by_n ? nb < most && most <= nb + n[k] : wb < enough && enough <= wb + w[k]) { sh.bin = tid * PB + k; sh.above_count = nb; sh.above_weight = wb; sh.n_list = 0; }
+          nb += n[k];
+          wb += w[k];
         }
-      });
+      }
       __syncthreads();
-      if (counts) {                                  // the one behind which top_k logits end, of its bin
-        const uint32_t wanted = (uint32_t)top_k - sh.above_count;
-        for (int i = tid; i < m; i += NT) {
+      const int bin = sh.bin;
+      if (sh.count[bin] <= (uint32_t)kList) {        // (uniform)
+        each_logit([&](float z, int i) {
+          if (in_bin(z, bin) && last.holds(order_of(z), i)) {
+            const uint32_t at = atomicAdd(&sh.n_list, 1u);
+            sh.list_key[at] = order_of(z);
+            sh.list_index[at] = i;
+            if (by_sum) sh.list_weight[at] = weigh(z);
+          }
+        });
+        __syncthreads();
+        // a wave ranks an entry: its lanes are the entries that may come before it (or are it)
+        const int m = (int)sh.n_list;
+        for (int i = wave; i < m; i += NW) {
           const Last me = {sh.list_key[i], sh.list_index[i]};
-          uint32_t rank = 0;                         // itself included
-          for (int j = 0; j < m; ++j) rank += sh.list_bin[j] == k_bin && me.holds(sh.list_key[j], sh.list_index[j]);
-          if (sh.list_bin[i] == k_bin && rank == wanted) { sh.last_key = me.key; sh.last_index = me.index; }
+          uint32_t rank = sh.above_count;
+          u64 upto = 0;
+          for (int j0 = 0; j0 < m; j0 += kWave) {
+            const int j = j0 + lane;
+            const bool in = j < m && me.holds(sh.list_key[min(j, m - 1)], sh.list_index[min(j, m - 1)]);
+            rank += (uint32_t)__popcll(__ballot(in));
+            if (!by_n) upto += in ? sh.list_weight[j] : 0;
+          }
+          bool ends = rank == most;
+          if (!by_n) {
+            upto = sh.above_weight + wave_sum(upto);
+            ends = upto >= enough && upto - sh.list_weight[i] < enough;
+          }
+          if (ends && lane == 0) { sh.last_key = me.key; sh.last_index = me.index; }
         }
         __syncthreads();
         last = {sh.last_key, sh.last_index};
+        return;
       }
-      if (by_sum) {                                  // the one behind which there is enough of what that leaves
-        if (counts) {
-          total = sh.above_weight;
-          for (int j = 0; j < m; ++j)
-            if (sh.list_bin[j] == k_bin && last.holds(sh.list_key[j], sh.list_index[j])) total += sh.list_weight[j];
-        }
-        const u64 enough = enough_of(total), above = sh.p_above;
-        __syncthreads();                             // (last_key and last_index have been read)
-        for (int i = tid; i < m; i += NT) {
-          const Last me = {sh.list_key[i], sh.list_index[i]};
-          u64 upto = above;                          // itself included
-          for (int j = 0; j < m; ++j)
-            if (sh.list_bin[j] <= p_last && me.holds(sh.list_key[j], sh.list_index[j])) upto += sh.list_weight[j];
-          if (sh.list_bin[i] <= p_last && upto >= enough && upto - sh.list_weight[i] < enough) { sh.last_key = me.key; sh.last_index = me.index; }
-        }
-        __syncthreads();
-        last = {sh.last_key, sh.last_index};
-      }
-    } else if (m > 0) {
       // Many equal logits: the largest key from which on there is enough, then, among that key's logits, the lowest index up to which.
-      auto cut = [&](bool by_n, uint32_t most, u64 enough) {
-        const Last held_by = last;
-        auto sum = [&](auto in, uint32_t* all_n, u64* all_w) {
-          uint32_t c = 0;
-          u64 x = 0;
-          each_logit([&](float z, int i) {
-            const uint32_t k = order_of(z);
-            if (live(z) && held_by.holds(k, i) && in(k, i)) { ++c; x += by_n ? 0 : Weigh::whole(weigh(z)); }
-          });
-          block_sum(c, x, all_n, all_w);
-        };
-        uint32_t key = 0, cn, on;
-        u64 cw, ow;
-        for (int bit = 31; bit >= 0; --bit) {
-          const uint32_t from = key | 1u << bit;
-          sum([&](uint32_t k, int) { return k >= from; }, &cn, &cw);
-          if (by_n ? cn >= most : cw >= enough) key = from;
-        }
-        sum([&](uint32_t k, int) { return k > key; }, &on, &ow);
-        int index = -1;                              // not enough up to here
-        for (int bit = 17; bit >= 0; --bit) {
-          const int upto = index + (1 << bit);
-          sum([&](uint32_t k, int i) { return k == key && i <= upto; }, &cn, &cw);
-          if (!(by_n ? on + cn >= most : ow + cw >= enough)) index = upto;
-        }
-        last = {key, index + 1};
+      const Last held_by = last;
+      auto sum = [&](auto in, uint32_t* all_n, u64* all_w) {
+        uint32_t c = 0;
+        u64 x = 0;
+        each_logit([&](float z, int i) {
+          const uint32_t k = order_of(z);
+          if (live(z) && held_by.holds(k, i) && in(k, i)) { ++c; x += by_n ? 0 : weigh(z); }
+        });
+        block_sum(c, x, all_n, all_w);
       };
-      if (counts) {
-        cut(true, (uint32_t)top_k, 0);
-        if (by_sum) {
-          uint32_t c;
-          u64 mine = 0;
-          each_logit([&](float z, int i) { mine += live(z) && last.holds(order_of(z), i) ? Weigh::whole(weigh(z)) : 0; });
-          block_sum(0, mine, &c, &total);
-        }
+      uint32_t key = 0, cn, on;
+      u64 cw, ow;
+      for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t from = key | 1u << bit;
+        sum([&](uint32_t k, int) { return k >= from; }, &cn, &cw);
+        if (by_n ? cn >= most : cw >= enough) key = from;
       }
-      if (by_sum) cut(false, 0, enough_of(total));
+      sum([&](uint32_t k, int) { return k > key; }, &on, &ow);
+      int index = -1;                                // not enough up to here
+      for (int bit = 17; bit >= 0; --bit) {
+        const int upto = index + (1 << bit);
+        sum([&](uint32_t k, int i) { return k == key && i <= upto; }, &cn, &cw);
+        if (!(by_n ? on + cn >= most : ow + cw >= enough)) index = upto;
+      }
+      last = {key, index + 1};
+    };
+    if (by_count && (uint32_t)top_k < n_live) {
+      cut(true, (uint32_t)top_k, 0);
+      if (by_sum) {                                  // the sum that top_p is a share of: whole bins, and what is left of the one that top-k ends in
+        const int bin = sh.bin;
+        const u64 above = sh.above_weight;
+        uint32_t none;
+        u64 mine = 0;
+        if (sh.count[bin] <= (uint32_t)kList) {      // (listed, without those that are left out: any entry's weight counts if it is held)
+          const int m = (int)sh.n_list;
+          for (int j = tid; j < m; j += NT) {
+            if (last.holds(sh.list_key[j], sh.list_index[j])) mine += sh.list_weight[j];
+          }
+        } else {
+          each_logit([&](float z, int i) {
+            if (in_bin(z, bin) && last.holds(order_of(z), i)) mine += weigh(z);
+          });
+        }
+        block_sum(0, mine, &none, &total);
+        total += above;
+      }
     }
-    __syncthreads();                                 // (the bins, whose place the groups take, and the sums have been read)
+    if (by_sum) cut(false, 0, enough_of(total));
+    __syncthreads();
   }
-  // ---- the candidates' weight by groups, and the group that the random number falls in
-  const double least = min_p > 0.0f ? (double)fminf(min_p, 1.0f) : 0.0;
+  // ---- the candidates' weight by runs, and the run that the random number falls in
+  const u64 least = min_p > 0.0f ? (u64)ceil((double)fminf(min_p, 1.0f) * kOne) : 0;
   auto weight_of = [&](float z, int i) -> u64 {
     if (!live(z) || !last.holds(order_of(z), i)) return 0;
-    const double w = weigh(z);
-    return w >= least ? Weigh::whole(w) : 0;
+    const u64 w = weigh(z);
+    return w >= least ? w : 0;
   };
-  for (int g = 0; g < groups; ++g) {
-    float z[4];
-    group_of(g, z);
+  for (int run = 0; run < runs; ++run) {
     u64 sum = 0;
+#pragma unroll 2
+    for (int g = run * kRun; g < min((run + 1) * kRun, groups); ++g) {
+      float z[4];
+      group_of(g, z);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum += weight_of(z[e], first + g * kGroup + e);
-    if (__ballot(sum != 0) != 0) sum = wave_sum(sum);
-    if (lane == 0) sh.group_weight[wave * groups + g] = sum;
+      for (int e = 0; e < 4; ++e) sum += weight_of(z[e], first + g * kGroup + e);
+    }
+    sum = wave_sum(sum);
+    if (lane == 0) sh.run_weight[wave * runs + run] = sum;
   }
   __syncthreads();
   {
-    const u64 mine = tid < NW * groups ? sh.group_weight[tid] : 0, upto = wave_scan(mine);
+    const u64 mine = tid < NW * runs ? sh.run_weight[tid] : 0, upto = wave_scan(mine);
     if (lane == kWave - 1) sh.wave_weight[0][wave] = upto;
     __syncthreads();
     u64 before = upto - mine, all = 0;
@@ -436,27 +421,34 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
     }
     u64 target = (u64)((u >= 0.0f ? (double)fminf(u, 0.99999994f) : 0.0) * (double)all);
     target = target < all ? target : all - 1;
-    if (target >= before && target - before < mine) { sh.group = tid; sh.left = target - before; sh.above_weight = all; }
+    if (target >= before && target - before < mine) { sh.run = tid; sh.left = target - before; sh.above_weight = all; }
     __syncthreads();
   }
   // ---- its own logits
-  if (wave != sh.group / groups) return;
-  const u64 left = sh.left;
-  float z[4];
-  group_of(sh.group % groups, z);
-  const int i = first + sh.group % groups * kGroup;
-  u64 w[4], sum = 0;
+  if (wave != sh.run / runs) return;
+  u64 left = sh.left;
+  for (int g = sh.run % runs * kRun; g < groups; ++g) {
+    const int i = first + g * kGroup;
+    float z[4];
+    group_of(g, z);
+    u64 w[4], sum = 0;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) { w[e] = weight_of(z[e], i + e); sum += w[e]; }
-  const u64 upto = wave_scan(sum);
-  u64 from = upto - sum;
-  if (left >= from && left < upto) {
-    int e = 0;
+    for (int e = 0; e < 4; ++e) { w[e] = weight_of(z[e], i + e); sum += w[e]; }
+    const u64 upto = wave_scan(sum), whole = lane_of(upto, kWave - 1);
+    if (left >= whole) {
+      left -= whole;
+      continue;
+    }
+    u64 from = upto - sum;
+    if (left >= from && left < upto) {
+      int e = 0;
 #pragma unroll
-    for (int k = 0; k < 3; ++k)
-      if (e == k && left - from >= w[k]) { from += w[k]; ++e; }
-    const float ze = e == 0 ? z[0] : e == 1 ? z[1] : e == 2 ? z[2] : z[3];
-    finish(i + e, (float)(((double)ze - (double)top) / (double)T - log((double)sh.above_weight * (1.0 / kOne))));
+      for (int k = 0; k < 3; ++k)
+        if (e == k && left - from >= w[k]) { from += w[k]; ++e; }
+      const float ze = e == 0 ? z[0] : e == 1 ? z[1] : e == 2 ? z[2] : z[3];
+      finish(i + e, (float)(((double)ze - (double)top) / (double)T - log((double)sh.above_weight * (1.0 / kOne))));
+    }
+    break;
   }
 }
 
