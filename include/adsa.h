@@ -422,7 +422,7 @@ typedef struct adsa_pages {    /* [host] */
   void* k;                     /* device: page 0 of the pool of K (dtype elements); 16-byte aligned, as is v */
   void* v;                     /* ... of V; may be the same memory as k, with strides that keep them apart */
   const int32_t* table;        /* device [n_seq][table_stride]: entry i of a row is the page of slots i * page_size .. + page_size - 1 */
-  int64_t page_stride;         /* elements from a page to the next, from a slot's row to the next slot's in a page, and from a */
+  int64_t page_stride;         /* (less than 4 GiB, else ADSA_ERR_UNSUPPORTED) elements from a page to the next, from a slot's row to the next slot's in a page, and from a */
   int64_t slot_stride;         /* head's row to the next head's; multiples of 16 bytes, nested [page][head][slot][D] or */
   int64_t head_stride;         /* [page][slot][head][D] */
   int32_t page_size;           /* slots of a page: a power of two from ADSA_MIN_PAGE to ADSA_MAX_CAP */

@@ -31,7 +31,7 @@ int resolve_paged(const adsa_params* p, const adsa_pages* g, adsa_params* eff, P
   *a = {};
   a->unit_shift = __builtin_ctzll((unsigned long long)((page | slot | head) * eb));
   const int64_t page_units = (page * eb) >> a->unit_shift;
-  if (page_units >= (1ll << 31) || page_units * g->n_pages >= (1ll << 31)) return ADSA_ERR_UNSUPPORTED;
+  if (page * eb >= (1ll << 32) || page_units >= (1ll << 31) || page_units * g->n_pages >= (1ll << 31)) return ADSA_ERR_UNSUPPORTED;
   a->slot_units = (uint32_t)((slot * eb) >> a->unit_shift);
   if (a->slot_units >= (1u << 24)) return ADSA_ERR_UNSUPPORTED;          // (products of 24 bits)
   a->table = g->table;

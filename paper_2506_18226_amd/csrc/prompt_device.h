@@ -92,10 +92,12 @@ struct Keys {
   int pos0;                    // positions are taken from here (slopes): fp32 holds near ones whole, whatever the absolute ones are
   // pages (k and v are then a head's rows of page 0): entry i is the page of slots i << shift on.  Every entry the keys need is a page (paged_job).
   const ADSA_CONST int32_t* table;
-  long long page_stride_b;
+  uint32_t page_stride_b;
   int shift;
-  __device__ __forceinline__ long long page_of(int slot) const { return (long long)table[slot >> shift]; }
+  __device__ __forceinline__ int page_of(int slot) const { return table[slot >> shift]; }
   __device__ __forceinline__ int place_of(int slot) const { return slot & ((1 << shift) - 1); }
+  // of a slot's row from page 0 (a page is less than 4 GiB)
+  __device__ __forceinline__ uint64_t offset(int page, int slot) const { return (uint64_t)(uint32_t)page * page_stride_b + (uint32_t)place_of(slot) * (uint32_t)stride_b; }
 };
 
 // A lane's row: what it sees are keys below `limit` (of its document).
@@ -215,7 +217,7 @@ struct Tile {
   int meta_slot;
   int meta_pos;
   int meta_doc;
-  long long page_next[2];      // PAGED: of the upper and the lower 16 rows of the next step
+  int page_next[2];            // PAGED: of the upper and the lower 16 rows of the next step
 
   __device__ __forceinline__ Tile(const Mods& mods_, const Keys& keys_, lchar* lds_)
       : mods(mods_), keys(keys_), lds(lds_), tid(threadIdx.x), lane(threadIdx.x % kWave), col(lane % 32), half(lane / 32),
@@ -254,8 +256,7 @@ struct Tile {
     for (int i = 0; i < NL; ++i) {
       const int slot = LIST ? slot_of(slot_next[i]) : min(base + staged(i), keys.end - 1);
       // (rows past the last one repeat it: then all of a round's 16 do, and the page is its page)
-      const long long off = PAGED ? page_next[i * RPT / 16] * keys.page_stride_b + ((long long)keys.place_of(slot) * keys.stride_b + (tid % CPR) * 16)
-                                  : (long long)slot * keys.stride_b + (tid % CPR) * 16;
+      const long long off = (PAGED ? (long long)keys.offset(page_next[i * RPT / 16], slot) : (long long)slot * keys.stride_b) + (tid % CPR) * 16;
       kr[i] = load16(keys.k + off);
       vr[i] = load16(keys.v + off);
     }
@@ -653,7 +654,7 @@ struct Flow {
   // with every tile (K's two lie TK * RB apart, an offset's bit of that value says which; so do V's).
   // FEW: registers are short (what is asked for ahead would be spilled, which waits for it), and offsets are formed from the first one's, of whose
   // bits they differ in some.  us without | with: 64 x 8 tokens x 64 heads over 8 x 128 behind 2000 slots, lowered with distance, 213 | 141.
-  static constexpr bool FEW = (MOD || SPLIT) && D == 128;
+  static constexpr bool FEW = (MOD || SPLIT || PAGED) && D == 128;
   static constexpr int KA = FEW ? 1 : KC, VA = FEW ? 1 : DT, RA = FEW ? 1 : NL;
   int k_at[KA], v_at[VA], k_to, v_to;
   uint32_t row_at[RA];         // offsets of the thread's rows of a tile from its first
@@ -695,17 +696,28 @@ struct Flow {
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         v_page[i] = k_page[i];
-        k_page[i] = (int)keys.page_of(min(base + i * RPT + wave * RPW, keys.end - 1));
+        k_page[i] = keys.page_of(min(base + i * RPT + wave * RPW, keys.end - 1));
       }
     }
   }
   __device__ __forceinline__ void load_pages(const gchar* from, int base, uint4 (&r)[NL], const int* page) {
     const int last = keys.end - 1 - base;
+    auto row = [&](int i, int first) { return from + keys.offset(page[i], base + first); };          // (uniform)
+    if (last >= TK - 1) {
+      if (keys.place_of(base) + TK <= 1 << keys.shift) {                               // the tile is on one page, as it is where pages have 64 slots and more
+        const gchar* const at = row(0, wave * RPW);
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int first = min(i * RPT + wave * RPW, last);             // (uniform; rows past the last one repeat it, which is on the same page as they would be)
-      const gchar* const at = from + ((long long)page[i] * keys.page_stride_b + (long long)keys.place_of(base + first) * keys.stride_b);
-      r[i] = load16(at + (last >= TK - 1 ? row_at[0] : (uint32_t)(min(lane / CPR, last - first) * (int)keys.stride_b + (tid % CPR) * 16)));
+        for (int i = 0; i < NL; ++i) r[i] = load16(at + i * RPT * (uint32_t)keys.stride_b + row_at[0]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) r[i] = load16(row(i, i * RPT + wave * RPW) + row_at[0]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {                 // rows past the last one repeat it, which is on the page that they would be on
+        const int first = min(i * RPT + wave * RPW, last);
+        r[i] = load16(row(i, first) + (uint32_t)(min(lane / CPR, last - first) * (int)keys.stride_b + (tid % CPR) * 16));
+      }
     }
   }
   // rows of a tile on their way: 32-bit offsets from the tile's first row, which hold for every tile but a last, shorter one
@@ -1140,7 +1152,7 @@ __device__ __forceinline__ bool job_of(const Args& A, Job& J) {
     keys.k = (const gchar*)A.pages.k + J.head * A.head_stride_b;
     keys.v = (const gchar*)A.pages.v + J.head * A.head_stride_b;
     keys.table = A.table_of(J.b);
-    keys.page_stride_b = A.pages.page_stride_b;
+    keys.page_stride_b = (uint32_t)A.pages.page_stride_b;
     keys.shift = A.pages.shift;
   } else {
     keys.k = (const gchar*)sq.k + J.head * A.head_stride_b;
