@@ -654,7 +654,7 @@ struct Flow {
   // with every tile (K's two lie TK * RB apart, an offset's bit of that value says which; so do V's).
   // FEW: registers are short (what is asked for ahead would be spilled, which waits for it), and offsets are formed from the first one's, of whose
   // bits they differ in some.  us without | with: 64 x 8 tokens x 64 heads over 8 x 128 behind 2000 slots, lowered with distance, 213 | 141.
-  static constexpr bool FEW = (MOD || SPLIT || PAGED) && D == 128;
+  static constexpr bool FEW = PAGED || ((MOD || SPLIT) && D == 128);
   static constexpr int KA = FEW ? 1 : KC, VA = FEW ? 1 : DT, RA = FEW ? 1 : NL;
   int k_at[KA], v_at[VA], k_to, v_to;
   uint32_t row_at[RA];         // offsets of the thread's rows of a tile from its first
