@@ -56,6 +56,9 @@ struct SlotList {
   __device__ __forceinline__ int operator[](int i) const { return (int)__builtin_amdgcn_raw_buffer_load_b32(row, i * 4, 0, 0); }
 };
 
+// How a kernel's rows are reached: slots of a dense cache; pages of a pool below 2 GiB, by 32-bit offsets; of a larger one.
+constexpr int kDense = 0, kNearPages = 1, kFarPages = 2;
+
 // One sequence's row of a page table in LDS, in units (see PageArgs): where each page begins, -1 where an entry is no page.
 // Loads leave at once (entries); put() says whether the thread's entries of the first `need` are pages.
 template <int THREADS>

@@ -181,6 +181,13 @@ struct PageArgs {
   int n_pages, shift, table_stride, unit_shift;      // page_size = 1 << shift; a unit is 1 << unit_shift bytes
   uint32_t page_units, slot_units;
 };
+static inline bool near_pages(const PageArgs& g) { return g.n_pages * g.page_stride_b < (1ll << 31); }
+static inline PageArgs in_bytes(PageArgs g) {        // ... with bytes for units
+  g.unit_shift = 0;
+  g.page_units = (uint32_t)g.page_stride_b;
+  g.slot_units = (uint32_t)g.slot_stride_b;
+  return g;
+}
 constexpr int kMostEntries = ADSA_MAX_CAP / ADSA_MIN_PAGE;       // of a table's row that a sequence can use
 
 hipError_t launch_append_paged(const adsa_params& p, const PageArgs& pages, const adsa_tokens& t, const adsa_rope* rope, adsa_seq* seqs, const void* q,

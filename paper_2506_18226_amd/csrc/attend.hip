@@ -208,13 +208,14 @@ static_assert(sizeof(PagedTail) == 128 && offsetof(PagedTail, k) == 64, "one dwo
 // drawn, and the loads leave after the last ticket has come back, so no cache is written back or invalidated for it.
 // The record's step stays, since workgroups that start later tell a row end from it: the next kernel advances it.
 // PAGED: rows lie in pages.  The sequence's row of the table goes to LDS with the first trip, and the staged list holds, instead of slots, where their
-// rows begin in the pool (in units: see PageArgs), so the loop looks nothing up; rows are reached with 64-bit addresses and masked as with WIDE.  The arguments
-// stride24 and head_stride16 are the table's address and the entries of a row, the head stride's bits of heads_flags the page size.
-template <int EB, int D, int HT, int U, int NW, bool VF, bool DIRECT, bool WIDE, int RANK = 0, int PLAN = 0, bool PAGED = false>
+// rows begin in the pool, so the loop looks nothing up: kNearPages, pools below 2 GiB, bytes, reached as a dense cache's rows are; kFarPages, units (see
+// PageArgs), reached with 64-bit addresses and masked as with WIDE.  32 x 24 lists x 673 x 64, us dense | near | far: 20.6 | 22.0 | 22.9; 2 x 20 x 427 x 64 4.4 | 5.1 | 5.2.
+// The arguments stride24 and head_stride16 are the table's address and the entries of a row, the head stride's bits of heads_flags the page size.
+template <int EB, int D, int HT, int U, int NW, bool VF, bool DIRECT, bool WIDE, int RANK = 0, int PLAN = 0, int PAGED = kDense>
 __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_t idx_lo, uint32_t cnt_lo, uint32_t q_lo, uint32_t kn_lo,
                                                       uint32_t vn_lo, uint32_t seqs_idx_hi, uint32_t cnt_q_hi, uint32_t kn_vn_hi,
                                                       uint32_t heads_flags, uint32_t caps, uint32_t stride24, uint32_t head_stride16,
-                                                      float scale_log2, std::conditional_t<PAGED, PagedTail, std::conditional_t<(RANK > 0), RankTail, std::conditional_t<(PLAN > 0), PlanTail, AttendTail>>> T) {
+                                                      float scale_log2, std::conditional_t<(PAGED != kDense), PagedTail, std::conditional_t<(RANK > 0), RankTail, std::conditional_t<(PLAN > 0), PlanTail, AttendTail>>> T) {
   constexpr int kAttThreads = NW * kWave;           // the waves of the workgroup share one token chunk
   constexpr int EPL = Elems<EB>::N;                 // elements per lane
   constexpr int LPR = D / EPL;                      // lanes per row
@@ -223,7 +224,7 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
   static_assert(RANK == 0 || (HT == 1 && DIRECT && !VF && !WIDE), "ranking: whole lists of one head");
   static_assert(PLAN == 0 || (RANK == 0 && HT == 1 && DIRECT && !VF && !WIDE), "plans: whole lists of one head");
   static_assert(!PAGED || (RANK == 0 && PLAN == 0 && HT == 1 && !VF && !WIDE), "pages: one head, a list that is there");
-  constexpr bool MASKED = WIDE || PAGED;            // what is not attended reads some row, and is masked when it is folded
+  constexpr bool MASKED = WIDE || PAGED == kFarPages;            // what is not attended reads some row, and is masked when it is folded
   constexpr int kSlots = RANK > 0 ? RANK : 1;       // slots per thread of the ranking
   constexpr int PF = 4;                             // list entries a thread fetches, and score read-modify-writes it starts, early
   constexpr int kRev = NW * U * RPW;                // tokens of one ring revolution of the workgroup
@@ -282,7 +283,7 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
   auto tail_address = [&](size_t at) { return address(tail_word(at / 4), tail_word(at / 4 + 1)); };
   if constexpr (RANK > 0 || PAGED) load_tail();
   const int page_shift = PAGED ? (int)(heads_flags >> 19 & 0x1F) : 0, table_stride = PAGED ? (int)(head_stride16 >> 16) : 0;
-  std::conditional_t<PAGED, PageEntries<kAttThreads>, int> page_entries = [&] {
+  std::conditional_t<(PAGED != kDense), PageEntries<kAttThreads>, int> page_entries = [&] {
     if constexpr (PAGED) {
       const gint* const table = (const gint*)address(stride24, head_stride16 & 0xFFFF) + (size_t)b * table_stride;
       return PageEntries<kAttThreads>(SlotList(table, min(table_stride, kMostEntries)));
@@ -517,16 +518,19 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
     };
     // Entries that are not attended read zeros without an access (RowBuffer; an entry that is a slot is at most the offset of its
     // row).  WIDE: they read slot 0 and are masked when they are folded.
-    const RowBuffer ku(k_base + (long long)head0 * head_stride_b), vu(v_base + (long long)head0 * head_stride_b);       // uniform
+    gchar *k_pool = k_base, *v_pool = v_base;
+    if constexpr (PAGED) { k_pool = (gchar*)tail_address(offsetof(PagedTail, k)); v_pool = (gchar*)tail_address(offsetof(PagedTail, v)); }
+    const RowBuffer ku(k_pool + (long long)head0 * head_stride_b), vu(v_pool + (long long)head0 * head_stride_b);       // uniform
     const uint32_t lane32 = (uint32_t)(head - head0) * (uint32_t)head_stride_b + (uint32_t)dl * 16u;
     auto load = [&](const RowBuffer& rows, const gchar* own, int e) -> uint4 {
-      if constexpr (PAGED) return load_stream16(own + ((uint64_t)(uint32_t)max(e, 0) << unit_shift));
+      if constexpr (PAGED == kNearPages) return rows[(uint32_t)e + lane32];
+      else if constexpr (PAGED == kFarPages) return load_stream16(own + ((uint64_t)(uint32_t)max(e, 0) << unit_shift));
       else if constexpr (!WIDE) return rows[max(__umul24((uint32_t)e, stride24) + lane32, (uint32_t)e)];
       else return load_stream16(own + (long long)max(e, 0) * stride_b);
     };
     auto entry = [&](int j, int slot) {
       const bool attended = j < len && slot != new_slot;
-      if constexpr (PAGED) return attended ? units_of(slot) : -1;
+      if constexpr (PAGED) return attended ? units_of(slot) : (int)kRowBufferBytes;     // (negative, and where a near row would read zeros)
       else return list_entry(slot, attended);
     };
     if constexpr (RANK > 0) {                      // the list is in LDS already, but for the entries of no token
@@ -1063,7 +1067,7 @@ hipError_t launch_attend_w(const AttendArgs& A, const AttendPlan& plan, int n_se
 }
 
 // The same over pages, one head a workgroup.
-template <int EB, int D, int NW, bool DIRECT>
+template <int EB, int D, int NW, bool DIRECT, int PAGED>
 hipError_t launch_paged_w(const AttendArgs& A, const PageArgs& pages, const AttendPlan& plan, int n_seq, hipStream_t st) {
   constexpr int U = 4, kRev = NW * U * (kWave * 16 / (D * EB));
   const size_t entries = (size_t)((plan.chunk_max - 1 + kRev - 1) / kRev + 1) * kRev, lds = 2 * entries * sizeof(float);
@@ -1071,7 +1075,7 @@ hipError_t launch_paged_w(const AttendArgs& A, const PageArgs& pages, const Atte
   const PagedTail T = {{A.out, A.lse, A.logits, A.part_ml, A.part_acc, A.lg_stride, A.advance, 0, 0}, pages.k, pages.v, pages.head_stride_b, pages.page_units, pages.slot_units,
                        pages.n_pages, pages.unit_shift, {}};
   const uint32_t table_hi = (uint32_t)(reinterpret_cast<uintptr_t>(pages.table) >> 32 & 0xFFFF) | (uint32_t)pages.table_stride << 16;
-  hipLaunchKernelGGL((k_attend<EB, D, 1, U, NW, false, DIRECT, false, 0, 0, true>), dim3(plan.n_chunks, A.n_heads, n_seq), dim3(NW * kWave), lds, st, lo32(A.seqs), lo32(A.sel_idx),
+  hipLaunchKernelGGL((k_attend<EB, D, 1, U, NW, false, DIRECT, false, 0, 0, PAGED>), dim3(plan.n_chunks, A.n_heads, n_seq), dim3(NW * kWave), lds, st, lo32(A.seqs), lo32(A.sel_idx),
                      lo32(A.sel_cnt), lo32(A.q), lo32(A.k_new), lo32(A.v_new), hi16s(A.seqs, A.sel_idx), hi16s(A.sel_cnt, A.q), hi16s(A.k_new, A.v_new), flags,
                      (uint32_t)A.cap | (uint32_t)A.sel_cap << 16, lo32(pages.table), table_hi, A.scale_log2, T);
   if constexpr (!DIRECT) {
@@ -1347,11 +1351,15 @@ hipError_t launch_attend_paged(const adsa_params& p, const PageArgs& pages, cons
                                bool accumulate, bool append, int advance, bool new_f32, hipStream_t st) {
   if (p.q_per_kv > 1) return launch_attend_gqa_paged(p, pages, plan, seqs, q, k_new, v_new, sel_idx, sel_cnt, out, lse, ws, w, accumulate, append, advance, new_f32, st);
   const AttendArgs A = attend_args(p, plan, seqs, q, k_new, v_new, sel_idx, sel_cnt, out, lse, ws, w, accumulate, append, advance, new_f32);
+  const PageArgs near = in_bytes(pages);
+  auto sized = [&](auto eb, auto d, auto paged, const PageArgs& g) {
+    constexpr int EB = decltype(eb)::value, D = decltype(d)::value, P = decltype(paged)::value;
+    if (plan.n_chunks > 1) return launch_paged_w<EB, D, 8, false, P>(A, g, plan, p.n_seq, st);
+    if (plan.waves == 8) return launch_paged_w<EB, D, 8, true, P>(A, g, plan, p.n_seq, st);
+    return launch_paged_w<EB, D, 4, true, P>(A, g, plan, p.n_seq, st);
+  };
   auto go = [&](auto eb, auto d) {
-    constexpr int EB = decltype(eb)::value, D = decltype(d)::value;
-    if (plan.n_chunks > 1) return launch_paged_w<EB, D, 8, false>(A, pages, plan, p.n_seq, st);
-    if (plan.waves == 8) return launch_paged_w<EB, D, 8, true>(A, pages, plan, p.n_seq, st);
-    return launch_paged_w<EB, D, 4, true>(A, pages, plan, p.n_seq, st);
+    return near_pages(pages) ? sized(eb, d, std::integral_constant<int, kNearPages>(), near) : sized(eb, d, std::integral_constant<int, kFarPages>(), pages);
   };
   using std::integral_constant;
   const integral_constant<int, 2> bf16;

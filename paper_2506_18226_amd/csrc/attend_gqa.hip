@@ -139,13 +139,13 @@ static_assert(sizeof(PagedGqaTail) == 128 && offsetof(PagedGqaTail, k) == 64, "o
 // R: tiles in flight per wave (a ring: the oldest is multiplied, then refilled).
 // (held to the 128 registers that let two 8-wave workgroups share a CU, but for the deep rings)
 // PAGED: rows lie in pages.  The sequence's row of the table goes to LDS with the first trip, and the staged list holds, instead of slots, where their
-// rows begin in the pool (in units: see PageArgs).  The arguments stride32 and head_stride16 are the table's address and the entries of a row,
-// the head stride's bits of heads_flags the page size.
-template <int D, int NW, bool SPLIT, int R, bool PAGED = false>
+// rows begin in the pool: kNearPages bytes, kFarPages units (see PageArgs).  32 x 8 lists x 300 .. 1378 x 128, G = 8, us dense | near | far: 23.7 | 25.2 | 28.7.
+// The arguments stride32 and head_stride16 are the table's address and the entries of a row, the head stride's bits of heads_flags the page size.
+template <int D, int NW, bool SPLIT, int R, int PAGED = kDense>
 __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(uint32_t seqs_lo, uint32_t idx_lo, uint32_t cnt_lo, uint32_t q_lo,
                                                           uint32_t kn_lo, uint32_t vn_lo, uint32_t seqs_idx_hi, uint32_t cnt_q_hi,
                                                           uint32_t kn_vn_hi, uint32_t heads_flags, uint32_t caps, uint32_t stride32,
-                                                          uint32_t head_stride16, float scale_log2, std::conditional_t<PAGED, PagedGqaTail, GqaTail> T) {
+                                                          uint32_t head_stride16, float scale_log2, std::conditional_t<(PAGED != kDense), PagedGqaTail, GqaTail> T) {
   constexpr int kThreads = NW * kWave;
   constexpr int ROWB = D * 2 + 16;          // bytes of a staged K row (padded against bank conflicts)
   constexpr int LPR = D / 8;                // lanes per K row with 16-byte loads
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
   auto tail_address = [&](size_t at) { return address(tail_word(at / 4), tail_word(at / 4 + 1)); };
   const int page_shift = PAGED ? (int)(heads_flags >> 19 & 0x1F) : 0, table_stride = PAGED ? (int)(head_stride16 >> 16) : 0;
   if constexpr (PAGED) load_tail();
-  std::conditional_t<PAGED, PageEntries<kThreads>, int> page_entries = [&] {
+  std::conditional_t<(PAGED != kDense), PageEntries<kThreads>, int> page_entries = [&] {
     if constexpr (PAGED) {
       const gint* const table = (const gint*)address(stride32, head_stride16 & 0xFFFF) + (size_t)b * table_stride;
       return PageEntries<kThreads>(SlotList(table, min(table_stride, kMostEntries)));
@@ -315,7 +315,8 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
   };
   const int new_place = PAGED && new_slot >= 0 ? place_of(new_slot) : new_slot;
   auto row_at = [&](const gchar* base, int place, uint32_t lane_off) {
-    if constexpr (PAGED) return base + (((uint64_t)(uint32_t)place << unit_shift) + lane_off);
+    if constexpr (PAGED == kNearPages) return base + ((uint32_t)place + lane_off);
+    else if constexpr (PAGED == kFarPages) return base + (((uint64_t)(uint32_t)place << unit_shift) + lane_off);
     else return base + ((uint32_t)place * stride32 + lane_off);
   };
 
@@ -726,13 +727,13 @@ hipError_t launch_gqa_w(const GqaArgs& A, int n_seq, int n_chunks, size_t lds, h
 }
 
 // The same over pages.
-template <int D, int NW, bool SPLIT, int R>
+template <int D, int NW, bool SPLIT, int R, int PAGED>
 hipError_t launch_gqa_paged_w(const GqaArgs& A, const PageArgs& pages, int n_seq, int n_chunks, size_t lds, hipStream_t st) {
   const uint32_t flags = A.n_heads | A.G << 9 | (A.append ? 0x10000 : 0) | (A.new_f32 ? 0x20000 : 0) | (A.accumulate ? 0x40000 : 0) | (uint32_t)pages.shift << 19 | n_chunks << 24;
   const PagedGqaTail T = {{A.out, A.lse, A.logits, A.part_ml, A.part_acc, A.lg_global, A.advance, {}}, pages.k, pages.v, pages.head_stride_b, pages.page_units, pages.slot_units,
                           pages.n_pages, pages.unit_shift, {}};
   const uint32_t table_hi = (uint32_t)(reinterpret_cast<uintptr_t>(pages.table) >> 32 & 0xFFFF) | (uint32_t)pages.table_stride << 16;
-  hipLaunchKernelGGL((k_attend_gqa<D, NW, SPLIT, R, true>), dim3(A.n_heads, n_seq, n_chunks), dim3(NW * kWave), lds, st, lo32(A.seqs), lo32(A.sel_idx), lo32(A.sel_cnt), lo32(A.q),
+  hipLaunchKernelGGL((k_attend_gqa<D, NW, SPLIT, R, PAGED>), dim3(A.n_heads, n_seq, n_chunks), dim3(NW * kWave), lds, st, lo32(A.seqs), lo32(A.sel_idx), lo32(A.sel_cnt), lo32(A.q),
                      lo32(A.k_new), lo32(A.v_new), hi16s(A.seqs, A.sel_idx), hi16s(A.sel_cnt, A.q), hi16s(A.k_new, A.v_new), flags, (uint32_t)A.cap | (uint32_t)A.sel_cap << 16,
                      lo32(pages.table), table_hi, A.scale_log2, T);
   if constexpr (SPLIT) {
@@ -747,12 +748,12 @@ hipError_t launch_gqa_paged_w(const GqaArgs& A, const PageArgs& pages, int n_seq
   return hipGetLastError();
 }
 
-template <int D>
+template <int D, int PAGED>
 hipError_t launch_gqa_paged_d(const GqaArgs& A, const PageArgs& pages, const AttendPlan& plan, int n_seq, size_t lds, hipStream_t st) {
-  if (plan.n_chunks > 1) return launch_gqa_paged_w<D, 4, true, ring(D)>(A, pages, n_seq, plan.n_chunks, lds, st);
-  if (plan.waves == 8) return launch_gqa_paged_w<D, 8, false, ring(D)>(A, pages, n_seq, 1, lds, st);
-  if (!gqa_two_fit(lds)) return launch_gqa_paged_w<D, 4, false, deep_ring(D)>(A, pages, n_seq, 1, lds, st);
-  return launch_gqa_paged_w<D, 4, false, ring(D)>(A, pages, n_seq, 1, lds, st);
+  if (plan.n_chunks > 1) return launch_gqa_paged_w<D, 4, true, ring(D), PAGED>(A, pages, n_seq, plan.n_chunks, lds, st);
+  if (plan.waves == 8) return launch_gqa_paged_w<D, 8, false, ring(D), PAGED>(A, pages, n_seq, 1, lds, st);
+  if (!gqa_two_fit(lds)) return launch_gqa_paged_w<D, 4, false, deep_ring(D), PAGED>(A, pages, n_seq, 1, lds, st);
+  return launch_gqa_paged_w<D, 4, false, ring(D), PAGED>(A, pages, n_seq, 1, lds, st);
 }
 
 template <int D>
@@ -770,7 +771,9 @@ hipError_t launch_gqa_d(const GqaArgs& A, const AttendPlan& plan, int n_seq, siz
 // here, at the library's first use of a device, not next to a launch (where it would also sit inside a captured graph).
 hipError_t gqa_prepare_kernels() {
   const int lim = (int)kGqaMaxLds;
-#define ADSA_GQA(D, ...) reinterpret_cast<const void*>(&k_attend_gqa<D, __VA_ARGS__>), reinterpret_cast<const void*>(&k_attend_gqa<D, __VA_ARGS__, true>)
+#define ADSA_GQA(D, ...)                                                                                                                      \
+  reinterpret_cast<const void*>(&k_attend_gqa<D, __VA_ARGS__>), reinterpret_cast<const void*>(&k_attend_gqa<D, __VA_ARGS__, kNearPages>),      \
+      reinterpret_cast<const void*>(&k_attend_gqa<D, __VA_ARGS__, kFarPages>)
   const void* kernels[] = {ADSA_GQA(64, 4, false, ring(64)),      ADSA_GQA(64, 8, false, ring(64)),        ADSA_GQA(128, 4, false, ring(128)),
                            ADSA_GQA(128, 8, false, ring(128)),    ADSA_GQA(64, 4, false, deep_ring(64)),   ADSA_GQA(128, 4, false, deep_ring(128)),
                            ADSA_GQA(64, 4, true, ring(64)),       ADSA_GQA(128, 4, true, ring(128))};
@@ -844,7 +847,11 @@ hipError_t launch_attend_gqa_paged(const adsa_params& p, const PageArgs& pages, 
   const GqaArgs A = gqa_args(p, seqs, q, k_new, v_new, sel_idx, sel_cnt, out, lse, ws, w, accumulate, append, advance, new_f32);
   const size_t lds = gqa_lds_bytes(p, plan.waves, plan.n_chunks);
   if (lds > kGqaMaxLds) return hipErrorInvalidValue;
-  return p.head_dim == 64 ? launch_gqa_paged_d<64>(A, pages, plan, p.n_seq, lds, st) : launch_gqa_paged_d<128>(A, pages, plan, p.n_seq, lds, st);
+  if (near_pages(pages)) {
+    const PageArgs near = in_bytes(pages);
+    return p.head_dim == 64 ? launch_gqa_paged_d<64, kNearPages>(A, near, plan, p.n_seq, lds, st) : launch_gqa_paged_d<128, kNearPages>(A, near, plan, p.n_seq, lds, st);
+  }
+  return p.head_dim == 64 ? launch_gqa_paged_d<64, kFarPages>(A, pages, plan, p.n_seq, lds, st) : launch_gqa_paged_d<128, kFarPages>(A, pages, plan, p.n_seq, lds, st);
 }
 
 }  // namespace adsa

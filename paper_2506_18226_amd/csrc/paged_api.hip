@@ -33,7 +33,7 @@ int resolve_paged(const adsa_params* p, const adsa_pages* g, adsa_params* eff, P
   const int64_t page_units = (page * eb) >> a->unit_shift;
   if (page * eb >= (1ll << 32) || page_units >= (1ll << 31) || page_units * g->n_pages >= (1ll << 31)) return ADSA_ERR_UNSUPPORTED;
   a->slot_units = (uint32_t)((slot * eb) >> a->unit_shift);
-  if (a->slot_units >= (1u << 24)) return ADSA_ERR_UNSUPPORTED;          // (products of 24 bits)
+  if (slot * eb >= (1ll << 24)) return ADSA_ERR_UNSUPPORTED;             // (products of 24 bits)
   a->table = g->table;
   a->k = (char*)g->k;
   a->v = (char*)g->v;

@@ -8,8 +8,9 @@ from paper_2506_18226_amd.batch import PagedBatch
 DEV = "cuda:0"
 
 
-def paged_twin(dense, page, *, layout="head_major", spare=3, seed=3, resident=None, interleaved=False):
-    """A PagedBatch with the records, positions, scores and rows of a LayerBatch.  resident: slots that have a page (all of cap if None)."""
+def paged_twin(dense, page, *, layout="head_major", spare=3, seed=3, resident=None, interleaved=False, far=False):
+    """A PagedBatch with the records, positions, scores and rows of a LayerBatch.  resident: slots that have a page (all of cap if None); far: pages so far
+    apart that a pool spans more than 4 GiB."""
     p = dense.params
     params = B.make_params(n_seq=p.n_seq, n_heads=p.n_heads, head_dim=p.head_dim, grid_h=p.grid_h, grid_w=p.grid_w, win_rows_back=p.win_rows_back,
                            win_col_radius=p.win_col_radius, dtype=p.dtype, score_mode=p.score_mode, cap=p.cap, sel_cap=p.sel_cap, layout=layout,
@@ -27,6 +28,10 @@ def paged_twin(dense, page, *, layout="head_major", spare=3, seed=3, resident=No
     if interleaved:                                          # K and V of a page side by side in one pool
         both = torch.empty((2, *paged.K.shape), dtype=paged.tdtype, device=DEV).transpose(0, 1).contiguous()
         paged.K, paged.V = both[:, 0], both[:, 1]
+        paged.pages = B.make_pages(paged.K, paged.V, paged.table, page_size=page, layout=layout)
+    if far:
+        stride = max((1 << 32) // paged.K.element_size() // paged.n_pages, paged.K.stride(0)) // 64 * 64 + 64
+        paged.K, paged.V = (torch.empty(paged.n_pages * stride, dtype=paged.tdtype, device=DEV).as_strided(paged.K.shape, (stride, *paged.K.stride()[1:])) for _ in range(2))
         paged.pages = B.make_pages(paged.K, paged.V, paged.table, page_size=page, layout=layout)
     paged.K.fill_(float("nan"))
     paged.V.fill_(float("nan"))

@@ -48,7 +48,10 @@ def prefill_both(p, page, layout, check=True, flags=0, twin=None, **mods):
     ([300, 1, 64], [17, 600, 0], 2, 64, "bf16", 0, 128, "head_major"), ([200], [1000], 2, 64, "bf16", 2, 8192, "head_major"), ([70, 33], [0, 95], 2, 128, "bf16", 4, 16, "head_major")])
 @pytest.mark.parametrize("mask", [B.MASK_CAUSAL, B.MASK_PREFIX])
 def test_prompts_against_the_definition_and_dense_caches(lens, past, h, D, dtype, G, page, layout, mask):
-    prefill_both(Prompt(lens, past, h, D, dtype, G, prefix=50), page, layout, mask=mask)
+    p = Prompt(lens, past, h, D, dtype, G, prefix=50)
+    prefill_both(p, page, layout, mask=mask)
+    p.batch.score.copy_(torch.from_numpy(p.score0).float())
+    prefill_both(p, page, layout, twin=twin_of(p, page, layout, far=True), check=False, mask=mask)
 
 
 @pytest.mark.parametrize("dtype,D,G", [("bf16", 64, 0), ("bf16", 128, 2), ("f32", 64, 0), ("f32", 128, 0)])
@@ -141,7 +144,7 @@ def test_append(page, layout, dtype, D, G, in_f32, pairing, lens, past):
     s["n_res"], s["grid_origin"], s["n_keep_prefix"], s["step"] = past, 20, 20, 0
     dense.upload_seqs()
     keys = [a + b for a, b in zip(lens, past)]
-    paged = paged_twin(dense, page, layout=layout, resident=keys)
+    paged = paged_twin(dense, page, layout=layout, resident=keys, far=page == 32)
     it = torch.float32 if in_f32 else dense.tdtype
     q, k, v = (randn(gen, T, heads * D, dtype=it).to(DEV) for heads in (hq, h, h))
     freq = torch.rand(2, D // 2, generator=torch.Generator().manual_seed(6), dtype=torch.float64).to(DEV)
@@ -268,10 +271,10 @@ class Decode:
     ([1], 1, 1, 64, "bf16", 2, 16, "head_major"), ([1, 2, 17, 0, 64], [1, 40, 17, 5, 70], 3, 64, "bf16", 8, 16, "slot_major"), ([5, 33, 100], 130, 2, 128, "bf16", 16, 32, "head_major"),
     ([300, 1378], 1471, 8, 128, "bf16", 8, 32, "head_major"), ([650] * 50, 700, 8, 64, "bf16", 5, 64, "slot_major"), ([5000, 77], 6000, 1, 128, "bf16", 8, 16, "head_major"),
     ([3000], 3100, 2, 64, "bf16", 3, 64, "head_major"), ([1300] * 40, 1400, 2, 128, "bf16", 16, 16, "head_major")])
-@pytest.mark.parametrize("f32_rows", [False, True])
-def test_single_tokens(lists, resident, h, D, dtype, G, page, layout, f32_rows):
+@pytest.mark.parametrize("f32_rows,far", [(False, False), (True, False), (True, True)])
+def test_single_tokens(lists, resident, h, D, dtype, G, page, layout, f32_rows, far):
     d = Decode(lists, resident, h, D, dtype, G)
-    paged = paged_twin(d.batch, page, layout=layout, resident=d.resident)
+    paged = paged_twin(d.batch, page, layout=layout, resident=d.resident, far=far)
     score0 = f64(paged.score)
     k, v = d.rows(f32_rows and d.bf16)
     flags = B.FLAG_APPEND | B.FLAG_ADVANCE | (B.FLAG_NEW_F32 if f32_rows else 0)
@@ -305,8 +308,8 @@ def test_single_tokens_whose_rows_are_there(G, dtype, D):
 @pytest.mark.parametrize("bad", [-1, 1 << 20, (1 << 31) - 1])
 def test_single_tokens_on_entries_that_are_no_pages(G, lists, resident, bad):
     d = Decode(lists, resident, 2, 64, "bf16", G, cap=resident + 40)
-    paged = paged_twin(d.batch, 16, resident=d.resident)
-    good = paged_twin(d.batch, 16, resident=d.resident)
+    paged = paged_twin(d.batch, 16, resident=d.resident, far=bad == -1)
+    good = paged_twin(d.batch, 16, resident=d.resident, far=bad == -1)
     k, v = d.rows(False)
     good.attend(d.q, B.FLAG_APPEND, k, v)
     paged.table[1, 0] = bad
@@ -362,14 +365,15 @@ def evicting(n, h, D, W, R, budget, rows, dtype="bf16", prefix=9, seed=1, ties=F
     return dense
 
 
+@pytest.mark.parametrize("far", [False, True])
 @pytest.mark.parametrize("n,h,D,W,R,budget,rows,dtype,page,layout,ties", [
     (1, 1, 64, 4, 0, 3, 3, "bf16", 16, "head_major", False), (5, 3, 64, 8, 1, 30, 6, "bf16", 16, "slot_major", True), (4, 2, 128, 16, 1, 100, 9, "f32", 32, "head_major", False),
     (6, 24, 64, 32, 1, 512, 22, "bf16", 64, "head_major", False), (3, 14, 128, 24, 2, 600, 30, "bf16", 16, "slot_major", True), (5, 2, 64, 64, 2, 1500, 40, "bf16", 128, "head_major", False),
     (4, 1, 64, 64, 2, 3800, 61, "f32", 16, "head_major", False), (140, 4, 64, 16, 1, 60, 9, "bf16", 16, "head_major", False)])
-def test_row_ends(n, h, D, W, R, budget, rows, dtype, page, layout, ties):
+def test_row_ends(n, h, D, W, R, budget, rows, dtype, page, layout, ties, far):
     dense = evicting(n, h, D, W, R, budget, rows, dtype, ties=ties)
     resident = dense.seqs_host["n_res"].copy()
-    paged = paged_twin(dense, page, layout=layout, resident=resident)
+    paged = paged_twin(dense, page, layout=layout, resident=resident, far=far)
     pos0, score0 = paged.pos.cpu().numpy(), paged.score.cpu().numpy()
     old = [[paged.cache_rows(t, b, int(r)).clone() for t in (paged.K, paged.V)] for b, r in enumerate(resident)]
     dense.compact(B.FLAG_ADVANCE)
@@ -523,8 +527,8 @@ def test_steps_over_pages_in_a_graph(G):
     q, k, v = (torch.zeros(n, heads, D, dtype=torch.bfloat16, device=DEV) for heads in (hq, h, h))
     eager, captured = batches
     stream = torch.cuda.Stream()
-    stream.wait_stream(torch.cuda.current_stream())
     saved = [t.clone() for t in (captured.seqs, captured.pos, captured.score, captured.K, captured.V)]
+    stream.wait_stream(torch.cuda.current_stream())              # after the copies, which the step must not overtake
     with torch.cuda.stream(stream):
         captured.step(q, k, v)
     torch.cuda.synchronize()
