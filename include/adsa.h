@@ -422,9 +422,9 @@ typedef struct adsa_pages {    /* [host] */
   void* k;                     /* device: page 0 of the pool of K (dtype elements); 16-byte aligned, as is v */
   void* v;                     /* ... of V; may be the same memory as k, with strides that keep them apart */
   const int32_t* table;        /* device [n_seq][table_stride]: entry i of a row is the page of slots i * page_size .. + page_size - 1 */
-  int64_t page_stride;         /* (less than 4 GiB, else ADSA_ERR_UNSUPPORTED) elements from a page to the next, from a slot's row to the next slot's in a page, and from a */
-  int64_t slot_stride;         /* head's row to the next head's; multiples of 16 bytes, nested [page][head][slot][D] or */
-  int64_t head_stride;         /* [page][slot][head][D] */
+  int64_t page_stride;         /* elements from a page to the next, from a slot's row to the next slot's in a page, and from a head's row to the next head's; */
+  int64_t slot_stride;         /* multiples of 16 bytes, nested [page][head][slot][D] or [page][slot][head][D]; a page's below 4 GiB and a slot's below */
+  int64_t head_stride;         /* 16 MiB, else ADSA_ERR_UNSUPPORTED */
   int32_t page_size;           /* slots of a page: a power of two from ADSA_MIN_PAGE to ADSA_MAX_CAP */
   int32_t n_pages;             /* pages of a pool; n_pages * page_stride, in units of the largest power of two (16 bytes at least) that divides the
                                   three strides, below 2^31 (rows of 128 bytes, one behind the other: 256 GiB), else ADSA_ERR_UNSUPPORTED */
@@ -456,7 +456,8 @@ size_t adsa_paged_workspace_bytes(const adsa_params* p);       /* of adsa_attend
  * order of index at which the running sum of the candidates' w exceeds uniform times their whole sum; logprob the natural logarithm of its share.
  * Temperature 0: the largest (the first of several), logprob 0.  A NaN counts as -infinity; where +infinities are, only these are
  * candidates; a row without a logit above -infinity gets token -1 and logprob -infinity.  Weights are summed as whole numbers of 2^-44, whatever
- * the order, so results repeat bit by bit; a w below that is 0.
+ * the order, so results repeat bit by bit; what is less than half of that, 31.19 temperatures below the largest, is 0.  A temperature between 0 and
+ * 2^-100 counts as 2^-100.
  */
 typedef struct adsa_sampling { /* [host] */
   int32_t n_rows;              /* tokens to draw: 1..2^20 */

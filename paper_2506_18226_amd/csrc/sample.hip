@@ -1,15 +1,19 @@
 // The next token of every row of logits (adsa_sample): temperature, top-k, top-p and min-p, from a random number that the caller brings.
 //
-//  k_sample<EB, NT, BINS, VEC>: a workgroup takes a row.  It reads it once and keeps it in LDS as far as that goes (28672 logits); what is beyond is read again in every pass.
+//  k_sample<EB, NT, BINS, VEC, GUIDED>: a workgroup takes a row.  It reads it once and keeps it in LDS as far as that goes (24576 logits); what is beyond is
+//  read again in every pass.
 //  What is kept of a row by top-k and top-p is the front of its descending order, so it is known by its last one: (z, index), and a logit is in if its z is
-//  larger, or the same and its index no larger.  That last one is found without sorting: logits are counted, and their weights summed, by
-//  BINS steps of z below the largest; running sums over the bins say in which bin a limit falls, and that bin's logits, some dozens, are listed in one more
-//  pass and ranked against each other.  Where they are more than kList (many equal ones), the last one is found bit by bit instead.
+//  larger, or the same and its index no larger.  That last one is found without sorting: logits are counted, or their weights summed, by
+//  BINS steps of z below the largest; running sums over the bins say in which bin a limit falls, and that bin's logits, some dozens, are listed and
+//  ranked against each other.  Where they are more than kList (many equal ones), the last one is found bit by bit instead.
+//  Where the candidates are few (kFew), the same pass gathers them, and what is left to do is done on that list: a top-k's weights are only formed there.
+//  Where they are many, the pass that sums their weights by runs of 1024 lists the border's logits too, and these are added when they are ranked.
 //  Weights are whole numbers of 2^-44 of the largest one's: their sums do not depend on an order, and what is less than half of that is nothing.  They are formed in 64
 //  bits, since a token is decided by where a random number falls among up to 2^18 of them: with weights good to 2^-24 every thousandth row of a large
 //  vocabulary would get its neighbour.
-//  The passes: the largest; bins (rows with top-k or top-p); a list for each limit; the candidates' weight by runs of 1024; the run that the random number falls in.
-//  What bounds it: memory for the first pass, from then on what the vector unit issues, about 18 instructions a weight, twice a logit.
+//  What bounds it: memory for the first pass (256 rows of 65536 fp32: 12.5 us, 5.4 TB/s), from then on operations in 64 bits, of which a weight has 10: 16 us for
+//  the bins of a row with top-p alone, 24 for its candidates, 57 in all; with top-k 1000 before it 8 and 18, 39 in all.  One row has a chain of some 20 barriers:
+//  16 us for a guided one of 16384 with top-k 2000 and top-p, of which the pair's reading takes 3.3.
 #include <type_traits>
 
 #include "adsa_device.h"
@@ -35,7 +39,8 @@ struct SampleArgs {
 constexpr int kGroup = 4 * kWave;        // logits of a group: 4 consecutive ones to a lane
 constexpr int kRun = 4;                  // groups of a run, whose weight is kept
 constexpr int kList = 512;
-constexpr float kReach = 31.25f;         // e^-31.25 < 2^-45: what is further below the largest (in temperatures) weighs nothing
+constexpr float kReach = 31.19f;         // what is further below the largest, in temperatures, weighs nothing: e^-31.19 = 1.0014 * 2^-45, which rounds to 2^-44
+constexpr int kTable = 256;
 constexpr double kOne = 17592186044416.0;            // 2^44
 
 __device__ __forceinline__ uint32_t order_of(float z) {            // ascending as z is; -0 and +0 are equal
@@ -43,19 +48,45 @@ __device__ __forceinline__ uint32_t order_of(float z) {            // ascending 
   return u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u);
 }
 
-// The weight of a live logit (see k_sample): exp((z - top) / T) * 2^44, by 2^(j / 32) from a table and a polynomial of degree 5, off by some 2^-49 of it, rounded
-// to a whole number.  Sums' low bits do the rounding: x + kRound holds the nearest whole number of x in its low bits, and w + 2^52 that of w.
+__device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xFFFFFFFFu)); }
+
+// The weight of a live logit (see k_sample): exp((z - top) / T) * 2^44, by 2^(j / 256) from a table and a polynomial of degree 4 (off by (ln(2) / 512)^5 / 120 =
+// 2^-54.5 of it; 1 / T's two roundings are worth x 2^-52 at x temperatures below the largest), rounded to a whole number.  Sums' low bits do the rounding:
+// x + kRound holds the nearest whole number of x in its low bits, and w + 2^52 that of w.  10 operations in 64 bits, which are most of a pass's time: with 32
+// entries and degree 5, one more, a pass over 256 rows of 65536 took 21 us and not 19, with 1024 and degree 3 as long as this.  Four at a time, whose chains
+// the unit can overlap.  (Of a logit that is not live it is any number.)
 struct Weigh {
   static constexpr double kRound = 6755399441055744.0;             // 1.5 * 2^52
-  const double* table;         // 2^(44 + j / 32), LDS
-  double inv, top;             // 32 log2(e) / T; the largest logit
+  const double* table;         // 2^(44 + j / 256), LDS
+  double inv, top;             // 256 log2(e) / T; the largest logit
+  template <int N>
+  __device__ __forceinline__ void operator()(const float (&z)[N], u64 (&w)[N]) const {
+    constexpr double a = 0.69314718055994530942 / kTable;
+    double d[N], t[N], r[N], p[N], power[N];
+    int steps[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      d[e] = (double)z[e] - top;
+      t[e] = fma(d[e], inv, kRound);
+      steps[e] = (int)(uint32_t)__double_as_longlong(t[e]);
+      power[e] = table[steps[e] & (kTable - 1)];
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      r[e] = fma(d[e], inv, kRound - t[e]);
+      p[e] = fma(r[e], fma(r[e], fma(r[e], fma(r[e], a * a * a * a / 24.0, a * a * a / 6.0), a * a / 2.0), a), 1.0);
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) {                    // (2^-2 at least: an exponent that there is)
+      power[e] = __hiloint2double(__double2hiint(power[e]) + (int)((uint32_t)(steps[e] & ~(kTable - 1)) * (1048576u / kTable)), __double2loint(power[e]));
+      w[e] = (u64)__double_as_longlong(fma(power[e], p[e], 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
+    }
+  }
   __device__ __forceinline__ u64 operator()(float z) const {
-    constexpr double a = 0.69314718055994530942 / 32.0;            // ln(2) / 32
-    const double d = (double)z - top, t = fma(d, inv, kRound), r = fma(d, inv, kRound - t);
-    const int steps = (int)(uint32_t)__double_as_longlong(t);
-    const double p = fma(r, fma(r, fma(r, fma(r, fma(r, a * a * a * a * a / 120.0, a * a * a * a / 24.0), a * a * a / 6.0), a * a / 2.0), a), 1.0);
-    const u64 power = (u64)__double_as_longlong(table[steps & 31]) + ((u64)(uint32_t)(steps >> 5) << 52);         // (2^-2 at least: an exponent that there is)
-    return (u64)__double_as_longlong(fma(__longlong_as_double((long long)power), p, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
+    const float one[1] = {z};
+    u64 w[1];
+    (*this)(one, w);
+    return w[0];
   }
 };
 
@@ -79,19 +110,21 @@ __device__ __forceinline__ T wave_sum(T x) { return lane_of(wave_scan(x), kWave 
 
 template <int NT, int BINS>
 struct SampleShared {
-  static constexpr int NW = NT / kWave;
-  double table[32];
-  u64 weight[BINS];            // of a bin
+  static constexpr int NW = NT / kWave, kFew = NT == 1024 ? 2048 : 1024;
+  double table[kTable];
+  u64 weight[BINS + kWave];    // of a bin
   u64 list_weight[kList];
-  u64 run_weight[NT / kRun];
+  u64 run_weight[NT];          // of a run, or of indices that agree but for their low bits
   u64 wave_weight[2][NW];
   u64 above_weight, left;      // weight before the bin that a limit falls in; of a run before the random number
-  uint32_t count[BINS];
+  uint32_t count[BINS + kWave];
   uint32_t list_key[kList];
   int list_index[kList];
+  uint32_t few_key[kFew];      // candidates, in any order
+  int few_index[kFew];
   uint32_t wave_count[2][NW];
   float wave_top[NW], wave_least[NW];
-  uint32_t above_count, n_list, last_key;
+  uint32_t above_count, in_count, n_list, n_few, last_key;
   int bin, last_index, token, run;
 };
 
@@ -102,73 +135,79 @@ struct Last {
   __device__ __forceinline__ bool holds(uint32_t k, int i) const { return k > key || (k == key && i <= index); }
 };
 
-template <int EB, int NT, int BINS, bool VEC>
+template <int EB, int NT, int BINS, bool VEC, bool GUIDED>
 __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
   constexpr int NW = NT / kWave;
   extern __shared__ __align__(16) float s_held[];    // [group of a wave][NT][4]
   __shared__ SampleShared<NT, BINS> sh;
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), r = blockIdx.x, V = A.vocab;
-  const bool guided = A.guided != 0;
   if (A.seqs) {
     const ADSA_GLOBAL adsa_seq& sq = ((const ADSA_GLOBAL adsa_seq*)A.seqs)[r];
     if (sq.step < 0 || sq.status != 0) {             // (a pair goes by its conditional row)
       if (tid == 0) {
         A.token[r] = -1;
-        if (guided) A.token[A.n_rows + r] = -1;
+        if (GUIDED) A.token[A.n_rows + r] = -1;
         if (A.logprob) A.logprob[r] = 0.0f;
       }
       return;
     }
   }
-  const float T = A.temperatures ? A.temperatures[r] : A.temperature, top_p = A.top_ps ? A.top_ps[r] : A.top_p, min_p = A.min_ps ? A.min_ps[r] : A.min_p;
+  const float T_given = A.temperatures ? A.temperatures[r] : A.temperature, top_p = A.top_ps ? A.top_ps[r] : A.top_p, min_p = A.min_ps ? A.min_ps[r] : A.min_p;
   const float u = A.uniform[r];
   const int top_k = A.top_ks ? A.top_ks[r] : A.top_k;
   const gchar* const row = (const gchar*)A.logits + (long long)r * A.stride_b;
   const gchar* const partner = row + (long long)A.n_rows * A.stride_b;
   // ---- logits: a wave takes consecutive ones, group by group
   const int groups = (V + NT * 4 - 1) / (NT * 4), runs = (groups + kRun - 1) / kRun, held = min(A.held, groups), first = wave * groups * kGroup + lane * 4;
-  auto read4 = [&](const gchar* from, int i, float (&f)[4]) {
-    if constexpr (VEC) {
-      if (i < V) {                                   // (V is a multiple of 4)
-        if constexpr (EB == 4) {
-          const uint4 x = load16(from + (long long)i * 4);
-          f[0] = __uint_as_float(x.x); f[1] = __uint_as_float(x.y); f[2] = __uint_as_float(x.z); f[3] = __uint_as_float(x.w);
-        } else {
-          const u32x2 x = *(const ADSA_GLOBAL u32x2*)(from + (long long)i * 2);
-          f[0] = __uint_as_float(x.x << 16); f[1] = __uint_as_float(x.x & 0xFFFF0000u); f[2] = __uint_as_float(x.y << 16); f[3] = __uint_as_float(x.y & 0xFFFF0000u);
-        }
-      } else f[0] = f[1] = f[2] = f[3] = -INFINITY;
+  constexpr int kWords = VEC && EB == 2 ? 2 : 4;
+  struct Raw { uint32_t own[kWords], partner[GUIDED ? kWords : 1]; };          // a lane's logits of a group, as they lie in memory
+  auto fetch4 = [&](const gchar* from, int i, uint32_t (&x)[kWords]) {
+    if constexpr (VEC && EB == 4) {                  // (V is a multiple of 4; behind the end, its last ones)
+      const uint4 q = load16(from + (long long)min(i, V - 4) * 4);
+      x[0] = q.x; x[1] = q.y; x[2] = q.z; x[3] = q.w;
+    } else if constexpr (VEC) {
+      const u32x2 q = *(const ADSA_GLOBAL u32x2*)(from + (long long)min(i, V - 4) * 2);
+      x[0] = q.x; x[1] = q.y;
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int at = min(i + e, V - 1);
-        const float x = EB == 4 ? ((const gfloat*)from)[at] : __uint_as_float((uint32_t)((const ADSA_GLOBAL uint16_t*)from)[at] << 16);
-        f[e] = i + e < V ? x : -INFINITY;
+        x[e] = EB == 4 ? ((const ADSA_GLOBAL uint32_t*)from)[at] : (uint32_t)((const ADSA_GLOBAL uint16_t*)from)[at] << 16;
       }
     }
   };
-  auto read_group = [&](int g, float (&z)[4]) {      // from memory
+  auto fetch = [&](int g, Raw& x) {
+    fetch4(row, first + g * kGroup, x.own);
+    if constexpr (GUIDED) fetch4(partner, first + g * kGroup, x.partner);
+  };
+  auto widen = [&](const uint32_t (&x)[kWords], float (&f)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(kWords == 4 ? x[e] : e % 2 ? x[e / 2] & 0xFFFF0000u : x[e / 2] << 16);
+  };
+  auto decode = [&](int g, const Raw& x, float (&z)[4]) {
     const int i = first + g * kGroup;
-    read4(row, i, z);
-    if (guided) {
+    widen(x.own, z);
+    if constexpr (GUIDED) {
       float f4[4];
-      read4(partner, i, f4);
+      widen(x.partner, f4);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
 #pragma clang fp contract(off)
         const double c = z[e], f = f4[e], step = c - f, far = (double)A.guidance * step;
-        z[e] = i + e < V ? (float)(f + far) : -INFINITY;
+        z[e] = (float)(f + far);
       }
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = z[e] != z[e] ? -INFINITY : z[e];
+    for (int e = 0; e < 4; ++e) z[e] = i + e >= V || z[e] != z[e] ? -INFINITY : z[e];
   };
   // ---- the largest, and the least that is finite
   float top = -INFINITY, least_z = INFINITY;
 #pragma unroll 4
   for (int g = 0; g < groups; ++g) {
+    Raw x;
     float z[4];
-    read_group(g, z);
+    fetch(g, x);
+    decode(g, x, z);
     if (g < held) *reinterpret_cast<float4*>(s_held + (g * NT + tid) * 4) = make_float4(z[0], z[1], z[2], z[3]);
     top = fmaxf(fmaxf(top, fmaxf(z[0], z[1])), fmaxf(z[2], z[3]));
 #pragma unroll
@@ -177,15 +216,15 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
 #pragma unroll
   for (int d = 1; d < kWave; d <<= 1) { top = fmaxf(top, __shfl_xor(top, d)); least_z = fminf(least_z, __shfl_xor(least_z, d)); }
   if (lane == 0) { sh.wave_top[wave] = top; sh.wave_least[wave] = least_z; }
-  if (tid < 32) sh.table[tid] = exp2((double)tid / 32.0) * kOne;
+  if (tid < kTable) sh.table[tid] = exp2((double)tid / kTable) * kOne;
   for (int i = tid; i < BINS; i += NT) { sh.weight[i] = 0; sh.count[i] = 0; }
-  if (tid == 0) { sh.token = V; sh.n_list = 0; }
+  if (tid == 0) { sh.token = V; sh.n_few = 0; }
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < NW; ++w) { top = fmaxf(top, sh.wave_top[w]); least_z = fminf(least_z, sh.wave_least[w]); }
   auto finish = [&](int token, float logprob) {
     A.token[r] = token;
-    if (guided) A.token[A.n_rows + r] = token;
+    if (GUIDED) A.token[A.n_rows + r] = token;
     if (A.logprob) A.logprob[r] = logprob;
   };
   if (top == -INFINITY) {
@@ -194,27 +233,52 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
   }
   const bool infinite = top == INFINITY;             // then only the infinities are candidates: as 0, and the others as -infinity
   top = infinite ? 0.0f : top;
-  auto group_of = [&](int g, float (&z)[4]) {
-    if (g < held) {
-      const float4 x = *reinterpret_cast<const float4*>(s_held + (g * NT + tid) * 4);
-      z[0] = x.x; z[1] = x.y; z[2] = x.z; z[3] = x.w;
-    } else read_group(g, z);
+  auto only_infinite = [&](float (&z)[4]) {
     if (infinite) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) z[e] = z[e] == INFINITY ? 0.0f : -INFINITY;
     }
   };
-  // f(logit, index) for each of the thread's, in ascending order
-  auto each_logit = [&](auto f) {
-#pragma unroll 2
-    for (int g = 0; g < groups; ++g) {
+  auto held_group = [&](int g, float (&z)[4]) {
+    const float4 x = *reinterpret_cast<const float4*>(s_held + (g * NT + tid) * 4);
+    z[0] = x.x; z[1] = x.y; z[2] = x.z; z[3] = x.w;
+    only_infinite(z);
+  };
+  // f(its four logits, the first one's index, the group) for each of the thread's groups, in ascending order; those in memory are asked for two groups ahead
+  auto each_group = [&](auto f) {
+#pragma clang loop unroll(disable)
+    for (int g = 0; g < held; ++g) {
       float z[4];
-      group_of(g, z);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) f(z[e], first + g * kGroup + e);
+      held_group(g, z);
+      f(z, first + g * kGroup, g);
+    }
+    if (held == groups) return;
+    Raw a, b;
+    fetch(held, a);
+    fetch(held + 1, b);
+#pragma clang loop unroll(disable)
+    for (int g = held; g < groups; g += 2) {
+      float z[4];
+      decode(g, a, z);
+      only_infinite(z);
+      fetch(g + 2, a);
+      f(z, first + g * kGroup, g);
+      if (g + 1 < groups) {
+        decode(g + 1, b, z);
+        only_infinite(z);
+        fetch(g + 3, b);
+        f(z, first + (g + 1) * kGroup, g + 1);
+      }
     }
   };
-  if (!(T > 0.0f)) {
+  // f(logit, index) for each of the thread's
+  auto each_logit = [&](auto f) {
+    each_group([&](const float (&z)[4], int i, int) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f(z[e], i + e);
+    });
+  };
+  if (!(T_given > 0.0f)) {
     int at = V;
     each_logit([&](float z, int i) { at = z == top ? min(at, i) : at; });
 #pragma unroll
@@ -224,11 +288,28 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
     if (tid == 0) finish(sh.token, 0.0f);
     return;
   }
-  const double inv = 46.166241308446828384 / (double)T;                    // 32 log2(e) / T
+  const float T = fmaxf(T_given, 0x1p-100f);         // (a bin's width, and its reciprocal, stay numbers)
+  const double inv = 1.4426950408889634074 * kTable / (double)T;
   const Weigh weigh = {sh.table, inv, (double)top};
-  const float reach = fminf(kReach * T, 1e38f), range = fminf(reach, infinite ? 1.0f : top - least_z), per_bin = range > 0.0f ? (float)BINS / range : 0.0f;
-  auto live = [&](float z) { return top - z <= reach; };
-  auto bin_of = [&](float below) { return min((int)(below * per_bin), BINS - 1); };            // below the largest
+  // Bins of equal width below the largest, to the least or as far as a weight can be: what lies further is in the bins from BINS on, which nobody reads, and not live.
+  const float range = fminf(fminf(kReach * T, 1e38f), infinite ? 1.0f : top - least_z);
+  const float per_bin = range > 0.0f ? fminf((float)BINS * (1.0f - 0x1p-20f) / range, 1e38f) : 1.0f;
+  const float furthest = (float)(BINS + lane);       // (lanes whose logits are not live do not meet in one bin: 16384 of which most are far below 5.9 -> 2.0 us)
+  auto bin_of = [&](float z) { return (int)fminf((top - z) * per_bin, furthest); };
+  // The least logit for which `in` holds, which holds for all larger ones too, the largest among them: a wave tries 64 at a time.
+  auto least_in = [&](auto in) {
+    const uint32_t top_key = order_of(top);          // (0x7FFFFF is -infinity's, what is less that of no number)
+    uint32_t from = 0;
+#pragma unroll
+    for (int shift = 26; shift >= -4; shift -= 6) {
+      const int s = max(shift, 0);
+      const uint32_t key = from + (((uint32_t)lane + 1u) << s) - 1u;       // the last one of the lane's keys
+      from += (uint32_t)__popcll(__ballot(!(key >= top_key || (key > 0x007FFFFFu && in(logit_of(key)))))) << s;
+    }
+    return logit_of(from);
+  };
+  auto least_of_bins = [&](int bin) { return bin < 0 ? INFINITY : least_in([&](float z) { return bin_of(z) <= bin; }); };      // up to this bin
+  auto live = [&](float z) { return bin_of(z) < BINS; };
   const bool by_count = top_k > 0 && top_k < V, by_sum = top_p < 1.0f;
   Last last = {0u, 0x7FFFFFFF};
   // sums of a count and a weight over the workgroup
@@ -250,204 +331,348 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
     if ((double)e < share) ++e;
     return e < 1 ? (u64)1 : e > total ? total : e;
   };
-  if (by_count || by_sum) {
-    each_logit([&](float z, int) {
-      const float below = top - z;
-      if (below <= reach) {
-        const int b = bin_of(below);
-        atomicAdd(&sh.count[b], 1u);
-        if (by_sum) atomicAdd(&sh.weight[b], weigh(z));
-      }
-    });
-    __syncthreads();
-    // running sums over the bins, PB of them a thread
-    constexpr int PB = BINS / NT;
-    static_assert(PB * NT == BINS, "whole bins");
-    uint32_t n[PB], n_sum = 0;
-    u64 w[PB], w_sum = 0;
-#pragma unroll
-    for (int k = 0; k < PB; ++k) {
-      n[k] = sh.count[tid * PB + k];
-      w[k] = sh.weight[tid * PB + k];
-      n_sum += n[k];
-      w_sum += w[k];
-    }
-    const uint32_t n_up = wave_scan(n_sum);
-    const u64 w_up = wave_scan(w_sum);
-    if (lane == kWave - 1) { sh.wave_count[0][wave] = n_up; sh.wave_weight[0][wave] = w_up; }
-    __syncthreads();
-    uint32_t n_at = n_up - n_sum, n_live = 0;
-    u64 w_at = w_up - w_sum, total = 0;
-#pragma unroll
-    for (int k = 0; k < NW; ++k) {
-      if (k < wave) { n_at += sh.wave_count[0][k]; w_at += sh.wave_weight[0][k]; }
-      n_live += sh.wave_count[0][k];
-      total += sh.wave_weight[0][k];
-    }
-    turn = 1;
-    // (what can be in the bin lies between `from` and `to`, a bin's width to either side: two comparisons for nearly all)
-    const float width = range / (float)BINS;
-    auto in_bin = [&](float z, int bin) {
-      const float below = top - z, from = ((float)bin - 1.0f) * width, to = bin == BINS - 1 || per_bin == 0.0f ? INFINITY : ((float)bin + 2.0f) * width;
-      return below >= from && below < to && below <= reach && bin_of(below) == bin;
-    };
-    // The last one up to which there are `most` logits, or `enough` of weight, among those that `last` holds.
-    auto cut = [&](bool by_n, uint32_t most, u64 enough) {
-      {
-        uint32_t nb = n_at;
-        u64 wb = w_at;
-#pragma unroll
-        for (int k = 0; k < PB; ++k) {
-          if (by_n ? nb < most && most <= nb + n[k] : wb < enough && enough <= wb + w[k]) { sh.bin = tid * PB + k; sh.above_count = nb; sh.above_weight = wb; sh.n_list = 0; }
-          nb += n[k];
-          wb += w[k];
-        }
-      }
-      __syncthreads();
-      const int bin = sh.bin;
-      if (sh.count[bin] <= (uint32_t)kList) {        // (uniform)
-        each_logit([&](float z, int i) {
-          if (in_bin(z, bin) && last.holds(order_of(z), i)) {
-            const uint32_t at = atomicAdd(&sh.n_list, 1u);
-            sh.list_key[at] = order_of(z);
-            sh.list_index[at] = i;
-            if (by_sum) sh.list_weight[at] = weigh(z);
-          }
-        });
-        __syncthreads();
-        // a wave ranks an entry: its lanes are the entries that may come before it (or are it)
-        const int m = (int)sh.n_list;
-        for (int i = wave; i < m; i += NW) {
-          const Last me = {sh.list_key[i], sh.list_index[i]};
-          uint32_t rank = sh.above_count;
-          u64 upto = 0;
-          for (int j0 = 0; j0 < m; j0 += kWave) {
-            const int j = j0 + lane;
-            const bool in = j < m && me.holds(sh.list_key[min(j, m - 1)], sh.list_index[min(j, m - 1)]);
-            rank += (uint32_t)__popcll(__ballot(in));
-            if (!by_n) upto += in ? sh.list_weight[j] : 0;
-          }
-          bool ends = rank == most;
-          if (!by_n) {
-            upto = sh.above_weight + wave_sum(upto);
-            ends = upto >= enough && upto - sh.list_weight[i] < enough;
-          }
-          if (ends && lane == 0) { sh.last_key = me.key; sh.last_index = me.index; }
-        }
-        __syncthreads();
-        last = {sh.last_key, sh.last_index};
-        return;
-      }
-      // Many equal logits: the largest key from which on there is enough, then, among that key's logits, the lowest index up to which.
-      const Last held_by = last;
-      auto sum = [&](auto in, uint32_t* all_n, u64* all_w) {
-        uint32_t c = 0;
-        u64 x = 0;
-        each_logit([&](float z, int i) {
-          const uint32_t k = order_of(z);
-          if (live(z) && held_by.holds(k, i) && in(k, i)) { ++c; x += by_n ? 0 : weigh(z); }
-        });
-        block_sum(c, x, all_n, all_w);
-      };
-      uint32_t key = 0, cn, on;
-      u64 cw, ow;
-      for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t from = key | 1u << bit;
-        sum([&](uint32_t k, int) { return k >= from; }, &cn, &cw);
-        if (by_n ? cn >= most : cw >= enough) key = from;
-      }
-      sum([&](uint32_t k, int) { return k > key; }, &on, &ow);
-      int index = -1;                                // not enough up to here
-      for (int bit = 17; bit >= 0; --bit) {
-        const int upto = index + (1 << bit);
-        sum([&](uint32_t k, int i) { return k == key && i <= upto; }, &cn, &cw);
-        if (!(by_n ? on + cn >= most : ow + cw >= enough)) index = upto;
-      }
-      last = {key, index + 1};
-    };
-    if (by_count && (uint32_t)top_k < n_live) {
-      cut(true, (uint32_t)top_k, 0);
-      if (by_sum) {                                  // the sum that top_p is a share of: whole bins, and what is left of the one that top-k ends in
-        const int bin = sh.bin;
-        const u64 above = sh.above_weight;
-        uint32_t none;
-        u64 mine = 0;
-        if (sh.count[bin] <= (uint32_t)kList) {      // (listed, without those that are left out: any entry's weight counts if it is held)
-          const int m = (int)sh.n_list;
-          for (int j = tid; j < m; j += NT) {
-            if (last.holds(sh.list_key[j], sh.list_index[j])) mine += sh.list_weight[j];
-          }
-        } else {
-          each_logit([&](float z, int i) {
-            if (in_bin(z, bin) && last.holds(order_of(z), i)) mine += weigh(z);
-          });
-        }
-        block_sum(0, mine, &none, &total);
-        total += above;
-      }
-    }
-    if (by_sum) cut(false, 0, enough_of(total));
-    __syncthreads();
+  float z_min = -INFINITY;     // what min_p leaves
+  if (min_p > 0.0f) {
+    const u64 least = (u64)ceil((double)fminf(min_p, 1.0f) * kOne);
+    z_min = least_in([&](float z) { return live(z) && weigh(z) >= least; });
   }
-  // ---- the candidates' weight by runs, and the run that the random number falls in
-  const u64 least = min_p > 0.0f ? (u64)ceil((double)fminf(min_p, 1.0f) * kOne) : 0;
-  auto weight_of = [&](float z, int i) -> u64 {
-    if (!live(z) || !last.holds(order_of(z), i)) return 0;
-    const u64 w = weigh(z);
-    return w >= least ? w : 0;
-  };
-  for (int run = 0; run < runs; ++run) {
-    u64 sum = 0;
-#pragma unroll 2
-    for (int g = run * kRun; g < min((run + 1) * kRun, groups); ++g) {
-      float z[4];
-      group_of(g, z);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum += weight_of(z[e], first + g * kGroup + e);
-    }
-    sum = wave_sum(sum);
-    if (lane == 0) sh.run_weight[wave * runs + run] = sum;
-  }
-  __syncthreads();
-  {
-    const u64 mine = tid < NW * runs ? sh.run_weight[tid] : 0, upto = wave_scan(mine);
-    if (lane == kWave - 1) sh.wave_weight[0][wave] = upto;
+  // The sums of NT weights, a thread's own each: in which of them the random number falls, and how far into it.
+  auto find_run = [&](u64 mine) {
+    const u64 upto = wave_scan(mine);
+    if (lane == kWave - 1) sh.wave_weight[turn][wave] = upto;
     __syncthreads();
     u64 before = upto - mine, all = 0;
 #pragma unroll
     for (int k = 0; k < NW; ++k) {
-      before += k < wave ? sh.wave_weight[0][k] : 0;
-      all += sh.wave_weight[0][k];
+      before += k < wave ? sh.wave_weight[turn][k] : 0;
+      all += sh.wave_weight[turn][k];
     }
     u64 target = (u64)((u >= 0.0f ? (double)fminf(u, 0.99999994f) : 0.0) * (double)all);
     target = target < all ? target : all - 1;
     if (target >= before && target - before < mine) { sh.run = tid; sh.left = target - before; sh.above_weight = all; }
     __syncthreads();
+  };
+  auto answer = [&](int token, float z) { finish(token, (float)(((double)z - (double)top) / (double)T - log((double)sh.above_weight * (1.0 / kOne)))); };
+  // Which of a lane's four weights, which end at upto, `left` falls in: -1 if none.
+  auto pick4 = [&](u64 left, const u64 (&w)[4], u64 sum, u64 upto) {
+    u64 from = upto - sum;
+    if (left < from || left >= upto) return -1;
+    int e = 0;
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (e == k && left - from >= w[k]) { from += w[k]; ++e; }
+    return e;
+  };
+  // ---- the limits.  Everything that decides between their paths is the same for all threads.
+  constexpr int kFew = SampleShared<NT, BINS>::kFew;
+  int end = BINS;              // the bin that the candidates end in,
+  bool few = false, listing = false;                 // with all of them in few_*, or its own ones still to be listed and ranked,
+  bool by_n = true;            // by their number, `most`,
+  uint32_t most = 0;
+  u64 enough = 0;              // or by their weight
+  auto list = [&](float z, int i) {
+    const uint32_t at = atomicAdd(&sh.n_list, 1u);
+    if (at >= (uint32_t)kList) return;               // (never)
+    sh.list_key[at] = order_of(z);
+    sh.list_index[at] = i;
+  };
+  auto keep = [&](uint32_t key, int i) {
+    const uint32_t at = atomicAdd(&sh.n_few, 1u);
+    if (at >= (uint32_t)kFew) return;                // (never)
+    sh.few_key[at] = key;
+    sh.few_index[at] = i;
+  };
+  // The last candidate, among the listed: a wave ranks an entry, its lanes are the entries that may come before it (or are it).
+  auto rank = [&]() {
+    __syncthreads();
+    const int m = min((int)sh.n_list, kList);
+    for (int i = tid; i < m; i += NT) sh.list_weight[i] = weigh(logit_of(sh.list_key[i]));
+    __syncthreads();
+    for (int i = wave; i < m; i += NW) {
+      const Last me = {sh.list_key[i], sh.list_index[i]};
+      uint32_t rank = sh.above_count;
+      u64 upto = 0;
+      for (int j0 = 0; j0 < m; j0 += kWave) {
+        const int j = j0 + lane;
+        const bool in = j < m && me.holds(sh.list_key[min(j, m - 1)], sh.list_index[min(j, m - 1)]);
+        rank += (uint32_t)__popcll(__ballot(in));
+        if (!by_n) upto += in ? sh.list_weight[j] : 0;
+      }
+      bool ends = rank == most;
+      if (!by_n) {
+        upto = sh.above_weight + wave_sum(upto);
+        ends = upto >= enough && upto - sh.list_weight[i] < enough;
+      }
+      if (ends && lane == 0) { sh.last_key = me.key; sh.last_index = me.index; }
+    }
+    __syncthreads();
+    last = {sh.last_key, sh.last_index};
+  };
+  auto each_few = [&](auto f) {
+    const int m = (int)sh.n_few;
+    for (int j = tid; j < m; j += NT) f(logit_of(sh.few_key[j]), sh.few_index[j]);
+  };
+  if (by_count || by_sum) {
+    const bool few_by_count = by_count && top_k <= kFew;           // then only those few are weighed, after they are found
+    bool weighed = by_sum && !few_by_count;
+    // running sums over the bins, PB of them a thread
+    constexpr int PB = BINS / NT;
+    static_assert(PB * NT == BINS, "whole bins");
+    uint32_t n[PB], n_at, n_live;
+    u64 w[PB], w_at, total;
+    auto scan_bins = [&]() {
+      uint32_t n_sum = 0;
+      u64 w_sum = 0;
+#pragma unroll
+      for (int k = 0; k < PB; ++k) {
+        w[k] = sh.weight[tid * PB + k];
+        if (by_count) n[k] = sh.count[tid * PB + k];
+        else {                                       // not counted: no more than have this weight if each has the least of the bin (and half a unit less, by its rounding)
+          const float each = exp2f(44.0f - (float)(tid * PB + k + 1) / per_bin * 1.0001f / T * 1.442695041f);
+          n[k] = (uint32_t)fminf((float)w[k] * 1.001f / fmaxf(each - 0.501f, 1.0f), (float)ADSA_MAX_VOCAB);
+        }
+        n_sum += n[k];
+        w_sum += w[k];
+      }
+      const uint32_t n_up = wave_scan(n_sum);
+      const u64 w_up = wave_scan(w_sum);
+      if (lane == kWave - 1) { sh.wave_count[turn][wave] = n_up; sh.wave_weight[turn][wave] = w_up; }
+      __syncthreads();
+      n_at = n_up - n_sum;
+      w_at = w_up - w_sum;
+      n_live = 0;
+      total = 0;
+#pragma unroll
+      for (int k = 0; k < NW; ++k) {
+        if (k < wave) { n_at += sh.wave_count[turn][k]; w_at += sh.wave_weight[turn][k]; }
+        n_live += sh.wave_count[turn][k];
+        total += sh.wave_weight[turn][k];
+      }
+      turn ^= 1;
+    };
+    // of each thread's bins, the one in which the last candidate is
+    auto find_bin = [&]() {
+      uint32_t nb = n_at;
+      u64 wb = w_at;
+#pragma unroll
+      for (int k = 0; k < PB; ++k) {
+        if (by_n ? nb < most && most <= nb + n[k] : wb < enough && enough <= wb + w[k]) {
+          sh.bin = tid * PB + k;
+          sh.above_count = nb;
+          sh.in_count = n[k];
+          sh.above_weight = wb;
+          sh.n_list = 0;
+        }
+        nb += n[k];
+        wb += w[k];
+      }
+      __syncthreads();
+      return sh.bin;
+    };
+    auto each = [&](auto f) {
+      if (few) each_few(f);
+      else each_logit(f);
+    };
+    if (weighed) {
+      each_group([&](const float (&z)[4], int, int) {
+        u64 w4[4];
+        weigh(z, w4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int b = bin_of(z[e]);
+          if (by_count) atomicAdd(&sh.count[b], 1u);
+          atomicAdd(&sh.weight[b], w4[e]);
+        }
+      });
+    } else each_logit([&](float z, int) { atomicAdd(&sh.count[bin_of(z)], 1u); });
+    __syncthreads();
+    scan_bins();
+    const bool counted = by_count && (uint32_t)top_k < n_live;
+    if (few_by_count && !counted) {                  // no more than those few are live
+      each_logit([&](float z, int i) { if (live(z)) keep(order_of(z), i); });
+      __syncthreads();
+      few = true;
+    }
+    bool listed = false;
+#pragma clang loop unroll(disable)
+    for (int limit = counted ? 0 : 1; limit < (by_sum ? 2 : 1); ++limit) {
+      by_n = limit == 0;
+      most = (uint32_t)top_k;
+      if (!by_n) {
+        if (!weighed) {
+          each([&](float z, int) { if (live(z)) atomicAdd(&sh.weight[bin_of(z)], weigh(z)); });
+          __syncthreads();
+          scan_bins();
+        }
+        if (counted && !few) {                       // top_p's share is one of whole bins, and of what top-k leaves of the one that it ends in
+          u64 mine = 0;
+          uint32_t none;
+#pragma unroll
+          for (int k = 0; k < PB; ++k) mine += tid * PB + k < end ? w[k] : 0;
+          if (listed) {
+            for (int j = tid; j < (int)sh.n_list; j += NT) mine += last.holds(sh.list_key[j], sh.list_index[j]) ? sh.list_weight[j] : 0;
+          } else {
+            each_logit([&](float z, int i) { if (bin_of(z) == end && last.holds(order_of(z), i)) mine += weigh(z); });
+          }
+          block_sum(0, mine, &none, &total);
+        }
+        enough = enough_of(total);
+      }
+      end = find_bin();
+      listed = sh.in_count <= (uint32_t)kList;
+      const bool gather = listed && !few && (by_n ? few_by_count : !counted && sh.above_count + sh.in_count <= (uint32_t)kFew);
+      if (!listed) {                                 // many equal logits
+        const Last held_by = last;
+        last = {0u, -1};                             // the largest key from which on there is enough, then, of that key, the lowest index up to which
+#pragma clang loop unroll(disable)
+        for (int step = 49; step >= 0; --step) {
+          const Last trial = step >= 18 ? Last{last.key | 1u << (step - 18), 0x7FFFFFFF} : Last{last.key, last.index + (1 << step)};
+          uint32_t c = 0, all_n;
+          u64 x = 0, all_w;
+          each([&](float z, int i) {
+            const uint32_t k = order_of(z);
+            if (live(z) && held_by.holds(k, i) && trial.holds(k, i)) { ++c; x += by_n ? 0 : weigh(z); }
+          });
+          block_sum(c, x, &all_n, &all_w);
+          const bool is_enough = by_n ? all_n >= most : all_w >= enough;
+          if (step >= 18 && is_enough) last.key = trial.key;
+          if (step < 18 && !is_enough) last.index = trial.index;
+        }
+        ++last.index;
+      } else if (few || gather || (by_n && by_sum)) {
+        if (few) {
+          each_few([&](float z, int i) {
+            if (bin_of(z) == end && last.holds(order_of(z), i)) list(z, i);
+          });
+        } else {
+          const float upto = least_of_bins(end);
+          each_logit([&](float z, int i) {
+            if (z >= upto) {
+              if (bin_of(z) == end) {
+                if (last.holds(order_of(z), i)) list(z, i);
+              } else if (gather) keep(order_of(z), i);
+            }
+          });
+        }
+        rank();
+        if (gather) {
+          for (int j = tid; j < (int)sh.n_list; j += NT)
+            if (last.holds(sh.list_key[j], sh.list_index[j])) keep(sh.list_key[j], sh.list_index[j]);
+          __syncthreads();
+          few = true;
+        }
+      } else listing = true;
+    }
   }
+  if (few) {
+    // ---- few candidates: their weights by the high bits of the index, then, where the random number falls, one by one
+    int low = 0;
+    while ((V - 1) >> low >= NT) ++low;
+    static_assert((ADSA_MAX_VOCAB - 1) / 1024 < 4 * kWave && kList >= 4 * kWave, "a wave's lanes take four");
+    __syncthreads();
+    sh.run_weight[tid] = 0;
+    if (tid < 4 * kWave) sh.list_weight[tid] = 0;
+    __syncthreads();
+    constexpr int PF = kFew / NT;
+    u64 weight[PF];
+#pragma unroll
+    for (int k = 0; k < PF; ++k) {
+      const int j = tid + k * NT;
+      weight[k] = 0;
+      if (j < (int)sh.n_few && last.holds(sh.few_key[j], sh.few_index[j]) && logit_of(sh.few_key[j]) >= z_min) {
+        weight[k] = weigh(logit_of(sh.few_key[j]));
+        atomicAdd(&sh.run_weight[sh.few_index[j] >> low], weight[k]);
+      }
+    }
+    __syncthreads();
+    find_run(sh.run_weight[tid]);
+    const int from = sh.run << low;
+#pragma unroll
+    for (int k = 0; k < PF; ++k) {
+      const int j = tid + k * NT;
+      if (weight[k] != 0 && sh.few_index[j] >> low << low == from) {
+        sh.list_weight[sh.few_index[j] - from] = weight[k];
+        sh.list_key[sh.few_index[j] - from] = sh.few_key[j];
+      }
+    }
+    __syncthreads();
+    if (wave == 0) {
+      u64 w[4], sum = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { w[e] = sh.list_weight[lane * 4 + e]; sum += w[e]; }
+      const int e = pick4(sh.left, w, sum, wave_scan(sum));
+      if (e >= 0) answer(from + lane * 4 + e, logit_of(sh.list_key[lane * 4 + e]));
+    }
+    return;
+  }
+  // ---- the candidates' weight by runs; where they end in a bin whose logits are still to be listed, these are added when they are ranked
+  {
+    const float whole = least_of_bins(end - 1), before = fmaxf(whole, z_min), upto = end < BINS ? least_of_bins(end) : INFINITY;
+    u64 sum = 0;
+    each_group([&](const float (&z)[4], int i, int g) {
+      bool in[4], on_border = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        in[e] = z[e] >= before;
+        on_border |= z[e] >= upto && z[e] < whole;
+      }
+      if (on_border) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (z[e] >= upto && z[e] < whole && last.holds(order_of(z[e]), i + e)) {
+            if (listing) list(z[e], i + e);
+            else in[e] = z[e] >= z_min;
+          }
+      }
+      if (in[0] | in[1] | in[2] | in[3]) {
+        u64 w[4];
+        weigh(z, w);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum += in[e] ? w[e] : 0;
+      }
+      if (g % kRun == kRun - 1 || g == groups - 1) {
+        sum = wave_sum(sum);
+        if (lane == 0) sh.run_weight[wave * runs + g / kRun] = sum;
+        sum = 0;
+      }
+    });
+  }
+  if (listing) {
+    rank();
+    for (int j = tid; j < (int)sh.n_list; j += NT) {
+      const int i = sh.list_index[j], of_wave = i / (groups * kGroup), at = i - of_wave * groups * kGroup;
+      if (last.holds(sh.list_key[j], i) && logit_of(sh.list_key[j]) >= z_min) atomicAdd(&sh.run_weight[of_wave * runs + at / (kRun * kGroup)], sh.list_weight[j]);
+    }
+  }
+  __syncthreads();
+  find_run(tid < NW * runs ? sh.run_weight[tid] : 0);
   // ---- its own logits
   if (wave != sh.run / runs) return;
   u64 left = sh.left;
   for (int g = sh.run % runs * kRun; g < groups; ++g) {
     const int i = first + g * kGroup;
     float z[4];
-    group_of(g, z);
+    if (g < held) held_group(g, z);
+    else {
+      Raw x;
+      fetch(g, x);
+      decode(g, x, z);
+      only_infinite(z);
+    }
     u64 w[4], sum = 0;
+    weigh(z, w);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) { w[e] = weight_of(z[e], i + e); sum += w[e]; }
+    for (int e = 0; e < 4; ++e) {
+      w[e] = z[e] >= z_min && live(z[e]) && last.holds(order_of(z[e]), i + e) ? w[e] : 0;
+      sum += w[e];
+    }
     const u64 upto = wave_scan(sum), whole = lane_of(upto, kWave - 1);
     if (left >= whole) {
       left -= whole;
       continue;
     }
-    u64 from = upto - sum;
-    if (left >= from && left < upto) {
-      int e = 0;
-#pragma unroll
-      for (int k = 0; k < 3; ++k)
-        if (e == k && left - from >= w[k]) { from += w[k]; ++e; }
-      const float ze = e == 0 ? z[0] : e == 1 ? z[1] : e == 2 ? z[2] : z[3];
-      finish(i + e, (float)(((double)ze - (double)top) / (double)T - log((double)sh.above_weight * (1.0 / kOne))));
-    }
+    const int e = pick4(left, w, sum, upto);
+    if (e >= 0) answer(i + e, e == 0 ? z[0] : e == 1 ? z[1] : e == 2 ? z[2] : z[3]);
     break;
   }
 }
@@ -462,8 +687,9 @@ hipError_t launch_n(SampleArgs A, bool vec, hipStream_t st) {
   const int most = kHeld<NT, BINS>;
   A.held = A.held < most ? A.held : most;
   const size_t lds = (size_t)A.held * NT * 16;
-  if (vec) k_sample<EB, NT, BINS, true><<<dim3((unsigned)A.n_rows), NT, lds, st>>>(A);
-  else k_sample<EB, NT, BINS, false><<<dim3((unsigned)A.n_rows), NT, lds, st>>>(A);
+  auto launch = [&](auto v, auto g) { k_sample<EB, NT, BINS, decltype(v)::value, decltype(g)::value><<<dim3((unsigned)A.n_rows), NT, lds, st>>>(A); };
+  auto of_pairs = [&](auto v) { A.guided ? launch(v, std::true_type()) : launch(v, std::false_type()); };
+  vec ? of_pairs(std::true_type()) : of_pairs(std::false_type());
   return hipGetLastError();
 }
 
@@ -484,8 +710,11 @@ hipError_t sample_prepare_kernels() {
   };
   auto both = [&](auto eb, auto nt, auto bins) {
     constexpr int EB = decltype(eb)::value, NT = decltype(nt)::value, BINS = decltype(bins)::value;
-    allow(k_sample<EB, NT, BINS, true>, kHeld<NT, BINS> * NT * 16);
-    allow(k_sample<EB, NT, BINS, false>, kHeld<NT, BINS> * NT * 16);
+    constexpr int bytes = kHeld<NT, BINS> * NT * 16;
+    allow(k_sample<EB, NT, BINS, true, false>, bytes);
+    allow(k_sample<EB, NT, BINS, true, true>, bytes);
+    allow(k_sample<EB, NT, BINS, false, false>, bytes);
+    allow(k_sample<EB, NT, BINS, false, true>, bytes);
   };
   auto sizes = [&](auto eb) {
     using std::integral_constant;

@@ -1,8 +1,9 @@
 """adsa_sample against its definition in 64 bits: limits alone and together, ties, odd sizes and rows, guided pairs, settings by row, what is not a number.
 
-Bounds.  A weight is off by half of 2^-44 of the largest one's at most (it is a whole number of those) and 2^-50 of itself, so sums over V logits are off by
-V 2^-45 + 2^-50 of themselves: where a limit or the random number falls closer to a border than twice that, either side is right (`near`).  logprob is rounded to 32 bits once,
-and off by the sum's error besides."""
+Bounds.  A weight is off by 2^-45 of the largest one's (it is a whole number of 2^-44 of it) and, relative to itself, by its polynomial's (ln(2) / 512)^5 / 120 =
+2^-54.5 and by two roundings of 1 / T, each 2^-53 of the exponent, which is 31.2 at most: 2^-47; the reference's own quotient is rounded once, 2^-48 the same way.
+Together less than 2^-46, so sums over V logits are off by V 2^-45 + 2^-46 of themselves: where a limit or the random number falls closer to a border than twice
+that, either side is right (`off`).  logprob is rounded to 32 bits once, and off by the sum's error besides."""
 import numpy as np
 import pytest
 import torch
@@ -27,7 +28,7 @@ def reference(z, u, T=1.0, k=0, p=1.0, m=0.0):
     with np.errstate(invalid="ignore", over="ignore"):
         d = np.where(z == top, 0.0, (z - top) / np.float64(T))
     w = np.exp(d)
-    off = V * 2.0 ** -44 + 2.0 ** -49 * w.sum()              # twice a sum's error
+    off = V * 2.0 ** -44 + 2.0 ** -45 * w.sum()              # twice a sum's error
     order = np.argsort(-z, kind="stable")
     if 0 < k < V:
         order = order[:k]
@@ -130,6 +131,17 @@ def test_ties_go_to_the_lowest_index(V, levels, settings):
     gen = torch.Generator().manual_seed(V + levels)
     logits = torch.randint(0, levels, (6, V), generator=gen).float().to(DEV) * 0.5
     u = torch.tensor([0.0, 0.1, 0.5, 0.9, 0.999, 0.99999994], device=DEV)
+    check(logits, u, ambiguous=1.0, **settings)
+
+
+@pytest.mark.parametrize("V", [4000, 16384, 20001, 70000, 200000])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("scale", [0.01, 0.5, 60.0])
+@pytest.mark.parametrize("settings", [dict(top_p=0.999, min_p=0.6), dict(top_p=0.3, min_p=0.97), dict(top_k=2500, top_p=0.999, min_p=0.6), dict(top_k=2048, top_p=0.5), dict(top_k=2049, min_p=0.5),
+                                      dict(top_p=0.02), dict(min_p=0.9)])
+def test_few_and_many_candidates(V, dtype, scale, settings):
+    """Flat rows, of which a limit leaves thousands, and steep ones; what min_p asks above and below where top_p ends."""
+    logits, u = some(4, V, dtype, V + 5, scale)
     check(logits, u, ambiguous=1.0, **settings)
 
 
