@@ -2,14 +2,18 @@
 
     python examples/shared_prompt.py                       # 4 prompts, 8 images each, bf16
     python examples/shared_prompt.py --dtype f32 --check   # ... and the same images with the prompt in every image's own cache
+    python examples/shared_prompt.py --sample --check --page 16        # ... whose tokens are drawn, and those caches in pages of 16 slots
 
 A step of the loop is what a serving program does around its matrix products:
 
     prompts:  adsa_append  (rotary positions on the way into the caches)  ->  adsa_prefill (the prompt sees itself whole)
     images:   adsa_rotate  ->  adsa_select  ->  adsa_attend_shared (own list and the group's prompt)  ->  adsa_compact
 
+    tokens:   adsa_sample (with --sample: temperature, top-k and top-p; otherwise the images are given)
+
 Rows and columns are the rotary axes of image tokens, text counts along both.  With --check the images are decoded a second time by
-adsa_step over caches that hold the prompt themselves, and the logits of the two runs are compared.
+adsa_step over caches that hold the prompt themselves, and the logits of the two runs are compared.  With --page these caches lie in pages, which an
+image gets as it grows and gives back as it evicts (adsa_append_paged, adsa_prefill_paged, adsa_attend_paged, adsa_compact_paged).
 """
 from __future__ import annotations
 
@@ -22,7 +26,7 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2506_18226_amd import binding as B  # noqa: E402
-from paper_2506_18226_amd.batch import LayerBatch  # noqa: E402
+from paper_2506_18226_amd.batch import LayerBatch, PagedBatch, Sampler  # noqa: E402
 
 DEV = "cuda:0"
 
@@ -106,10 +110,11 @@ def run(args):
                   dtype=B.F32 if args.dtype == "f32" else B.BF16, score_mode=B.SCORE_ATTN_MASS)
     own_cap = args.budget + 3 * W
 
-    def caches(n_seq, cap, prefix, step):
+    def caches(n_seq, cap, prefix, step, page=0):
         out = []
         for _ in model.layers:
-            batch = LayerBatch(B.make_params(n_seq=n_seq, cap=cap, **common), DEV)
+            params = B.make_params(n_seq=n_seq, cap=cap, **common)
+            batch = PagedBatch(params, n_pages=n_seq * -(-cap // page), page_size=page, device=DEV) if page else LayerBatch(params, DEV)
             s = batch.seqs_host
             s["grid_origin"] = s["n_keep_prefix"] = prefix
             s["budget"], s["step"] = args.budget, step
@@ -130,26 +135,52 @@ def run(args):
         own[i].attend_shared(shared[i], q, k, v, flags=B.FLAG_APPEND)
         own[i].compact(B.FLAG_ADVANCE)
 
+    sampler = Sampler(n, args.vocab, B.F32, device=DEV, temperature=args.temperature, top_k=args.top_k, top_p=args.top_p) if args.sample else None
+    uniform = torch.rand(args.steps, n, generator=gen).to(DEV)
     logits, ms = [], 0.0
     for t in range(args.steps):
         torch.cuda.synchronize()
         t0 = time.perf_counter()
         out = model.step(own, images[t], attend_shared)
+        if sampler is not None:
+            sampler.sample(out, uniform[t], own[0].seqs)
+            if t + 1 < args.steps:
+                images[t + 1] = sampler.token
         torch.cuda.synchronize()
         ms += (time.perf_counter() - t0) * 1e3 if t else 0.0                 # (the first step allocates workspaces)
         logits.append(out.cpu())
     for batch in own + kept:
         assert not batch.read_seqs()["status"].any()
     rows = 2 * args.layers * args.heads * args.head_dim * (4 if args.dtype == "f32" else 2)
-    result = dict(logits=torch.stack(logits), ms_per_step=ms / max(1, args.steps - 1), cache_mib=rows * (sum(lens) + n * own_cap) / 2 ** 20,
+    result = dict(logits=torch.stack(logits), images=images.cpu(), ms_per_step=ms / max(1, args.steps - 1), cache_mib=rows * (sum(lens) + n * own_cap) / 2 ** 20,
                   cache_mib_whole=rows * (sum(of_image) + n * own_cap) / 2 ** 20)
     print(f"{groups} prompts of up to {max(lens)} tokens, {each} images each, {args.layers} layers: {result['ms_per_step']:.3f} ms a step; "
           f"caches {result['cache_mib']:.1f} MiB, with the prompt in each {result['cache_mib_whole']:.1f}", flush=True)
     if args.check:
         # ---- the prompt in every image's own cache
-        whole = caches(n, own_cap + max(lens), of_image, 0)
+        whole = caches(n, own_cap + max(lens), of_image, 0, args.page)
+
+        def pages():                                                         # for what an image has, and its next token: every layer has as many
+            if not args.page:
+                return
+            n_res = whole[0].read_seqs()["n_res"]
+            for batch in whole:
+                for b in range(n):
+                    slots = int(n_res[b]) + 1 if n_res[b] else lens[b // each]
+                    batch.release(b, slots)
+                    batch.reserve(b, slots)
+                batch.upload_table()
+
+        pages()
         model.prompts(whole, of_image, torch.cat([p for p in prompts for _ in range(each)]).to(DEV))
-        ref = [model.step(whole, images[t], lambda i, q, k, v: whole[i].step(q, k, v)).cpu() for t in range(args.steps)]
+        ref, used = [], 0
+        for t in range(args.steps):
+            pages()
+            used = max(used, sum(int((batch.table_host >= 0).sum()) for batch in whole) if args.page else 0)
+            ref.append(model.step(whole, images[t], lambda i, q, k, v: whole[i].step(q, k, v)).cpu())
+        if args.page:
+            assert not any(batch.read_seqs()["status"].any() for batch in whole)
+            print(f"at most {used} of {sum(batch.n_pages for batch in whole)} pages of {args.page} slots in use", flush=True)
         result["difference"] = float((torch.stack(ref) - result["logits"]).abs().max() / result["logits"].abs().max())
         print(f"largest difference of logits from caches that hold the prompt: {result['difference']:.2e} of the largest logit", flush=True)
     return result
@@ -158,8 +189,11 @@ def run(args):
 def parser():
     p = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     for name, value in (("layers", 4), ("heads", 4), ("q_per_kv", 2), ("head_dim", 64), ("vocab", 1024), ("prompts", 4), ("images", 8), ("prompt_len", 120),
-                        ("grid", 16), ("steps", 40), ("budget", 24), ("seed", 0)):
+                        ("grid", 16), ("steps", 40), ("budget", 24), ("seed", 0), ("page", 0), ("top_k", 100)):
         p.add_argument("--" + name.replace("_", "-"), type=int, default=value)
+    for name, value in (("temperature", 0.9), ("top_p", 0.95)):
+        p.add_argument("--" + name.replace("_", "-"), type=float, default=value)
+    p.add_argument("--sample", action="store_true")
     p.add_argument("--dtype", choices=("bf16", "f32"), default="bf16")
     p.add_argument("--check", action="store_true")
     return p

@@ -1,5 +1,8 @@
 """Caches in pages: each call against its definition in 64 bits, and against the dense call on the same rows, which it has to repeat bit by bit (the same
 sums in the same order, from other places)."""
+import importlib.util
+import os
+
 import numpy as np
 import pytest
 import torch
@@ -629,3 +632,16 @@ def test_rows_beyond_four_gib_of_a_pool():
     B.adsa_prefill_paged(p, pages, tokens, None, d.batch.seqs, q, outs[1], lses[1], ws, B.FLAG_NO_ACCUMULATE)
     torch.cuda.synchronize()
     assert same_bits(*outs) and same_bits(*lses)
+
+
+def test_images_drawn_and_decoded_over_pages_by_the_example():
+    """The example's images with drawn tokens, once beside a kept prompt and once with it in caches of pages; fp32 as in its own test: 1e-4 of a logit."""
+    spec = importlib.util.spec_from_file_location("shared_prompt", os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "shared_prompt.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    args = "--layers 3 --prompts 2 --images 3 --prompt-len 45 --grid 6 --steps 15 --budget 8 --heads 2 --q-per-kv 1 --dtype f32 --vocab 500 --check --page 16 --sample --top-k 20"
+    r = m.run(m.parser().parse_args(args.split()))
+    assert torch.isfinite(r["logits"]).all() and r["difference"] < 1e-4
+    logits, drawn = r["logits"][:-1], r["images"][1:].long()
+    rank = (logits > logits.gather(2, drawn[..., None])).sum(2)
+    assert int(rank.max()) < 20 and len(drawn.unique()) > 1
