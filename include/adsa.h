@@ -478,7 +478,7 @@ typedef struct adsa_sampling { /* [host] */
 } adsa_sampling;
 
 /*
- *   logits   dtype rows, aligned to their elements      uniform  float [n_rows] in [0, 1) (outside: the nearest that is)
+ *   logits   dtype rows, aligned to their elements, as all arrays are (else ADSA_ERR_ALIGN)      uniform  float [n_rows] in [0, 1) (outside: the nearest that is)
  *   token    int32 [n_rows], guided [2 * n_rows]: the partner gets the same token      logprob  float [n_rows], or NULL
  *   seqs     NULL, or as many records as token has numbers: a row whose record is inactive (step < 0 or a status) gets token -1 and logprob 0
  */

@@ -289,6 +289,7 @@ class PagedBatch(LayerBatch):
     def __init__(self, params: B.AdsaParams, n_pages: int, page_size: int = 64, device: str = "cuda:0"):
         self.page_size, self.n_pages = page_size, n_pages
         super().__init__(params, device)
+        self.upload_seqs()                                                     # inactive until the caller's own are there
 
     def _allocate_caches(self) -> None:
         p = self.params

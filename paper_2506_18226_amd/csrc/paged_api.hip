@@ -118,6 +118,9 @@ int adsa_sample(const adsa_sampling* s, const adsa_seq* seqs, const void* logits
   if (!s->temperatures && !(s->temperature >= 0.0f && std::isfinite(s->temperature))) return ADSA_ERR_SHAPE;
   if ((!s->top_ps && std::isnan(s->top_p)) || (!s->min_ps && std::isnan(s->min_p))) return ADSA_ERR_SHAPE;
   if (reinterpret_cast<uintptr_t>(logits) % (s->dtype == ADSA_F32 ? 4 : 2) != 0) return ADSA_ERR_ALIGN;
+  for (const void* x : {(const void*)uniform, (const void*)token, (const void*)logprob, (const void*)s->temperatures, (const void*)s->top_ks, (const void*)s->top_ps,
+                        (const void*)s->min_ps})
+    if ((reinterpret_cast<uintptr_t>(x) & 3u) != 0) return ADSA_ERR_ALIGN;
   const int rc = ensure_device_ready();
   if (rc) return rc;
   return launch_sample(*s, seqs, logits, uniform, token, logprob, reinterpret_cast<hipStream_t>(stream)) == hipSuccess ? ADSA_OK : ADSA_ERR_LAUNCH;

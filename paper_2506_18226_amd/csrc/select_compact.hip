@@ -827,21 +827,22 @@ hipError_t launch_step_finish(const adsa_params& p, adsa_seq* seqs, int32_t* kee
 static hipError_t launch_paged_plan(const adsa_params& p, const PageArgs& pages, adsa_seq* seqs, int32_t* keep_map, int32_t* plan, bool advance_step, hipStream_t st) {
   const float* const none = nullptr;
 #define ADSA_PAGED_PLAN(NT, S, RB)                                                                                                              \
-  do {                                                                                                                                          \
+  if (p.cap <= NT * S) {                                                                                                                        \
     hipLaunchKernelGGL((k_compact_plan<NT, S, RB, true>), dim3(p.n_seq), dim3(NT), 0, st, lo32(seqs), lo32(keep_map), lo32(plan), lo32(none),     \
                        hi16s(seqs, keep_map), hi16s(plan, none), (uint32_t)p.cap, rank_flags(p, advance_step, moved_with_cache(p)),               \
                        p.grid_h * p.grid_w, p.grid_w, p.win_rows_back, p.win_recent_m, inv_width(p), p.n_heads * p.head_dim, pages);              \
     return hipGetLastError();                                                                                                                   \
-  } while (0)
-  if (p.cap <= 256) ADSA_PAGED_PLAN(256, 1, rank_batch(1));
-  if (p.cap <= 512) ADSA_PAGED_PLAN(256, 2, rank_batch(2));
-  if (p.cap <= 768) ADSA_PAGED_PLAN(256, 3, 12);
-  if (p.cap <= 1024) ADSA_PAGED_PLAN(512, 2, rank_batch(2));
-  if (p.cap <= 2048) ADSA_PAGED_PLAN(512, 4, rank_batch(4));
-  if (p.cap <= 3072) ADSA_PAGED_PLAN(512, 6, rank_batch(6));
-  if (p.cap <= 4096) ADSA_PAGED_PLAN(1024, 4, rank_batch(4));
-  if (p.cap <= 6144) ADSA_PAGED_PLAN(1024, 6, rank_batch(6));
-  ADSA_PAGED_PLAN(1024, 8, rank_batch(8));
+  }
+  ADSA_PAGED_PLAN(256, 1, rank_batch(1))
+  ADSA_PAGED_PLAN(256, 2, rank_batch(2))
+  ADSA_PAGED_PLAN(256, 3, 12)
+  ADSA_PAGED_PLAN(512, 2, rank_batch(2))
+  ADSA_PAGED_PLAN(512, 4, rank_batch(4))
+  ADSA_PAGED_PLAN(512, 6, rank_batch(6))
+  ADSA_PAGED_PLAN(1024, 4, rank_batch(4))
+  ADSA_PAGED_PLAN(1024, 6, rank_batch(6))
+  ADSA_PAGED_PLAN(1024, 8, rank_batch(8))
+  return hipErrorInvalidValue;                       // (resolve_params allows no longer cache)
 }
 
 static hipError_t launch_move(const adsa_params& p, const adsa_seq* seqs, const int32_t* keep_map, const int32_t* plan, bool scores, bool advance, hipStream_t st) {

@@ -645,3 +645,158 @@ def test_images_drawn_and_decoded_over_pages_by_the_example():
     logits, drawn = r["logits"][:-1], r["images"][1:].long()
     rank = (logits > logits.gather(2, drawn[..., None])).sum(2)
     assert int(rank.max()) < 20 and len(drawn.unique()) > 1
+
+
+def small(n, cap, G, W=5, budget=8, page=16, **kw):
+    params = B.make_params(n_seq=n, n_heads=3, head_dim=64, grid_h=9, grid_w=W, win_rows_back=1, win_col_radius=2, dtype=B.BF16, score_mode=B.SCORE_ATTN_MASS, cap=cap, q_per_kv=G, **kw)
+    return PagedBatch(params, n_pages=n * -(-cap // page) + 2, page_size=page, device=DEV)
+
+
+@pytest.mark.parametrize("G", [0, 4])
+def test_sequences_that_share_the_pages_of_a_prompt(G):
+    """The pages of a pinned prompt in all sequences' tables, against one copy for each: evictions write behind them only."""
+    n, h, D, W, budget, P = 4, 3, 64, 5, 8, 32
+    cap = P + budget + 3 * W
+    gen = torch.Generator().manual_seed(12)
+    K, V = (randn(gen, P, h, D, dtype=torch.bfloat16).to(DEV) for _ in range(2))
+    batches = [small(n, cap, G) for _ in range(2)]
+    for which, batch in enumerate(batches):
+        s = batch.seqs_host
+        s["grid_origin"] = s["n_keep_prefix"] = s["n_res"] = P
+        s["budget"], s["step"] = budget, 1
+        batch.upload_seqs()
+        batch.pos[:] = torch.arange(cap, dtype=torch.int32, device=DEV)
+        for b in range(n):
+            batch.reserve(b, cap)
+            if which and b:
+                batch.table_host[b, :P // 16] = batch.table_host[0, :P // 16]
+        batch.upload_table()
+        for b in range(n):
+            batch._put_rows(b, K, V)
+    hq = h * max(G, 1)
+    own, shared = batches
+    prompt = shared.cache_rows(shared.K, 0, P).clone(), shared.cache_rows(shared.V, 0, P).clone()
+    for t in range(4 * W + 1):
+        q, k, v = (randn(gen, n, heads, D, dtype=torch.bfloat16).to(DEV) for heads in (hq, h, h))
+        for batch in batches:
+            batch.step(q, k, v)
+        same_records(own, shared)
+        assert same_bits(own.out, shared.out) and same_bits(own.lse, shared.lse), t
+    n_res = own.read_seqs()["n_res"]
+    assert (n_res < P + 4 * W).all()
+    for b in range(n):
+        for pools in ((own.K, shared.K), (own.V, shared.V)):
+            assert same_bits(*(batch.cache_rows(pool, b, int(n_res[b])) for batch, pool in zip(batches, pools))), b
+    assert same_bits(prompt[0], shared.cache_rows(shared.K, 0, P)) and same_bits(prompt[1], shared.cache_rows(shared.V, 0, P))
+
+
+@pytest.mark.parametrize("G", [0, 4])
+def test_prompts_in_a_graph(G):
+    """A captured append and prefill, replayed with other rows and tables and with eager ones between, against eager calls on another batch."""
+    h, D, lens = 3, 64, [70, 1, 33]
+    n, cap, hq, T = len(lens), 96, 3 * max(G, 1), sum(lens)
+    begin = torch.tensor([0, 70, 71, 104], dtype=torch.int32, device=DEV)
+    tokens = B.make_tokens(begin, torch.zeros(n, dtype=torch.int32, device=DEV), T, max(lens))
+    batches = [small(n, cap, G) for _ in range(2)]
+    for batch in batches:
+        for b in range(n):
+            batch.reserve(b, lens[b])
+        batch.upload_table()
+        batch.seqs_host["step"] = 0
+        batch.upload_seqs()
+    gen = torch.Generator().manual_seed(21)
+    q, k, v = (torch.zeros(T, heads, D, dtype=torch.bfloat16, device=DEV) for heads in (hq, h, h))
+    rows = [(torch.zeros(T, hq, D, dtype=torch.bfloat16, device=DEV), torch.zeros(T, hq, D, dtype=torch.bfloat16, device=DEV), torch.zeros(T, hq, device=DEV)) for _ in batches]
+    empty = [batch.seqs.clone() for batch in batches]            # (records hold their own batch's addresses)
+
+    def run(i):
+        q_out, out, lse = rows[i]
+        batches[i].append(tokens, None, q, k, v, q_out, flags=B.FLAG_ADVANCE)
+        batches[i].prefill(tokens, q_out, out, lse)
+
+    def reset(i):
+        batches[i].seqs.copy_(empty[i])
+        batches[i].score.zero_()
+        batches[i].K.fill_(float("nan"))
+        batches[i].V.fill_(float("nan"))
+
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        run(1)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        run(1)
+    for t in range(6):
+        for x in (q, k, v):
+            x.copy_(randn(gen, *x.shape, dtype=torch.bfloat16))
+        if t == 3:
+            assert (batches[1].table_host[[0, 2], :3] >= 0).all()
+            batches[1].table_host[[0, 2], :3] = batches[1].table_host[[2, 0], :3]        # pages change places (both sequences have three at least)
+            batches[1].upload_table()
+        for i in range(2):
+            reset(i)
+        run(0)
+        if t % 3 == 1:
+            run(1)
+        else:
+            graph.replay()
+        torch.cuda.synchronize()
+        same_records(*batches)
+        for a, b in zip(*rows):
+            assert same_bits(a, b), t
+        assert torch.equal(batches[0].score, batches[1].score) and torch.isfinite(rows[0][1].float()).all()
+        for b in range(n):
+            assert same_bits(batches[0].cache_rows(batches[0].K, b, lens[b]), batches[1].cache_rows(batches[1].K, b, lens[b])), (t, b)
+
+
+def test_calls_on_two_streams_at_once():
+    """Two batches over one pool (other pages of it), each on its own stream, many steps without a wait, against the same one after the other."""
+    n, h, D, W, P = 3, 3, 64, 5, 16
+    cap, gen = P + 8 + 3 * W, torch.Generator().manual_seed(5)
+    rows = [[tuple(randn(gen, n, h, D, dtype=torch.bfloat16).to(DEV) for _ in range(3)) for _ in range(12)] for _ in range(2)]
+    K = [randn(gen, n, P, h, D, dtype=torch.bfloat16).to(DEV) for _ in range(2)]
+    results = []
+    for together in (False, True):
+        batches = [small(n, cap, 0) for _ in range(2)]
+        pool = [torch.full((2 * batches[0].n_pages, *batches[0].K.shape[1:]), float("nan"), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+        for i, batch in enumerate(batches):
+            batch.free_pages = list(range(i, 2 * batch.n_pages, 2))
+            batch.K, batch.V = pool
+            batch.pages = B.make_pages(batch.K, batch.V, batch.table, page_size=16)
+            s = batch.seqs_host
+            s["grid_origin"] = s["n_keep_prefix"] = s["n_res"] = P
+            s["budget"], s["step"] = 8, 1
+            batch.upload_seqs()
+            batch.pos[:] = torch.arange(cap, dtype=torch.int32, device=DEV)
+            for b in range(n):
+                batch.reserve(b, cap)
+            batch.upload_table()
+            for b in range(n):
+                batch._put_rows(b, K[i][b], -K[i][b])
+        torch.cuda.synchronize()
+        streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+        for t in range(12):
+            for batch, stream, given in zip(batches, streams, rows):
+                batch.step(*given[t], stream=stream)
+                if not together:
+                    torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        results.append([(batch.out.clone(), batch.lse.clone(), batch.score.clone(), batch.read_seqs()["n_res"].copy()) for batch in batches])
+    for a, b in zip(*results):
+        assert same_bits(a[0], b[0]) and same_bits(a[1], b[1]) and torch.equal(a[2], b[2]) and (a[3] == b[3]).all()
+
+
+def test_a_batch_without_records_is_inactive():
+    batch = small(2, 64, 0)
+    batch.reserve(0, 40)
+    batch.upload_table()
+    rows = [torch.ones(2, 3, 64, dtype=torch.bfloat16, device=DEV) for _ in range(3)]
+    batch.out.fill_(7)
+    batch.step(*rows)
+    begin = torch.tensor([0, 1, 2], dtype=torch.int32, device=DEV)
+    tokens = B.make_tokens(begin, torch.zeros(2, dtype=torch.int32, device=DEV), 2, 1)
+    batch.append(tokens, None, *rows, torch.empty_like(rows[0]), flags=B.FLAG_ADVANCE)
+    torch.cuda.synchronize()
+    assert (batch.out == 0).all() and (batch.K == 0).all() and (batch.read_seqs()["n_res"] == 0).all() and (batch.seqs_host["step"] == -1).all()

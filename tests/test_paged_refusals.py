@@ -144,6 +144,16 @@ def test_sampling_pointers(lib):
     for name in ("logits", "uniform", "token"):
         assert sample(lib, sampling(), **{name: None}) == NULL, name
     assert sample(lib, sampling(), logits=OK + 2) == ALIGN and sample(lib, sampling(dtype=B.BF16), logits=OK + 1) == ALIGN
+    for name in ("uniform", "token", "logprob"):
+        assert sample(lib, sampling(), **{name: OK + 2}) == ALIGN, name
+    for name in ("temperatures", "top_ks", "top_ps", "min_ps"):
+        assert sample(lib, sampling(**{name: OK + 1})) == ALIGN, name
+
+
+def test_struct_sizes_match_the_header():
+    """3 addresses, 3 distances, 4 numbers; 4 numbers, a distance, 6 numbers, 4 addresses."""
+    assert C.sizeof(B.AdsaPages) == 6 * 8 + 4 * 4 and B.AdsaPages.page_size.offset == 48
+    assert C.sizeof(B.AdsaSampling) == 4 * 4 + 8 + 6 * 4 + 4 * 8 and B.AdsaSampling.row_stride.offset == 16 and B.AdsaSampling.temperatures.offset == 48
 
 
 # ---- the binding's checks
