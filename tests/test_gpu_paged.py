@@ -789,14 +789,19 @@ def test_calls_on_two_streams_at_once():
 
 
 def test_a_batch_without_records_is_inactive():
+    """A step writes zeros and no cache; tokens enter whatever a sequence's step is, where it has a page for them."""
     batch = small(2, 64, 0)
     batch.reserve(0, 40)
     batch.upload_table()
     rows = [torch.ones(2, 3, 64, dtype=torch.bfloat16, device=DEV) for _ in range(3)]
     batch.out.fill_(7)
     batch.step(*rows)
+    torch.cuda.synchronize()
+    assert (batch.out == 0).all() and (batch.K == 0).all() and (batch.read_seqs()["n_res"] == 0).all() and (batch.seqs_host["step"] == -1).all()
     begin = torch.tensor([0, 1, 2], dtype=torch.int32, device=DEV)
     tokens = B.make_tokens(begin, torch.zeros(2, dtype=torch.int32, device=DEV), 2, 1)
     batch.append(tokens, None, *rows, torch.empty_like(rows[0]), flags=B.FLAG_ADVANCE)
     torch.cuda.synchronize()
-    assert (batch.out == 0).all() and (batch.K == 0).all() and (batch.read_seqs()["n_res"] == 0).all() and (batch.seqs_host["step"] == -1).all()
+    assert batch.read_seqs()["n_res"].tolist() == [1, 0] and batch.seqs_host["status"].tolist() == [0, B.SEQ_CACHE_FULL]
+    page = int(batch.table_host[0, 0])
+    assert (batch.K[page, :, 0] == 1).all() and int((batch.K != 0).sum()) == 3 * 64 and int((batch.V != 0).sum()) == 3 * 64
