@@ -292,8 +292,8 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
   const double inv = 1.4426950408889634074 * kTable / (double)T;
   const Weigh weigh = {sh.table, inv, (double)top};
   // Bins of equal width below the largest, to the least or as far as a weight can be: what lies further is in the bins from BINS on, which nobody reads, and not live.
-  const float range = fminf(fminf(kReach * T, 1e38f), infinite ? 1.0f : top - least_z);
-  const float per_bin = range > 0.0f ? fminf((float)BINS * (1.0f - 0x1p-20f) / range, 1e38f) : 1.0f;
+  const float range = fminf(fminf(kReach * T, 1e38f), infinite ? 0.0f : top - least_z);
+  const float per_bin = fminf((float)BINS * (1.0f - 0x1p-20f) / range, 1e38f);         // (no range: all that is live is in bin 0, which is narrow)
   const float furthest = (float)(BINS + lane);       // (lanes whose logits are not live do not meet in one bin: 16384 of which most are far below 5.9 -> 2.0 us)
   auto bin_of = [&](float z) { return (int)fminf((top - z) * per_bin, furthest); };
   // The least logit for which `in` holds, which holds for all larger ones too, the largest among them: a wave tries 64 at a time.

@@ -145,6 +145,19 @@ def test_few_and_many_candidates(V, dtype, scale, settings):
     check(logits, u, ambiguous=1.0, **settings)
 
 
+@pytest.mark.parametrize("V", [300, 16384, 70000])
+@pytest.mark.parametrize("T", [0.01, 1.0, 50.0])
+@pytest.mark.parametrize("settings", [dict(top_p=0.9), dict(top_k=2), dict(top_p=0.5, min_p=0.1), dict(top_k=50, top_p=0.9), dict()])
+def test_rows_of_which_a_mask_leaves_one_or_a_few(V, T, settings):
+    gen = torch.Generator().manual_seed(V)
+    logits = torch.full((6, V), -INF)
+    for r, left in enumerate((1, 2, 3, 1, 600 if V > 600 else 200, 2)):
+        at = torch.randperm(V, generator=gen)[:left]
+        logits[r, at] = torch.randn(left, generator=gen) if r < 3 else torch.tensor(INF if r == 5 else -3.0)
+    u = torch.tensor([0.3, 0.6, 0.95, 0.0, 0.5, 0.7])
+    check(logits.to(DEV), u.to(DEV), temperature=T, ambiguous=1.0, **settings)
+
+
 def test_signed_zeros_are_equal():
     z = torch.zeros(4, 50, device=DEV)
     z[:, ::2] = -0.0
