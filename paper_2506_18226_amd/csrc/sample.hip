@@ -124,6 +124,7 @@ struct SampleShared {
   int few_index[kFew];
   uint32_t wave_count[2][NW];
   float wave_top[NW], wave_least[NW];
+  uint32_t least_key, most_key;          // in a bin
   uint32_t above_count, in_count, n_list, n_few, last_key;
   int bin, last_index, token, run;
 };
@@ -468,6 +469,8 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
           sh.in_count = n[k];
           sh.above_weight = wb;
           sh.n_list = 0;
+          sh.least_key = 0xFFFFFFFFu;
+          sh.most_key = 0u;
         }
         nb += n[k];
         wb += w[k];
@@ -528,21 +531,39 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
       listed = sh.in_count <= (uint32_t)kList;
       const bool gather = listed && !few && (by_n ? few_by_count : !counted && sh.above_count + sh.in_count <= (uint32_t)kFew);
       if (!listed) {                                 // many equal logits
+        // Of the bin's: the largest key from which on there is enough, then, of that key, the lowest index up to which.  (Between the least and the largest key of the
+        // bin, and weighing its logits alone: a row of 65536 fp32 of seven values, top-p 0.9, 270 us; over all keys and all logits 1100.)
+        const float least = least_of_bins(end), above = least_of_bins(end - 1);
         const Last held_by = last;
-        last = {0u, -1};                             // the largest key from which on there is enough, then, of that key, the lowest index up to which
+        uint32_t least_key = 0xFFFFFFFFu, most_key = 0u;
+        each([&](float z, int i) {
+          const uint32_t k = order_of(z);
+          if (z >= least && z < above && held_by.holds(k, i)) { least_key = min(least_key, k); most_key = max(most_key, k); }
+        });
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) { least_key = min(least_key, (uint32_t)__shfl_xor((int)least_key, d)); most_key = max(most_key, (uint32_t)__shfl_xor((int)most_key, d)); }
+        if (lane == 0) { atomicMin(&sh.least_key, least_key); atomicMax(&sh.most_key, most_key); }
+        __syncthreads();
+        const uint32_t first_key = sh.least_key, keys = sh.most_key - first_key;
+        const int index_bits = V > 1 ? 32 - __clz(V - 1) : 0, key_bits = keys ? 32 - __clz((int)keys) : 0;
+        last = {first_key, -1};
 #pragma clang loop unroll(disable)
-        for (int step = 49; step >= 0; --step) {
-          const Last trial = step >= 18 ? Last{last.key | 1u << (step - 18), 0x7FFFFFFF} : Last{last.key, last.index + (1 << step)};
+        for (int step = key_bits + index_bits - 1; step >= 0; --step) {
+          const bool by_key = step >= index_bits;
+          const Last trial = by_key ? Last{last.key + (1u << (step - index_bits)), 0x7FFFFFFF} : Last{last.key, last.index + (1 << step)};
+          if (by_key && trial.key - first_key > keys) continue;              // (no such key in the bin; the difference is below 2^key_bits)
           uint32_t c = 0, all_n;
           u64 x = 0, all_w;
           each([&](float z, int i) {
-            const uint32_t k = order_of(z);
-            if (live(z) && held_by.holds(k, i) && trial.holds(k, i)) { ++c; x += by_n ? 0 : weigh(z); }
+            if (z >= least && z < above) {
+              const uint32_t k = order_of(z);
+              if (held_by.holds(k, i) && trial.holds(k, i)) { ++c; x += by_n ? 0 : weigh(z); }
+            }
           });
           block_sum(c, x, &all_n, &all_w);
-          const bool is_enough = by_n ? all_n >= most : all_w >= enough;
-          if (step >= 18 && is_enough) last.key = trial.key;
-          if (step < 18 && !is_enough) last.index = trial.index;
+          const bool is_enough = by_n ? sh.above_count + all_n >= most : sh.above_weight + all_w >= enough;
+          if (by_key && is_enough) last.key = trial.key;
+          if (!by_key && !is_enough) last.index = trial.index;
         }
         ++last.index;
       } else if (few || gather || (by_n && by_sum)) {
