@@ -326,9 +326,12 @@ class PagedBatch(LayerBatch):
         self.table.copy_(torch.from_numpy(self.table_host))
 
     def _slots(self, b: int, n: int):
-        """Page and place in it of slots 0 .. n - 1 of sequence b."""
+        """Page and place in it of slots 0 .. n - 1 of sequence b, by the device's table."""
         slot = torch.arange(n, device=self.device)
-        return self.table[b].long()[slot // self.page_size], slot % self.page_size
+        page = self.table[b].long()[slot // self.page_size]
+        if not bool(((page >= 0) & (page < len(self.K))).all()):             # (as an index, -1 would be the pool's last page)
+            raise ValueError(f"sequence {b}: not all of its first {n} slots have a page of the pool in the device's table (reserve, then upload_table)")
+        return page, slot % self.page_size
 
     def _put_rows(self, b, k, v):
         page, place = self._slots(b, len(k))
