@@ -14,6 +14,7 @@ def host_batch(n_seq=4, cap=64, page=16, n_pages=8, layout="head_major"):
     batch.seqs_host, batch.vcos_u = np.zeros(n_seq, dtype=B.SEQ_DTYPE), None
     batch.pos, batch.score = torch.zeros(n_seq, cap, dtype=torch.int32), torch.zeros(n_seq, 2, cap)
     batch._allocate_caches()
+    batch.table = batch.table.clone()                        # (host tensors of numpy arrays share their memory)
     return batch
 
 
