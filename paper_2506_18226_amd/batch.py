@@ -302,25 +302,60 @@ class PagedBatch(LayerBatch):
         self.pages = B.make_pages(self.K, self.V, self.table, page_size=self.page_size, layout="head_major" if self.head_major else "slot_major")
 
     # ---- pages, on the host
+    def _named(self, page) -> np.ndarray:
+        """Whether a row of the table names each of these pages."""
+        return np.isin(page, self.table_host)
+
+    def _give_back(self, pages: np.ndarray) -> None:
+        """Pages that a row has just lost, the last first: free are those that no row names any more."""
+        free, n_pages = set(self.free_pages), getattr(self, "pages", self).n_pages         # (a pool may be larger than this batch's part of it)
+        for page, named in zip(pages[::-1].tolist(), self._named(pages[::-1])):
+            if not named and page not in free and 0 <= page < n_pages:
+                free.add(page)
+                self.free_pages.append(page)
+
     def reserve(self, b: int, slots: int) -> None:
-        """Pages for the first `slots` slots of sequence b; nothing changes if there are not as many."""
+        """Pages for the first `slots` slots of sequence b, which no row of the table names yet; nothing changes if there are not as many."""
         row = self.table_host[b]
         need = -(-slots // self.page_size)
         if not 0 <= slots <= self.params.cap:
             raise ValueError(f"slots: 0..{self.params.cap} expected, {slots} given")
         missing = [i for i in range(need) if row[i] < 0]
-        if len(missing) > len(self.free_pages):
-            raise MemoryError(f"{len(missing)} pages wanted, {len(self.free_pages)} free")
-        for i in missing:
-            row[i] = self.free_pages.pop()
+        taken, at = [], len(self.free_pages)
+        while len(taken) < len(missing) and at > 0:          # from the end, without what a row that was written by hand names
+            some = self.free_pages[max(0, at - len(missing) + len(taken)):at][::-1]
+            at -= len(some)
+            taken += [page for page, named in zip(some, self._named(some)) if not named]
+        if len(taken) < len(missing):
+            raise MemoryError(f"{len(missing)} pages wanted, {len(taken)} free")
+        if missing:
+            del self.free_pages[at:]
+            row[missing] = taken
 
     def release(self, b: int, slots: int = 0) -> None:
-        """Gives back the pages of sequence b that hold none of its first `slots` slots."""
+        """Gives back the pages of sequence b that hold none of its first `slots` slots.  One that other rows of the table name is free when the last of them
+        gives it back; a number that is no page of the pool is forgotten."""
         row = self.table_host[b]
-        for i in range(len(row) - 1, -(-slots // self.page_size) - 1, -1):
-            if row[i] >= 0:
-                self.free_pages.append(int(row[i]))
-                row[i] = -1
+        first = max(0, -(-slots // self.page_size))
+        given_up = row[first:].copy()
+        if (given_up >= 0).any():
+            row[first:] = -1
+            self._give_back(given_up)
+
+    def share(self, b: int, of: int, slots: int) -> None:
+        """Sequence b gets the pages that the first `slots` slots of sequence `of` fill (a page that they fill in part is left out), in place of its own.  Nothing
+        may write to them while both have them: a pinned prefix does not move."""
+        if not 0 <= slots <= self.params.cap:
+            raise ValueError(f"slots: 0..{self.params.cap} expected, {slots} given")
+        n = slots // self.page_size
+        given = self.table_host[of, :n].copy()
+        if (given < 0).any():
+            raise ValueError(f"sequence {of}: no pages for {slots} slots")
+        if b == of:
+            return
+        given_up = self.table_host[b, :n].copy()
+        self.table_host[b, :n] = given
+        self._give_back(given_up)
 
     def upload_table(self) -> None:
         self.table.copy_(torch.from_numpy(self.table_host))

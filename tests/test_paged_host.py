@@ -52,3 +52,89 @@ def test_rows_of_slots_without_a_page_are_refused(layout):
     batch.set_sequence(0, k=rows(0, 9.0), v=rows(0, 8.0), **{**call, "pos": np.arange(0)})           # (no row, no page)
     assert (batch.cache_rows(batch.K, 3, 5) == 9.0).all() and (batch.cache_rows(batch.V, 3, 5) == 8.0).all() and int((batch.K != 3.0).sum()) == 5 * 2 * 64
     assert batch.cache_rows(batch.K, 0, 0).shape[0] == 0
+
+
+# ---------------------------------------------------------------------------------------------------- pages of several sequences
+def in_use(batch):
+    return set(batch.table_host[batch.table_host >= 0].tolist())
+
+
+def all_there(batch, lost=()):
+    """Every page is free, once, or in the table."""
+    assert len(set(batch.free_pages)) == len(batch.free_pages) and not in_use(batch) & set(batch.free_pages)
+    assert in_use(batch) | set(batch.free_pages) | set(lost) == set(range(batch.n_pages))
+
+
+def test_a_shared_page_is_free_when_the_last_of_its_sequences_gives_it_back():
+    batch = host_batch(n_pages=9)
+    batch.reserve(0, 64)
+    batch.share(1, 0, 40)                                    # two whole pages
+    batch.reserve(1, 64)
+    assert list(batch.table_host[1, :2]) == list(batch.table_host[0, :2]) and not set(batch.table_host[1, 2:]) & set(batch.table_host[0]) and len(batch.free_pages) == 3
+    all_there(batch)
+    prompt = set(batch.table_host[0, :2].tolist())
+    batch.release(0)
+    assert len(batch.free_pages) == 5 and not prompt & set(batch.free_pages)
+    batch.reserve(2, 64)                                     # none of the pages that 1 still has
+    assert not set(batch.table_host[2].tolist()) & set(batch.table_host[1].tolist())
+    all_there(batch)
+    batch.release(1, 32)
+    all_there(batch)
+    batch.release(1)
+    batch.release(1)
+    all_there(batch)
+    assert prompt <= set(batch.free_pages)
+    batch.release(2, 17)
+    all_there(batch)
+    batch.reserve(3, 64)
+    with pytest.raises(MemoryError):
+        batch.reserve(0, 64)
+    assert (batch.table_host[0] == -1).all()
+    all_there(batch)
+
+
+def test_pages_that_sharing_replaces_are_free():
+    batch = host_batch(n_pages=9)
+    for b in (0, 1):
+        batch.reserve(b, 64)
+    own = set(batch.table_host[1, :3].tolist())
+    batch.share(1, 0, 48)
+    assert own <= set(batch.free_pages)
+    batch.share(1, 0, 48)                                    # once more: as it is
+    batch.share(0, 0, 64)
+    all_there(batch)
+    for what in ((2, 3, 16), (2, 0, 65), (2, 0, -1)):        # who has no page; no such slots
+        with pytest.raises(ValueError):
+            batch.share(*what)
+    batch.share(2, 0, 15)                                    # no whole page
+    assert (batch.table_host[2] == -1).all()
+    all_there(batch)
+
+
+def test_rows_written_by_hand():
+    """Numbers that a program writes into the table: a page in two rows is given back once, one that is taken is not given again, what is no page is forgotten."""
+    batch = host_batch(n_pages=9)
+    batch.reserve(0, 32)
+    batch.table_host[1, :2] = batch.table_host[0, :2]
+    batch.table_host[2, :2] = batch.free_pages[-1], 0x7FFFFFFF
+    hand = batch.free_pages[-1]
+    batch.reserve(3, 64)
+    assert hand not in batch.table_host[3] and hand not in batch.free_pages
+    all_there(type("without", (), dict(table_host=np.where(batch.table_host == 0x7FFFFFFF, -1, batch.table_host), free_pages=batch.free_pages, n_pages=9)))
+    for b in range(4):
+        batch.release(b)
+    assert sorted(batch.free_pages) == list(range(9)) and (batch.table_host == -1).all()
+
+
+def test_batches_that_take_their_pages_from_one_list():
+    a, b = host_batch(n_seq=2, n_pages=8), host_batch(n_seq=2, n_pages=8)
+    b.free_pages = a.free_pages
+    a.reserve(0, 64)
+    b.reserve(0, 48)
+    a.reserve(1, 16)
+    assert not b.free_pages and b.free_pages is a.free_pages and sorted(in_use(a) | in_use(b)) == list(range(8))
+    with pytest.raises(MemoryError):
+        b.reserve(1, 16)
+    a.release(0, 20)
+    b.reserve(1, 32)
+    assert not a.free_pages and sorted(in_use(a) | in_use(b)) == list(range(8))
