@@ -438,7 +438,8 @@ int adsa_append_paged(const adsa_params* p, const adsa_pages* pages, const adsa_
 int adsa_prefill_paged(const adsa_params* p, const adsa_pages* pages, const adsa_tokens* tokens, const adsa_mods* mods, adsa_seq* seqs, const void* q,
                        void* out, float* lse, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
 size_t adsa_prefill_paged_workspace_bytes(const adsa_params* p, const adsa_pages* pages, const adsa_tokens* tokens);   /* 0 if something is invalid */
-/* Listed slots have to be resident.  flags: ADSA_FLAG_NO_ACCUMULATE, ADSA_FLAG_APPEND, ADSA_FLAG_NEW_F32, ADSA_FLAG_ADVANCE. */
+/* Listed slots have to be resident.  A sequence with a status is skipped and gets zeros, whatever its list.
+   flags: ADSA_FLAG_NO_ACCUMULATE, ADSA_FLAG_APPEND, ADSA_FLAG_NEW_F32, ADSA_FLAG_ADVANCE. */
 int adsa_attend_paged(const adsa_params* p, const adsa_pages* pages, adsa_seq* seqs, const void* q, const void* k_new, const void* v_new,
                       const int32_t* sel_idx, const int32_t* sel_cnt, void* out, float* lse, uint32_t flags, void* workspace, size_t workspace_bytes,
                       void* stream);

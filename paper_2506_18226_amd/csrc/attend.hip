@@ -258,7 +258,7 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
   gchar* const v_base = (gchar*)sqp->v;
   gfloat* const score = (gfloat*)sqp->score;
   // (RANK: the rest of the record, as the ranking needs it)
-  const int step = RANK > 0 || PLAN > 0 ? sqp->step : 0, status_in = RANK > 0 ? sqp->status : 0;
+  const int step = RANK > 0 || PLAN > 0 ? sqp->step : 0, status_in = RANK > 0 || PAGED ? sqp->status : 0;
   const gint* const pos = RANK > 0 ? (const gint*)sqp->pos : nullptr;
   const BudgetOf budget(*sqp);
   const int n_keep_prefix = RANK > 0 ? sqp->n_keep_prefix : 0;
@@ -310,12 +310,14 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
       if (new_f32) { nk[1] = load16(k_new_g + 16); nv[1] = load16(v_new_g + 16); }
   }
   pin_uniform(cnt);
-  if constexpr (PAGED) pin_uniform(n_res);
+  if constexpr (PAGED) { pin_uniform(n_res); pin_uniform(status_in); }
   else { pin_uniform(k_base); pin_uniform(v_base); }
   pin_uniform(score); pin_uniform(pending);
   if constexpr (VF) pin_uniform(u_state);
 
-  cnt = min(cnt, sel_cap);
+  // (PAGED: a sequence with a status is skipped whatever its list.  One whose pages are no pages gets its status from this launch, so workgroups that start later
+  // may take this way to the same zeros; k_attend_finish goes by the status alone.)
+  cnt = PAGED && status_in != 0 ? 0 : min(cnt, sel_cap);
   // ---- RANK: k_select's part, of which this thread keeps the places of its slots and their old scores of this head
   uint32_t dest[kSlots], take = 0;
   float old_score[kSlots];
@@ -944,7 +946,7 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
 // normaliser from the chunks' (m, l), in chunk order; slice 0 merges the partial outputs and writes out / lse; every
 // slice adds the probabilities of its kFinishTokens tokens to the head's score row.
 constexpr int kFinishThreads = 256, kFinishTokens = 4 * kFinishThreads;
-// (PAGED: a sequence whose pages were not in order has its zeros already.)
+// (PAGED: a sequence with a status, which it had before the call or has for its pages, has its zeros already.)
 template <int EB, int D, bool PAGED = false>
 __global__ __launch_bounds__(kFinishThreads) void k_attend_finish(
     uint32_t seqs_lo, uint32_t idx_lo, uint32_t cnt_lo, uint32_t out_lo, uint32_t lse_lo, uint32_t lg_lo, uint32_t ml_lo, uint32_t acc_lo,

@@ -176,7 +176,7 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
   gchar* const k_rec = (gchar*)sqp->k;
   gchar* const v_rec = (gchar*)sqp->v;
   gfloat* const score_rec = (gfloat*)sqp->score;
-  const int pending = sqp->pending_slot, n_res = PAGED ? sqp->n_res : 0;
+  const int pending = sqp->pending_slot, n_res = PAGED ? sqp->n_res : 0, status_in = PAGED ? sqp->status : 0;
   __builtin_amdgcn_sched_barrier(0);                       // (the scalar loads leave first)
   const gint* const idx = (const gint*)address(idx_lo, seqs_idx_hi >> 16) + (size_t)b * sel_cap;
   const SlotList list(idx, sel_cap);
@@ -237,7 +237,7 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
     }
   }
   pin_uniform(cnt_raw);
-  if constexpr (PAGED) pin_uniform(n_res);
+  if constexpr (PAGED) { pin_uniform(n_res); pin_uniform(status_in); }
   else { pin_uniform(k_rec); pin_uniform(v_rec); }
   pin_uniform(score_rec); pin_uniform(pending);
   const long long head_stride_b = PAGED ? (long long)tail_address(offsetof(PagedGqaTail, head_stride_b)) : (long long)address(head_stride16, (heads_flags >> 19) & 0x1F) * 16;
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
   gchar* const v_base = (PAGED ? (gchar*)tail_address(offsetof(PagedGqaTail, v)) : v_rec) + hk * head_stride_b;
   gfloat* const score = score_rec + (size_t)hk * cap;
 
-  const int cnt = min(cnt_raw, sel_cap);
+  const int cnt = PAGED && status_in != 0 ? 0 : min(cnt_raw, sel_cap);          // (a sequence with a status is skipped: see k_attend)
   const GqaTail& block = [&]() -> const GqaTail& {
     if constexpr (PAGED) return T.a;
     else return T;
@@ -614,7 +614,7 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
 // the queries in ascending order, to the cache head's score row.
 constexpr int kFinishThreads = 256, kFinishTokens = 2 * kFinishThreads;
 static_assert(kMaxChunks == 16 && kFinishThreads == 16 * 16, "one thread per (query, chunk), a query's chunks in one 16-lane row");
-// (PAGED: a sequence whose pages were not in order has its zeros already.)
+// (PAGED: a sequence with a status, which it had before the call or has for its pages, has its zeros already.)
 template <int D, bool PAGED = false>
 __global__ __launch_bounds__(kFinishThreads) void k_gqa_finish(
     uint32_t seqs_lo, uint32_t idx_lo, uint32_t cnt_lo, uint32_t out_lo, uint32_t lse_lo, uint32_t lg_lo, uint32_t ml_lo, uint32_t acc_lo,
