@@ -450,7 +450,8 @@ size_t adsa_paged_workspace_bytes(const adsa_params* p);       /* of adsa_attend
 
 /* ---------------------------------------------------------------------------------------------------------------------------------
  * The next token of every row of logits, from random numbers that the caller brings.
- *   z[i]   the logit; guided: fp32(u + guidance * (c - u)), formed in 64 bits, of the conditional row's c and its partner's u
+ *   z[i]   the logit; guided: fp32(u + guidance * (c - u)), formed in 64 bits, of the conditional row's c and its partner's u; -infinity where c or u is
+ *          (a token that either row masks is masked); with guidance 1 it is c, whatever u is
  *   w[i]   exp((z[i] - max z) / temperature)
  * In descending order of z (equal ones: the lower index first) the candidates are the first top_k, of these as few as have together top_p of
  * their sum of w, and of these those with w >= min_p (relative to the largest, whose w is 1).  The token is the first candidate in ascending
@@ -481,7 +482,8 @@ typedef struct adsa_sampling { /* [host] */
 /*
  *   logits   dtype rows, aligned to their elements, as all arrays are (else ADSA_ERR_ALIGN)      uniform  float [n_rows] in [0, 1) (outside: the nearest that is)
  *   token    int32 [n_rows], guided [2 * n_rows]: the partner gets the same token      logprob  float [n_rows], or NULL
- *   seqs     NULL, or as many records as token has numbers: a row whose record is inactive (step < 0 or a status) gets token -1 and logprob 0
+ *   seqs     NULL, or as many records as token has numbers: a row whose record is inactive (step < 0 or a status) gets token -1 and logprob 0;
+ *            a pair goes by the record of its conditional row
  */
 int adsa_sample(const adsa_sampling* s, const adsa_seq* seqs, const void* logits, const float* uniform, int32_t* token, float* logprob, void* stream);
 

@@ -194,6 +194,7 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
     widen(x.own, z);
     one_by_one(row, i, z);
     if constexpr (GUIDED) {
+      const bool alone = A.guidance == 1.0f;         // the conditional row, whatever is in the other
       float f4[4];
       widen(x.partner, f4);
       one_by_one(partner, i, f4);
@@ -201,7 +202,9 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
       for (int e = 0; e < 4; ++e) {
 #pragma clang fp contract(off)
         const double c = z[e], f = f4[e], step = c - f, far = (double)A.guidance * step;
-        z[e] = (float)(f + far);
+        // (a token that the conditional row masks stays masked, which a negative guidance would turn into +infinity; one that only the other row masks is no
+        // number, which counts as masked, or -infinity)
+        z[e] = alone || z[e] == -INFINITY ? z[e] : (float)(f + far);
       }
     }
 #pragma unroll

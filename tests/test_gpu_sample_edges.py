@@ -1,0 +1,49 @@
+"""adsa_sample where its numbers end: masked logits of guided pairs, the largest vocabulary, the largest temperatures.  Bounds as in test_gpu_sample."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_sample import DEV, INF, NAN, draw, reference, some
+
+pytestmark = pytest.mark.gpu
+
+
+def check_rows(z, u, got, **settings):
+    """z: the logits as the definition has them, fp32 values on the host."""
+    token, logprob = got
+    for r in range(len(z)):
+        right, logs = reference(z[r], u[r].item(), float(np.float32(settings.get("temperature", 1.0))), settings.get("top_k", 0), settings.get("top_p", 1.0), settings.get("min_p", 0.0))
+        assert token[r] in right, (r, token[r], right)
+        assert any(logprob[r] == x or abs(logprob[r] - x) <= 2.0 ** -24 * abs(x) + len(z[r]) * 2.0 ** -44 + 2.0 ** -46 for x in logs[token[r]]), (r, logprob[r], logs[token[r]])
+
+
+# ---------------------------------------------------------------------------------------------------- guided pairs
+def mixed(c, f, g):
+    """The definition: a token that either row masks is masked; guidance 1 is the conditional row alone."""
+    if g == 1.0:
+        return c
+    with np.errstate(invalid="ignore", over="ignore"):
+        z = (f.astype(np.float64) + np.float64(np.float32(g)) * (c.astype(np.float64) - f.astype(np.float64))).astype(np.float32)
+    return np.where((c == -np.inf) | (f == -np.inf), np.float32(-np.inf), z)
+
+
+@pytest.mark.parametrize("V", [40, 5003, 70001])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("g", [-1.0, 0.0, 0.5, 1.0, 3.0])
+@pytest.mark.parametrize("settings", [dict(temperature=0.0), dict(top_k=9), dict(top_p=0.8), dict()])
+def test_tokens_that_a_row_of_a_pair_masks(V, dtype, g, settings):
+    n = 7
+    logits, _ = some(2 * n, V, dtype, V + 3)
+    u = torch.tensor([0.0, 0.2, 0.4, 0.6, 0.8, 0.95, 0.5], device=DEV)
+    c, f = logits[:n], logits[n:]
+    c[0, ::3] = -INF                                         # in the conditional row only
+    f[1, ::3] = -INF                                         # in the unconditional row only
+    c[2, ::2], f[2, ::2] = -INF, -INF                        # in both
+    c[3, :V // 2], f[3, V // 3:] = -INF, -INF                # in one or the other: with most guidances none is left
+    c[4, 5:], f[4, 7:] = -INF, -INF
+    f[5] = -INF                                              # the whole unconditional row
+    c[6, 3], c[6, 4], f[6, 8], f[6, 9] = INF, NAN, INF, NAN
+    z = mixed(c.float().cpu().numpy(), f.float().cpu().numpy(), g)
+    token, logprob = draw(logits, u, g, **settings)
+    assert np.array_equal(token[:n], token[n:])
+    check_rows(z, u, (token, logprob), **settings)
