@@ -473,7 +473,7 @@ typedef struct adsa_sampling { /* [host] */
   float   top_p;               /* 1 and more: not limited; 0 and less: the largest alone */
   float   min_p;               /* 0 and less: not limited; more than 1 counts as 1 */
   int32_t reserved;
-  const float* temperatures;   /* device [n_rows], or NULL: the number above for every row (negative or NaN counts as 0) */
+  const float* temperatures;   /* device [n_rows], or NULL: the number above for every row (negative or NaN counts as 0; +infinity: all that is above -infinity weighs alike) */
   const int32_t* top_ks;       /* the same for the others (a NaN: not limited) */
   const float* top_ps;
   const float* min_ps;

@@ -302,10 +302,13 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
   const double inv = 1.4426950408889634074 * kTable / (double)T;
   const Weigh weigh = {sh.table, inv, (double)top};
   // Bins of equal width below the largest, to the least or as far as a weight can be: what lies further is in the bins from BINS on, which nobody reads, and not live.
-  const float range = fminf(fminf(kReach * T, 1e38f), infinite ? 0.0f : top - least_z);
+  // By half the distances, which are numbers whatever the logits and the temperature (one rounding each, as of the whole ones).
+  const float half_top = 0.5f * top;
+  auto half_below = [&](float z) { return fmaf(-0.5f, z, half_top); };
+  const float range = fminf(0.5f * kReach * T, infinite ? 0.0f : half_below(least_z));
   const float per_bin = fminf((float)BINS * (1.0f - 0x1p-20f) / range, 1e38f);         // (no range: all that is live is in bin 0, which is narrow)
   const float furthest = (float)(BINS + lane);       // (lanes whose logits are not live do not meet in one bin: 16384 of which most are far below 5.9 -> 2.0 us)
-  auto bin_of = [&](float z) { return (int)fminf((top - z) * per_bin, furthest); };
+  auto bin_of = [&](float z) { return (int)fminf(half_below(z) * per_bin, furthest); };
   // The least logit for which `in` holds, which holds for all larger ones too, the largest among them: a wave tries 64 at a time.
   auto least_in = [&](auto in) {
     const uint32_t top_key = order_of(top);          // (0x7FFFFF is -infinity's, what is less that of no number)
@@ -438,7 +441,7 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs A) {
         w[k] = sh.weight[tid * PB + k];
         if (by_count) n[k] = sh.count[tid * PB + k];
         else {                                       // not counted: no more than have this weight if each has the least of the bin (and half a unit less, by its rounding)
-          const float each = exp2f(44.0f - (float)(tid * PB + k + 1) / per_bin * 1.0001f / T * 1.442695041f);
+          const float each = exp2f(44.0f - (float)(tid * PB + k + 1) / per_bin / T * (2.0f * 1.0001f * 1.442695041f));
           n[k] = (uint32_t)fminf((float)w[k] * 1.001f / fmaxf(each - 0.501f, 1.0f), (float)ADSA_MAX_VOCAB);
         }
         n_sum += n[k];

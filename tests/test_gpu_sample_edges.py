@@ -11,8 +11,9 @@ pytestmark = pytest.mark.gpu
 def check_rows(z, u, got, **settings):
     """z: the logits as the definition has them, fp32 values on the host."""
     token, logprob = got
+    T = min(float(np.float32(settings.get("temperature", 1.0))), 1e300)          # (an infinite one: weights of 1, and -infinity / 1e300 stays what it is)
     for r in range(len(z)):
-        right, logs = reference(z[r], u[r].item(), float(np.float32(settings.get("temperature", 1.0))), settings.get("top_k", 0), settings.get("top_p", 1.0), settings.get("min_p", 0.0))
+        right, logs = reference(z[r], u[r].item(), T, settings.get("top_k", 0), settings.get("top_p", 1.0), settings.get("min_p", 0.0))
         assert token[r] in right, (r, token[r], right)
         assert any(logprob[r] == x or abs(logprob[r] - x) <= 2.0 ** -24 * abs(x) + len(z[r]) * 2.0 ** -44 + 2.0 ** -46 for x in logs[token[r]]), (r, logprob[r], logs[token[r]])
 
@@ -47,3 +48,22 @@ def test_tokens_that_a_row_of_a_pair_masks(V, dtype, g, settings):
     token, logprob = draw(logits, u, g, **settings)
     assert np.array_equal(token[:n], token[n:])
     check_rows(z, u, (token, logprob), **settings)
+
+
+# ---------------------------------------------------------------------------------------------------- the largest numbers
+@pytest.mark.parametrize("V", [50, 3000, 20000, 70001])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T", [1e30, 2e36, 5e37, 1.5e38, 3.4e38, INF])
+@pytest.mark.parametrize("settings", [dict(), dict(top_k=40), dict(top_k=3000, top_p=0.7), dict(top_p=0.5), dict(min_p=0.3)])
+def test_logits_and_temperatures_as_large_as_there_are(V, dtype, T, settings):
+    """What is below the largest by less than 31 temperatures has a weight, also where the distance, or 31 temperatures, pass the largest number."""
+    gen = torch.Generator().manual_seed(V)
+    logits = ((torch.rand(6, V, generator=gen) * 2 - 1) * 3.38e38).to(dtype)
+    logits[1, ::2] = -INF
+    logits[2] *= 0.3
+    logits[3, 0], logits[3, 1:] = 3.38e38, -3.38e38
+    logits[4, :V // 2] = INF
+    assert torch.isfinite(logits[0]).all()
+    u = torch.tensor([0.1, 0.3, 0.5, 0.7, 0.9, 0.99], device=DEV)
+    got = draw(logits.to(DEV), u, temperature=torch.full((6,), T, device=DEV), **settings)
+    check_rows(logits.float().numpy(), u, got, **dict(settings, temperature=T))
