@@ -67,3 +67,42 @@ def test_logits_and_temperatures_as_large_as_there_are(V, dtype, T, settings):
     u = torch.tensor([0.1, 0.3, 0.5, 0.7, 0.9, 0.99], device=DEV)
     got = draw(logits.to(DEV), u, temperature=torch.full((6,), T, device=DEV), **settings)
     check_rows(logits.float().numpy(), u, got, **dict(settings, temperature=T))
+
+
+# ---------------------------------------------------------------------------------------------------- the largest vocabulary
+LAST = torch.tensor([0.0, 0.37, 0.99999994], device=DEV if torch.cuda.is_available() else "cpu")
+
+
+@pytest.mark.parametrize("V", [262144, 262143])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("settings", [dict(), dict(temperature=0.0), dict(top_k=1000), dict(top_k=1024, top_p=0.9), dict(top_k=5000), dict(top_k=200000, top_p=0.8, min_p=0.001), dict(top_p=0.9),
+                                      dict(top_p=0.01), dict(top_k=262142), dict(min_p=0.5)])
+def test_the_largest_vocabulary(V, dtype, settings):
+    """Few candidates and many, and the draw at its ends."""
+    logits, _ = some(3, V, dtype, V)
+    logits[:, -1] = logits.max()                             # the last index is a candidate, and the last of them
+    token, logprob = draw(logits, LAST, **settings)
+    check_rows(logits.float().cpu().numpy(), LAST, (token, logprob), **settings)
+    if settings.get("temperature", 1.0) > 0:
+        assert token[2] == V - 1
+
+
+@pytest.mark.parametrize("V", [262144, 262143])
+@pytest.mark.parametrize("levels", [1, 2, 7])
+@pytest.mark.parametrize("settings", [dict(top_k=262142), dict(top_k=37), dict(top_p=0.6), dict(top_k=100000, top_p=0.99), dict()])
+def test_ties_in_the_largest_vocabulary(V, levels, settings):
+    gen = torch.Generator().manual_seed(levels)
+    logits = torch.randint(0, levels, (3, V), generator=gen).float().to(DEV) * 0.5
+    check_rows(logits.cpu().numpy(), LAST, draw(logits, LAST, **settings), **settings)
+
+
+@pytest.mark.parametrize("V", [70001, 262143, 262144])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("settings", [dict(), dict(top_k=50), dict(top_k=6000, top_p=0.9), dict(top_p=0.9), dict(temperature=0.0)])
+def test_guided_pairs_of_large_vocabularies(V, dtype, settings):
+    """Rows of which most is read again in every pass, both of a pair."""
+    logits, _ = some(6, V, dtype, V + 1)
+    c, f = (x.float().cpu().numpy() for x in logits.chunk(2))
+    token, logprob = draw(logits, LAST, 2.5, **settings)
+    assert np.array_equal(token[:3], token[3:])
+    check_rows(mixed(c, f, 2.5), LAST, (token, logprob), **settings)
