@@ -54,7 +54,7 @@ struct Workspace {
   int lg_stride;           // sel_cap rounded up to a multiple of 4
 };
 
-AttendPlan make_attend_plan(const adsa_params& p);
+AttendPlan make_attend_plan(const adsa_params& p, bool paged = false);
 Workspace make_workspace(const adsa_params& p, const AttendPlan& plan);
 
 static inline int elem_bytes(const adsa_params& p) { return p.dtype == ADSA_F32 ? 4 : 2; }
@@ -91,7 +91,10 @@ hipError_t launch_attend(const adsa_params& p, const AttendPlan& plan, adsa_seq*
                          int advance, bool new_f32, hipStream_t st, hipEvent_t ev_start, hipEvent_t ev_stop);
 // grouped-query path (q_per_kv >= 2): matrix-core kernel, one workgroup per (sequence, cache head, chunk of the list)
 constexpr size_t kGqaMaxLds = 128 * 1024;     // dynamic LDS one workgroup may ask for
-static inline bool gqa_two_fit(size_t lds) { return 2 * (lds + 2048) <= 160 * 1024; }      // on a CU, static words included
+// Two workgroups on a CU, static words included: 512 bytes with 4 waves and 1024 with 8 (taken for 2048); over pages these, a sequence's row of the table and a
+// word a wave.
+constexpr size_t gqa_words(int waves, bool paged) { return paged ? 4 * (ADSA_MAX_CAP / ADSA_MIN_PAGE) + (size_t)waves * 132 : 2048; }
+static inline bool gqa_two_fit(size_t lds, int waves, bool paged) { return 2 * (lds + gqa_words(waves, paged)) <= 160 * 1024; }
 int gqa_logit_stride(const adsa_params& p, int n_chunks);
 int gqa_global_logit_stride(const adsa_params& p);
 size_t gqa_lds_bytes(const adsa_params& p, int waves, int n_chunks);

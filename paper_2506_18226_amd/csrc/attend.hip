@@ -1184,7 +1184,7 @@ static bool short_offsets(const adsa_params& p, int heads) {
 // K and V bytes of the longest list that 4 waves read as fast as 8: see make_attend_plan.
 static long long short_list(const adsa_params& p) { return (p.score_mode == ADSA_SCORE_VCOS_FUSED ? 32ll : 72ll) << 10; }
 
-AttendPlan make_attend_plan(const adsa_params& p) {
+AttendPlan make_attend_plan(const adsa_params& p, bool paged) {
   AttendPlan a;
   if (p.q_per_kv > 1) {      // grouped queries: one workgroup per (sequence, cache head, chunk of whole 16-token tiles)
     const long long wgs = (long long)p.n_seq * p.n_heads;
@@ -1192,7 +1192,8 @@ AttendPlan make_attend_plan(const adsa_params& p) {
     // tiles of two 8-wave workgroups do not fit a CU and those of two 4-wave ones do.  Measured, 4 | 8 waves: 256 pairs x 649 x 128,
     // G = 8 20.1 | 17.6 us; 512 31.6 | 30.9; 512 x 649 x 64 19.0 | 17.8; 384 x 300 x 128 15.3 | 15.9; 640 x 200 x 64 10.9 | 12.0;
     // 512 x 649 x 128 with G = 16 (two fit with 4) 33.8 | 37.3; 390 x 1230 x 128 in 2336 slots (one fits either way) 58.7 | 46.3.
-    const bool four = !gqa_two_fit(gqa_lds_bytes(p, 8, 1)) && gqa_two_fit(gqa_lds_bytes(p, 4, 1));
+    // (Over pages the words of the table count: 384 pairs x 1700 x 128, G = 8, whose 4-wave workgroups fit a CU twice only without them, with 4 | 8 waves 67.2 | 60.6.)
+    const bool four = !gqa_two_fit(gqa_lds_bytes(p, 8, 1), 8, paged) && gqa_two_fit(gqa_lds_bytes(p, 4, 1), 4, paged);
     a.waves = wgs >= 384 && (p.sel_cap < 448 || four) ? 4 : 8;
     // Lists are split only when they must be (the logits of a whole list, all G queries, do not fit in LDS even
     // with 4 waves) or when it was measured to pay: long lists (>= 2560 slots) of at most 32 (sequence, cache head)

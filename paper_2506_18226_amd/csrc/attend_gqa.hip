@@ -752,7 +752,7 @@ template <int D, int PAGED>
 hipError_t launch_gqa_paged_d(const GqaArgs& A, const PageArgs& pages, const AttendPlan& plan, int n_seq, size_t lds, hipStream_t st) {
   if (plan.n_chunks > 1) return launch_gqa_paged_w<D, 4, true, ring(D), PAGED>(A, pages, n_seq, plan.n_chunks, lds, st);
   if (plan.waves == 8) return launch_gqa_paged_w<D, 8, false, ring(D), PAGED>(A, pages, n_seq, 1, lds, st);
-  if (!gqa_two_fit(lds)) return launch_gqa_paged_w<D, 4, false, deep_ring(D), PAGED>(A, pages, n_seq, 1, lds, st);
+  if (!gqa_two_fit(lds, 4, true)) return launch_gqa_paged_w<D, 4, false, deep_ring(D), PAGED>(A, pages, n_seq, 1, lds, st);
   return launch_gqa_paged_w<D, 4, false, ring(D), PAGED>(A, pages, n_seq, 1, lds, st);
 }
 
@@ -761,7 +761,7 @@ hipError_t launch_gqa_d(const GqaArgs& A, const AttendPlan& plan, int n_seq, siz
                         hipEvent_t e1) {
   if (plan.n_chunks > 1) return launch_gqa_w<D, 4, true, ring(D)>(A, n_seq, plan.n_chunks, lds, st, e0, e1);     // split lists: 4 waves
   if (plan.waves == 8) return launch_gqa_w<D, 8, false, ring(D)>(A, n_seq, 1, lds, st, e0, e1);
-  if (!gqa_two_fit(lds)) return launch_gqa_w<D, 4, false, deep_ring(D)>(A, n_seq, 1, lds, st, e0, e1);
+  if (!gqa_two_fit(lds, 4, false)) return launch_gqa_w<D, 4, false, deep_ring(D)>(A, n_seq, 1, lds, st, e0, e1);
   return launch_gqa_w<D, 4, false, ring(D)>(A, n_seq, 1, lds, st, e0, e1);
 }
 

@@ -68,7 +68,7 @@ size_t adsa_paged_workspace_bytes(const adsa_params* p) {
   dense.kv_slot_stride = p->head_dim;
   dense.kv_head_stride = (int64_t)p->cap * p->head_dim;
   if (resolve_params(&dense, &eff) != ADSA_OK || is_vcos(eff)) return 0;
-  return make_workspace(eff, make_attend_plan(eff)).total;
+  return make_workspace(eff, make_attend_plan(eff, true)).total;
 }
 
 int adsa_attend_paged(const adsa_params* p, const adsa_pages* pages, adsa_seq* seqs, const void* q, const void* k_new, const void* v_new,
@@ -82,7 +82,7 @@ int adsa_attend_paged(const adsa_params* p, const adsa_pages* pages, adsa_seq* s
   const bool append = (flags & ADSA_FLAG_APPEND) != 0;
   if (append && (!k_new || !v_new)) return ADSA_ERR_NULL;
   if (!aligned16(q) || !aligned16(out) || (append && (!aligned16(k_new) || !aligned16(v_new)))) return ADSA_ERR_ALIGN;
-  const AttendPlan plan = make_attend_plan(eff);
+  const AttendPlan plan = make_attend_plan(eff, true);
   const Workspace w = make_workspace(eff, plan);
   if ((rc = check_space(workspace, workspace_bytes, w.total)) || (rc = ensure_device_ready())) return rc;
   const bool accumulate = eff.score_mode == ADSA_SCORE_ATTN_MASS && !(flags & ADSA_FLAG_NO_ACCUMULATE);
@@ -100,7 +100,7 @@ int adsa_compact_paged(const adsa_params* p, const adsa_pages* pages, adsa_seq* 
   int rc = resolve_paged(p, pages, &eff, &args);
   if (rc) return rc;
   if (!seqs || !keep_map) return ADSA_ERR_NULL;
-  const AttendPlan plan = make_attend_plan(eff);
+  const AttendPlan plan = make_attend_plan(eff, true);
   const Workspace w = make_workspace(eff, plan);
   if ((rc = check_space(workspace, workspace_bytes, w.total)) || (rc = ensure_device_ready())) return rc;
   if (launch_compact_paged(eff, args, seqs, keep_map, (char*)workspace, w, (flags & ADSA_FLAG_ADVANCE) != 0, reinterpret_cast<hipStream_t>(stream)) != hipSuccess)
