@@ -315,9 +315,7 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
   pin_uniform(score); pin_uniform(pending);
   if constexpr (VF) pin_uniform(u_state);
 
-  // (PAGED: a sequence with a status is skipped whatever its list.  One whose pages are no pages gets its status from this launch, so workgroups that start later
-  // may take this way to the same zeros; k_attend_finish goes by the status alone.)
-  cnt = PAGED && status_in != 0 ? 0 : min(cnt, sel_cap);
+  cnt = min(cnt, sel_cap);
   // ---- RANK: k_select's part, of which this thread keeps the places of its slots and their old scores of this head
   uint32_t dest[kSlots], take = 0;
   float old_score[kSlots];
@@ -426,14 +424,16 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
   if constexpr (PAGED) {
     const int need = n_res >= 1 && n_res <= cap ? ((n_res - 1) >> page_shift) + 1 : kMostEntries + 1;      // (a count that cannot be is no good either)
     const bool good = page_entries.put(s_units, (int)tail_word(offsetof(PagedTail, n_pages) / 4), tail_word(offsetof(PagedTail, page_units) / 4), need);
-    const bool wave_good = __ballot(!good) == 0 && need <= kMostEntries;
+    // A sequence with a status is skipped, whatever its list.  One whose entries are no pages gets its status from this launch, which the waves of a workgroup that
+    // starts later may or may not see yet: they decide together.
+    const bool wave_good = __ballot(!good) == 0 && need <= kMostEntries && status_in == 0;
     if (lane == 0) s_good[wave] = wave_good;
     __syncthreads();
     bool all = true;
 #pragma unroll
     for (int w = 0; w < NW; ++w) all &= s_good[w] != 0;
     last_slot = n_res - 1;
-    if (!all) {                                     // (every workgroup of the sequence finds the same)
+    if (!all) {                                     // (every workgroup of the sequence finds the same; k_attend_finish goes by the status)
       if (chunk == 0) {
         const size_t row = (size_t)b * n_heads + head0;
         for (int o = tid; o < D; o += kAttThreads) {
@@ -441,7 +441,7 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
           else ((ADSA_GLOBAL uint16_t*)tail_address(offsetof(AttendTail, out)))[row * D + o] = 0;
         }
         if (tid == 0) ((gfloat*)tail_address(offsetof(AttendTail, lse)))[row] = 0.0f;
-        if (head0 == 0 && tid == 0) sqp->status = sqp->status | ADSA_SEQ_BAD_STATE;
+        if (head0 == 0 && tid == 0 && status_in == 0) sqp->status = ADSA_SEQ_BAD_STATE;         // (which no other workgroup writes)
       }
       return;
     }

@@ -245,7 +245,7 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
   gchar* const v_base = (PAGED ? (gchar*)tail_address(offsetof(PagedGqaTail, v)) : v_rec) + hk * head_stride_b;
   gfloat* const score = score_rec + (size_t)hk * cap;
 
-  const int cnt = PAGED && status_in != 0 ? 0 : min(cnt_raw, sel_cap);          // (a sequence with a status is skipped: see k_attend)
+  const int cnt = min(cnt_raw, sel_cap);
   const GqaTail& block = [&]() -> const GqaTail& {
     if constexpr (PAGED) return T.a;
     else return T;
@@ -267,7 +267,7 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
   if constexpr (PAGED) {                             // (as in k_attend)
     const int need = n_res >= 1 && n_res <= cap ? ((n_res - 1) >> page_shift) + 1 : kMostEntries + 1;
     const bool good = page_entries.put(s_units, (int)tail_word(offsetof(PagedGqaTail, n_pages) / 4), tail_word(offsetof(PagedGqaTail, page_units) / 4), need);
-    const bool wave_good = __ballot(!good) == 0 && need <= kMostEntries;
+    const bool wave_good = __ballot(!good) == 0 && need <= kMostEntries && status_in == 0;
     if (lane == 0) s_good[wave] = wave_good;
     __syncthreads();
     bool all = true;
@@ -279,7 +279,7 @@ __global__ __launch_bounds__(NW * kWave, R > ring(D) ? 1 : 4) void k_attend_gqa(
         const size_t row = (size_t)b * HQ + (size_t)hk * G;
         for (int o = tid; o < G * D; o += kThreads) ((ADSA_GLOBAL uint16_t*)tail_address(offsetof(GqaTail, out)))[row * D + o] = 0;
         if (tid < G) ((gfloat*)tail_address(offsetof(GqaTail, lse)))[row + tid] = 0.0f;
-        if (hk == 0 && tid == 0) sqp->status = sqp->status | ADSA_SEQ_BAD_STATE;
+        if (hk == 0 && tid == 0 && status_in == 0) sqp->status = ADSA_SEQ_BAD_STATE;
       }
       return;
     }

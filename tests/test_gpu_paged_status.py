@@ -3,10 +3,11 @@ import pytest
 import torch
 
 from paper_2506_18226_amd import binding as B
+from paper_2506_18226_amd.batch import PagedBatch
 
 from common import plan_of
 from paged_common import paged_twin, same_bits
-from test_gpu_paged import Decode
+from test_gpu_paged import DEV, Decode
 
 pytestmark = pytest.mark.gpu
 
@@ -43,3 +44,30 @@ def test_single_tokens_of_a_sequence_with_a_status(G, lists, resident, split, st
     torch.cuda.synchronize()
     assert same_bits(paged.out, good.out) and same_bits(paged.lse, good.lse)
     assert list(paged.read_seqs()["step"]) == [6, 5, 6]
+
+
+@pytest.mark.parametrize("G,D", [(0, 64), (0, 128), (8, 64), (8, 128)])
+@pytest.mark.parametrize("length,entry", [(40, 250), (300, 131), (300, 0), (300, 255)])
+def test_workgroups_that_start_after_a_sequence_got_its_status(G, D, length, entry):
+    """More workgroups than the card holds at once, of which the first find that an entry is no page: the later ones, some of whose waves see the status, skip their sequences all the same."""
+    n, h, resident = 24, 32 if G else 96, 4090              # 256 pages a sequence: every thread has some, and the bad one is some thread's alone
+    p = B.make_params(n_seq=n, n_heads=h, head_dim=D, grid_h=90, grid_w=90, win_rows_back=1, win_col_radius=2, dtype=B.BF16, score_mode=B.SCORE_ATTN_MASS, cap=4096, sel_cap=length, q_per_kv=G)
+    paged = PagedBatch(p, n_pages=64, page_size=16, device=DEV)
+    assert plan_of(p).chunks == 1
+    paged.table.copy_(torch.randint(0, 64, tuple(paged.table.shape), generator=torch.Generator().manual_seed(3)).to(torch.int32))          # (any pages of the pool will do)
+    paged.table[::2, entry] = 64
+    paged.K.fill_(0.5)
+    paged.V.fill_(0.5)
+    paged.sel_idx.copy_(torch.arange(length, dtype=torch.int32) * 13)
+    paged.sel_cnt.fill_(length)
+    paged.seqs_host["n_res"], paged.seqs_host["step"] = resident, 4
+    paged.upload_seqs()
+    q = torch.ones(n, h * max(G, 1), D, dtype=torch.bfloat16, device=DEV)
+    paged.out.fill_(3.0)
+    paged.lse.fill_(3.0)
+    score = paged.score.clone()
+    paged.attend(q, 0)
+    torch.cuda.synchronize()
+    assert list(paged.read_seqs()["status"]) == [B.SEQ_BAD_STATE, 0] * (n // 2)
+    assert not paged.out[::2].any() and not paged.lse[::2].any() and same_bits(paged.score[::2], score[::2])
+    assert (paged.out[1::2] == 0.5).all() and torch.isfinite(paged.lse[1::2]).all()
