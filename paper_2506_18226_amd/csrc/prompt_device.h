@@ -1076,6 +1076,7 @@ template <bool PAGED> using PromptArgsOf = std::conditional_t<PAGED, PagedPrompt
 // A sequence's new tokens: where they stand in the packed rows and in the cache.
 struct Prompt {
   int from, len, slot0, prefix, status;      // status: 0, or why the record does not fit (one without new tokens does)
+  bool fits;                                 // has the new tokens' slots, whatever its status
 };
 __device__ __forceinline__ Prompt prompt_of(const PromptArgs& A, int b) {
   const ADSA_GLOBAL adsa_seq& sq = ((const ADSA_GLOBAL adsa_seq*)A.seqs)[b];
@@ -1087,7 +1088,8 @@ __device__ __forceinline__ Prompt prompt_of(const PromptArgs& A, int b) {
   const int n_res = sq.n_res;
   pr.prefix = A.mask == ADSA_MASK_PREFIX ? sq.n_keep_prefix : 0;
   if (pr.from < 0 || pr.len < 0 || pr.len > A.n_tokens || pr.from > A.n_tokens - pr.len) pr.len = 0;        // (begin[] is not what it should be)
-  if (pr.status == 0 && pr.len > 0 && (n_res < 0 || n_res > A.cap || pr.slot0 < 0 || pr.len > A.max_len || pr.slot0 > n_res - pr.len)) pr.status = ADSA_SEQ_BAD_STATE;
+  pr.fits = pr.len > 0 && n_res >= 0 && n_res <= A.cap && pr.slot0 >= 0 && pr.len <= A.max_len && pr.slot0 <= n_res - pr.len;
+  if (pr.status == 0 && pr.len > 0 && !pr.fits) pr.status = ADSA_SEQ_BAD_STATE;
   return pr;
 }
 // keys below this are seen by the token in slot s
@@ -1121,13 +1123,15 @@ __device__ __forceinline__ bool job_of(const Args& A, Job& J) {
   const int tile = A.tiles - 1 - unit / A.chunks, tid = threadIdx.x, hq = A.h * A.G;       // (the longest rows first)
   ADSA_GLOBAL adsa_seq& sq = ((ADSA_GLOBAL adsa_seq*)A.seqs)[J.b];
   J.pr = prompt_of(A, J.b);
-  if constexpr (PAGED) {                             // every page of the slots is one of the pool (all workgroups of the sequence look at all of them)
-    if (J.pr.status == 0 && J.pr.len > 0) {
+  if constexpr (PAGED) {
+    // Every page of the slots is one of the pool: all workgroups of the sequence look at all of them, and all waves, whatever status they see: it may be written
+    // meanwhile, by another workgroup, for these pages, and a wave that went by it would leave its entries to nobody.
+    if (J.pr.fits) {                                 // (the same for all: no launch that reads n_res writes it)
       const gint* const table = (const gint*)A.pages.table + (size_t)J.b * A.pages.table_stride;
       const int need = ((J.pr.slot0 + J.pr.len - 1) >> A.pages.shift) + 1;
       bool bad = false;
       for (int i = tid; i < need; i += THREADS) bad |= (uint32_t)table[i] >= (uint32_t)A.pages.n_pages;
-      if (__syncthreads_or(bad)) J.pr.status = ADSA_SEQ_BAD_STATE;
+      if (__syncthreads_or(bad) && J.pr.status == 0) J.pr.status = ADSA_SEQ_BAD_STATE;
     }
   }
   if (J.pr.status != 0) {                            // zeros, by the workgroups of the sequence together

@@ -71,3 +71,33 @@ def test_workgroups_that_start_after_a_sequence_got_its_status(G, D, length, ent
     assert list(paged.read_seqs()["status"]) == [B.SEQ_BAD_STATE, 0] * (n // 2)
     assert not paged.out[::2].any() and not paged.lse[::2].any() and same_bits(paged.score[::2], score[::2])
     assert (paged.out[1::2] == 0.5).all() and torch.isfinite(paged.lse[1::2]).all()
+
+
+@pytest.mark.parametrize("dtype,D,G", [(B.BF16, 64, 0), (B.BF16, 128, 4), (B.F32, 64, 0), (B.F32, 128, 0)])
+@pytest.mark.parametrize("tokens,h", [(2, 32), (200, 32)])
+@pytest.mark.parametrize("entry", [0, 63, 250])
+def test_prompts_whose_workgroups_start_after_a_sequence_got_its_status(dtype, D, G, tokens, h, entry):
+    """As above, for chunks of new tokens behind some 4000 slots, few rows and many."""
+    n, resident = 12, 4090
+    p = B.make_params(n_seq=n, n_heads=h, head_dim=D, grid_h=90, grid_w=90, win_rows_back=1, win_col_radius=2, dtype=dtype, score_mode=B.SCORE_ATTN_MASS, cap=4096, q_per_kv=G)
+    paged = PagedBatch(p, n_pages=64, page_size=16, device=DEV)
+    paged.table.copy_(torch.randint(0, 64, tuple(paged.table.shape), generator=torch.Generator().manual_seed(3)).to(torch.int32))
+    paged.table[::2, entry] = -1
+    paged.K.fill_(0.5)
+    paged.V.fill_(0.5)
+    paged.seqs_host["n_res"], paged.seqs_host["step"] = resident, 4
+    paged.upload_seqs()
+    hq, T = h * max(G, 1), n * tokens
+    begin = torch.arange(n + 1, dtype=torch.int32, device=DEV) * tokens
+    new = B.make_tokens(begin, torch.full((n,), resident - tokens, dtype=torch.int32, device=DEV), T, tokens)
+    q = torch.ones(T, hq, D, dtype=paged.tdtype, device=DEV)
+    out, lse = torch.full((T, hq, D), 3.0, dtype=paged.tdtype, device=DEV), torch.full((T, hq), 3.0, device=DEV)
+    paged.prefill(new, q, out, lse)
+    torch.cuda.synchronize()
+    assert list(paged.read_seqs()["status"]) == [B.SEQ_BAD_STATE, 0] * (n // 2)
+    out, lse = out.view(n, tokens, hq, D), lse.view(n, tokens, hq)
+    assert not out[::2].any() and not lse[::2].any() and not paged.score[::2].any()
+    # a mean of halves, whose probabilities and sum are off by 2^-8 at most, and a rounding
+    assert ((out[1::2].float() - 0.5).abs() <= 0.5 * 2.0 ** -7).all() and torch.isfinite(lse[1::2]).all()
+    mass = paged.score[1::2].double().sum(-1)                # every row gives 1 in all: tokens * G a cache head, each share off by some 2^-16
+    assert ((mass - tokens * max(G, 1)).abs() <= tokens * max(G, 1) * 2.0 ** -7).all()
