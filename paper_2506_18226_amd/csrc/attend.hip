@@ -395,9 +395,9 @@ __global__ __launch_bounds__(NW * kWave) void k_attend(uint32_t seqs_lo, uint32_
     pending = reject == 0 && active ? slot_new : -1;
     gint* const plan = (gint*)tail_address(offsetof(RankTail, plan)) + 4 * b;
     if (head0 == 0 && tid == 0) {
-      *reinterpret_cast<ADSA_GLOBAL u32x4*>(plan) = u32x4{0u, (uint32_t)(active && reject == 0 ? step : -1), (uint32_t)n, (uint32_t)cnt};
+      // (A status is the next kernel's to write: this launch's waves read it, and those of a workgroup that starts later have to see the same.)
+      *reinterpret_cast<ADSA_GLOBAL u32x4*>(plan) = u32x4{0u, (uint32_t)(active && reject == 0 ? step : -1), (uint32_t)n, reject != 0 ? reject : (uint32_t)cnt};
       ((gint*)address(cnt_lo, cnt_q_hi & 0xFFFF))[b] = cnt;
-      if (reject != 0) sqp->status = status_in | (int)reject;
       if (!active || reject != 0) sqp->pending_slot = -1;
     }
   }
