@@ -282,7 +282,7 @@ class PagedBatch(LayerBatch):
     "slot_major", [n_pages][page_size][h][D]; table int32 [n_seq][ceil(cap / page_size)] on the device, -1 where a sequence has no page.
     Which page is whose is kept on the host: reserve() gives a sequence pages, release() takes them back; the device's table is brought up to
     date by upload_table(), on the current stream.  (A caller with an allocator of its own may fill `table` and leave those alone.)
-    The calls are those of LayerBatch; several batches (the layers of a model) may share one table where all of them keep as many tokens."""
+    The calls are those of LayerBatch; several batches (the layers of a model) may go by one table where all of them keep as many tokens (use_table)."""
 
     dense = False
 
@@ -356,6 +356,14 @@ class PagedBatch(LayerBatch):
         given_up = self.table_host[b, :n].copy()
         self.table_host[b, :n] = given
         self._give_back(given_up)
+
+    def use_table(self, other: "PagedBatch") -> None:
+        """This batch goes by other's table and free pages from now on, with pools of its own: pages that one of them reserves, shares, releases and uploads are
+        both's.  (Graphs captured before hold the old table's address.)"""
+        if other.page_size != self.page_size or other.n_pages != self.n_pages or other.table.shape != self.table.shape or other.table.device != self.table.device:
+            raise ValueError("use_table: a batch of as many pages, of the same size, and of as many sequences and slots expected")
+        self.table, self.table_host, self.free_pages = other.table, other.table_host, other.free_pages
+        self.pages = B.make_pages(self.K, self.V, self.table, page_size=self.page_size, layout="head_major" if self.head_major else "slot_major")
 
     def upload_table(self) -> None:
         self.table.copy_(torch.from_numpy(self.table_host))

@@ -138,3 +138,22 @@ def test_batches_that_take_their_pages_from_one_list():
     a.release(0, 20)
     b.reserve(1, 32)
     assert not a.free_pages and sorted(in_use(a) | in_use(b)) == list(range(8))
+
+
+def test_layers_that_go_by_one_table():
+    first, second = host_batch(n_pages=8), host_batch(n_pages=8)
+    second.reserve(0, 16)
+    second.use_table(first)
+    assert second.pages.table == first.table.data_ptr() and second.pages.k == second.K.data_ptr() != first.K.data_ptr()
+    first.reserve(1, 40)
+    second.share(2, 1, 32)
+    second.upload_table()
+    for value, batch in ((2.0, first), (5.0, second)):
+        batch.set_sequence(1, k=rows(40, value), v=rows(40, value), pos=np.arange(40), score=None, step=1, grid_origin=40)
+    assert (first.cache_rows(first.K, 2, 32) == 2.0).all() and (second.cache_rows(second.K, 2, 32) == 5.0).all()
+    first.release(1)
+    second.release(2)
+    assert len(first.free_pages) == 8 and second.free_pages is first.free_pages
+    for other in (host_batch(n_pages=9), host_batch(page=32), host_batch(n_seq=3), host_batch(cap=65)):
+        with pytest.raises(ValueError):
+            second.use_table(other)
