@@ -84,6 +84,7 @@ class LayerBatch:
         self.prompt_workspace = None            # that of the last prompt call
         self._prompt_workspaces = {}            # (entry point, stream) -> its workspace
         self._outgrown = []
+        self.upload_seqs()                      # inactive until the caller's own are there (records of zeros would be active, without positions)
 
     dense = True                                # every sequence has a cache of its own, cap slots long
 
@@ -289,7 +290,6 @@ class PagedBatch(LayerBatch):
     def __init__(self, params: B.AdsaParams, n_pages: int, page_size: int = 64, device: str = "cuda:0"):
         self.page_size, self.n_pages = page_size, n_pages
         super().__init__(params, device)
-        self.upload_seqs()                                                     # inactive until the caller's own are there
 
     def _allocate_caches(self) -> None:
         p = self.params
