@@ -121,7 +121,7 @@ typedef enum {
                                        the call is done; give it to the LAST call of a decode step only
                                        (adsa_compact tests the row end on the step before the increment) */
 
-#define ADSA_FLAG_SPLIT_P      64u  /* adsa_prefill with a bf16 cache: probabilities meet V with 16 bits in calls of any size, as
+#define ADSA_FLAG_SPLIT_P      64u  /* adsa_prefill and adsa_prefill_paged with a bf16 cache: probabilities meet V with 16 bits in calls of any size, as
                                        those of the other calls do, for half as many products again.  Without it
                                        they may be rounded to bf16, by 2^-8 of themselves at most (calls of more
                                        than 32 rows a cache head).  No effect with an fp32 cache */
@@ -416,7 +416,8 @@ size_t adsa_shared_workspace_bytes(const adsa_params* p, const adsa_shared* shar
  * ADSA_SCORE_VCOS and ADSA_SCORE_VCOS_FUSED, which rank by V, and sel_groups != 1 are ADSA_ERR_UNSUPPORTED in the calls below.
  * Table entries of slots a sequence does not have are not read as pages; a sequence with resident slots on an entry that is no page of
  * the pool gets ADSA_SEQ_BAD_STATE and zeros (adsa_append_paged: ADSA_SEQ_CACHE_FULL where it is the new tokens' slots), and its pages stay
- * as they are.  A page may be in several sequences' tables as long as no call writes to it: pinned prefixes do not move.
+ * as they are.  A page may be in several sequences' tables as long as no call writes to it: pinned prefixes do not move.  A step whose new token's slot,
+ * which adsa_select has reserved, has no page is such a case: ADSA_SEQ_BAD_STATE, and n_res counts the slot already.
  */
 typedef struct adsa_pages {    /* [host] */
   void* k;                     /* device: page 0 of the pool of K (dtype elements); 16-byte aligned, as is v */

@@ -1275,7 +1275,7 @@ template <int D, int W, int MODS, bool SPLIT, bool PAGED = false> using PromptFl
 // some reloaded in the loops; plain and capped forms spill 4 outside theirs.  Three waves a SIMD at head size 64, but for distances and documents (16 x 300..600 x 24 x 64 with
 // three | two 92 | 59 us: spills).
 // Over pages the page numbers are beside these registers: at head size 64 plain and capped forms spill 40 and 65 words at three waves a SIMD (4 x 1000 behind 1000 x 24 x 64
-// 80 us, dense 73), at 128 plain and capped ones none, with probabilities of two numbers 60 and 64, with distances and documents 25 to 133.
+// 79 us, dense 66), at 128 plain and capped ones none, with probabilities of two numbers 60 and 64, with distances and documents 25 to 133.
 template <int D, int MODS, bool SPLIT> constexpr int kFlowWaves = D == 64 && MODS < kAny && !SPLIT ? 3 : 2;
 template <int D, int W, int MODS, bool SPLIT, bool PAGED>
 __device__ __forceinline__ void prompt_flow(PromptArgsOf<PAGED> A) {

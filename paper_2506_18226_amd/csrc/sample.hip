@@ -1,7 +1,7 @@
 // The next token of every row of logits (adsa_sample): temperature, top-k, top-p and min-p, from a random number that the caller brings.
 //
-//  k_sample<EB, NT, BINS, RAGGED, GUIDED>: a workgroup takes a row.  It reads it once and keeps it in LDS as far as that goes (24576 logits); what is beyond is
-//  read again in every pass.
+//  k_sample<EB, NT, BINS, RAGGED, GUIDED>: a workgroup takes a row.  It reads it once and keeps it in LDS as far as that goes (24576 logits, 4096 of rows longer than
+//  65536, whose bins take the room); what is beyond is read again in every pass.
 //  What is kept of a row by top-k and top-p is the front of its descending order, so it is known by its last one: (z, index), and a logit is in if its z is
 //  larger, or the same and its index no larger.  That last one is found without sorting: logits are counted, or their weights summed, by
 //  BINS steps of z below the largest; running sums over the bins say in which bin a limit falls, and that bin's logits, some dozens, are listed and
@@ -13,7 +13,7 @@
 //  vocabulary would get its neighbour.
 //  What bounds it: memory for the first pass (256 rows of 65536 fp32: 12.5 us, 5.4 TB/s), from then on operations in 64 bits, of which a weight has 10: 16 us for
 //  the bins of a row with top-p alone, 24 for its candidates, 57 in all; with top-k 1000 before it 8 and 18, 39 in all.  One row has a chain of some 20 barriers:
-//  16 us for a guided one of 16384 with top-k 2000 and top-p, of which the pair's reading takes 3.3.
+//  20 us for a guided one of 16384 with top-k 2000 and top-p, of which the pair's reading takes 3.3.  With 8192 bins 23 to 54 words of a thread's bins are spilled.
 #include <type_traits>
 
 #include "adsa_device.h"
