@@ -302,15 +302,18 @@ class PagedBatch(LayerBatch):
         self.pages = B.make_pages(self.K, self.V, self.table, page_size=self.page_size, layout="head_major" if self.head_major else "slot_major")
 
     # ---- pages, on the host
+    def _pool_pages(self) -> int:
+        return getattr(self, "pages", self).n_pages            # (a pool may be larger than this batch's part of it)
+
     def _named(self, page) -> np.ndarray:
         """Whether a row of the table names each of these pages."""
         return np.isin(page, self.table_host)
 
     def _give_back(self, pages: np.ndarray) -> None:
         """Pages that a row has just lost, the last first: free are those that no row names any more."""
-        free, n_pages = set(self.free_pages), getattr(self, "pages", self).n_pages         # (a pool may be larger than this batch's part of it)
+        free = set(self.free_pages)
         for page, named in zip(pages[::-1].tolist(), self._named(pages[::-1])):
-            if not named and page not in free and 0 <= page < n_pages:
+            if not named and page not in free and 0 <= page < self._pool_pages():
                 free.add(page)
                 self.free_pages.append(page)
 
@@ -320,7 +323,7 @@ class PagedBatch(LayerBatch):
         need = -(-slots // self.page_size)
         if not 0 <= slots <= self.params.cap:
             raise ValueError(f"slots: 0..{self.params.cap} expected, {slots} given")
-        missing = [i for i in range(need) if row[i] < 0]
+        missing = [i for i in range(need) if not 0 <= row[i] < self._pool_pages()]
         taken, at = [], len(self.free_pages)
         while len(taken) < len(missing) and at > 0:          # from the end, without what a row that was written by hand names
             some = self.free_pages[max(0, at - len(missing) + len(taken)):at][::-1]
@@ -349,7 +352,7 @@ class PagedBatch(LayerBatch):
             raise ValueError(f"slots: 0..{self.params.cap} expected, {slots} given")
         n = slots // self.page_size
         given = self.table_host[of, :n].copy()
-        if (given < 0).any():
+        if ((given < 0) | (given >= self._pool_pages())).any():
             raise ValueError(f"sequence {of}: no pages for {slots} slots")
         if b == of:
             return

@@ -121,6 +121,10 @@ def test_rows_written_by_hand():
     batch.reserve(3, 64)
     assert hand not in batch.table_host[3] and hand not in batch.free_pages
     all_there(type("without", (), dict(table_host=np.where(batch.table_host == 0x7FFFFFFF, -1, batch.table_host), free_pages=batch.free_pages, n_pages=9)))
+    with pytest.raises(ValueError):
+        batch.share(0, 2, 32)                                # one of them is no page
+    batch.reserve(2, 32)                                     # gets one in its place
+    assert 0 <= batch.table_host[2, 1] < 9 and batch.table_host[2, 0] == hand
     for b in range(4):
         batch.release(b)
     assert sorted(batch.free_pages) == list(range(9)) and (batch.table_host == -1).all()
